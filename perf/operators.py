@@ -1,9 +1,10 @@
 """The operators of a fine-tuning step under the HPD mask, as cases to be measured.
 
-Four operators: attention over packed training sequences under the fine-tuning mask (paper
-Section 4.4), its gradient, the log probabilities of given tokens with entropy and top
-alternatives, and the gradient of those.  ``run`` computes them in elementary torch operations
-where ``own`` is false and through the library where it is true.
+Five operators: the rotation of queries and keys at the position IDs of packed training sequences
+(and its inverse, for gradients), attention over them under the fine-tuning mask (paper Section
+4.4), its gradient, the log probabilities of given tokens with entropy and top alternatives, and
+the gradient of those.  ``run`` computes them in elementary torch operations where ``own`` is
+false and through the library where it is true.
 
 Sizes: heads, header / document / value lengths and attribute counts are those of the benchmark
 configurations (``workloads.config``) and of the tests' ragged batches; vocabularies are generic.
@@ -19,23 +20,28 @@ own = False
 # the largest cases that are drawn: forward operations of an attention (a gradient has 2.5 times as many), bytes of logits
 F32_FLOPS, BF16_FLOPS = 4e11, 2.1e12
 LOGIT_BYTES = 1.58e9
+SEQUENCE_OPS = ("rotate", "attn", "attn_grad")
 
 
 def listed():
     return [
+        # queries and keys of a training batch, views of one projection's output
+        dict(name="rotate_batch", op="rotate", inverse=False, dtype="bf16", hq=32, hkv=8, d=128, base=500000.0,
+             k_max=16, n_seq=32, prompt_lo=300, prompt_hi=576, n_attr=16, fused=True, lens=2),
+        # gradients of the small fp32 layer, turned back
+        dict(name="rotate_back_f32", op="rotate", inverse=True, dtype="f32", hq=4, hkv=4, d=64, base=10000.0,
+             k_max=8, n_seq=16, prompt_lo=16, prompt_hi=700, n_attr=8, fused=False, lens=4),
         # one short sequence, the smallest call: a header, four attributes
         dict(name="attn_one_short", op="attn", dtype="bf16", hq=32, hkv=8, d=128, base=500000.0, k_max=8,
              n_seq=1, prompt_lo=40, prompt_hi=40, n_attr=4, fused=False, lens=1),
-        # a training batch of single documents with 16 attributes each; q, k, v in one projection's output
-        dict(name="attn_batch", op="attn", dtype="bf16", hq=32, hkv=8, d=128, base=500000.0, k_max=16,
-             n_seq=32, prompt_lo=300, prompt_hi=576, n_attr=16, fused=True, lens=2),
         # two long stacked documents, 96 attributes, 64 query heads
         dict(name="attn_long", op="attn", dtype="bf16", hq=64, hkv=8, d=128, base=500000.0, k_max=32,
              n_seq=4, prompt_lo=4000, prompt_hi=4224, n_attr=96, fused=False, lens=3),
         # the small fp32 layer, ragged
         dict(name="attn_f32", op="attn", dtype="f32", hq=4, hkv=4, d=64, base=10000.0, k_max=8,
              n_seq=16, prompt_lo=16, prompt_hi=700, n_attr=8, fused=False, lens=4),
-        # gradients of the training batch
+        # gradients of a training batch of single documents with 16 attributes each; v and dv in the
+        # projection's output and its gradient
         dict(name="attn_grad_batch", op="attn_grad", dtype="bf16", hq=32, hkv=8, d=128, base=500000.0, k_max=16,
              n_seq=32, prompt_lo=300, prompt_hi=576, n_attr=16, fused=True, lens=2),
         # ... of the long sequences
@@ -44,8 +50,6 @@ def listed():
         # ... of the small fp32 layer
         dict(name="attn_grad_f32", op="attn_grad", dtype="f32", hq=4, hkv=4, d=64, base=10000.0, k_max=8,
              n_seq=16, prompt_lo=16, prompt_hi=700, n_attr=8, fused=False, lens=4),
-        # one decode step of 96 branches: the sampled tokens' log probabilities and 8 alternatives
-        dict(name="logprobs_decode", op="logprobs", dtype="bf16", rows=96, vocab=32001, stride=32008, top=8),
         # the value tokens of a training batch over a large padded vocabulary
         dict(name="logprobs_batch", op="logprobs", dtype="bf16", rows=6144, vocab=130013, stride=130048, top=1),
         # few fp32 rows, many alternatives: the teacher's side of a distillation, token by token
@@ -64,9 +68,9 @@ def _log_int(rng, lo, hi):
 
 
 def draw(rng):
-    op = rng.choice(["attn", "attn_grad", "logprobs", "logprobs_grad"])
+    op = rng.choice(["rotate", "attn", "attn", "attn_grad", "attn_grad", "logprobs", "logprobs_grad"])
     dtype = rng.choice(["bf16", "bf16", "bf16", "f32"])
-    if op in ("attn", "attn_grad"):
+    if op in SEQUENCE_OPS:
         hq, hkv, d = rng.choice([(4, 4, 64), (8, 2, 64), (32, 8, 128), (64, 8, 128), (40, 8, 128), (16, 16, 128),
                                  (12, 2, 96), (6, 1, 80)])
         cap = (BF16_FLOPS if dtype == "bf16" else F32_FLOPS) / (1.0 if op == "attn" else 2.0)
@@ -76,6 +80,8 @@ def draw(rng):
                         k_max=rng.choice([7, 8, 12, 16, 32]), n_seq=_log_int(rng, 1, 64),
                         prompt_lo=rng.randint(0, hi), prompt_hi=hi, n_attr=_log_int(rng, 1, 96),
                         fused=rng.random() < 0.5, lens=rng.randint(10, 10 ** 6))
+            if op == "rotate":
+                case["inverse"] = rng.random() < 0.5
             prompt, attr_ptr, attr_len, value_len = _lengths(case)
             n = sum(prompt) + sum(attr_len) + sum(value_len)
             if 4.0 * d * hq * _pairs(case) <= cap and n * hq * d <= 2 ** 28:
@@ -153,7 +159,7 @@ def _heads(buf, case):
 
 
 def _qkv_buffers(case, n, make):
-    """q, k, v of n tokens: three tensors, or views of one."""
+    """What belongs to q, k and v of n tokens: three tensors, or views of one."""
     hq, hkv, d = case["hq"], case["hkv"], case["d"]
     if case["fused"]:
         return _heads(make((n, hq + 2 * hkv, d)), case)
@@ -169,10 +175,13 @@ def _make_inputs(case, seed):
         return torch.randn(shape, generator=gen, device="cuda", dtype=torch.float32).to(dt)
 
     st = dict(case=case)
-    if case["op"] in ("attn", "attn_grad"):
+    if case["op"] in SEQUENCE_OPS:
         seqs = _sequences(case)
         n = sum(p.size for p, _ in seqs)
-        st["q"], st["k"], st["v"] = _qkv_buffers(case, n, normal)
+        q, k, st["v"] = _qkv_buffers(case, n, normal)
+        if case["op"] != "rotate":  # the rotation has written its results next to each other
+            q, k = q.contiguous(), k.contiguous()
+        st["q"], st["k"] = q, k
         st["seqs"] = [(torch.from_numpy(p).cuda(), torch.from_numpy(r).cuda()) for p, r in seqs]
         if case["op"] == "attn_grad":
             st["d_out"] = normal((n, case["hq"], case["d"]))
@@ -211,10 +220,12 @@ def prepare(case, seed):
 
 def work(case):
     eb = 4 if case["dtype"] == "f32" else 2
-    if case["op"] in ("attn", "attn_grad"):
+    if case["op"] in SEQUENCE_OPS:
         hq, hkv, d = case["hq"], case["hkv"], case["d"]
         prompt, _, attr_len, value_len = _lengths(case)
         n = sum(prompt) + sum(attr_len) + sum(value_len)
+        if case["op"] == "rotate":
+            return dict(bytes=n * 2 * (hq + hkv) * d * eb, flops=3.0 * n * (hq + hkv) * d)
         pairs = _pairs(case)
         if case["op"] == "attn":
             return dict(bytes=n * ((2 * hq + 2 * hkv) * d * eb + 4 * hq), flops=4.0 * pairs * hq * d)
@@ -232,6 +243,8 @@ def run(st):
     op = st["case"]["op"]
     if own:
         return _OWN[op](st)
+    if op == "rotate":
+        return _plain_rotate(st)
     if op == "attn":
         return _plain_attention(st)
     if op == "attn_grad":
@@ -248,11 +261,16 @@ def _angles(pos, case):
     return torch.cos(a).float(), torch.sin(a).float()
 
 
-def _rotate(x, cos, sin):
-    """x [heads, tokens, d], cos / sin [tokens, d/2]: pairs (m, m + d/2)."""
-    h = x.shape[-1] // 2
-    a, b = x[..., :h], x[..., h:]
-    return torch.cat([a * cos - b * sin, b * cos + a * sin], dim=-1)
+def _plain_rotate(st):
+    """Channel pairs (m, m + d/2) of q and k turned by the token's position ID."""
+    case = st["case"]
+    cos, sin = _angles(torch.cat([pos for pos, _ in st["seqs"]]), case)
+    cos, sin = cos[:, None], (-sin if case["inverse"] else sin)[:, None]
+    h, out = case["d"] // 2, []
+    for x in (st["q"], st["k"]):
+        a, b = x[..., :h].float(), x[..., h:].float()
+        out.append(torch.cat([a * cos - b * sin, b * cos + a * sin], dim=-1).to(x.dtype))
+    return tuple(out)
 
 
 def _head_groups(case, s):
@@ -262,18 +280,17 @@ def _head_groups(case, s):
     return [(a, min(a + per, case["hkv"])) for a in range(0, case["hkv"], per)]
 
 
-def _plain_scores(st, a, b, lo, hi, pos, rank):
-    """Masked scores of kv heads a..b of one sequence, [b-a, G*S, S], with the rotated q and k."""
+def _plain_scores(st, a, b, lo, hi, rank):
+    """Masked scores of kv heads a..b of one sequence, [b-a, G*S, S], with q and k in 32 bits."""
     case = st["case"]
     g, s, d = case["hq"] // case["hkv"], hi - lo, case["d"]
-    cos, sin = _angles(pos, case)
-    q = _rotate(st["q"][lo:hi, a * g:b * g].float().transpose(0, 1), cos, sin).reshape(b - a, g * s, d)
-    k = _rotate(st["k"][lo:hi, a:b].float().transpose(0, 1), cos, sin)
+    q = st["q"][lo:hi, a * g:b * g].float().transpose(0, 1).reshape(b - a, g * s, d)
+    k = st["k"][lo:hi, a:b].float().transpose(0, 1)
     scores = torch.matmul(q, k.transpose(1, 2)) / math.sqrt(d)
-    at = torch.arange(s, device=pos.device)
+    at = torch.arange(s, device=rank.device)
     seen = (at[None, :] <= at[:, None]) & (rank[None, :] <= rank[:, None])
     scores = torch.where(seen, scores.view(b - a, g, s, s), -math.inf).view(b - a, g * s, s)
-    return q, k, scores, cos, sin
+    return q, k, scores
 
 
 def _plain_attention(st):
@@ -283,12 +300,12 @@ def _plain_attention(st):
     out = torch.empty((n, hq, d), dtype=st["q"].dtype, device=st["q"].device)
     lse = torch.empty((hq, n), dtype=torch.float32, device=st["q"].device)
     lo = 0
-    for pos, rank in st["seqs"]:
-        s = pos.numel()
+    for _, rank in st["seqs"]:
+        s = rank.numel()
         hi = lo + s
         if s:
             for a, b in _head_groups(case, s):
-                _, _, scores, _, _ = _plain_scores(st, a, b, lo, hi, pos, rank)
+                _, _, scores = _plain_scores(st, a, b, lo, hi, rank)
                 top = scores.amax(dim=-1, keepdim=True)
                 p = torch.exp(scores - top)
                 total = p.sum(dim=-1, keepdim=True)
@@ -310,12 +327,12 @@ def _plain_attention_grad(st):
     dk = torch.empty((n, hkv, d), dtype=dt, device=dev)
     dv = torch.empty((n, hkv, d), dtype=dt, device=dev)
     lo = 0
-    for pos, rank in st["seqs"]:
-        s = pos.numel()
+    for _, rank in st["seqs"]:
+        s = rank.numel()
         hi = lo + s
         if s:
             for a, b in _head_groups(case, s):
-                q, k, scores, cos, sin = _plain_scores(st, a, b, lo, hi, pos, rank)
+                q, k, scores = _plain_scores(st, a, b, lo, hi, rank)
                 p = torch.exp(scores - st["lse"][a * g:b * g, lo:hi].reshape(b - a, g * s, 1))
                 v = st["v"][lo:hi, a:b].float().transpose(0, 1)
                 do = st["d_out"][lo:hi, a * g:b * g].float().transpose(0, 1).reshape(b - a, g * s, d)
@@ -325,8 +342,8 @@ def _plain_attention_grad(st):
                 ds = p * (torch.matmul(do, v.transpose(1, 2)) - delta) / math.sqrt(d)
                 dq_ = torch.matmul(ds, k).view((b - a) * g, s, d)
                 dk_ = torch.matmul(ds.transpose(1, 2), q)
-                dq[lo:hi, a * g:b * g] = _rotate(dq_, cos, -sin).transpose(0, 1).to(dt)
-                dk[lo:hi, a:b] = _rotate(dk_, cos, -sin).transpose(0, 1).to(dt)
+                dq[lo:hi, a * g:b * g] = dq_.transpose(0, 1).to(dt)
+                dk[lo:hi, a:b] = dk_.transpose(0, 1).to(dt)
                 dv[lo:hi, a:b] = dv_.transpose(0, 1).to(dt)
         lo = hi
     return dq, dk, dv
@@ -381,23 +398,30 @@ def _prepare_own(st):
     case = st["case"]
     dt = B.HPD_F32 if case["dtype"] == "f32" else B.HPD_BF16
     st["B"], st["dt"] = B, dt
-    if case["op"] in ("attn", "attn_grad"):
+    if case["op"] in SEQUENCE_OPS:
+        hq, hkv, d = case["hq"], case["hkv"], case["d"]
         prompt, attr_ptr, attr_len, value_len = _lengths(case)
-        stride = st["q"].stride(0) if case["fused"] else 0
-        cfg = B.hpd_finetune_config(case["hq"], case["hkv"], case["d"], dt, case["base"], case["k_max"], 0, stride,
-                                    stride)
+        cfg = B.hpd_finetune_config(hq, hkv, d, dt, case["base"], case["k_max"], 0)
         st["layout"] = B.hpd_build_finetune_layout(cfg, prompt, attr_ptr, attr_len, value_len)
         n = st["q"].shape[0]
-        st["workspace"] = B.alloc_finetune_workspace(st["layout"], backward=case["op"] == "attn_grad")
 
         def empty(shape):
             return torch.empty(shape, dtype=_dtype(case), device="cuda")
 
+        if case["op"] == "rotate":  # gradients go back into the layout of what they belong to
+            st["q_out"], st["k_out"], _ = _qkv_buffers(dict(case, fused=case["fused"] and case["inverse"]), n, empty)
+            st["strides"] = B.hpd_finetune_strides(st["q"].stride(0), st["k"].stride(0), 0, st["q_out"].stride(0),
+                                                   st["k_out"].stride(0), 0)
+            return
+        st["workspace"] = B.alloc_finetune_workspace(st["layout"], backward=case["op"] == "attn_grad")
         if case["op"] == "attn":
-            st["out"] = empty((n, case["hq"], case["d"]))
-            st["lse"] = torch.empty((case["hq"], n), dtype=torch.float32, device="cuda")
+            st["out"] = empty((n, hq, d))
+            st["lse"] = torch.empty((hq, n), dtype=torch.float32, device="cuda")
+            st["strides"] = B.hpd_finetune_strides(v=st["v"].stride(0))
         else:
-            st["dq"], st["dk"], st["dv"] = _qkv_buffers(case, n, empty)
+            st["dq"], st["dk"] = empty((n, hq, d)), empty((n, hkv, d))
+            st["dv"] = _qkv_buffers(case, n, empty)[2]
+            st["strides"] = B.hpd_finetune_strides(v=st["v"].stride(0), v_out=st["dv"].stride(0))
         return
     rows, vocab = case["rows"], case["vocab"]
     if case["op"] == "logprobs":
@@ -410,14 +434,21 @@ def _prepare_own(st):
         st["d_logits"] = torch.empty((rows, vocab), dtype=_dtype(case), device="cuda")
 
 
+def _own_rotate(st):
+    st["B"].hpd_finetune_rotate(st["layout"], st["case"]["inverse"], st["q"], st["k"], st["q_out"], st["k_out"],
+                                st["strides"])
+    return st["q_out"], st["k_out"]
+
+
 def _own_attention(st):
-    st["B"].hpd_finetune_attention(st["layout"], st["q"], st["k"], st["v"], st["out"], st["lse"], st["workspace"])
+    st["B"].hpd_finetune_attention(st["layout"], st["q"], st["k"], st["v"], st["out"], st["lse"], st["workspace"],
+                                   st["strides"])
     return st["out"], st["lse"]
 
 
 def _own_attention_grad(st):
     st["B"].hpd_finetune_attention_backward(st["layout"], st["q"], st["k"], st["v"], st["out"], st["lse"],
-                                            st["d_out"], st["dq"], st["dk"], st["dv"], st["workspace"])
+                                            st["d_out"], st["dq"], st["dk"], st["dv"], st["workspace"], st["strides"])
     return st["dq"], st["dk"], st["dv"]
 
 
@@ -437,7 +468,7 @@ def _own_logprobs_grad(st):
     return st["d_logits"]
 
 
-_OWN = dict(attn=_own_attention, attn_grad=_own_attention_grad, logprobs=_own_logprobs,
+_OWN = dict(rotate=_own_rotate, attn=_own_attention, attn_grad=_own_attention_grad, logprobs=_own_logprobs,
             logprobs_grad=_own_logprobs_grad)
 
 
@@ -455,6 +486,10 @@ def _exact_turn(x, pos, base):
 
 def exact(case, seed):
     st = _make_inputs(case, seed)
+    if case["op"] == "rotate":
+        pos = torch.cat([p for p, _ in st["seqs"]]) * (-1 if case["inverse"] else 1)
+        return tuple(torch.stack([_exact_turn(x[:, h], pos, case["base"]) for h in range(x.shape[1])], dim=1)
+                     for x in (st["q"], st["k"]))
     if case["op"] in ("attn", "attn_grad"):
         n, hq, d = st["q"].shape
         hkv = case["hkv"]
@@ -475,8 +510,7 @@ def exact(case, seed):
             hidden |= rank.unsqueeze(0) > rank.unsqueeze(1)
             for h in range(hq):
                 c = h // (hq // hkv)
-                qh = _exact_turn(st["q"][sl, h], pos, case["base"]) / math.sqrt(d)
-                kh = _exact_turn(st["k"][sl, c], pos, case["base"])
+                qh, kh = st["q"][sl, h].double() / math.sqrt(d), st["k"][sl, c].double()
                 vh = st["v"][sl, c].double()
                 logits = (qh @ kh.T).masked_fill_(hidden, -math.inf)
                 norm = torch.logsumexp(logits, dim=1)
@@ -487,8 +521,8 @@ def exact(case, seed):
                     gh = st["d_out"][sl, h].double()
                     dv[sl, c] += prob.T @ gh
                     prob *= gh @ vh.T - (gh * oh).sum(dim=1, keepdim=True)
-                    dq[sl, h] = _exact_turn(prob @ kh, -pos, case["base"]) / math.sqrt(d)
-                    dk[sl, c] += _exact_turn(prob.T @ qh, -pos, case["base"])
+                    dq[sl, h] = prob @ kh / math.sqrt(d)
+                    dk[sl, c] += prob.T @ qh
         return (dq, dk, dv) if grad else (out, lse)
     logits, targets = st["logits"], st["targets"].long()
     parts = []
