@@ -371,6 +371,148 @@ int hpd_finetune_mask(int32_t prompt_len, int32_t n_attr, const int32_t* attr_le
                       const int32_t* value_len, int32_t k_max, int32_t* pos_out, uint8_t* mask_out,
                       int64_t* s_out, void* stream);
 
+/* ---------------------------------------------------------------------------------------------
+ * Fine-tuning - Section 4.4 ("Fine-tuning and Distillation").  The operators of a training step
+ * under the mask of hpd_finetune_mask, over a batch of sequences packed one after another without
+ * padding, and of the loss over the value tokens.
+ *
+ *   hpd_build_finetune_layout  positions, ranks and work lists of a batch; shared by all layers
+ *   hpd_finetune_rotate        rotates q and k at the position IDs (backward: turns dq and dk back)
+ *   hpd_finetune_attention     attention under the mask; keeps the log-sum-exp of every row
+ *   hpd_finetune_attention_backward
+ *                              dq, dk, dv; recomputes the probabilities from q, k and the log-sum-exp
+ *   hpd_token_logprobs         log probability of a given token per row of logits, entropy, the most
+ *                              likely tokens (also the scores of the tokens sampled at inference)
+ *   hpd_token_logprobs_backward
+ *                              the logits' gradient for given gradients of log probability and entropy
+ *
+ * The mask of hpd_finetune_mask as a comparison: a token's rank is k for the k-th (1-based) token
+ * of a value and 0 for prompt and attribute names; token i of a sequence sees token j of it iff
+ * j <= i and rank_j <= rank_i.  Every token sees itself, so no row is empty.
+ *
+ * Tensors are device memory, token-major: q, out [N][Hq][D], k, v [N][Hkv][D] in the layout's
+ * dtype, N = HPD_FTC_N_TOKENS tokens, sequence after sequence, each in the order of
+ * hpd_finetune_mask.  They start on 16 bytes; hpd_finetune_strides gives the distance between the
+ * tokens of those that are views of a wider buffer (a fused projection's output).  lse is fp32
+ * [Hq][N], natural logarithms.  Query head h uses kv head h / (Hq/Hkv); dk and dv are sums over
+ * the query heads that share them.  Sums, softmax and gradients are accumulated in fp32; under
+ * HPD_BF16 the probabilities and the scores' gradients are rounded to bf16 for the second
+ * products, and every output is rounded once.  No atomics: equal calls give equal bits.
+ * A non-finite element of a sequence can reach every output of its own sequence (a masked
+ * probability is a zero factor), and no other sequence's.
+ * The calls only enqueue kernels, allocate nothing and may be captured in a HIP graph.
+ */
+enum hpd_finetune_limits {
+  HPD_FINETUNE_MAX_DIM = 128, /* head_dim: a multiple of 8 up to this */
+  HPD_MAX_TOP = 64            /* most alternatives of hpd_token_logprobs */
+};
+
+typedef struct hpd_finetune_config {
+  int32_t n_q_heads;
+  int32_t n_kv_heads; /* divides n_q_heads */
+  int32_t head_dim;
+  int32_t dtype; /* hpd_dtype of q, k, v, out and of their gradients */
+  double rope_base;
+  int32_t k_max; /* K_max: the gap after every attribute, the longest value */
+  int32_t flags; /* hpd_flags: HPD_FLAG_HOST_ONLY builds the host tables only */
+} hpd_finetune_config;
+
+typedef struct hpd_finetune_layout hpd_finetune_layout; /* opaque */
+
+/* Elements from one token to the next (0 = the tokens lie next to each other); a multiple of 16
+ * bytes, at least the token's heads * D.  A NULL pointer in a call is all zeros. */
+typedef struct hpd_finetune_strides {
+  int64_t q, k, v;             /* inputs */
+  int64_t q_out, k_out, v_out; /* what hpd_finetune_rotate writes; dq, dk, dv of the backward call */
+} hpd_finetune_strides;
+
+enum hpd_finetune_query {
+  HPD_FTQ_COUNTS = 0,  /* int64[HPD_N_FT_COUNTS] */
+  HPD_FTQ_SEQ_OFF = 1, /* int32[n_seq + 1]: first token of every sequence */
+  HPD_FTQ_POS = 2,     /* int32[N]: position IDs */
+  HPD_FTQ_RANK = 3     /* int32[N] */
+};
+enum hpd_finetune_count {
+  HPD_FTC_N_SEQ = 0,
+  HPD_FTC_N_TOKENS = 1, /* N */
+  HPD_FTC_MAX_LEN = 2,  /* longest sequence */
+  HPD_FTC_MAX_POS = 3,  /* largest position ID (-1 without tokens) */
+  HPD_FTC_FORWARD_BYTES = 4,  /* workspace of hpd_finetune_attention */
+  HPD_FTC_BACKWARD_BYTES = 5, /* ... and of hpd_finetune_attention_backward */
+  HPD_N_FT_COUNTS = 6
+};
+
+/*
+ * hpd_build_finetune_layout - all input arrays are host memory and are copied; synchronises
+ * `stream` once.
+ *   prompt_len [n_seq] >= 0
+ *   attr_ptr   [n_seq+1]   CSR sequences -> attributes, attr_ptr[0] = 0, non-decreasing
+ *   attr_len   [n_attr]    >= 1 tokens of the attribute's name
+ *   value_len  [n_attr]    in [0, k_max] tokens of its value
+ * A sequence may be empty.  HPD_E_OVERFLOW if a position exceeds 2^30, the number of tokens 2^25, or
+ * tokens times query heads 2^27.
+ */
+int hpd_build_finetune_layout(const hpd_finetune_config* cfg, int32_t n_seq, const int32_t* prompt_len,
+                              const int32_t* attr_ptr, const int32_t* attr_len, const int32_t* value_len,
+                              void* stream, hpd_finetune_layout** out);
+void hpd_finetune_layout_free(hpd_finetune_layout* layout);
+/* Copies one table to host memory.  `bytes` must be at least the table's size. */
+int hpd_finetune_layout_query(const hpd_finetune_layout* layout, int32_t what, void* host_out, size_t bytes);
+
+/* hpd_finetune_rotate - channel pairs (m, m + D/2) of q and k, turned by the token's position ID
+ * times rope_base^(-2m/D); inverse != 0: by the negative angle (the gradient of the rotation).
+ * q_out may be q and k_out may be k with equal strides. */
+int hpd_finetune_rotate(const hpd_finetune_layout* layout, int32_t inverse, const void* q, const void* k, void* q_out,
+                        void* k_out, const hpd_finetune_strides* strides, void* stream);
+
+/* hpd_finetune_attention - out = softmax(q . k^T / sqrt(D)) v over the visible tokens, q and k as
+ * hpd_finetune_rotate leaves them.
+ *   workspace : device, HPD_FTC_FORWARD_BYTES (may be NULL if that is 0), 16-byte aligned, not shared
+ *               by calls that overlap */
+int hpd_finetune_attention(const hpd_finetune_layout* layout, const void* q, const void* k, const void* v, void* out,
+                           float* lse, void* workspace, const hpd_finetune_strides* strides, void* stream);
+
+/* hpd_finetune_attention_backward - gradients of the rotated q and k and of v, from d_out and from
+ * what the forward call has left in out and lse.
+ *   out, d_out : [N][Hq][D] without gaps
+ *   workspace  : device, HPD_FTC_BACKWARD_BYTES, as above */
+int hpd_finetune_attention_backward(const hpd_finetune_layout* layout, const void* q, const void* k, const void* v,
+                                    const void* out, const float* lse, const void* d_out, void* dq, void* dk, void* dv,
+                                    void* workspace, const hpd_finetune_strides* strides, void* stream);
+
+/*
+ * hpd_token_logprobs - per row x of logits (fp32 or bf16, hpd_dtype; any alignment):
+ *   lse = log sum_c exp x_c;  logprob = x_target - lse;  entropy = -sum_c p_c log p_c, p = exp(x - lse);
+ *   top_id, top_logprob: the top_k largest logits in descending order, the lowest index first
+ *   among equals (NaN counts as -infinity there).
+ *   row_stride : elements between rows, at least vocab
+ *   targets    : device int32 [n_rows] or NULL (then logprob is not written); a row whose target is
+ *                outside [0, vocab) has logprob 0
+ *   logprob, lse, entropy : device fp32 [n_rows], each may be NULL
+ *   top_id     : device int32 [n_rows][top_k], top_logprob: fp32 [n_rows][top_k]; 0 <= top_k <=
+ *                min(vocab, HPD_MAX_TOP)
+ *   workspace  : device, the bytes that hpd_token_logprobs_workspace reports (NULL if 0), 16-byte aligned
+ * A logit of -infinity has probability 0.  A row of nothing else: lse and the log probabilities are
+ * -infinity, entropy 0.  A row with a NaN or +infinity: lse, log probabilities and entropy are NaN.
+ */
+int hpd_token_logprobs(int32_t dtype, int64_t n_rows, int32_t vocab, int64_t row_stride, const void* logits,
+                       const int32_t* targets, int32_t top_k, float* logprob, float* lse, float* entropy,
+                       int32_t* top_id, float* top_logprob, void* workspace, void* stream);
+int hpd_token_logprobs_workspace(int32_t dtype, int64_t n_rows, int32_t vocab, int32_t top_k, int64_t* bytes);
+
+/*
+ * hpd_token_logprobs_backward - d_logits_c = g_logprob ([c = target] - p_c) - g_entropy p_c (log p_c + entropy)
+ *   lse, entropy (needed with g_entropy only) : as hpd_token_logprobs has left them
+ *   g_logprob : device fp32 [n_rows] or NULL (0); rows without a target inside [0, vocab) take 0
+ *   g_entropy : device fp32 [n_rows] or NULL (0)
+ *   d_logits  : [n_rows] rows of vocab elements of the same dtype, d_stride elements apart; may be
+ *               logits with d_stride = row_stride
+ * A row whose logits are all -infinity has gradient 0.
+ */
+int hpd_token_logprobs_backward(int32_t dtype, int64_t n_rows, int32_t vocab, int64_t row_stride, const void* logits,
+                                const int32_t* targets, const float* lse, const float* entropy, const float* g_logprob,
+                                const float* g_entropy, void* d_logits, int64_t d_stride, void* stream);
+
 /* Selects the attention kernel: 0 = automatic (bf16: as 2 where that is allowed; fp32 decode under
  * HPD_MASK_BLOCK with head_dim 32, 64 or 128, up to 16 query heads per kv head and pools that start on
  * 16 bytes: a kernel on the fp32 matrix instruction, or the generic one for the steps for which the layout

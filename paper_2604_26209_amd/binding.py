@@ -50,11 +50,19 @@ HPD_KEY_BLOCK = 32
 (HPD_C_N_PROMPTS, HPD_C_N_DOCS, HPD_C_N_BRANCHES, HPD_C_N_PREFIX_TOKENS, HPD_C_N_PREFIX_SLOTS,
  HPD_C_N_TAIL_SLOTS, HPD_C_MAX_POS, HPD_C_TOTAL_LIVE, HPD_N_COUNTS) = range(9)
 
+HPD_FINETUNE_MAX_DIM, HPD_MAX_TOP = 128, 64
+HPD_FTQ_COUNTS, HPD_FTQ_SEQ_OFF, HPD_FTQ_POS, HPD_FTQ_RANK = range(4)
+(HPD_FTC_N_SEQ, HPD_FTC_N_TOKENS, HPD_FTC_MAX_LEN, HPD_FTC_MAX_POS, HPD_FTC_FORWARD_BYTES,
+ HPD_FTC_BACKWARD_BYTES, HPD_N_FT_COUNTS) = range(7)
+
 EXPORTS = ["hpd_build_layout", "hpd_layout_free", "hpd_layout_query", "hpd_prefix_fill",
            "hpd_rope_positions", "hpd_kv_append", "hpd_decode_attention", "hpd_decode_step",
            "hpd_expand_mask", "hpd_set_kernel_mode", "hpd_status_string", "hpd_finetune_mask",
            "hpd_prefill_attention", "hpd_dynamic_begin", "hpd_dynamic_prune", "hpd_dynamic_step",
-           "hpd_dynamic_state", "hpd_dynamic_read", "hpd_set_tail_pages", "hpd_dynamic_begin_static"]
+           "hpd_dynamic_state", "hpd_dynamic_read", "hpd_set_tail_pages", "hpd_dynamic_begin_static",
+           "hpd_build_finetune_layout", "hpd_finetune_layout_free", "hpd_finetune_layout_query", "hpd_finetune_rotate",
+           "hpd_finetune_attention", "hpd_finetune_attention_backward", "hpd_token_logprobs",
+           "hpd_token_logprobs_workspace", "hpd_token_logprobs_backward"]
 # include/hpd_peaks.h: reference kernels for the benchmark's measured peaks
 PEAK_EXPORTS = ["hpd_peak_read", "hpd_peak_copy", "hpd_peak_mfma"]
 
@@ -65,6 +73,17 @@ class hpd_config(ctypes.Structure):
                 ("rope_base", ctypes.c_double), ("max_new", ctypes.c_int32),
                 ("pos_mode", ctypes.c_int32), ("mask_mode", ctypes.c_int32),
                 ("flags", ctypes.c_int32), ("out_dtype", ctypes.c_int32)]
+
+
+class hpd_finetune_config(ctypes.Structure):
+    _fields_ = [("n_q_heads", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32),
+                ("head_dim", ctypes.c_int32), ("dtype", ctypes.c_int32),
+                ("rope_base", ctypes.c_double), ("k_max", ctypes.c_int32), ("flags", ctypes.c_int32)]
+
+
+class hpd_finetune_strides(ctypes.Structure):
+    """Elements between tokens; 0 = no gap."""
+    _fields_ = [(_f, ctypes.c_int64) for _f in ("q", "k", "v", "q_out", "k_out", "v_out")]
 
 
 _vp, _i32, _i64p = ctypes.c_void_p, ctypes.c_int32, ctypes.POINTER(ctypes.c_int64)
@@ -90,6 +109,17 @@ _lib.hpd_dynamic_state.argtypes = [_vp, ctypes.POINTER(_vp), ctypes.POINTER(_vp)
 _lib.hpd_dynamic_read.argtypes = [_vp, _i32p, _i32, _i32p, _vp]
 _lib.hpd_set_tail_pages.argtypes = [_vp, _i32, _i32, _vp]
 _lib.hpd_finetune_mask.argtypes = [_i32, _i32, _vp, _vp, _i32, _vp, _vp, ctypes.POINTER(ctypes.c_int64), _vp]
+_i64 = ctypes.c_int64
+_lib.hpd_build_finetune_layout.argtypes = [ctypes.POINTER(hpd_finetune_config), _i32, _i32p, _i32p, _i32p, _i32p, _vp,
+                                           ctypes.POINTER(_vp)]
+_lib.hpd_finetune_layout_free.argtypes = [_vp]
+_lib.hpd_finetune_layout_query.argtypes = [_vp, _i32, _vp, ctypes.c_size_t]
+_lib.hpd_finetune_rotate.argtypes = [_vp, _i32] + [_vp] * 6
+_lib.hpd_finetune_attention.argtypes = [_vp] * 9
+_lib.hpd_finetune_attention_backward.argtypes = [_vp] * 13
+_lib.hpd_token_logprobs.argtypes = [_i32, _i64, _i32, _i64, _vp, _vp, _i32] + [_vp] * 7
+_lib.hpd_token_logprobs_workspace.argtypes = [_i32, _i64, _i32, _i32, _i64p]
+_lib.hpd_token_logprobs_backward.argtypes = [_i32, _i64, _i32, _i64] + [_vp] * 7 + [_i64, _vp]
 _lib.hpd_peak_read.argtypes = [_vp, ctypes.c_size_t, _vp, _vp]
 _lib.hpd_peak_copy.argtypes = [_vp, _vp, ctypes.c_size_t, _vp]
 _lib.hpd_peak_mfma.argtypes = [_vp, _i32, ctypes.POINTER(ctypes.c_double), _vp]
@@ -98,8 +128,9 @@ for _name in PEAK_EXPORTS:
 _lib.hpd_status_string.argtypes = [ctypes.c_int]
 _lib.hpd_status_string.restype = ctypes.c_char_p
 for _name in EXPORTS:
-    if _name not in ("hpd_layout_free", "hpd_status_string"):
+    if _name not in ("hpd_layout_free", "hpd_finetune_layout_free", "hpd_status_string"):
         getattr(_lib, _name).restype = ctypes.c_int
+_lib.hpd_finetune_layout_free.restype = None
 
 
 class HpdError(RuntimeError):
@@ -314,6 +345,109 @@ def hpd_finetune_mask(prompt_len, attr_len, value_len, k_max, pos_out=None, mask
     _check(_lib.hpd_finetune_mask(int(prompt_len), a.shape[0], a.ctypes.data, v.ctypes.data, int(k_max), _ptr(pos_out),
                                   _ptr(mask_out), ctypes.byref(s), _stream(stream)), "hpd_finetune_mask")
     return int(s.value)
+
+
+class hpd_finetune_layout:
+    """Owner of an opaque ``hpd_finetune_layout*``."""
+
+    def __init__(self, handle, cfg):
+        self.handle = handle
+        self.cfg = cfg
+
+    def free(self):
+        if self.handle:
+            _lib.hpd_finetune_layout_free(self.handle)
+            self.handle = None
+
+    def __del__(self):
+        try:
+            self.free()
+        except Exception:
+            pass
+
+    def counts(self):
+        return hpd_finetune_layout_query(self, HPD_FTQ_COUNTS)
+
+
+def hpd_build_finetune_layout(cfg: hpd_finetune_config, prompt_len, attr_ptr, attr_len, value_len,
+                              stream=None) -> hpd_finetune_layout:
+    keep = [_host_i32(a) for a in (prompt_len, attr_ptr, attr_len, value_len)]
+    n_seq = int(keep[0][0].shape[0])
+    if keep[1][0].shape[0] != n_seq + 1 or any(a.shape[0] < keep[1][0][-1] for a, _ in keep[2:]):
+        raise ValueError("attr_ptr has n_seq + 1 entries, attr_len and value_len one for every attribute")
+    out = _vp()
+    st = None if (cfg.flags & HPD_FLAG_HOST_ONLY) else _stream(stream)
+    _check(_lib.hpd_build_finetune_layout(ctypes.byref(cfg), n_seq, *[p for _, p in keep], st, ctypes.byref(out)),
+           "hpd_build_finetune_layout")
+    return hpd_finetune_layout(out.value, cfg)
+
+
+def hpd_finetune_layout_free(layout: hpd_finetune_layout):
+    layout.free()
+
+
+def hpd_finetune_layout_query(layout: hpd_finetune_layout, what: int):
+    """Returns the selected table as a NumPy array."""
+    c = np.zeros(HPD_N_FT_COUNTS, dtype=np.int64)
+    _check(_lib.hpd_finetune_layout_query(layout.handle, HPD_FTQ_COUNTS, c.ctypes.data, c.nbytes),
+           "hpd_finetune_layout_query")
+    if what == HPD_FTQ_COUNTS:
+        return c
+    size = int(c[HPD_FTC_N_SEQ]) + 1 if what == HPD_FTQ_SEQ_OFF else int(c[HPD_FTC_N_TOKENS])
+    out = np.zeros(max(size, 1), dtype=np.int32)
+    _check(_lib.hpd_finetune_layout_query(layout.handle, int(what), out.ctypes.data, out.nbytes),
+           "hpd_finetune_layout_query")
+    return out[:size]
+
+
+def alloc_finetune_workspace(layout, backward=True, device="cuda"):
+    """The workspace of hpd_finetune_attention, or of the backward call."""
+    n = int(layout.counts()[HPD_FTC_BACKWARD_BYTES if backward else HPD_FTC_FORWARD_BYTES])
+    return torch.empty(n, dtype=torch.uint8, device=device) if n else None
+
+
+def _strides(s):
+    return None if s is None else ctypes.addressof(s)
+
+
+def hpd_finetune_rotate(layout, inverse, q, k, q_out, k_out, strides=None, stream=None):
+    _check(_lib.hpd_finetune_rotate(layout.handle, int(inverse), _ptr(q), _ptr(k), _ptr(q_out), _ptr(k_out),
+                                    _strides(strides), _stream(stream)), "hpd_finetune_rotate")
+
+
+def hpd_finetune_attention(layout, q, k, v, out, lse, workspace=None, strides=None, stream=None):
+    _check(_lib.hpd_finetune_attention(layout.handle, _ptr(q), _ptr(k), _ptr(v), _ptr(out), _ptr(lse),
+                                       _ptr(workspace), _strides(strides), _stream(stream)), "hpd_finetune_attention")
+
+
+def hpd_finetune_attention_backward(layout, q, k, v, out, lse, d_out, dq, dk, dv, workspace=None, strides=None,
+                                    stream=None):
+    _check(_lib.hpd_finetune_attention_backward(layout.handle, _ptr(q), _ptr(k), _ptr(v), _ptr(out), _ptr(lse),
+                                                _ptr(d_out), _ptr(dq), _ptr(dk), _ptr(dv), _ptr(workspace),
+                                                _strides(strides), _stream(stream)),
+           "hpd_finetune_attention_backward")
+
+
+def hpd_token_logprobs_workspace(dtype, n_rows, vocab, top_k) -> int:
+    n = ctypes.c_int64(0)
+    _check(_lib.hpd_token_logprobs_workspace(int(dtype), int(n_rows), int(vocab), int(top_k), ctypes.byref(n)),
+           "hpd_token_logprobs_workspace")
+    return int(n.value)
+
+
+def hpd_token_logprobs(dtype, n_rows, vocab, row_stride, logits, targets=None, top_k=0, logprob=None, lse=None,
+                       entropy=None, top_id=None, top_logprob=None, workspace=None, stream=None):
+    _check(_lib.hpd_token_logprobs(int(dtype), int(n_rows), int(vocab), int(row_stride), _ptr(logits), _ptr(targets),
+                                   int(top_k), _ptr(logprob), _ptr(lse), _ptr(entropy), _ptr(top_id),
+                                   _ptr(top_logprob), _ptr(workspace), _stream(stream)), "hpd_token_logprobs")
+
+
+def hpd_token_logprobs_backward(dtype, n_rows, vocab, row_stride, logits, targets, lse, entropy, g_logprob, g_entropy,
+                                d_logits, d_stride, stream=None):
+    _check(_lib.hpd_token_logprobs_backward(int(dtype), int(n_rows), int(vocab), int(row_stride), _ptr(logits),
+                                            _ptr(targets), _ptr(lse), _ptr(entropy), _ptr(g_logprob), _ptr(g_entropy),
+                                            _ptr(d_logits), int(d_stride), _stream(stream)),
+           "hpd_token_logprobs_backward")
 
 
 def hpd_peak_read(src, nbytes, sink, stream=None):

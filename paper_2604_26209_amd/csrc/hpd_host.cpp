@@ -12,14 +12,16 @@
 
 #include "hpd_internal.h"
 
-namespace {
+static thread_local std::string g_hip_text = "no HIP error recorded";
 
-thread_local std::string g_hip_text = "no HIP error recorded";
-
-int hip_fail(hipError_t e) {
+int hpd_hip_fail(hipError_t e) {
   g_hip_text = std::string("HIP error: ") + hipGetErrorString(e);
   return HPD_E_HIP;
 }
+
+namespace {
+
+int hip_fail(hipError_t e) { return hpd_hip_fail(e); }
 
 #define HPD_HIP(expr)                        \
   do {                                       \

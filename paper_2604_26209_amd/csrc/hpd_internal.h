@@ -9,6 +9,9 @@
 
 #include "hpd.h"
 
+// Keeps the text that hpd_status_string(HPD_E_HIP) gives (per thread) and returns HPD_E_HIP.
+int hpd_hip_fail(hipError_t e);
+
 // Device-resident tables of one layout.  All int32 tables live in one allocation.
 struct hpd_dev_tables {
   const int32_t* seg_off;       // [n_seg] first pool slot of header p (index p) / document d (index P+d)

@@ -1,0 +1,424 @@
+// Log probabilities of given tokens with entropy and the most likely alternatives, and their gradient.
+//
+// With m = max x, s = sum exp(x - m), t = sum exp(x - m) (x - m):
+//   lse = m + log s,  logprob = x_target - lse,  entropy = log s - t / s.
+// One pass over the logits: every lane keeps (m, s, t) of its share and rescales s and t when its
+// maximum moves (t' = (t - d s) e^-d for a maximum that rises by d); partial results are joined by the
+// same rule.  The pass is bound by the bytes of the logits.
+//
+// Alternatives: a wave keeps its 64 largest (value, index) keys, lane i the i-th.  A vector of logits
+// costs one comparison of its maximum with the last key that counts; what passes is inserted.
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include <algorithm>
+
+#include "hpd_attn_bf16.h"
+#include "hpd_finetune.h"
+
+namespace {
+
+constexpr float LOG2E = 1.44269504088896340736f;
+constexpr float LOWEST = -3.402823466e38f;
+constexpr int UNROLL = 4;          // vectors in flight per lane
+constexpr int64_t MAX_GRID = 1 << 20;
+
+// 16 bytes at any address that the element type allows
+template <typename T>
+struct Vec;
+template <>
+struct Vec<float> {
+  static constexpr int N = 4;
+  struct __attribute__((packed, aligned(4))) Raw { uint32_t w[4]; };
+  static __device__ __forceinline__ void unpack(const Raw& r, float* f) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) f[i] = __uint_as_float(r.w[i]);
+  }
+  static __device__ __forceinline__ Raw pack(const float* f) {
+    Raw r;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) r.w[i] = __float_as_uint(f[i]);
+    return r;
+  }
+};
+template <>
+struct Vec<hpd::bf16_t> {
+  static constexpr int N = 8;
+  struct __attribute__((packed, aligned(2))) Raw { uint32_t w[4]; };
+  static __device__ __forceinline__ void unpack(const Raw& r, float* f) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      f[2 * i] = __uint_as_float(r.w[i] << 16);
+      f[2 * i + 1] = __uint_as_float(r.w[i] & 0xffff0000u);
+    }
+  }
+  static __device__ __forceinline__ Raw pack(const float* f) {
+    Raw r;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) r.w[i] = cvt_pk_bf16(f[2 * i], f[2 * i + 1]);
+    return r;
+  }
+};
+
+// ---- sums
+struct Sums {
+  float m, s, t;
+};
+// exp and x - m of one logit; -infinity counts nothing, NaN and +infinity make s NaN
+__device__ __forceinline__ void add_logit(Sums& a, float x) {
+  const float d = x - a.m, e = fast_exp2(d * LOG2E);
+  a.s += e;
+  a.t = fmaf(e, fmaxf(d, -200.f), a.t);
+}
+// raises the maximum to m >= a.m
+__device__ __forceinline__ void raise(Sums& a, float m) {
+  const float d = fminf(m - a.m, 1.0e4f), f = fast_exp2(-d * LOG2E);
+  a.t = fmaf(-d, a.s, a.t) * f;
+  a.s *= f;
+  a.m = m;
+}
+__device__ __forceinline__ Sums join(Sums a, Sums b) {
+  const float m = fmaxf(a.m, b.m);
+  raise(a, m);
+  raise(b, m);
+  return {m, a.s + b.s, a.t + b.t};
+}
+__device__ __forceinline__ Sums join_wave(Sums a) {
+#pragma unroll
+  for (int d = 32; d; d >>= 1) a = join(a, {__shfl_xor(a.m, d), __shfl_xor(a.s, d), __shfl_xor(a.t, d)});
+  return a;
+}
+
+// ---- keys: larger = larger logit, then lower index; 0 = none
+__device__ __forceinline__ uint64_t make_key(float x, int32_t index) {
+  x = x == x ? x + 0.f : -INFINITY;  // (-0 = +0)
+  const uint32_t u = __float_as_uint(x);
+  const uint32_t o = u & 0x80000000u ? ~u : u | 0x80000000u;
+  return ((uint64_t)o << 32) | (uint32_t)~index;
+}
+__device__ __forceinline__ float key_value(uint64_t k) {
+  const uint32_t o = (uint32_t)(k >> 32);
+  return __uint_as_float(o & 0x80000000u ? o & 0x7fffffffu : ~o);
+}
+__device__ __forceinline__ uint64_t shuffle(uint64_t k, int from) {
+  return ((uint64_t)(uint32_t)__shfl((int)(k >> 32), from) << 32) | (uint32_t)__shfl((int)(uint32_t)k, from);
+}
+__device__ __forceinline__ uint64_t read_lane(uint64_t k, int from) {
+  return ((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(k >> 32), from) << 32) |
+         (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)k, from);
+}
+__device__ __forceinline__ uint64_t larger(uint64_t a, uint64_t b) { return a > b ? a : b; }
+__device__ __forceinline__ uint64_t smaller(uint64_t a, uint64_t b) { return a > b ? b : a; }
+
+// one stage of a bitonic network over the 64 lanes; up: the lane belongs to a run sorted upwards
+__device__ __forceinline__ uint64_t stage(uint64_t k, int distance, bool up, int lane) {
+  const uint64_t o = shuffle(k, lane ^ distance);
+  const bool low = (lane & distance) == 0;
+  return low != up ? larger(k, o) : smaller(k, o);
+}
+// a bitonic sequence sorted downwards
+__device__ __forceinline__ uint64_t settle(uint64_t k, int lane) {
+#pragma nounroll
+  for (int d = 32; d; d >>= 1) k = stage(k, d, false, lane);
+  return k;
+}
+__device__ __forceinline__ uint64_t sort_down(uint64_t k, int lane) {
+#pragma nounroll
+  for (int n = 2; n <= 64; n <<= 1)
+#pragma nounroll
+    for (int d = n >> 1; d; d >>= 1) k = stage(k, d, (lane & n) != 0, lane);
+  return k;
+}
+// the 64 largest of two lists sorted downwards
+__device__ __forceinline__ uint64_t merge(uint64_t a, uint64_t b, int lane) {
+  return settle(larger(a, shuffle(b, 63 - lane)), lane);
+}
+
+struct Top {
+  uint64_t list = 0;  // lane i: the i-th largest
+  uint64_t last = 0;  // the K-th, in every lane
+  float bar = 0.f;    // its value once there are K
+  bool full = false;
+  __device__ __forceinline__ void update(int K) {
+    last = read_lane(list, K - 1);
+    full = last != 0;
+    bar = key_value(last);
+  }
+  // one candidate per lane
+  __device__ __forceinline__ void add(uint64_t key, int K, int lane) {
+    uint64_t left = __ballot(key > last);
+    if (left == 0) return;
+    if (__popcll(left) > 6) {
+      list = merge(list, sort_down(key > last ? key : 0, lane), lane);
+      update(K);
+      return;
+    }
+    while (left) {
+      const uint64_t c = read_lane(key, __builtin_ctzll(left));
+      const int at = __popcll(__ballot(list > c));
+      const uint64_t above = shuffle(list, lane ? lane - 1 : 0);
+      list = lane < at ? list : lane == at ? c : above;
+      update(K);
+      left &= left - 1;
+      left &= __ballot(key > last);
+    }
+  }
+};
+
+struct Shared {
+  uint64_t list[4][64];
+  Sums sums[4];
+};
+
+// results of a row, by one wave (x - m - log s: where all logits lie far from 0, log s is less than a step of lse)
+__device__ __forceinline__ void finish(const hpd_logprobs_args& a, int64_t row, Sums s, uint64_t list, float x_target,
+                                       bool has_target, int lane) {
+  const bool none = s.s == 0.f;  // nothing but -infinity
+  const float log_s = logf(s.s), lse = none ? -INFINITY : s.m + log_s;
+  if (lane == 0) {
+    if (a.lse) a.lse[row] = lse;
+    if (a.entropy) a.entropy[row] = none ? 0.f : log_s - s.t / s.s;
+    if (a.targets && a.logprob) a.logprob[row] = !has_target ? 0.f : none ? -INFINITY : x_target - s.m - log_s;
+  }
+  if (lane < a.top_k) {
+    a.top_id[row * a.top_k + lane] = (int32_t)~(uint32_t)list;
+    a.top_logprob[row * a.top_k + lane] = none ? -INFINITY : key_value(list) - s.m - log_s;
+  }
+}
+
+// The piece [begin, end) of a row by WV waves, of which this is number w.
+template <typename T, bool TOP>
+__device__ __forceinline__ void scan(const T* x, int32_t begin, int32_t end, int w, int WV, int K, int lane, Sums& sums, Top& top) {
+  using V = Vec<T>;
+  sums = {LOWEST, 0.f, 0.f};
+  // one vector per lane, the first logit of which is number `index`; n of its logits exist
+  auto take = [&](const float* f, int32_t index, int n) __attribute__((always_inline)) {
+    float m = f[0];
+#pragma unroll
+    for (int e = 1; e < V::N; ++e) m = fmaxf(m, f[e]);
+    if (m > sums.m) raise(sums, m);
+#pragma unroll
+    for (int e = 0; e < V::N; ++e) add_logit(sums, f[e]);
+    if constexpr (TOP) {
+      if (__any(!top.full || m > top.bar)) {
+#pragma unroll
+        for (int e = 0; e < V::N; ++e) top.add(e < n ? make_key(f[e], index + e) : 0, K, lane);
+      }
+    }
+  };
+  constexpr int32_t STEP = 64 * V::N, RUN = STEP * UNROLL;  // logits of a vector of all lanes, of a turn of the wave
+  int32_t at = begin + w * RUN;
+  for (; at + RUN <= end; at += WV * RUN) {
+    typename V::Raw r[UNROLL];
+#pragma unroll
+    for (int u = 0; u < UNROLL; ++u) r[u] = *reinterpret_cast<const typename V::Raw*>(x + at + u * STEP + lane * V::N);
+#pragma unroll
+    for (int u = 0; u < UNROLL; ++u) {
+      float f[V::N];
+      V::unpack(r[u], f);
+      take(f, at + u * STEP + lane * V::N, V::N);
+    }
+  }
+  // the wave's part of a turn that the end cuts: vectors that are not whole logit by logit, -infinity behind the end
+  if (at < end) {
+    typename V::Raw r[UNROLL];
+#pragma unroll
+    for (int u = 0; u < UNROLL; ++u)
+      if (at + u * STEP + (lane + 1) * V::N <= end)
+        r[u] = *reinterpret_cast<const typename V::Raw*>(x + at + u * STEP + lane * V::N);
+#pragma unroll
+    for (int u = 0; u < UNROLL; ++u) {
+      const int32_t index = at + u * STEP + lane * V::N;
+      if (at + u * STEP >= end) break;
+      float f[V::N];
+      if (index + V::N <= end) {
+        V::unpack(r[u], f);
+      } else {
+#pragma unroll
+        for (int e = 0; e < V::N; ++e) f[e] = index + e < end ? hpd::to_float(x[index + e]) : -INFINITY;
+      }
+      take(f, index, end - index);
+    }
+  }
+}
+
+template <typename T, bool TOP>
+__global__ void __launch_bounds__(256) logprobs_kernel(hpd_logprobs_args a, int32_t parts, int32_t span, int32_t waves) {
+  __shared__ Shared sh;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int K = a.top_k;
+  const T* logits = reinterpret_cast<const T*>(a.logits);
+  const int64_t per = 4 / waves, items = (a.n_rows * parts + per - 1) / per;
+  for (int64_t item = blockIdx.x; item < items; item += gridDim.x) {
+    const int64_t piece = item * per + (waves == 1 ? wave : 0);
+    if (waves == 1 && piece >= a.n_rows) continue;  // (a wave of its own: no barrier below)
+    const int64_t row = piece / parts;
+    const int32_t part = (int32_t)(piece % parts);
+    const T* x = logits + row * a.row_stride;
+    const int32_t begin = part * span, end = min(begin + span, a.vocab);
+    Sums sums;
+    Top top;
+    scan<T, TOP>(x, begin, end, waves == 1 ? 0 : wave, waves, K, lane, sums, top);
+    sums = join_wave(sums);
+    if (waves > 1) {
+      if (TOP) sh.list[wave][lane] = top.list;
+      if (lane == 0) sh.sums[wave] = sums;
+      __syncthreads();
+      if (wave == 0) {
+#pragma unroll
+        for (int w = 1; w < 4; ++w) {
+          sums = join(sums, sh.sums[w]);
+          if (TOP) top.list = merge(top.list, sh.list[w][lane], lane);
+        }
+      }
+    }
+    if (wave == 0 || waves == 1) {
+      if (parts == 1) {
+        const int32_t t = a.targets ? a.targets[row] : -1;
+        const bool has = t >= 0 && t < a.vocab;
+        finish(a, row, sums, top.list, has ? hpd::to_float(x[t]) : 0.f, has, lane);
+      } else {
+        float4* ws = reinterpret_cast<float4*>(a.workspace);
+        if (lane == 0) ws[piece] = make_float4(sums.m, sums.s, sums.t, 0.f);
+        if (TOP && lane < K) reinterpret_cast<uint64_t*>(ws + a.n_rows * parts)[piece * K + lane] = top.list;
+      }
+    }
+    if (waves > 1) __syncthreads();
+  }
+}
+
+// joins the pieces of a row: four waves take every fourth
+template <typename T, bool TOP>
+__global__ void __launch_bounds__(256) logprobs_join_kernel(hpd_logprobs_args a, int32_t parts) {
+  __shared__ Shared sh;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int K = a.top_k;
+  const float4* ws = reinterpret_cast<const float4*>(a.workspace);
+  const uint64_t* lists = reinterpret_cast<const uint64_t*>(ws + a.n_rows * parts);
+  for (int64_t row = blockIdx.x; row < a.n_rows; row += gridDim.x) {
+    Sums sums{LOWEST, 0.f, 0.f};
+    if (lane < parts && lane % 4 == wave) {
+      const float4 p = ws[row * parts + lane];
+      sums = {p.x, p.y, p.z};
+    }
+    uint64_t list = 0;
+    if constexpr (TOP) {
+      for (int32_t p = wave; p < parts; p += 4) list = merge(list, lane < K ? lists[(row * parts + p) * K + lane] : 0, lane);
+      sh.list[wave][lane] = list;
+    }
+    sums = join_wave(sums);
+    if (lane == 0) sh.sums[wave] = sums;
+    __syncthreads();
+    if (wave == 0) {
+#pragma unroll
+      for (int w = 1; w < 4; ++w) {
+        sums = join(sums, sh.sums[w]);
+        if (TOP) list = merge(list, sh.list[w][lane], lane);
+      }
+      const int32_t t = a.targets ? a.targets[row] : -1;
+      const bool has = t >= 0 && t < a.vocab;
+      const T* x = reinterpret_cast<const T*>(a.logits) + row * a.row_stride;
+      finish(a, row, sums, list, has ? hpd::to_float(x[t]) : 0.f, has, lane);
+    }
+    __syncthreads();
+  }
+}
+
+// d_c = g ([c = target] - p_c) - h p_c (log p_c + H), 4 vectors per lane and turn
+template <typename T>
+__global__ void __launch_bounds__(256) logprobs_backward_kernel(hpd_logprobs_backward_args a, int32_t pieces) {
+  using V = Vec<T>;
+  constexpr int32_t RUN = 256 * V::N * UNROLL;
+  for (int64_t item = blockIdx.x; item < a.n_rows * pieces; item += gridDim.x) {
+    const int64_t row = item / pieces;
+    const int32_t begin = (int32_t)(item % pieces) * RUN, end = min(begin + RUN, a.vocab);
+    const T* x = reinterpret_cast<const T*>(a.logits) + row * a.row_stride;
+    T* dx = reinterpret_cast<T*>(a.d_logits) + row * a.d_stride;
+    const float lse = a.lse[row];
+    const int32_t target = a.targets ? a.targets[row] : -1;
+    const bool has = target >= 0 && target < a.vocab;
+    const float g = a.g_logprob && has ? a.g_logprob[row] : 0.f, hg = a.g_entropy ? a.g_entropy[row] : 0.f;
+    const float H = a.g_entropy ? a.entropy[row] : 0.f;
+    const bool none = lse == -INFINITY;
+    auto gradient = [&](float f, int32_t c) -> float {
+      const float lp = f - lse, p = fast_exp2(lp * LOG2E);
+      const float d = (c == target ? g : 0.f) - p * fmaf(hg, fmaxf(lp, -1.0e4f) + H, g);
+      return none ? 0.f : d;
+    };
+    if (end - begin == RUN) {
+      typename V::Raw r[UNROLL];
+#pragma unroll
+      for (int u = 0; u < UNROLL; ++u)
+        r[u] = *reinterpret_cast<const typename V::Raw*>(x + begin + (u * 256 + threadIdx.x) * V::N);
+#pragma unroll
+      for (int u = 0; u < UNROLL; ++u) {
+        const int32_t c = begin + (u * 256 + threadIdx.x) * V::N;
+        float f[V::N];
+        V::unpack(r[u], f);
+#pragma unroll
+        for (int e = 0; e < V::N; ++e) f[e] = gradient(f[e], c + e);
+        *reinterpret_cast<typename V::Raw*>(dx + c) = V::pack(f);
+      }
+    } else {
+      for (int32_t c = begin + threadIdx.x * V::N; c < end; c += 256 * V::N) {
+        if (c + V::N <= end) {
+          float f[V::N];
+          V::unpack(*reinterpret_cast<const typename V::Raw*>(x + c), f);
+#pragma unroll
+          for (int e = 0; e < V::N; ++e) f[e] = gradient(f[e], c + e);
+          *reinterpret_cast<typename V::Raw*>(dx + c) = V::pack(f);
+        } else {
+          for (int32_t e = c; e < end; ++e) dx[e] = hpd::from_float<T>(gradient(hpd::to_float(x[e]), e));
+        }
+      }
+    }
+  }
+}
+
+template <typename T>
+hipError_t launch(const hpd_logprobs_args& a, const hpd_logprobs_plan& p, hipStream_t s) {
+  const int64_t per = 4 / p.waves, items = (a.n_rows * p.parts + per - 1) / per;
+  const dim3 grid((unsigned)std::min(items, MAX_GRID));
+  if (a.top_k) logprobs_kernel<T, true><<<grid, 256, 0, s>>>(a, p.parts, p.span, p.waves);
+  else logprobs_kernel<T, false><<<grid, 256, 0, s>>>(a, p.parts, p.span, p.waves);
+  if (p.parts > 1) {
+    const dim3 rows((unsigned)std::min(a.n_rows, MAX_GRID));
+    if (a.top_k) logprobs_join_kernel<T, true><<<rows, 256, 0, s>>>(a, p.parts);
+    else logprobs_join_kernel<T, false><<<rows, 256, 0, s>>>(a, p.parts);
+  }
+  return hipGetLastError();
+}
+
+template <typename T>
+hipError_t launch_backward(const hpd_logprobs_backward_args& a, hipStream_t s) {
+  constexpr int32_t RUN = 256 * Vec<T>::N * UNROLL;
+  const int32_t pieces = (a.vocab + RUN - 1) / RUN;
+  logprobs_backward_kernel<T><<<dim3((unsigned)std::min(a.n_rows * pieces, MAX_GRID)), 256, 0, s>>>(a, pieces);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hpd_logprobs_plan hpd_plan_logprobs(int32_t dtype, int64_t n_rows, int32_t vocab) {
+  const int32_t n = dtype == HPD_F32 ? 4 : 8, run = 64 * n * UNROLL;  // logits that a wave takes at once
+  if (vocab <= 2 * run) return {1, vocab, 1};
+  // pieces of at least one turn of four waves, at most 64 (one per lane of the joining wave)
+  const int64_t want = std::min<int64_t>((1024 + n_rows - 1) / n_rows, std::min<int64_t>(64, (vocab + 4 * run - 1) / (4 * run)));
+  if (want <= 1) return {1, vocab, 4};
+  const int32_t span = (int32_t)(((vocab + want - 1) / want + run - 1) / run * run);
+  return {(vocab + span - 1) / span, span, 4};
+}
+
+int64_t hpd_logprobs_bytes(int32_t dtype, int64_t n_rows, int32_t vocab, int32_t top_k) {
+  const hpd_logprobs_plan p = hpd_plan_logprobs(dtype, n_rows, vocab);
+  return p.parts == 1 ? 0 : n_rows * p.parts * (16 + 8 * (int64_t)top_k);
+}
+
+hipError_t hpd_launch_logprobs(int32_t dtype, const hpd_logprobs_args& a, hipStream_t s) {
+  const hpd_logprobs_plan p = hpd_plan_logprobs(dtype, a.n_rows, a.vocab);
+  return dtype == HPD_F32 ? launch<float>(a, p, s) : launch<hpd::bf16_t>(a, p, s);
+}
+
+hipError_t hpd_launch_logprobs_backward(int32_t dtype, const hpd_logprobs_backward_args& a, hipStream_t s) {
+  return dtype == HPD_F32 ? launch_backward<float>(a, s) : launch_backward<hpd::bf16_t>(a, s);
+}
