@@ -10,13 +10,18 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libhpd.so")
 SOURCES = ["hpd_host.cpp", "hpd_kernels.hip", "hpd_attn_stream.hip", "hpd_attn_dense.hip", "hpd_attn_f32.hip", "hpd_peaks.hip",
-           "hpd_finetune_host.cpp", "hpd_finetune_attn.hip", "hpd_logprobs.hip"]
+           "hpd_finetune_host.cpp", "hpd_finetune_attn.hip", "hpd_finetune_stream.hip",
+           "hpd_logprobs.hip"]
 # packed fp32 instructions are switched off for all device code
 FLAGS = ["-O3", "-std=c++17", "-fPIC", "--offload-arch=gfx950", "-Wall", "-Wno-unused-function",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
          # the first arguments of a kernel are in registers when it starts: what its first lookup needs stands in front
          "-mllvm", "-amdgpu-kernarg-preload-count=8",
          "-I", os.path.join(ROOT, "include"), "-I", CSRC]
+
+# The compiler's own matrix instructions write vector registers there; accumulation registers are for the sums that the
+# gradient kernels place in them.
+EXTRA_FLAGS = {"hpd_finetune_stream.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"]}
 
 
 def build(verbose: bool = False) -> str:
@@ -25,7 +30,7 @@ def build(verbose: bool = False) -> str:
     procs = []
     for src in SOURCES:
         obj = os.path.join(CSRC, os.path.splitext(src)[0] + ".o")
-        cmd = [hipcc, *FLAGS, "-c", os.path.join(CSRC, src), "-o", obj]
+        cmd = [hipcc, *FLAGS, *EXTRA_FLAGS.get(src, []), "-c", os.path.join(CSRC, src), "-o", obj]
         if src.endswith(".cpp"):
             cmd.insert(1, "-x"), cmd.insert(2, "hip")
         procs.append((src, subprocess.Popen(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)))

@@ -15,18 +15,13 @@
 // left operand of the second products, whose right operand is the result of the first as it lies in
 // the registers: register r of a lane in half h of the wave holds row 8 (r / 4) + 4 h + r % 4 of the
 // lane's column, and the column reads take the rows in that order.
-#include "hpd_attn_bf16.h"
-#include "hpd_finetune.h"
+#include "hpd_finetune_dev.h"
 
 namespace {
 
 constexpr int ROWS = HPD_FT_ROWS;
 constexpr int BLK = HPD_FT_BLOCK;
 constexpr int WAVES = ROWS / 32;
-constexpr float LOG2E = 1.44269504088896340736f;
-constexpr float LN2 = 0.69314718055994530942f;
-
-typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
 
 // Operand layouts by element type.  A fragment is 16 bytes a lane: the chunk 2 * step + h of the row
 // of the lane (h = lane / 32).
@@ -98,15 +93,6 @@ struct Elem<float> {
   }
 };
 
-struct FtArgs {
-  const hpd_ft_tile* tiles;
-  const int32_t* rank;
-  const int2* blk_rank;
-  int64_t N, sq, sk, sv, sdq, sdk, sdv;  // tokens, elements between tokens
-  int32_t Hq, Hkv, D;
-  float scale;  // 1 / sqrt(D)
-};
-
 // Generic kernels: any D up to DP (zeros behind it), tiles through registers, one tile at a time.
 template <typename T, int DP>
 struct Tile {
@@ -162,15 +148,6 @@ struct Tile {
       }
   }
 };
-
-__device__ __forceinline__ void zero(floatx16* acc, int n) {
-#pragma unroll
-  for (int b = 0; b < n; ++b)
-#pragma unroll
-    for (int i = 0; i < 16; ++i) acc[b][i] = 0.f;
-}
-
-__device__ __forceinline__ int tile_row(int r, int h) { return 8 * (r / 4) + 4 * h + r % 4; }
 
 template <typename T, int DP>
 __global__ void __launch_bounds__(WAVES * 64) ft_forward_kernel(FtArgs a, const T* __restrict__ q, const T* __restrict__ k,
@@ -491,7 +468,7 @@ hipError_t rotate(const hpd_finetune_layout* L, float sign, const void* q, const
 }  // namespace
 
 int64_t hpd_ft_forward_bytes(const hpd_finetune_layout*) { return 0; }
-int64_t hpd_ft_backward_bytes(const hpd_finetune_layout* L) { return (int64_t)L->n_tokens * L->cfg.n_q_heads * 4; }
+int64_t hpd_ft_backward_bytes(const hpd_finetune_layout* L) { return (int64_t)L->n_tokens * L->cfg.n_q_heads * 8; }
 
 hipError_t hpd_launch_ft_rope_table(const hpd_finetune_layout* L, hipStream_t s) {
   const int32_t half = L->cfg.head_dim / 2;
@@ -512,6 +489,7 @@ hipError_t hpd_launch_ft_rotate(const hpd_finetune_layout* L, bool inverse, cons
 hipError_t hpd_launch_ft_attention(const hpd_finetune_layout* L, const void* q, const void* k, const void* v, void* out,
                                    float* lse, void*, const hpd_finetune_strides& st, hipStream_t s) {
   const FtArgs a = make_args(L, st);
+  if (hpd_ft_stream_supported(L)) return hpd_launch_ft_stream_forward(L, a, q, k, v, out, lse, s);
   if (L->cfg.dtype == HPD_F32)
     return a.D <= 64 ? forward<float, 64>(L, a, q, k, v, out, lse, s) : forward<float, 128>(L, a, q, k, v, out, lse, s);
   return a.D <= 64 ? forward<hpd::bf16_t, 64>(L, a, q, k, v, out, lse, s)
@@ -522,6 +500,8 @@ hipError_t hpd_launch_ft_attention_backward(const hpd_finetune_layout* L, const 
                                             const void* out, const float* lse, const void* d_out, void* dq, void* dk,
                                             void* dv, void* workspace, const hpd_finetune_strides& st, hipStream_t s) {
   const FtArgs a = make_args(L, st);
+  if (hpd_ft_stream_supported(L))
+    return hpd_launch_ft_stream_backward(L, a, q, k, v, out, lse, d_out, dq, dk, dv, workspace, s);
   float* delta = (float*)workspace;
   if (L->cfg.dtype == HPD_F32)
     return a.D <= 64 ? backward<float, 64>(L, a, q, k, v, out, lse, d_out, dq, dk, dv, delta, s)
