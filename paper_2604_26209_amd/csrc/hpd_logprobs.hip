@@ -7,7 +7,7 @@
 // same rule.  The pass is bound by the bytes of the logits.
 //
 // Alternatives: a wave keeps its 64 largest (value, index) keys, lane i the i-th.  A vector of logits
-// costs one comparison of its maximum with the last key that counts; what passes is inserted.
+// costs one comparison of its maximum with the K-th; what passes is collected and sorted in, 64 at a time.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -100,73 +100,116 @@ __device__ __forceinline__ float key_value(uint64_t k) {
   const uint32_t o = (uint32_t)(k >> 32);
   return __uint_as_float(o & 0x80000000u ? o & 0x7fffffffu : ~o);
 }
-__device__ __forceinline__ uint64_t shuffle(uint64_t k, int from) {
-  return ((uint64_t)(uint32_t)__shfl((int)(k >> 32), from) << 32) | (uint32_t)__shfl((int)(uint32_t)k, from);
+// the value of lane (own ^ M), without the LDS unit
+template <int M>
+__device__ __forceinline__ uint32_t lane_xor(uint32_t v, int lane) {
+  auto dpp = [](uint32_t x, auto control) __attribute__((always_inline)) -> uint32_t {
+    return (uint32_t)__builtin_amdgcn_mov_dpp((int)x, decltype(control)::value, 0xf, 0xf, true);
+  };
+  if constexpr (M == 1) return dpp(v, std::integral_constant<int, 0xB1>{});   // quad_perm 1 0 3 2
+  if constexpr (M == 2) return dpp(v, std::integral_constant<int, 0x4E>{});   // quad_perm 2 3 0 1
+  if constexpr (M == 4)                                                       // ^ 7 (half mirror), ^ 3 (quad_perm 3 2 1 0)
+    return dpp(dpp(v, std::integral_constant<int, 0x141>{}), std::integral_constant<int, 0x1B>{});
+  if constexpr (M == 8) return dpp(v, std::integral_constant<int, 0x128>{});  // rotation by 8 in rows of 16
+  if constexpr (M == 16) {
+    const auto p = __builtin_amdgcn_permlane16_swap(v, v, false, false);  // rows 0 0 2 2, rows 1 1 3 3
+    return lane & 16 ? p[0] : p[1];
+  }
+  if constexpr (M == 32) {
+    const auto p = __builtin_amdgcn_permlane32_swap(v, v, false, false);  // lower halves, upper halves
+    return lane & 32 ? p[0] : p[1];
+  }
+}
+template <int M>
+__device__ __forceinline__ uint64_t lane_xor(uint64_t k, int lane) {
+  return ((uint64_t)lane_xor<M>((uint32_t)(k >> 32), lane) << 32) | lane_xor<M>((uint32_t)k, lane);
 }
 __device__ __forceinline__ uint64_t read_lane(uint64_t k, int from) {
   return ((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(k >> 32), from) << 32) |
          (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)k, from);
 }
-__device__ __forceinline__ uint64_t larger(uint64_t a, uint64_t b) { return a > b ? a : b; }
-__device__ __forceinline__ uint64_t smaller(uint64_t a, uint64_t b) { return a > b ? b : a; }
+template <typename K>
+__device__ __forceinline__ K larger(K a, K b) { return a > b ? a : b; }
 
-// one stage of a bitonic network over the 64 lanes; up: the lane belongs to a run sorted upwards
-__device__ __forceinline__ uint64_t stage(uint64_t k, int distance, bool up, int lane) {
-  const uint64_t o = shuffle(k, lane ^ distance);
-  const bool low = (lane & distance) == 0;
-  return low != up ? larger(k, o) : smaller(k, o);
+// one stage of a bitonic network over the 64 lanes; UP: the lane bit that marks runs sorted upwards (64: none)
+template <int M, int UP, typename K>
+__device__ __forceinline__ K stage(K k, int lane) {
+  const K o = lane_xor<M>(k, lane);
+  const bool low = (lane & M) == 0, up = (lane & UP) != 0;
+  return (k > o) == (low != up) ? k : o;
+}
+template <int N, int M, typename K>
+__device__ __forceinline__ K stages(K k, int lane) {  // distances M, M / 2 .. 1 of runs of N
+  k = stage<M, N>(k, lane);
+  if constexpr (M > 1) k = stages<N, M / 2>(k, lane);
+  return k;
 }
 // a bitonic sequence sorted downwards
-__device__ __forceinline__ uint64_t settle(uint64_t k, int lane) {
-#pragma nounroll
-  for (int d = 32; d; d >>= 1) k = stage(k, d, false, lane);
+template <typename K>
+__device__ __forceinline__ K settle(K k, int lane) { return stages<64, 32>(k, lane); }
+template <int N = 2, typename K>
+__device__ __forceinline__ K sort_down(K k, int lane) {
+  k = stages<N, N / 2>(k, lane);
+  if constexpr (N < 64) k = sort_down<N * 2>(k, lane);
   return k;
-}
-__device__ __forceinline__ uint64_t sort_down(uint64_t k, int lane) {
-#pragma nounroll
-  for (int n = 2; n <= 64; n <<= 1)
-#pragma nounroll
-    for (int d = n >> 1; d; d >>= 1) k = stage(k, d, (lane & n) != 0, lane);
-  return k;
-}
-// the 64 largest of two lists sorted downwards
-__device__ __forceinline__ uint64_t merge(uint64_t a, uint64_t b, int lane) {
-  return settle(larger(a, shuffle(b, 63 - lane)), lane);
 }
 
+// The K largest keys of what a wave has seen: the sorted list, and a buffer of candidates in LDS that is
+// sorted into it when it is full.  Candidates are those above the K-th of the list as it was
+// then; the more logits have been seen, the rarer they are.
 struct Top {
   uint64_t list = 0;  // lane i: the i-th largest
-  uint64_t last = 0;  // the K-th, in every lane
-  float bar = 0.f;    // its value once there are K
+  uint64_t last = 0;  // what a candidate has to exceed, in every lane
+  float bar = 0.f;    // its value, once there is one
   bool full = false;
-  __device__ __forceinline__ void update(int K) {
-    last = read_lane(list, K - 1);
-    full = last != 0;
-    bar = key_value(last);
+  int count = 0;           // candidates in the buffer
+  uint64_t* buffer = nullptr;  // 128 keys of this wave
+  // (a wave's LDS accesses happen in order; what other lanes have written is behind the compiler's back)
+  static __device__ __forceinline__ void order() { asm volatile("" ::: "memory"); }
+  __device__ __forceinline__ void flush(int K, int lane) {
+    const int n = min(count, 64);
+    order();
+    uint64_t c = lane < n ? buffer[lane] : 0;
+    const uint64_t rest = lane + 64 < count ? buffer[lane + 64] : 0;
+    c = sort_down(c, lane);
+    order();
+    buffer[64 + lane] = c;  // turned around through LDS: the list and the candidates are one bitonic sequence
+    order();
+    list = settle(larger(list, buffer[64 + 63 - lane]), lane);
+    order();
+    buffer[lane] = rest;
+    count -= n;
+    const uint64_t k = read_lane(list, K - 1);
+    if (k > last) last = k;
+    if (k) {
+      full = true;
+      bar = key_value(last);
+    }
   }
-  // one candidate per lane
+  // one candidate per lane; 0: none
   __device__ __forceinline__ void add(uint64_t key, int K, int lane) {
-    uint64_t left = __ballot(key > last);
-    if (left == 0) return;
-    if (__popcll(left) > 6) {
-      list = merge(list, sort_down(key > last ? key : 0, lane), lane);
-      update(K);
-      return;
-    }
-    while (left) {
-      const uint64_t c = read_lane(key, __builtin_ctzll(left));
-      const int at = __popcll(__ballot(list > c));
-      const uint64_t above = shuffle(list, lane ? lane - 1 : 0);
-      list = lane < at ? list : lane == at ? c : above;
-      update(K);
-      left &= left - 1;
-      left &= __ballot(key > last);
-    }
+    const bool in = key > last;
+    const uint64_t mask = __ballot(in);
+    if (mask == 0) return;
+    if (in) buffer[count + __builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, 0))] = key;
+    count += __popcll(mask);
+    order();
+    if (count >= 64) flush(K, lane);
   }
+  // m: the largest logit of each lane's share of what comes next.  The K-th largest of these is reached by K logits.
+  __device__ __forceinline__ void expect(float m, int K, int lane) {
+    const uint32_t o = (uint32_t)(make_key(m, 0) >> 32);
+    const uint32_t k = (uint32_t)__builtin_amdgcn_readlane((int)sort_down(o, lane), K - 1);
+    last = ((uint64_t)k << 32) - 1;
+    bar = key_value((uint64_t)k << 32);
+    full = true;
+  }
+  // the largest of two sorted lists; other: in LDS
+  __device__ __forceinline__ void merge(const uint64_t* other, int lane) { list = settle(larger(list, other[63 - lane]), lane); }
 };
 
 struct Shared {
-  uint64_t list[4][64];
+  uint64_t keys[4][128];  // every wave's candidates, then its list
   Sums sums[4];
 };
 
@@ -200,7 +243,7 @@ __device__ __forceinline__ void scan(const T* x, int32_t begin, int32_t end, int
 #pragma unroll
     for (int e = 0; e < V::N; ++e) add_logit(sums, f[e]);
     if constexpr (TOP) {
-      if (__any(!top.full || m > top.bar)) {
+      if (__any(!top.full || m >= top.bar)) {
 #pragma unroll
         for (int e = 0; e < V::N; ++e) top.add(e < n ? make_key(f[e], index + e) : 0, K, lane);
       }
@@ -212,6 +255,19 @@ __device__ __forceinline__ void scan(const T* x, int32_t begin, int32_t end, int
     typename V::Raw r[UNROLL];
 #pragma unroll
     for (int u = 0; u < UNROLL; ++u) r[u] = *reinterpret_cast<const typename V::Raw*>(x + at + u * STEP + lane * V::N);
+    if constexpr (TOP) {
+      if (!top.full) {  // the first turn
+        float m = -INFINITY;
+#pragma unroll
+        for (int u = 0; u < UNROLL; ++u) {
+          float f[V::N];
+          V::unpack(r[u], f);
+#pragma unroll
+          for (int e = 0; e < V::N; ++e) m = fmaxf(m, f[e]);
+        }
+        top.expect(m, K, lane);
+      }
+    }
 #pragma unroll
     for (int u = 0; u < UNROLL; ++u) {
       float f[V::N];
@@ -240,6 +296,9 @@ __device__ __forceinline__ void scan(const T* x, int32_t begin, int32_t end, int
       take(f, index, end - index);
     }
   }
+  if constexpr (TOP) {
+    while (top.count) top.flush(K, lane);
+  }
 }
 
 template <typename T, bool TOP>
@@ -258,17 +317,18 @@ __global__ void __launch_bounds__(256) logprobs_kernel(hpd_logprobs_args a, int3
     const int32_t begin = part * span, end = min(begin + span, a.vocab);
     Sums sums;
     Top top;
+    top.buffer = sh.keys[wave];
     scan<T, TOP>(x, begin, end, waves == 1 ? 0 : wave, waves, K, lane, sums, top);
     sums = join_wave(sums);
     if (waves > 1) {
-      if (TOP) sh.list[wave][lane] = top.list;
+      if (TOP) sh.keys[wave][lane] = top.list;
       if (lane == 0) sh.sums[wave] = sums;
       __syncthreads();
       if (wave == 0) {
 #pragma unroll
         for (int w = 1; w < 4; ++w) {
           sums = join(sums, sh.sums[w]);
-          if (TOP) top.list = merge(top.list, sh.list[w][lane], lane);
+          if (TOP) top.merge(sh.keys[w], lane);
         }
       }
     }
@@ -301,10 +361,16 @@ __global__ void __launch_bounds__(256) logprobs_join_kernel(hpd_logprobs_args a,
       const float4 p = ws[row * parts + lane];
       sums = {p.x, p.y, p.z};
     }
-    uint64_t list = 0;
-    if constexpr (TOP) {
-      for (int32_t p = wave; p < parts; p += 4) list = merge(list, lane < K ? lists[(row * parts + p) * K + lane] : 0, lane);
-      sh.list[wave][lane] = list;
+    Top top;
+    top.buffer = sh.keys[wave];
+    if constexpr (TOP) {  // the wave's keys side by side
+      const int32_t n = (parts - wave + 3) / 4 * K;  // of the pieces wave, wave + 4 ..
+      for (int32_t i = 0; i < n; i += 64) {
+        const int32_t at = i + lane, piece = wave + at / K * 4;
+        top.add(at < n ? lists[(row * parts + piece) * K + at % K] : 0, K, lane);
+      }
+      while (top.count) top.flush(K, lane);
+      sh.keys[wave][lane] = top.list;
     }
     sums = join_wave(sums);
     if (lane == 0) sh.sums[wave] = sums;
@@ -313,12 +379,12 @@ __global__ void __launch_bounds__(256) logprobs_join_kernel(hpd_logprobs_args a,
 #pragma unroll
       for (int w = 1; w < 4; ++w) {
         sums = join(sums, sh.sums[w]);
-        if (TOP) list = merge(list, sh.list[w][lane], lane);
+        if (TOP) top.merge(sh.keys[w], lane);
       }
       const int32_t t = a.targets ? a.targets[row] : -1;
       const bool has = t >= 0 && t < a.vocab;
       const T* x = reinterpret_cast<const T*>(a.logits) + row * a.row_stride;
-      finish(a, row, sums, list, has ? hpd::to_float(x[t]) : 0.f, has, lane);
+      finish(a, row, sums, top.list, has ? hpd::to_float(x[t]) : 0.f, has, lane);
     }
     __syncthreads();
   }
