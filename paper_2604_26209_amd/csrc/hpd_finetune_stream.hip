@@ -301,34 +301,16 @@ __global__ void __launch_bounds__(256, 2) ft_stream_forward_kernel(FtArgs a, con
 // ---------------------------------------------------------------------------------------
 // Gradients.  stat: per (head, token) -lse * sqrt(D), where its row's score products start, then -delta,
 // delta_i = do_i . o_i, where its row's products with v start: p = exp((q . k - lse sqrt(D)) / sqrt(D)).
+// The dq kernel, which runs first, makes them.
 // ---------------------------------------------------------------------------------------
-__global__ void __launch_bounds__(256) ft_stat_kernel(int64_t N, int32_t Hq, int32_t D, float root, const uint16_t* __restrict__ out,
-                                                      const uint16_t* __restrict__ d_out, const float* __restrict__ lse,
-                                                      float* __restrict__ stat) {
-  const int32_t lanes = D / 8;  // of a row: 8 or 16
-  const int64_t row = ((int64_t)blockIdx.x * 256 + threadIdx.x) / lanes;
-  if (row >= N * Hq) return;
-  const int32_t c = threadIdx.x % lanes * 8;
-  float x[8], y[8], s = 0.f;
-  unpack8(*reinterpret_cast<const uint4*>(out + row * D + c), x);
-  unpack8(*reinterpret_cast<const uint4*>(d_out + row * D + c), y);
-#pragma unroll
-  for (int e = 0; e < 8; ++e) s = fmaf(x[e], y[e], s);
-  for (int d = lanes / 2; d; d >>= 1) s += __shfl_xor(s, d);
-  if (c == 0) {
-    const int64_t at = row % Hq * N + row / Hq;
-    stat[at] = -root * lse[at];
-    stat[N * Hq + at] = -s;
-  }
-}
-
 // dq: two waves of 64 queries of one head, the wave's queries as two columns of results that share every
 // operand from LDS; rounds of 32 keys, four in LDS.
 template <int D>
 __global__ void __launch_bounds__(128, 1) ft_stream_dq_kernel(FtArgs a, const uint16_t* __restrict__ q,
                                                              const uint16_t* __restrict__ k, const uint16_t* __restrict__ v,
-                                                             const uint16_t* __restrict__ d_out,
-                                                             const float* __restrict__ stat, uint16_t* __restrict__ dq) {
+                                                             const uint16_t* __restrict__ out, const uint16_t* __restrict__ d_out,
+                                                             const float* __restrict__ lse, float* __restrict__ stat,
+                                                             uint16_t* __restrict__ dq) {
   using R = Rows<D>;
   constexpr int STAGE = 2 * R::TILE, SLOTS = 4, LOADS = R::TILE / 1024;
   __shared__ __attribute__((aligned(1024))) char ring[SLOTS * STAGE];
@@ -358,19 +340,35 @@ __global__ void __launch_bounds__(128, 1) ft_stream_dq_kernel(FtArgs a, const ui
   bf16x8 qf[2][R::STEPS], of[2][R::STEPS];
   float nl[2], nd[2];
   int32_t ic[2], rank_i[2];
+  const float root = 1.f / a.scale;
 #pragma unroll
   for (int x = 0; x < 2; ++x) {
     ic[x] = min(q_first + 32 * x + n, t.len - 1);
     const int64_t token = t.seq0 + (int64_t)ic[x];
     const uint16_t* qrow = q + token * a.sq + hq * D + h * 8;
-    const uint16_t* orow = d_out + (token * a.Hq + hq) * D + h * 8;
+    const int64_t orow = (token * a.Hq + hq) * D + h * 8;
+    bf16x8 o[R::STEPS];
 #pragma unroll
     for (int s = 0; s < R::STEPS; ++s) {
       qf[x][s] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const uint4*>(qrow + s * 16));
-      of[x][s] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const uint4*>(orow + s * 16));
+      of[x][s] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const uint4*>(d_out + orow + s * 16));
+      o[s] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const uint4*>(out + orow + s * 16));
     }
-    nl[x] = stat[hq * a.N + token];
-    nd[x] = stat[(a.Hq + hq) * a.N + token];
+    nl[x] = -root * lse[hq * a.N + token];
+    float delta = 0.f;
+#pragma unroll
+    for (int s = 0; s < R::STEPS; ++s) {
+      float y[8], z[8];
+      unpack8(__builtin_bit_cast(uint4, of[x][s]), y);
+      unpack8(__builtin_bit_cast(uint4, o[s]), z);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) delta = fmaf(y[e], z[e], delta);
+    }
+    nd[x] = -(delta + __shfl_xor(delta, 32));
+    if (h == 0 && q_first + 32 * x + n < t.len) {
+      stat[hq * a.N + token] = nl[x];
+      stat[(a.Hq + hq) * a.N + token] = nd[x];
+    }
     rank_i[x] = a.rank[token];
   }
   arrived(qf[0]);
@@ -709,9 +707,8 @@ template <int D>
 hipError_t backward(const hpd_finetune_layout* L, FtArgs a, const uint16_t* q, const uint16_t* k, const uint16_t* v,
                     const uint16_t* out, const float* lse, const uint16_t* d_out, uint16_t* dq, uint16_t* dk, uint16_t* dv,
                     float* stat, hipStream_t s) {
-  ft_stat_kernel<<<dim3((unsigned)((a.N * a.Hq * (D / 8) + 255) / 256)), 256, 0, s>>>(a.N, a.Hq, D, sqrtf((float)D), out, d_out, lse, stat);
   const unsigned tiles = (unsigned)L->tiles.size();
-  ft_stream_dq_kernel<D><<<dim3(tiles * a.Hq), 128, 0, s>>>(a, q, k, v, d_out, stat, dq);
+  ft_stream_dq_kernel<D><<<dim3(tiles * a.Hq), 128, 0, s>>>(a, q, k, v, out, d_out, lse, stat, dq);
   a.tiles = L->d_key_tiles;
   ft_stream_dkv_kernel<D><<<dim3(tiles * a.Hkv), 128, 0, s>>>(a, q, k, v, d_out, stat, dk, dv);
   return hipGetLastError();
