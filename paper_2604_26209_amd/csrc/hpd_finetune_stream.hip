@@ -11,6 +11,7 @@
 
 namespace {
 
+typedef uint32_t uint4v __attribute__((ext_vector_type(4)));
 constexpr uint32_t BIAS = 4096;  // keeps a lane's offset positive (see Loader)
 
 __device__ __forceinline__ void wait_lds_and_barrier() {
@@ -110,6 +111,13 @@ __device__ __forceinline__ uint32_t lds_address(const void* p) {
 __device__ __forceinline__ bf16x8 lds_rows(const char* p) {
   return __builtin_bit_cast(bf16x8, *reinterpret_cast<const uint4*>(p));
 }
+// the same by LDS address
+__device__ __forceinline__ bf16x8 lds_read(uint32_t at) {
+  return __builtin_bit_cast(bf16x8, *(const __attribute__((address_space(3))) uint4v*)(uintptr_t)at);
+}
+__device__ __forceinline__ uint2 lds_read_tr(uint32_t at) {
+  return __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) hpd::short4v*)(uintptr_t)at));
+}
 template <int D>
 __device__ __forceinline__ bf16x8 lds_columns(const char* tile, uint32_t col, int b, int k) {
   using R = Rows<D>;
@@ -179,31 +187,52 @@ __device__ __forceinline__ void store_rows(char* turn, const floatx16* acc, floa
 }
 
 // ---------------------------------------------------------------------------------------
-// Forward.  Four waves of 32 queries of one head; rounds of 64 keys, two rounds in LDS.
+// Forward and dq: four waves of 32 queries of one head; rounds of 64 keys, two rounds in LDS.
 // ---------------------------------------------------------------------------------------
 template <int D>
-__global__ void __launch_bounds__(256, 2) ft_stream_forward_kernel(FtArgs a, const uint16_t* __restrict__ q,
-                                                                  const uint16_t* __restrict__ k,
-                                                                  const uint16_t* __restrict__ v, uint16_t* __restrict__ out,
-                                                                  float* __restrict__ lse) {
+struct QueryTile {
   using R = Rows<D>;
-  constexpr int STAGE = 4 * R::TILE;  // 64 rows of k, 64 rows of v
-  __shared__ __attribute__((aligned(1024))) char ring[2 * STAGE];
-  const int lane = threadIdx.x & 63, n = lane & 31, h = lane >> 5;
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  // workgroup b runs on XCD b % 8: the query tiles and heads that read the same keys stay together
-  const int32_t G = a.Hq / a.Hkv, hk = blockIdx.x % a.Hkv, rest = blockIdx.x / a.Hkv, hq = hk * G + rest % G;
-  const hpd_ft_tile t = a.tiles[rest / G];
-  const int32_t q_first = t.row0 + wave * 32, i = q_first + n, ic = min(i, t.len - 1);
-  const bool active = q_first < t.len;
-  const int64_t token = t.seq0 + (int64_t)ic;
-
-  // this wave's part of a round: waves 0 and 1 keys, 2 and 3 values
+  static constexpr int STAGE = 4 * R::TILE;  // 64 rows of k, 64 rows of v
+  const FtArgs& a;
+  hpd_ft_tile t;
+  int lane, n, h, wave;
+  int32_t hq, hk, q_first, i, ic, rounds;
+  int64_t token;
+  bool active;
+  int32_t q_min, q_max;  // ranks of the wave's queries
+  const int32_t* ranks;
+  const const_i32* blk_rank;
   Loader<D> loader;
-  loader.init(wave < 2 ? a.sk : a.sv, lane);
-  const char* const src = reinterpret_cast<const char*>(wave < 2 ? k + t.seq0 * a.sk : v + t.seq0 * a.sv) + (int64_t)hk * D * 2;
-  const uint32_t ring_lds = lds_address(ring);
-  auto issue = [&](int32_t round) {
+  const char* src;
+  uint32_t ring_lds;
+
+  __device__ __forceinline__ QueryTile(const FtArgs& args, const uint16_t* k, const uint16_t* v, const char* ring) : a(args) {
+    lane = threadIdx.x & 63;
+    n = lane & 31;
+    h = lane >> 5;
+    wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    // workgroup b runs on XCD b % 8: the query tiles and heads that read the same keys stay together
+    const int32_t G = a.Hq / a.Hkv, rest = blockIdx.x / a.Hkv;
+    hk = blockIdx.x % a.Hkv;
+    hq = hk * G + rest % G;
+    t = a.tiles[rest / G];
+    q_first = t.row0 + wave * 32;
+    i = q_first + n;
+    ic = min(i, t.len - 1);
+    active = q_first < t.len;
+    token = t.seq0 + (int64_t)ic;
+    rounds = (min(t.row0 + 128, t.len) + 63) / 64;
+    // this wave's part of a round: waves 0 and 1 keys, 2 and 3 values
+    loader.init(wave < 2 ? a.sk : a.sv, lane);
+    src = reinterpret_cast<const char*>(wave < 2 ? k + t.seq0 * a.sk : v + t.seq0 * a.sv) + (int64_t)hk * D * 2;
+    ring_lds = lds_address(ring);
+    ranks = a.rank + t.seq0;
+    blk_rank = (const const_i32*)(uintptr_t)(a.blk_rank + t.blk0);
+    const int32_t own = min(q_first, t.len - 1) / 32;
+    q_min = blk_rank[2 * own];
+    q_max = blk_rank[2 * own + 1];
+  }
+  __device__ __forceinline__ void issue(int32_t round) const {
     const uint32_t dst = ring_lds + (round & 1) * STAGE + (wave >> 1) * 2 * R::TILE;
 #pragma unroll
     for (int j = 0; j < 32 / R::GROUP; ++j) {
@@ -211,40 +240,76 @@ __global__ void __launch_bounds__(256, 2) ft_stream_forward_kernel(FtArgs a, con
       const int32_t first = min(round * 64 + row, t.len - 1);
       loader.load(src + first * loader.stride, dst + row * R::RB, t.len - 1 - first, lane);
     }
-  };
-  const int32_t rounds = (min(t.row0 + 128, t.len) + 63) / 64;
-  issue(0);
-  bf16x8 qf[R::STEPS];
-  {
-    const uint16_t* row = q + token * a.sq + hq * D + h * 8;
-#pragma unroll
-    for (int s = 0; s < R::STEPS; ++s) qf[s] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const uint4*>(row + s * 16));
   }
-  int32_t rank_i[1] = {a.rank[token]};
+  static __device__ __forceinline__ void own_row(const uint16_t* row, bf16x8* f) {
+#pragma unroll
+    for (int s = 0; s < R::STEPS; ++s) f[s] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const uint4*>(row + s * 16));
+  }
+  // block b of 32 keys has a key that a query of the wave sees / one that a query does not see
+  __device__ __forceinline__ bool reaches(int32_t b) const { return active && b * 32 <= q_first && blk_rank[2 * b] <= q_max; }
+  __device__ __forceinline__ bool masked(int32_t b) const { return b * 32 == q_first || blk_rank[2 * b + 1] > q_min; }
+  __device__ __forceinline__ void mask(floatx16& s, int32_t b, int32_t rank_i) const {
+    BlockRanks rk;
+    rk.load(ranks + b * 32);
+#pragma unroll
+    for (int r = 0; r < 16; ++r) s[r] = b * 32 + tile_row(r, h) <= ic && rk.of(r, h) <= rank_i ? s[r] : -INFINITY;
+  }
+};
+
+// LDS addresses of a lane's operands in the first tile of a stage
+template <int D>
+struct Addresses {
+  using R = Rows<D>;
+  uint32_t row[R::STEPS], col[2 * R::BLOCKS];
+  __device__ __forceinline__ Addresses(uint32_t base, int lane) {
+#pragma unroll
+    for (int s = 0; s < R::STEPS; ++s) row[s] = base + (R::row_offset(lane & 31, lane >> 5) ^ (s << 5));
+#pragma unroll
+    for (int c = 0; c < 2 * R::BLOCKS; ++c) col[c] = base + (R::column_offset(lane) ^ (c >> 1 << 6) ^ ((c & 1) << 5));
+  }
+  // to the other stage (base is a multiple of 2 * stage)
+  __device__ __forceinline__ void flip(uint32_t stage) {
+#pragma unroll
+    for (int s = 0; s < R::STEPS; ++s) row[s] ^= stage;
+#pragma unroll
+    for (int c = 0; c < 2 * R::BLOCKS; ++c) col[c] ^= stage;
+  }
+  __device__ __forceinline__ bf16x8 rows(int s, int at) const { return lds_read(row[s] + at); }
+  __device__ __forceinline__ bf16x8 columns(int b, int k, int at) const {
+    const uint2 lo = lds_read_tr(col[2 * b] + at + 16 * k * R::RB);
+    const uint2 hi = lds_read_tr(col[2 * b + 1] + at + (16 * k + 8) * R::RB);
+    return __builtin_bit_cast(bf16x8, make_uint4(lo.x, lo.y, hi.x, hi.y));
+  }
+};
+
+template <int D>
+__global__ void __launch_bounds__(256, 2) ft_stream_forward_kernel(FtArgs a, const uint16_t* __restrict__ q,
+                                                                  const uint16_t* __restrict__ k,
+                                                                  const uint16_t* __restrict__ v, uint16_t* __restrict__ out,
+                                                                  float* __restrict__ lse) {
+  using R = Rows<D>;
+  using Q = QueryTile<D>;
+  __shared__ __attribute__((aligned(2 * Q::STAGE))) char ring[2 * Q::STAGE];
+  const Q w(a, k, v, ring);
+  w.issue(0);
+  bf16x8 qf[R::STEPS];
+  Q::own_row(q + w.token * a.sq + w.hq * D + w.h * 8, qf);
+  int32_t rank_i[1] = {a.rank[w.token]};
   arrived(qf);
   arrived(rank_i);
-  const int32_t* const ranks = a.rank + t.seq0;
-  const const_i32* const blk_rank = (const const_i32*)(uintptr_t)(a.blk_rank + t.blk0);
-  const int32_t own_blk = min(q_first, t.len - 1) / 32;
-  const int32_t q_min = blk_rank[2 * own_blk], q_max = blk_rank[2 * own_blk + 1];
   const float c = a.scale * LOG2E;
-  const uint32_t row_at = R::row_offset(n, h), col_at = R::column_offset(lane);
+  Addresses<D> at(w.ring_lds, w.lane);
 
   floatx16 acc[R::BLOCKS];
   zero(acc, R::BLOCKS);
   float m = NEG_BIG, l = 0.f;  // reference point (log2 units; within 2^8 of the maximum) and this lane's share of the sum
 
   // one block of 32 keys
-  auto block = [&](const char* tk, const char* tv, int32_t b, bool masked) __attribute__((always_inline)) {
+  auto block = [&](int kt, int vt, int32_t b) __attribute__((always_inline)) {
     floatx16 s = {};
-    if (masked) {  // what is hidden starts at -infinity and stays there
-      BlockRanks rk;
-      rk.load(ranks + b * 32);
 #pragma unroll
-      for (int r = 0; r < 16; ++r) s[r] = b * 32 + tile_row(r, h) <= ic && rk.of(r, h) <= rank_i[0] ? 0.f : -INFINITY;
-    }
-#pragma unroll
-    for (int x = 0; x < R::STEPS; ++x) s = mfma(lds_rows(tk + (row_at ^ (x << 5))), qf[x], s);
+    for (int x = 0; x < R::STEPS; ++x) s = mfma(at.rows(x, kt), qf[x], s);
+    if (w.masked(b)) w.mask(s, b, rank_i[0]);
     float top = s[0];
 #pragma unroll
     for (int r = 1; r < 16; ++r) top = fmaxf(top, s[r]);
@@ -272,221 +337,104 @@ __global__ void __launch_bounds__(256, 2) ft_stream_forward_kernel(FtArgs a, con
     const bf16x8 p0 = pack8(p), p1 = pack8(p + 8);
 #pragma unroll
     for (int x = 0; x < R::BLOCKS; ++x) {
-      acc[x] = mfma(lds_columns<D>(tv, col_at, x, 0), p0, acc[x]);
-      acc[x] = mfma(lds_columns<D>(tv, col_at, x, 1), p1, acc[x]);
+      acc[x] = mfma(at.columns(x, 0, vt), p0, acc[x]);
+      acc[x] = mfma(at.columns(x, 1, vt), p1, acc[x]);
     }
   };
-  for (int32_t round = 0; round < rounds; ++round) {
+  for (int32_t round = 0; round < w.rounds; ++round) {
     wait_vector_memory<0>();
     wait_lds_and_barrier();  // the round is in LDS, the other half of the ring is free
-    if (round + 1 < rounds) issue(round + 1);
-    const char* const tk = ring + (round & 1) * STAGE;
-#pragma unroll
-    for (int j = 0; j < 2; ++j) {
-      const int32_t b = 2 * round + j;
-      if (!active || b * 32 > q_first) continue;  // (behind the wave's own rows)
-      const int32_t k_min = blk_rank[2 * b], k_max = blk_rank[2 * b + 1];
-      if (k_min > q_max) continue;
-      block(tk + j * R::TILE, tk + (2 + j) * R::TILE, b, b * 32 == q_first || k_max > q_min);
-    }
+    if (round + 1 < w.rounds) w.issue(round + 1);
+    if (w.reaches(2 * round)) block(0, 2 * R::TILE, 2 * round);
+    if (w.reaches(2 * round + 1)) block(R::TILE, 3 * R::TILE, 2 * round + 1);
+    at.flip(Q::STAGE);
   }
   wait_lds_and_barrier();
-  if (!active) return;
+  if (!w.active) return;
   l += __shfl_xor(l, 32);
-  if (h == 0 && i < t.len) lse[hq * a.N + token] = (m + __builtin_amdgcn_logf(l)) * LN2;
-  store_rows<D>(ring + wave * R::TILE, acc, 1.f / l, out + ((t.seq0 + (int64_t)q_first) * a.Hq + hq) * D, (int64_t)a.Hq * D,
-                t.len - q_first, lane);
+  if (w.h == 0 && w.i < w.t.len) lse[w.hq * a.N + w.token] = (m + __builtin_amdgcn_logf(l)) * LN2;
+  store_rows<D>(ring + w.wave * R::TILE, acc, 1.f / l, out + ((w.t.seq0 + (int64_t)w.q_first) * a.Hq + w.hq) * D,
+                (int64_t)a.Hq * D, w.t.len - w.q_first, w.lane);
 }
 
-// ---------------------------------------------------------------------------------------
-// Gradients.  stat: per (head, token) -lse * sqrt(D), where its row's score products start, then -delta,
-// delta_i = do_i . o_i, where its row's products with v start: p = exp((q . k - lse sqrt(D)) / sqrt(D)).
-// The dq kernel, which runs first, makes them.
-// ---------------------------------------------------------------------------------------
-// dq: two waves of 64 queries of one head, the wave's queries as two columns of results that share every
-// operand from LDS; rounds of 32 keys, four in LDS.
+// stat, which this kernel makes and the dk/dv kernel reads: per (head, token) -lse * sqrt(D), where its row's score
+// products start, then -delta, delta_i = do_i . o_i, where its row's products with v start:
+// p = exp((q . k - lse sqrt(D)) / sqrt(D)).
 template <int D>
-__global__ void __launch_bounds__(128, 1) ft_stream_dq_kernel(FtArgs a, const uint16_t* __restrict__ q,
+__global__ void __launch_bounds__(256, 2) ft_stream_dq_kernel(FtArgs a, const uint16_t* __restrict__ q,
                                                              const uint16_t* __restrict__ k, const uint16_t* __restrict__ v,
                                                              const uint16_t* __restrict__ out, const uint16_t* __restrict__ d_out,
                                                              const float* __restrict__ lse, float* __restrict__ stat,
                                                              uint16_t* __restrict__ dq) {
   using R = Rows<D>;
-  constexpr int STAGE = 2 * R::TILE, SLOTS = 4, LOADS = R::TILE / 1024;
-  __shared__ __attribute__((aligned(1024))) char ring[SLOTS * STAGE];
-  const int lane = threadIdx.x & 63, n = lane & 31, h = lane >> 5;
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int32_t G = a.Hq / a.Hkv, hk = blockIdx.x % a.Hkv, rest = blockIdx.x / a.Hkv, hq = hk * G + rest % G;
-  const hpd_ft_tile t = a.tiles[rest / G];
-  const int32_t q_first = t.row0 + wave * 64;
-  const bool active = q_first < t.len;
-
-  Loader<D> loader;
-  loader.init(wave == 0 ? a.sk : a.sv, lane);
-  const char* const src = reinterpret_cast<const char*>(wave == 0 ? k + t.seq0 * a.sk : v + t.seq0 * a.sv) + (int64_t)hk * D * 2;
-  const uint32_t ring_lds = lds_address(ring);
-  auto issue = [&](int32_t round) {
-    const uint32_t dst = ring_lds + (round & (SLOTS - 1)) * STAGE + wave * R::TILE;
-#pragma unroll
-    for (int j = 0; j < 32 / R::GROUP; ++j) {
-      const int32_t first = min(round * 32 + j * R::GROUP, t.len - 1);
-      loader.load(src + first * loader.stride, dst + j * R::GROUP * R::RB, t.len - 1 - first, lane);
-    }
-  };
-  const int32_t rounds = (min(t.row0 + 128, t.len) + 31) / 32;
-  issue(0);
-  if (rounds > 1) issue(1);
-  if (rounds > 2) issue(2);
-  bf16x8 qf[2][R::STEPS], of[2][R::STEPS];
-  float nl[2], nd[2];
-  int32_t ic[2], rank_i[2];
-  const float root = 1.f / a.scale;
-#pragma unroll
-  for (int x = 0; x < 2; ++x) {
-    ic[x] = min(q_first + 32 * x + n, t.len - 1);
-    const int64_t token = t.seq0 + (int64_t)ic[x];
-    const uint16_t* qrow = q + token * a.sq + hq * D + h * 8;
-    const int64_t orow = (token * a.Hq + hq) * D + h * 8;
+  using Q = QueryTile<D>;
+  __shared__ __attribute__((aligned(2 * Q::STAGE))) char ring[2 * Q::STAGE];
+  const Q w(a, k, v, ring);
+  w.issue(0);
+  bf16x8 qf[R::STEPS], of[R::STEPS];
+  float nl[1], nd[1];
+  {
     bf16x8 o[R::STEPS];
-#pragma unroll
-    for (int s = 0; s < R::STEPS; ++s) {
-      qf[x][s] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const uint4*>(qrow + s * 16));
-      of[x][s] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const uint4*>(d_out + orow + s * 16));
-      o[s] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const uint4*>(out + orow + s * 16));
-    }
-    nl[x] = -root * lse[hq * a.N + token];
+    const int64_t row = (w.token * a.Hq + w.hq) * D + w.h * 8;
+    Q::own_row(q + w.token * a.sq + w.hq * D + w.h * 8, qf);
+    Q::own_row(d_out + row, of);
+    Q::own_row(out + row, o);
+    const float minus_lse = -lse[w.hq * a.N + w.token];
     float delta = 0.f;
 #pragma unroll
     for (int s = 0; s < R::STEPS; ++s) {
       float y[8], z[8];
-      unpack8(__builtin_bit_cast(uint4, of[x][s]), y);
+      unpack8(__builtin_bit_cast(uint4, of[s]), y);
       unpack8(__builtin_bit_cast(uint4, o[s]), z);
 #pragma unroll
       for (int e = 0; e < 8; ++e) delta = fmaf(y[e], z[e], delta);
     }
-    nd[x] = -(delta + __shfl_xor(delta, 32));
-    if (h == 0 && q_first + 32 * x + n < t.len) {
-      stat[hq * a.N + token] = nl[x];
-      stat[(a.Hq + hq) * a.N + token] = nd[x];
+    nd[0] = -(delta + __shfl_xor(delta, 32));
+    nl[0] = LOG2E * minus_lse;
+    if (w.h == 0 && w.i < w.t.len) {
+      stat[w.hq * a.N + w.token] = minus_lse / a.scale;
+      stat[(a.Hq + w.hq) * a.N + w.token] = nd[0];
     }
-    rank_i[x] = a.rank[token];
   }
-  arrived(qf[0]);
-  arrived(qf[1]);
-  arrived(of[0]);
-  arrived(of[1]);
+  int32_t rank_i[1] = {a.rank[w.token]};
+  arrived(qf);
+  arrived(of);
   arrived(nl);
   arrived(nd);
   arrived(rank_i);
-  const int32_t* const ranks = a.rank + t.seq0;
-  const const_i32* const blk_rank = (const const_i32*)(uintptr_t)(a.blk_rank + t.blk0);
-  const int32_t b0 = min(q_first, t.len - 1) / 32, b1 = min(q_first + 32, t.len - 1) / 32;
-  const int32_t q_min = min(blk_rank[2 * b0], blk_rank[2 * b1]), q_max = max(blk_rank[2 * b0 + 1], blk_rank[2 * b1 + 1]);
   const float c = a.scale * LOG2E;
-  const uint32_t row_at = R::row_offset(n, h), col_at = R::column_offset(lane);
-
-  floatx16 acc[2][R::BLOCKS];
-  zero(acc[0], R::BLOCKS);
-  zero(acc[1], R::BLOCKS);
-  hold<R::BLOCKS>(acc[0]);
-  hold<R::BLOCKS>(acc[1]);
-  // The scores of the two columns one after the other (both at once do not fit the registers), each
-  // while the other's exponentials run.  One operand from LDS is requested two products ahead; the schedule is
-  // kept as written.
-  auto block = [&](const char* tk, const char* tv, int32_t b, bool masked) __attribute__((always_inline)) {
-    uint32_t rows = row_at, cols = col_at;
-    asm volatile("" : "+v"(rows), "+v"(cols));  // (the addresses made from them are not kept for the next round: they are 16 registers)
-    constexpr int S = R::STEPS, C = 2 * R::BLOCKS;  // operands: rows of k, v, k, v (S each), columns of k
-    // where a score starts: hidden ones at -infinity, where they stay (weight 0)
-    auto start = [&](int x) __attribute__((always_inline)) {
-      floatx16 v;
+  Addresses<D> at(w.ring_lds, w.lane);
+  floatx16 acc[R::BLOCKS];
+  zero(acc, R::BLOCKS);
+  auto block = [&](int kt, int vt, int32_t b) __attribute__((always_inline)) {
+    floatx16 s = {}, dp = {};
 #pragma unroll
-      for (int r = 0; r < 16; ++r) v[r] = nl[x];
-      if (masked) {
-        BlockRanks rk;
-        rk.load(ranks + b * 32);
+    for (int x = 0; x < R::STEPS; ++x) s = mfma(at.rows(x, kt), qf[x], s);
 #pragma unroll
-        for (int r = 0; r < 16; ++r) v[r] = b * 32 + tile_row(r, h) <= ic[x] && rk.of(r, h) <= rank_i[x] ? v[r] : -INFINITY;
-      }
-      return v;
-    };
-    auto ld = [&](int i) __attribute__((always_inline)) -> bf16x8 {
-      if (i < 4 * S) return lds_rows(((i / S) & 1 ? tv : tk) + (rows ^ ((i % S) << 5)));
-      i -= 4 * S;
-      return lds_columns<D>(tk, cols, i / 2, i % 2);
-    };
-    bf16x8 f[3], ds[2][2];
-    floatx16 s, dp;
-    auto weight = [&](int r) __attribute__((always_inline)) { s[r] = fast_exp2(s[r] * c); };
-    auto pack_half = [&](int x, int z) __attribute__((always_inline)) {
-      float e[8];
+    for (int x = 0; x < R::STEPS; ++x) dp = mfma(at.rows(x, vt), of[x], dp);
+    if (w.masked(b)) w.mask(s, b, rank_i[0]);
+    float e[16];
 #pragma unroll
-      for (int r = 0; r < 8; ++r) {
-        e[r] = s[8 * z + r] * dp[8 * z + r];
-      }
-      ds[x][z] = pack8(e);
-    };
-    f[0] = ld(0);
-    f[1] = ld(1);
+    for (int r = 0; r < 16; ++r) e[r] = fast_exp2(fmaf(s[r], c, nl[0])) * (dp[r] + nd[0]);
+    const bf16x8 d0 = pack8(e), d1 = pack8(e + 8);
 #pragma unroll
-    for (int x = 0; x < 2; ++x) {
-      floatx16 next = start(x);
-#pragma unroll
-      for (int i = 0; i < S; ++i) {
-        const int at = 2 * x * S + i;
-        f[(at + 2) % 3] = ld(at + 2);
-        next = mfma(f[at % 3], qf[x][i], next);
-        if (x == 1 && i == S / 2 - 1) pack_half(0, 0);
-        if (x == 1 && i == S - 1) pack_half(0, 1);
-        __builtin_amdgcn_sched_barrier(0);
-      }
-      s = next;
-#pragma unroll
-      for (int r = 0; r < 16; ++r) dp[r] = nd[x];
-#pragma unroll
-      for (int i = 0; i < S; ++i) {
-        const int at = (2 * x + 1) * S + i;
-        f[(at + 2) % 3] = ld(at + 2);
-        dp = mfma(f[at % 3], of[x][i], dp);
-#pragma unroll
-        for (int r = 16 * (i - 1) / (S - 1); i > 0 && r < 16 * i / (S - 1); ++r) weight(r);
-        __builtin_amdgcn_sched_barrier(0);
-      }
-    }
-    pack_half(1, 0);
-    pack_half(1, 1);
-    __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-    for (int i = 0; i < C; ++i) {
-      const int at = 4 * S + i;
-      if (i + 2 < C) f[(at + 2) % 3] = ld(at + 2);
-      add_product(f[at % 3], ds[0][i % 2], acc[0][i / 2]);
-      add_product(f[at % 3], ds[1][i % 2], acc[1][i / 2]);
-      __builtin_amdgcn_sched_barrier(0);
+    for (int x = 0; x < R::BLOCKS; ++x) {
+      acc[x] = mfma(at.columns(x, 0, kt), d0, acc[x]);
+      acc[x] = mfma(at.columns(x, 1, kt), d1, acc[x]);
     }
   };
-  for (int32_t round = 0; round < rounds; ++round) {
-    const int32_t ahead = rounds - 1 - round;  // rounds requested after this one: at most 2
-    if (ahead >= 2) wait_vector_memory<2 * LOADS>();
-    else if (ahead == 1) wait_vector_memory<LOADS>();
-    else wait_vector_memory<0>();
+  for (int32_t round = 0; round < w.rounds; ++round) {
+    wait_vector_memory<0>();
     wait_lds_and_barrier();
-    if (round + 3 < rounds) issue(round + 3);
-    if (!active || round * 32 > q_first + 63) continue;
-    const int32_t k_min = blk_rank[2 * round], k_max = blk_rank[2 * round + 1];
-    if (k_min > q_max) continue;
-    const char* const tk = ring + (round & (SLOTS - 1)) * STAGE;
-    block(tk, tk + R::TILE, round, round * 32 + 31 > q_first || k_max > q_min);
+    if (round + 1 < w.rounds) w.issue(round + 1);
+    if (w.reaches(2 * round)) block(0, 2 * R::TILE, 2 * round);
+    if (w.reaches(2 * round + 1)) block(R::TILE, 3 * R::TILE, 2 * round + 1);
+    at.flip(Q::STAGE);
   }
-  settle();
-  hold<R::BLOCKS>(acc[0]);
-  hold<R::BLOCKS>(acc[1]);
   wait_lds_and_barrier();
-  if (!active) return;
-#pragma unroll
-  for (int x = 0; x < 2; ++x)
-    store_rows<D>(ring + wave * R::TILE, acc[x], a.scale,
-                  dq + (t.seq0 + (int64_t)q_first + 32 * x) * a.sdq + hq * D, a.sdq, t.len - q_first - 32 * x, lane);
+  if (!w.active) return;
+  store_rows<D>(ring + w.wave * R::TILE, acc, a.scale, dq + (w.t.seq0 + (int64_t)w.q_first) * a.sdq + w.hq * D, a.sdq,
+                w.t.len - w.q_first, w.lane);
 }
 
 // dk and dv: two waves of 64 keys of one kv head, over the queries of all its heads; rounds of 32 queries.
@@ -708,7 +656,7 @@ hipError_t backward(const hpd_finetune_layout* L, FtArgs a, const uint16_t* q, c
                     const uint16_t* out, const float* lse, const uint16_t* d_out, uint16_t* dq, uint16_t* dk, uint16_t* dv,
                     float* stat, hipStream_t s) {
   const unsigned tiles = (unsigned)L->tiles.size();
-  ft_stream_dq_kernel<D><<<dim3(tiles * a.Hq), 128, 0, s>>>(a, q, k, v, out, d_out, lse, stat, dq);
+  ft_stream_dq_kernel<D><<<dim3(tiles * a.Hq), 256, 0, s>>>(a, q, k, v, out, d_out, lse, stat, dq);
   a.tiles = L->d_key_tiles;
   ft_stream_dkv_kernel<D><<<dim3(tiles * a.Hkv), 128, 0, s>>>(a, q, k, v, d_out, stat, dk, dv);
   return hipGetLastError();
