@@ -92,9 +92,9 @@ int build_tables(hpd_finetune_layout* L, const int32_t* prompt_len, const int32_
 int upload(hpd_finetune_layout* L, hipStream_t s) {
   // one allocation: tables, then the (cos, sin) rows, which a kernel writes
   auto pad = [](size_t words) { return (words + 3) / 4 * 4; };
-  // (the kernels read the ranks of whole blocks: 32 more behind the last)
+  // (the kernels read the ranks of two whole blocks at a time: up to 63 more behind the last token)
   const size_t n = (size_t)L->n_tokens, nt = L->tiles.size() * 4;
-  const size_t o_rank = pad(n), o_blk = o_rank + pad(n + HPD_FT_BLOCK), o_tiles = o_blk + pad(L->blk_rank.size()),
+  const size_t o_rank = pad(n), o_blk = o_rank + pad(n + 2 * HPD_FT_BLOCK), o_tiles = o_blk + pad(L->blk_rank.size()),
                o_ktiles = o_tiles + nt, words = o_ktiles + nt;
   std::vector<int32_t> host(words, 0);
   std::copy(L->pos.begin(), L->pos.end(), host.begin());

@@ -247,7 +247,7 @@ struct QueryTile {
   }
   // block b of 32 keys has a key that a query of the wave sees / one that a query does not see
   __device__ __forceinline__ bool reaches(int32_t b) const { return active && b * 32 <= q_first && blk_rank[2 * b] <= q_max; }
-  __device__ __forceinline__ bool masked(int32_t b) const { return b * 32 == q_first || blk_rank[2 * b + 1] > q_min; }
+  __device__ __forceinline__ bool masked(int32_t b) const { return b * 32 >= q_first || blk_rank[2 * b + 1] > q_min; }
   __device__ __forceinline__ void mask(floatx16& s, int32_t b, int32_t rank_i) const {
     BlockRanks rk;
     rk.load(ranks + b * 32);
@@ -304,15 +304,22 @@ __global__ void __launch_bounds__(256, 2) ft_stream_forward_kernel(FtArgs a, con
   zero(acc, R::BLOCKS);
   float m = NEG_BIG, l = 0.f;  // reference point (log2 units; within 2^8 of the maximum) and this lane's share of the sum
 
-  // one block of 32 keys
-  auto block = [&](int kt, int vt, int32_t b) __attribute__((always_inline)) {
-    floatx16 s = {};
+  // One round, two blocks of 32 keys: both scores, one look at the maximum, then the second block's weights while the
+  // first block's products with v run.
+  auto step = [&](int32_t b) __attribute__((always_inline)) {
+    floatx16 s[2] = {};
 #pragma unroll
-    for (int x = 0; x < R::STEPS; ++x) s = mfma(at.rows(x, kt), qf[x], s);
-    if (w.masked(b)) w.mask(s, b, rank_i[0]);
-    float top = s[0];
+    for (int j = 0; j < 2; ++j)
 #pragma unroll
-    for (int r = 1; r < 16; ++r) top = fmaxf(top, s[r]);
+      for (int x = 0; x < R::STEPS; ++x) s[j] = mfma(at.rows(x, j * R::TILE), qf[x], s[j]);
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+      if (w.masked(b + j)) w.mask(s[j], b + j, rank_i[0]);
+    float top = s[0][0];
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) top = fmaxf(top, s[j][r]);
     top *= c;
     if (__any(top > m + MAX_SLACK)) {
       top = fmaxf(top, __shfl_xor(top, 32));
@@ -324,29 +331,43 @@ __global__ void __launch_bounds__(256, 2) ft_stream_forward_kernel(FtArgs a, con
 #pragma unroll
         for (int r = 0; r < 16; ++r) acc[x][r] *= alpha;
     }
-    float p[16];
+    float p[2][16], l0 = 0.f, l1 = 0.f;
+    auto weights = [&](int j, int first, int last) __attribute__((always_inline)) {
 #pragma unroll
-    for (int r = 0; r < 16; ++r) p[r] = fast_exp2(fmaf(s[r], c, -m));
-    float l0 = 0.f, l1 = 0.f;
+      for (int r = first; r < last; ++r) {
+        p[j][r] = fast_exp2(fmaf(s[j][r], c, -m));
+        if (r & 1) l1 += p[j][r];
+        else l0 += p[j][r];
+      }
+    };
+    bf16x8 f[3], pf[2][2];
+    auto ld = [&](int i) __attribute__((always_inline)) -> bf16x8 {  // columns of v, block by block
+      constexpr int C = 2 * R::BLOCKS;
+      return at.columns(i % C / 2, i % 2, (2 + i / C) * R::TILE);
+    };
+    f[0] = ld(0);
+    f[1] = ld(1);
+    weights(0, 0, 16);
+    pf[0][0] = pack8(p[0]);
+    pf[0][1] = pack8(p[0] + 8);
+    __builtin_amdgcn_sched_barrier(0);
+    constexpr int C = 2 * R::BLOCKS;
 #pragma unroll
-    for (int r = 0; r < 16; r += 2) {
-      l0 += p[r];
-      l1 += p[r + 1];
+    for (int i = 0; i < 2 * C; ++i) {
+      if (i + 2 < 2 * C) f[(i + 2) % 3] = ld(i + 2);
+      acc[i % C / 2] = mfma(f[i % 3], pf[i / C][i % 2], acc[i % C / 2]);
+      if (i < C) weights(1, 16 * i / C, 16 * (i + 1) / C);
+      if (i == C / 2 - 1) pf[1][0] = pack8(p[1]);
+      if (i == C - 1) pf[1][1] = pack8(p[1] + 8);
+      __builtin_amdgcn_sched_barrier(0);
     }
     l += l0 + l1;
-    const bf16x8 p0 = pack8(p), p1 = pack8(p + 8);
-#pragma unroll
-    for (int x = 0; x < R::BLOCKS; ++x) {
-      acc[x] = mfma(at.columns(x, 0, vt), p0, acc[x]);
-      acc[x] = mfma(at.columns(x, 1, vt), p1, acc[x]);
-    }
   };
   for (int32_t round = 0; round < w.rounds; ++round) {
     wait_vector_memory<0>();
     wait_lds_and_barrier();  // the round is in LDS, the other half of the ring is free
     if (round + 1 < w.rounds) w.issue(round + 1);
-    if (w.reaches(2 * round)) block(0, 2 * R::TILE, 2 * round);
-    if (w.reaches(2 * round + 1)) block(R::TILE, 3 * R::TILE, 2 * round + 1);
+    if (w.reaches(2 * round) || w.reaches(2 * round + 1)) step(2 * round);
     at.flip(Q::STAGE);
   }
   wait_lds_and_barrier();
