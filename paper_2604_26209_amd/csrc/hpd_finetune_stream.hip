@@ -427,29 +427,57 @@ __global__ void __launch_bounds__(256, 2) ft_stream_dq_kernel(FtArgs a, const ui
   Addresses<D> at(w.ring_lds, w.lane);
   floatx16 acc[R::BLOCKS];
   zero(acc, R::BLOCKS);
-  auto block = [&](int kt, int vt, int32_t b) __attribute__((always_inline)) {
-    floatx16 s = {}, dp = {};
+  // One round, two blocks of 32 keys.  The first block's weights and gradients are made while the second block's
+  // score products run, the second block's while the first block's last products do.
+  auto step = [&](int32_t b) __attribute__((always_inline)) {
+    constexpr int S = R::STEPS, C = 2 * R::BLOCKS;
+    floatx16 s[2] = {}, dp[2] = {};
+    bf16x8 f[3], df[2][2];
+    float e[2][16];
+    // operands: rows of k, v of block 0, then of block 1, then columns of k
+    auto ld = [&](int i) __attribute__((always_inline)) -> bf16x8 {
+      if (i < 4 * S) return at.rows(i % S, (2 * (i / S % 2) + i / (2 * S)) * R::TILE);
+      i -= 4 * S;
+      return at.columns(i % C / 2, i % 2, i / C * R::TILE);
+    };
+    auto gradient = [&](int j, int first, int last) __attribute__((always_inline)) {
 #pragma unroll
-    for (int x = 0; x < R::STEPS; ++x) s = mfma(at.rows(x, kt), qf[x], s);
+      for (int r = first; r < last; ++r) e[j][r] = fast_exp2(fmaf(s[j][r], c, nl[0])) * (dp[j][r] + nd[0]);
+    };
+    f[0] = ld(0);
+    f[1] = ld(1);
 #pragma unroll
-    for (int x = 0; x < R::STEPS; ++x) dp = mfma(at.rows(x, vt), of[x], dp);
-    if (w.masked(b)) w.mask(s, b, rank_i[0]);
-    float e[16];
+    for (int i = 0; i < 4 * S; ++i) {
+      f[(i + 2) % 3] = ld(i + 2);
+      const int j = i / (2 * S), x = i % S;
+      if (i / S % 2 == 0) s[j] = mfma(f[i % 3], qf[x], s[j]);
+      else dp[j] = mfma(f[i % 3], of[x], dp[j]);
+      if (i == 2 * S - 1 && w.masked(b)) w.mask(s[0], b, rank_i[0]);
+      if (i >= 2 * S) {  // (a step behind: the last product is on its way)
+        const int y = i - 2 * S;
+        gradient(0, 16 * (y > 0 ? y - 1 : 0) / (2 * S - 1), 16 * y / (2 * S - 1));
+        if (y == S) df[0][0] = pack8(e[0]);
+        if (y == 2 * S - 1) df[0][1] = pack8(e[0] + 8);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    if (w.masked(b + 1)) w.mask(s[1], b + 1, rank_i[0]);
 #pragma unroll
-    for (int r = 0; r < 16; ++r) e[r] = fast_exp2(fmaf(s[r], c, nl[0])) * (dp[r] + nd[0]);
-    const bf16x8 d0 = pack8(e), d1 = pack8(e + 8);
-#pragma unroll
-    for (int x = 0; x < R::BLOCKS; ++x) {
-      acc[x] = mfma(at.columns(x, 0, kt), d0, acc[x]);
-      acc[x] = mfma(at.columns(x, 1, kt), d1, acc[x]);
+    for (int i = 0; i < 2 * C; ++i) {
+      const int at_ = 4 * S + i;
+      if (i + 2 < 2 * C) f[(at_ + 2) % 3] = ld(at_ + 2);
+      acc[i % C / 2] = mfma(f[at_ % 3], df[i / C][i % 2], acc[i % C / 2]);
+      if (i < C) gradient(1, 16 * i / C, 16 * (i + 1) / C);
+      if (i == C / 2 - 1) df[1][0] = pack8(e[1]);
+      if (i == C - 1) df[1][1] = pack8(e[1] + 8);
+      __builtin_amdgcn_sched_barrier(0);
     }
   };
   for (int32_t round = 0; round < w.rounds; ++round) {
     wait_vector_memory<0>();
     wait_lds_and_barrier();
     if (round + 1 < w.rounds) w.issue(round + 1);
-    if (w.reaches(2 * round)) block(0, 2 * R::TILE, 2 * round);
-    if (w.reaches(2 * round + 1)) block(R::TILE, 3 * R::TILE, 2 * round + 1);
+    if (w.reaches(2 * round) || w.reaches(2 * round + 1)) step(2 * round);
     at.flip(Q::STAGE);
   }
   wait_lds_and_barrier();
