@@ -19,10 +19,6 @@ FLAGS = ["-O3", "-std=c++17", "-fPIC", "--offload-arch=gfx950", "-Wall", "-Wno-u
          "-mllvm", "-amdgpu-kernarg-preload-count=8",
          "-I", os.path.join(ROOT, "include"), "-I", CSRC]
 
-# The compiler's own matrix instructions write vector registers there; accumulation registers are for the sums that the
-# gradient kernels place in them.
-EXTRA_FLAGS = {"hpd_finetune_stream.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"]}
-
 
 def build(verbose: bool = False) -> str:
     hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
@@ -30,7 +26,7 @@ def build(verbose: bool = False) -> str:
     procs = []
     for src in SOURCES:
         obj = os.path.join(CSRC, os.path.splitext(src)[0] + ".o")
-        cmd = [hipcc, *FLAGS, *EXTRA_FLAGS.get(src, []), "-c", os.path.join(CSRC, src), "-o", obj]
+        cmd = [hipcc, *FLAGS, "-c", os.path.join(CSRC, src), "-o", obj]
         if src.endswith(".cpp"):
             cmd.insert(1, "-x"), cmd.insert(2, "hip")
         procs.append((src, subprocess.Popen(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)))

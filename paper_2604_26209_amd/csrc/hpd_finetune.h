@@ -20,6 +20,14 @@ struct hpd_ft_tile {
   int32_t blk0;  // the sequence's first entry in blk_rank
 };
 
+// A run of the rounds (32 queries of one head each, head by head) of a key tile and of one kv head.
+struct hpd_ft_item {
+  int32_t seq0, len, row0, blk0;  // of the tile
+  int32_t begin, end;             // rounds
+  int32_t slot;                   // partial sums, or -1: the item is the whole tile
+  int32_t pad;
+};
+
 struct hpd_finetune_layout {
   hpd_finetune_config cfg;
   int32_t n_seq = 0, n_tokens = 0, max_len = 0, max_pos = -1;
@@ -27,18 +35,27 @@ struct hpd_finetune_layout {
   std::vector<int32_t> blk_rank;        // [blocks][2]: lowest and highest rank of 32 tokens of a sequence
   std::vector<hpd_ft_tile> tiles;       // query tiles, those with most keys first
   std::vector<hpd_ft_tile> key_tiles;   // the same tiles, those with most queries first
+  // hpd_finetune_stream.hip: the key tiles as items, longest first, and for those of several items the first slot and
+  // (as `end`) their number
+  std::vector<hpd_ft_item> items, joins;
+  int32_t slots = 0;
 
   bool on_device = false;
   void* d_mem = nullptr;
   const int32_t *d_pos = nullptr, *d_rank = nullptr;
   const int2* d_blk_rank = nullptr;
   const hpd_ft_tile *d_tiles = nullptr, *d_key_tiles = nullptr;
+  const hpd_ft_item *d_items = nullptr, *d_joins = nullptr;
   // (cos, sin) rows of D/2: one per position ID, or one per token where that is fewer
   float2* d_rope = nullptr;
   int32_t rope_rows = 0;
   bool rope_by_token = false;
 };
 
+// The kernels for bf16 with head_dim 64 or 128 (hpd_finetune_stream.hip) run.
+inline bool hpd_ft_stream_supported(const hpd_finetune_layout* L) {
+  return L->cfg.dtype == HPD_BF16 && (L->cfg.head_dim == 64 || L->cfg.head_dim == 128);
+}
 // Bytes of the calls' workspaces.
 int64_t hpd_ft_forward_bytes(const hpd_finetune_layout* L);
 int64_t hpd_ft_backward_bytes(const hpd_finetune_layout* L);

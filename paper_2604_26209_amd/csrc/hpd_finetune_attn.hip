@@ -467,9 +467,6 @@ hipError_t rotate(const hpd_finetune_layout* L, float sign, const void* q, const
 
 }  // namespace
 
-int64_t hpd_ft_forward_bytes(const hpd_finetune_layout*) { return 0; }
-int64_t hpd_ft_backward_bytes(const hpd_finetune_layout* L) { return (int64_t)L->n_tokens * L->cfg.n_q_heads * 8; }
-
 hipError_t hpd_launch_ft_rope_table(const hpd_finetune_layout* L, hipStream_t s) {
   const int32_t half = L->cfg.head_dim / 2;
   const int64_t n = (int64_t)L->rope_rows * half;

@@ -15,7 +15,6 @@ struct FtArgs {
 };
 
 // Kernels for bf16 with head_dim 64 or 128 (hpd_finetune_stream.hip).
-bool hpd_ft_stream_supported(const hpd_finetune_layout* L);
 hipError_t hpd_launch_ft_stream_forward(const hpd_finetune_layout* L, FtArgs a, const void* q, const void* k, const void* v,
                                         void* out, float* lse, hipStream_t s);
 hipError_t hpd_launch_ft_stream_backward(const hpd_finetune_layout* L, FtArgs a, const void* q, const void* k, const void* v,

@@ -34,9 +34,30 @@ int validate(const hpd_finetune_config* c) {
   return HPD_OK;
 }
 
+// The items of the dk/dv kernel.  Two workgroups run on a CU at a time; a key tile at the start of a long sequence
+// has many times the rounds of others, and a batch may have fewer tiles than the GPU has room for.  Tiles are
+// cut so that an item is at most a third of what a workgroup's place has to do, but not below 24 rounds: an
+// item starts and ends with the time of four, and its sums are written and read once more.
+void plan_items(hpd_finetune_layout* L, int32_t n_cus) {
+  const int64_t Hkv = L->cfg.n_kv_heads, G = L->cfg.n_q_heads / Hkv;
+  auto rounds = [&](const hpd_ft_tile& t) { return G * ((t.len + 31) / 32 - t.row0 / 32); };
+  int64_t total = 0;
+  for (const hpd_ft_tile& t : L->key_tiles) total += rounds(t) * Hkv;
+  const int64_t most = std::max<int64_t>(24, total / (2 * n_cus) / 3);
+  for (const hpd_ft_tile& t : L->key_tiles) {
+    const int64_t r = rounds(t), parts = r * 2 > most * 3 ? (r + most - 1) / most : 1;
+    if (parts > 1) L->joins.push_back({t.seq0, t.len, t.row0, t.blk0, 0, (int32_t)parts, L->slots, 0});
+    for (int64_t p = 0; p < parts; ++p)
+      L->items.push_back({t.seq0, t.len, t.row0, t.blk0, (int32_t)(r * p / parts), (int32_t)(r * (p + 1) / parts),
+                          parts > 1 ? L->slots++ : -1, 0});
+  }
+  std::stable_sort(L->items.begin(), L->items.end(),
+                   [](const hpd_ft_item& a, const hpd_ft_item& b) { return a.end - a.begin > b.end - b.begin; });
+}
+
 // Positions (Algorithm 2, values at pos_id[end(a_n)] + k), ranks, rank ranges of blocks, work tiles.
 int build_tables(hpd_finetune_layout* L, const int32_t* prompt_len, const int32_t* attr_ptr, const int32_t* attr_len,
-                 const int32_t* value_len) {
+                 const int32_t* value_len, int32_t n_cus) {
   const int64_t k_max = L->cfg.k_max;
   int64_t total = 0;
   for (int32_t s = 0; s < L->n_seq; ++s) {
@@ -84,6 +105,7 @@ int build_tables(hpd_finetune_layout* L, const int32_t* prompt_len, const int32_
   });
   std::stable_sort(L->key_tiles.begin(), L->key_tiles.end(),
                    [](const hpd_ft_tile& a, const hpd_ft_tile& b) { return a.len - a.row0 > b.len - b.row0; });
+  if (hpd_ft_stream_supported(L)) plan_items(L, n_cus);
   L->rope_by_token = L->max_pos >= L->n_tokens;
   L->rope_rows = L->rope_by_token ? L->n_tokens : L->max_pos + 1;
   return HPD_OK;
@@ -95,13 +117,16 @@ int upload(hpd_finetune_layout* L, hipStream_t s) {
   // (the kernels read the ranks of two whole blocks at a time: up to 63 more behind the last token)
   const size_t n = (size_t)L->n_tokens, nt = L->tiles.size() * 4;
   const size_t o_rank = pad(n), o_blk = o_rank + pad(n + 2 * HPD_FT_BLOCK), o_tiles = o_blk + pad(L->blk_rank.size()),
-               o_ktiles = o_tiles + nt, words = o_ktiles + nt;
+               o_ktiles = o_tiles + nt, o_items = o_ktiles + nt, o_joins = o_items + L->items.size() * 8,
+               words = o_joins + L->joins.size() * 8;
   std::vector<int32_t> host(words, 0);
   std::copy(L->pos.begin(), L->pos.end(), host.begin());
   std::copy(L->rank.begin(), L->rank.end(), host.begin() + o_rank);
   std::copy(L->blk_rank.begin(), L->blk_rank.end(), host.begin() + o_blk);
   std::memcpy(host.data() + o_tiles, L->tiles.data(), nt * 4);
   std::memcpy(host.data() + o_ktiles, L->key_tiles.data(), nt * 4);
+  if (!L->items.empty()) std::memcpy(host.data() + o_items, L->items.data(), L->items.size() * sizeof(hpd_ft_item));
+  if (!L->joins.empty()) std::memcpy(host.data() + o_joins, L->joins.data(), L->joins.size() * sizeof(hpd_ft_item));
   const size_t rope_bytes = (size_t)L->rope_rows * (size_t)(L->cfg.head_dim / 2) * sizeof(float2);
   HPD_HIP(hipMalloc(&L->d_mem, words * 4 + rope_bytes));
   const int32_t* base = (const int32_t*)L->d_mem;
@@ -110,6 +135,8 @@ int upload(hpd_finetune_layout* L, hipStream_t s) {
   L->d_blk_rank = (const int2*)(base + o_blk);
   L->d_tiles = (const hpd_ft_tile*)(base + o_tiles);
   L->d_key_tiles = (const hpd_ft_tile*)(base + o_ktiles);
+  L->d_items = (const hpd_ft_item*)(base + o_items);
+  L->d_joins = (const hpd_ft_item*)(base + o_joins);
   L->d_rope = (float2*)(base + words);
   HPD_HIP(hipMemcpyAsync(L->d_mem, host.data(), words * 4, hipMemcpyHostToDevice, s));
   hipError_t e = hpd_launch_ft_rope_table(L, s);
@@ -146,6 +173,13 @@ int check_logits(int32_t dtype, int64_t n_rows, int32_t vocab) {
 
 }  // namespace
 
+int64_t hpd_ft_forward_bytes(const hpd_finetune_layout*) { return 0; }
+// two numbers per (head, token), then the partial sums of dk and dv
+int64_t hpd_ft_backward_bytes(const hpd_finetune_layout* L) {
+  const int64_t rows = (int64_t)L->n_tokens * L->cfg.n_q_heads;
+  return (rows * 8 + 15) / 16 * 16 + (int64_t)L->slots * L->cfg.n_kv_heads * 2 * HPD_FT_ROWS * L->cfg.head_dim * 4;
+}
+
 extern "C" {
 
 int hpd_build_finetune_layout(const hpd_finetune_config* cfg, int32_t n_seq, const int32_t* prompt_len,
@@ -167,7 +201,13 @@ int hpd_build_finetune_layout(const hpd_finetune_config* cfg, int32_t n_seq, con
     L = new hpd_finetune_layout();
     L->cfg = *cfg;
     L->n_seq = n_seq;
-    rc = build_tables(L, prompt_len, attr_ptr, attr_len, value_len);
+    int32_t n_cus = 256, device = 0;
+    if (!(cfg->flags & HPD_FLAG_HOST_ONLY)) {
+      hipError_t e = hipGetDevice(&device);
+      if (e == hipSuccess) e = hipDeviceGetAttribute(&n_cus, hipDeviceAttributeMultiprocessorCount, device);
+      if (e != hipSuccess) rc = hpd_hip_fail(e);
+    }
+    if (rc == HPD_OK) rc = build_tables(L, prompt_len, attr_ptr, attr_len, value_len, n_cus);
     if (rc == HPD_OK && !(cfg->flags & HPD_FLAG_HOST_ONLY)) {
       if (L->n_tokens > 0) rc = upload(L, (hipStream_t)stream);
       L->on_device = rc == HPD_OK;

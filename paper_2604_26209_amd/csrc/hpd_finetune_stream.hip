@@ -108,41 +108,15 @@ __device__ __forceinline__ void arrived(T (&v)[N]) {
 __device__ __forceinline__ uint32_t lds_address(const void* p) {
   return (uint32_t)reinterpret_cast<uintptr_t>((const __attribute__((address_space(3))) char*)p);
 }
-__device__ __forceinline__ bf16x8 lds_rows(const char* p) {
-  return __builtin_bit_cast(bf16x8, *reinterpret_cast<const uint4*>(p));
-}
-// the same by LDS address
 __device__ __forceinline__ bf16x8 lds_read(uint32_t at) {
   return __builtin_bit_cast(bf16x8, *(const __attribute__((address_space(3))) uint4v*)(uintptr_t)at);
 }
 __device__ __forceinline__ uint2 lds_read_tr(uint32_t at) {
   return __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) hpd::short4v*)(uintptr_t)at));
 }
-template <int D>
-__device__ __forceinline__ bf16x8 lds_columns(const char* tile, uint32_t col, int b, int k) {
-  using R = Rows<D>;
-  const uint2 lo = hpd::lds_read_tr16(tile + (col ^ (b << 6)) + 16 * k * R::RB);
-  const uint2 hi = hpd::lds_read_tr16(tile + (col ^ (b << 6) ^ 32) + (16 * k + 8) * R::RB);
-  return __builtin_bit_cast(bf16x8, make_uint4(lo.x, lo.y, hi.x, hi.y));
-}
 __device__ __forceinline__ floatx16 mfma(bf16x8 a, bf16x8 b, floatx16 c) {
   return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
 }
-// The same, adding up in the accumulation registers, which only these instructions touch between
-// the two hold(): the gradient kernels have a wave per SIMD and up to 256 accumulators, and left to
-// itself the compiler moves them to and fro.
-__device__ __forceinline__ void add_product(bf16x8 a, bf16x8 b, floatx16& c) {
-  asm("v_mfma_f32_32x32x16_bf16 %0, %1, %2, %0" : "+a"(c) : "v"(a), "v"(b));
-}
-// In front of the loop and behind it, so that inside they are never anywhere else.
-template <int N>
-__device__ __forceinline__ void hold(floatx16* c) {
-#pragma unroll
-  for (int i = 0; i < N; ++i) asm volatile("" : "+a"(c[i]));
-}
-// Behind the loop: waits out the last product (8 passes of 4 cycles).
-__device__ __forceinline__ void settle() { asm volatile("s_nop 15\n\ts_nop 15" ::: "memory"); }
-
 // the ranks of a block's 32 tokens in scalar registers (wave-uniform address)
 typedef int32_t int32x16 __attribute__((ext_vector_type(16)));
 struct BlockRanks {
@@ -486,209 +460,235 @@ __global__ void __launch_bounds__(256, 2) ft_stream_dq_kernel(FtArgs a, const ui
                 w.t.len - w.q_first, w.lane);
 }
 
-// dk and dv: two waves of 64 keys of one kv head, over the queries of all its heads; rounds of 32 queries.
+// dk and dv: four waves of 32 keys of one kv head, over the queries of all its heads; rounds of 32 queries, two in
+// LDS.  The wave's keys are in registers, its values, for want of room there, in LDS.  An item is a run of
+// a tile's rounds; the sums of a tile that is cut into several go to `partial`, register by register, and a
+// second kernel adds them up.
 template <int D>
-__global__ void __launch_bounds__(128, 1) ft_stream_dkv_kernel(FtArgs a, const uint16_t* __restrict__ q,
-                                                              const uint16_t* __restrict__ k, const uint16_t* __restrict__ v,
-                                                              const uint16_t* __restrict__ d_out,
-                                                              const float* __restrict__ stat, uint16_t* __restrict__ dk,
-                                                              uint16_t* __restrict__ dv) {
+struct KeyTile {
   using R = Rows<D>;
-  constexpr int STAGE = 2 * R::TILE + 512, SLOTS = 4, LOADS = R::TILE / 1024 + 1;  // rows of q and do; each wave's own -lse, -delta
-  __shared__ __attribute__((aligned(1024))) char ring[SLOTS * STAGE];
+  static constexpr int SUMS = 32 * D;                // fp32 sums of a wave
+  static constexpr int PARTIAL = 2 * 4 * SUMS;       // of an item and kv head: dk and dv of four waves
+};
+template <int D>
+__global__ void __launch_bounds__(256, 2) ft_stream_dkv_kernel(FtArgs a, const hpd_ft_item* __restrict__ items,
+                                                              const uint16_t* __restrict__ q, const uint16_t* __restrict__ k,
+                                                              const uint16_t* __restrict__ v, const uint16_t* __restrict__ d_out,
+                                                              const float* __restrict__ stat, float* __restrict__ partial,
+                                                              uint16_t* __restrict__ dk, uint16_t* __restrict__ dv) {
+  using R = Rows<D>;
+  constexpr int STAGE = 2 * R::TILE;  // rows of q and of do
+  __shared__ __attribute__((aligned(2 * STAGE))) char ring[2 * STAGE];
+  __shared__ __attribute__((aligned(1024))) char values[4 * R::TILE];
+  __shared__ __attribute__((aligned(1024))) float stats[2][64];  // of a round's rows: -lse sqrt(D), then -delta
   const int lane = threadIdx.x & 63, n = lane & 31, h = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int32_t G = a.Hq / a.Hkv, hk = blockIdx.x % a.Hkv;
-  const hpd_ft_tile t = a.tiles[blockIdx.x / a.Hkv];
-  const int32_t k_first = t.row0 + wave * 64;
+  const hpd_ft_item t = items[blockIdx.x / a.Hkv];
+  const int32_t k_first = t.row0 + wave * 32, j = k_first + n;
   const bool active = k_first < t.len;
+  const int32_t own = min(k_first, t.len - 1);  // first key of the wave, if it has one
+  const int64_t token = t.seq0 + (int64_t)min(j, t.len - 1);
 
+  // this wave's part of a round: waves 0 and 1 queries, 2 and 3 gradients of the output
   Loader<D> loader;
-  loader.init(wave == 0 ? a.sq : (int64_t)a.Hq * D, lane);
-  const char* const src = reinterpret_cast<const char*>(wave == 0 ? q + t.seq0 * a.sq : d_out + (int64_t)t.seq0 * a.Hq * D);
-  const uint32_t ring_lds = lds_address(ring);
-  const int32_t b_first = t.row0 / 32, per_head = (t.len + 31) / 32 - b_first, rounds = G * per_head;
-  int32_t next_g = 0, next_b = b_first;  // the round that is requested next
-  auto issue = [&](int32_t round) {
-    const uint32_t slot = ring_lds + (round & (SLOTS - 1)) * STAGE;
+  loader.init(wave < 2 ? a.sq : (int64_t)a.Hq * D, lane);
+  const char* const src = reinterpret_cast<const char*>(wave < 2 ? q + t.seq0 * a.sq : d_out + (int64_t)t.seq0 * a.Hq * D);
+  const uint32_t ring_lds = lds_address(ring), stats_lds = lds_address(stats);
+  const int32_t b_first = t.row0 / 32, per_head = (t.len + 31) / 32 - b_first;
+  int32_t next_g = t.begin / per_head, next_b = b_first + t.begin % per_head;  // the round that is requested next
+  auto issue = [&](int32_t slot) {
     const int32_t hq = hk * G + next_g;
-#pragma unroll
-    for (int j = 0; j < 32 / R::GROUP; ++j) {
-      const int32_t first = min(next_b * 32 + j * R::GROUP, t.len - 1);
-      loader.load(src + first * loader.stride + hq * D * 2, slot + wave * R::TILE + j * R::GROUP * R::RB,
+    if (D == 128 || (wave & 1) == 0) {  // (a tile of 64 channels is one group)
+      const int32_t row = D == 128 ? 16 * (wave & 1) : 0, first = min(next_b * 32 + row, t.len - 1);
+      loader.load(src + first * loader.stride + hq * D * 2, ring_lds + slot * STAGE + (wave >> 1) * R::TILE + row * R::RB,
                   t.len - 1 - first, lane);
     }
-    const float* p = stat + (h * (int64_t)a.Hq + hq) * a.N + t.seq0 + min(next_b * 32 + n, t.len - 1);
-    const uint32_t dst = __builtin_amdgcn_readfirstlane(slot + 2 * R::TILE + wave * 256);
-    uint32_t keep;
-    asm volatile(
-        "s_mov_b32 %0, m0\n\ts_mov_b32 m0, %2\n\ts_nop 0\n\t"
-        "global_load_lds_dword %1, off\n\ts_mov_b32 m0, %0"
-        : "=&s"(keep)
-        : "v"(p), "s"(dst)
-        : "memory");
+    if (wave == 3) {
+      const float* p = stat + (h * (int64_t)a.Hq + hq) * a.N + t.seq0 + min(next_b * 32 + n, t.len - 1);
+      const uint32_t dst = __builtin_amdgcn_readfirstlane(stats_lds + slot * 256);
+      uint32_t keep;
+      asm volatile(
+          "s_mov_b32 %0, m0\n\ts_mov_b32 m0, %2\n\ts_nop 0\n\t"
+          "global_load_lds_dword %1, off\n\ts_mov_b32 m0, %0"
+          : "=&s"(keep)
+          : "v"(p), "s"(dst)
+          : "memory");
+    }
     if (++next_b == b_first + per_head) {
       next_b = b_first;
       ++next_g;
     }
   };
-  issue(0);
-  if (rounds > 1) issue(1);
-  if (rounds > 2) issue(2);
-  bf16x8 kf[2][R::STEPS], vf[2][R::STEPS];
-  int32_t j[2], rank_j[2];
+  int32_t b = next_b;
+  if (t.begin < t.end) issue(0);
+  {
+    Loader<D> own_values;
+    own_values.init(a.sv, lane);
+    const char* const base = reinterpret_cast<const char*>(v + t.seq0 * a.sv + (int64_t)hk * D);
 #pragma unroll
-  for (int x = 0; x < 2; ++x) {
-    j[x] = k_first + 32 * x + n;
-    const int64_t token = t.seq0 + (int64_t)min(j[x], t.len - 1);
-    const uint16_t* krow = k + token * a.sk + hk * D + h * 8;
-    const uint16_t* vrow = v + token * a.sv + hk * D + h * 8;
-#pragma unroll
-    for (int s = 0; s < R::STEPS; ++s) {
-      kf[x][s] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const uint4*>(krow + s * 16));
-      vf[x][s] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const uint4*>(vrow + s * 16));
+    for (int x = 0; x < 32 / R::GROUP; ++x) {
+      const int32_t first = min(own + x * R::GROUP, t.len - 1);
+      own_values.load(base + first * own_values.stride, lds_address(values) + wave * R::TILE + x * R::GROUP * R::RB,
+                      t.len - 1 - first, lane);
     }
-    rank_j[x] = a.rank[token];
   }
-  arrived(kf[0]);
-  arrived(kf[1]);
-  arrived(vf[0]);
-  arrived(vf[1]);
+  bf16x8 kf[R::STEPS];
+  {
+    const uint16_t* row = k + token * a.sk + (int64_t)hk * D + h * 8;
+#pragma unroll
+    for (int s = 0; s < R::STEPS; ++s) kf[s] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const uint4*>(row + s * 16));
+  }
+  int32_t rank_j[1] = {a.rank[token]};
+  arrived(kf);
   arrived(rank_j);
   const int32_t* const ranks = a.rank + t.seq0;
   const const_i32* const blk_rank = (const const_i32*)(uintptr_t)(a.blk_rank + t.blk0);
-  const int32_t b0 = min(k_first, t.len - 1) / 32, b1 = min(k_first + 32, t.len - 1) / 32;
-  const int32_t k_min = min(blk_rank[2 * b0], blk_rank[2 * b1]), k_max = max(blk_rank[2 * b0 + 1], blk_rank[2 * b1 + 1]);
+  const int32_t k_min = blk_rank[2 * (own / 32)], k_max = blk_rank[2 * (own / 32) + 1];
   const float c = a.scale * LOG2E;
-  const uint32_t row_at = R::row_offset(n, h), col_at = R::column_offset(lane);
+  const uint32_t row_at = ring_lds + R::row_offset(n, h), col_at = ring_lds + R::column_offset(lane);
+  const uint32_t to_values = lds_address(values) + wave * R::TILE - ring_lds;
 
-  floatx16 acc_k[2][R::BLOCKS], acc_v[2][R::BLOCKS];
-  zero(acc_k[0], R::BLOCKS);
-  zero(acc_k[1], R::BLOCKS);
-  zero(acc_v[0], R::BLOCKS);
-  zero(acc_v[1], R::BLOCKS);
-  hold<R::BLOCKS>(acc_k[0]);
-  hold<R::BLOCKS>(acc_k[1]);
-  hold<R::BLOCKS>(acc_v[0]);
-  hold<R::BLOCKS>(acc_v[1]);
-  // The scores of the two columns one after the other (both at once do not fit the registers), each
-  // while the other's exponentials run.
-  auto block = [&](const char* tq, const char* to, const char* st, int32_t b, bool masked) __attribute__((always_inline)) {
-    uint32_t rows = row_at, cols = col_at;
-    asm volatile("" : "+v"(rows), "+v"(cols));  // (the addresses made from them are not kept for the next round: they are 16 registers)
-    constexpr int S = R::STEPS, C = 2 * R::BLOCKS;  // operands: rows of q, do, q, do (S each), columns of do and q (C each)
-    auto ld = [&](int i) __attribute__((always_inline)) -> bf16x8 {
-      if (i < 4 * S) return lds_rows(((i / S) & 1 ? to : tq) + (rows ^ ((i % S) << 5)));
-      i -= 4 * S;
-      return lds_columns<D>(i < C ? to : tq, cols, i % C / 2, i % 2);
-    };
-    auto stats = [&](const char* p) __attribute__((always_inline)) {  // one number per row of the tile, as a result's registers lie
-      floatx16 v;
+  floatx16 acc_k[R::BLOCKS], acc_v[R::BLOCKS];
+  zero(acc_k, R::BLOCKS);
+  zero(acc_v, R::BLOCKS);
+  auto step = [&](int slot, bool masked) __attribute__((always_inline)) {
+    constexpr int S = R::STEPS, C = 2 * R::BLOCKS;
+    uint32_t row = row_at, col = col_at;
+    asm volatile("" : "+v"(row), "+v"(col));  // (the addresses made from them are not kept for the next round: there is no room)
+    auto start = [&](int at) __attribute__((always_inline)) {  // one number per row of the tile, as a result's registers lie
+      floatx16 x;
 #pragma unroll
       for (int z = 0; z < 4; ++z) {
-        const float4 w = *reinterpret_cast<const float4*>(p + (8 * z + 4 * h) * 4);
-        v[4 * z] = w.x; v[4 * z + 1] = w.y; v[4 * z + 2] = w.z; v[4 * z + 3] = w.w;
+        const float4 w = *reinterpret_cast<const float4*>(&stats[slot][at + 8 * z + 4 * h]);
+        x[4 * z] = w.x; x[4 * z + 1] = w.y; x[4 * z + 2] = w.z; x[4 * z + 3] = w.w;
       }
-      return v;
+      return x;
     };
-    // where a score starts: hidden ones at -infinity, where they stay (weight 0)
-    auto start = [&](int x) __attribute__((always_inline)) {
-      floatx16 v = stats(st);
-      if (masked) {
-        BlockRanks rk;
-        rk.load(ranks + b * 32);
-#pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          const int32_t i = b * 32 + tile_row(r, h);
-          v[r] = i < t.len && i >= j[x] && rank_j[x] <= rk.of(r, h) ? v[r] : -INFINITY;
-        }
-      }
-      return v;
+    // left operands: rows of q, rows of do, columns of do, columns of q
+    auto ld = [&](int i) __attribute__((always_inline)) -> bf16x8 {
+      if (i < 2 * S) return lds_read((row ^ (i % S << 5)) + slot * STAGE + i / S * R::TILE);
+      i -= 2 * S;
+      const uint32_t at = (col ^ (i % C / 2 << 6)) + slot * STAGE + (i < C ? R::TILE : 0) + i % 2 * 16 * R::RB;
+      const uint32_t at8 = (col ^ (i % C / 2 << 6) ^ 32) + slot * STAGE + (i < C ? R::TILE : 0) + (i % 2 * 16 + 8) * R::RB;
+      const uint2 lo = lds_read_tr(at), hi = lds_read_tr(at8);
+      return __builtin_bit_cast(bf16x8, make_uint4(lo.x, lo.y, hi.x, hi.y));
     };
-    bf16x8 f[3], pf[2][2], df[2][2];
-    floatx16 s, dp;
-    auto weight = [&](int r) __attribute__((always_inline)) { s[r] = fast_exp2(s[r] * c); };
-    auto pack_half = [&](int x, int z) __attribute__((always_inline)) {
-      float p[8], e[8];
-#pragma unroll
-      for (int r = 0; r < 8; ++r) {
-        p[r] = s[8 * z + r];
-        e[r] = p[r] * dp[8 * z + r];
-      }
-      pf[x][z] = pack8(p);
-      df[x][z] = pack8(e);
-    };
+    bf16x8 f[3], g[2], pf[2], df[2];
+    floatx16 s = start(0), dp;
     f[0] = ld(0);
     f[1] = ld(1);
 #pragma unroll
-    for (int x = 0; x < 2; ++x) {
-      floatx16 next = start(x);
+    for (int i = 0; i < S; ++i) {
+      f[(i + 2) % 3] = ld(i + 2);
+      s = mfma(f[i % 3], kf[i], s);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    if (masked) {
+      BlockRanks rk;
+      rk.load(ranks + b * 32);
 #pragma unroll
-      for (int i = 0; i < S; ++i) {
-        const int at = 2 * x * S + i;
-        f[(at + 2) % 3] = ld(at + 2);
-        next = mfma(f[at % 3], kf[x][i], next);
-        if (x == 1 && i == S / 2 - 1) pack_half(0, 0);
-        if (x == 1 && i == S - 1) pack_half(0, 1);
-        __builtin_amdgcn_sched_barrier(0);
-      }
-      s = next;
-      dp = stats(st + 128);
-#pragma unroll
-      for (int i = 0; i < S; ++i) {
-        const int at = (2 * x + 1) * S + i;
-        f[(at + 2) % 3] = ld(at + 2);
-        dp = mfma(f[at % 3], vf[x][i], dp);
-#pragma unroll
-        for (int r = 16 * (i - 1) / (S - 1); i > 0 && r < 16 * i / (S - 1); ++r) weight(r);
-        __builtin_amdgcn_sched_barrier(0);
+      for (int r = 0; r < 16; ++r) {
+        const int32_t i = b * 32 + tile_row(r, h);
+        s[r] = i < t.len && i >= j && rank_j[0] <= rk.of(r, h) ? s[r] : -INFINITY;
       }
     }
-    pack_half(1, 0);
-    pack_half(1, 1);
+    dp = start(32);
+    g[0] = lds_read(row + to_values);
+#pragma unroll
+    for (int i = 0; i < S; ++i) {
+      f[(S + i + 2) % 3] = ld(S + i + 2);
+      if (i + 1 < S) g[(i + 1) % 2] = lds_read((row ^ ((i + 1) << 5)) + to_values);
+      dp = mfma(f[(S + i) % 3], g[i % 2], dp);
+#pragma unroll
+      for (int r = 16 * i / S; r < 16 * (i + 1) / S; ++r) s[r] = fast_exp2(s[r] * c);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    float e[16];
+#pragma unroll
+    for (int r = 0; r < 16; ++r) e[r] = s[r];
+    pf[0] = pack8(e);
+    pf[1] = pack8(e + 8);
     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
     for (int i = 0; i < 2 * C; ++i) {
-      const int at = 4 * S + i;
+      const int at = 2 * S + i;
       if (i + 2 < 2 * C) f[(at + 2) % 3] = ld(at + 2);
       if (i < C) {
-        add_product(f[at % 3], pf[0][i % 2], acc_v[0][i / 2]);
-        add_product(f[at % 3], pf[1][i % 2], acc_v[1][i / 2]);
+        acc_v[i / 2] = mfma(f[at % 3], pf[i % 2], acc_v[i / 2]);
+#pragma unroll
+        for (int r = 16 * i / C; r < 16 * (i + 1) / C; ++r) e[r] *= dp[r];
+        if (i == C / 2 - 1) df[0] = pack8(e);
+        if (i == C - 1) df[1] = pack8(e + 8);
       } else {
-        add_product(f[at % 3], df[0][i % 2], acc_k[0][(i - C) / 2]);
-        add_product(f[at % 3], df[1][i % 2], acc_k[1][(i - C) / 2]);
+        acc_k[(i - C) / 2] = mfma(f[at % 3], df[i % 2], acc_k[(i - C) / 2]);
       }
       __builtin_amdgcn_sched_barrier(0);
     }
   };
-  int32_t b = b_first;
-  for (int32_t round = 0; round < rounds; ++round) {
-    const int32_t ahead = rounds - 1 - round;
-    if (ahead >= 2) wait_vector_memory<2 * LOADS>();
-    else if (ahead == 1) wait_vector_memory<LOADS>();
-    else wait_vector_memory<0>();
+  auto turn = [&](int32_t round, int slot) __attribute__((always_inline)) {
+    wait_vector_memory<0>();
     wait_lds_and_barrier();
-    if (round + 3 < rounds) issue(round + 3);
+    if (round + 1 < t.end) issue(slot ^ 1);
     const int32_t q_min = blk_rank[2 * b], q_max = blk_rank[2 * b + 1];
-    const char* const slot = ring + (round & (SLOTS - 1)) * STAGE;
-    const char* const st = slot + 2 * R::TILE + wave * 256;
-    if (active && b * 32 + 31 >= k_first && k_min <= q_max)
-      block(slot, slot + R::TILE, st, b, b * 32 < k_first + 63 || k_max > q_min || (b + 1) * 32 > t.len);
+    if (active && b * 32 + 31 >= k_first && k_min <= q_max) step(slot, b * 32 < k_first + 31 || k_max > q_min || (b + 1) * 32 > t.len);
     if (++b == b_first + per_head) b = b_first;
+  };
+  for (int32_t round = t.begin; round < t.end; round += 2) {
+    turn(round, 0);
+    if (round + 1 < t.end) turn(round + 1, 1);
   }
-  settle();
-  hold<R::BLOCKS>(acc_k[0]);
-  hold<R::BLOCKS>(acc_k[1]);
-  hold<R::BLOCKS>(acc_v[0]);
-  hold<R::BLOCKS>(acc_v[1]);
+  wait_vector_memory<0>();
   wait_lds_and_barrier();
-  if (!active) return;
+  if (t.slot >= 0) {
+    float* p = partial + ((int64_t)t.slot * a.Hkv + hk) * KeyTile<D>::PARTIAL + wave * KeyTile<D>::SUMS + lane * 4;
 #pragma unroll
-  for (int x = 0; x < 2; ++x) {
-    const int64_t token = t.seq0 + (int64_t)k_first + 32 * x;
-    const int rows = t.len - k_first - 32 * x;
-    store_rows<D>(ring + wave * R::TILE, acc_v[x], 1.f, dv + token * a.sdv + hk * D, a.sdv, rows, lane);
-    store_rows<D>(ring + wave * R::TILE, acc_k[x], a.scale, dk + token * a.sdk + hk * D, a.sdk, rows, lane);
+    for (int x = 0; x < R::BLOCKS; ++x)
+#pragma unroll
+      for (int z = 0; z < 4; ++z) {
+        const int at = (x * 4 + z) * 256;
+        *reinterpret_cast<float4*>(p + at) = make_float4(acc_k[x][4 * z], acc_k[x][4 * z + 1], acc_k[x][4 * z + 2], acc_k[x][4 * z + 3]);
+        *reinterpret_cast<float4*>(p + at + 4 * KeyTile<D>::SUMS) =
+            make_float4(acc_v[x][4 * z], acc_v[x][4 * z + 1], acc_v[x][4 * z + 2], acc_v[x][4 * z + 3]);
+      }
+    return;
+  }
+  if (!active) return;
+  const int64_t first = t.seq0 + (int64_t)k_first;
+  store_rows<D>(ring + wave * R::TILE, acc_v, 1.f, dv + first * a.sdv + hk * D, a.sdv, t.len - k_first, lane);
+  store_rows<D>(ring + wave * R::TILE, acc_k, a.scale, dk + first * a.sdk + hk * D, a.sdk, t.len - k_first, lane);
+}
+
+// adds up a tile's partial sums, in the order of its items
+template <int D>
+__global__ void __launch_bounds__(256) ft_stream_dkv_join_kernel(FtArgs a, const hpd_ft_item* __restrict__ joins,
+                                                               const float* __restrict__ partial, uint16_t* __restrict__ dk,
+                                                               uint16_t* __restrict__ dv) {
+  using R = Rows<D>;
+  __shared__ __attribute__((aligned(1024))) char turn[4 * R::TILE];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int32_t hk = blockIdx.x % a.Hkv;
+  const hpd_ft_item t = joins[blockIdx.x / a.Hkv];  // slots [slot, slot + end)
+  const int32_t k_first = t.row0 + wave * 32;
+  if (k_first >= t.len) return;
+  const int64_t first = t.seq0 + (int64_t)k_first;
+#pragma unroll
+  for (int y = 0; y < 2; ++y) {
+    floatx16 acc[R::BLOCKS];
+    zero(acc, R::BLOCKS);
+    for (int32_t i = 0; i < t.end; ++i) {
+      const float* p = partial + ((int64_t)(t.slot + i) * a.Hkv + hk) * KeyTile<D>::PARTIAL + (4 * y + wave) * KeyTile<D>::SUMS + lane * 4;
+#pragma unroll
+      for (int x = 0; x < R::BLOCKS; ++x)
+#pragma unroll
+        for (int z = 0; z < 4; ++z) {
+          const float4 w = *reinterpret_cast<const float4*>(p + (x * 4 + z) * 256);
+          acc[x][4 * z] += w.x; acc[x][4 * z + 1] += w.y; acc[x][4 * z + 2] += w.z; acc[x][4 * z + 3] += w.w;
+        }
+    }
+    if (y == 0) store_rows<D>(turn + wave * R::TILE, acc, a.scale, dk + first * a.sdk + hk * D, a.sdk, t.len - k_first, lane);
+    else store_rows<D>(turn + wave * R::TILE, acc, 1.f, dv + first * a.sdv + hk * D, a.sdv, t.len - k_first, lane);
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
   }
 }
 
@@ -704,18 +704,16 @@ template <int D>
 hipError_t backward(const hpd_finetune_layout* L, FtArgs a, const uint16_t* q, const uint16_t* k, const uint16_t* v,
                     const uint16_t* out, const float* lse, const uint16_t* d_out, uint16_t* dq, uint16_t* dk, uint16_t* dv,
                     float* stat, hipStream_t s) {
-  const unsigned tiles = (unsigned)L->tiles.size();
-  ft_stream_dq_kernel<D><<<dim3(tiles * a.Hq), 256, 0, s>>>(a, q, k, v, out, d_out, lse, stat, dq);
-  a.tiles = L->d_key_tiles;
-  ft_stream_dkv_kernel<D><<<dim3(tiles * a.Hkv), 128, 0, s>>>(a, q, k, v, d_out, stat, dk, dv);
+  ft_stream_dq_kernel<D><<<dim3((unsigned)L->tiles.size() * a.Hq), 256, 0, s>>>(a, q, k, v, out, d_out, lse, stat, dq);
+  float* partial = stat + 2 * a.N * a.Hq + (-2 * a.N * a.Hq & 3);  // (on 16 bytes)
+  ft_stream_dkv_kernel<D><<<dim3((unsigned)L->items.size() * a.Hkv), 256, 0, s>>>(a, L->d_items, q, k, v, d_out, stat, partial,
+                                                                               dk, dv);
+  if (!L->joins.empty())
+    ft_stream_dkv_join_kernel<D><<<dim3((unsigned)L->joins.size() * a.Hkv), 256, 0, s>>>(a, L->d_joins, partial, dk, dv);
   return hipGetLastError();
 }
 
 }  // namespace
-
-bool hpd_ft_stream_supported(const hpd_finetune_layout* L) {
-  return L->cfg.dtype == HPD_BF16 && (L->cfg.head_dim == 64 || L->cfg.head_dim == 128);
-}
 
 hipError_t hpd_launch_ft_stream_forward(const hpd_finetune_layout* L, FtArgs a, const void* q, const void* k, const void* v,
                                         void* out, float* lse, hipStream_t s) {
