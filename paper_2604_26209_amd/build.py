@@ -10,7 +10,7 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libhpd.so")
 SOURCES = ["hpd_host.cpp", "hpd_kernels.hip", "hpd_attn_stream.hip", "hpd_attn_dense.hip", "hpd_attn_f32.hip", "hpd_peaks.hip",
-           "hpd_finetune_host.cpp", "hpd_finetune_attn.hip", "hpd_finetune_stream.hip",
+           "hpd_finetune_host.cpp", "hpd_finetune_attn.hip", "hpd_finetune_stream.hip", "hpd_finetune_f32.hip",
            "hpd_logprobs.hip"]
 # packed fp32 instructions are switched off for all device code
 FLAGS = ["-O3", "-std=c++17", "-fPIC", "--offload-arch=gfx950", "-Wall", "-Wno-unused-function",

@@ -23,12 +23,10 @@ constexpr int ROWS = HPD_FT_ROWS;
 constexpr int BLK = HPD_FT_BLOCK;
 constexpr int WAVES = ROWS / 32;
 
-// Operand layouts by element type.  A fragment is 16 bytes a lane: the chunk 2 * step + h of the row
-// of the lane (h = lane / 32).
-template <typename T>
-struct Elem;
-template <>
-struct Elem<hpd::bf16_t> {
+typedef hpd::bf16_t T;
+
+// Operand layouts.  A fragment is 16 bytes a lane: the chunk 2 * step + h of the row of the lane (h = lane / 32).
+struct Elem {
   static constexpr int CHUNK = 8;  // elements of 16 bytes
   static __device__ __forceinline__ floatx16 product(uint4 a, uint4 b, floatx16 c) {
     return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
@@ -57,46 +55,10 @@ struct Elem<hpd::bf16_t> {
     *reinterpret_cast<uint2*>(p) = make_uint2(cvt_pk_bf16(v[0], v[1]), cvt_pk_bf16(v[2], v[3]));
   }
 };
-template <>
-struct Elem<float> {
-  static constexpr int CHUNK = 4;
-  static __device__ __forceinline__ floatx16 product(uint4 a, uint4 b, floatx16 c) {
-    const float4 x = __builtin_bit_cast(float4, a), y = __builtin_bit_cast(float4, b);
-    c = __builtin_amdgcn_mfma_f32_32x32x2f32(x.x, y.x, c, 0, 0, 0);
-    c = __builtin_amdgcn_mfma_f32_32x32x2f32(x.y, y.y, c, 0, 0, 0);
-    c = __builtin_amdgcn_mfma_f32_32x32x2f32(x.z, y.z, c, 0, 0, 0);
-    return __builtin_amdgcn_mfma_f32_32x32x2f32(x.w, y.w, c, 0, 0, 0);
-  }
-  struct Right {
-    float f[16];
-  };
-  static __device__ __forceinline__ Right right(const float* p) {
-    Right r;
-#pragma unroll
-    for (int i = 0; i < 16; ++i) r.f[i] = p[i];
-    return r;
-  }
-  template <int PITCH>
-  static __device__ __forceinline__ floatx16 columns(const char* at, const Right& p, floatx16 c) {
-#pragma unroll
-    for (int r = 0; r < 16; ++r)
-      c = __builtin_amdgcn_mfma_f32_32x32x2f32(*reinterpret_cast<const float*>(at + (8 * (r / 4) + r % 4) * PITCH), p.f[r], c,
-                                               0, 0, 0);
-    return c;
-  }
-  template <int PITCH>
-  static __device__ __forceinline__ int column_address(int lane) {
-    return 4 * (lane >> 5) * PITCH + (lane & 31) * 4;
-  }
-  static __device__ __forceinline__ void store4(float* p, const float* v) {
-    *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1], v[2], v[3]);
-  }
-};
-
-// Generic kernels: any D up to DP (zeros behind it), tiles through registers, one tile at a time.
-template <typename T, int DP>
+// Kernels for bf16 with any D up to DP (zeros behind it): tiles through registers, one tile at a time.
+template <int DP>
 struct Tile {
-  using E = Elem<T>;
+  using E = Elem;
   static constexpr int PITCH = DP * (int)sizeof(T) + 16;  // odd in chunks: the rows of a read start in different banks
   static constexpr int CHUNKS = DP / E::CHUNK;
   static constexpr int STEPS = CHUNKS / 2;
@@ -129,10 +91,10 @@ struct Tile {
     for (int s = 0; s < STEPS; ++s) c = E::product(*reinterpret_cast<const uint4*>(at + s * 32), f[s], c);
     return c;
   }
-  static __device__ __forceinline__ void add_columns(const char* lds, const typename E::Right& p, floatx16* acc, int lane) {
-    const char* at = lds + E::template column_address<PITCH>(lane);
+  static __device__ __forceinline__ void add_columns(const char* lds, const E::Right& p, floatx16* acc, int lane) {
+    const char* at = lds + E::column_address<PITCH>(lane);
 #pragma unroll
-    for (int b = 0; b < DP / 32; ++b) acc[b] = E::template columns<PITCH>(at + b * 32 * (int)sizeof(T), p, acc[b]);
+    for (int b = 0; b < DP / 32; ++b) acc[b] = E::columns<PITCH>(at + b * 32 * (int)sizeof(T), p, acc[b]);
   }
   // acc * f to one row of the output
   static __device__ __forceinline__ void store(T* row, const floatx16* acc, float f, int h, int32_t D) {
@@ -149,11 +111,11 @@ struct Tile {
   }
 };
 
-template <typename T, int DP>
+template <int DP>
 __global__ void __launch_bounds__(WAVES * 64) ft_forward_kernel(FtArgs a, const T* __restrict__ q, const T* __restrict__ k,
                                                                const T* __restrict__ v, T* __restrict__ out,
                                                                float* __restrict__ lse) {
-  using TL = Tile<T, DP>;
+  using TL = Tile<DP>;
   __shared__ __attribute__((aligned(16))) char lds_k[TL::BYTES], lds_v[TL::BYTES];
   __shared__ int32_t lds_rank[BLK];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = lane & 31, h = lane >> 5;
@@ -218,8 +180,7 @@ __global__ void __launch_bounds__(WAVES * 64) ft_forward_kernel(FtArgs a, const 
   if (h == 0) lse[hq * a.N + token] = (m + __builtin_amdgcn_logf(l)) * LN2;
 }
 
-// delta_i = do_i . o_i: a wave takes 64 rows (token, head) of D elements, D / CHUNK lanes a row at a time
-template <typename T>
+// delta_i = do_i . o_i: 16 lanes a row
 __global__ void __launch_bounds__(256) ft_delta_kernel(int64_t N, int32_t Hq, int32_t D, const T* __restrict__ out,
                                                        const T* __restrict__ d_out, float* __restrict__ delta) {
   const int64_t row = (int64_t)blockIdx.x * 16 + threadIdx.x / 16;  // 16 lanes a row
@@ -237,12 +198,12 @@ __global__ void __launch_bounds__(256) ft_delta_kernel(int64_t N, int32_t Hq, in
   if (threadIdx.x % 16 == 0) delta[(row % Hq) * N + row / Hq] = s;
 }
 
-template <typename T, int DP>
+template <int DP>
 __global__ void __launch_bounds__(WAVES * 64, 1) ft_dq_kernel(FtArgs a, const T* __restrict__ q, const T* __restrict__ k,
                                                           const T* __restrict__ v, const T* __restrict__ d_out,
                                                           const float* __restrict__ lse, const float* __restrict__ delta,
                                                           T* __restrict__ dq) {
-  using TL = Tile<T, DP>;
+  using TL = Tile<DP>;
   __shared__ __attribute__((aligned(16))) char lds_k[TL::BYTES], lds_v[TL::BYTES];
   __shared__ int32_t lds_rank[BLK];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = lane & 31, h = lane >> 5;
@@ -288,12 +249,12 @@ __global__ void __launch_bounds__(WAVES * 64, 1) ft_dq_kernel(FtArgs a, const T*
   TL::store(dq + token * a.sdq + hq * (int64_t)a.D, acc, a.scale, h, a.D);
 }
 
-template <typename T, int DP>
+template <int DP>
 __global__ void __launch_bounds__(WAVES * 64, 1) ft_dkv_kernel(FtArgs a, const T* __restrict__ q, const T* __restrict__ k,
                                                            const T* __restrict__ v, const T* __restrict__ d_out,
                                                            const float* __restrict__ lse, const float* __restrict__ delta,
                                                            T* __restrict__ dk, T* __restrict__ dv) {
-  using TL = Tile<T, DP>;
+  using TL = Tile<DP>;
   __shared__ __attribute__((aligned(16))) char lds_q[TL::BYTES], lds_o[TL::BYTES];
   __shared__ int32_t lds_rank[BLK];
   __shared__ float lds_lse[BLK], lds_delta[BLK];
@@ -366,9 +327,9 @@ __global__ void __launch_bounds__(256) ft_rope_table_kernel(const int32_t* __res
 }
 
 // V consecutive elements to fp32 and back
-template <int V, typename T>
-__device__ __forceinline__ void load_vec(const T* p, float* f) {
-  if constexpr (sizeof(T) == 4) {
+template <int V, typename E>
+__device__ __forceinline__ void load_vec(const E* p, float* f) {
+  if constexpr (sizeof(E) == 4) {
     const float4 x = *reinterpret_cast<const float4*>(p);
     f[0] = x.x; f[1] = x.y; f[2] = x.z; f[3] = x.w;
   } else if constexpr (V == 8) {
@@ -379,24 +340,20 @@ __device__ __forceinline__ void load_vec(const T* p, float* f) {
     f[2] = __uint_as_float(x.y << 16); f[3] = __uint_as_float(x.y & 0xffff0000u);
   }
 }
-template <int V, typename T>
-__device__ __forceinline__ void store_vec(T* p, const float* f) {
-#pragma unroll
-  for (int e = 0; e < V; e += 4)
-    if constexpr (V == 8 && sizeof(T) == 2) {
-      if (e == 0) *reinterpret_cast<uint4*>(p) = __builtin_bit_cast(uint4, pack8(f));
-    } else {
-      Elem<T>::store4(p + e, f + e);
-    }
+template <int V, typename E>
+__device__ __forceinline__ void store_vec(E* p, const float* f) {
+  if constexpr (sizeof(E) == 4) *reinterpret_cast<float4*>(p) = make_float4(f[0], f[1], f[2], f[3]);
+  else if constexpr (V == 8) *reinterpret_cast<uint4*>(p) = __builtin_bit_cast(uint4, pack8(f));
+  else Elem::store4(p, f);
 }
 
 // A wave per token: D / (2 V) lanes a head, as many heads side by side as fit; the token's (cos, sin)
 // stay in registers over its heads.  Bytes-bound.
-template <typename T, int V>
+template <typename E, int V>
 __global__ void __launch_bounds__(256) ft_rotate_kernel(int32_t N, int32_t Hq, int32_t Hkv, int32_t D, int64_t sq, int64_t sk,
                                                         int64_t sqo, int64_t sko, float sign, const float2* __restrict__ rope,
-                                                        const int32_t* __restrict__ row, const T* q, const T* k, T* q_out,
-                                                        T* k_out) {
+                                                        const int32_t* __restrict__ row, const E* q, const E* k, E* q_out,
+                                                        E* k_out) {
   const int32_t token = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
   if (token >= N) return;
   const int32_t half = D / 2, lanes = half / V, side = 64 / lanes;
@@ -410,8 +367,8 @@ __global__ void __launch_bounds__(256) ft_rotate_kernel(int32_t N, int32_t Hq, i
     s[e] = cs[e].y * sign;
   }
   for (int32_t h = lane / lanes; h < Hq + Hkv; h += side) {
-    const T* in = h < Hq ? q + token * sq + (int64_t)h * D : k + token * sk + (int64_t)(h - Hq) * D;
-    T* to = h < Hq ? q_out + token * sqo + (int64_t)h * D : k_out + token * sko + (int64_t)(h - Hq) * D;
+    const E* in = h < Hq ? q + token * sq + (int64_t)h * D : k + token * sk + (int64_t)(h - Hq) * D;
+    E* to = h < Hq ? q_out + token * sqo + (int64_t)h * D : k_out + token * sko + (int64_t)(h - Hq) * D;
     float x[V], y[V], rx[V], ry[V];
     load_vec<V>(in + m, x);
     load_vec<V>(in + half + m, y);
@@ -435,33 +392,33 @@ FtArgs make_args(const hpd_finetune_layout* L, const hpd_finetune_strides& st) {
   return a;
 }
 
-template <typename T, int DP>
+template <int DP>
 hipError_t forward(const hpd_finetune_layout* L, const FtArgs& a, const void* q, const void* k, const void* v, void* out,
                    float* lse, hipStream_t s) {
-  ft_forward_kernel<T, DP><<<dim3((unsigned)L->tiles.size() * a.Hq), WAVES * 64, 0, s>>>(
+  ft_forward_kernel<DP><<<dim3((unsigned)L->tiles.size() * a.Hq), WAVES * 64, 0, s>>>(
       a, (const T*)q, (const T*)k, (const T*)v, (T*)out, lse);
   return hipGetLastError();
 }
 
-template <typename T, int DP>
+template <int DP>
 hipError_t backward(const hpd_finetune_layout* L, FtArgs a, const void* q, const void* k, const void* v, const void* out,
                     const float* lse, const void* d_out, void* dq, void* dk, void* dv, float* delta, hipStream_t s) {
-  ft_delta_kernel<T><<<dim3((unsigned)((a.N * a.Hq + 15) / 16)), 256, 0, s>>>(a.N, a.Hq, a.D, (const T*)out, (const T*)d_out,
+  ft_delta_kernel<<<dim3((unsigned)((a.N * a.Hq + 15) / 16)), 256, 0, s>>>(a.N, a.Hq, a.D, (const T*)out, (const T*)d_out,
                                                                             delta);
-  ft_dq_kernel<T, DP><<<dim3((unsigned)L->tiles.size() * a.Hq), WAVES * 64, 0, s>>>(
+  ft_dq_kernel<DP><<<dim3((unsigned)L->tiles.size() * a.Hq), WAVES * 64, 0, s>>>(
       a, (const T*)q, (const T*)k, (const T*)v, (const T*)d_out, lse, delta, (T*)dq);
   a.tiles = L->d_key_tiles;
-  ft_dkv_kernel<T, DP><<<dim3((unsigned)L->tiles.size() * a.Hkv), WAVES * 64, 0, s>>>(
+  ft_dkv_kernel<DP><<<dim3((unsigned)L->tiles.size() * a.Hkv), WAVES * 64, 0, s>>>(
       a, (const T*)q, (const T*)k, (const T*)v, (const T*)d_out, lse, delta, (T*)dk, (T*)dv);
   return hipGetLastError();
 }
 
-template <typename T, int V>
+template <typename E, int V>
 hipError_t rotate(const hpd_finetune_layout* L, float sign, const void* q, const void* k, void* q_out, void* k_out,
                   const hpd_finetune_strides& st, hipStream_t s) {
-  ft_rotate_kernel<T, V><<<dim3((unsigned)(L->n_tokens + 3) / 4), 256, 0, s>>>(
+  ft_rotate_kernel<E, V><<<dim3((unsigned)(L->n_tokens + 3) / 4), 256, 0, s>>>(
       L->n_tokens, L->cfg.n_q_heads, L->cfg.n_kv_heads, L->cfg.head_dim, st.q, st.k, st.q_out, st.k_out, sign, L->d_rope,
-      L->rope_by_token ? nullptr : L->d_pos, (const T*)q, (const T*)k, (T*)q_out, (T*)k_out);
+      L->rope_by_token ? nullptr : L->d_pos, (const E*)q, (const E*)k, (E*)q_out, (E*)k_out);
   return hipGetLastError();
 }
 
@@ -487,10 +444,9 @@ hipError_t hpd_launch_ft_attention(const hpd_finetune_layout* L, const void* q, 
                                    float* lse, void*, const hpd_finetune_strides& st, hipStream_t s) {
   const FtArgs a = make_args(L, st);
   if (hpd_ft_stream_supported(L)) return hpd_launch_ft_stream_forward(L, a, q, k, v, out, lse, s);
-  if (L->cfg.dtype == HPD_F32)
-    return a.D <= 64 ? forward<float, 64>(L, a, q, k, v, out, lse, s) : forward<float, 128>(L, a, q, k, v, out, lse, s);
-  return a.D <= 64 ? forward<hpd::bf16_t, 64>(L, a, q, k, v, out, lse, s)
-                   : forward<hpd::bf16_t, 128>(L, a, q, k, v, out, lse, s);
+  if (L->cfg.dtype == HPD_F32) return hpd_launch_ft_f32_forward(L, a, q, k, v, out, lse, s);
+  return a.D <= 64 ? forward<64>(L, a, q, k, v, out, lse, s)
+                   : forward<128>(L, a, q, k, v, out, lse, s);
 }
 
 hipError_t hpd_launch_ft_attention_backward(const hpd_finetune_layout* L, const void* q, const void* k, const void* v,
@@ -499,10 +455,8 @@ hipError_t hpd_launch_ft_attention_backward(const hpd_finetune_layout* L, const 
   const FtArgs a = make_args(L, st);
   if (hpd_ft_stream_supported(L))
     return hpd_launch_ft_stream_backward(L, a, q, k, v, out, lse, d_out, dq, dk, dv, workspace, s);
+  if (L->cfg.dtype == HPD_F32) return hpd_launch_ft_f32_backward(L, a, q, k, v, out, lse, d_out, dq, dk, dv, workspace, s);
   float* delta = (float*)workspace;
-  if (L->cfg.dtype == HPD_F32)
-    return a.D <= 64 ? backward<float, 64>(L, a, q, k, v, out, lse, d_out, dq, dk, dv, delta, s)
-                     : backward<float, 128>(L, a, q, k, v, out, lse, d_out, dq, dk, dv, delta, s);
-  return a.D <= 64 ? backward<hpd::bf16_t, 64>(L, a, q, k, v, out, lse, d_out, dq, dk, dv, delta, s)
-                   : backward<hpd::bf16_t, 128>(L, a, q, k, v, out, lse, d_out, dq, dk, dv, delta, s);
+  return a.D <= 64 ? backward<64>(L, a, q, k, v, out, lse, d_out, dq, dk, dv, delta, s)
+                   : backward<128>(L, a, q, k, v, out, lse, d_out, dq, dk, dv, delta, s);
 }

@@ -1,0 +1,489 @@
+// Fine-tuning attention in fp32: forward and gradients (formulas and operand scheme: hpd_finetune_attn.hip).
+//
+// The matrix instruction (32 x 32 x 2, 64 cycles) is what bounds these kernels: the chain of products of one wave
+// is long before the GPU is full.  So the four waves of a workgroup share 32 tokens and take every fourth block of
+// the other side, each through tiles of its own in LDS, without barriers; their sums meet at the end.  There is one
+// tile of each kind: it is loaded again (global_load_lds) as soon as its last product has read it, and the order of the
+// products leaves one of them between that and the tile's next use.
+//
+// Tiles: 32 rows of DP values (64 or 128; zeros from D on).  Chunk c (16 bytes) of row r lies at c ^ f(r),
+// f(r) = 8 (r / 4 % 2) + 4 (r / 8 % 2) + r % 4: sixteen rows' chunk c in different banks (left operand of four score products),
+// and 32 channels of the rows r and r + 4 too (left operand of a second product).
+#include "hpd_finetune_dev.h"
+
+namespace {
+
+__device__ __forceinline__ floatx16 mfma(float a, float b, floatx16 c) {
+  return __builtin_amdgcn_mfma_f32_32x32x2f32(a, b, c, 0, 0, 0);
+}
+
+template <int DP>
+struct Tile {
+  static constexpr int RB = DP * 4, BYTES = 32 * RB, CHUNKS = RB / 16, STEPS = DP / 8, NB = DP / 32;
+  static constexpr int LOADS = BYTES / 1024;  // load instructions
+  static __device__ __forceinline__ int swizzle(int r) { return ((r >> 2) & 1) << 3 | ((r >> 3) & 1) << 2 | (r & 3); }
+
+  // rows first .. first + 31 of a sequence's head; src: its row 0, last: its last row, which stands for those behind it; zeros:
+  // 16 bytes of them
+  static __device__ __forceinline__ void load(uint32_t lds, const float* src, int64_t stride, int32_t first, int32_t last,
+                                              int32_t D, const void* zeros, int lane) {
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // (the tile's last reads)
+#pragma unroll
+    for (int g = 0; g < LOADS / 4; ++g) {
+      const char* p[4];
+#pragma unroll
+      for (int f = 0; f < 4; ++f) {
+        const int r = (4 * g + f) * (1024 / RB) + lane / CHUNKS, c = (lane % CHUNKS) ^ swizzle(r);
+        p[f] = c * 4 < D ? reinterpret_cast<const char*>(src + min(first + r, last) * stride + c * 4)
+                         : reinterpret_cast<const char*>(zeros);
+        p[f] -= f * 1024;  // (the instruction's offset moves both addresses)
+      }
+      const uint32_t dst = __builtin_amdgcn_readfirstlane(lds + g * 4096);
+      uint32_t keep;  // M0 is the compiler's
+      asm volatile(
+          "s_mov_b32 %0, m0\n\ts_mov_b32 m0, %5\n\ts_nop 0\n\t"
+          "global_load_lds_dwordx4 %1, off\n\t"
+          "global_load_lds_dwordx4 %2, off offset:1024\n\t"
+          "global_load_lds_dwordx4 %3, off offset:2048\n\t"
+          "global_load_lds_dwordx4 %4, off offset:3072\n\t"
+          "s_mov_b32 m0, %0"
+          : "=&s"(keep)
+          : "v"(p[0]), "v"(p[1]), "v"(p[2]), "v"(p[3]), "s"(dst)
+          : "memory");
+    }
+  }
+  struct Own { float4 f[STEPS]; };  // chunk 2 s + h of the lane's row
+  static __device__ __forceinline__ void load(Own& x, const float* row, int h, int32_t D) {
+#pragma unroll
+    for (int s = 0; s < STEPS; ++s) {
+      const int c = (2 * s + h) * 4;
+      x.f[s] = *reinterpret_cast<const float4*>(row + (c < D ? c : 0));
+      if (c >= D) x.f[s] = make_float4(0.f, 0.f, 0.f, 0.f);
+    }
+  }
+  // tile rows x own rows; at: row_offset
+  static __device__ __forceinline__ uint32_t row_offset(int n, int h) { return n * RB + ((h ^ swizzle(n)) << 4); }
+  static __device__ __forceinline__ floatx16 scores(uint32_t tile, uint32_t at, const Own& b, floatx16 s) {
+#pragma unroll
+    for (int x = 0; x < STEPS; ++x) {
+      const float4 a = __builtin_bit_cast(float4, *(const __attribute__((address_space(3))) uint4v*)(uintptr_t)(tile + (at ^ (x << 5))));
+      s = mfma(a.x, b.f[x].x, s);
+      s = mfma(a.y, b.f[x].y, s);
+      s = mfma(a.z, b.f[x].z, s);
+      s = mfma(a.w, b.f[x].w, s);
+    }
+    return s;
+  }
+  // the same, own rows in a tile too
+  static __device__ __forceinline__ floatx16 scores(uint32_t tile, uint32_t at, uint32_t own, floatx16 s) {
+#pragma unroll
+    for (int x = 0; x < STEPS; ++x) {
+      const float4 a = __builtin_bit_cast(float4, *(const __attribute__((address_space(3))) uint4v*)(uintptr_t)(tile + (at ^ (x << 5))));
+      const float4 b = __builtin_bit_cast(float4, *(const __attribute__((address_space(3))) uint4v*)(uintptr_t)(own + (at ^ (x << 5))));
+      s = mfma(a.x, b.x, s);
+      s = mfma(a.y, b.y, s);
+      s = mfma(a.z, b.z, s);
+      s = mfma(a.w, b.w, s);
+    }
+    return s;
+  }
+  // (columns of the tile)^T x p
+  static __device__ __forceinline__ void add(uint32_t tile, int n, int h, const float* p, floatx16* acc) {
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      const int row = tile_row(r, h);  // swizzle: 8 h + (4 (row / 8 % 2) + row % 4), the latter of r alone
+      const uint32_t at = tile + row * RB + (((n >> 2) ^ (h << 3) ^ (((r >> 2) & 1) << 2 | (r & 3))) << 4) + (n & 3) * 4;
+#pragma unroll
+      for (int b = 0; b < NB; ++b)
+        acc[b] = mfma(*(const __attribute__((address_space(3))) float*)(uintptr_t)(at ^ (b << 7)), p[r], acc[b]);
+    }
+  }
+};
+
+template <int N>
+__device__ __forceinline__ void own_arrived(float4 (&f)[N]) {
+#pragma unroll
+  for (int i = 0; i < N; ++i) asm volatile("" : "+v"(f[i].x), "+v"(f[i].y), "+v"(f[i].z), "+v"(f[i].w));
+}
+
+// 32 tokens of a sequence: block s of a work tile
+struct Block {
+  hpd_ft_tile t;
+  int lane, n, h, wave;
+  int32_t first, i, ic;  // first token, the lane's, and the last one instead of what lies behind it
+  __device__ __forceinline__ Block(const hpd_ft_tile& tile, int32_t s) : t(tile) {
+    lane = threadIdx.x & 63;
+    n = lane & 31;
+    h = lane >> 5;
+    wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    first = t.row0 + s * 32;
+    i = first + n;
+    ic = min(i, t.len - 1);
+  }
+};
+
+// Two tiles of every wave; at the end its sums, row by row
+template <int DP>
+union Shared {
+  struct {
+    float sums[4][32][DP + 4];
+    float m[4][32], l[4][32];
+  } end;
+  char tiles[4][2 * Tile<DP>::BYTES];
+};
+template <int DP>
+__device__ __forceinline__ void put(Shared<DP>& sh, const Block& w, const floatx16* acc, float f) {
+#pragma unroll
+  for (int b = 0; b < DP / 32; ++b)
+#pragma unroll
+    for (int a = 0; a < 4; ++a)
+      *reinterpret_cast<float4*>(&sh.end.sums[w.wave][w.n][32 * b + 8 * a + 4 * w.h]) =
+          make_float4(acc[b][4 * a] * f, acc[b][4 * a + 1] * f, acc[b][4 * a + 2] * f, acc[b][4 * a + 3] * f);
+}
+// the sum of the waves' rows r to out + r * stride
+template <int DP>
+__device__ __forceinline__ void join(const Shared<DP>& sh, const Block& w, float* out, int64_t stride, int32_t D) {
+  for (int x = threadIdx.x; x < 32 * DP / 4; x += 256) {
+    const int r = x / (DP / 4), c = x % (DP / 4) * 4;
+    if (w.first + r >= w.t.len || c >= D) continue;
+    float4 s = *reinterpret_cast<const float4*>(&sh.end.sums[0][r][c]);
+#pragma unroll
+    for (int y = 1; y < 4; ++y) {
+      const float4 z = *reinterpret_cast<const float4*>(&sh.end.sums[y][r][c]);
+      s.x += z.x; s.y += z.y; s.z += z.z; s.w += z.w;
+    }
+    *reinterpret_cast<float4*>(out + r * stride + c) = s;
+  }
+}
+
+// What the forward and the dq kernel share: 32 queries of a head and the blocks of keys that they see
+template <int DP>
+struct Queries : Block {
+  using TL = Tile<DP>;
+  const FtArgs& a;
+  int32_t hq, hk, own, q_min, q_max;
+  const int32_t* ranks;
+  const const_i32* blk_rank;
+  const float *keys, *values;
+  uint32_t key_tile, value_tile;
+  int64_t token;
+  __device__ __forceinline__ Queries(const FtArgs& args, const float* k, const float* v, const char* tiles)
+      : Block(args.tiles[blockIdx.x / args.Hq / 4], blockIdx.x / args.Hq % 4), a(args) {
+    const int32_t G = a.Hq / a.Hkv, x = blockIdx.x % a.Hq;
+    hk = x % a.Hkv;
+    hq = hk * G + x / a.Hkv;
+    token = t.seq0 + (int64_t)ic;
+    keys = k + t.seq0 * a.sk + (int64_t)hk * a.D;
+    values = v + t.seq0 * a.sv + (int64_t)hk * a.D;
+    ranks = a.rank + t.seq0;
+    blk_rank = (const const_i32*)(uintptr_t)(a.blk_rank + t.blk0);
+    own = min(first, t.len - 1) / 32;
+    q_min = blk_rank[2 * own];
+    q_max = blk_rank[2 * own + 1];
+    key_tile = lds_address(tiles) + wave * 2 * TL::BYTES;
+    value_tile = key_tile + TL::BYTES;
+  }
+  // the wave's first block from b on that a query sees; past `own`: none
+  __device__ __forceinline__ int32_t next(int32_t b) const {
+    while (b <= own && blk_rank[2 * b] > q_max) b += 4;
+    return b;
+  }
+  __device__ __forceinline__ void load_keys(int32_t b) const {
+    TL::load(key_tile, keys, a.sk, b * 32, t.len - 1, a.D, a.rank + a.N, lane);
+  }
+  __device__ __forceinline__ void load_values(int32_t b) const {
+    TL::load(value_tile, values, a.sv, b * 32, t.len - 1, a.D, a.rank + a.N, lane);
+  }
+  __device__ __forceinline__ void mask(floatx16& s, int32_t b, int32_t rank_i) const {
+    if (b < own && blk_rank[2 * b + 1] <= q_min) return;
+    BlockRanks rk;
+    rk.load(ranks + b * 32);
+#pragma unroll
+    for (int r = 0; r < 16; ++r) s[r] = b * 32 + tile_row(r, h) <= ic && rk.of(r, h) <= rank_i ? s[r] : -INFINITY;
+  }
+};
+
+template <int DP>
+__global__ void __launch_bounds__(256, DP > 64 ? 1 : 2) ft_f32_forward_kernel(FtArgs a, const float* __restrict__ q,
+                                                                            const float* __restrict__ k,
+                                                                            const float* __restrict__ v, float* __restrict__ out,
+                                                                            float* __restrict__ lse) {
+  using TL = Tile<DP>;
+  __shared__ __attribute__((aligned(1024))) Shared<DP> sh;
+  const Queries<DP> w(a, k, v, &sh.tiles[0][0]);
+  if (w.first >= w.t.len) return;
+  int32_t b = w.next(w.wave);
+  if (b <= w.own) {
+    w.load_keys(b);
+    w.load_values(b);
+  }
+  typename TL::Own qf;
+  TL::load(qf, q + w.token * a.sq + (int64_t)w.hq * a.D, w.h, a.D);
+  int32_t rank_i[1] = {w.ranks[w.ic]};
+  own_arrived(qf.f);
+  arrived(rank_i);
+  const float c = a.scale * LOG2E;
+  const uint32_t at = TL::row_offset(w.n, w.h);
+  floatx16 acc[TL::NB];
+  zero(acc, TL::NB);
+  float m = NEG_BIG, l = 0.f;  // maximum (log2 units), this lane's share of the sum
+  while (b <= w.own) {
+    const int32_t after = w.next(b + 4);
+    wait_vector_memory<TL::LOADS>();  // the keys; the values were requested behind them
+    floatx16 s = TL::scores(w.key_tile, at, qf, floatx16{});
+    if (after <= w.own) w.load_keys(after);
+    w.mask(s, b, rank_i[0]);
+    float p[16], top = s[0];
+#pragma unroll
+    for (int r = 1; r < 16; ++r) top = fmaxf(top, s[r]);
+    top = fmaxf(m, fmaxf(top, __shfl_xor(top, 32)) * c);
+    const float alpha = fast_exp2(m - top);
+    m = top;
+    l *= alpha;
+#pragma unroll
+    for (int x = 0; x < TL::NB; ++x)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) acc[x][r] *= alpha;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      p[r] = fast_exp2(fmaf(s[r], c, -m));
+      l += p[r];
+    }
+    if (after <= w.own) wait_vector_memory<TL::LOADS>();  // the values
+    else wait_vector_memory<0>();
+    TL::add(w.value_tile, w.n, w.h, p, acc);
+    if (after <= w.own) w.load_values(after);
+    b = after;
+  }
+  __syncthreads();
+  l += __shfl_xor(l, 32);
+  if (w.h == 0) {
+    sh.end.m[w.wave][w.n] = m;
+    sh.end.l[w.wave][w.n] = l;
+  }
+  __syncthreads();
+  const float top = fmaxf(fmaxf(sh.end.m[0][w.n], sh.end.m[1][w.n]), fmaxf(sh.end.m[2][w.n], sh.end.m[3][w.n]));
+  float total = 0.f;
+#pragma unroll
+  for (int x = 0; x < 4; ++x) total = fmaf(sh.end.l[x][w.n], fast_exp2(sh.end.m[x][w.n] - top), total);
+  put<DP>(sh, w, acc, fast_exp2(m - top) / total);
+  if (w.wave == 0 && w.h == 0 && w.i < w.t.len) lse[w.hq * a.N + w.token] = (top + __builtin_amdgcn_logf(total)) * LN2;
+  __syncthreads();
+  join<DP>(sh, w, out + ((w.t.seq0 + (int64_t)w.first) * a.Hq + w.hq) * a.D, (int64_t)a.Hq * a.D, a.D);
+}
+
+// delta_i = do_i . o_i: 16 lanes a row
+__global__ void __launch_bounds__(256) ft_f32_delta_kernel(int64_t N, int32_t Hq, int32_t D, const float* __restrict__ out,
+                                                         const float* __restrict__ d_out, float* __restrict__ delta) {
+  const int64_t row = (int64_t)blockIdx.x * 16 + threadIdx.x / 16;
+  if (row >= N * Hq) return;
+  float s = 0.f;
+  for (int32_t c = (threadIdx.x % 16) * 4; c < D; c += 64) {
+    const float4 x = *reinterpret_cast<const float4*>(out + row * D + c), y = *reinterpret_cast<const float4*>(d_out + row * D + c);
+    s = fmaf(x.x, y.x, fmaf(x.y, y.y, fmaf(x.z, y.z, fmaf(x.w, y.w, s))));
+  }
+#pragma unroll
+  for (int d = 8; d; d >>= 1) s += __shfl_xor(s, d);
+  if (threadIdx.x % 16 == 0) delta[(row % Hq) * N + row / Hq] = s;
+}
+
+// Products in the order do . v, q . k, ds . k: the next values are on their way during the last two, the next keys
+// during the first.
+template <int DP>
+__global__ void __launch_bounds__(256, DP > 64 ? 1 : 2) ft_f32_dq_kernel(FtArgs a, const float* __restrict__ q,
+                                                                       const float* __restrict__ k, const float* __restrict__ v,
+                                                                       const float* __restrict__ d_out,
+                                                                       const float* __restrict__ lse,
+                                                                       const float* __restrict__ delta, float* __restrict__ dq) {
+  using TL = Tile<DP>;
+  __shared__ __attribute__((aligned(1024))) Shared<DP> sh;
+  const Queries<DP> w(a, k, v, &sh.tiles[0][0]);
+  if (w.first >= w.t.len) return;
+  int32_t b = w.next(w.wave);
+  if (b <= w.own) {
+    w.load_values(b);
+    w.load_keys(b);
+  }
+  typename TL::Own qf, of;
+  TL::load(qf, q + w.token * a.sq + (int64_t)w.hq * a.D, w.h, a.D);
+  TL::load(of, d_out + (w.token * a.Hq + w.hq) * a.D, w.h, a.D);
+  float row[2] = {lse[w.hq * a.N + w.token], delta[w.hq * a.N + w.token]};
+  int32_t rank_i[1] = {w.ranks[w.ic]};
+  own_arrived(qf.f);
+  own_arrived(of.f);
+  arrived(row);
+  arrived(rank_i);
+  const float c = a.scale * LOG2E, lse2 = row[0] * LOG2E;
+  const uint32_t at = TL::row_offset(w.n, w.h);
+  floatx16 acc[TL::NB];
+  zero(acc, TL::NB);
+  while (b <= w.own) {
+    const int32_t after = w.next(b + 4);
+    wait_vector_memory<TL::LOADS>();  // the values; the keys were requested behind them
+    const floatx16 dp = TL::scores(w.value_tile, at, of, floatx16{});
+    if (after <= w.own) {
+      w.load_values(after);
+      wait_vector_memory<TL::LOADS>();
+    } else {
+      wait_vector_memory<0>();
+    }
+    floatx16 s = TL::scores(w.key_tile, at, qf, floatx16{});
+    w.mask(s, b, rank_i[0]);
+    float ds[16];
+#pragma unroll
+    for (int r = 0; r < 16; ++r) ds[r] = fast_exp2(fmaf(s[r], c, -lse2)) * (dp[r] - row[1]);
+    TL::add(w.key_tile, w.n, w.h, ds, acc);
+    if (after <= w.own) w.load_keys(after);
+    b = after;
+  }
+  __syncthreads();
+  put<DP>(sh, w, acc, a.scale);
+  __syncthreads();
+  join<DP>(sh, w, dq + (w.t.seq0 + (int64_t)w.first) * a.sdq + (int64_t)w.hq * a.D, a.sdq, a.D);
+}
+
+// Products in the order q . k, do . v, ds . q, p . do: the next queries are on their way during the last, the next
+// gradients of the output during the first.
+template <int DP>
+__global__ void __launch_bounds__(256, DP > 64 ? 1 : 2) ft_f32_dkv_kernel(FtArgs a, const float* __restrict__ q,
+                                                                        const float* __restrict__ k, const float* __restrict__ v,
+                                                                        const float* __restrict__ d_out,
+                                                                        const float* __restrict__ lse,
+                                                                        const float* __restrict__ delta, float* __restrict__ dk,
+                                                                        float* __restrict__ dv) {
+  using TL = Tile<DP>;
+  __shared__ __attribute__((aligned(1024))) Shared<DP> sh;
+  __shared__ __attribute__((aligned(256))) float stats[4][64];  // of every wave: lse, then delta of its 32 queries
+  // the block's values, for 128 channels: the registers are full
+  constexpr bool LDS_VALUES = DP > 64;
+  __shared__ __attribute__((aligned(1024))) char values[LDS_VALUES ? TL::BYTES : 16];
+  const int32_t G = a.Hq / a.Hkv, hk = blockIdx.x % a.Hkv, rest = blockIdx.x / a.Hkv;
+  const Block w(a.tiles[rest / 4], rest % 4);
+  if (w.first >= w.t.len) return;
+  const int32_t* const ranks = a.rank + w.t.seq0;
+  const const_i32* const blk_rank = (const const_i32*)(uintptr_t)(a.blk_rank + w.t.blk0);
+  const int64_t token = w.t.seq0 + (int64_t)w.ic, so = (int64_t)a.Hq * a.D;
+  const int32_t own = w.first / 32, blocks = (w.t.len + 31) / 32, k_min = blk_rank[2 * own], k_max = blk_rank[2 * own + 1];
+  const uint32_t q_tile = lds_address(&sh.tiles[0][0]) + w.wave * 2 * TL::BYTES, o_tile = q_tile + TL::BYTES;
+  // the wave takes every fourth (head, block of queries)
+  struct Where { int32_t g, b; };
+  auto settle = [&](Where x) -> Where {  // the first from x on with a query that sees a key; head G: none
+    for (;; x.b += 4) {
+      while (x.b >= blocks && x.g < G) {
+        x.b += own - blocks;
+        ++x.g;
+      }
+      if (x.g >= G || k_min <= blk_rank[2 * x.b + 1]) return x;
+    }
+  };
+  auto load_queries = [&](Where x) {
+    TL::load(q_tile, q + w.t.seq0 * a.sq + (int64_t)(hk * G + x.g) * a.D, a.sq, x.b * 32, w.t.len - 1, a.D, a.rank + a.N, w.lane);
+  };
+  auto load_gradients = [&](Where x) {
+    const int32_t hq = hk * G + x.g;
+    TL::load(o_tile, d_out + w.t.seq0 * so + (int64_t)hq * a.D, so, x.b * 32, w.t.len - 1, a.D, a.rank + a.N, w.lane);
+    const float* p = (w.h ? delta : lse) + hq * a.N + w.t.seq0 + min(x.b * 32 + w.n, w.t.len - 1);
+    const uint32_t dst = __builtin_amdgcn_readfirstlane(lds_address(&stats[w.wave][0]));
+    uint32_t keep;
+    asm volatile(
+        "s_mov_b32 %0, m0\n\ts_mov_b32 m0, %2\n\ts_nop 0\n\t"
+        "global_load_lds_dword %1, off\n\ts_mov_b32 m0, %0"
+        : "=&s"(keep)
+        : "v"(p), "s"(dst)
+        : "memory");
+  };
+  if (LDS_VALUES) {
+    if (w.wave == 0) {
+      TL::load(lds_address(values), v + w.t.seq0 * a.sv + (int64_t)hk * a.D, a.sv, w.first, w.t.len - 1, a.D, a.rank + a.N, w.lane);
+      wait_vector_memory<0>();
+    }
+    __syncthreads();
+  }
+  Where x = settle({0, own + w.wave});
+  if (x.g < G) {
+    load_queries(x);
+    load_gradients(x);
+  }
+  typename TL::Own kf, vf;
+  TL::load(kf, k + token * a.sk + (int64_t)hk * a.D, w.h, a.D);
+  if (!LDS_VALUES) TL::load(vf, v + token * a.sv + (int64_t)hk * a.D, w.h, a.D);
+  int32_t rank_j[1] = {ranks[w.ic]};
+  own_arrived(kf.f);
+  if (!LDS_VALUES) own_arrived(vf.f);
+  arrived(rank_j);
+  const float c = a.scale * LOG2E;
+  const uint32_t at = TL::row_offset(w.n, w.h);
+  floatx16 acc_k[TL::NB], acc_v[TL::NB];
+  zero(acc_k, TL::NB);
+  zero(acc_v, TL::NB);
+  while (x.g < G) {
+    const Where after = settle({x.g, x.b + 4});
+    wait_vector_memory<TL::LOADS + 1>();  // the queries; the gradients and the rows' numbers were requested behind them
+    floatx16 s = TL::scores(q_tile, at, kf, floatx16{});
+    wait_vector_memory<0>();
+    const floatx16 dp = LDS_VALUES ? TL::scores(o_tile, at, lds_address(values), floatx16{})
+                                   : TL::scores(o_tile, at, vf, floatx16{});
+    if (x.b == own || k_max > blk_rank[2 * x.b] || (x.b + 1) * 32 > w.t.len) {
+      BlockRanks rk;
+      rk.load(ranks + x.b * 32);
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const int32_t i = x.b * 32 + tile_row(r, w.h);
+        s[r] = i < w.t.len && i >= w.i && rank_j[0] <= rk.of(r, w.h) ? s[r] : -INFINITY;
+      }
+    }
+    float p[16], ds[16];
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      p[r] = fast_exp2(fmaf(s[r], c, -LOG2E * stats[w.wave][tile_row(r, w.h)]));
+      ds[r] = p[r] * (dp[r] - stats[w.wave][32 + tile_row(r, w.h)]);
+    }
+    TL::add(q_tile, w.n, w.h, ds, acc_k);
+    if (after.g < G) load_queries(after);
+    TL::add(o_tile, w.n, w.h, p, acc_v);
+    if (after.g < G) load_gradients(after);
+    x = after;
+  }
+  __syncthreads();
+  put<DP>(sh, w, acc_v, 1.f);
+  __syncthreads();
+  join<DP>(sh, w, dv + (w.t.seq0 + (int64_t)w.first) * a.sdv + (int64_t)hk * a.D, a.sdv, a.D);
+  __syncthreads();
+  put<DP>(sh, w, acc_k, a.scale);
+  __syncthreads();
+  join<DP>(sh, w, dk + (w.t.seq0 + (int64_t)w.first) * a.sdk + (int64_t)hk * a.D, a.sdk, a.D);
+}
+
+template <int DP>
+hipError_t forward(const hpd_finetune_layout* L, const FtArgs& a, const float* q, const float* k, const float* v, float* out,
+                   float* lse, hipStream_t s) {
+  ft_f32_forward_kernel<DP><<<dim3((unsigned)L->tiles.size() * 4 * a.Hq), 256, 0, s>>>(a, q, k, v, out, lse);
+  return hipGetLastError();
+}
+
+template <int DP>
+hipError_t backward(const hpd_finetune_layout* L, FtArgs a, const float* q, const float* k, const float* v, const float* out,
+                    const float* lse, const float* d_out, float* dq, float* dk, float* dv, float* delta, hipStream_t s) {
+  ft_f32_delta_kernel<<<dim3((unsigned)((a.N * a.Hq + 15) / 16)), 256, 0, s>>>(a.N, a.Hq, a.D, out, d_out, delta);
+  const unsigned blocks = (unsigned)L->tiles.size() * 4;
+  ft_f32_dq_kernel<DP><<<dim3(blocks * a.Hq), 256, 0, s>>>(a, q, k, v, d_out, lse, delta, dq);
+  a.tiles = L->d_key_tiles;
+  ft_f32_dkv_kernel<DP><<<dim3(blocks * a.Hkv), 256, 0, s>>>(a, q, k, v, d_out, lse, delta, dk, dv);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t hpd_launch_ft_f32_forward(const hpd_finetune_layout* L, FtArgs a, const void* q, const void* k, const void* v,
+                                     void* out, float* lse, hipStream_t s) {
+  const auto run = a.D <= 64 ? forward<64> : forward<128>;
+  return run(L, a, (const float*)q, (const float*)k, (const float*)v, (float*)out, lse, s);
+}
+
+hipError_t hpd_launch_ft_f32_backward(const hpd_finetune_layout* L, FtArgs a, const void* q, const void* k, const void* v,
+                                      const void* out, const float* lse, const void* d_out, void* dq, void* dk, void* dv,
+                                      void* workspace, hipStream_t s) {
+  const auto run = a.D <= 64 ? backward<64> : backward<128>;
+  return run(L, a, (const float*)q, (const float*)k, (const float*)v, (const float*)out, lse, (const float*)d_out, (float*)dq,
+             (float*)dk, (float*)dv, (float*)workspace, s);
+}

@@ -11,18 +11,7 @@
 
 namespace {
 
-typedef uint32_t uint4v __attribute__((ext_vector_type(4)));
 constexpr uint32_t BIAS = 4096;  // keeps a lane's offset positive (see Loader)
-
-__device__ __forceinline__ void wait_lds_and_barrier() {
-  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-  __builtin_amdgcn_s_barrier();
-  asm volatile("" ::: "memory");
-}
-template <int N>
-__device__ __forceinline__ void wait_vector_memory() {
-  asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
-}
 
 template <int D>
 struct Rows {
@@ -97,17 +86,6 @@ struct Loader {
   }
 };
 
-// Waits for values loaded in front of a loop.  The compiler would wait for them inside it, at every turn, and so
-// for the loads to LDS that follow them, which it does not see.
-template <typename T, int N>
-__device__ __forceinline__ void arrived(T (&v)[N]) {
-#pragma unroll
-  for (int i = 0; i < N; ++i) asm volatile("" : "+v"(v[i]));
-}
-
-__device__ __forceinline__ uint32_t lds_address(const void* p) {
-  return (uint32_t)reinterpret_cast<uintptr_t>((const __attribute__((address_space(3))) char*)p);
-}
 __device__ __forceinline__ bf16x8 lds_read(uint32_t at) {
   return __builtin_bit_cast(bf16x8, *(const __attribute__((address_space(3))) uint4v*)(uintptr_t)at);
 }
@@ -117,23 +95,6 @@ __device__ __forceinline__ uint2 lds_read_tr(uint32_t at) {
 __device__ __forceinline__ floatx16 mfma(bf16x8 a, bf16x8 b, floatx16 c) {
   return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
 }
-// the ranks of a block's 32 tokens in scalar registers (wave-uniform address)
-typedef int32_t int32x16 __attribute__((ext_vector_type(16)));
-struct BlockRanks {
-  int32x16 lo, hi;
-  __device__ __forceinline__ void load(const int32_t* p) {
-    p = reinterpret_cast<const int32_t*>(uniform(reinterpret_cast<const char*>(p)));
-    asm volatile("s_load_dwordx16 %0, %2, 0x0\n\ts_load_dwordx16 %1, %2, 0x40\n\ts_waitcnt lgkmcnt(0)"
-                 : "=&s"(lo), "=&s"(hi) : "s"(p) : "memory");
-  }
-  __device__ __forceinline__ int32_t at(int row) const { return row < 16 ? lo[row] : hi[row - 16]; }
-  // of register r's row in half h
-  __device__ __forceinline__ int32_t of(int r, int h) const {
-    const int32_t x = at(tile_row(r, 0)), y = at(tile_row(r, 1));
-    return h ? y : x;
-  }
-};
-
 // 32 columns of a transposed result (lane n: column n) times f, as 32 rows of D values through `turn`
 // (TILE bytes of LDS of this wave's own); row r of the tile goes to out + r * stride, r < rows
 template <int D>
