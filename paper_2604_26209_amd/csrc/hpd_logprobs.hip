@@ -1,10 +1,12 @@
 // Log probabilities of given tokens with entropy and the most likely alternatives, and their gradient.
 //
-// With m = max x, s = sum exp(x - m), t = sum exp(x - m) (x - m):
-//   lse = m + log s,  logprob = x_target - lse,  entropy = log s - t / s.
-// One pass over the logits: every lane keeps (m, s, t) of its share and rescales s and t when its
-// maximum moves (t' = (t - d s) e^-d for a maximum that rises by d); partial results are joined by the
-// same rule.  The pass is bound by the bytes of the logits.
+// In log2 units, y = x log2(e), with a reference point k, s = sum 2^(y - k), t = sum 2^(y - k) (y - k):
+//   lse = (k + log2 s) ln 2,  logprob = (y_target - k - log2 s) ln 2,  entropy = (log2 s - t / s) ln 2.
+// One pass over the logits: every lane keeps (k, s, t) of its share; k is a whole number not below the lane's maximum, so
+// that y - k is one multiply-add and moving k by d is exact: t' = (t - d s) 2^-d, s' = s 2^-d.  Partial
+// results are joined by the same rule.  The pass is bound by the bytes of the logits, with the vector instructions (an exponential
+// and five to six more per logit) close behind: 6144 x 130013 bf16 logits with one alternative 295 us, 5.4 TB/s; without 5.4,
+// with eight 4.0, with fifty 3.3 TB/s.
 //
 // Alternatives: a wave keeps its 64 largest (value, index) keys, lane i the i-th.  A vector of logits
 // costs one comparison of its maximum with the K-th; what passes is collected and sorted in, 64 at a time.
@@ -19,7 +21,7 @@
 namespace {
 
 constexpr float LOG2E = 1.44269504088896340736f;
-constexpr float LOWEST = -3.402823466e38f;
+constexpr float LN2 = 0.69314718055994530942f;
 constexpr int UNROLL = 4;          // vectors in flight per lane
 constexpr int64_t MAX_GRID = 1 << 20;
 
@@ -61,32 +63,79 @@ struct Vec<hpd::bf16_t> {
 };
 
 // ---- sums
+constexpr float HUGE_LOGIT = 1.0e38f;  // beyond it x log2(e) may not be finite
+constexpr float LOWEST_REFERENCE = -1.25f * HUGE_LOGIT;  // below x log2(e) / 4 of every finite logit
 struct Sums {
-  float m, s, t;
+  float m;  // largest logit
+  float r;  // reference point / 4 (finite for every finite logit)
+  float s, t;
 };
-// exp and x - m of one logit; -infinity counts nothing, NaN and +infinity make s NaN
-__device__ __forceinline__ void add_logit(Sums& a, float x) {
-  const float d = x - a.m, e = fast_exp2(d * LOG2E);
-  a.s += e;
-  a.t = fmaf(e, fmaxf(d, -200.f), a.t);
-}
-// raises the maximum to m >= a.m
-__device__ __forceinline__ void raise(Sums& a, float m) {
-  const float d = fminf(m - a.m, 1.0e4f), f = fast_exp2(-d * LOG2E);
+__device__ __forceinline__ Sums no_sums() { return {-INFINITY, -0.25f * HUGE_LOGIT, 0.f, 0.f}; }
+// raises the reference point to 4 r >= 4 a.r
+__device__ __forceinline__ void raise(Sums& a, float r) {
+  const float d = fminf(4.f * (r - a.r), 1.0e4f), f = fast_exp2(-d);
   a.t = fmaf(-d, a.s, a.t) * f;
   a.s *= f;
-  a.m = m;
+  a.r = r;
 }
 __device__ __forceinline__ Sums join(Sums a, Sums b) {
-  const float m = fmaxf(a.m, b.m);
-  raise(a, m);
-  raise(b, m);
-  return {m, a.s + b.s, a.t + b.t};
+  if (a.s == 0.f) a.r = LOWEST_REFERENCE;  // (nothing there: its reference point says nothing)
+  if (b.s == 0.f) b.r = LOWEST_REFERENCE;
+  const float r = fmaxf(a.r, b.r);
+  raise(a, r);
+  raise(b, r);
+  return {fmaxf(a.m, b.m), r, a.s + b.s, a.t + b.t};
 }
 __device__ __forceinline__ Sums join_wave(Sums a) {
 #pragma unroll
-  for (int d = 32; d; d >>= 1) a = join(a, {__shfl_xor(a.m, d), __shfl_xor(a.s, d), __shfl_xor(a.t, d)});
+  for (int d = 32; d; d >>= 1) a = join(a, {__shfl_xor(a.m, d), __shfl_xor(a.r, d), __shfl_xor(a.s, d), __shfl_xor(a.t, d)});
   return a;
+}
+// (y - k) / 4 of a logit.  WIDE: the reference point is the rounded y of the largest logit, and has to be met.
+template <bool WIDE>
+__device__ __forceinline__ float quarter(float x, float r) {
+  if (!WIDE) return fmaf(x, 0.25f * LOG2E, -r);
+  float y = x * (0.25f * LOG2E);
+  asm("" : "+v"(y));  // (rounded: no multiply-add)
+  return y - r;
+}
+// The logits of one vector.  -infinity counts nothing, NaN and +infinity make s NaN.  WIDE: for rows whose largest logit
+// is beyond HUGE_LOGIT in magnitude.
+template <int N, bool WIDE>
+__device__ __forceinline__ void add_logits(Sums& a, const float* x, float m) {
+  a.m = fmaxf(a.m, m);
+  if constexpr (WIDE) {
+    const float r = m * (0.25f * LOG2E);
+    if (r > a.r) raise(a, r);
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const float d = 4.f * quarter<WIDE>(x[i], a.r), e = fast_exp2(d);
+      a.s += e;
+      a.t = fmaf(e, fmaxf(d, -200.f), a.t);
+    }
+  } else {
+    const float y = m * LOG2E;
+    if (y > 4.f * a.r) raise(a, 0.25f * ceilf(y));
+    float low = x[0];
+#pragma unroll
+    for (int i = 1; i < N; ++i) low = fminf(low, x[i]);
+    const float k = 4.f * a.r;
+    if (__any(low < -0.1f * HUGE_LOGIT)) {
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        const float d = fmaf(x[i], LOG2E, -k), e = fast_exp2(d);
+        a.s += e;
+        a.t = fmaf(e, fmaxf(d, -200.f), a.t);  // (0 times -infinity)
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        const float d = fmaf(x[i], LOG2E, -k), e = fast_exp2(d);
+        a.s += e;
+        a.t = fmaf(e, d, a.t);
+      }
+    }
+  }
 }
 
 // ---- keys: larger = larger logit, then lower index; 0 = none
@@ -155,29 +204,27 @@ __device__ __forceinline__ K sort_down(K k, int lane) {
 }
 
 // The K largest keys of what a wave has seen: the sorted list, and a buffer of candidates in LDS that is
-// sorted into it when it is full.  Candidates are those above the K-th of the list as it was
-// then; the more logits have been seen, the rarer they are.
+// sorted into it when it is full.  Candidates are the keys above a bar that rises with what has been seen.
 struct Top {
   uint64_t list = 0;  // lane i: the i-th largest
   uint64_t last = 0;  // what a candidate has to exceed, in every lane
   float bar = 0.f;    // its value, once there is one
   bool full = false;
-  int count = 0;           // candidates in the buffer
-  uint64_t* buffer = nullptr;  // 128 keys of this wave
+  int count = 0;               // candidates in the buffer
+  uint64_t* buffer = nullptr;  // BUFFER keys of this wave
   // (a wave's LDS accesses happen in order; what other lanes have written is behind the compiler's back)
   static __device__ __forceinline__ void order() { asm volatile("" ::: "memory"); }
+  // sorts the last 64 candidates in, or what there is
   __device__ __forceinline__ void flush(int K, int lane) {
     const int n = min(count, 64);
+    uint64_t* const from = buffer + count - n;
     order();
-    uint64_t c = lane < n ? buffer[lane] : 0;
-    const uint64_t rest = lane + 64 < count ? buffer[lane + 64] : 0;
-    c = sort_down(c, lane);
+    const uint64_t c = sort_down(lane < n ? from[lane] : 0, lane);
     order();
-    buffer[64 + lane] = c;  // turned around through LDS: the list and the candidates are one bitonic sequence
+    buffer[count - n + lane] = c;  // turned around through LDS: the list and the candidates are one bitonic sequence
     order();
-    list = settle(larger(list, buffer[64 + 63 - lane]), lane);
+    list = settle(larger(list, from[63 - lane]), lane);
     order();
-    buffer[lane] = rest;
     count -= n;
     const uint64_t k = read_lane(list, K - 1);
     if (k > last) last = k;
@@ -193,111 +240,151 @@ struct Top {
     if (mask == 0) return;
     if (in) buffer[count + __builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, 0))] = key;
     count += __popcll(mask);
-    order();
-    if (count >= 64) flush(K, lane);
   }
-  // m: the largest logit of each lane's share of what comes next.  The K-th largest of these is reached by K logits.
-  __device__ __forceinline__ void expect(float m, int K, int lane) {
-    const uint32_t o = (uint32_t)(make_key(m, 0) >> 32);
-    const uint32_t k = (uint32_t)__builtin_amdgcn_readlane((int)sort_down(o, lane), K - 1);
-    last = ((uint64_t)k << 32) - 1;
-    bar = key_value((uint64_t)k << 32);
+  // m: each lane's largest logit of what has been seen or comes next.  The K-th largest of the 64 is one that K logits reach.
+  __device__ __forceinline__ void raise_bar(float m, int K, int lane) {
+    uint32_t o = (uint32_t)(make_key(m, 0) >> 32);
+    if (K == 1) {
+      o = larger(o, lane_xor<1>(o, lane));
+      o = larger(o, lane_xor<2>(o, lane));
+      o = larger(o, lane_xor<4>(o, lane));
+      o = larger(o, lane_xor<8>(o, lane));
+      o = larger(o, lane_xor<16>(o, lane));
+      o = larger(o, lane_xor<32>(o, lane));
+    } else {
+      o = sort_down(o, lane);
+    }
+    o = (uint32_t)__builtin_amdgcn_readlane((int)o, K - 1);
+    const uint64_t k = ((uint64_t)o << 32) - 1;
+    if (k > last) {
+      last = k;
+      bar = key_value((uint64_t)o << 32);
+    }
     full = true;
   }
   // the largest of two sorted lists; other: in LDS
   __device__ __forceinline__ void merge(const uint64_t* other, int lane) { list = settle(larger(list, other[63 - lane]), lane); }
 };
 
+constexpr int BUFFER = 64 + 8 * 64 + 64;  // what a flush leaves, a vector of every lane, room for a flush to write 64
 struct Shared {
-  uint64_t keys[4][128];  // every wave's candidates, then its list
+  uint64_t keys[4][BUFFER];  // every wave's candidates, then its list
   Sums sums[4];
 };
 
-// results of a row, by one wave (x - m - log s: where all logits lie far from 0, log s is less than a step of lse)
+// results of a row, by one wave (y - k - log2 s: where all logits lie far from 0, log s is less than a step of lse)
 __device__ __forceinline__ void finish(const hpd_logprobs_args& a, int64_t row, Sums s, uint64_t list, float x_target,
                                        bool has_target, int lane) {
   const bool none = s.s == 0.f;  // nothing but -infinity
-  const float log_s = logf(s.s), lse = none ? -INFINITY : s.m + log_s;
+  const float log_s = log2f(s.s);
+  auto log_probability = [&](float x) {
+    const float d = fabsf(s.m) > HUGE_LOGIT ? quarter<true>(x, s.r) : quarter<false>(x, s.r);
+    return none ? -INFINITY : fmaf(d, 4.f * LN2, -log_s * LN2);
+  };
   if (lane == 0) {
-    if (a.lse) a.lse[row] = lse;
-    if (a.entropy) a.entropy[row] = none ? 0.f : log_s - s.t / s.s;
-    if (a.targets && a.logprob) a.logprob[row] = !has_target ? 0.f : none ? -INFINITY : x_target - s.m - log_s;
+    if (a.lse) a.lse[row] = none ? -INFINITY : fmaf(s.r, 4.f * LN2, log_s * LN2);
+    if (a.entropy) a.entropy[row] = none ? 0.f : (log_s - s.t / s.s) * LN2;
+    if (a.targets && a.logprob) a.logprob[row] = has_target ? log_probability(x_target) : 0.f;
   }
   if (lane < a.top_k) {
     a.top_id[row * a.top_k + lane] = (int32_t)~(uint32_t)list;
-    a.top_logprob[row * a.top_k + lane] = none ? -INFINITY : key_value(list) - s.m - log_s;
+    a.top_logprob[row * a.top_k + lane] = log_probability(key_value(list));
   }
 }
 
 // The piece [begin, end) of a row by WV waves, of which this is number w.
-template <typename T, bool TOP>
+template <typename T, bool TOP, bool WIDE>
 __device__ __forceinline__ void scan(const T* x, int32_t begin, int32_t end, int w, int WV, int K, int lane, Sums& sums, Top& top) {
   using V = Vec<T>;
-  sums = {LOWEST, 0.f, 0.f};
-  // one vector per lane, the first logit of which is number `index`; n of its logits exist
-  auto take = [&](const float* f, int32_t index, int n) __attribute__((always_inline)) {
+  sums = no_sums();
+  if (WIDE) sums.r = LOWEST_REFERENCE;
+  // one vector per lane, the first logit of which is number `index`; its logits first .. last - 1 count
+  auto take = [&](const float* f, int32_t index, int first, int last) __attribute__((always_inline)) {
     float m = f[0];
 #pragma unroll
     for (int e = 1; e < V::N; ++e) m = fmaxf(m, f[e]);
-    if (m > sums.m) raise(sums, m);
-#pragma unroll
-    for (int e = 0; e < V::N; ++e) add_logit(sums, f[e]);
+    add_logits<V::N, WIDE>(sums, f, m);
     if constexpr (TOP) {
       if (__any(!top.full || m >= top.bar)) {
 #pragma unroll
-        for (int e = 0; e < V::N; ++e) top.add(e < n ? make_key(f[e], index + e) : 0, K, lane);
+        for (int e = 0; e < V::N; ++e) top.add(e >= first && e < last ? make_key(f[e], index + e) : 0, K, lane);
+        while (top.count >= 64) top.flush(K, lane);
       }
     }
   };
   constexpr int32_t STEP = 64 * V::N, RUN = STEP * UNROLL;  // logits of a vector of all lanes, of a turn of the wave
-  int32_t at = begin + w * RUN;
-  for (; at + RUN <= end; at += WV * RUN) {
+  int32_t at = begin + w * RUN, turns = 0;
+  for (; at + RUN <= end; at += WV * RUN, ++turns) {
     typename V::Raw r[UNROLL];
 #pragma unroll
     for (int u = 0; u < UNROLL; ++u) r[u] = *reinterpret_cast<const typename V::Raw*>(x + at + u * STEP + lane * V::N);
     if constexpr (TOP) {
-      if (!top.full) {  // the first turn
-        float m = -INFINITY;
+      if (turns == 0 || turns == 3) {  // (later the candidates themselves raise it, 64 at a time)
+        float m = sums.m;
+        if (turns == 0) {
 #pragma unroll
-        for (int u = 0; u < UNROLL; ++u) {
-          float f[V::N];
-          V::unpack(r[u], f);
+          for (int u = 0; u < UNROLL; ++u) {
+            float f[V::N];
+            V::unpack(r[u], f);
 #pragma unroll
-          for (int e = 0; e < V::N; ++e) m = fmaxf(m, f[e]);
+            for (int e = 0; e < V::N; ++e) m = fmaxf(m, f[e]);
+          }
         }
-        top.expect(m, K, lane);
+        top.raise_bar(m, K, lane);
       }
     }
 #pragma unroll
     for (int u = 0; u < UNROLL; ++u) {
       float f[V::N];
       V::unpack(r[u], f);
-      take(f, at + u * STEP + lane * V::N, V::N);
+      take(f, at + u * STEP + lane * V::N, 0, V::N);
     }
   }
-  // the wave's part of a turn that the end cuts: vectors that are not whole logit by logit, -infinity behind the end
+  // The wave's part of a turn that the end cuts.  A lane whose vector is not whole takes the last N logits and leaves out
+  // those that are not its own (a piece of fewer than N: one by one).
   if (at < end) {
     typename V::Raw r[UNROLL];
-#pragma unroll
-    for (int u = 0; u < UNROLL; ++u)
-      if (at + u * STEP + (lane + 1) * V::N <= end)
-        r[u] = *reinterpret_cast<const typename V::Raw*>(x + at + u * STEP + lane * V::N);
+    auto first_of = [&](int u) __attribute__((always_inline)) -> int32_t {  // of the lane's own logits
+      return at + u * STEP + lane * V::N;
+    };
+    auto from_of = [&](int u) __attribute__((always_inline)) -> int32_t { return max(min(first_of(u), end - V::N), begin); };
 #pragma unroll
     for (int u = 0; u < UNROLL; ++u) {
-      const int32_t index = at + u * STEP + lane * V::N;
+      if (first_of(u) >= end) continue;
+      if (end - begin >= V::N) {
+        r[u] = *reinterpret_cast<const typename V::Raw*>(x + from_of(u));
+      } else {
+        T few[V::N] = {};
+#pragma unroll
+        for (int e = 0; e < V::N; ++e)
+          if (begin + e < end) few[e] = x[begin + e];
+        r[u] = __builtin_bit_cast(typename V::Raw, few);
+      }
+    }
+    auto logits_of = [&](int u, float* f) __attribute__((always_inline)) {
+      V::unpack(r[u], f);
+#pragma unroll
+      for (int e = 0; e < V::N; ++e)
+        if (from_of(u) + e < first_of(u) || from_of(u) + e >= end) f[e] = -INFINITY;
+    };
+    if constexpr (TOP) {
+      float m = sums.m;
+#pragma unroll
+      for (int u = 0; u < UNROLL; ++u) {
+        float f[V::N];
+        logits_of(u, f);
+#pragma unroll
+        for (int e = 0; e < V::N; ++e) m = fmaxf(m, f[e]);
+      }
+      top.raise_bar(m, K, lane);
+    }
+#pragma unroll
+    for (int u = 0; u < UNROLL; ++u) {
       if (at + u * STEP >= end) break;
       float f[V::N];
-      if (index + V::N <= end) {
-        V::unpack(r[u], f);
-      } else {
-#pragma unroll
-        for (int e = 0; e < V::N; ++e) f[e] = index + e < end ? hpd::to_float(x[index + e]) : -INFINITY;
-      }
-      take(f, index, end - index);
+      logits_of(u, f);
+      take(f, from_of(u), first_of(u) - from_of(u), end - from_of(u));
     }
-  }
-  if constexpr (TOP) {
-    while (top.count) top.flush(K, lane);
   }
 }
 
@@ -318,8 +405,16 @@ __global__ void __launch_bounds__(256) logprobs_kernel(hpd_logprobs_args a, int3
     Sums sums;
     Top top;
     top.buffer = sh.keys[wave];
-    scan<T, TOP>(x, begin, end, waves == 1 ? 0 : wave, waves, K, lane, sums, top);
+    scan<T, TOP, false>(x, begin, end, waves == 1 ? 0 : wave, waves, K, lane, sums, top);
     sums = join_wave(sums);
+    if (fabsf(sums.m) > HUGE_LOGIT && sums.m != -INFINITY) {
+      Top unused;
+      scan<T, false, true>(x, begin, end, waves == 1 ? 0 : wave, waves, K, lane, sums, unused);
+      sums = join_wave(sums);
+    }
+    if constexpr (TOP) {
+      while (top.count) top.flush(K, lane);
+    }
     if (waves > 1) {
       if (TOP) sh.keys[wave][lane] = top.list;
       if (lane == 0) sh.sums[wave] = sums;
@@ -339,7 +434,7 @@ __global__ void __launch_bounds__(256) logprobs_kernel(hpd_logprobs_args a, int3
         finish(a, row, sums, top.list, has ? hpd::to_float(x[t]) : 0.f, has, lane);
       } else {
         float4* ws = reinterpret_cast<float4*>(a.workspace);
-        if (lane == 0) ws[piece] = make_float4(sums.m, sums.s, sums.t, 0.f);
+        if (lane == 0) ws[piece] = make_float4(sums.m, sums.r, sums.s, sums.t);
         if (TOP && lane < K) reinterpret_cast<uint64_t*>(ws + a.n_rows * parts)[piece * K + lane] = top.list;
       }
     }
@@ -356,10 +451,10 @@ __global__ void __launch_bounds__(256) logprobs_join_kernel(hpd_logprobs_args a,
   const float4* ws = reinterpret_cast<const float4*>(a.workspace);
   const uint64_t* lists = reinterpret_cast<const uint64_t*>(ws + a.n_rows * parts);
   for (int64_t row = blockIdx.x; row < a.n_rows; row += gridDim.x) {
-    Sums sums{LOWEST, 0.f, 0.f};
+    Sums sums = no_sums();
     if (lane < parts && lane % 4 == wave) {
       const float4 p = ws[row * parts + lane];
-      sums = {p.x, p.y, p.z};
+      sums = {p.x, p.y, p.z, p.w};
     }
     Top top;
     top.buffer = sh.keys[wave];
@@ -368,6 +463,7 @@ __global__ void __launch_bounds__(256) logprobs_join_kernel(hpd_logprobs_args a,
       for (int32_t i = 0; i < n; i += 64) {
         const int32_t at = i + lane, piece = wave + at / K * 4;
         top.add(at < n ? lists[(row * parts + piece) * K + at % K] : 0, K, lane);
+        while (top.count >= 64) top.flush(K, lane);
       }
       while (top.count) top.flush(K, lane);
       sh.keys[wave][lane] = top.list;
