@@ -392,7 +392,7 @@ int hpd_finetune_mask(int32_t prompt_len, int32_t n_attr, const int32_t* attr_le
  *
  * Tensors are device memory, token-major: q, out [N][Hq][D], k, v [N][Hkv][D] in the layout's
  * dtype, N = HPD_FTC_N_TOKENS tokens, sequence after sequence, each in the order of
- * hpd_finetune_mask.  They start on 16 bytes; hpd_finetune_strides gives the distance between the
+ * hpd_finetune_mask.  They start on 16 bytes (lse on 4); hpd_finetune_strides gives the distance between the
  * tokens of those that are views of a wider buffer (a fused projection's output).  lse is fp32
  * [Hq][N], natural logarithms.  Query head h uses kv head h / (Hq/Hkv); dk and dv are sums over
  * the query heads that share them.  Sums, softmax and gradients are accumulated in fp32; under

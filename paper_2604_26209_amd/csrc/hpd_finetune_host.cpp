@@ -273,8 +273,9 @@ int hpd_finetune_attention(const hpd_finetune_layout* L, const void* q, const vo
   hpd_finetune_strides st;
   if (!complete(L, strides, &st)) return HPD_E_INVALID;
   if (L->n_tokens == 0) return HPD_OK;
-  for (const void* p : {q, k, v, (const void*)out, (const void*)lse})
+  for (const void* p : {q, k, v, (const void*)out})
     if (!p || !aligned(p)) return HPD_E_INVALID;
+  if (!lse || ((uintptr_t)lse & 3)) return HPD_E_INVALID;
   if ((hpd_ft_forward_bytes(L) && !workspace) || !aligned(workspace)) return HPD_E_INVALID;
   HPD_HIP(hpd_launch_ft_attention(L, q, k, v, out, lse, workspace, st, (hipStream_t)stream));
   return HPD_OK;
@@ -287,8 +288,9 @@ int hpd_finetune_attention_backward(const hpd_finetune_layout* L, const void* q,
   hpd_finetune_strides st;
   if (!complete(L, strides, &st)) return HPD_E_INVALID;
   if (L->n_tokens == 0) return HPD_OK;
-  for (const void* p : {q, k, v, out, (const void*)lse, d_out, (const void*)dq, (const void*)dk, (const void*)dv})
+  for (const void* p : {q, k, v, out, d_out, (const void*)dq, (const void*)dk, (const void*)dv})
     if (!p || !aligned(p)) return HPD_E_INVALID;
+  if (!lse || ((uintptr_t)lse & 3)) return HPD_E_INVALID;
   if ((hpd_ft_backward_bytes(L) && !workspace) || !aligned(workspace)) return HPD_E_INVALID;
   HPD_HIP(hpd_launch_ft_attention_backward(L, q, k, v, out, lse, d_out, dq, dk, dv, workspace, st, (hipStream_t)stream));
   return HPD_OK;

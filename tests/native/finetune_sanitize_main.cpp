@@ -1,0 +1,174 @@
+// Host-side exerciser for a sanitizer build (-fsanitize=address,undefined on the host pass) of
+// hpd_finetune_host.cpp: random valid and broken batches through hpd_build_finetune_layout with HPD_FLAG_HOST_ONLY (no
+// GPU call), every table read back into a buffer of exactly its size, the work lists checked, the argument checks of the
+// calls.  The kernel launchers are stubbed out: nothing here may reach them.  Exit code 0 = no finding.
+#include <algorithm>
+#include <cstdint>
+#include <cstdio>
+#include <cstdlib>
+#include <map>
+#include <random>
+#include <vector>
+
+#include "hpd_finetune.h"
+#include "hpd_internal.h"
+
+static int g_stub_calls = 0;
+#define STUB(...) { ++g_stub_calls; return hipErrorInvalidValue; }
+int hpd_hip_fail(hipError_t) { ++g_stub_calls; return HPD_E_HIP; }
+hipError_t hpd_launch_ft_rope_table(const hpd_finetune_layout*, hipStream_t) STUB()
+hipError_t hpd_launch_ft_rotate(const hpd_finetune_layout*, bool, const void*, const void*, void*, void*,
+                                const hpd_finetune_strides&, hipStream_t) STUB()
+hipError_t hpd_launch_ft_attention(const hpd_finetune_layout*, const void*, const void*, const void*, void*, float*, void*,
+                                   const hpd_finetune_strides&, hipStream_t) STUB()
+hipError_t hpd_launch_ft_attention_backward(const hpd_finetune_layout*, const void*, const void*, const void*, const void*,
+                                            const float*, const void*, void*, void*, void*, void*, const hpd_finetune_strides&,
+                                            hipStream_t) STUB()
+int64_t hpd_logprobs_bytes(int32_t, int64_t n, int32_t, int32_t) { return n; }
+hipError_t hpd_launch_logprobs(int32_t, const hpd_logprobs_args&, hipStream_t) STUB()
+hipError_t hpd_launch_logprobs_backward(int32_t, const hpd_logprobs_backward_args&, hipStream_t) STUB()
+
+#define CHECK(cond)                                                          \
+  do {                                                                       \
+    if (!(cond)) {                                                           \
+      std::fprintf(stderr, "CHECK failed at line %d: %s\n", __LINE__, #cond); \
+      std::exit(1);                                                          \
+    }                                                                        \
+  } while (0)
+
+static std::vector<int32_t> table(const hpd_finetune_layout* L, int32_t what, size_t n) {
+  std::vector<int32_t> v(n);
+  int32_t dummy;
+  CHECK(hpd_finetune_layout_query(L, what, n ? (void*)v.data() : (void*)&dummy, n * 4) == HPD_OK);
+  if (n > 0) CHECK(hpd_finetune_layout_query(L, what, v.data(), n * 4 - 1) == HPD_E_INVALID);
+  return v;
+}
+
+// every 128 tokens of every sequence are one query tile and one key tile, longest first
+static void check_tiles(const hpd_finetune_layout* L, const std::vector<int32_t>& off) {
+  size_t expect = 0;
+  for (int32_t s = 0; s < L->n_seq; ++s) expect += (off[s + 1] - off[s] + 127) / 128;
+  CHECK(L->tiles.size() == expect && L->key_tiles.size() == expect);
+  std::map<std::pair<int32_t, int32_t>, int> seen;
+  for (size_t i = 0; i < expect; ++i) {
+    const hpd_ft_tile &a = L->tiles[i], &b = L->key_tiles[i];
+    CHECK(a.row0 < a.len && a.row0 % 128 == 0 && a.seq0 + a.len <= L->n_tokens);
+    CHECK((size_t)(a.blk0 + (a.len + 31) / 32) * 2 <= L->blk_rank.size());
+    seen[{a.seq0, a.row0}] += 1;
+    seen[{b.seq0, b.row0}] += 16;
+    if (i) CHECK(std::min(L->tiles[i - 1].row0 + 128, L->tiles[i - 1].len) >= std::min(a.row0 + 128, a.len));
+    if (i) CHECK(L->key_tiles[i - 1].len - L->key_tiles[i - 1].row0 >= b.len - b.row0);
+  }
+  for (const auto& x : seen) CHECK(x.second == 17);
+}
+
+// the items of a key tile are its rounds, each once; a tile of several has as many slots in a row
+static void check_items(const hpd_finetune_layout* L) {
+  if (!hpd_ft_stream_supported(L)) {
+    CHECK(L->items.empty() && L->joins.empty() && L->slots == 0);
+    return;
+  }
+  const int64_t G = L->cfg.n_q_heads / L->cfg.n_kv_heads;
+  std::map<std::pair<int32_t, int32_t>, std::map<int32_t, hpd_ft_item>> tiles;
+  for (size_t i = 0; i < L->items.size(); ++i) {
+    const hpd_ft_item& x = L->items[i];
+    CHECK(x.begin < x.end && x.slot < L->slots);
+    if (i) CHECK(L->items[i - 1].end - L->items[i - 1].begin >= x.end - x.begin);
+    const bool fresh = tiles[{x.seq0, x.row0}].emplace(x.begin, x).second;
+    CHECK(fresh);
+  }
+  CHECK(tiles.size() == L->key_tiles.size());
+  std::map<std::pair<int32_t, int32_t>, hpd_ft_item> joins;
+  int32_t slots = 0;
+  for (const hpd_ft_item& x : L->joins) {
+    CHECK(joins.emplace(std::make_pair(x.seq0, x.row0), x).second);
+    slots += x.end;
+  }
+  CHECK(slots == L->slots);
+  for (const auto& t : tiles) {
+    const hpd_ft_item& first = t.second.begin()->second;
+    int64_t at = 0;
+    const auto join = joins.find(t.first);
+    CHECK((t.second.size() > 1) == (join != joins.end()));
+    int32_t n = 0;
+    for (const auto& x : t.second) {
+      CHECK(x.second.begin == at);
+      at = x.second.end;
+      CHECK(x.second.slot == (join == joins.end() ? -1 : join->second.slot + n));
+      ++n;
+    }
+    CHECK(at == G * ((first.len + 31) / 32 - first.row0 / 32));
+    if (join != joins.end()) CHECK(join->second.end == n);
+  }
+  const int64_t rows = (int64_t)L->n_tokens * L->cfg.n_q_heads;
+  CHECK(hpd_ft_backward_bytes(L) >= rows * 8 + (int64_t)L->slots * L->cfg.n_kv_heads * 256 * L->cfg.head_dim * 4);
+}
+
+int main() {
+  std::mt19937 rng(7);
+  auto pick = [&](int32_t lo, int32_t hi) { return std::uniform_int_distribution<int32_t>(lo, hi)(rng); };
+  bool cut = false, whole = false;
+  for (int round = 0; round < 400; ++round) {
+    hpd_finetune_config cfg{};
+    cfg.n_kv_heads = pick(1, 8);
+    cfg.n_q_heads = cfg.n_kv_heads * pick(1, 8);
+    cfg.head_dim = round % 3 ? 64 * pick(1, 2) : 8 * pick(1, 16);
+    cfg.dtype = pick(0, 3) ? HPD_BF16 : HPD_F32;
+    cfg.rope_base = 10000.0;
+    cfg.k_max = pick(1, 40);
+    cfg.flags = HPD_FLAG_HOST_ONLY;
+    const int32_t n_seq = pick(0, 6);
+    std::vector<int32_t> prompt, attr_ptr{0}, attr_len, value_len;
+    for (int32_t s = 0; s < n_seq; ++s) {
+      prompt.push_back(pick(0, round % 7 == 0 ? 6000 : 300));
+      const int32_t n = pick(0, 12);
+      for (int32_t i = 0; i < n; ++i) {
+        attr_len.push_back(pick(1, 4));
+        value_len.push_back(pick(0, cfg.k_max));
+      }
+      attr_ptr.push_back((int32_t)attr_len.size());
+    }
+    // (copies of exactly the arrays' sizes: a read behind one is a finding)
+    hpd_finetune_layout* L = nullptr;
+    CHECK(hpd_build_finetune_layout(&cfg, n_seq, prompt.data(), attr_ptr.data(), attr_len.data(), value_len.data(), nullptr, &L) == HPD_OK);
+    int64_t c[HPD_N_FT_COUNTS];
+    CHECK(hpd_finetune_layout_query(L, HPD_FTQ_COUNTS, c, sizeof(c)) == HPD_OK);
+    CHECK(hpd_finetune_layout_query(L, HPD_FTQ_COUNTS, c, sizeof(c) - 1) == HPD_E_INVALID);
+    CHECK(hpd_finetune_layout_query(L, 17, c, sizeof(c)) == HPD_E_INVALID);
+    const auto off = table(L, HPD_FTQ_SEQ_OFF, (size_t)n_seq + 1), pos = table(L, HPD_FTQ_POS, (size_t)c[HPD_FTC_N_TOKENS]),
+               rank = table(L, HPD_FTQ_RANK, (size_t)c[HPD_FTC_N_TOKENS]);
+    CHECK(off[n_seq] == c[HPD_FTC_N_TOKENS]);
+    for (int32_t p : pos) CHECK(p >= 0 && p <= c[HPD_FTC_MAX_POS]);
+    for (int32_t r : rank) CHECK(r >= 0 && r <= cfg.k_max);
+    CHECK(L->rope_rows <= L->n_tokens && (L->rope_by_token ? L->rope_rows == L->n_tokens : L->rope_rows == c[HPD_FTC_MAX_POS] + 1));
+    check_tiles(L, off);
+    check_items(L);
+    cut = cut || !L->joins.empty();
+    whole = whole || (L->joins.empty() && !L->items.empty());
+    float x[4];
+    CHECK(hpd_finetune_attention(L, x, x, x, x, x, x, nullptr, nullptr) == HPD_E_INVALID);  // not on the device
+    hpd_finetune_layout_free(L);
+    // one field broken
+    hpd_finetune_config bad = cfg;
+    switch (pick(0, 5)) {
+      case 0: bad.n_q_heads = 0; break;
+      case 1: bad.n_kv_heads = bad.n_q_heads + 1; break;
+      case 2: bad.head_dim = 7; break;
+      case 3: bad.k_max = 0; break;
+      case 4: bad.dtype = 9; break;
+      default: bad.rope_base = 0.5;
+    }
+    L = nullptr;
+    CHECK(hpd_build_finetune_layout(&bad, n_seq, prompt.data(), attr_ptr.data(), attr_len.data(), value_len.data(), nullptr, &L) < 0);
+    CHECK(L == nullptr);
+    if (!value_len.empty()) {
+      value_len[pick(0, (int32_t)value_len.size() - 1)] = pick(0, 1) ? -1 : cfg.k_max + 1;
+      CHECK(hpd_build_finetune_layout(&cfg, n_seq, prompt.data(), attr_ptr.data(), attr_len.data(), value_len.data(), nullptr, &L) == HPD_E_INVALID);
+    }
+  }
+  CHECK(cut && whole);
+  hpd_finetune_layout_free(nullptr);
+  CHECK(g_stub_calls == 0);
+  std::puts("no finding");
+  return 0;
+}
