@@ -36,14 +36,16 @@ int validate(const hpd_finetune_config* c) {
 
 // The items of the dk/dv kernel.  Two workgroups run on a CU at a time; a key tile at the start of a long sequence
 // has many times the rounds of others, and a batch may have fewer tiles than the GPU has room for.  Tiles are
-// cut so that an item is at most a third of what a workgroup's place has to do, but not below 24 rounds: an
-// item starts and ends with the time of four, and its sums are written and read once more.
+// cut so that an item is at most a third of what a workgroup's place has to do (a half: 4045 -> 4140 us on 2 x 6100 tokens,
+// 64/8 heads), but not below 64 rounds, or 24 where there is room for more workgroups than tiles: an item starts and ends with
+// the time of four, and its sums are written and read once more (24 always: 545 -> 585 us on 32 x 420 tokens, 32/8 heads).
 void plan_items(hpd_finetune_layout* L, int32_t n_cus) {
   const int64_t Hkv = L->cfg.n_kv_heads, G = L->cfg.n_q_heads / Hkv;
   auto rounds = [&](const hpd_ft_tile& t) { return G * ((t.len + 31) / 32 - t.row0 / 32); };
   int64_t total = 0;
   for (const hpd_ft_tile& t : L->key_tiles) total += rounds(t) * Hkv;
-  const int64_t most = std::max<int64_t>(24, total / (2 * n_cus) / 3);
+  const int64_t places = 2 * n_cus;
+  const int64_t most = std::max<int64_t>((int64_t)L->key_tiles.size() * Hkv < places ? 24 : 64, total / places / 3);
   for (const hpd_ft_tile& t : L->key_tiles) {
     const int64_t r = rounds(t), parts = r * 2 > most * 3 ? (r + most - 1) / most : 1;
     if (parts > 1) L->joins.push_back({t.seq0, t.len, t.row0, t.blk0, 0, (int32_t)parts, L->slots, 0});
