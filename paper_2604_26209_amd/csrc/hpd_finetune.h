@@ -20,7 +20,7 @@ struct hpd_ft_tile {
   int32_t blk0;  // the sequence's first entry in blk_rank
 };
 
-// A run of the rounds (32 queries of one head each, head by head) of a key tile and of one kv head.
+// A run of the rounds (32 queries of one head each, head by head) of a tile of keys and of one kv head.
 struct hpd_ft_item {
   int32_t seq0, len, row0, blk0;  // of the tile
   int32_t begin, end;             // rounds
@@ -34,9 +34,7 @@ struct hpd_finetune_layout {
   std::vector<int32_t> seq_off, pos, rank;
   std::vector<int32_t> blk_rank;        // [blocks][2]: lowest and highest rank of 32 tokens of a sequence
   std::vector<hpd_ft_tile> tiles;       // query tiles, those with most keys first
-  std::vector<hpd_ft_tile> key_tiles;   // the same tiles, those with most queries first
-  // hpd_finetune_stream.hip: the key tiles as items, longest first, and for those of several items the first slot and
-  // (as `end`) their number
+  // the tiles of keys as items, longest first, and for those of several items the first slot and (as `end`) their number
   std::vector<hpd_ft_item> items, joins;
   int32_t slots = 0;
 
@@ -44,7 +42,7 @@ struct hpd_finetune_layout {
   void* d_mem = nullptr;
   const int32_t *d_pos = nullptr, *d_rank = nullptr;
   const int2* d_blk_rank = nullptr;
-  const hpd_ft_tile *d_tiles = nullptr, *d_key_tiles = nullptr;
+  const hpd_ft_tile* d_tiles = nullptr;
   const hpd_ft_item *d_items = nullptr, *d_joins = nullptr;
   // (cos, sin) rows of D/2: one per position ID, or one per token where that is fewer
   float2* d_rope = nullptr;
@@ -52,9 +50,11 @@ struct hpd_finetune_layout {
   bool rope_by_token = false;
 };
 
-// The kernels for bf16 with head_dim 64 or 128 (hpd_finetune_stream.hip) run.
-inline bool hpd_ft_stream_supported(const hpd_finetune_layout* L) {
-  return L->cfg.dtype == HPD_BF16 && (L->cfg.head_dim == 64 || L->cfg.head_dim == 128);
+// Tokens of a tile of keys, and channels that the kernels are made for.
+inline int32_t hpd_ft_key_rows(const hpd_finetune_layout* L) { return L->cfg.dtype == HPD_BF16 ? HPD_FT_ROWS : HPD_FT_BLOCK; }
+inline int32_t hpd_ft_padded_dim(const hpd_finetune_layout* L) {
+  const int32_t d = (L->cfg.head_dim + 31) / 32 * 32;
+  return L->cfg.dtype == HPD_F32 && d < 64 ? 64 : d;
 }
 // Bytes of the calls' workspaces.
 int64_t hpd_ft_forward_bytes(const hpd_finetune_layout* L);

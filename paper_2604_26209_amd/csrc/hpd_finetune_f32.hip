@@ -6,7 +6,7 @@
 // tile of each kind: it is loaded again (global_load_lds) as soon as its last product has read it, and the order of the
 // products leaves one of them between that and the tile's next use.
 //
-// Tiles: 32 rows of DP values (64 or 128; zeros from D on).  Chunk c (16 bytes) of row r lies at c ^ f(r),
+// Tiles: 32 rows of 64 or 128 values, of which the first DP count (64, 96 or 128; zeros from D on).  Chunk c (16 bytes) of row r lies at c ^ f(r),
 // f(r) = 8 (r / 4 % 2) + 4 (r / 8 % 2) + r % 4: sixteen rows' chunk c in different banks (left operand of four score products),
 // and 32 channels of the rows r and r + 4 too (left operand of a second product).
 #include "hpd_finetune_dev.h"
@@ -19,7 +19,7 @@ __device__ __forceinline__ floatx16 mfma(float a, float b, floatx16 c) {
 
 template <int DP>
 struct Tile {
-  static constexpr int RB = DP * 4, BYTES = 32 * RB, CHUNKS = RB / 16, STEPS = DP / 8, NB = DP / 32;
+  static constexpr int RB = DP <= 64 ? 256 : 512, BYTES = 32 * RB, CHUNKS = RB / 16, STEPS = DP / 8, NB = DP / 32;
   static constexpr int LOADS = BYTES / 1024;  // load instructions
   static __device__ __forceinline__ int swizzle(int r) { return ((r >> 2) & 1) << 3 | ((r >> 3) & 1) << 2 | (r & 3); }
 
@@ -343,13 +343,16 @@ __global__ void __launch_bounds__(256, DP > 64 ? 1 : 2) ft_f32_dq_kernel(FtArgs 
 }
 
 // Products in the order q . k, do . v, ds . q, p . do: the next queries are on their way during the last, the next
-// gradients of the output during the first.
+// gradients of the output during the first.  An item is a run of the (head, block of queries) of 32 keys, head by head; the
+// sums of keys with several items go to `partial`, and a second kernel adds them up.
 template <int DP>
-__global__ void __launch_bounds__(256, DP > 64 ? 1 : 2) ft_f32_dkv_kernel(FtArgs a, const float* __restrict__ q,
+__global__ void __launch_bounds__(256, DP > 64 ? 1 : 2) ft_f32_dkv_kernel(FtArgs a, const hpd_ft_item* __restrict__ items,
+                                                                        const float* __restrict__ q,
                                                                         const float* __restrict__ k, const float* __restrict__ v,
                                                                         const float* __restrict__ d_out,
                                                                         const float* __restrict__ lse,
-                                                                        const float* __restrict__ delta, float* __restrict__ dk,
+                                                                        const float* __restrict__ delta, float* __restrict__ partial,
+                                                                        float* __restrict__ dk,
                                                                         float* __restrict__ dv) {
   using TL = Tile<DP>;
   __shared__ __attribute__((aligned(1024))) Shared<DP> sh;
@@ -357,24 +360,24 @@ __global__ void __launch_bounds__(256, DP > 64 ? 1 : 2) ft_f32_dkv_kernel(FtArgs
   // the block's values, for 128 channels: the registers are full
   constexpr bool LDS_VALUES = DP > 64;
   __shared__ __attribute__((aligned(1024))) char values[LDS_VALUES ? TL::BYTES : 16];
-  const int32_t G = a.Hq / a.Hkv, hk = blockIdx.x % a.Hkv, rest = blockIdx.x / a.Hkv;
-  const Block w(a.tiles[rest / 4], rest % 4);
-  if (w.first >= w.t.len) return;
+  const int32_t G = a.Hq / a.Hkv, hk = blockIdx.x % a.Hkv;
+  const hpd_ft_item item = items[blockIdx.x / a.Hkv];
+  const Block w({item.seq0, item.len, item.row0, item.blk0}, 0);
   const int32_t* const ranks = a.rank + w.t.seq0;
   const const_i32* const blk_rank = (const const_i32*)(uintptr_t)(a.blk_rank + w.t.blk0);
   const int64_t token = w.t.seq0 + (int64_t)w.ic, so = (int64_t)a.Hq * a.D;
   const int32_t own = w.first / 32, blocks = (w.t.len + 31) / 32, k_min = blk_rank[2 * own], k_max = blk_rank[2 * own + 1];
   const uint32_t q_tile = lds_address(&sh.tiles[0][0]) + w.wave * 2 * TL::BYTES, o_tile = q_tile + TL::BYTES;
-  // the wave takes every fourth (head, block of queries)
-  struct Where { int32_t g, b; };
-  auto settle = [&](Where x) -> Where {  // the first from x on with a query that sees a key; head G: none
-    for (;; x.b += 4) {
-      while (x.b >= blocks && x.g < G) {
-        x.b += own - blocks;
-        ++x.g;
-      }
-      if (x.g >= G || k_min <= blk_rank[2 * x.b + 1]) return x;
+  // the wave takes every fourth round
+  const int32_t per_head = blocks - own;
+  struct Where { int32_t round, g, b; };
+  auto settle = [&](int32_t round) -> Where {  // the first from this one on, in steps of four, with a query that sees a key
+    Where x{round, round / per_head, own + round % per_head};
+    while (x.round < item.end && k_min > blk_rank[2 * x.b + 1]) {
+      x.round += 4;
+      for (x.b += 4; x.b >= blocks; ++x.g) x.b -= per_head;
     }
+    return x;
   };
   auto load_queries = [&](Where x) {
     TL::load(q_tile, q + w.t.seq0 * a.sq + (int64_t)(hk * G + x.g) * a.D, a.sq, x.b * 32, w.t.len - 1, a.D, a.rank + a.N, w.lane);
@@ -399,8 +402,8 @@ __global__ void __launch_bounds__(256, DP > 64 ? 1 : 2) ft_f32_dkv_kernel(FtArgs
     }
     __syncthreads();
   }
-  Where x = settle({0, own + w.wave});
-  if (x.g < G) {
+  Where x = settle(item.begin + w.wave);
+  if (x.round < item.end) {
     load_queries(x);
     load_gradients(x);
   }
@@ -416,8 +419,8 @@ __global__ void __launch_bounds__(256, DP > 64 ? 1 : 2) ft_f32_dkv_kernel(FtArgs
   floatx16 acc_k[TL::NB], acc_v[TL::NB];
   zero(acc_k, TL::NB);
   zero(acc_v, TL::NB);
-  while (x.g < G) {
-    const Where after = settle({x.g, x.b + 4});
+  while (x.round < item.end) {
+    const Where after = settle(x.round + 4);
     wait_vector_memory<TL::LOADS + 1>();  // the queries; the gradients and the rows' numbers were requested behind them
     floatx16 s = TL::scores(q_tile, at, kf, floatx16{});
     wait_vector_memory<0>();
@@ -439,19 +442,58 @@ __global__ void __launch_bounds__(256, DP > 64 ? 1 : 2) ft_f32_dkv_kernel(FtArgs
       ds[r] = p[r] * (dp[r] - stats[w.wave][32 + tile_row(r, w.h)]);
     }
     TL::add(q_tile, w.n, w.h, ds, acc_k);
-    if (after.g < G) load_queries(after);
+    if (after.round < item.end) load_queries(after);
     TL::add(o_tile, w.n, w.h, p, acc_v);
-    if (after.g < G) load_gradients(after);
+    if (after.round < item.end) load_gradients(after);
     x = after;
   }
   __syncthreads();
   put<DP>(sh, w, acc_v, 1.f);
   __syncthreads();
+  if (item.slot >= 0) {
+    float* const p = partial + ((int64_t)item.slot * a.Hkv + hk) * (2 * 32 * DP);
+    join<DP>(sh, w, p + 32 * DP, DP, DP);
+    __syncthreads();
+    put<DP>(sh, w, acc_k, 1.f);
+    __syncthreads();
+    join<DP>(sh, w, p, DP, DP);
+    return;
+  }
   join<DP>(sh, w, dv + (w.t.seq0 + (int64_t)w.first) * a.sdv + (int64_t)hk * a.D, a.sdv, a.D);
   __syncthreads();
   put<DP>(sh, w, acc_k, a.scale);
   __syncthreads();
   join<DP>(sh, w, dk + (w.t.seq0 + (int64_t)w.first) * a.sdk + (int64_t)hk * a.D, a.sdk, a.D);
+}
+
+// Adds up the partial sums of 32 keys, in the order of their items, those of four items on their way at a time.  A
+// workgroup has eight keys of dk (even) or dv.
+template <int DP>
+__global__ void __launch_bounds__(8 * DP / 4) ft_f32_dkv_join_kernel(FtArgs a, const hpd_ft_item* __restrict__ joins,
+                                                                    const float* __restrict__ partial,
+                                                                    float* __restrict__ dk, float* __restrict__ dv) {
+  const int32_t y = blockIdx.x & 1, r = (blockIdx.x >> 1 & 3) * 8 + threadIdx.x / (DP / 4), c = threadIdx.x % (DP / 4) * 4;
+  const int32_t hk = (blockIdx.x >> 3) % a.Hkv;
+  const hpd_ft_item t = joins[(blockIdx.x >> 3) / a.Hkv];  // slots [slot, slot + end)
+  if (t.row0 + r >= t.len || c >= a.D) return;
+  const int64_t step = (int64_t)a.Hkv * (2 * 32 * DP);
+  const float* p = partial + ((int64_t)t.slot * a.Hkv + hk) * (2 * 32 * DP) + (y * 32 + r) * DP + c;
+  float4 sum = {};
+  for (int32_t i = 0; i < t.end; i += 4) {
+    float4 w[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      if (i + j < t.end) w[j] = *reinterpret_cast<const float4*>(p + (i + j) * step);
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      if (i + j < t.end) {
+        sum.x += w[j].x; sum.y += w[j].y; sum.z += w[j].z; sum.w += w[j].w;
+      }
+  }
+  const float f = y ? 1.f : a.scale;
+  const int64_t token = t.seq0 + (int64_t)t.row0 + r;
+  *reinterpret_cast<float4*>((y ? dv + token * a.sdv : dk + token * a.sdk) + (int64_t)hk * a.D + c) =
+      make_float4(sum.x * f, sum.y * f, sum.z * f, sum.w * f);
 }
 
 template <int DP>
@@ -467,8 +509,11 @@ hipError_t backward(const hpd_finetune_layout* L, FtArgs a, const float* q, cons
   ft_f32_delta_kernel<<<dim3((unsigned)((a.N * a.Hq + 15) / 16)), 256, 0, s>>>(a.N, a.Hq, a.D, out, d_out, delta);
   const unsigned blocks = (unsigned)L->tiles.size() * 4;
   ft_f32_dq_kernel<DP><<<dim3(blocks * a.Hq), 256, 0, s>>>(a, q, k, v, d_out, lse, delta, dq);
-  a.tiles = L->d_key_tiles;
-  ft_f32_dkv_kernel<DP><<<dim3(blocks * a.Hkv), 256, 0, s>>>(a, q, k, v, d_out, lse, delta, dk, dv);
+  float* partial = delta + 2 * a.N * a.Hq + (-2 * a.N * a.Hq & 3);  // (on 16 bytes)
+  ft_f32_dkv_kernel<DP><<<dim3((unsigned)L->items.size() * a.Hkv), 256, 0, s>>>(a, L->d_items, q, k, v, d_out, lse, delta, partial,
+                                                                               dk, dv);
+  if (!L->joins.empty())
+    ft_f32_dkv_join_kernel<DP><<<dim3((unsigned)L->joins.size() * a.Hkv * 8), 2 * DP, 0, s>>>(a, L->d_joins, partial, dk, dv);
   return hipGetLastError();
 }
 
@@ -476,14 +521,14 @@ hipError_t backward(const hpd_finetune_layout* L, FtArgs a, const float* q, cons
 
 hipError_t hpd_launch_ft_f32_forward(const hpd_finetune_layout* L, FtArgs a, const void* q, const void* k, const void* v,
                                      void* out, float* lse, hipStream_t s) {
-  const auto run = a.D <= 64 ? forward<64> : forward<128>;
+  const auto run = a.D <= 64 ? forward<64> : a.D <= 96 ? forward<96> : forward<128>;
   return run(L, a, (const float*)q, (const float*)k, (const float*)v, (float*)out, lse, s);
 }
 
 hipError_t hpd_launch_ft_f32_backward(const hpd_finetune_layout* L, FtArgs a, const void* q, const void* k, const void* v,
                                       const void* out, const float* lse, const void* d_out, void* dq, void* dk, void* dv,
                                       void* workspace, hipStream_t s) {
-  const auto run = a.D <= 64 ? backward<64> : backward<128>;
+  const auto run = a.D <= 64 ? backward<64> : a.D <= 96 ? backward<96> : backward<128>;
   return run(L, a, (const float*)q, (const float*)k, (const float*)v, (const float*)out, lse, (const float*)d_out, (float*)dq,
              (float*)dk, (float*)dv, (float*)workspace, s);
 }

@@ -34,19 +34,27 @@ int validate(const hpd_finetune_config* c) {
   return HPD_OK;
 }
 
-// The items of the dk/dv kernel.  Two workgroups run on a CU at a time; a key tile at the start of a long sequence
-// has many times the rounds of others, and a batch may have fewer tiles than the GPU has room for.  Tiles are
-// cut so that an item is at most a third of what a workgroup's place has to do (a half: 4045 -> 4140 us on 2 x 6100 tokens,
-// 64/8 heads), but not below 64 rounds, or 24 where there is room for more workgroups than tiles: an item starts and ends with
-// the time of four, and its sums are written and read once more (24 always: 545 -> 585 us on 32 x 420 tokens, 32/8 heads).
+// The items of the dk/dv kernels.  Two workgroups run on a CU at a time (one for fp32 with more than 64 channels); a tile
+// at the start of a long sequence has many times the rounds of others, and a batch may have fewer tiles than the GPU has room for.
+// Tiles are cut so that an item is at most a third of what a workgroup's place has to do (a half: 4045 -> 4140 us on 2 x 6100
+// tokens, 64/8 heads), but in bf16 not below 64 rounds, or 24 where there is room for more workgroups than tiles: an item
+// starts and ends with the time of four, and its sums are written and read once more (24 always: 545 -> 585 us on 32 x 420
+// tokens, 32/8 heads).  In fp32 the waves share the rounds, 16 at least: four each (8 and 32: 1 % faster and 2 % slower in the
+// mean of 24 random batches; not cut at all: 473 -> 84 us on one sequence of 774 tokens, 12/2 heads of 96).
 void plan_items(hpd_finetune_layout* L, int32_t n_cus) {
   const int64_t Hkv = L->cfg.n_kv_heads, G = L->cfg.n_q_heads / Hkv;
+  const int32_t rows = hpd_ft_key_rows(L);
+  const bool bf16 = L->cfg.dtype == HPD_BF16;
+  std::vector<hpd_ft_tile> tiles;
+  for (const hpd_ft_tile& t : L->tiles)
+    for (int32_t r = t.row0; r < std::min(t.row0 + HPD_FT_ROWS, t.len); r += rows) tiles.push_back({t.seq0, t.len, r, t.blk0});
   auto rounds = [&](const hpd_ft_tile& t) { return G * ((t.len + 31) / 32 - t.row0 / 32); };
   int64_t total = 0;
-  for (const hpd_ft_tile& t : L->key_tiles) total += rounds(t) * Hkv;
-  const int64_t places = 2 * n_cus;
-  const int64_t most = std::max<int64_t>((int64_t)L->key_tiles.size() * Hkv < places ? 24 : 64, total / places / 3);
-  for (const hpd_ft_tile& t : L->key_tiles) {
+  for (const hpd_ft_tile& t : tiles) total += rounds(t) * Hkv;
+  const int64_t places = (bf16 || L->cfg.head_dim <= 64 ? 2 : 1) * n_cus;
+  const int64_t least = bf16 ? ((int64_t)tiles.size() * Hkv < places ? 24 : 64) : 16;
+  const int64_t most = std::max<int64_t>(least, total / places / 3);
+  for (const hpd_ft_tile& t : tiles) {
     const int64_t r = rounds(t), parts = r * 2 > most * 3 ? (r + most - 1) / most : 1;
     if (parts > 1) L->joins.push_back({t.seq0, t.len, t.row0, t.blk0, 0, (int32_t)parts, L->slots, 0});
     for (int64_t p = 0; p < parts; ++p)
@@ -99,15 +107,11 @@ int build_tables(hpd_finetune_layout* L, const int32_t* prompt_len, const int32_
     for (int32_t r = 0; r < len; r += HPD_FT_ROWS) L->tiles.push_back({seq0, len, r, blk0});
   }
   for (int32_t p : L->pos) L->max_pos = std::max(L->max_pos, p);
-  // Longest first: what starts last is short.  A query tile has keys up to its last row, a key tile
-  // queries from its first row on.
-  L->key_tiles = L->tiles;
+  // Longest first: what starts last is short.  A tile of queries has keys up to its last row.
   std::stable_sort(L->tiles.begin(), L->tiles.end(), [](const hpd_ft_tile& a, const hpd_ft_tile& b) {
     return std::min(a.row0 + HPD_FT_ROWS, a.len) > std::min(b.row0 + HPD_FT_ROWS, b.len);
   });
-  std::stable_sort(L->key_tiles.begin(), L->key_tiles.end(),
-                   [](const hpd_ft_tile& a, const hpd_ft_tile& b) { return a.len - a.row0 > b.len - b.row0; });
-  if (hpd_ft_stream_supported(L)) plan_items(L, n_cus);
+  plan_items(L, n_cus);
   L->rope_by_token = L->max_pos >= L->n_tokens;
   L->rope_rows = L->rope_by_token ? L->n_tokens : L->max_pos + 1;
   return HPD_OK;
@@ -119,14 +123,13 @@ int upload(hpd_finetune_layout* L, hipStream_t s) {
   // (the kernels read the ranks of two whole blocks at a time: up to 63 more behind the last token)
   const size_t n = (size_t)L->n_tokens, nt = L->tiles.size() * 4;
   const size_t o_rank = pad(n), o_blk = o_rank + pad(n + 2 * HPD_FT_BLOCK), o_tiles = o_blk + pad(L->blk_rank.size()),
-               o_ktiles = o_tiles + nt, o_items = o_ktiles + nt, o_joins = o_items + L->items.size() * 8,
+               o_items = o_tiles + nt, o_joins = o_items + L->items.size() * 8,
                words = o_joins + L->joins.size() * 8;
   std::vector<int32_t> host(words, 0);
   std::copy(L->pos.begin(), L->pos.end(), host.begin());
   std::copy(L->rank.begin(), L->rank.end(), host.begin() + o_rank);
   std::copy(L->blk_rank.begin(), L->blk_rank.end(), host.begin() + o_blk);
   std::memcpy(host.data() + o_tiles, L->tiles.data(), nt * 4);
-  std::memcpy(host.data() + o_ktiles, L->key_tiles.data(), nt * 4);
   if (!L->items.empty()) std::memcpy(host.data() + o_items, L->items.data(), L->items.size() * sizeof(hpd_ft_item));
   if (!L->joins.empty()) std::memcpy(host.data() + o_joins, L->joins.data(), L->joins.size() * sizeof(hpd_ft_item));
   const size_t rope_bytes = (size_t)L->rope_rows * (size_t)(L->cfg.head_dim / 2) * sizeof(float2);
@@ -136,7 +139,6 @@ int upload(hpd_finetune_layout* L, hipStream_t s) {
   L->d_rank = base + o_rank;
   L->d_blk_rank = (const int2*)(base + o_blk);
   L->d_tiles = (const hpd_ft_tile*)(base + o_tiles);
-  L->d_key_tiles = (const hpd_ft_tile*)(base + o_ktiles);
   L->d_items = (const hpd_ft_item*)(base + o_items);
   L->d_joins = (const hpd_ft_item*)(base + o_joins);
   L->d_rope = (float2*)(base + words);
@@ -179,7 +181,7 @@ int64_t hpd_ft_forward_bytes(const hpd_finetune_layout*) { return 0; }
 // two numbers per (head, token), then the partial sums of dk and dv
 int64_t hpd_ft_backward_bytes(const hpd_finetune_layout* L) {
   const int64_t rows = (int64_t)L->n_tokens * L->cfg.n_q_heads;
-  return (rows * 8 + 15) / 16 * 16 + (int64_t)L->slots * L->cfg.n_kv_heads * 2 * HPD_FT_ROWS * L->cfg.head_dim * 4;
+  return (rows * 8 + 15) / 16 * 16 + (int64_t)L->slots * L->cfg.n_kv_heads * 2 * hpd_ft_key_rows(L) * hpd_ft_padded_dim(L) * 4;
 }
 
 extern "C" {

@@ -1,8 +1,8 @@
-// Fine-tuning attention in bf16 with head_dim 64 or 128: forward and gradients (formulas and operand
-// scheme: hpd_finetune_attn.hip).  The other side's tokens stream through a ring of tiles in LDS that
+// Fine-tuning attention in bf16: forward and gradients (formulas and operand scheme:
+// hpd_finetune_attn.hip).  The other side's tokens stream through a ring of tiles in LDS that
 // global_load_lds fills ahead of their use.
 //
-// Tiles: 32 rows of D bf16 values as they lie in memory, the 16-byte chunks of a row permuted: chunk c
+// Tiles: 32 rows of up to 64 or 128 bf16 values as they lie in memory, the 16-byte chunks of a row permuted: chunk c
 // of row r lies at c ^ f(r), f(r) = 4 (r % 4) + (r / 4) % 4 for rows of 16 chunks and
 // 4 (r / 2 % 2) + (r / 4) % 4 for rows of 8.  So both ways of reading a tile spread over all banks:
 // one chunk of 16 successive rows (left operand of a score product), and the same 64 bytes of four
@@ -13,16 +13,18 @@ namespace {
 
 constexpr uint32_t BIAS = 4096;  // keeps a lane's offset positive (see Loader)
 
-template <int D>
+// The kernels are made for NB blocks of 32 channels.  Where a head ends inside the last block, its first chunk stands for
+// the chunks behind it and the other side's operand is zero there.
+template <int NB>
 struct Rows {
-  static constexpr int RB = D * 2;           // bytes of a row
+  static constexpr int RB = NB <= 2 ? 128 : 256;  // bytes of a row
   static constexpr int TILE = 32 * RB;       // bytes of a tile
   static constexpr int CHUNKS = RB / 16;     // of a row
-  static constexpr int STEPS = D / 16;       // products of a score
-  static constexpr int BLOCKS = D / 32;      // blocks of 32 channels
+  static constexpr int STEPS = 2 * NB;       // products of a score
+  static constexpr int BLOCKS = NB;          // blocks of 32 channels
   static constexpr int GROUP = 4096 / RB;    // rows that four load instructions bring
   static __device__ __forceinline__ int swizzle(int r) {
-    return D == 128 ? ((r & 3) << 2) | ((r >> 2) & 3) : (((r >> 1) & 1) << 2) | ((r >> 2) & 3);
+    return RB == 256 ? ((r & 3) << 2) | ((r >> 2) & 3) : (((r >> 1) & 1) << 2) | ((r >> 2) & 3);
   }
   // offset of chunk h of row n in a tile; chunk 2 s + h: ^ (s << 5)
   static __device__ __forceinline__ uint32_t row_offset(int n, int h) { return n * RB + ((h ^ swizzle(n)) << 4); }
@@ -37,27 +39,31 @@ struct Rows {
 // Four load instructions bring GROUP rows; instruction f rows f * GROUP / 4 .. .  Its offset field moves
 // the address in memory and the one in LDS alike, so the lanes' offsets are f KB less, and a bias more.
 // M0 is the compiler's: both forms put back what it held.
-template <int D>
+template <int NB>
 struct Loader {
-  using R = Rows<D>;
+  using R = Rows<NB>;
   uint32_t off[4];
   int64_t stride;  // bytes between rows
+  int32_t chunks;  // of a head's row
   bool near;       // a group's offsets fit 32 bits
-  __device__ __forceinline__ void init(int64_t stride_elements, int lane) {
+  __device__ __forceinline__ void init(int64_t stride_elements, int32_t D, int lane) {
     stride = stride_elements * 2;
+    chunks = D / 8;
     near = stride < 1 << 25;
 #pragma unroll
     for (int f = 0; f < 4; ++f) off[f] = row(f, lane) * (uint32_t)stride + chunk(f, lane) - f * 1024 + BIAS;
   }
   static __device__ __forceinline__ int32_t row(int f, int lane) { return f * (1024 / R::RB) + lane / R::CHUNKS; }
-  static __device__ __forceinline__ uint32_t chunk(int f, int lane) {
-    return ((lane % R::CHUNKS) ^ R::swizzle(row(f, lane))) << 4;
+  __device__ __forceinline__ uint32_t chunk(int f, int lane) const {
+    const int32_t c = (lane % R::CHUNKS) ^ R::swizzle(row(f, lane));
+    return c < chunks ? c << 4 : 0;
   }
   // GROUP rows from base (wave-uniform) to lds; rows past `last` (counted from base) are row `last` again
-  __device__ __forceinline__ void load(const char* base, uint32_t lds, int32_t last, int lane) const {
+  // (zeros: 16 bytes of them, for the chunks behind the row's end)
+  __device__ __forceinline__ void load(const char* base, uint32_t lds, int32_t last, int lane, const void* zeros = nullptr) const {
     lds = __builtin_amdgcn_readfirstlane(lds);
     uint32_t keep;
-    if (near && last >= R::GROUP - 1) {
+    if (!zeros && near && last >= R::GROUP - 1) {
       asm volatile(
           "s_mov_b32 %0, m0\n\ts_mov_b32 m0, %5\n\ts_nop 0\n\t"
           "global_load_lds_dwordx4 %1, %6\n\t"
@@ -71,7 +77,10 @@ struct Loader {
     } else {
       const char* p[4];
 #pragma unroll
-      for (int f = 0; f < 4; ++f) p[f] = base + min(row(f, lane), last) * stride + chunk(f, lane) - f * 1024;
+      for (int f = 0; f < 4; ++f) {
+        const bool behind = zeros && ((lane % R::CHUNKS) ^ R::swizzle(row(f, lane))) >= chunks;
+        p[f] = (behind ? reinterpret_cast<const char*>(zeros) : base + min(row(f, lane), last) * stride + chunk(f, lane)) - f * 1024;
+      }
       asm volatile(
           "s_mov_b32 %0, m0\n\ts_mov_b32 m0, %5\n\ts_nop 0\n\t"
           "global_load_lds_dwordx4 %1, off\n\t"
@@ -95,12 +104,12 @@ __device__ __forceinline__ uint2 lds_read_tr(uint32_t at) {
 __device__ __forceinline__ floatx16 mfma(bf16x8 a, bf16x8 b, floatx16 c) {
   return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
 }
-// 32 columns of a transposed result (lane n: column n) times f, as 32 rows of D values through `turn`
+// 32 columns of a transposed result (lane n: column n) times f, as 32 rows of D bf16 values through `turn`
 // (TILE bytes of LDS of this wave's own); row r of the tile goes to out + r * stride, r < rows
-template <int D>
+template <int NB>
 __device__ __forceinline__ void store_rows(char* turn, const floatx16* acc, float f, uint16_t* out, int64_t stride, int rows,
-                                           int lane) {
-  using R = Rows<D>;
+                                           int32_t D, int lane) {
+  using R = Rows<NB>;
   const int n = lane & 31, h = lane >> 5;
 #pragma unroll
   for (int b = 0; b < R::BLOCKS; ++b)
@@ -117,16 +126,28 @@ __device__ __forceinline__ void store_rows(char* turn, const floatx16* acc, floa
   for (int i = 0; i < R::TILE / 1024; ++i) {
     const int r = i * (64 / R::CHUNKS) + lane / R::CHUNKS, c = lane % R::CHUNKS;
     const uint4 w = *reinterpret_cast<const uint4*>(turn + r * R::RB + ((c ^ (r & (R::CHUNKS - 1))) << 4));
-    if (r < rows) *reinterpret_cast<uint4*>(out + r * stride + c * 8) = w;
+    if (r < rows && c * 8 < D) *reinterpret_cast<uint4*>(out + r * stride + c * 8) = w;
+  }
+}
+
+// a lane's chunks of a row of its own, zero from channel D on
+template <int STEPS>
+__device__ __forceinline__ void own_row(const uint16_t* row, int32_t D, int h, bf16x8 (&f)[STEPS]) {
+#pragma unroll
+  for (int s = 0; s < STEPS; ++s) {
+    const int32_t c = (2 * s + h) * 8;
+    uint4 w = *reinterpret_cast<const uint4*>(row + (c < D ? c : 0));
+    if (c >= D) w = make_uint4(0, 0, 0, 0);
+    f[s] = __builtin_bit_cast(bf16x8, w);
   }
 }
 
 // ---------------------------------------------------------------------------------------
 // Forward and dq: four waves of 32 queries of one head; rounds of 64 keys, two rounds in LDS.
 // ---------------------------------------------------------------------------------------
-template <int D>
+template <int NB>
 struct QueryTile {
-  using R = Rows<D>;
+  using R = Rows<NB>;
   static constexpr int STAGE = 4 * R::TILE;  // 64 rows of k, 64 rows of v
   const FtArgs& a;
   hpd_ft_tile t;
@@ -137,7 +158,7 @@ struct QueryTile {
   int32_t q_min, q_max;  // ranks of the wave's queries
   const int32_t* ranks;
   const const_i32* blk_rank;
-  Loader<D> loader;
+  Loader<NB> loader;
   const char* src;
   uint32_t ring_lds;
 
@@ -158,8 +179,8 @@ struct QueryTile {
     token = t.seq0 + (int64_t)ic;
     rounds = (min(t.row0 + 128, t.len) + 63) / 64;
     // this wave's part of a round: waves 0 and 1 keys, 2 and 3 values
-    loader.init(wave < 2 ? a.sk : a.sv, lane);
-    src = reinterpret_cast<const char*>(wave < 2 ? k + t.seq0 * a.sk : v + t.seq0 * a.sv) + (int64_t)hk * D * 2;
+    loader.init(wave < 2 ? a.sk : a.sv, a.D, lane);
+    src = reinterpret_cast<const char*>(wave < 2 ? k + t.seq0 * a.sk : v + t.seq0 * a.sv) + (int64_t)hk * a.D * 2;
     ring_lds = lds_address(ring);
     ranks = a.rank + t.seq0;
     blk_rank = (const const_i32*)(uintptr_t)(a.blk_rank + t.blk0);
@@ -171,14 +192,10 @@ struct QueryTile {
     const uint32_t dst = ring_lds + (round & 1) * STAGE + (wave >> 1) * 2 * R::TILE;
 #pragma unroll
     for (int j = 0; j < 32 / R::GROUP; ++j) {
-      const int32_t row = D == 128 ? 32 * j + 16 * (wave & 1) : 32 * (wave & 1);
+      const int32_t row = R::RB == 256 ? 32 * j + 16 * (wave & 1) : 32 * (wave & 1);
       const int32_t first = min(round * 64 + row, t.len - 1);
       loader.load(src + first * loader.stride, dst + row * R::RB, t.len - 1 - first, lane);
     }
-  }
-  static __device__ __forceinline__ void own_row(const uint16_t* row, bf16x8* f) {
-#pragma unroll
-    for (int s = 0; s < R::STEPS; ++s) f[s] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const uint4*>(row + s * 16));
   }
   // block b of 32 keys has a key that a query of the wave sees / one that a query does not see
   __device__ __forceinline__ bool reaches(int32_t b) const { return active && b * 32 <= q_first && blk_rank[2 * b] <= q_max; }
@@ -192,9 +209,9 @@ struct QueryTile {
 };
 
 // LDS addresses of a lane's operands in the first tile of a stage
-template <int D>
+template <int NB>
 struct Addresses {
-  using R = Rows<D>;
+  using R = Rows<NB>;
   uint32_t row[R::STEPS], col[2 * R::BLOCKS];
   __device__ __forceinline__ Addresses(uint32_t base, int lane) {
 #pragma unroll
@@ -217,23 +234,23 @@ struct Addresses {
   }
 };
 
-template <int D>
+template <int NB>
 __global__ void __launch_bounds__(256, 2) ft_stream_forward_kernel(FtArgs a, const uint16_t* __restrict__ q,
                                                                   const uint16_t* __restrict__ k,
                                                                   const uint16_t* __restrict__ v, uint16_t* __restrict__ out,
                                                                   float* __restrict__ lse) {
-  using R = Rows<D>;
-  using Q = QueryTile<D>;
+  using R = Rows<NB>;
+  using Q = QueryTile<NB>;
   __shared__ __attribute__((aligned(2 * Q::STAGE))) char ring[2 * Q::STAGE];
   const Q w(a, k, v, ring);
   w.issue(0);
   bf16x8 qf[R::STEPS];
-  Q::own_row(q + w.token * a.sq + w.hq * D + w.h * 8, qf);
+  own_row(q + w.token * a.sq + w.hq * a.D, a.D, w.h, qf);
   int32_t rank_i[1] = {a.rank[w.token]};
   arrived(qf);
   arrived(rank_i);
   const float c = a.scale * LOG2E;
-  Addresses<D> at(w.ring_lds, w.lane);
+  Addresses<NB> at(w.ring_lds, w.lane);
 
   floatx16 acc[R::BLOCKS];
   zero(acc, R::BLOCKS);
@@ -309,21 +326,21 @@ __global__ void __launch_bounds__(256, 2) ft_stream_forward_kernel(FtArgs a, con
   if (!w.active) return;
   l += __shfl_xor(l, 32);
   if (w.h == 0 && w.i < w.t.len) lse[w.hq * a.N + w.token] = (m + __builtin_amdgcn_logf(l)) * LN2;
-  store_rows<D>(ring + w.wave * R::TILE, acc, 1.f / l, out + ((w.t.seq0 + (int64_t)w.q_first) * a.Hq + w.hq) * D,
-                (int64_t)a.Hq * D, w.t.len - w.q_first, w.lane);
+  store_rows<NB>(ring + w.wave * R::TILE, acc, 1.f / l, out + ((w.t.seq0 + (int64_t)w.q_first) * a.Hq + w.hq) * a.D,
+                 (int64_t)a.Hq * a.D, w.t.len - w.q_first, a.D, w.lane);
 }
 
 // stat, which this kernel makes and the dk/dv kernel reads: per (head, token) -lse * sqrt(D), where its row's score
 // products start, then -delta, delta_i = do_i . o_i, where its row's products with v start:
 // p = exp((q . k - lse sqrt(D)) / sqrt(D)).
-template <int D>
+template <int NB>
 __global__ void __launch_bounds__(256, 2) ft_stream_dq_kernel(FtArgs a, const uint16_t* __restrict__ q,
                                                              const uint16_t* __restrict__ k, const uint16_t* __restrict__ v,
                                                              const uint16_t* __restrict__ out, const uint16_t* __restrict__ d_out,
                                                              const float* __restrict__ lse, float* __restrict__ stat,
                                                              uint16_t* __restrict__ dq) {
-  using R = Rows<D>;
-  using Q = QueryTile<D>;
+  using R = Rows<NB>;
+  using Q = QueryTile<NB>;
   __shared__ __attribute__((aligned(2 * Q::STAGE))) char ring[2 * Q::STAGE];
   const Q w(a, k, v, ring);
   w.issue(0);
@@ -331,10 +348,10 @@ __global__ void __launch_bounds__(256, 2) ft_stream_dq_kernel(FtArgs a, const ui
   float nl[1], nd[1];
   {
     bf16x8 o[R::STEPS];
-    const int64_t row = (w.token * a.Hq + w.hq) * D + w.h * 8;
-    Q::own_row(q + w.token * a.sq + w.hq * D + w.h * 8, qf);
-    Q::own_row(d_out + row, of);
-    Q::own_row(out + row, o);
+    const int64_t row = (w.token * a.Hq + w.hq) * a.D;
+    own_row(q + w.token * a.sq + w.hq * a.D, a.D, w.h, qf);
+    own_row(d_out + row, a.D, w.h, of);
+    own_row(out + row, a.D, w.h, o);
     const float minus_lse = -lse[w.hq * a.N + w.token];
     float delta = 0.f;
 #pragma unroll
@@ -359,7 +376,7 @@ __global__ void __launch_bounds__(256, 2) ft_stream_dq_kernel(FtArgs a, const ui
   arrived(nd);
   arrived(rank_i);
   const float c = a.scale * LOG2E;
-  Addresses<D> at(w.ring_lds, w.lane);
+  Addresses<NB> at(w.ring_lds, w.lane);
   floatx16 acc[R::BLOCKS];
   zero(acc, R::BLOCKS);
   // One round, two blocks of 32 keys.  The first block's weights and gradients are made while the second block's
@@ -417,27 +434,26 @@ __global__ void __launch_bounds__(256, 2) ft_stream_dq_kernel(FtArgs a, const ui
   }
   wait_lds_and_barrier();
   if (!w.active) return;
-  store_rows<D>(ring + w.wave * R::TILE, acc, a.scale, dq + (w.t.seq0 + (int64_t)w.q_first) * a.sdq + w.hq * D, a.sdq,
-                w.t.len - w.q_first, w.lane);
+  store_rows<NB>(ring + w.wave * R::TILE, acc, a.scale, dq + (w.t.seq0 + (int64_t)w.q_first) * a.sdq + w.hq * a.D, a.sdq,
+                 w.t.len - w.q_first, a.D, w.lane);
 }
 
 // dk and dv: four waves of 32 keys of one kv head, over the queries of all its heads; rounds of 32 queries, two in
 // LDS.  The wave's keys are in registers, its values, for want of room there, in LDS.  An item is a run of
 // a tile's rounds; the sums of a tile that is cut into several go to `partial`, register by register, and a
 // second kernel adds them up.
-template <int D>
+template <int NB>
 struct KeyTile {
-  using R = Rows<D>;
-  static constexpr int SUMS = 32 * D;                // fp32 sums of a wave
+  static constexpr int SUMS = 32 * 32 * NB;          // fp32 sums of a wave
   static constexpr int PARTIAL = 2 * 4 * SUMS;       // of an item and kv head: dk and dv of four waves
 };
-template <int D>
+template <int NB>
 __global__ void __launch_bounds__(256, 2) ft_stream_dkv_kernel(FtArgs a, const hpd_ft_item* __restrict__ items,
                                                               const uint16_t* __restrict__ q, const uint16_t* __restrict__ k,
                                                               const uint16_t* __restrict__ v, const uint16_t* __restrict__ d_out,
                                                               const float* __restrict__ stat, float* __restrict__ partial,
                                                               uint16_t* __restrict__ dk, uint16_t* __restrict__ dv) {
-  using R = Rows<D>;
+  using R = Rows<NB>;
   constexpr int STAGE = 2 * R::TILE;  // rows of q and of do
   __shared__ __attribute__((aligned(2 * STAGE))) char ring[2 * STAGE];
   __shared__ __attribute__((aligned(1024))) char values[4 * R::TILE];
@@ -452,17 +468,17 @@ __global__ void __launch_bounds__(256, 2) ft_stream_dkv_kernel(FtArgs a, const h
   const int64_t token = t.seq0 + (int64_t)min(j, t.len - 1);
 
   // this wave's part of a round: waves 0 and 1 queries, 2 and 3 gradients of the output
-  Loader<D> loader;
-  loader.init(wave < 2 ? a.sq : (int64_t)a.Hq * D, lane);
-  const char* const src = reinterpret_cast<const char*>(wave < 2 ? q + t.seq0 * a.sq : d_out + (int64_t)t.seq0 * a.Hq * D);
+  Loader<NB> loader;
+  loader.init(wave < 2 ? a.sq : (int64_t)a.Hq * a.D, a.D, lane);
+  const char* const src = reinterpret_cast<const char*>(wave < 2 ? q + t.seq0 * a.sq : d_out + (int64_t)t.seq0 * a.Hq * a.D);
   const uint32_t ring_lds = lds_address(ring), stats_lds = lds_address(stats);
   const int32_t b_first = t.row0 / 32, per_head = (t.len + 31) / 32 - b_first;
   int32_t next_g = t.begin / per_head, next_b = b_first + t.begin % per_head;  // the round that is requested next
   auto issue = [&](int32_t slot) {
     const int32_t hq = hk * G + next_g;
-    if (D == 128 || (wave & 1) == 0) {  // (a tile of 64 channels is one group)
-      const int32_t row = D == 128 ? 16 * (wave & 1) : 0, first = min(next_b * 32 + row, t.len - 1);
-      loader.load(src + first * loader.stride + hq * D * 2, ring_lds + slot * STAGE + (wave >> 1) * R::TILE + row * R::RB,
+    if (R::RB == 256 || (wave & 1) == 0) {  // (a tile of 64 channels is one group)
+      const int32_t row = R::RB == 256 ? 16 * (wave & 1) : 0, first = min(next_b * 32 + row, t.len - 1);
+      loader.load(src + first * loader.stride + hq * a.D * 2, ring_lds + slot * STAGE + (wave >> 1) * R::TILE + row * R::RB,
                   t.len - 1 - first, lane);
     }
     if (wave == 3) {
@@ -484,22 +500,19 @@ __global__ void __launch_bounds__(256, 2) ft_stream_dkv_kernel(FtArgs a, const h
   int32_t b = next_b;
   if (t.begin < t.end) issue(0);
   {
-    Loader<D> own_values;
-    own_values.init(a.sv, lane);
-    const char* const base = reinterpret_cast<const char*>(v + t.seq0 * a.sv + (int64_t)hk * D);
+    Loader<NB> own_values;
+    own_values.init(a.sv, a.D, lane);
+    const char* const base = reinterpret_cast<const char*>(v + t.seq0 * a.sv + (int64_t)hk * a.D);
+    const void* const zeros = a.D < 32 * NB ? a.rank + a.N : nullptr;
 #pragma unroll
     for (int x = 0; x < 32 / R::GROUP; ++x) {
       const int32_t first = min(own + x * R::GROUP, t.len - 1);
       own_values.load(base + first * own_values.stride, lds_address(values) + wave * R::TILE + x * R::GROUP * R::RB,
-                      t.len - 1 - first, lane);
+                      t.len - 1 - first, lane, zeros);
     }
   }
   bf16x8 kf[R::STEPS];
-  {
-    const uint16_t* row = k + token * a.sk + (int64_t)hk * D + h * 8;
-#pragma unroll
-    for (int s = 0; s < R::STEPS; ++s) kf[s] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const uint4*>(row + s * 16));
-  }
+  own_row(k + token * a.sk + (int64_t)hk * a.D, a.D, h, kf);
   int32_t rank_j[1] = {a.rank[token]};
   arrived(kf);
   arrived(rank_j);
@@ -602,75 +615,89 @@ __global__ void __launch_bounds__(256, 2) ft_stream_dkv_kernel(FtArgs a, const h
   wait_vector_memory<0>();
   wait_lds_and_barrier();
   if (t.slot >= 0) {
-    float* p = partial + ((int64_t)t.slot * a.Hkv + hk) * KeyTile<D>::PARTIAL + wave * KeyTile<D>::SUMS + lane * 4;
+    float* p = partial + ((int64_t)t.slot * a.Hkv + hk) * KeyTile<NB>::PARTIAL + wave * KeyTile<NB>::SUMS + lane * 4;
 #pragma unroll
     for (int x = 0; x < R::BLOCKS; ++x)
 #pragma unroll
       for (int z = 0; z < 4; ++z) {
         const int at = (x * 4 + z) * 256;
         *reinterpret_cast<float4*>(p + at) = make_float4(acc_k[x][4 * z], acc_k[x][4 * z + 1], acc_k[x][4 * z + 2], acc_k[x][4 * z + 3]);
-        *reinterpret_cast<float4*>(p + at + 4 * KeyTile<D>::SUMS) =
+        *reinterpret_cast<float4*>(p + at + 4 * KeyTile<NB>::SUMS) =
             make_float4(acc_v[x][4 * z], acc_v[x][4 * z + 1], acc_v[x][4 * z + 2], acc_v[x][4 * z + 3]);
       }
     return;
   }
   if (!active) return;
   const int64_t first = t.seq0 + (int64_t)k_first;
-  store_rows<D>(ring + wave * R::TILE, acc_v, 1.f, dv + first * a.sdv + hk * D, a.sdv, t.len - k_first, lane);
-  store_rows<D>(ring + wave * R::TILE, acc_k, a.scale, dk + first * a.sdk + hk * D, a.sdk, t.len - k_first, lane);
+  store_rows<NB>(ring + wave * R::TILE, acc_v, 1.f, dv + first * a.sdv + hk * a.D, a.sdv, t.len - k_first, a.D, lane);
+  store_rows<NB>(ring + wave * R::TILE, acc_k, a.scale, dk + first * a.sdk + hk * a.D, a.sdk, t.len - k_first, a.D, lane);
 }
 
-// adds up a tile's partial sums, in the order of its items
-template <int D>
-__global__ void __launch_bounds__(256) ft_stream_dkv_join_kernel(FtArgs a, const hpd_ft_item* __restrict__ joins,
-                                                               const float* __restrict__ partial, uint16_t* __restrict__ dk,
-                                                               uint16_t* __restrict__ dv) {
-  using R = Rows<D>;
-  __shared__ __attribute__((aligned(1024))) char turn[4 * R::TILE];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int32_t hk = blockIdx.x % a.Hkv;
-  const hpd_ft_item t = joins[blockIdx.x / a.Hkv];  // slots [slot, slot + end)
-  const int32_t k_first = t.row0 + wave * 32;
+// Adds up a tile's partial sums, in the order of its items.  A workgroup has 32 keys of dk (even) or dv, a wave one block of
+// channels; the sums of four items are on their way at a time.
+template <int NB>
+__global__ void __launch_bounds__(64 * NB) ft_stream_dkv_join_kernel(FtArgs a, const hpd_ft_item* __restrict__ joins,
+                                                                   const float* __restrict__ partial, uint16_t* __restrict__ dk,
+                                                                   uint16_t* __restrict__ dv) {
+  constexpr int PITCH = 64 * NB + 16;  // bytes of a row of the result
+  __shared__ __attribute__((aligned(16))) char turn[32 * PITCH];
+  const int lane = threadIdx.x & 63, n = lane & 31, h = lane >> 5, x = threadIdx.x >> 6;
+  const int32_t y = blockIdx.x & 1, rows32 = blockIdx.x >> 1 & 3, hk = (blockIdx.x >> 3) % a.Hkv;
+  const hpd_ft_item t = joins[(blockIdx.x >> 3) / a.Hkv];  // slots [slot, slot + end)
+  const int32_t k_first = t.row0 + rows32 * 32;
   if (k_first >= t.len) return;
-  const int64_t first = t.seq0 + (int64_t)k_first;
+  const int64_t step = (int64_t)a.Hkv * KeyTile<NB>::PARTIAL;
+  const float* p = partial + ((int64_t)t.slot * a.Hkv + hk) * KeyTile<NB>::PARTIAL + (4 * y + rows32) * KeyTile<NB>::SUMS +
+                   x * 1024 + lane * 4;
+  float4 sum[4] = {};
+  for (int32_t i = 0; i < t.end; i += 4) {
+    float4 w[4][4];
 #pragma unroll
-  for (int y = 0; y < 2; ++y) {
-    floatx16 acc[R::BLOCKS];
-    zero(acc, R::BLOCKS);
-    for (int32_t i = 0; i < t.end; ++i) {
-      const float* p = partial + ((int64_t)(t.slot + i) * a.Hkv + hk) * KeyTile<D>::PARTIAL + (4 * y + wave) * KeyTile<D>::SUMS + lane * 4;
+    for (int j = 0; j < 4; ++j)
 #pragma unroll
-      for (int x = 0; x < R::BLOCKS; ++x)
+      for (int z = 0; z < 4; ++z)
+        if (i + j < t.end) w[j][z] = *reinterpret_cast<const float4*>(p + (i + j) * step + z * 256);
 #pragma unroll
-        for (int z = 0; z < 4; ++z) {
-          const float4 w = *reinterpret_cast<const float4*>(p + (x * 4 + z) * 256);
-          acc[x][4 * z] += w.x; acc[x][4 * z + 1] += w.y; acc[x][4 * z + 2] += w.z; acc[x][4 * z + 3] += w.w;
+    for (int j = 0; j < 4; ++j)
+#pragma unroll
+      for (int z = 0; z < 4; ++z)
+        if (i + j < t.end) {
+          sum[z].x += w[j][z].x; sum[z].y += w[j][z].y; sum[z].z += w[j][z].z; sum[z].w += w[j][z].w;
         }
-    }
-    if (y == 0) store_rows<D>(turn + wave * R::TILE, acc, a.scale, dk + first * a.sdk + hk * D, a.sdk, t.len - k_first, lane);
-    else store_rows<D>(turn + wave * R::TILE, acc, 1.f, dv + first * a.sdv + hk * D, a.sdv, t.len - k_first, lane);
-    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+  }
+  const float f = y ? 1.f : a.scale;
+#pragma unroll
+  for (int z = 0; z < 4; ++z)  // channels 32 x + 8 z + 4 h ..
+    *reinterpret_cast<uint2*>(turn + n * PITCH + x * 64 + z * 16 + h * 8) =
+        make_uint2(cvt_pk_bf16(sum[z].x * f, sum[z].y * f), cvt_pk_bf16(sum[z].z * f, sum[z].w * f));
+  __syncthreads();
+  const int64_t stride = y ? a.sdv : a.sdk;
+  uint16_t* const out = (y ? dv : dk) + (t.seq0 + (int64_t)k_first) * stride + hk * a.D;
+  for (int i = threadIdx.x; i < 32 * 4 * NB; i += 64 * NB) {
+    const int r = i / (4 * NB), c = i % (4 * NB);
+    if (k_first + r < t.len && c * 8 < a.D)
+      *reinterpret_cast<uint4*>(out + r * stride + c * 8) = *reinterpret_cast<const uint4*>(turn + r * PITCH + c * 16);
   }
 }
 
-template <int D>
+template <int NB>
 hipError_t forward(const hpd_finetune_layout* L, const FtArgs& a, const void* q, const void* k, const void* v, void* out,
                    float* lse, hipStream_t s) {
-  ft_stream_forward_kernel<D><<<dim3((unsigned)L->tiles.size() * a.Hq), 256, 0, s>>>(
+  ft_stream_forward_kernel<NB><<<dim3((unsigned)L->tiles.size() * a.Hq), 256, 0, s>>>(
       a, (const uint16_t*)q, (const uint16_t*)k, (const uint16_t*)v, (uint16_t*)out, lse);
   return hipGetLastError();
 }
 
-template <int D>
+template <int NB>
 hipError_t backward(const hpd_finetune_layout* L, FtArgs a, const uint16_t* q, const uint16_t* k, const uint16_t* v,
                     const uint16_t* out, const float* lse, const uint16_t* d_out, uint16_t* dq, uint16_t* dk, uint16_t* dv,
                     float* stat, hipStream_t s) {
-  ft_stream_dq_kernel<D><<<dim3((unsigned)L->tiles.size() * a.Hq), 256, 0, s>>>(a, q, k, v, out, d_out, lse, stat, dq);
+  ft_stream_dq_kernel<NB><<<dim3((unsigned)L->tiles.size() * a.Hq), 256, 0, s>>>(a, q, k, v, out, d_out, lse, stat, dq);
   float* partial = stat + 2 * a.N * a.Hq + (-2 * a.N * a.Hq & 3);  // (on 16 bytes)
-  ft_stream_dkv_kernel<D><<<dim3((unsigned)L->items.size() * a.Hkv), 256, 0, s>>>(a, L->d_items, q, k, v, d_out, stat, partial,
+  ft_stream_dkv_kernel<NB><<<dim3((unsigned)L->items.size() * a.Hkv), 256, 0, s>>>(a, L->d_items, q, k, v, d_out, stat, partial,
                                                                                dk, dv);
   if (!L->joins.empty())
-    ft_stream_dkv_join_kernel<D><<<dim3((unsigned)L->joins.size() * a.Hkv), 256, 0, s>>>(a, L->d_joins, partial, dk, dv);
+    ft_stream_dkv_join_kernel<NB><<<dim3((unsigned)L->joins.size() * a.Hkv * 8), 64 * NB, 0, s>>>(a, L->d_joins, partial, dk, dv);
   return hipGetLastError();
 }
 
@@ -678,13 +705,14 @@ hipError_t backward(const hpd_finetune_layout* L, FtArgs a, const uint16_t* q, c
 
 hipError_t hpd_launch_ft_stream_forward(const hpd_finetune_layout* L, FtArgs a, const void* q, const void* k, const void* v,
                                         void* out, float* lse, hipStream_t s) {
-  return a.D == 64 ? forward<64>(L, a, q, k, v, out, lse, s) : forward<128>(L, a, q, k, v, out, lse, s);
+  const auto run = a.D <= 32 ? forward<1> : a.D <= 64 ? forward<2> : a.D <= 96 ? forward<3> : forward<4>;
+  return run(L, a, q, k, v, out, lse, s);
 }
 
 hipError_t hpd_launch_ft_stream_backward(const hpd_finetune_layout* L, FtArgs a, const void* q, const void* k, const void* v,
                                          const void* out, const float* lse, const void* d_out, void* dq, void* dk, void* dv,
                                          void* workspace, hipStream_t s) {
-  const auto run = a.D == 64 ? backward<64> : backward<128>;
+  const auto run = a.D <= 32 ? backward<1> : a.D <= 64 ? backward<2> : a.D <= 96 ? backward<3> : backward<4>;
   return run(L, a, (const uint16_t*)q, (const uint16_t*)k, (const uint16_t*)v, (const uint16_t*)out, lse,
              (const uint16_t*)d_out, (uint16_t*)dq, (uint16_t*)dk, (uint16_t*)dv, (float*)workspace, s);
 }

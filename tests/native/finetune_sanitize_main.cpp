@@ -44,40 +44,37 @@ static std::vector<int32_t> table(const hpd_finetune_layout* L, int32_t what, si
   return v;
 }
 
-// every 128 tokens of every sequence are one query tile and one key tile, longest first
+// every 128 tokens of every sequence are one tile of queries, longest first
 static void check_tiles(const hpd_finetune_layout* L, const std::vector<int32_t>& off) {
   size_t expect = 0;
   for (int32_t s = 0; s < L->n_seq; ++s) expect += (off[s + 1] - off[s] + 127) / 128;
-  CHECK(L->tiles.size() == expect && L->key_tiles.size() == expect);
+  CHECK(L->tiles.size() == expect);
   std::map<std::pair<int32_t, int32_t>, int> seen;
   for (size_t i = 0; i < expect; ++i) {
-    const hpd_ft_tile &a = L->tiles[i], &b = L->key_tiles[i];
+    const hpd_ft_tile& a = L->tiles[i];
     CHECK(a.row0 < a.len && a.row0 % 128 == 0 && a.seq0 + a.len <= L->n_tokens);
     CHECK((size_t)(a.blk0 + (a.len + 31) / 32) * 2 <= L->blk_rank.size());
     seen[{a.seq0, a.row0}] += 1;
-    seen[{b.seq0, b.row0}] += 16;
     if (i) CHECK(std::min(L->tiles[i - 1].row0 + 128, L->tiles[i - 1].len) >= std::min(a.row0 + 128, a.len));
-    if (i) CHECK(L->key_tiles[i - 1].len - L->key_tiles[i - 1].row0 >= b.len - b.row0);
   }
-  for (const auto& x : seen) CHECK(x.second == 17);
+  for (const auto& x : seen) CHECK(x.second == 1);
 }
 
 // the items of a key tile are its rounds, each once; a tile of several has as many slots in a row
 static void check_items(const hpd_finetune_layout* L) {
-  if (!hpd_ft_stream_supported(L)) {
-    CHECK(L->items.empty() && L->joins.empty() && L->slots == 0);
-    return;
-  }
+  const int32_t rows_of = hpd_ft_key_rows(L);
+  size_t expect = 0;
+  for (int32_t s = 0; s < L->n_seq; ++s) expect += (L->seq_off[s + 1] - L->seq_off[s] + rows_of - 1) / rows_of;
   const int64_t G = L->cfg.n_q_heads / L->cfg.n_kv_heads;
   std::map<std::pair<int32_t, int32_t>, std::map<int32_t, hpd_ft_item>> tiles;
   for (size_t i = 0; i < L->items.size(); ++i) {
     const hpd_ft_item& x = L->items[i];
-    CHECK(x.begin < x.end && x.slot < L->slots);
+    CHECK(x.begin < x.end && x.slot < L->slots && x.row0 < x.len && x.row0 % rows_of == 0);
     if (i) CHECK(L->items[i - 1].end - L->items[i - 1].begin >= x.end - x.begin);
     const bool fresh = tiles[{x.seq0, x.row0}].emplace(x.begin, x).second;
     CHECK(fresh);
   }
-  CHECK(tiles.size() == L->key_tiles.size());
+  CHECK(tiles.size() == expect);
   std::map<std::pair<int32_t, int32_t>, hpd_ft_item> joins;
   int32_t slots = 0;
   for (const hpd_ft_item& x : L->joins) {
@@ -101,7 +98,7 @@ static void check_items(const hpd_finetune_layout* L) {
     if (join != joins.end()) CHECK(join->second.end == n);
   }
   const int64_t rows = (int64_t)L->n_tokens * L->cfg.n_q_heads;
-  CHECK(hpd_ft_backward_bytes(L) >= rows * 8 + (int64_t)L->slots * L->cfg.n_kv_heads * 256 * L->cfg.head_dim * 4);
+  CHECK(hpd_ft_backward_bytes(L) >= rows * 8 + (int64_t)L->slots * L->cfg.n_kv_heads * 2 * rows_of * hpd_ft_padded_dim(L) * 4);
 }
 
 int main() {
