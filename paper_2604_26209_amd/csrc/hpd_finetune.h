@@ -20,7 +20,8 @@ struct hpd_ft_tile {
   int32_t blk0;  // the sequence's first entry in blk_rank
 };
 
-// A run of the rounds (32 queries of one head each, head by head) of a tile of keys and of one kv head.
+// A run of the rounds of a tile: for one of keys and a kv head, 32 queries of one head each, head by head; for one of
+// queries and a head, 64 keys each.
 struct hpd_ft_item {
   int32_t seq0, len, row0, blk0;  // of the tile
   int32_t begin, end;             // rounds
@@ -34,16 +35,17 @@ struct hpd_finetune_layout {
   std::vector<int32_t> seq_off, pos, rank;
   std::vector<int32_t> blk_rank;        // [blocks][2]: lowest and highest rank of 32 tokens of a sequence
   std::vector<hpd_ft_tile> tiles;       // query tiles, those with most keys first
-  // the tiles of keys as items, longest first, and for those of several items the first slot and (as `end`) their number
-  std::vector<hpd_ft_item> items, joins;
-  int32_t slots = 0;
+  // the tiles of keys and (bf16) of queries as items, longest first, and for those of several items the first slot and (as
+  // `end`) their number
+  std::vector<hpd_ft_item> items, joins, query_items, query_joins;
+  int32_t slots = 0, query_slots = 0;
 
   bool on_device = false;
   void* d_mem = nullptr;
   const int32_t *d_pos = nullptr, *d_rank = nullptr;
   const int2* d_blk_rank = nullptr;
   const hpd_ft_tile* d_tiles = nullptr;
-  const hpd_ft_item *d_items = nullptr, *d_joins = nullptr;
+  const hpd_ft_item *d_items = nullptr, *d_joins = nullptr, *d_query_items = nullptr, *d_query_joins = nullptr;
   // (cos, sin) rows of D/2: one per position ID, or one per token where that is fewer
   float2* d_rope = nullptr;
   int32_t rope_rows = 0;

@@ -124,10 +124,10 @@ hipError_t hpd_launch_ft_rotate(const hpd_finetune_layout* L, bool inverse, cons
 }
 
 hipError_t hpd_launch_ft_attention(const hpd_finetune_layout* L, const void* q, const void* k, const void* v, void* out,
-                                   float* lse, void*, const hpd_finetune_strides& st, hipStream_t s) {
+                                   float* lse, void* workspace, const hpd_finetune_strides& st, hipStream_t s) {
   const FtArgs a = make_args(L, st);
   if (L->cfg.dtype == HPD_F32) return hpd_launch_ft_f32_forward(L, a, q, k, v, out, lse, s);
-  return hpd_launch_ft_stream_forward(L, a, q, k, v, out, lse, s);
+  return hpd_launch_ft_stream_forward(L, a, q, k, v, out, lse, workspace, s);
 }
 
 hipError_t hpd_launch_ft_attention_backward(const hpd_finetune_layout* L, const void* q, const void* k, const void* v,

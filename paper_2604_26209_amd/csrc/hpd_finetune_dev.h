@@ -22,7 +22,7 @@ hipError_t hpd_launch_ft_f32_backward(const hpd_finetune_layout* L, FtArgs a, co
                                       void* workspace, hipStream_t s);
 // Kernels for bf16 (hpd_finetune_stream.hip).
 hipError_t hpd_launch_ft_stream_forward(const hpd_finetune_layout* L, FtArgs a, const void* q, const void* k, const void* v,
-                                        void* out, float* lse, hipStream_t s);
+                                        void* out, float* lse, void* workspace, hipStream_t s);
 hipError_t hpd_launch_ft_stream_backward(const hpd_finetune_layout* L, FtArgs a, const void* q, const void* k, const void* v,
                                          const void* out, const float* lse, const void* d_out, void* dq, void* dk, void* dv,
                                          void* workspace, hipStream_t s);

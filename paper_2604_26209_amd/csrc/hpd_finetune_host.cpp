@@ -34,35 +34,48 @@ int validate(const hpd_finetune_config* c) {
   return HPD_OK;
 }
 
-// The items of the dk/dv kernels.  Two workgroups run on a CU at a time (one for fp32 with more than 64 channels); a tile
-// at the start of a long sequence has many times the rounds of others, and a batch may have fewer tiles than the GPU has room for.
-// Tiles are cut so that an item is at most a third of what a workgroup's place has to do (a half: 4045 -> 4140 us on 2 x 6100
-// tokens, 64/8 heads), but in bf16 not below 64 rounds, or 24 where there is room for more workgroups than tiles: an item
-// starts and ends with the time of four, and its sums are written and read once more (24 always: 545 -> 585 us on 32 x 420
-// tokens, 32/8 heads).  In fp32 the waves share the rounds, 16 at least: four each (8 and 32: 1 % faster and 2 % slower in the
-// mean of 24 random batches; not cut at all: 473 -> 84 us on one sequence of 774 tokens, 12/2 heads of 96).
+// Cuts tiles into items of about `most` rounds, longest first.
+template <typename Rounds>
+void cut(const std::vector<hpd_ft_tile>& tiles, int64_t most, Rounds rounds, std::vector<hpd_ft_item>& items,
+         std::vector<hpd_ft_item>& joins, int32_t& slots) {
+  for (const hpd_ft_tile& t : tiles) {
+    const int64_t r = rounds(t), parts = r * 2 > most * 3 ? (r + most - 1) / most : 1;
+    if (parts > 1) joins.push_back({t.seq0, t.len, t.row0, t.blk0, 0, (int32_t)parts, slots, 0});
+    for (int64_t p = 0; p < parts; ++p)
+      items.push_back({t.seq0, t.len, t.row0, t.blk0, (int32_t)(r * p / parts), (int32_t)(r * (p + 1) / parts),
+                       parts > 1 ? slots++ : -1, 0});
+  }
+  std::stable_sort(items.begin(), items.end(),
+                   [](const hpd_ft_item& a, const hpd_ft_item& b) { return a.end - a.begin > b.end - b.begin; });
+}
+
+// The items of the kernels.  Two workgroups run on a CU at a time (one for fp32 with more than 64 channels).  A tile at
+// the start of a long sequence has many times the rounds of others, and a batch may have fewer tiles than the GPU has room
+// for: an item has at most a third of what a workgroup's place has to do (a half: 4045 -> 4140 us for the gradients of
+// 2 x 6100 tokens, 64/8 heads).  It starts and ends with the time of four rounds, and its sums are written and read once more, so
+// it has no fewer than four and those of a place, up to 64.  bf16 gradients of 50 random batches, geometric means over 24 rounds
+// at least (64 where there are more tiles than places): 0.89; with three 0.89, six 0.91, with 0.6 or 1.5 times those of a place 0.90 and
+// 0.91.  The queries, over whole tiles (of 50 random batches ten are cut): 0.98, up to 0.71 for a single sequence; with six or ten
+// 0.985 and 0.99.  In fp32 the waves of a workgroup share the rounds: 16 at least (8 and 32: 1 % faster, 2 % slower over 24 batches;
+// not cut: 473 -> 89 us for a sequence of 774 tokens, 12/2 heads of 96).
 void plan_items(hpd_finetune_layout* L, int32_t n_cus) {
-  const int64_t Hkv = L->cfg.n_kv_heads, G = L->cfg.n_q_heads / Hkv;
+  const int64_t Hq = L->cfg.n_q_heads, Hkv = L->cfg.n_kv_heads, G = Hq / Hkv;
   const int32_t rows = hpd_ft_key_rows(L);
   const bool bf16 = L->cfg.dtype == HPD_BF16;
   std::vector<hpd_ft_tile> tiles;
   for (const hpd_ft_tile& t : L->tiles)
     for (int32_t r = t.row0; r < std::min(t.row0 + HPD_FT_ROWS, t.len); r += rows) tiles.push_back({t.seq0, t.len, r, t.blk0});
-  auto rounds = [&](const hpd_ft_tile& t) { return G * ((t.len + 31) / 32 - t.row0 / 32); };
-  int64_t total = 0;
-  for (const hpd_ft_tile& t : tiles) total += rounds(t) * Hkv;
   const int64_t places = (bf16 || L->cfg.head_dim <= 64 ? 2 : 1) * n_cus;
-  const int64_t least = bf16 ? ((int64_t)tiles.size() * Hkv < places ? 24 : 64) : 16;
-  const int64_t most = std::max<int64_t>(least, total / places / 3);
-  for (const hpd_ft_tile& t : tiles) {
-    const int64_t r = rounds(t), parts = r * 2 > most * 3 ? (r + most - 1) / most : 1;
-    if (parts > 1) L->joins.push_back({t.seq0, t.len, t.row0, t.blk0, 0, (int32_t)parts, L->slots, 0});
-    for (int64_t p = 0; p < parts; ++p)
-      L->items.push_back({t.seq0, t.len, t.row0, t.blk0, (int32_t)(r * p / parts), (int32_t)(r * (p + 1) / parts),
-                          parts > 1 ? L->slots++ : -1, 0});
-  }
-  std::stable_sort(L->items.begin(), L->items.end(),
-                   [](const hpd_ft_item& a, const hpd_ft_item& b) { return a.end - a.begin > b.end - b.begin; });
+  auto most = [&](int64_t total) { return std::max(std::min<int64_t>(64, 4 + total / places), total / places / 3); };
+  auto key_rounds = [&](const hpd_ft_tile& t) { return G * ((t.len + 31) / 32 - t.row0 / 32); };
+  auto query_rounds = [&](const hpd_ft_tile& t) { return (int64_t)(std::min(t.row0 + HPD_FT_ROWS, t.len) + 63) / 64; };
+  int64_t total = 0;
+  for (const hpd_ft_tile& t : tiles) total += key_rounds(t) * Hkv;
+  cut(tiles, bf16 ? most(total) : std::max<int64_t>(16, total / places / 3), key_rounds, L->items, L->joins, L->slots);
+  if (!bf16) return;
+  total = 0;
+  for (const hpd_ft_tile& t : L->tiles) total += query_rounds(t) * Hq;
+  cut(L->tiles, most(total), query_rounds, L->query_items, L->query_joins, L->query_slots);
 }
 
 // Positions (Algorithm 2, values at pos_id[end(a_n)] + k), ranks, rank ranges of blocks, work tiles.
@@ -123,15 +136,20 @@ int upload(hpd_finetune_layout* L, hipStream_t s) {
   // (the kernels read the ranks of two whole blocks at a time: up to 63 more behind the last token)
   const size_t n = (size_t)L->n_tokens, nt = L->tiles.size() * 4;
   const size_t o_rank = pad(n), o_blk = o_rank + pad(n + 2 * HPD_FT_BLOCK), o_tiles = o_blk + pad(L->blk_rank.size()),
-               o_items = o_tiles + nt, o_joins = o_items + L->items.size() * 8,
-               words = o_joins + L->joins.size() * 8;
+               o_items = o_tiles + nt;
+  const std::vector<hpd_ft_item>* const lists[] = {&L->items, &L->joins, &L->query_items, &L->query_joins};
+  size_t words = o_items;
+  for (const auto* l : lists) words += l->size() * 8;
   std::vector<int32_t> host(words, 0);
   std::copy(L->pos.begin(), L->pos.end(), host.begin());
   std::copy(L->rank.begin(), L->rank.end(), host.begin() + o_rank);
   std::copy(L->blk_rank.begin(), L->blk_rank.end(), host.begin() + o_blk);
   std::memcpy(host.data() + o_tiles, L->tiles.data(), nt * 4);
-  if (!L->items.empty()) std::memcpy(host.data() + o_items, L->items.data(), L->items.size() * sizeof(hpd_ft_item));
-  if (!L->joins.empty()) std::memcpy(host.data() + o_joins, L->joins.data(), L->joins.size() * sizeof(hpd_ft_item));
+  size_t at = o_items;
+  for (const auto* l : lists) {
+    if (!l->empty()) std::memcpy(host.data() + at, l->data(), l->size() * sizeof(hpd_ft_item));
+    at += l->size() * 8;
+  }
   const size_t rope_bytes = (size_t)L->rope_rows * (size_t)(L->cfg.head_dim / 2) * sizeof(float2);
   HPD_HIP(hipMalloc(&L->d_mem, words * 4 + rope_bytes));
   const int32_t* base = (const int32_t*)L->d_mem;
@@ -140,7 +158,9 @@ int upload(hpd_finetune_layout* L, hipStream_t s) {
   L->d_blk_rank = (const int2*)(base + o_blk);
   L->d_tiles = (const hpd_ft_tile*)(base + o_tiles);
   L->d_items = (const hpd_ft_item*)(base + o_items);
-  L->d_joins = (const hpd_ft_item*)(base + o_joins);
+  L->d_joins = L->d_items + L->items.size();
+  L->d_query_items = L->d_joins + L->joins.size();
+  L->d_query_joins = L->d_query_items + L->query_items.size();
   L->d_rope = (float2*)(base + words);
   HPD_HIP(hipMemcpyAsync(L->d_mem, host.data(), words * 4, hipMemcpyHostToDevice, s));
   hipError_t e = hpd_launch_ft_rope_table(L, s);
@@ -177,11 +197,15 @@ int check_logits(int32_t dtype, int64_t n_rows, int32_t vocab) {
 
 }  // namespace
 
-int64_t hpd_ft_forward_bytes(const hpd_finetune_layout*) { return 0; }
-// two numbers per (head, token), then the partial sums of dk and dv
+// partial results of the queries: sums, and two numbers per token
+int64_t hpd_ft_forward_bytes(const hpd_finetune_layout* L) {
+  return (int64_t)L->query_slots * L->cfg.n_q_heads * HPD_FT_ROWS * (hpd_ft_padded_dim(L) + 2) * 4;
+}
+// two numbers per (head, token), then the partial sums of dk and dv, then those of dq
 int64_t hpd_ft_backward_bytes(const hpd_finetune_layout* L) {
   const int64_t rows = (int64_t)L->n_tokens * L->cfg.n_q_heads;
-  return (rows * 8 + 15) / 16 * 16 + (int64_t)L->slots * L->cfg.n_kv_heads * 2 * hpd_ft_key_rows(L) * hpd_ft_padded_dim(L) * 4;
+  return (rows * 8 + 15) / 16 * 16 + (int64_t)L->slots * L->cfg.n_kv_heads * 2 * hpd_ft_key_rows(L) * hpd_ft_padded_dim(L) * 4 +
+         hpd_ft_forward_bytes(L);
 }
 
 extern "C" {

@@ -142,17 +142,41 @@ __device__ __forceinline__ void own_row(const uint16_t* row, int32_t D, int h, b
   }
 }
 
+// The end of the kernels that join items: a workgroup of NB waves has 32 rows, wave x channels 32 x + 8 z + 4 h .. of row n
+template <int NB>
+struct Turn {
+  static constexpr int PITCH = 64 * NB + 16, BYTES = 32 * PITCH;
+  static __device__ __forceinline__ void store(char* turn, const float4* sum, float f, uint16_t* out, int64_t stride, int rows,
+                                               int32_t D) {
+    const int lane = threadIdx.x & 63, n = lane & 31, h = lane >> 5, x = threadIdx.x >> 6;
+#pragma unroll
+    for (int z = 0; z < 4; ++z)
+      *reinterpret_cast<uint2*>(turn + n * PITCH + x * 64 + z * 16 + h * 8) =
+          make_uint2(cvt_pk_bf16(sum[z].x * f, sum[z].y * f), cvt_pk_bf16(sum[z].z * f, sum[z].w * f));
+    __syncthreads();
+    for (int i = threadIdx.x; i < 32 * 4 * NB; i += 64 * NB) {
+      const int r = i / (4 * NB), c = i % (4 * NB);
+      if (r < rows && c * 8 < D)
+        *reinterpret_cast<uint4*>(out + r * stride + c * 8) = *reinterpret_cast<const uint4*>(turn + r * PITCH + c * 16);
+    }
+  }
+};
+
 // ---------------------------------------------------------------------------------------
-// Forward and dq: four waves of 32 queries of one head; rounds of 64 keys, two rounds in LDS.
+// Forward and dq: four waves of 32 queries of one head; rounds of 64 keys, two rounds in LDS.  An item is a run of a
+// tile's rounds; what the waves of a tile with several have goes to `partial`, register by register, and a second kernel
+// joins it.
 // ---------------------------------------------------------------------------------------
 template <int NB>
 struct QueryTile {
   using R = Rows<NB>;
   static constexpr int STAGE = 4 * R::TILE;  // 64 rows of k, 64 rows of v
+  static constexpr int SUMS = 32 * 32 * NB;  // fp32 sums of a wave
+  static constexpr int PARTIAL = SUMS + 64;  // of a wave in `partial`: sums; forward: reference points, sums of the weights
   const FtArgs& a;
-  hpd_ft_tile t;
+  hpd_ft_item t;
   int lane, n, h, wave;
-  int32_t hq, hk, q_first, i, ic, rounds;
+  int32_t hq, hk, q_first, i, ic;
   int64_t token;
   bool active;
   int32_t q_min, q_max;  // ranks of the wave's queries
@@ -162,7 +186,9 @@ struct QueryTile {
   const char* src;
   uint32_t ring_lds;
 
-  __device__ __forceinline__ QueryTile(const FtArgs& args, const uint16_t* k, const uint16_t* v, const char* ring) : a(args) {
+  __device__ __forceinline__ QueryTile(const FtArgs& args, const hpd_ft_item* items, const uint16_t* k, const uint16_t* v,
+                                     const char* ring)
+      : a(args) {
     lane = threadIdx.x & 63;
     n = lane & 31;
     h = lane >> 5;
@@ -171,13 +197,12 @@ struct QueryTile {
     const int32_t G = a.Hq / a.Hkv, rest = blockIdx.x / a.Hkv;
     hk = blockIdx.x % a.Hkv;
     hq = hk * G + rest % G;
-    t = a.tiles[rest / G];
+    t = items[rest / G];
     q_first = t.row0 + wave * 32;
     i = q_first + n;
     ic = min(i, t.len - 1);
     active = q_first < t.len;
     token = t.seq0 + (int64_t)ic;
-    rounds = (min(t.row0 + 128, t.len) + 63) / 64;
     // this wave's part of a round: waves 0 and 1 keys, 2 and 3 values
     loader.init(wave < 2 ? a.sk : a.sv, a.D, lane);
     src = reinterpret_cast<const char*>(wave < 2 ? k + t.seq0 * a.sk : v + t.seq0 * a.sv) + (int64_t)hk * a.D * 2;
@@ -189,13 +214,24 @@ struct QueryTile {
     q_max = blk_rank[2 * own + 1];
   }
   __device__ __forceinline__ void issue(int32_t round) const {
-    const uint32_t dst = ring_lds + (round & 1) * STAGE + (wave >> 1) * 2 * R::TILE;
+    const uint32_t dst = ring_lds + ((round - t.begin) & 1) * STAGE + (wave >> 1) * 2 * R::TILE;
 #pragma unroll
     for (int j = 0; j < 32 / R::GROUP; ++j) {
       const int32_t row = R::RB == 256 ? 32 * j + 16 * (wave & 1) : 32 * (wave & 1);
       const int32_t first = min(round * 64 + row, t.len - 1);
       loader.load(src + first * loader.stride, dst + row * R::RB, t.len - 1 - first, lane);
     }
+  }
+  __device__ __forceinline__ float* partial_of(float* partial) const {
+    return partial + (((int64_t)t.slot * a.Hq + hq) * 4 + wave) * PARTIAL;
+  }
+  __device__ __forceinline__ void put(float* p, const floatx16* acc) const {
+#pragma unroll
+    for (int x = 0; x < NB; ++x)
+#pragma unroll
+      for (int z = 0; z < 4; ++z)
+        *reinterpret_cast<float4*>(p + (x * 4 + z) * 256 + lane * 4) =
+            make_float4(acc[x][4 * z], acc[x][4 * z + 1], acc[x][4 * z + 2], acc[x][4 * z + 3]);
   }
   // block b of 32 keys has a key that a query of the wave sees / one that a query does not see
   __device__ __forceinline__ bool reaches(int32_t b) const { return active && b * 32 <= q_first && blk_rank[2 * b] <= q_max; }
@@ -235,15 +271,16 @@ struct Addresses {
 };
 
 template <int NB>
-__global__ void __launch_bounds__(256, 2) ft_stream_forward_kernel(FtArgs a, const uint16_t* __restrict__ q,
+__global__ void __launch_bounds__(256, 2) ft_stream_forward_kernel(FtArgs a, const hpd_ft_item* __restrict__ items,
+                                                                  const uint16_t* __restrict__ q,
                                                                   const uint16_t* __restrict__ k,
                                                                   const uint16_t* __restrict__ v, uint16_t* __restrict__ out,
-                                                                  float* __restrict__ lse) {
+                                                                  float* __restrict__ lse, float* __restrict__ partial) {
   using R = Rows<NB>;
   using Q = QueryTile<NB>;
   __shared__ __attribute__((aligned(2 * Q::STAGE))) char ring[2 * Q::STAGE];
-  const Q w(a, k, v, ring);
-  w.issue(0);
+  const Q w(a, items, k, v, ring);
+  w.issue(w.t.begin);
   bf16x8 qf[R::STEPS];
   own_row(q + w.token * a.sq + w.hq * a.D, a.D, w.h, qf);
   int32_t rank_i[1] = {a.rank[w.token]};
@@ -315,35 +352,92 @@ __global__ void __launch_bounds__(256, 2) ft_stream_forward_kernel(FtArgs a, con
     }
     l += l0 + l1;
   };
-  for (int32_t round = 0; round < w.rounds; ++round) {
+  for (int32_t round = w.t.begin; round < w.t.end; ++round) {
     wait_vector_memory<0>();
     wait_lds_and_barrier();  // the round is in LDS, the other half of the ring is free
-    if (round + 1 < w.rounds) w.issue(round + 1);
+    if (round + 1 < w.t.end) w.issue(round + 1);
     if (w.reaches(2 * round) || w.reaches(2 * round + 1)) step(2 * round);
     at.flip(Q::STAGE);
   }
   wait_lds_and_barrier();
   if (!w.active) return;
   l += __shfl_xor(l, 32);
+  if (w.t.slot >= 0) {
+    float* const p = w.partial_of(partial);
+    w.put(p, acc);
+    p[Q::SUMS + w.lane] = w.h ? l : m;
+    return;
+  }
   if (w.h == 0 && w.i < w.t.len) lse[w.hq * a.N + w.token] = (m + __builtin_amdgcn_logf(l)) * LN2;
   store_rows<NB>(ring + w.wave * R::TILE, acc, 1.f / l, out + ((w.t.seq0 + (int64_t)w.q_first) * a.Hq + w.hq) * a.D,
                  (int64_t)a.Hq * a.D, w.t.len - w.q_first, a.D, w.lane);
+}
+
+// Joins the items of a tile.  A workgroup has 32 queries of a head, a wave one block of channels; four items are on
+// their way at a time.
+template <int NB>
+__global__ void __launch_bounds__(64 * NB) ft_stream_join_kernel(FtArgs a, const hpd_ft_item* __restrict__ joins,
+                                                               const float* __restrict__ partial, uint16_t* __restrict__ out,
+                                                               float* __restrict__ lse) {
+  using Q = QueryTile<NB>;
+  __shared__ __attribute__((aligned(16))) char turn[Turn<NB>::BYTES];
+  const int lane = threadIdx.x & 63, n = lane & 31, x = threadIdx.x >> 6;
+  const int32_t rows32 = blockIdx.x & 3, hq = (blockIdx.x >> 2) % a.Hq;
+  const hpd_ft_item t = joins[(blockIdx.x >> 2) / a.Hq];  // slots [slot, slot + end)
+  const int32_t first = t.row0 + rows32 * 32;
+  if (first >= t.len) return;
+  const int64_t step = (int64_t)a.Hq * 4 * Q::PARTIAL;
+  const float* const p = partial + (((int64_t)t.slot * a.Hq + hq) * 4 + rows32) * Q::PARTIAL;
+  float4 sum[4] = {};
+  float m = NEG_BIG, l = 0.f;
+  for (int32_t i = 0; i < t.end; i += 4) {
+    float4 w[4][4];
+    float mi[4], li[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      mi[j] = NEG_BIG;
+      if (i + j >= t.end) continue;
+      const float* const from = p + (i + j) * step;
+      mi[j] = from[Q::SUMS + n];
+      li[j] = from[Q::SUMS + 32 + n];
+#pragma unroll
+      for (int z = 0; z < 4; ++z) w[j][z] = *reinterpret_cast<const float4*>(from + (x * 4 + z) * 256 + lane * 4);
+    }
+    const float top = fmaxf(fmaxf(fmaxf(mi[0], mi[1]), fmaxf(mi[2], mi[3])), m), alpha = fast_exp2(m - top);
+    m = top;
+    l *= alpha;
+#pragma unroll
+    for (int z = 0; z < 4; ++z) sum[z] = make_float4(sum[z].x * alpha, sum[z].y * alpha, sum[z].z * alpha, sum[z].w * alpha);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      if (i + j >= t.end) continue;
+      const float f = fast_exp2(mi[j] - m);
+      l = fmaf(li[j], f, l);
+#pragma unroll
+      for (int z = 0; z < 4; ++z)
+        sum[z] = make_float4(fmaf(w[j][z].x, f, sum[z].x), fmaf(w[j][z].y, f, sum[z].y), fmaf(w[j][z].z, f, sum[z].z),
+                             fmaf(w[j][z].w, f, sum[z].w));
+    }
+  }
+  if (threadIdx.x < 32 && first + n < t.len) lse[hq * a.N + t.seq0 + first + n] = (m + __builtin_amdgcn_logf(l)) * LN2;
+  Turn<NB>::store(turn, sum, 1.f / l, out + ((t.seq0 + (int64_t)first) * a.Hq + hq) * a.D, (int64_t)a.Hq * a.D, t.len - first, a.D);
 }
 
 // stat, which this kernel makes and the dk/dv kernel reads: per (head, token) -lse * sqrt(D), where its row's score
 // products start, then -delta, delta_i = do_i . o_i, where its row's products with v start:
 // p = exp((q . k - lse sqrt(D)) / sqrt(D)).
 template <int NB>
-__global__ void __launch_bounds__(256, 2) ft_stream_dq_kernel(FtArgs a, const uint16_t* __restrict__ q,
+__global__ void __launch_bounds__(256, 2) ft_stream_dq_kernel(FtArgs a, const hpd_ft_item* __restrict__ items,
+                                                             const uint16_t* __restrict__ q,
                                                              const uint16_t* __restrict__ k, const uint16_t* __restrict__ v,
                                                              const uint16_t* __restrict__ out, const uint16_t* __restrict__ d_out,
                                                              const float* __restrict__ lse, float* __restrict__ stat,
-                                                             uint16_t* __restrict__ dq) {
+                                                             float* __restrict__ partial, uint16_t* __restrict__ dq) {
   using R = Rows<NB>;
   using Q = QueryTile<NB>;
   __shared__ __attribute__((aligned(2 * Q::STAGE))) char ring[2 * Q::STAGE];
-  const Q w(a, k, v, ring);
-  w.issue(0);
+  const Q w(a, items, k, v, ring);
+  w.issue(w.t.begin);
   bf16x8 qf[R::STEPS], of[R::STEPS];
   float nl[1], nd[1];
   {
@@ -364,7 +458,7 @@ __global__ void __launch_bounds__(256, 2) ft_stream_dq_kernel(FtArgs a, const ui
     }
     nd[0] = -(delta + __shfl_xor(delta, 32));
     nl[0] = LOG2E * minus_lse;
-    if (w.h == 0 && w.i < w.t.len) {
+    if (w.t.begin == 0 && w.h == 0 && w.i < w.t.len) {
       stat[w.hq * a.N + w.token] = minus_lse / a.scale;
       stat[(a.Hq + w.hq) * a.N + w.token] = nd[0];
     }
@@ -425,15 +519,19 @@ __global__ void __launch_bounds__(256, 2) ft_stream_dq_kernel(FtArgs a, const ui
       __builtin_amdgcn_sched_barrier(0);
     }
   };
-  for (int32_t round = 0; round < w.rounds; ++round) {
+  for (int32_t round = w.t.begin; round < w.t.end; ++round) {
     wait_vector_memory<0>();
     wait_lds_and_barrier();
-    if (round + 1 < w.rounds) w.issue(round + 1);
+    if (round + 1 < w.t.end) w.issue(round + 1);
     if (w.reaches(2 * round) || w.reaches(2 * round + 1)) step(2 * round);
     at.flip(Q::STAGE);
   }
   wait_lds_and_barrier();
   if (!w.active) return;
+  if (w.t.slot >= 0) {
+    w.put(w.partial_of(partial), acc);
+    return;
+  }
   store_rows<NB>(ring + w.wave * R::TILE, acc, a.scale, dq + (w.t.seq0 + (int64_t)w.q_first) * a.sdq + w.hq * a.D, a.sdq,
                  w.t.len - w.q_first, a.D, w.lane);
 }
@@ -633,22 +731,31 @@ __global__ void __launch_bounds__(256, 2) ft_stream_dkv_kernel(FtArgs a, const h
   store_rows<NB>(ring + wave * R::TILE, acc_k, a.scale, dk + first * a.sdk + hk * a.D, a.sdk, t.len - k_first, a.D, lane);
 }
 
-// Adds up a tile's partial sums, in the order of its items.  A workgroup has 32 keys of dk (even) or dv, a wave one block of
-// channels; the sums of four items are on their way at a time.
+// Adds up the partial sums of the tiles of keys (n_key workgroups) and of queries, in the order of their items.  A
+// workgroup has 32 rows of dk, dv or dq of one head, a wave one block of channels; the sums of four items are on their way at a
+// time.
 template <int NB>
-__global__ void __launch_bounds__(64 * NB) ft_stream_dkv_join_kernel(FtArgs a, const hpd_ft_item* __restrict__ joins,
-                                                                   const float* __restrict__ partial, uint16_t* __restrict__ dk,
-                                                                   uint16_t* __restrict__ dv) {
-  constexpr int PITCH = 64 * NB + 16;  // bytes of a row of the result
-  __shared__ __attribute__((aligned(16))) char turn[32 * PITCH];
-  const int lane = threadIdx.x & 63, n = lane & 31, h = lane >> 5, x = threadIdx.x >> 6;
-  const int32_t y = blockIdx.x & 1, rows32 = blockIdx.x >> 1 & 3, hk = (blockIdx.x >> 3) % a.Hkv;
-  const hpd_ft_item t = joins[(blockIdx.x >> 3) / a.Hkv];  // slots [slot, slot + end)
-  const int32_t k_first = t.row0 + rows32 * 32;
-  if (k_first >= t.len) return;
-  const int64_t step = (int64_t)a.Hkv * KeyTile<NB>::PARTIAL;
-  const float* p = partial + ((int64_t)t.slot * a.Hkv + hk) * KeyTile<NB>::PARTIAL + (4 * y + rows32) * KeyTile<NB>::SUMS +
-                   x * 1024 + lane * 4;
+__global__ void __launch_bounds__(64 * NB) ft_stream_join_gradients_kernel(FtArgs a, uint32_t n_key,
+                                                                         const hpd_ft_item* __restrict__ key_joins,
+                                                                         const hpd_ft_item* __restrict__ query_joins,
+                                                                         const float* __restrict__ key_partial,
+                                                                         const float* __restrict__ query_partial,
+                                                                         uint16_t* __restrict__ dq, uint16_t* __restrict__ dk,
+                                                                         uint16_t* __restrict__ dv) {
+  using K = KeyTile<NB>;
+  using Q = QueryTile<NB>;
+  __shared__ __attribute__((aligned(16))) char turn[Turn<NB>::BYTES];
+  const int lane = threadIdx.x & 63, x = threadIdx.x >> 6;
+  const bool keys = blockIdx.x < n_key;
+  const uint32_t rest = keys ? blockIdx.x >> 1 : blockIdx.x - n_key;
+  const int32_t y = blockIdx.x & 1, rows32 = rest & 3, heads = keys ? a.Hkv : a.Hq, head = (rest >> 2) % heads;  // (y: dv)
+  const hpd_ft_item t = (keys ? key_joins : query_joins)[(rest >> 2) / heads];  // slots [slot, slot + end)
+  const int32_t first = t.row0 + rows32 * 32;
+  if (first >= t.len) return;
+  const int64_t step = keys ? (int64_t)heads * K::PARTIAL : (int64_t)heads * 4 * Q::PARTIAL;
+  const float* const p = (keys ? key_partial + ((int64_t)t.slot * heads + head) * K::PARTIAL + (4 * y + rows32) * K::SUMS
+                               : query_partial + (((int64_t)t.slot * heads + head) * 4 + rows32) * Q::PARTIAL) +
+                         x * 1024 + lane * 4;
   float4 sum[4] = {};
   for (int32_t i = 0; i < t.end; i += 4) {
     float4 w[4][4];
@@ -665,26 +772,20 @@ __global__ void __launch_bounds__(64 * NB) ft_stream_dkv_join_kernel(FtArgs a, c
           sum[z].x += w[j][z].x; sum[z].y += w[j][z].y; sum[z].z += w[j][z].z; sum[z].w += w[j][z].w;
         }
   }
-  const float f = y ? 1.f : a.scale;
-#pragma unroll
-  for (int z = 0; z < 4; ++z)  // channels 32 x + 8 z + 4 h ..
-    *reinterpret_cast<uint2*>(turn + n * PITCH + x * 64 + z * 16 + h * 8) =
-        make_uint2(cvt_pk_bf16(sum[z].x * f, sum[z].y * f), cvt_pk_bf16(sum[z].z * f, sum[z].w * f));
-  __syncthreads();
-  const int64_t stride = y ? a.sdv : a.sdk;
-  uint16_t* const out = (y ? dv : dk) + (t.seq0 + (int64_t)k_first) * stride + hk * a.D;
-  for (int i = threadIdx.x; i < 32 * 4 * NB; i += 64 * NB) {
-    const int r = i / (4 * NB), c = i % (4 * NB);
-    if (k_first + r < t.len && c * 8 < a.D)
-      *reinterpret_cast<uint4*>(out + r * stride + c * 8) = *reinterpret_cast<const uint4*>(turn + r * PITCH + c * 16);
-  }
+  uint16_t* const to = keys ? (y ? dv : dk) : dq;
+  const int64_t stride = keys ? (y ? a.sdv : a.sdk) : a.sdq;
+  Turn<NB>::store(turn, sum, keys && y ? 1.f : a.scale, to + (t.seq0 + (int64_t)first) * stride + head * a.D, stride, t.len - first,
+                  a.D);
 }
 
 template <int NB>
-hipError_t forward(const hpd_finetune_layout* L, const FtArgs& a, const void* q, const void* k, const void* v, void* out,
-                   float* lse, hipStream_t s) {
-  ft_stream_forward_kernel<NB><<<dim3((unsigned)L->tiles.size() * a.Hq), 256, 0, s>>>(
-      a, (const uint16_t*)q, (const uint16_t*)k, (const uint16_t*)v, (uint16_t*)out, lse);
+hipError_t forward(const hpd_finetune_layout* L, const FtArgs& a, const uint16_t* q, const uint16_t* k, const uint16_t* v,
+                   uint16_t* out, float* lse, float* partial, hipStream_t s) {
+  ft_stream_forward_kernel<NB><<<dim3((unsigned)L->query_items.size() * a.Hq), 256, 0, s>>>(a, L->d_query_items, q, k, v, out, lse,
+                                                                                        partial);
+  if (!L->query_joins.empty())
+    ft_stream_join_kernel<NB><<<dim3((unsigned)L->query_joins.size() * a.Hq * 4), 64 * NB, 0, s>>>(a, L->d_query_joins, partial, out,
+                                                                                             lse);
   return hipGetLastError();
 }
 
@@ -692,21 +793,25 @@ template <int NB>
 hipError_t backward(const hpd_finetune_layout* L, FtArgs a, const uint16_t* q, const uint16_t* k, const uint16_t* v,
                     const uint16_t* out, const float* lse, const uint16_t* d_out, uint16_t* dq, uint16_t* dk, uint16_t* dv,
                     float* stat, hipStream_t s) {
-  ft_stream_dq_kernel<NB><<<dim3((unsigned)L->tiles.size() * a.Hq), 256, 0, s>>>(a, q, k, v, out, d_out, lse, stat, dq);
-  float* partial = stat + 2 * a.N * a.Hq + (-2 * a.N * a.Hq & 3);  // (on 16 bytes)
-  ft_stream_dkv_kernel<NB><<<dim3((unsigned)L->items.size() * a.Hkv), 256, 0, s>>>(a, L->d_items, q, k, v, d_out, stat, partial,
-                                                                               dk, dv);
-  if (!L->joins.empty())
-    ft_stream_dkv_join_kernel<NB><<<dim3((unsigned)L->joins.size() * a.Hkv * 8), 64 * NB, 0, s>>>(a, L->d_joins, partial, dk, dv);
+  float* const key_partial = stat + 2 * a.N * a.Hq + (-2 * a.N * a.Hq & 3);  // (on 16 bytes)
+  float* const query_partial = key_partial + (int64_t)L->slots * a.Hkv * KeyTile<NB>::PARTIAL;
+  ft_stream_dq_kernel<NB><<<dim3((unsigned)L->query_items.size() * a.Hq), 256, 0, s>>>(a, L->d_query_items, q, k, v, out, d_out, lse,
+                                                                                  stat, query_partial, dq);
+  ft_stream_dkv_kernel<NB><<<dim3((unsigned)L->items.size() * a.Hkv), 256, 0, s>>>(a, L->d_items, q, k, v, d_out, stat, key_partial,
+                                                                                dk, dv);
+  const uint32_t n_key = (uint32_t)L->joins.size() * a.Hkv * 8, n_query = (uint32_t)L->query_joins.size() * a.Hq * 4;
+  if (n_key + n_query)
+    ft_stream_join_gradients_kernel<NB><<<dim3(n_key + n_query), 64 * NB, 0, s>>>(a, n_key, L->d_joins, L->d_query_joins, key_partial,
+                                                                                query_partial, dq, dk, dv);
   return hipGetLastError();
 }
 
 }  // namespace
 
 hipError_t hpd_launch_ft_stream_forward(const hpd_finetune_layout* L, FtArgs a, const void* q, const void* k, const void* v,
-                                        void* out, float* lse, hipStream_t s) {
+                                        void* out, float* lse, void* workspace, hipStream_t s) {
   const auto run = a.D <= 32 ? forward<1> : a.D <= 64 ? forward<2> : a.D <= 96 ? forward<3> : forward<4>;
-  return run(L, a, q, k, v, out, lse, s);
+  return run(L, a, (const uint16_t*)q, (const uint16_t*)k, (const uint16_t*)v, (uint16_t*)out, lse, (float*)workspace, s);
 }
 
 hipError_t hpd_launch_ft_stream_backward(const hpd_finetune_layout* L, FtArgs a, const void* q, const void* k, const void* v,

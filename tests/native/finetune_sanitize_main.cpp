@@ -60,28 +60,28 @@ static void check_tiles(const hpd_finetune_layout* L, const std::vector<int32_t>
   for (const auto& x : seen) CHECK(x.second == 1);
 }
 
-// the items of a key tile are its rounds, each once; a tile of several has as many slots in a row
-static void check_items(const hpd_finetune_layout* L) {
-  const int32_t rows_of = hpd_ft_key_rows(L);
+// the items of a tile are its rounds, each once, the longest items first; a tile of several has as many slots in a row
+template <typename Rounds>
+static void check_cut(const hpd_finetune_layout* L, int32_t rows_of, const std::vector<hpd_ft_item>& items,
+                      const std::vector<hpd_ft_item>& join_list, int32_t n_slots, Rounds rounds) {
   size_t expect = 0;
   for (int32_t s = 0; s < L->n_seq; ++s) expect += (L->seq_off[s + 1] - L->seq_off[s] + rows_of - 1) / rows_of;
-  const int64_t G = L->cfg.n_q_heads / L->cfg.n_kv_heads;
   std::map<std::pair<int32_t, int32_t>, std::map<int32_t, hpd_ft_item>> tiles;
-  for (size_t i = 0; i < L->items.size(); ++i) {
-    const hpd_ft_item& x = L->items[i];
-    CHECK(x.begin < x.end && x.slot < L->slots && x.row0 < x.len && x.row0 % rows_of == 0);
-    if (i) CHECK(L->items[i - 1].end - L->items[i - 1].begin >= x.end - x.begin);
+  for (size_t i = 0; i < items.size(); ++i) {
+    const hpd_ft_item& x = items[i];
+    CHECK(x.begin < x.end && x.slot < n_slots && x.row0 < x.len && x.row0 % rows_of == 0 && x.seq0 + x.len <= L->n_tokens);
+    if (i) CHECK(items[i - 1].end - items[i - 1].begin >= x.end - x.begin);
     const bool fresh = tiles[{x.seq0, x.row0}].emplace(x.begin, x).second;
     CHECK(fresh);
   }
   CHECK(tiles.size() == expect);
   std::map<std::pair<int32_t, int32_t>, hpd_ft_item> joins;
   int32_t slots = 0;
-  for (const hpd_ft_item& x : L->joins) {
+  for (const hpd_ft_item& x : join_list) {
     CHECK(joins.emplace(std::make_pair(x.seq0, x.row0), x).second);
     slots += x.end;
   }
-  CHECK(slots == L->slots);
+  CHECK(slots == n_slots);
   for (const auto& t : tiles) {
     const hpd_ft_item& first = t.second.begin()->second;
     int64_t at = 0;
@@ -94,11 +94,27 @@ static void check_items(const hpd_finetune_layout* L) {
       CHECK(x.second.slot == (join == joins.end() ? -1 : join->second.slot + n));
       ++n;
     }
-    CHECK(at == G * ((first.len + 31) / 32 - first.row0 / 32));
+    CHECK(at == rounds(first));
     if (join != joins.end()) CHECK(join->second.end == n);
   }
-  const int64_t rows = (int64_t)L->n_tokens * L->cfg.n_q_heads;
-  CHECK(hpd_ft_backward_bytes(L) >= rows * 8 + (int64_t)L->slots * L->cfg.n_kv_heads * 2 * rows_of * hpd_ft_padded_dim(L) * 4);
+}
+static void check_items(const hpd_finetune_layout* L) {
+  const int64_t Hq = L->cfg.n_q_heads, Hkv = L->cfg.n_kv_heads, G = Hq / Hkv;
+  const int32_t rows_of = hpd_ft_key_rows(L);
+  check_cut(L, rows_of, L->items, L->joins, L->slots,
+            [&](const hpd_ft_item& x) { return G * ((x.len + 31) / 32 - x.row0 / 32); });
+  int64_t forward = 0;
+  if (L->cfg.dtype == HPD_BF16) {
+    check_cut(L, 128, L->query_items, L->query_joins, L->query_slots,
+              [](const hpd_ft_item& x) { return (int64_t)(std::min(x.row0 + 128, x.len) + 63) / 64; });
+    forward = (int64_t)L->query_slots * Hq * 128 * (hpd_ft_padded_dim(L) + 2) * 4;
+  } else {
+    CHECK(L->query_items.empty() && L->query_joins.empty() && L->query_slots == 0);
+  }
+  CHECK(hpd_ft_padded_dim(L) >= L->cfg.head_dim && hpd_ft_padded_dim(L) % 32 == 0);
+  CHECK(hpd_ft_forward_bytes(L) == forward);
+  const int64_t rows = (int64_t)L->n_tokens * Hq;
+  CHECK(hpd_ft_backward_bytes(L) >= rows * 8 + (int64_t)L->slots * Hkv * 2 * rows_of * hpd_ft_padded_dim(L) * 4 + forward);
 }
 
 int main() {

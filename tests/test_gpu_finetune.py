@@ -126,6 +126,25 @@ def test_long_values_hide_whole_tiles_of_keys(dtype):
     r.check(f"long values {dtype}")
 
 
+@pytest.mark.parametrize("dtype, d", [("f32", 64), ("f32", 96), ("f32", 112), ("bf16", 24), ("bf16", 64), ("bf16", 80), ("bf16", 128)])
+def test_tiles_cut_into_items(dtype, d):
+    """One long sequence and few heads: a tile's rounds are shared by several workgroups.  Of the values of 600 tokens, the
+    second's first ones see nothing of most of the first's, so neither do items of their tile."""
+    from paper_2604_26209_amd import binding as B
+    batch = Batch([(5, [1, 2, 1], [600, 600, 90]), (300, [1] * 4, [6, 0, 3, 7])], 600)
+    r = Run(batch, 3, 1, d, dtype, 14, wide=True)
+    counts = r.layout.counts()
+    assert (counts[B.HPD_FTC_FORWARD_BYTES] > 0) == (dtype == "bf16")
+    assert counts[B.HPD_FTC_BACKWARD_BYTES] > 8 * batch.n * 3 + 16
+    r.forward()
+    r.backward()
+    r.check(f"items {dtype} {d}")
+    first = [x.clone() for x in r.results()]
+    r.forward()
+    r.backward()
+    assert all(torch.equal(a, b) for a, b in zip(first, r.results()))
+
+
 @pytest.mark.parametrize("dtype, d", [("f32", 64), ("bf16", 64), ("bf16", 128), ("bf16", 96)])
 def test_mask_of_the_gradients_row_by_row(dtype, d):
     """With the gradient of one query row per head, dv of every token is that row's weight times the row's gradient: exactly
