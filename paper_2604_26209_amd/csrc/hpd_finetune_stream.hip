@@ -167,10 +167,37 @@ struct Turn {
 // tile's rounds; what the waves of a tile with several have goes to `partial`, register by register, and a second kernel
 // joins it.
 // ---------------------------------------------------------------------------------------
+// LDS addresses of a lane's operands in the first tile of a stage
+template <int NB>
+struct Addresses {
+  using R = Rows<NB>;
+  uint32_t row[R::STEPS], col[2 * R::BLOCKS];
+  __device__ __forceinline__ Addresses(uint32_t base, int lane) {
+#pragma unroll
+    for (int s = 0; s < R::STEPS; ++s) row[s] = base + (R::row_offset(lane & 31, lane >> 5) ^ (s << 5));
+#pragma unroll
+    for (int c = 0; c < 2 * R::BLOCKS; ++c) col[c] = base + (R::column_offset(lane) ^ (c >> 1 << 6) ^ ((c & 1) << 5));
+  }
+  // to the other stage (base is a multiple of 2 * stage)
+  __device__ __forceinline__ void flip(uint32_t stage) {
+#pragma unroll
+    for (int s = 0; s < R::STEPS; ++s) row[s] ^= stage;
+#pragma unroll
+    for (int c = 0; c < 2 * R::BLOCKS; ++c) col[c] ^= stage;
+  }
+  __device__ __forceinline__ bf16x8 rows(int s, int at) const { return lds_read(row[s] + at); }
+  __device__ __forceinline__ bf16x8 columns(int b, int k, int at) const {
+    const uint2 lo = lds_read_tr(col[2 * b] + at + 16 * k * R::RB);
+    const uint2 hi = lds_read_tr(col[2 * b + 1] + at + (16 * k + 8) * R::RB);
+    return __builtin_bit_cast(bf16x8, make_uint4(lo.x, lo.y, hi.x, hi.y));
+  }
+};
+
 template <int NB>
 struct QueryTile {
   using R = Rows<NB>;
   static constexpr int STAGE = 4 * R::TILE;  // 64 rows of k, 64 rows of v
+  static constexpr int LOADS = 128 / R::GROUP;  // load instructions of a wave for a round, and for 32 rows of its own
   static constexpr int SUMS = 32 * 32 * NB;  // fp32 sums of a wave
   static constexpr int PARTIAL = SUMS + 64;  // of a wave in `partial`: sums; forward: reference points, sums of the weights
   const FtArgs& a;
@@ -222,6 +249,27 @@ struct QueryTile {
       loader.load(src + first * loader.stride, dst + row * R::RB, t.len - 1 - first, lane);
     }
   }
+  // The wave's own rows of a tensor, through its quarter of a stage that is free: whole rows at a time (the operand's layout
+  // straight from memory: 32 lines for every 16 bytes of 32 rows, fetched again for the next ones).
+  __device__ __forceinline__ void load_own(const uint16_t* x, int64_t stride, int stage) const {
+    Loader<NB> own;
+    own.init(stride, a.D, lane);
+    const int32_t row0 = min(q_first, t.len - 1);
+    const char* const base = reinterpret_cast<const char*>(x + (t.seq0 + (int64_t)row0) * stride + hq * a.D);
+#pragma unroll
+    for (int j = 0; j < 32 / R::GROUP; ++j) {
+      const int32_t first = min(j * R::GROUP, t.len - 1 - row0);
+      own.load(base + first * own.stride, ring_lds + stage * STAGE + wave * R::TILE + j * R::GROUP * R::RB, t.len - 1 - row0 - first,
+               lane);
+    }
+  }
+  __device__ __forceinline__ void read_own(const Addresses<NB>& at, int stage, bf16x8 (&f)[R::STEPS]) const {
+#pragma unroll
+    for (int s = 0; s < R::STEPS; ++s) {
+      const bf16x8 x = at.rows(s, stage * STAGE + wave * R::TILE);
+      f[s] = (2 * s + h) * 8 < a.D ? x : bf16x8{};
+    }
+  }
   __device__ __forceinline__ float* partial_of(float* partial) const {
     return partial + (((int64_t)t.slot * a.Hq + hq) * 4 + wave) * PARTIAL;
   }
@@ -244,32 +292,6 @@ struct QueryTile {
   }
 };
 
-// LDS addresses of a lane's operands in the first tile of a stage
-template <int NB>
-struct Addresses {
-  using R = Rows<NB>;
-  uint32_t row[R::STEPS], col[2 * R::BLOCKS];
-  __device__ __forceinline__ Addresses(uint32_t base, int lane) {
-#pragma unroll
-    for (int s = 0; s < R::STEPS; ++s) row[s] = base + (R::row_offset(lane & 31, lane >> 5) ^ (s << 5));
-#pragma unroll
-    for (int c = 0; c < 2 * R::BLOCKS; ++c) col[c] = base + (R::column_offset(lane) ^ (c >> 1 << 6) ^ ((c & 1) << 5));
-  }
-  // to the other stage (base is a multiple of 2 * stage)
-  __device__ __forceinline__ void flip(uint32_t stage) {
-#pragma unroll
-    for (int s = 0; s < R::STEPS; ++s) row[s] ^= stage;
-#pragma unroll
-    for (int c = 0; c < 2 * R::BLOCKS; ++c) col[c] ^= stage;
-  }
-  __device__ __forceinline__ bf16x8 rows(int s, int at) const { return lds_read(row[s] + at); }
-  __device__ __forceinline__ bf16x8 columns(int b, int k, int at) const {
-    const uint2 lo = lds_read_tr(col[2 * b] + at + 16 * k * R::RB);
-    const uint2 hi = lds_read_tr(col[2 * b + 1] + at + (16 * k + 8) * R::RB);
-    return __builtin_bit_cast(bf16x8, make_uint4(lo.x, lo.y, hi.x, hi.y));
-  }
-};
-
 template <int NB>
 __global__ void __launch_bounds__(256, 2) ft_stream_forward_kernel(FtArgs a, const hpd_ft_item* __restrict__ items,
                                                                   const uint16_t* __restrict__ q,
@@ -280,14 +302,16 @@ __global__ void __launch_bounds__(256, 2) ft_stream_forward_kernel(FtArgs a, con
   using Q = QueryTile<NB>;
   __shared__ __attribute__((aligned(2 * Q::STAGE))) char ring[2 * Q::STAGE];
   const Q w(a, items, k, v, ring);
-  w.issue(w.t.begin);
-  bf16x8 qf[R::STEPS];
-  own_row(q + w.token * a.sq + w.hq * a.D, a.D, w.h, qf);
+  Addresses<NB> at(w.ring_lds, w.lane);
   int32_t rank_i[1] = {a.rank[w.token]};
+  bf16x8 qf[R::STEPS];
+  w.load_own(q, a.sq, 1);
+  w.issue(w.t.begin);
+  wait_vector_memory<Q::LOADS>();  // the queries
+  w.read_own(at, 1, qf);
   arrived(qf);
   arrived(rank_i);
   const float c = a.scale * LOG2E;
-  Addresses<NB> at(w.ring_lds, w.lane);
 
   floatx16 acc[R::BLOCKS];
   zero(acc, R::BLOCKS);
@@ -437,16 +461,26 @@ __global__ void __launch_bounds__(256, 2) ft_stream_dq_kernel(FtArgs a, const hp
   using Q = QueryTile<NB>;
   __shared__ __attribute__((aligned(2 * Q::STAGE))) char ring[2 * Q::STAGE];
   const Q w(a, items, k, v, ring);
-  w.issue(w.t.begin);
+  Addresses<NB> at(w.ring_lds, w.lane);
   bf16x8 qf[R::STEPS], of[R::STEPS];
   float nl[1], nd[1];
+  const float minus_lse = -lse[w.hq * a.N + w.token];
+  int32_t rank_i[1] = {a.rank[w.token]};
   {
+    const int64_t row = (int64_t)a.Hq * a.D;
     bf16x8 o[R::STEPS];
-    const int64_t row = (w.token * a.Hq + w.hq) * a.D;
-    own_row(q + w.token * a.sq + w.hq * a.D, a.D, w.h, qf);
-    own_row(d_out + row, a.D, w.h, of);
-    own_row(out + row, a.D, w.h, o);
-    const float minus_lse = -lse[w.hq * a.N + w.token];
+    w.load_own(q, a.sq, 0);
+    w.load_own(d_out, row, 1);
+    wait_vector_memory<0>();
+    w.read_own(at, 0, qf);
+    w.read_own(at, 1, of);
+    arrived(qf);
+    arrived(of);
+    wait_lds_and_barrier();  // (stage 0 is the round's from here on)
+    w.load_own(out, row, 1);
+    w.issue(w.t.begin);
+    wait_vector_memory<Q::LOADS>();
+    w.read_own(at, 1, o);
     float delta = 0.f;
 #pragma unroll
     for (int s = 0; s < R::STEPS; ++s) {
@@ -463,14 +497,10 @@ __global__ void __launch_bounds__(256, 2) ft_stream_dq_kernel(FtArgs a, const hp
       stat[(a.Hq + w.hq) * a.N + w.token] = nd[0];
     }
   }
-  int32_t rank_i[1] = {a.rank[w.token]};
-  arrived(qf);
-  arrived(of);
   arrived(nl);
   arrived(nd);
   arrived(rank_i);
   const float c = a.scale * LOG2E;
-  Addresses<NB> at(w.ring_lds, w.lane);
   floatx16 acc[R::BLOCKS];
   zero(acc, R::BLOCKS);
   // One round, two blocks of 32 keys.  The first block's weights and gradients are made while the second block's
