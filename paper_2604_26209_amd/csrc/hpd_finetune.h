@@ -34,6 +34,10 @@ struct hpd_finetune_layout {
   int32_t n_seq = 0, n_tokens = 0, max_len = 0, max_pos = -1;
   std::vector<int32_t> seq_off, pos, rank;
   std::vector<int32_t> blk_rank;        // [blocks][2]: lowest and highest rank of 32 tokens of a sequence
+  // bf16: which tokens of a block have ranks up to r, for r from one below its lowest (none) to its highest rank (all); seen_off
+  // [block] + r: the index of the word.  A block where a value of L tokens ends has L and two words, others 33 at most.
+  std::vector<uint32_t> seen;
+  std::vector<int32_t> seen_off;
   std::vector<hpd_ft_tile> tiles;       // query tiles, those with most keys first
   // the tiles of keys and (bf16) of queries as items, longest first, and for those of several items the first slot and (as
   // `end`) their number
@@ -44,6 +48,8 @@ struct hpd_finetune_layout {
   void* d_mem = nullptr;
   const int32_t *d_pos = nullptr, *d_rank = nullptr;
   const int2* d_blk_rank = nullptr;
+  const int32_t* d_seen_off = nullptr;
+  const uint32_t* d_seen = nullptr;
   const hpd_ft_tile* d_tiles = nullptr;
   const hpd_ft_item *d_items = nullptr, *d_joins = nullptr, *d_query_items = nullptr, *d_query_joins = nullptr;
   // (cos, sin) rows of D/2: one per position ID, or one per token where that is fewer

@@ -88,6 +88,8 @@ FtArgs make_args(const hpd_finetune_layout* L, const hpd_finetune_strides& st) {
   a.tiles = L->d_tiles;
   a.rank = L->d_rank;
   a.blk_rank = L->d_blk_rank;
+  a.seen_off = L->d_seen_off;
+  a.seen = L->d_seen;
   a.N = L->n_tokens;
   a.sq = st.q; a.sk = st.k; a.sv = st.v;
   a.sdq = st.q_out; a.sdk = st.k_out; a.sdv = st.v_out;

@@ -9,6 +9,8 @@ struct FtArgs {
   const hpd_ft_tile* tiles;
   const int32_t* rank;
   const int2* blk_rank;
+  const int32_t* seen_off;
+  const uint32_t* seen;
   int64_t N, sq, sk, sv, sdq, sdk, sdv;
   int32_t Hq, Hkv, D;
   float scale;  // 1 / sqrt(D)

@@ -116,6 +116,13 @@ int build_tables(hpd_finetune_layout* L, const int32_t* prompt_len, const int32_
       const auto mm = std::minmax_element(L->rank.begin() + seq0 + b, L->rank.begin() + seq0 + std::min(b + HPD_FT_BLOCK, len));
       L->blk_rank.push_back(*mm.first);
       L->blk_rank.push_back(*mm.second);
+      if (L->cfg.dtype != HPD_BF16) continue;
+      const size_t at = L->seen.size();
+      L->seen_off.push_back((int32_t)at - (*mm.first - 1));
+      L->seen.resize(at + (size_t)(*mm.second - *mm.first + 2), 0);
+      for (int32_t i = b; i < std::min(b + HPD_FT_BLOCK, len); ++i)
+        L->seen[at + (size_t)(L->rank[seq0 + i] - *mm.first + 1)] |= 1u << (i - b);
+      for (size_t r = at + 1; r < L->seen.size(); ++r) L->seen[r] |= L->seen[r - 1];
     }
     for (int32_t r = 0; r < len; r += HPD_FT_ROWS) L->tiles.push_back({seq0, len, r, blk0});
   }
@@ -135,7 +142,8 @@ int upload(hpd_finetune_layout* L, hipStream_t s) {
   auto pad = [](size_t words) { return (words + 3) / 4 * 4; };
   // (the kernels read the ranks of two whole blocks at a time: up to 63 more behind the last token)
   const size_t n = (size_t)L->n_tokens, nt = L->tiles.size() * 4;
-  const size_t o_rank = pad(n), o_blk = o_rank + pad(n + 2 * HPD_FT_BLOCK), o_tiles = o_blk + pad(L->blk_rank.size()),
+  const size_t o_rank = pad(n), o_blk = o_rank + pad(n + 2 * HPD_FT_BLOCK), o_seen_off = o_blk + pad(L->blk_rank.size()),
+               o_seen = o_seen_off + pad(L->seen_off.size()), o_tiles = o_seen + pad(L->seen.size()),
                o_items = o_tiles + nt;
   const std::vector<hpd_ft_item>* const lists[] = {&L->items, &L->joins, &L->query_items, &L->query_joins};
   size_t words = o_items;
@@ -144,6 +152,8 @@ int upload(hpd_finetune_layout* L, hipStream_t s) {
   std::copy(L->pos.begin(), L->pos.end(), host.begin());
   std::copy(L->rank.begin(), L->rank.end(), host.begin() + o_rank);
   std::copy(L->blk_rank.begin(), L->blk_rank.end(), host.begin() + o_blk);
+  std::copy(L->seen_off.begin(), L->seen_off.end(), host.begin() + o_seen_off);
+  std::copy(L->seen.begin(), L->seen.end(), host.begin() + o_seen);
   std::memcpy(host.data() + o_tiles, L->tiles.data(), nt * 4);
   size_t at = o_items;
   for (const auto* l : lists) {
@@ -156,6 +166,8 @@ int upload(hpd_finetune_layout* L, hipStream_t s) {
   L->d_pos = base;
   L->d_rank = base + o_rank;
   L->d_blk_rank = (const int2*)(base + o_blk);
+  L->d_seen_off = base + o_seen_off;
+  L->d_seen = (const uint32_t*)(base + o_seen);
   L->d_tiles = (const hpd_ft_tile*)(base + o_tiles);
   L->d_items = (const hpd_ft_item*)(base + o_items);
   L->d_joins = L->d_items + L->items.size();

@@ -142,6 +142,29 @@ __device__ __forceinline__ void own_row(const uint16_t* row, int32_t D, int h, b
   }
 }
 
+// The mask of a block of 32 tokens whose ranks differ (fine-tuning layout): a word per rank, bit i: token i's rank is no
+// higher.  A lane fetches its word a round ahead; of a score it costs two instructions then.
+struct Seen {
+  const const_i32* off;     // of the sequence's blocks
+  const const_i32* ranks;   // lowest and highest of them
+  const uint32_t* words;
+  __device__ __forceinline__ Seen(const FtArgs& a, int32_t blk0)
+      : off((const const_i32*)(uintptr_t)(a.seen_off + blk0)), ranks((const const_i32*)(uintptr_t)(a.blk_rank + blk0)), words(a.seen) {}
+  // tokens of block b with ranks up to this one
+  __device__ __forceinline__ uint32_t word(int32_t b, int32_t rank) const {
+    return words[(uint32_t)(off[b] + min(max(rank, ranks[2 * b] - 1), ranks[2 * b + 1]))];
+  }
+};
+// -infinity where a bit is 0; bits: of the lane's column, by rows of the tile
+__device__ __forceinline__ void hide(floatx16& s, uint32_t bits, int h) {
+  bits >>= 4 * h;
+#pragma unroll
+  for (int r = 0; r < 16; ++r) {
+    const uint32_t seen = (uint32_t)__builtin_amdgcn_sbfe((int32_t)bits, tile_row(r, 0), 1);
+    s[r] = __uint_as_float((__float_as_uint(s[r]) & seen) | (0xff800000u & ~seen));
+  }
+}
+
 // The end of the kernels that join items: a workgroup of NB waves has 32 rows, wave x channels 32 x + 8 z + 4 h .. of row n
 template <int NB>
 struct Turn {
@@ -207,7 +230,6 @@ struct QueryTile {
   int64_t token;
   bool active;
   int32_t q_min, q_max;  // ranks of the wave's queries
-  const int32_t* ranks;
   const const_i32* blk_rank;
   Loader<NB> loader;
   const char* src;
@@ -234,7 +256,6 @@ struct QueryTile {
     loader.init(wave < 2 ? a.sk : a.sv, a.D, lane);
     src = reinterpret_cast<const char*>(wave < 2 ? k + t.seq0 * a.sk : v + t.seq0 * a.sv) + (int64_t)hk * a.D * 2;
     ring_lds = lds_address(ring);
-    ranks = a.rank + t.seq0;
     blk_rank = (const const_i32*)(uintptr_t)(a.blk_rank + t.blk0);
     const int32_t own = min(q_first, t.len - 1) / 32;
     q_min = blk_rank[2 * own];
@@ -284,11 +305,17 @@ struct QueryTile {
   // block b of 32 keys has a key that a query of the wave sees / one that a query does not see
   __device__ __forceinline__ bool reaches(int32_t b) const { return active && b * 32 <= q_first && blk_rank[2 * b] <= q_max; }
   __device__ __forceinline__ bool masked(int32_t b) const { return b * 32 >= q_first || blk_rank[2 * b + 1] > q_min; }
-  __device__ __forceinline__ void mask(floatx16& s, int32_t b, int32_t rank_i) const {
-    BlockRanks rk;
-    rk.load(ranks + b * 32);
+  // words of the blocks of a round, for the lane's query
+  __device__ __forceinline__ void fetch(const Seen& seen, int32_t round, int32_t rank, uint32_t (&bits)[2]) const {
 #pragma unroll
-    for (int r = 0; r < 16; ++r) s[r] = b * 32 + tile_row(r, h) <= ic && rk.of(r, h) <= rank_i ? s[r] : -INFINITY;
+    for (int j = 0; j < 2; ++j) {
+      const int32_t b = 2 * round + j;
+      bits[j] = 0;
+      if (active && b * 32 <= q_first) bits[j] = masked(b) ? seen.word(b, rank) : ~0u;
+    }
+  }
+  __device__ __forceinline__ void mask(floatx16& s, int32_t b, uint32_t bits) const {
+    hide(s, b * 32 == q_first ? bits & ~0u >> (31 - n) : bits, h);
   }
 };
 
@@ -311,6 +338,9 @@ __global__ void __launch_bounds__(256, 2) ft_stream_forward_kernel(FtArgs a, con
   w.read_own(at, 1, qf);
   arrived(qf);
   arrived(rank_i);
+  const Seen seen(a, w.t.blk0);
+  uint32_t bits[2], next[2];
+  w.fetch(seen, w.t.begin, rank_i[0], next);
   const float c = a.scale * LOG2E;
 
   floatx16 acc[R::BLOCKS];
@@ -327,7 +357,7 @@ __global__ void __launch_bounds__(256, 2) ft_stream_forward_kernel(FtArgs a, con
       for (int x = 0; x < R::STEPS; ++x) s[j] = mfma(at.rows(x, j * R::TILE), qf[x], s[j]);
 #pragma unroll
     for (int j = 0; j < 2; ++j)
-      if (w.masked(b + j)) w.mask(s[j], b + j, rank_i[0]);
+      if (w.masked(b + j)) w.mask(s[j], b + j, bits[j]);
     float top = s[0][0];
 #pragma unroll
     for (int j = 0; j < 2; ++j)
@@ -378,8 +408,14 @@ __global__ void __launch_bounds__(256, 2) ft_stream_forward_kernel(FtArgs a, con
   };
   for (int32_t round = w.t.begin; round < w.t.end; ++round) {
     wait_vector_memory<0>();
+    arrived(next);
+    bits[0] = next[0];
+    bits[1] = next[1];
     wait_lds_and_barrier();  // the round is in LDS, the other half of the ring is free
-    if (round + 1 < w.t.end) w.issue(round + 1);
+    if (round + 1 < w.t.end) {
+      w.issue(round + 1);
+      w.fetch(seen, round + 1, rank_i[0], next);
+    }
     if (w.reaches(2 * round) || w.reaches(2 * round + 1)) step(2 * round);
     at.flip(Q::STAGE);
   }
@@ -500,6 +536,9 @@ __global__ void __launch_bounds__(256, 2) ft_stream_dq_kernel(FtArgs a, const hp
   arrived(nl);
   arrived(nd);
   arrived(rank_i);
+  const Seen seen(a, w.t.blk0);
+  uint32_t bits[2], next[2];
+  w.fetch(seen, w.t.begin, rank_i[0], next);
   const float c = a.scale * LOG2E;
   floatx16 acc[R::BLOCKS];
   zero(acc, R::BLOCKS);
@@ -528,7 +567,7 @@ __global__ void __launch_bounds__(256, 2) ft_stream_dq_kernel(FtArgs a, const hp
       const int j = i / (2 * S), x = i % S;
       if (i / S % 2 == 0) s[j] = mfma(f[i % 3], qf[x], s[j]);
       else dp[j] = mfma(f[i % 3], of[x], dp[j]);
-      if (i == 2 * S - 1 && w.masked(b)) w.mask(s[0], b, rank_i[0]);
+      if (i == 2 * S - 1 && w.masked(b)) w.mask(s[0], b, bits[0]);
       if (i >= 2 * S) {  // (a step behind: the last product is on its way)
         const int y = i - 2 * S;
         gradient(0, 16 * (y > 0 ? y - 1 : 0) / (2 * S - 1), 16 * y / (2 * S - 1));
@@ -537,7 +576,7 @@ __global__ void __launch_bounds__(256, 2) ft_stream_dq_kernel(FtArgs a, const hp
       }
       __builtin_amdgcn_sched_barrier(0);
     }
-    if (w.masked(b + 1)) w.mask(s[1], b + 1, rank_i[0]);
+    if (w.masked(b + 1)) w.mask(s[1], b + 1, bits[1]);
 #pragma unroll
     for (int i = 0; i < 2 * C; ++i) {
       const int at_ = 4 * S + i;
@@ -551,8 +590,14 @@ __global__ void __launch_bounds__(256, 2) ft_stream_dq_kernel(FtArgs a, const hp
   };
   for (int32_t round = w.t.begin; round < w.t.end; ++round) {
     wait_vector_memory<0>();
+    arrived(next);
+    bits[0] = next[0];
+    bits[1] = next[1];
     wait_lds_and_barrier();
-    if (round + 1 < w.t.end) w.issue(round + 1);
+    if (round + 1 < w.t.end) {
+      w.issue(round + 1);
+      w.fetch(seen, round + 1, rank_i[0], next);
+    }
     if (w.reaches(2 * round) || w.reaches(2 * round + 1)) step(2 * round);
     at.flip(Q::STAGE);
   }
@@ -644,7 +689,8 @@ __global__ void __launch_bounds__(256, 2) ft_stream_dkv_kernel(FtArgs a, const h
   int32_t rank_j[1] = {a.rank[token]};
   arrived(kf);
   arrived(rank_j);
-  const int32_t* const ranks = a.rank + t.seq0;
+  const Seen seen(a, t.blk0);
+  uint32_t next[1], bits;  // of a round's queries: ranks below the lane's key's
   const const_i32* const blk_rank = (const const_i32*)(uintptr_t)(a.blk_rank + t.blk0);
   const int32_t k_min = blk_rank[2 * (own / 32)], k_max = blk_rank[2 * (own / 32) + 1];
   const float c = a.scale * LOG2E;
@@ -687,13 +733,10 @@ __global__ void __launch_bounds__(256, 2) ft_stream_dkv_kernel(FtArgs a, const h
       __builtin_amdgcn_sched_barrier(0);
     }
     if (masked) {
-      BlockRanks rk;
-      rk.load(ranks + b * 32);
-#pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        const int32_t i = b * 32 + tile_row(r, h);
-        s[r] = i < t.len && i >= j && rank_j[0] <= rk.of(r, h) ? s[r] : -INFINITY;
-      }
+      uint32_t x = ~bits;
+      if (b * 32 == k_first) x &= ~0u << n;
+      if ((b + 1) * 32 > t.len) x &= ~(~0u << (t.len - b * 32));
+      hide(s, x, h);
     }
     dp = start(32);
     g[0] = lds_read(row + to_values);
@@ -728,13 +771,24 @@ __global__ void __launch_bounds__(256, 2) ft_stream_dkv_kernel(FtArgs a, const h
       __builtin_amdgcn_sched_barrier(0);
     }
   };
+  auto masked = [&](int32_t x) { return x * 32 < k_first + 31 || k_max > blk_rank[2 * x] || (x + 1) * 32 > t.len; };
+  auto fetch = [&](int32_t x) {
+    next[0] = 0;
+    if (masked(x)) next[0] = seen.word(x, rank_j[0] - 1);
+  };
+  fetch(b);
   auto turn = [&](int32_t round, int slot) __attribute__((always_inline)) {
     wait_vector_memory<0>();
+    arrived(next);
+    bits = next[0];
     wait_lds_and_barrier();
-    if (round + 1 < t.end) issue(slot ^ 1);
-    const int32_t q_min = blk_rank[2 * b], q_max = blk_rank[2 * b + 1];
-    if (active && b * 32 + 31 >= k_first && k_min <= q_max) step(slot, b * 32 < k_first + 31 || k_max > q_min || (b + 1) * 32 > t.len);
-    if (++b == b_first + per_head) b = b_first;
+    const int32_t after = b + 1 == b_first + per_head ? b_first : b + 1;
+    if (round + 1 < t.end) {
+      issue(slot ^ 1);
+      fetch(after);
+    }
+    if (active && b * 32 + 31 >= k_first && k_min <= blk_rank[2 * b + 1]) step(slot, masked(b));
+    b = after;
   };
   for (int32_t round = t.begin; round < t.end; round += 2) {
     turn(round, 0);

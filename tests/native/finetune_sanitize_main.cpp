@@ -60,6 +60,26 @@ static void check_tiles(const hpd_finetune_layout* L, const std::vector<int32_t>
   for (const auto& x : seen) CHECK(x.second == 1);
 }
 
+// every word of a block's mask: bit i iff token i's rank is no higher
+static void check_seen(const hpd_finetune_layout* L) {
+  if (L->cfg.dtype != HPD_BF16) {
+    CHECK(L->seen.empty() && L->seen_off.empty());
+    return;
+  }
+  size_t words = 0, block = 0;
+  for (int32_t s = 0; s < L->n_seq; ++s)
+    for (int32_t b = L->seq_off[s]; b < L->seq_off[s + 1]; b += 32, ++block) {
+      const int32_t lo = L->blk_rank[2 * block], hi = L->blk_rank[2 * block + 1];
+      for (int32_t r = lo - 1; r <= hi; ++r, ++words) {
+        uint32_t want = 0;
+        for (int32_t i = b; i < std::min(b + 32, L->seq_off[s + 1]); ++i)
+          if (L->rank[i] <= r) want |= 1u << (i - b);
+        CHECK((size_t)(L->seen_off[block] + r) == words && L->seen[words] == want);
+      }
+    }
+  CHECK(words == L->seen.size() && block == L->seen_off.size());
+}
+
 // the items of a tile are its rounds, each once, the longest items first; a tile of several has as many slots in a row
 template <typename Rounds>
 static void check_cut(const hpd_finetune_layout* L, int32_t rows_of, const std::vector<hpd_ft_item>& items,
@@ -155,6 +175,7 @@ int main() {
     for (int32_t r : rank) CHECK(r >= 0 && r <= cfg.k_max);
     CHECK(L->rope_rows <= L->n_tokens && (L->rope_by_token ? L->rope_rows == L->n_tokens : L->rope_rows == c[HPD_FTC_MAX_POS] + 1));
     check_tiles(L, off);
+    check_seen(L);
     check_items(L);
     cut = cut || !L->joins.empty();
     whole = whole || (L->joins.empty() && !L->items.empty());
