@@ -26,7 +26,7 @@ struct hpd_ft_item {
   int32_t seq0, len, row0, blk0;  // of the tile
   int32_t begin, end;             // rounds
   int32_t slot;                   // partial sums, or -1: the item is the whole tile
-  int32_t pad;
+  int32_t plain;                  // leading blocks of the sequence with nothing but rank 0
 };
 
 struct hpd_finetune_layout {

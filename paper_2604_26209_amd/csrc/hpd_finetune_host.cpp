@@ -36,14 +36,14 @@ int validate(const hpd_finetune_config* c) {
 
 // Cuts tiles into items of about `most` rounds, longest first.
 template <typename Rounds>
-void cut(const std::vector<hpd_ft_tile>& tiles, int64_t most, Rounds rounds, std::vector<hpd_ft_item>& items,
-         std::vector<hpd_ft_item>& joins, int32_t& slots) {
+void cut(const std::vector<hpd_ft_tile>& tiles, const std::vector<int32_t>& plain, int64_t most, Rounds rounds,
+         std::vector<hpd_ft_item>& items, std::vector<hpd_ft_item>& joins, int32_t& slots) {
   for (const hpd_ft_tile& t : tiles) {
     const int64_t r = rounds(t), parts = r * 2 > most * 3 ? (r + most - 1) / most : 1;
     if (parts > 1) joins.push_back({t.seq0, t.len, t.row0, t.blk0, 0, (int32_t)parts, slots, 0});
     for (int64_t p = 0; p < parts; ++p)
       items.push_back({t.seq0, t.len, t.row0, t.blk0, (int32_t)(r * p / parts), (int32_t)(r * (p + 1) / parts),
-                       parts > 1 ? slots++ : -1, 0});
+                       parts > 1 ? slots++ : -1, plain[(size_t)t.blk0]});
   }
   std::stable_sort(items.begin(), items.end(),
                    [](const hpd_ft_item& a, const hpd_ft_item& b) { return a.end - a.begin > b.end - b.begin; });
@@ -58,7 +58,7 @@ void cut(const std::vector<hpd_ft_tile>& tiles, int64_t most, Rounds rounds, std
 // 0.91.  The queries, over whole tiles (of 50 random batches ten are cut): 0.98, up to 0.71 for a single sequence; with six or ten
 // 0.985 and 0.99.  In fp32 the waves of a workgroup share the rounds: 16 at least (8 and 32: 1 % faster, 2 % slower over 24 batches;
 // not cut: 473 -> 89 us for a sequence of 774 tokens, 12/2 heads of 96).
-void plan_items(hpd_finetune_layout* L, int32_t n_cus) {
+void plan_items(hpd_finetune_layout* L, const std::vector<int32_t>& plain, int32_t n_cus) {
   const int64_t Hq = L->cfg.n_q_heads, Hkv = L->cfg.n_kv_heads, G = Hq / Hkv;
   const int32_t rows = hpd_ft_key_rows(L);
   const bool bf16 = L->cfg.dtype == HPD_BF16;
@@ -71,11 +71,11 @@ void plan_items(hpd_finetune_layout* L, int32_t n_cus) {
   auto query_rounds = [&](const hpd_ft_tile& t) { return (int64_t)(std::min(t.row0 + HPD_FT_ROWS, t.len) + 63) / 64; };
   int64_t total = 0;
   for (const hpd_ft_tile& t : tiles) total += key_rounds(t) * Hkv;
-  cut(tiles, bf16 ? most(total) : std::max<int64_t>(16, total / places / 3), key_rounds, L->items, L->joins, L->slots);
+  cut(tiles, plain, bf16 ? most(total) : std::max<int64_t>(16, total / places / 3), key_rounds, L->items, L->joins, L->slots);
   if (!bf16) return;
   total = 0;
   for (const hpd_ft_tile& t : L->tiles) total += query_rounds(t) * Hq;
-  cut(L->tiles, most(total), query_rounds, L->query_items, L->query_joins, L->query_slots);
+  cut(L->tiles, plain, most(total), query_rounds, L->query_items, L->query_joins, L->query_slots);
 }
 
 // Positions (Algorithm 2, values at pos_id[end(a_n)] + k), ranks, rank ranges of blocks, work tiles.
@@ -96,6 +96,7 @@ int build_tables(hpd_finetune_layout* L, const int32_t* prompt_len, const int32_
   L->rank.assign((size_t)total, 0);
   L->seq_off.push_back(0);
   int32_t at = 0;
+  std::vector<int32_t> plain;  // at a sequence's first block: how many from there on have nothing but rank 0
   for (int32_t s = 0; s < L->n_seq; ++s) {
     const int32_t seq0 = at;
     for (int32_t i = 0; i < prompt_len[s]; ++i) L->pos[at++] = i;
@@ -116,6 +117,8 @@ int build_tables(hpd_finetune_layout* L, const int32_t* prompt_len, const int32_
       const auto mm = std::minmax_element(L->rank.begin() + seq0 + b, L->rank.begin() + seq0 + std::min(b + HPD_FT_BLOCK, len));
       L->blk_rank.push_back(*mm.first);
       L->blk_rank.push_back(*mm.second);
+      plain.push_back(0);
+      if (*mm.second == 0 && plain[(size_t)blk0] * HPD_FT_BLOCK == b) ++plain[(size_t)blk0];
       if (L->cfg.dtype != HPD_BF16) continue;
       const size_t at = L->seen.size();
       L->seen_off.push_back((int32_t)at - (*mm.first - 1));
@@ -131,7 +134,7 @@ int build_tables(hpd_finetune_layout* L, const int32_t* prompt_len, const int32_
   std::stable_sort(L->tiles.begin(), L->tiles.end(), [](const hpd_ft_tile& a, const hpd_ft_tile& b) {
     return std::min(a.row0 + HPD_FT_ROWS, a.len) > std::min(b.row0 + HPD_FT_ROWS, b.len);
   });
-  plan_items(L, n_cus);
+  plan_items(L, plain, n_cus);
   L->rope_by_token = L->max_pos >= L->n_tokens;
   L->rope_rows = L->rope_by_token ? L->n_tokens : L->max_pos + 1;
   return HPD_OK;

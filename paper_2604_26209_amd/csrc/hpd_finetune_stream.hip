@@ -302,9 +302,14 @@ struct QueryTile {
         *reinterpret_cast<float4*>(p + (x * 4 + z) * 256 + lane * 4) =
             make_float4(acc[x][4 * z], acc[x][4 * z + 1], acc[x][4 * z + 2], acc[x][4 * z + 3]);
   }
-  // block b of 32 keys has a key that a query of the wave sees / one that a query does not see
-  __device__ __forceinline__ bool reaches(int32_t b) const { return active && b * 32 <= q_first && blk_rank[2 * b] <= q_max; }
-  __device__ __forceinline__ bool masked(int32_t b) const { return b * 32 >= q_first || blk_rank[2 * b + 1] > q_min; }
+  // block b of 32 keys has a key that a query of the wave sees / one that a query does not see (the first blocks of a
+  // sequence, its prompt, without a look at their ranks: it takes as long as the rest of a round's scalar work)
+  __device__ __forceinline__ bool reaches(int32_t b) const {
+    return active && b * 32 <= q_first && (b < t.plain || blk_rank[2 * b] <= q_max);
+  }
+  __device__ __forceinline__ bool masked(int32_t b) const {
+    return b * 32 >= q_first || (b >= t.plain && blk_rank[2 * b + 1] > q_min);
+  }
   // words of the blocks of a round, for the lane's query
   __device__ __forceinline__ void fetch(const Seen& seen, int32_t round, int32_t rank, uint32_t (&bits)[2]) const {
 #pragma unroll
@@ -771,7 +776,9 @@ __global__ void __launch_bounds__(256, 2) ft_stream_dkv_kernel(FtArgs a, const h
       __builtin_amdgcn_sched_barrier(0);
     }
   };
-  auto masked = [&](int32_t x) { return x * 32 < k_first + 31 || k_max > blk_rank[2 * x] || (x + 1) * 32 > t.len; };
+  auto masked = [&](int32_t x) {
+    return x * 32 < k_first + 31 || (x + 1) * 32 > t.len || (k_max > 0 && k_max > blk_rank[2 * x]);
+  };
   auto fetch = [&](int32_t x) {
     next[0] = 0;
     if (masked(x)) next[0] = seen.word(x, rank_j[0] - 1);
@@ -787,7 +794,7 @@ __global__ void __launch_bounds__(256, 2) ft_stream_dkv_kernel(FtArgs a, const h
       issue(slot ^ 1);
       fetch(after);
     }
-    if (active && b * 32 + 31 >= k_first && k_min <= blk_rank[2 * b + 1]) step(slot, masked(b));
+    if (active && b * 32 + 31 >= k_first && (k_min == 0 || k_min <= blk_rank[2 * b + 1])) step(slot, masked(b));
     b = after;
   };
   for (int32_t round = t.begin; round < t.end; round += 2) {

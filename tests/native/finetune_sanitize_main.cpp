@@ -91,6 +91,9 @@ static void check_cut(const hpd_finetune_layout* L, int32_t rows_of, const std::
     const hpd_ft_item& x = items[i];
     CHECK(x.begin < x.end && x.slot < n_slots && x.row0 < x.len && x.row0 % rows_of == 0 && x.seq0 + x.len <= L->n_tokens);
     if (i) CHECK(items[i - 1].end - items[i - 1].begin >= x.end - x.begin);
+    int32_t plain = 0;
+    while (plain < (x.len + 31) / 32 && L->blk_rank[2 * (x.blk0 + plain) + 1] == 0) ++plain;
+    CHECK(x.plain == plain);
     const bool fresh = tiles[{x.seq0, x.row0}].emplace(x.begin, x).second;
     CHECK(fresh);
   }
