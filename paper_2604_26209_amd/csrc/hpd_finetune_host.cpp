@@ -56,8 +56,9 @@ void cut(const std::vector<hpd_ft_tile>& tiles, const std::vector<int32_t>& plai
 // it has no fewer than four and those of a place, up to 64.  bf16 gradients of 50 random batches, geometric means over 24 rounds
 // at least (64 where there are more tiles than places): 0.89; with three 0.89, six 0.91, with 0.6 or 1.5 times those of a place 0.90 and
 // 0.91.  The queries, over whole tiles (of 50 random batches ten are cut): 0.98, up to 0.71 for a single sequence; with six or ten
-// 0.985 and 0.99.  In fp32 the waves of a workgroup share the rounds: 16 at least (8 and 32: 1 % faster, 2 % slower over 24 batches;
-// not cut: 473 -> 89 us for a sequence of 774 tokens, 12/2 heads of 96).
+// 0.985 and 0.99.  In fp32 the waves of a workgroup share the rounds, and a start is two of
+// them: from two, up to 32 (30 random batches, over 16 at least: 0.946; from 4 or 8 on 0.966 and 0.99; not cut at all: 473 -> 89 us
+// for a sequence of 774 tokens, 12/2 heads of 96).
 void plan_items(hpd_finetune_layout* L, const std::vector<int32_t>& plain, int32_t n_cus) {
   const int64_t Hq = L->cfg.n_q_heads, Hkv = L->cfg.n_kv_heads, G = Hq / Hkv;
   const int32_t rows = hpd_ft_key_rows(L);
@@ -66,16 +67,16 @@ void plan_items(hpd_finetune_layout* L, const std::vector<int32_t>& plain, int32
   for (const hpd_ft_tile& t : L->tiles)
     for (int32_t r = t.row0; r < std::min(t.row0 + HPD_FT_ROWS, t.len); r += rows) tiles.push_back({t.seq0, t.len, r, t.blk0});
   const int64_t places = (bf16 || L->cfg.head_dim <= 64 ? 2 : 1) * n_cus;
-  auto most = [&](int64_t total) { return std::max(std::min<int64_t>(64, 4 + total / places), total / places / 3); };
+  auto most = [&](int64_t total, int64_t start, int64_t cap) { return std::max(std::min(cap, start + total / places), total / places / 3); };
   auto key_rounds = [&](const hpd_ft_tile& t) { return G * ((t.len + 31) / 32 - t.row0 / 32); };
   auto query_rounds = [&](const hpd_ft_tile& t) { return (int64_t)(std::min(t.row0 + HPD_FT_ROWS, t.len) + 63) / 64; };
   int64_t total = 0;
   for (const hpd_ft_tile& t : tiles) total += key_rounds(t) * Hkv;
-  cut(tiles, plain, bf16 ? most(total) : std::max<int64_t>(16, total / places / 3), key_rounds, L->items, L->joins, L->slots);
+  cut(tiles, plain, bf16 ? most(total, 4, 64) : most(total, 2, 32), key_rounds, L->items, L->joins, L->slots);
   if (!bf16) return;
   total = 0;
   for (const hpd_ft_tile& t : L->tiles) total += query_rounds(t) * Hq;
-  cut(L->tiles, plain, most(total), query_rounds, L->query_items, L->query_joins, L->query_slots);
+  cut(L->tiles, plain, most(total, 4, 64), query_rounds, L->query_items, L->query_joins, L->query_slots);
 }
 
 // Positions (Algorithm 2, values at pos_id[end(a_n)] + k), ranks, rank ranges of blocks, work tiles.
