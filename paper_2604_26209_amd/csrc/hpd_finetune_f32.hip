@@ -122,17 +122,17 @@ struct Block {
   }
 };
 
-// Two tiles of every wave; at the end its sums, row by row
-template <int DP>
+// One or two tiles of every wave; at the end its sums, row by row
+template <int DP, int TILES>
 union Shared {
   struct {
     float sums[4][32][DP + 4];
     float m[4][32], l[4][32];
   } end;
-  char tiles[4][2 * Tile<DP>::BYTES];
+  char tiles[4][TILES * Tile<DP>::BYTES];
 };
-template <int DP>
-__device__ __forceinline__ void put(Shared<DP>& sh, const Block& w, const floatx16* acc, float f) {
+template <int DP, int TILES>
+__device__ __forceinline__ void put(Shared<DP, TILES>& sh, const Block& w, const floatx16* acc, float f) {
 #pragma unroll
   for (int b = 0; b < DP / 32; ++b)
 #pragma unroll
@@ -141,8 +141,8 @@ __device__ __forceinline__ void put(Shared<DP>& sh, const Block& w, const floatx
           make_float4(acc[b][4 * a] * f, acc[b][4 * a + 1] * f, acc[b][4 * a + 2] * f, acc[b][4 * a + 3] * f);
 }
 // the sum of the waves' rows r to out + r * stride
-template <int DP>
-__device__ __forceinline__ void join(const Shared<DP>& sh, const Block& w, float* out, int64_t stride, int32_t D) {
+template <int DP, int TILES>
+__device__ __forceinline__ void join(const Shared<DP, TILES>& sh, const Block& w, float* out, int64_t stride, int32_t D) {
   for (int x = threadIdx.x; x < 32 * DP / 4; x += 256) {
     const int r = x / (DP / 4), c = x % (DP / 4) * 4;
     if (w.first + r >= w.t.len || c >= D) continue;
@@ -157,7 +157,7 @@ __device__ __forceinline__ void join(const Shared<DP>& sh, const Block& w, float
 }
 
 // What the forward and the dq kernel share: 32 queries of a head and the blocks of keys that they see
-template <int DP>
+template <int DP, int TILES>
 struct Queries : Block {
   using TL = Tile<DP>;
   const FtArgs& a;
@@ -165,7 +165,7 @@ struct Queries : Block {
   const int32_t* ranks;
   const const_i32* blk_rank;
   const float *keys, *values;
-  uint32_t key_tile, value_tile;
+  uint32_t key_tile, value_tile;  // (one tile: keys and values by turns)
   int64_t token;
   __device__ __forceinline__ Queries(const FtArgs& args, const float* k, const float* v, const char* tiles)
       : Block(args.tiles[blockIdx.x / args.Hq / 4], blockIdx.x / args.Hq % 4), a(args) {
@@ -180,8 +180,8 @@ struct Queries : Block {
     own = min(first, t.len - 1) / 32;
     q_min = blk_rank[2 * own];
     q_max = blk_rank[2 * own + 1];
-    key_tile = lds_address(tiles) + wave * 2 * TL::BYTES;
-    value_tile = key_tile + TL::BYTES;
+    key_tile = lds_address(tiles) + wave * TILES * TL::BYTES;
+    value_tile = key_tile + (TILES - 1) * TL::BYTES;
   }
   // the wave's first block from b on that a query sees; past `own`: none
   __device__ __forceinline__ int32_t next(int32_t b) const {
@@ -204,19 +204,17 @@ struct Queries : Block {
 };
 
 template <int DP>
-__global__ void __launch_bounds__(256, DP > 64 ? 1 : 2) ft_f32_forward_kernel(FtArgs a, const float* __restrict__ q,
+__global__ void __launch_bounds__(256, DP > 64 ? 2 : 3) ft_f32_forward_kernel(FtArgs a, const float* __restrict__ q,
                                                                             const float* __restrict__ k,
                                                                             const float* __restrict__ v, float* __restrict__ out,
                                                                             float* __restrict__ lse) {
   using TL = Tile<DP>;
-  __shared__ __attribute__((aligned(1024))) Shared<DP> sh;
-  const Queries<DP> w(a, k, v, &sh.tiles[0][0]);
+  constexpr int TILES = 1;
+  __shared__ __attribute__((aligned(1024))) Shared<DP, TILES> sh;
+  const Queries<DP, TILES> w(a, k, v, &sh.tiles[0][0]);
   if (w.first >= w.t.len) return;
   int32_t b = w.next(w.wave);
-  if (b <= w.own) {
-    w.load_keys(b);
-    w.load_values(b);
-  }
+  if (b <= w.own) w.load_keys(b);
   typename TL::Own qf;
   TL::load(qf, q + w.token * a.sq + (int64_t)w.hq * a.D, w.h, a.D);
   int32_t rank_i[1] = {w.ranks[w.ic]};
@@ -229,9 +227,9 @@ __global__ void __launch_bounds__(256, DP > 64 ? 1 : 2) ft_f32_forward_kernel(Ft
   float m = NEG_BIG, l = 0.f;  // maximum (log2 units), this lane's share of the sum
   while (b <= w.own) {
     const int32_t after = w.next(b + 4);
-    wait_vector_memory<TL::LOADS>();  // the keys; the values were requested behind them
+    wait_vector_memory<0>();
     floatx16 s = TL::scores(w.key_tile, at, qf, floatx16{});
-    if (after <= w.own) w.load_keys(after);
+    w.load_values(b);
     w.mask(s, b, rank_i[0]);
     float p[16], top = s[0];
 #pragma unroll
@@ -249,10 +247,9 @@ __global__ void __launch_bounds__(256, DP > 64 ? 1 : 2) ft_f32_forward_kernel(Ft
       p[r] = fast_exp2(fmaf(s[r], c, -m));
       l += p[r];
     }
-    if (after <= w.own) wait_vector_memory<TL::LOADS>();  // the values
-    else wait_vector_memory<0>();
+    wait_vector_memory<0>();
     TL::add(w.value_tile, w.n, w.h, p, acc);
-    if (after <= w.own) w.load_values(after);
+    if (after <= w.own) w.load_keys(after);
     b = after;
   }
   __syncthreads();
@@ -266,10 +263,10 @@ __global__ void __launch_bounds__(256, DP > 64 ? 1 : 2) ft_f32_forward_kernel(Ft
   float total = 0.f;
 #pragma unroll
   for (int x = 0; x < 4; ++x) total = fmaf(sh.end.l[x][w.n], fast_exp2(sh.end.m[x][w.n] - top), total);
-  put<DP>(sh, w, acc, fast_exp2(m - top) / total);
+  put(sh, w, acc, fast_exp2(m - top) / total);
   if (w.wave == 0 && w.h == 0 && w.i < w.t.len) lse[w.hq * a.N + w.token] = (top + __builtin_amdgcn_logf(total)) * LN2;
   __syncthreads();
-  join<DP>(sh, w, out + ((w.t.seq0 + (int64_t)w.first) * a.Hq + w.hq) * a.D, (int64_t)a.Hq * a.D, a.D);
+  join(sh, w, out + ((w.t.seq0 + (int64_t)w.first) * a.Hq + w.hq) * a.D, (int64_t)a.Hq * a.D, a.D);
 }
 
 // delta_i = do_i . o_i: 16 lanes a row
@@ -287,22 +284,23 @@ __global__ void __launch_bounds__(256) ft_f32_delta_kernel(int64_t N, int32_t Hq
   if (threadIdx.x % 16 == 0) delta[(row % Hq) * N + row / Hq] = s;
 }
 
-// Products in the order do . v, q . k, ds . k: the next values are on their way during the last two, the next keys
-// during the first.
+// Products in the order do . v, q . k, ds . k: with two tiles the next values are on their way during the last two, the next
+// keys during the first.
 template <int DP>
-__global__ void __launch_bounds__(256, DP > 64 ? 1 : 2) ft_f32_dq_kernel(FtArgs a, const float* __restrict__ q,
+__global__ void __launch_bounds__(256, DP > 96 ? 1 : 2) ft_f32_dq_kernel(FtArgs a, const float* __restrict__ q,
                                                                        const float* __restrict__ k, const float* __restrict__ v,
                                                                        const float* __restrict__ d_out,
                                                                        const float* __restrict__ lse,
                                                                        const float* __restrict__ delta, float* __restrict__ dq) {
   using TL = Tile<DP>;
-  __shared__ __attribute__((aligned(1024))) Shared<DP> sh;
-  const Queries<DP> w(a, k, v, &sh.tiles[0][0]);
+  constexpr int TILES = DP == 96 ? 1 : 2;
+  __shared__ __attribute__((aligned(1024))) Shared<DP, TILES> sh;
+  const Queries<DP, TILES> w(a, k, v, &sh.tiles[0][0]);
   if (w.first >= w.t.len) return;
   int32_t b = w.next(w.wave);
   if (b <= w.own) {
     w.load_values(b);
-    w.load_keys(b);
+    if (TILES == 2) w.load_keys(b);
   }
   typename TL::Own qf, of;
   TL::load(qf, q + w.token * a.sq + (int64_t)w.hq * a.D, w.h, a.D);
@@ -319,9 +317,11 @@ __global__ void __launch_bounds__(256, DP > 64 ? 1 : 2) ft_f32_dq_kernel(FtArgs 
   zero(acc, TL::NB);
   while (b <= w.own) {
     const int32_t after = w.next(b + 4);
-    wait_vector_memory<TL::LOADS>();  // the values; the keys were requested behind them
+    if (TILES == 2) wait_vector_memory<TL::LOADS>();  // the values; the keys were requested behind them
+    else wait_vector_memory<0>();
     const floatx16 dp = TL::scores(w.value_tile, at, of, floatx16{});
-    if (after <= w.own) {
+    if (TILES == 1) w.load_keys(b);
+    if (TILES == 2 && after <= w.own) {
       w.load_values(after);
       wait_vector_memory<TL::LOADS>();
     } else {
@@ -333,13 +333,16 @@ __global__ void __launch_bounds__(256, DP > 64 ? 1 : 2) ft_f32_dq_kernel(FtArgs 
 #pragma unroll
     for (int r = 0; r < 16; ++r) ds[r] = fast_exp2(fmaf(s[r], c, -lse2)) * (dp[r] - row[1]);
     TL::add(w.key_tile, w.n, w.h, ds, acc);
-    if (after <= w.own) w.load_keys(after);
+    if (after <= w.own) {
+      if (TILES == 1) w.load_values(after);
+      else w.load_keys(after);
+    }
     b = after;
   }
   __syncthreads();
-  put<DP>(sh, w, acc, a.scale);
+  put(sh, w, acc, a.scale);
   __syncthreads();
-  join<DP>(sh, w, dq + (w.t.seq0 + (int64_t)w.first) * a.sdq + (int64_t)w.hq * a.D, a.sdq, a.D);
+  join(sh, w, dq + (w.t.seq0 + (int64_t)w.first) * a.sdq + (int64_t)w.hq * a.D, a.sdq, a.D);
 }
 
 // Products in the order q . k, do . v, ds . q, p . do: the next queries are on their way during the last, the next
@@ -355,7 +358,7 @@ __global__ void __launch_bounds__(256, DP > 64 ? 1 : 2) ft_f32_dkv_kernel(FtArgs
                                                                         float* __restrict__ dk,
                                                                         float* __restrict__ dv) {
   using TL = Tile<DP>;
-  __shared__ __attribute__((aligned(1024))) Shared<DP> sh;
+  __shared__ __attribute__((aligned(1024))) Shared<DP, 2> sh;
   __shared__ __attribute__((aligned(256))) float stats[4][64];  // of every wave: lse, then delta of its 32 queries
   // the block's values, for 128 channels: the registers are full
   constexpr bool LDS_VALUES = DP > 64;
@@ -448,22 +451,22 @@ __global__ void __launch_bounds__(256, DP > 64 ? 1 : 2) ft_f32_dkv_kernel(FtArgs
     x = after;
   }
   __syncthreads();
-  put<DP>(sh, w, acc_v, 1.f);
+  put(sh, w, acc_v, 1.f);
   __syncthreads();
   if (item.slot >= 0) {
     float* const p = partial + ((int64_t)item.slot * a.Hkv + hk) * (2 * 32 * DP);
-    join<DP>(sh, w, p + 32 * DP, DP, DP);
+    join(sh, w, p + 32 * DP, DP, DP);
     __syncthreads();
-    put<DP>(sh, w, acc_k, 1.f);
+    put(sh, w, acc_k, 1.f);
     __syncthreads();
-    join<DP>(sh, w, p, DP, DP);
+    join(sh, w, p, DP, DP);
     return;
   }
-  join<DP>(sh, w, dv + (w.t.seq0 + (int64_t)w.first) * a.sdv + (int64_t)hk * a.D, a.sdv, a.D);
+  join(sh, w, dv + (w.t.seq0 + (int64_t)w.first) * a.sdv + (int64_t)hk * a.D, a.sdv, a.D);
   __syncthreads();
-  put<DP>(sh, w, acc_k, a.scale);
+  put(sh, w, acc_k, a.scale);
   __syncthreads();
-  join<DP>(sh, w, dk + (w.t.seq0 + (int64_t)w.first) * a.sdk + (int64_t)hk * a.D, a.sdk, a.D);
+  join(sh, w, dk + (w.t.seq0 + (int64_t)w.first) * a.sdk + (int64_t)hk * a.D, a.sdk, a.D);
 }
 
 // Adds up the partial sums of 32 keys, in the order of their items, those of four items on their way at a time.  A
