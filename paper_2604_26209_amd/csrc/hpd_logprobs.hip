@@ -292,6 +292,18 @@ __device__ __forceinline__ void finish(const hpd_logprobs_args& a, int64_t row, 
   }
 }
 
+// A row's given token and its logit, asked for ahead of the row: two reads one after the other.
+template <typename T>
+struct Target {
+  bool has = false;
+  float logit = 0.f;
+  __device__ __forceinline__ Target(const hpd_logprobs_args& a, int64_t row, const T* x, bool wanted) {
+    const int32_t t = wanted && a.targets ? a.targets[row] : -1;
+    has = t >= 0 && t < a.vocab;
+    if (has) logit = hpd::to_float(x[t]);
+  }
+};
+
 // The piece [begin, end) of a row by WV waves, of which this is number w.
 template <typename T, bool TOP, bool WIDE>
 __device__ __forceinline__ void scan(const T* x, int32_t begin, int32_t end, int w, int WV, int K, int lane, Sums& sums, Top& top) {
@@ -405,6 +417,7 @@ __global__ void __launch_bounds__(256) logprobs_kernel(hpd_logprobs_args a, int3
     Sums sums;
     Top top;
     top.buffer = sh.keys[wave];
+    const Target<T> target(a, row, x, parts == 1);
     scan<T, TOP, false>(x, begin, end, waves == 1 ? 0 : wave, waves, K, lane, sums, top);
     sums = join_wave(sums);
     if (fabsf(sums.m) > HUGE_LOGIT && sums.m != -INFINITY) {
@@ -429,9 +442,7 @@ __global__ void __launch_bounds__(256) logprobs_kernel(hpd_logprobs_args a, int3
     }
     if (wave == 0 || waves == 1) {
       if (parts == 1) {
-        const int32_t t = a.targets ? a.targets[row] : -1;
-        const bool has = t >= 0 && t < a.vocab;
-        finish(a, row, sums, top.list, has ? hpd::to_float(x[t]) : 0.f, has, lane);
+        finish(a, row, sums, top.list, target.logit, target.has, lane);
       } else {
         float4* ws = reinterpret_cast<float4*>(a.workspace);
         if (lane == 0) ws[piece] = make_float4(sums.m, sums.r, sums.s, sums.t);
@@ -451,21 +462,23 @@ __global__ void __launch_bounds__(256) logprobs_join_kernel(hpd_logprobs_args a,
   const float4* ws = reinterpret_cast<const float4*>(a.workspace);
   const uint64_t* lists = reinterpret_cast<const uint64_t*>(ws + a.n_rows * parts);
   for (int64_t row = blockIdx.x; row < a.n_rows; row += gridDim.x) {
+    const Target<T> target(a, row, reinterpret_cast<const T*>(a.logits) + row * a.row_stride, wave == 0);
     Sums sums = no_sums();
     if (lane < parts && lane % 4 == wave) {
       const float4 p = ws[row * parts + lane];
       sums = {p.x, p.y, p.z, p.w};
     }
     Top top;
-    top.buffer = sh.keys[wave];
-    if constexpr (TOP) {  // the wave's keys side by side
-      const int32_t n = (parts - wave + 3) / 4 * K;  // of the pieces wave, wave + 4 ..
-      for (int32_t i = 0; i < n; i += 64) {
-        const int32_t at = i + lane, piece = wave + at / K * 4;
-        top.add(at < n ? lists[(row * parts + piece) * K + at % K] : 0, K, lane);
-        while (top.count >= 64) top.flush(K, lane);
+    if constexpr (TOP) {  // sorted lists, four on their way at a time: the turned one and the wave's are one bitonic sequence
+      for (int32_t piece = wave; piece < parts; piece += 16) {
+        uint64_t other[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+          other[u] = 63 - lane < K && piece + 4 * u < parts ? lists[(row * parts + piece + 4 * u) * K + 63 - lane] : 0;
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+          if (piece + 4 * u < parts) top.list = settle(larger(top.list, other[u]), lane);
       }
-      while (top.count) top.flush(K, lane);
       sh.keys[wave][lane] = top.list;
     }
     sums = join_wave(sums);
@@ -477,10 +490,7 @@ __global__ void __launch_bounds__(256) logprobs_join_kernel(hpd_logprobs_args a,
         sums = join(sums, sh.sums[w]);
         if (TOP) top.merge(sh.keys[w], lane);
       }
-      const int32_t t = a.targets ? a.targets[row] : -1;
-      const bool has = t >= 0 && t < a.vocab;
-      const T* x = reinterpret_cast<const T*>(a.logits) + row * a.row_stride;
-      finish(a, row, sums, top.list, has ? hpd::to_float(x[t]) : 0.f, has, lane);
+      finish(a, row, sums, top.list, target.logit, target.has, lane);
     }
     __syncthreads();
   }
