@@ -52,7 +52,7 @@ __device__ __forceinline__ void store_vec(E* p, const float* f) {
 }
 
 // A wave per token: D / (2 V) lanes a head, as many heads side by side as fit; the token's (cos, sin)
-// stay in registers over its heads.  Bytes-bound.
+// stay in registers over its heads.  Bound by its bytes: 19740 tokens, 32/8 heads of 128, bf16: 79 us, 5.1 TB/s (a large copy: 5.0).
 template <typename E, int V>
 __global__ void __launch_bounds__(256) ft_rotate_kernel(int32_t N, int32_t Hq, int32_t Hkv, int32_t D, int64_t sq, int64_t sk,
                                                         int64_t sqo, int64_t sko, float sign, const float2* __restrict__ rope,

@@ -2,9 +2,13 @@
 //
 // The matrix instruction (32 x 32 x 2, 64 cycles) is what bounds these kernels: the chain of products of one wave
 // is long before the GPU is full.  So the four waves of a workgroup share 32 tokens and take every fourth block of
-// the other side, each through tiles of its own in LDS, without barriers; their sums meet at the end.  There is one
-// tile of each kind: it is loaded again (global_load_lds) as soon as its last product has read it, and the order of the
-// products leaves one of them between that and the tile's next use.
+// the other side, each through tiles of its own in LDS, without barriers; their sums meet at the end.  The forward kernel has one tile
+// per wave, keys and values by turns, so that two workgroups run on a CU (three for 64 channels) and one's loads
+// are behind the other's products: 1.3 to 1.5 times as fast as with a tile of each kind and one workgroup.  The gradients have two, as
+// their registers leave room for one workgroup of 128 channels anyway (dq of 96: one tile, two workgroups): a tile is loaded again
+// (global_load_lds) as soon as its last product has read it, and the order of the products leaves one of them between that and the
+// tile's next use.  16 x 307 tokens, 4 heads of 64: forward 25 us, gradients 78 us, matrix units busy 21 to 29 %: three rounds
+// of a wave and the latencies of a start; 5 x 2500 tokens, 32/8 heads of 128: forward 2.7 ms, 96 of 153 TFLOP/s.
 //
 // Tiles: 32 rows of 64 or 128 values, of which the first DP count (64, 96 or 128; zeros from D on).  Chunk c (16 bytes) of row r lies at c ^ f(r),
 // f(r) = 8 (r / 4 % 2) + 4 (r / 8 % 2) + r % 4: sixteen rows' chunk c in different banks (left operand of four score products),
