@@ -7,10 +7,10 @@
 // are behind the other's products: 1.3 to 1.5 times as fast as with a tile of each kind and one workgroup.  The gradients have two, as
 // their registers leave room for one workgroup of 128 channels anyway (dq of 96: one tile, two workgroups): a tile is loaded again
 // (global_load_lds) as soon as its last product has read it, and the order of the products leaves one of them between that and the
-// tile's next use.  16 x 307 tokens, 4 heads of 64: forward 25 us, gradients 78 us, matrix units busy 21 to 29 %: three rounds
-// of a wave and the latencies of a start; 5 x 2500 tokens, 32/8 heads of 128: forward 2.7 ms, 96 of 153 TFLOP/s.
+// tile's next use.  16 x 307 tokens, 4 heads of 64: forward 24 us, gradients 76 us, matrix units busy 21 to 29 %: three rounds
+// of a wave and the latencies of a start; 5 x 2500 tokens, 32/8 heads of 128: forward 2.3 ms, 112 of 153 TFLOP/s.
 //
-// Tiles: 32 rows of 64 or 128 values, of which the first DP count (64, 96 or 128; zeros from D on).  Chunk c (16 bytes) of row r lies at c ^ f(r),
+// Tiles: 32 rows of 64 or 128 values, of which the first DP count (64, 96 or 128).  Chunk c (16 bytes) of row r lies at c ^ f(r),
 // f(r) = 8 (r / 4 % 2) + 4 (r / 8 % 2) + r % 4: sixteen rows' chunk c in different banks (left operand of four score products),
 // and 32 channels of the rows r and r + 4 too (left operand of a second product).
 #include "hpd_finetune_dev.h"
@@ -27,35 +27,80 @@ struct Tile {
   static constexpr int LOADS = BYTES / 1024;  // load instructions
   static __device__ __forceinline__ int swizzle(int r) { return ((r >> 2) & 1) << 3 | ((r >> 3) & 1) << 2 | (r & 3); }
 
-  // rows first .. first + 31 of a sequence's head; src: its row 0, last: its last row, which stands for those behind it; zeros:
-  // 16 bytes of them
-  static __device__ __forceinline__ void load(uint32_t lds, const float* src, int64_t stride, int32_t first, int32_t last,
-                                              int32_t D, const void* zeros, int lane) {
-    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // (the tile's last reads)
+  // Rows first .. first + 31 of a sequence's head; src: its row 0, last: its last row, which stands for those behind it.  The
+  // lanes' offsets in whole tiles are kept: 0.92 of the time with the address of every row made anew, in the mean of 36 random batches,
+  // down to 0.84.
+  struct Source {
+    static constexpr int SETS = RB / 256;  // the chunks of odd groups of 8 rows differ
+    static constexpr uint32_t BIAS = 4096;
+    const char* src;
+    int64_t stride;  // bytes
+    uint32_t off[SETS][4];
+    int32_t D, last;
+    bool near;  // a group's offsets fit 32 bits
+    static __device__ __forceinline__ int32_t row(int g, int f, int lane) { return (4 * g + f) * (1024 / RB) + lane / CHUNKS; }
+    static __device__ __forceinline__ int32_t chunk(int g, int f, int lane) { return (lane % CHUNKS) ^ swizzle(row(g, f, lane)); }
+    __device__ __forceinline__ void init(const float* x, int64_t elements, int32_t len, int32_t D_, int lane) {
+      src = reinterpret_cast<const char*>(x);
+      stride = elements * 4;
+      D = D_;
+      last = len - 1;
+      near = elements < 1 << 24;
 #pragma unroll
-    for (int g = 0; g < LOADS / 4; ++g) {
-      const char* p[4];
+      for (int g = 0; g < SETS; ++g)
 #pragma unroll
-      for (int f = 0; f < 4; ++f) {
-        const int r = (4 * g + f) * (1024 / RB) + lane / CHUNKS, c = (lane % CHUNKS) ^ swizzle(r);
-        p[f] = c * 4 < D ? reinterpret_cast<const char*>(src + min(first + r, last) * stride + c * 4)
-                         : reinterpret_cast<const char*>(zeros);
-        p[f] -= f * 1024;  // (the instruction's offset moves both addresses)
-      }
-      const uint32_t dst = __builtin_amdgcn_readfirstlane(lds + g * 4096);
-      uint32_t keep;  // M0 is the compiler's
-      asm volatile(
-          "s_mov_b32 %0, m0\n\ts_mov_b32 m0, %5\n\ts_nop 0\n\t"
-          "global_load_lds_dwordx4 %1, off\n\t"
-          "global_load_lds_dwordx4 %2, off offset:1024\n\t"
-          "global_load_lds_dwordx4 %3, off offset:2048\n\t"
-          "global_load_lds_dwordx4 %4, off offset:3072\n\t"
-          "s_mov_b32 m0, %0"
-          : "=&s"(keep)
-          : "v"(p[0]), "v"(p[1]), "v"(p[2]), "v"(p[3]), "s"(dst)
-          : "memory");
+        for (int f = 0; f < 4; ++f) {  // (behind the row's end: its first chunk, the other side's operand is zero there)
+          const int32_t c = chunk(g, f, lane);
+          off[g][f] = row(0, f, lane) * (uint32_t)stride + (c * 4 < D ? c << 4 : 0) - f * 1024 + BIAS;
+        }
     }
-  }
+    // shift: bytes from src to the head; zeros: 16 bytes of them for the chunks behind the row's end
+    __device__ __forceinline__ void load(uint32_t lds, int32_t first, int lane, int64_t shift = 0, const void* zeros = nullptr) const {
+      const char* const head = src + shift;
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // (the tile's last reads)
+      const bool whole = !zeros && near && first + 31 <= last;
+#pragma unroll
+      for (int g = 0; g < LOADS / 4; ++g) {
+        const uint32_t dst = __builtin_amdgcn_readfirstlane(lds + g * 4096);
+        uint32_t keep;  // M0 is the compiler's
+        if (whole) {
+          const uint32_t* o = off[g % SETS];
+          asm volatile(
+              "s_mov_b32 %0, m0\n\ts_mov_b32 m0, %5\n\ts_nop 0\n\t"
+              "global_load_lds_dwordx4 %1, %6\n\t"
+              "global_load_lds_dwordx4 %2, %6 offset:1024\n\t"
+              "global_load_lds_dwordx4 %3, %6 offset:2048\n\t"
+              "global_load_lds_dwordx4 %4, %6 offset:3072\n\t"
+              "s_mov_b32 m0, %0"
+              : "=&s"(keep)
+              : "v"(o[0]), "v"(o[1]), "v"(o[2]), "v"(o[3]), "s"(dst),
+                "s"(uniform(head + (first + g * (4096 / RB)) * stride) - BIAS)
+              : "memory");
+          continue;
+        }
+        const char* p[4];
+        int32_t here = lane;
+        asm volatile("" : "+v"(here));  // (nothing of this is kept from tile to tile)
+#pragma unroll
+        for (int f = 0; f < 4; ++f) {
+          const int32_t c = chunk(g, f, here);
+          p[f] = c * 4 < D || !zeros ? head + min(first + row(g, f, here), last) * stride + (c * 4 < D ? c << 4 : 0)
+                                     : reinterpret_cast<const char*>(zeros);
+          p[f] -= f * 1024;  // (the instruction's offset moves both addresses)
+        }
+        asm volatile(
+            "s_mov_b32 %0, m0\n\ts_mov_b32 m0, %5\n\ts_nop 0\n\t"
+            "global_load_lds_dwordx4 %1, off\n\t"
+            "global_load_lds_dwordx4 %2, off offset:1024\n\t"
+            "global_load_lds_dwordx4 %3, off offset:2048\n\t"
+            "global_load_lds_dwordx4 %4, off offset:3072\n\t"
+            "s_mov_b32 m0, %0"
+            : "=&s"(keep)
+            : "v"(p[0]), "v"(p[1]), "v"(p[2]), "v"(p[3]), "s"(dst)
+            : "memory");
+      }
+    }
+  };
   struct Own { float4 f[STEPS]; };  // chunk 2 s + h of the lane's row
   static __device__ __forceinline__ void load(Own& x, const float* row, int h, int32_t D) {
 #pragma unroll
@@ -168,7 +213,7 @@ struct Queries : Block {
   int32_t hq, hk, own, q_min, q_max;
   const int32_t* ranks;
   const const_i32* blk_rank;
-  const float *keys, *values;
+  typename TL::Source keys, values;
   uint32_t key_tile, value_tile;  // (one tile: keys and values by turns)
   int64_t token;
   __device__ __forceinline__ Queries(const FtArgs& args, const float* k, const float* v, const char* tiles)
@@ -177,8 +222,8 @@ struct Queries : Block {
     hk = x % a.Hkv;
     hq = hk * G + x / a.Hkv;
     token = t.seq0 + (int64_t)ic;
-    keys = k + t.seq0 * a.sk + (int64_t)hk * a.D;
-    values = v + t.seq0 * a.sv + (int64_t)hk * a.D;
+    keys.init(k + t.seq0 * a.sk + (int64_t)hk * a.D, a.sk, t.len, a.D, lane);
+    values.init(v + t.seq0 * a.sv + (int64_t)hk * a.D, a.sv, t.len, a.D, lane);
     ranks = a.rank + t.seq0;
     blk_rank = (const const_i32*)(uintptr_t)(a.blk_rank + t.blk0);
     own = min(first, t.len - 1) / 32;
@@ -192,12 +237,8 @@ struct Queries : Block {
     while (b <= own && blk_rank[2 * b] > q_max) b += 4;
     return b;
   }
-  __device__ __forceinline__ void load_keys(int32_t b) const {
-    TL::load(key_tile, keys, a.sk, b * 32, t.len - 1, a.D, a.rank + a.N, lane);
-  }
-  __device__ __forceinline__ void load_values(int32_t b) const {
-    TL::load(value_tile, values, a.sv, b * 32, t.len - 1, a.D, a.rank + a.N, lane);
-  }
+  __device__ __forceinline__ void load_keys(int32_t b) const { keys.load(key_tile, b * 32, lane); }
+  __device__ __forceinline__ void load_values(int32_t b) const { values.load(value_tile, b * 32, lane); }
   __device__ __forceinline__ void mask(floatx16& s, int32_t b, int32_t rank_i) const {
     if (b < own && blk_rank[2 * b + 1] <= q_min) return;
     BlockRanks rk;
@@ -386,12 +427,13 @@ __global__ void __launch_bounds__(256, DP > 64 ? 1 : 2) ft_f32_dkv_kernel(FtArgs
     }
     return x;
   };
-  auto load_queries = [&](Where x) {
-    TL::load(q_tile, q + w.t.seq0 * a.sq + (int64_t)(hk * G + x.g) * a.D, a.sq, x.b * 32, w.t.len - 1, a.D, a.rank + a.N, w.lane);
-  };
+  typename TL::Source queries, gradients;
+  queries.init(q + w.t.seq0 * a.sq, a.sq, w.t.len, a.D, w.lane);
+  gradients.init(d_out + w.t.seq0 * so, so, w.t.len, a.D, w.lane);
+  auto load_queries = [&](Where x) { queries.load(q_tile, x.b * 32, w.lane, (int64_t)(hk * G + x.g) * a.D * 4); };
   auto load_gradients = [&](Where x) {
     const int32_t hq = hk * G + x.g;
-    TL::load(o_tile, d_out + w.t.seq0 * so + (int64_t)hq * a.D, so, x.b * 32, w.t.len - 1, a.D, a.rank + a.N, w.lane);
+    gradients.load(o_tile, x.b * 32, w.lane, (int64_t)hq * a.D * 4);
     const float* p = (w.h ? delta : lse) + hq * a.N + w.t.seq0 + min(x.b * 32 + w.n, w.t.len - 1);
     const uint32_t dst = __builtin_amdgcn_readfirstlane(lds_address(&stats[w.wave][0]));
     uint32_t keep;
@@ -404,7 +446,9 @@ __global__ void __launch_bounds__(256, DP > 64 ? 1 : 2) ft_f32_dkv_kernel(FtArgs
   };
   if (LDS_VALUES) {
     if (w.wave == 0) {
-      TL::load(lds_address(values), v + w.t.seq0 * a.sv + (int64_t)hk * a.D, a.sv, w.first, w.t.len - 1, a.D, a.rank + a.N, w.lane);
+      typename TL::Source own;
+      own.init(v + w.t.seq0 * a.sv + (int64_t)hk * a.D, a.sv, w.t.len, a.D, w.lane);
+      own.load(lds_address(values), w.first, w.lane, 0, a.D < DP ? a.rank + a.N : nullptr);
       wait_vector_memory<0>();
     }
     __syncthreads();
