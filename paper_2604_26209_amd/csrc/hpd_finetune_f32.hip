@@ -4,11 +4,12 @@
 // is long before the GPU is full.  So the four waves of a workgroup share 32 tokens and take every fourth block of
 // the other side, each through tiles of its own in LDS, without barriers; their sums meet at the end.  The forward kernel has one tile
 // per wave, keys and values by turns, so that two workgroups run on a CU (three for 64 channels) and one's loads
-// are behind the other's products: 1.3 to 1.5 times as fast as with a tile of each kind and one workgroup.  The gradients have two, as
-// their registers leave room for one workgroup of 128 channels anyway (dq of 96: one tile, two workgroups): a tile is loaded again
-// (global_load_lds) as soon as its last product has read it, and the order of the products leaves one of them between that and the
-// tile's next use.  16 x 307 tokens, 4 heads of 64: forward 24 us, gradients 76 us, matrix units busy 21 to 29 %: three rounds
-// of a wave and the latencies of a start; 5 x 2500 tokens, 32/8 heads of 128: forward 2.3 ms, 112 of 153 TFLOP/s.
+// are behind the other's products: 1.3 to 1.5 times as fast as with a tile of each kind and one workgroup.  So has dq from 96 channels
+// on, for 128 with the gradients of the output in LDS as well (up to 1.3 times the gradients' speed).  dq of 64 channels and dk/dv, whose
+// sums leave no room for a second workgroup of 96 or 128 channels, have two: a tile is loaded again (global_load_lds) as soon as its
+// last product has read it, and the order of the products leaves one of them between that and the tile's next use.
+// 16 x 307 tokens, 4 heads of 64: forward 24 us, gradients 76 us, matrix units busy 23 to 30 %: three rounds
+// of a wave and the latencies of a start; 5 x 2500 tokens, 32/8 heads of 128: forward 2.2 ms, 104 of 153 TFLOP/s.
 //
 // Tiles: 32 rows of 64 or 128 values, of which the first DP count (64, 96 or 128).  Chunk c (16 bytes) of row r lies at c ^ f(r),
 // f(r) = 8 (r / 4 % 2) + 4 (r / 8 % 2) + r % 4: sixteen rows' chunk c in different banks (left operand of four score products),
@@ -171,17 +172,17 @@ struct Block {
   }
 };
 
-// One or two tiles of every wave; at the end its sums, row by row
-template <int DP, int TILES>
+// One or two tiles of every wave and OWN of the workgroup; at the end the waves' sums, row by row
+template <int DP, int TILES, int OWN = 0>
 union Shared {
   struct {
     float sums[4][32][DP + 4];
     float m[4][32], l[4][32];
   } end;
-  char tiles[4][TILES * Tile<DP>::BYTES];
+  char tiles[4 * TILES + OWN][Tile<DP>::BYTES];
 };
-template <int DP, int TILES>
-__device__ __forceinline__ void put(Shared<DP, TILES>& sh, const Block& w, const floatx16* acc, float f) {
+template <int DP, int TILES, int OWN>
+__device__ __forceinline__ void put(Shared<DP, TILES, OWN>& sh, const Block& w, const floatx16* acc, float f) {
 #pragma unroll
   for (int b = 0; b < DP / 32; ++b)
 #pragma unroll
@@ -190,8 +191,8 @@ __device__ __forceinline__ void put(Shared<DP, TILES>& sh, const Block& w, const
           make_float4(acc[b][4 * a] * f, acc[b][4 * a + 1] * f, acc[b][4 * a + 2] * f, acc[b][4 * a + 3] * f);
 }
 // the sum of the waves' rows r to out + r * stride
-template <int DP, int TILES>
-__device__ __forceinline__ void join(const Shared<DP, TILES>& sh, const Block& w, float* out, int64_t stride, int32_t D) {
+template <int DP, int TILES, int OWN>
+__device__ __forceinline__ void join(const Shared<DP, TILES, OWN>& sh, const Block& w, float* out, int64_t stride, int32_t D) {
   for (int x = threadIdx.x; x < 32 * DP / 4; x += 256) {
     const int r = x / (DP / 4), c = x % (DP / 4) * 4;
     if (w.first + r >= w.t.len || c >= D) continue;
@@ -332,14 +333,14 @@ __global__ void __launch_bounds__(256) ft_f32_delta_kernel(int64_t N, int32_t Hq
 // Products in the order do . v, q . k, ds . k: with two tiles the next values are on their way during the last two, the next
 // keys during the first.
 template <int DP>
-__global__ void __launch_bounds__(256, DP > 96 ? 1 : 2) ft_f32_dq_kernel(FtArgs a, const float* __restrict__ q,
+__global__ void __launch_bounds__(256, 2) ft_f32_dq_kernel(FtArgs a, const float* __restrict__ q,
                                                                        const float* __restrict__ k, const float* __restrict__ v,
                                                                        const float* __restrict__ d_out,
                                                                        const float* __restrict__ lse,
                                                                        const float* __restrict__ delta, float* __restrict__ dq) {
   using TL = Tile<DP>;
-  constexpr int TILES = DP == 96 ? 1 : 2;
-  __shared__ __attribute__((aligned(1024))) Shared<DP, TILES> sh;
+  constexpr int TILES = DP >= 96 ? 1 : 2, OWN = DP > 96 ? 1 : 0;  // (what two workgroups per CU have room for)
+  __shared__ __attribute__((aligned(1024))) Shared<DP, TILES, OWN> sh;
   const Queries<DP, TILES> w(a, k, v, &sh.tiles[0][0]);
   if (w.first >= w.t.len) return;
   int32_t b = w.next(w.wave);
@@ -348,12 +349,23 @@ __global__ void __launch_bounds__(256, DP > 96 ? 1 : 2) ft_f32_dq_kernel(FtArgs 
     if (TILES == 2) w.load_keys(b);
   }
   typename TL::Own qf, of;
+  const uint32_t own = lds_address(&sh.tiles[4 * TILES + OWN - 1][0]);
   TL::load(qf, q + w.token * a.sq + (int64_t)w.hq * a.D, w.h, a.D);
-  TL::load(of, d_out + (w.token * a.Hq + w.hq) * a.D, w.h, a.D);
+  if (OWN) {
+    if (w.wave == 0) {
+      typename TL::Source rows;
+      rows.init(d_out + (w.t.seq0 * (int64_t)a.Hq + w.hq) * a.D, (int64_t)a.Hq * a.D, w.t.len, a.D, w.lane);
+      rows.load(own, w.first, w.lane, 0, a.D < DP ? a.rank + a.N : nullptr);
+      wait_vector_memory<0>();
+    }
+    __syncthreads();
+  } else {
+    TL::load(of, d_out + (w.token * a.Hq + w.hq) * a.D, w.h, a.D);
+  }
   float row[2] = {lse[w.hq * a.N + w.token], delta[w.hq * a.N + w.token]};
   int32_t rank_i[1] = {w.ranks[w.ic]};
   own_arrived(qf.f);
-  own_arrived(of.f);
+  if (!OWN) own_arrived(of.f);
   arrived(row);
   arrived(rank_i);
   const float c = a.scale * LOG2E, lse2 = row[0] * LOG2E;
@@ -364,7 +376,7 @@ __global__ void __launch_bounds__(256, DP > 96 ? 1 : 2) ft_f32_dq_kernel(FtArgs 
     const int32_t after = w.next(b + 4);
     if (TILES == 2) wait_vector_memory<TL::LOADS>();  // the values; the keys were requested behind them
     else wait_vector_memory<0>();
-    const floatx16 dp = TL::scores(w.value_tile, at, of, floatx16{});
+    const floatx16 dp = OWN ? TL::scores(w.value_tile, at, own, floatx16{}) : TL::scores(w.value_tile, at, of, floatx16{});
     if (TILES == 1) w.load_keys(b);
     if (TILES == 2 && after <= w.own) {
       w.load_values(after);
