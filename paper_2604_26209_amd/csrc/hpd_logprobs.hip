@@ -2,9 +2,12 @@
 //
 // In log2 units, y = x log2(e), with a reference point k, s = sum 2^(y - k), t = sum 2^(y - k) (y - k):
 //   lse = (k + log2 s) ln 2,  logprob = (y_target - k - log2 s) ln 2,  entropy = (log2 s - t / s) ln 2.
-// One pass over the logits: every lane keeps (k, s, t) of its share; k is a whole number not below the lane's maximum, so
+// One pass over the logits: every lane keeps (k, s, t) of its share; k is a whole number, the lane's maximum rounded up, so
 // that y - k is one multiply-add and moving k by d is exact: t' = (t - d s) 2^-d, s' = s 2^-d.  Partial
-// results are joined by the same rule.  The pass is bound by the bytes of the logits, with the vector instructions (an exponential
+// results are joined by the same rule.  A k beyond 2^24 would not be whole, and its rounding not small: k starts at -2^22, below
+// which a logit counts nothing beside others, and where the largest logit of a wave's share is further from 0 than 2^21 (all
+// tokens excluded by a finite value, or a diverged row), the wave goes over it again with the maximum itself as
+// reference point, as a sum of two numbers.  The pass is bound by the bytes of the logits, with the vector instructions (an exponential
 // and five to six more per logit) close behind: 6144 x 130013 bf16 logits with one alternative 295 us, 5.4 TB/s; without 5.4,
 // with eight 4.0, with fifty 3.3 TB/s.
 //
@@ -63,64 +66,67 @@ struct Vec<hpd::bf16_t> {
 };
 
 // ---- sums
-constexpr float HUGE_LOGIT = 1.0e38f;  // beyond it x log2(e) may not be finite
-constexpr float LOWEST_REFERENCE = -1.25f * HUGE_LOGIT;  // below x log2(e) / 4 of every finite logit
+constexpr float NARROW = 2097152.f;          // 2^21: largest logit, in magnitude, up to which a reference point is a whole number
+constexpr float NARROW_START = -1048576.f;   // -2^22 / 4
+constexpr float OVERFLOWING = -1.0e37f;      // below it y - k may not be finite
+constexpr float LOWEST_REFERENCE = -1.25e38f;  // below x log2(e) / 4 of every finite logit
 struct Sums {
-  float m;  // largest logit
-  float r;  // reference point / 4 (finite for every finite logit)
+  float m;      // largest logit
+  float r, lo;  // reference point / 4 (finite for every finite logit): r + lo, lo = 0 for a whole number
   float s, t;
 };
-__device__ __forceinline__ Sums no_sums() { return {-INFINITY, -0.25f * HUGE_LOGIT, 0.f, 0.f}; }
-// raises the reference point to 4 r >= 4 a.r
-__device__ __forceinline__ void raise(Sums& a, float r) {
-  const float d = fminf(4.f * (r - a.r), 1.0e4f), f = fast_exp2(-d);
+template <bool WIDE>
+__device__ __forceinline__ Sums no_sums() { return {-INFINITY, WIDE ? LOWEST_REFERENCE : NARROW_START, 0.f, 0.f, 0.f}; }
+// raises the reference point to 4 (r + lo) >= 4 (a.r + a.lo)
+__device__ __forceinline__ void raise(Sums& a, float r, float lo) {
+  const float d = fminf(4.f * ((r - a.r) + (lo - a.lo)), 1.0e4f), f = fast_exp2(-d);
   a.t = fmaf(-d, a.s, a.t) * f;
   a.s *= f;
   a.r = r;
+  a.lo = lo;
 }
 __device__ __forceinline__ Sums join(Sums a, Sums b) {
   if (a.s == 0.f) a.r = LOWEST_REFERENCE;  // (nothing there: its reference point says nothing)
   if (b.s == 0.f) b.r = LOWEST_REFERENCE;
-  const float r = fmaxf(a.r, b.r);
-  raise(a, r);
-  raise(b, r);
-  return {fmaxf(a.m, b.m), r, a.s + b.s, a.t + b.t};
+  const bool first = a.r > b.r || (a.r == b.r && a.lo >= b.lo);
+  const float r = first ? a.r : b.r, lo = first ? a.lo : b.lo;
+  raise(a, r, lo);
+  raise(b, r, lo);
+  return {fmaxf(a.m, b.m), r, lo, a.s + b.s, a.t + b.t};
 }
+// (lo is 0 in a narrow share; what a wide one's largest logit was does not matter any more)
+template <bool WIDE>
 __device__ __forceinline__ Sums join_wave(Sums a) {
 #pragma unroll
-  for (int d = 32; d; d >>= 1) a = join(a, {__shfl_xor(a.m, d), __shfl_xor(a.r, d), __shfl_xor(a.s, d), __shfl_xor(a.t, d)});
+  for (int d = 32; d; d >>= 1)
+    a = join(a, {WIDE ? a.m : __shfl_xor(a.m, d), __shfl_xor(a.r, d), WIDE ? __shfl_xor(a.lo, d) : 0.f, __shfl_xor(a.s, d),
+                 __shfl_xor(a.t, d)});
   return a;
 }
-// (y - k) / 4 of a logit.  WIDE: the reference point is the rounded y of the largest logit, and has to be met.
-template <bool WIDE>
-__device__ __forceinline__ float quarter(float x, float r) {
-  if (!WIDE) return fmaf(x, 0.25f * LOG2E, -r);
-  float y = x * (0.25f * LOG2E);
-  asm("" : "+v"(y));  // (rounded: no multiply-add)
-  return y - r;
-}
-// The logits of one vector.  -infinity counts nothing, NaN and +infinity make s NaN.  WIDE: for rows whose largest logit
-// is beyond HUGE_LOGIT in magnitude.
+// (y - k) / 4 of a logit, rounded by its own size however far y and k are from 0
+__device__ __forceinline__ float quarter(float x, const Sums& a) { return fmaf(x, 0.25f * LOG2E, -a.r) - a.lo; }
+// The logits of one vector.  -infinity counts nothing, NaN and +infinity make s NaN.  WIDE: for shares whose largest logit
+// is beyond NARROW in magnitude.
 template <int N, bool WIDE>
 __device__ __forceinline__ void add_logits(Sums& a, const float* x, float m) {
   a.m = fmaxf(a.m, m);
   if constexpr (WIDE) {
-    const float r = m * (0.25f * LOG2E);
-    if (r > a.r) raise(a, r);
+    const float r = m * (0.25f * LOG2E), lo = fmaf(m, 0.25f * LOG2E, -r);
+    if (r > a.r || (r == a.r && lo > a.lo)) raise(a, r, lo);
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-      const float d = 4.f * quarter<WIDE>(x[i], a.r), e = fast_exp2(d);
+      const float d = 4.f * quarter(x[i], a), e = fast_exp2(d);
       a.s += e;
       a.t = fmaf(e, fmaxf(d, -200.f), a.t);
     }
   } else {
     const float y = m * LOG2E;
-    if (y > 4.f * a.r) raise(a, 0.25f * ceilf(y));
+    if (y > 4.f * a.r) raise(a, 0.25f * ceilf(y), 0.f);
     float low = x[0];
 #pragma unroll
     for (int i = 1; i < N; ++i) low = fminf(low, x[i]);
     const float k = 4.f * a.r;
-    if (__any(low < -0.1f * HUGE_LOGIT)) {
+    if (__any(low < OVERFLOWING)) {
 #pragma unroll
       for (int i = 0; i < N; ++i) {
         const float d = fmaf(x[i], LOG2E, -k), e = fast_exp2(d);
@@ -277,12 +283,9 @@ __device__ __forceinline__ void finish(const hpd_logprobs_args& a, int64_t row, 
                                        bool has_target, int lane) {
   const bool none = s.s == 0.f;  // nothing but -infinity
   const float log_s = log2f(s.s);
-  auto log_probability = [&](float x) {
-    const float d = fabsf(s.m) > HUGE_LOGIT ? quarter<true>(x, s.r) : quarter<false>(x, s.r);
-    return none ? -INFINITY : fmaf(d, 4.f * LN2, -log_s * LN2);
-  };
+  auto log_probability = [&](float x) { return none ? -INFINITY : fmaf(quarter(x, s), 4.f * LN2, -log_s * LN2); };
   if (lane == 0) {
-    if (a.lse) a.lse[row] = none ? -INFINITY : fmaf(s.r, 4.f * LN2, log_s * LN2);
+    if (a.lse) a.lse[row] = none ? -INFINITY : fmaf(s.r, 4.f * LN2, fmaf(s.lo, 4.f * LN2, log_s * LN2));
     if (a.entropy) a.entropy[row] = none ? 0.f : (log_s - s.t / s.s) * LN2;
     if (a.targets && a.logprob) a.logprob[row] = has_target ? log_probability(x_target) : 0.f;
   }
@@ -308,8 +311,7 @@ struct Target {
 template <typename T, bool TOP, bool WIDE>
 __device__ __forceinline__ void scan(const T* x, int32_t begin, int32_t end, int w, int WV, int K, int lane, Sums& sums, Top& top) {
   using V = Vec<T>;
-  sums = no_sums();
-  if (WIDE) sums.r = LOWEST_REFERENCE;
+  sums = no_sums<WIDE>();
   // one vector per lane, the first logit of which is number `index`; its logits first .. last - 1 count
   auto take = [&](const float* f, int32_t index, int first, int last) __attribute__((always_inline)) {
     float m = f[0];
@@ -419,11 +421,11 @@ __global__ void __launch_bounds__(256) logprobs_kernel(hpd_logprobs_args a, int3
     top.buffer = sh.keys[wave];
     const Target<T> target(a, row, x, parts == 1);
     scan<T, TOP, false>(x, begin, end, waves == 1 ? 0 : wave, waves, K, lane, sums, top);
-    sums = join_wave(sums);
-    if (fabsf(sums.m) > HUGE_LOGIT && sums.m != -INFINITY) {
+    sums = join_wave<false>(sums);
+    if (fabsf(sums.m) > NARROW && sums.m != -INFINITY) {
       Top unused;
       scan<T, false, true>(x, begin, end, waves == 1 ? 0 : wave, waves, K, lane, sums, unused);
-      sums = join_wave(sums);
+      sums = join_wave<true>(sums);
     }
     if constexpr (TOP) {
       while (top.count) top.flush(K, lane);
@@ -445,7 +447,7 @@ __global__ void __launch_bounds__(256) logprobs_kernel(hpd_logprobs_args a, int3
         finish(a, row, sums, top.list, target.logit, target.has, lane);
       } else {
         float4* ws = reinterpret_cast<float4*>(a.workspace);
-        if (lane == 0) ws[piece] = make_float4(sums.m, sums.r, sums.s, sums.t);
+        if (lane == 0) ws[piece] = make_float4(sums.r, sums.lo, sums.s, sums.t);
         if (TOP && lane < K) reinterpret_cast<uint64_t*>(ws + a.n_rows * parts)[piece * K + lane] = top.list;
       }
     }
@@ -453,7 +455,7 @@ __global__ void __launch_bounds__(256) logprobs_kernel(hpd_logprobs_args a, int3
   }
 }
 
-// joins the pieces of a row: four waves take every fourth
+// joins the pieces of a row: four waves take every fourth list, the last one the sums as well
 template <typename T, bool TOP>
 __global__ void __launch_bounds__(256) logprobs_join_kernel(hpd_logprobs_args a, int32_t parts) {
   __shared__ Shared sh;
@@ -463,10 +465,10 @@ __global__ void __launch_bounds__(256) logprobs_join_kernel(hpd_logprobs_args a,
   const uint64_t* lists = reinterpret_cast<const uint64_t*>(ws + a.n_rows * parts);
   for (int64_t row = blockIdx.x; row < a.n_rows; row += gridDim.x) {
     const Target<T> target(a, row, reinterpret_cast<const T*>(a.logits) + row * a.row_stride, wave == 0);
-    Sums sums = no_sums();
-    if (lane < parts && lane % 4 == wave) {
+    Sums sums = no_sums<true>();
+    if (wave == 3 && lane < parts) {
       const float4 p = ws[row * parts + lane];
-      sums = {p.x, p.y, p.z, p.w};
+      sums = {-INFINITY, p.x, p.y, p.z, p.w};
     }
     Top top;
     if constexpr (TOP) {  // sorted lists, four on their way at a time: the turned one and the wave's are one bitonic sequence
@@ -481,16 +483,17 @@ __global__ void __launch_bounds__(256) logprobs_join_kernel(hpd_logprobs_args a,
       }
       sh.keys[wave][lane] = top.list;
     }
-    sums = join_wave(sums);
-    if (lane == 0) sh.sums[wave] = sums;
+    if (wave == 3) {
+      sums = join_wave<true>(sums);
+      if (lane == 0) sh.sums[0] = sums;
+    }
     __syncthreads();
     if (wave == 0) {
+      if constexpr (TOP) {
 #pragma unroll
-      for (int w = 1; w < 4; ++w) {
-        sums = join(sums, sh.sums[w]);
-        if (TOP) top.merge(sh.keys[w], lane);
+        for (int w = 1; w < 4; ++w) top.merge(sh.keys[w], lane);
       }
-      finish(a, row, sums, top.list, target.logit, target.has, lane);
+      finish(a, row, sh.sums[0], top.list, target.logit, target.has, lane);
     }
     __syncthreads();
   }
