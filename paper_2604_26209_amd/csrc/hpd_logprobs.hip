@@ -319,7 +319,7 @@ __device__ __forceinline__ void scan(const T* x, int32_t begin, int32_t end, int
     for (int e = 1; e < V::N; ++e) m = fmaxf(m, f[e]);
     add_logits<V::N, WIDE>(sums, f, m);
     if constexpr (TOP) {
-      if (__any(!top.full || m >= top.bar)) {
+      if (__any(!top.full || !(m < top.bar))) {  // (a vector of NaN too: its keys are those of -infinity)
 #pragma unroll
         for (int e = 0; e < V::N; ++e) top.add(e >= first && e < last ? make_key(f[e], index + e) : 0, K, lane);
         while (top.count >= 64) top.flush(K, lane);

@@ -74,3 +74,29 @@ def test_rows_of_magnitudes_drawn_at_random(rows, vocab, dtype):
     x[::2] = -np.abs(x[::2])                                # (the largest: near 0)
     x[1::4] = -top[1::4] + np.abs(x[1::4]) / 3              # (all far below 0)
     _compare(torch.from_numpy(x).to(TD[dtype]), rng.integers(0, vocab, rows), 4)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("top", [1, 7, 64])
+@pytest.mark.parametrize("vocab", [70, 900, 4000, 8000, 32000, 32768, 128256])
+def test_alternatives_among_nan(vocab, top, dtype):
+    """NaN counts as -infinity among the alternatives: the lowest indices come first where too few others are left."""
+    inf = float("inf")
+    x = torch.full((9, vocab), float("nan"))
+    x[1, vocab - 1] = 2.0
+    x[2, : min(5, top)] = torch.arange(min(5, top)) * 1.0
+    x[3, vocab // 2:] = 0.5                        # enough others
+    x[4, ::1000] = -torch.arange(len(x[4, ::1000])) * 1.0
+    x[5, vocab // 3] = -inf                        # equal to the NaN around it
+    x[6, vocab // 3] = -1.0e30
+    x[7, vocab - 1] = inf
+    x[8] = torch.randn(vocab, generator=torch.Generator().manual_seed(vocab))
+    x[8, 8: vocab - vocab // 4] = float("nan")
+    x = x.to(TD[dtype])
+    target = torch.zeros(len(x), dtype=torch.int32, device="cuda")
+    logprob, lse, entropy, ids, vals = _run_logprobs(x.cuda(), target, top)
+    x64 = R.to_numpy(x)
+    want = np.argsort(-np.where(np.isnan(x64), -np.inf, x64), axis=1, kind="stable")[:, :top]
+    assert np.array_equal(ids.cpu().numpy(), want)
+    for t in (logprob, lse, entropy, vals):
+        assert bool(torch.isnan(t).all())
