@@ -461,7 +461,7 @@ int hpd_finetune_layout_query(const hpd_finetune_layout* layout, int32_t what, v
 
 /* hpd_finetune_rotate - channel pairs (m, m + D/2) of q and k, turned by the token's position ID
  * times rope_base^(-2m/D); inverse != 0: by the negative angle (the gradient of the rotation).
- * q_out may be q and k_out may be k with equal strides. */
+ * q_out may be q and k_out may be k with equal strides (HPD_E_INVALID with others). */
 int hpd_finetune_rotate(const hpd_finetune_layout* layout, int32_t inverse, const void* q, const void* k, void* q_out,
                         void* k_out, const hpd_finetune_strides* strides, void* stream);
 

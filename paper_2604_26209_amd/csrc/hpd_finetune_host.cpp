@@ -307,6 +307,8 @@ int hpd_finetune_rotate(const hpd_finetune_layout* L, int32_t inverse, const voi
   if (L->n_tokens == 0) return HPD_OK;
   for (const void* p : {q, k, (const void*)q_out, (const void*)k_out})
     if (!p || !aligned(p)) return HPD_E_INVALID;
+  // in place: a token's wave has read what it writes, but not what other tokens' waves read
+  if ((q_out == q && st.q_out != st.q) || (k_out == k && st.k_out != st.k)) return HPD_E_INVALID;
   HPD_HIP(hpd_launch_ft_rotate(L, inverse != 0, q, k, q_out, k_out, st, (hipStream_t)stream));
   return HPD_OK;
 }
