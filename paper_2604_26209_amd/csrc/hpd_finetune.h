@@ -64,6 +64,11 @@ inline int32_t hpd_ft_padded_dim(const hpd_finetune_layout* L) {
   const int32_t d = (L->cfg.head_dim + 31) / 32 * 32;
   return L->cfg.dtype == HPD_F32 && d < 64 ? 64 : d;
 }
+// Workgroups of 256 threads of the kernels that go by queries and of those that go by keys.
+inline int64_t hpd_ft_query_groups(const hpd_finetune_layout* L) {
+  return (int64_t)(L->cfg.dtype == HPD_BF16 ? L->query_items.size() : L->tiles.size() * (HPD_FT_ROWS / HPD_FT_BLOCK)) * L->cfg.n_q_heads;
+}
+inline int64_t hpd_ft_key_groups(const hpd_finetune_layout* L) { return (int64_t)L->items.size() * L->cfg.n_kv_heads; }
 // Bytes of the calls' workspaces.
 int64_t hpd_ft_forward_bytes(const hpd_finetune_layout* L);
 int64_t hpd_ft_backward_bytes(const hpd_finetune_layout* L);

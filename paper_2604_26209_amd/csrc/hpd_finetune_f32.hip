@@ -562,7 +562,7 @@ __global__ void __launch_bounds__(8 * DP / 4) ft_f32_dkv_join_kernel(FtArgs a, c
 template <int DP>
 hipError_t forward(const hpd_finetune_layout* L, const FtArgs& a, const float* q, const float* k, const float* v, float* out,
                    float* lse, hipStream_t s) {
-  ft_f32_forward_kernel<DP><<<dim3((unsigned)L->tiles.size() * 4 * a.Hq), 256, 0, s>>>(a, q, k, v, out, lse);
+  ft_f32_forward_kernel<DP><<<dim3((unsigned)hpd_ft_query_groups(L)), 256, 0, s>>>(a, q, k, v, out, lse);
   return hipGetLastError();
 }
 
@@ -570,11 +570,9 @@ template <int DP>
 hipError_t backward(const hpd_finetune_layout* L, FtArgs a, const float* q, const float* k, const float* v, const float* out,
                     const float* lse, const float* d_out, float* dq, float* dk, float* dv, float* delta, hipStream_t s) {
   ft_f32_delta_kernel<<<dim3((unsigned)((a.N * a.Hq + 15) / 16)), 256, 0, s>>>(a.N, a.Hq, a.D, out, d_out, delta);
-  const unsigned blocks = (unsigned)L->tiles.size() * 4;
-  ft_f32_dq_kernel<DP><<<dim3(blocks * a.Hq), 256, 0, s>>>(a, q, k, v, d_out, lse, delta, dq);
+  ft_f32_dq_kernel<DP><<<dim3((unsigned)hpd_ft_query_groups(L)), 256, 0, s>>>(a, q, k, v, d_out, lse, delta, dq);
   float* partial = delta + 2 * a.N * a.Hq + (-2 * a.N * a.Hq & 3);  // (on 16 bytes)
-  ft_f32_dkv_kernel<DP><<<dim3((unsigned)L->items.size() * a.Hkv), 256, 0, s>>>(a, L->d_items, q, k, v, d_out, lse, delta, partial,
-                                                                               dk, dv);
+  ft_f32_dkv_kernel<DP><<<dim3((unsigned)hpd_ft_key_groups(L)), 256, 0, s>>>(a, L->d_items, q, k, v, d_out, lse, delta, partial, dk, dv);
   if (!L->joins.empty())
     ft_f32_dkv_join_kernel<DP><<<dim3((unsigned)L->joins.size() * a.Hkv * 8), 2 * DP, 0, s>>>(a, L->d_joins, partial, dk, dv);
   return hipGetLastError();

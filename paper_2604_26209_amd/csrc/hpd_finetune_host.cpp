@@ -18,8 +18,9 @@ namespace {
   } while (0)
 
 constexpr int64_t LIMIT = (int64_t)1 << 30;      // positions, rows and columns of logits
-constexpr int64_t MAX_TOKENS = (int64_t)1 << 25;  // (a launch has less than 2^32 threads)
+constexpr int64_t MAX_TOKENS = (int64_t)1 << 25;
 constexpr int64_t MAX_ROWS = (int64_t)1 << 27;    // tokens times query heads
+constexpr int64_t MAX_THREADS = ((int64_t)1 << 32) - 1;  // of a launch
 
 int elem_bytes(int32_t dtype) { return dtype == HPD_F32 ? 4 : 2; }
 
@@ -136,6 +137,8 @@ int build_tables(hpd_finetune_layout* L, const int32_t* prompt_len, const int32_
     return std::min(a.row0 + HPD_FT_ROWS, a.len) > std::min(b.row0 + HPD_FT_ROWS, b.len);
   });
   plan_items(L, plain, n_cus);
+  // (MAX_TOKENS and MAX_ROWS are enough for the kernels that go by tokens, and few tiles are cut and joined)
+  if (std::max(hpd_ft_query_groups(L), hpd_ft_key_groups(L)) * 256 > MAX_THREADS) return HPD_E_OVERFLOW;
   L->rope_by_token = L->max_pos >= L->n_tokens;
   L->rope_rows = L->rope_by_token ? L->n_tokens : L->max_pos + 1;
   return HPD_OK;

@@ -882,8 +882,7 @@ __global__ void __launch_bounds__(64 * NB) ft_stream_join_gradients_kernel(FtArg
 template <int NB>
 hipError_t forward(const hpd_finetune_layout* L, const FtArgs& a, const uint16_t* q, const uint16_t* k, const uint16_t* v,
                    uint16_t* out, float* lse, float* partial, hipStream_t s) {
-  ft_stream_forward_kernel<NB><<<dim3((unsigned)L->query_items.size() * a.Hq), 256, 0, s>>>(a, L->d_query_items, q, k, v, out, lse,
-                                                                                        partial);
+  ft_stream_forward_kernel<NB><<<dim3((unsigned)hpd_ft_query_groups(L)), 256, 0, s>>>(a, L->d_query_items, q, k, v, out, lse, partial);
   if (!L->query_joins.empty())
     ft_stream_join_kernel<NB><<<dim3((unsigned)L->query_joins.size() * a.Hq * 4), 64 * NB, 0, s>>>(a, L->d_query_joins, partial, out,
                                                                                              lse);
@@ -896,10 +895,9 @@ hipError_t backward(const hpd_finetune_layout* L, FtArgs a, const uint16_t* q, c
                     float* stat, hipStream_t s) {
   float* const key_partial = stat + 2 * a.N * a.Hq + (-2 * a.N * a.Hq & 3);  // (on 16 bytes)
   float* const query_partial = key_partial + (int64_t)L->slots * a.Hkv * KeyTile<NB>::PARTIAL;
-  ft_stream_dq_kernel<NB><<<dim3((unsigned)L->query_items.size() * a.Hq), 256, 0, s>>>(a, L->d_query_items, q, k, v, out, d_out, lse,
-                                                                                  stat, query_partial, dq);
-  ft_stream_dkv_kernel<NB><<<dim3((unsigned)L->items.size() * a.Hkv), 256, 0, s>>>(a, L->d_items, q, k, v, d_out, stat, key_partial,
-                                                                                dk, dv);
+  ft_stream_dq_kernel<NB><<<dim3((unsigned)hpd_ft_query_groups(L)), 256, 0, s>>>(a, L->d_query_items, q, k, v, out, d_out, lse, stat,
+                                                                             query_partial, dq);
+  ft_stream_dkv_kernel<NB><<<dim3((unsigned)hpd_ft_key_groups(L)), 256, 0, s>>>(a, L->d_items, q, k, v, d_out, stat, key_partial, dk, dv);
   const uint32_t n_key = (uint32_t)L->joins.size() * a.Hkv * 8, n_query = (uint32_t)L->query_joins.size() * a.Hq * 4;
   if (n_key + n_query)
     ft_stream_join_gradients_kernel<NB><<<dim3(n_key + n_query), 64 * NB, 0, s>>>(a, n_key, L->d_joins, L->d_query_joins, key_partial,

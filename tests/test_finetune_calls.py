@@ -1,8 +1,9 @@
 """What the calls of the fine-tuning operators refuse before a kernel is launched (CPU build of their host side with the
-launchers replaced, tests/native/finetune_calls_main.cpp)."""
+launchers replaced, tests/native/finetune_calls_main.cpp), and batches that no launch can hold."""
 import os
 import subprocess
 
+import numpy as np
 import pytest
 
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
@@ -20,3 +21,19 @@ def test_calls_are_run_or_refused_as_declared(tmp_path):
     assert build.returncode == 0, build.stderr[-3000:]
     run = subprocess.run([exe], capture_output=True, text=True, timeout=120)
     assert run.returncode == 0 and "as declared" in run.stdout, (run.stdout + run.stderr)[-2000:]
+
+
+@pytest.mark.parametrize("dtype, heads, most", [("f32", (32, 8), 2 ** 17 - 1), ("bf16", (32, 8), 2 ** 19 - 1),
+                                                ("f32", (16, 16), 2 ** 18 - 1), ("bf16", (16, 16), 2 ** 20 - 1)])
+def test_batches_of_more_sequences_than_a_launch_holds(dtype, heads, most):
+    """A launch has less than 2^32 threads: 256 for every sequence and query head at least, in fp32 1024.  The tokens are
+    few enough."""
+    from paper_2604_26209_amd import binding as B
+    cfg = B.hpd_finetune_config(*heads, 64, B.HPD_F32 if dtype == "f32" else B.HPD_BF16, 10000.0, 4, B.HPD_FLAG_HOST_ONLY)
+
+    def build(n):
+        return B.hpd_build_finetune_layout(cfg, np.ones(n, np.int32), np.zeros(n + 1, np.int32), [], [])
+    assert build(most).counts()[B.HPD_FTC_N_SEQ] == most
+    with pytest.raises(B.HpdError) as e:
+        build(most + 1)
+    assert e.value.status == B.HPD_E_OVERFLOW
