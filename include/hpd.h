@@ -449,8 +449,8 @@ enum hpd_finetune_count {
  *   attr_ptr   [n_seq+1]   CSR sequences -> attributes, attr_ptr[0] = 0, non-decreasing
  *   attr_len   [n_attr]    >= 1 tokens of the attribute's name
  *   value_len  [n_attr]    in [0, k_max] tokens of its value
- * A sequence may be empty.  HPD_E_OVERFLOW if a position exceeds 2^30, the number of tokens 2^25,
- * tokens times query heads 2^27, or if a launch would need 2^32 threads: 256 (HPD_F32: 1024) for every query
+ * A sequence may be empty.  HPD_E_OVERFLOW if a position or n_q_heads * head_dim exceeds 2^30, the number of
+ * tokens 2^25, tokens times query heads 2^27, or if a launch would need 2^32 threads: 256 (HPD_F32: 1024) for every query
  * head and 128 tokens of a sequence or part of them.
  */
 int hpd_build_finetune_layout(const hpd_finetune_config* cfg, int32_t n_seq, const int32_t* prompt_len,

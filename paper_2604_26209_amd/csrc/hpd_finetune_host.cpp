@@ -17,7 +17,7 @@ namespace {
     if (e_ != hipSuccess) return hpd_hip_fail(e_); \
   } while (0)
 
-constexpr int64_t LIMIT = (int64_t)1 << 30;      // positions, rows and columns of logits
+constexpr int64_t LIMIT = (int64_t)1 << 30;      // positions, a token's elements, rows and columns of logits
 constexpr int64_t MAX_TOKENS = (int64_t)1 << 25;
 constexpr int64_t MAX_ROWS = (int64_t)1 << 27;    // tokens times query heads
 constexpr int64_t MAX_THREADS = ((int64_t)1 << 32) - 1;  // of a launch
@@ -32,6 +32,7 @@ int validate(const hpd_finetune_config* c) {
   if (c->flags & ~HPD_FLAG_HOST_ONLY) return HPD_E_INVALID;
   if (c->dtype != HPD_F32 && c->dtype != HPD_BF16) return HPD_E_UNSUPPORTED;
   if (c->head_dim % 8 != 0 || c->head_dim > HPD_FINETUNE_MAX_DIM) return HPD_E_UNSUPPORTED;
+  if ((int64_t)c->n_q_heads * c->head_dim > LIMIT) return HPD_E_OVERFLOW;  // (a head's place in its token: 32 bits of bytes)
   return HPD_OK;
 }
 

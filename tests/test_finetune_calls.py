@@ -37,3 +37,17 @@ def test_batches_of_more_sequences_than_a_launch_holds(dtype, heads, most):
     with pytest.raises(B.HpdError) as e:
         build(most + 1)
     assert e.value.status == B.HPD_E_OVERFLOW
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_heads_of_a_token_beyond_32_bits(dtype):
+    """A head's place in its token is a 32-bit number of bytes or elements in the kernels."""
+    from paper_2604_26209_amd import binding as B
+
+    def build(heads):
+        cfg = B.hpd_finetune_config(heads, 1, 128, B.HPD_F32 if dtype == "f32" else B.HPD_BF16, 10000.0, 4, B.HPD_FLAG_HOST_ONLY)
+        return B.hpd_build_finetune_layout(cfg, [1], [0, 0], [], [])
+    assert build(2 ** 20).counts()[B.HPD_FTC_N_TOKENS] == 1
+    with pytest.raises(B.HpdError) as e:
+        build(2 ** 23 + 2 ** 10)
+    assert e.value.status == B.HPD_E_OVERFLOW
