@@ -7,9 +7,10 @@
 // results are joined by the same rule.  A k beyond 2^24 would not be whole, and its rounding not small: k starts at -2^22, below
 // which a logit counts nothing beside others, and where the largest logit of a wave's share is further from 0 than 2^21 (all
 // tokens excluded by a finite value, or a diverged row), the wave goes over it again with the maximum itself as
-// reference point, as a sum of two numbers.  The pass is bound by the bytes of the logits, with the vector instructions (an exponential
-// and five to six more per logit) close behind: 6144 x 130013 bf16 logits with one alternative 295 us, 5.4 TB/s; without 5.4,
-// with eight 4.0, with fifty 3.3 TB/s.
+// reference point, as a sum of two numbers (its cost: 256 x 32000 bf16 logits, half of every row excluded by -1e9: 26.5 -> 30 us;
+// nothing where every share has an ordinary logit).  The pass is bound by the bytes of the logits without alternatives, by
+// vector instructions with them: 6144 x 130013 bf16 logits, 290 us and 5.5 TB/s without (8.9 instructions a logit), with one
+// alternative 294 us and 5.4 TB/s (11.5), with eight 4.6, twenty 4.1, fifty 3.6 TB/s (16, 19, 22 instructions, busy all the time).
 //
 // Alternatives: a wave keeps its 64 largest (value, index) keys, lane i the i-th.  A vector of logits
 // costs one comparison of its maximum with the K-th; what passes is collected and sorted in, 64 at a time.
@@ -77,30 +78,32 @@ struct Sums {
 };
 template <bool WIDE>
 __device__ __forceinline__ Sums no_sums() { return {-INFINITY, WIDE ? LOWEST_REFERENCE : NARROW_START, 0.f, 0.f, 0.f}; }
-// raises the reference point to 4 (r + lo) >= 4 (a.r + a.lo)
+// raises the reference point to 4 (r + lo) >= 4 (a.r + a.lo); narrow: lo and a.lo are 0
+template <bool WIDE>
 __device__ __forceinline__ void raise(Sums& a, float r, float lo) {
-  const float d = fminf(4.f * ((r - a.r) + (lo - a.lo)), 1.0e4f), f = fast_exp2(-d);
+  const float d = fminf(4.f * (WIDE ? (r - a.r) + (lo - a.lo) : r - a.r), 1.0e4f), f = fast_exp2(-d);
   a.t = fmaf(-d, a.s, a.t) * f;
   a.s *= f;
   a.r = r;
   a.lo = lo;
 }
+// (what the largest logit of a wide share was does not matter any more)
+template <bool WIDE>
 __device__ __forceinline__ Sums join(Sums a, Sums b) {
   if (a.s == 0.f) a.r = LOWEST_REFERENCE;  // (nothing there: its reference point says nothing)
   if (b.s == 0.f) b.r = LOWEST_REFERENCE;
-  const bool first = a.r > b.r || (a.r == b.r && a.lo >= b.lo);
-  const float r = first ? a.r : b.r, lo = first ? a.lo : b.lo;
-  raise(a, r, lo);
-  raise(b, r, lo);
-  return {fmaxf(a.m, b.m), r, lo, a.s + b.s, a.t + b.t};
+  const bool first = WIDE && (a.r > b.r || (a.r == b.r && a.lo >= b.lo));
+  const float r = WIDE ? (first ? a.r : b.r) : fmaxf(a.r, b.r), lo = WIDE ? (first ? a.lo : b.lo) : 0.f;
+  raise<WIDE>(a, r, lo);
+  raise<WIDE>(b, r, lo);
+  return {WIDE ? a.m : fmaxf(a.m, b.m), r, lo, a.s + b.s, a.t + b.t};
 }
-// (lo is 0 in a narrow share; what a wide one's largest logit was does not matter any more)
 template <bool WIDE>
 __device__ __forceinline__ Sums join_wave(Sums a) {
 #pragma unroll
   for (int d = 32; d; d >>= 1)
-    a = join(a, {WIDE ? a.m : __shfl_xor(a.m, d), __shfl_xor(a.r, d), WIDE ? __shfl_xor(a.lo, d) : 0.f, __shfl_xor(a.s, d),
-                 __shfl_xor(a.t, d)});
+    a = join<WIDE>(a, {WIDE ? a.m : __shfl_xor(a.m, d), __shfl_xor(a.r, d), WIDE ? __shfl_xor(a.lo, d) : 0.f, __shfl_xor(a.s, d),
+                       __shfl_xor(a.t, d)});
   return a;
 }
 // (y - k) / 4 of a logit, rounded by its own size however far y and k are from 0
@@ -112,7 +115,7 @@ __device__ __forceinline__ void add_logits(Sums& a, const float* x, float m) {
   a.m = fmaxf(a.m, m);
   if constexpr (WIDE) {
     const float r = m * (0.25f * LOG2E), lo = fmaf(m, 0.25f * LOG2E, -r);
-    if (r > a.r || (r == a.r && lo > a.lo)) raise(a, r, lo);
+    if (r > a.r || (r == a.r && lo > a.lo)) raise<true>(a, r, lo);
 #pragma unroll
     for (int i = 0; i < N; ++i) {
       const float d = 4.f * quarter(x[i], a), e = fast_exp2(d);
@@ -121,7 +124,7 @@ __device__ __forceinline__ void add_logits(Sums& a, const float* x, float m) {
     }
   } else {
     const float y = m * LOG2E;
-    if (y > 4.f * a.r) raise(a, 0.25f * ceilf(y), 0.f);
+    if (y > 4.f * a.r) raise<false>(a, 0.25f * ceilf(y), 0.f);
     float low = x[0];
 #pragma unroll
     for (int i = 1; i < N; ++i) low = fminf(low, x[i]);
@@ -437,7 +440,7 @@ __global__ void __launch_bounds__(256) logprobs_kernel(hpd_logprobs_args a, int3
       if (wave == 0) {
 #pragma unroll
         for (int w = 1; w < 4; ++w) {
-          sums = join(sums, sh.sums[w]);
+          sums = join<true>(sums, sh.sums[w]);
           if (TOP) top.merge(sh.keys[w], lane);
         }
       }
