@@ -398,6 +398,8 @@ int hpd_finetune_mask(int32_t prompt_len, int32_t n_attr, const int32_t* attr_le
  * the query heads that share them.  Sums, softmax and gradients are accumulated in fp32; under
  * HPD_BF16 the probabilities and the scores' gradients are rounded to bf16 for the second
  * products, and every output is rounded once.  No atomics: equal calls give equal bits.
+ * A probability is relatively as good as its score and the row's log-sum-exp are in fp32, about 2^-23 times their
+ * magnitude; scores q . k / sqrt(D) of 2^24 and more in magnitude are not supported.
  * A non-finite element of a sequence can reach every output of its own sequence (a masked
  * probability is a zero factor), and no other sequence's.
  * The calls only enqueue kernels, allocate nothing and may be captured in a HIP graph.
@@ -493,6 +495,7 @@ int hpd_finetune_attention_backward(const hpd_finetune_layout* layout, const voi
  *   top_id     : device int32 [n_rows][top_k], top_logprob: fp32 [n_rows][top_k]; 0 <= top_k <=
  *                min(vocab, HPD_MAX_TOP)
  *   workspace  : device, the bytes that hpd_token_logprobs_workspace reports (NULL if 0), 16-byte aligned
+ * Finite logits may be of any size (tokens excluded by a finite value among them).
  * A logit of -infinity has probability 0.  A row of nothing else: lse and the log probabilities are
  * -infinity, entropy 0.  A row with a NaN or +infinity: lse, log probabilities and entropy are NaN.
  */
@@ -508,7 +511,9 @@ int hpd_token_logprobs_workspace(int32_t dtype, int64_t n_rows, int32_t vocab, i
  *   g_entropy : device fp32 [n_rows] or NULL (0)
  *   d_logits  : [n_rows] rows of vocab elements of the same dtype, d_stride elements apart; may be
  *               logits with d_stride = row_stride
- * A row whose logits are all -infinity has gradient 0.
+ * A row whose logits are all -infinity has gradient 0.  p = exp(x - lse) is relatively good to 2^-24 |lse|: where the
+ * largest logit is far from 0 (a row whose tokens are all excluded by a finite value such as -1e9) lse has no room for
+ * the logarithm of the sum, and the row needs gradients of 0 or, without g_entropy, a target outside [0, vocab).
  */
 int hpd_token_logprobs_backward(int32_t dtype, int64_t n_rows, int32_t vocab, int64_t row_stride, const void* logits,
                                 const int32_t* targets, const float* lse, const float* entropy, const float* g_logprob,

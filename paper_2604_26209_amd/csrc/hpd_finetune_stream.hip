@@ -7,6 +7,12 @@
 // 4 (r / 2 % 2) + (r / 4) % 4 for rows of 8.  So both ways of reading a tile spread over all banks:
 // one chunk of 16 successive rows (left operand of a score product), and the same 64 bytes of four
 // successive rows (transposing read, left operand of a second product).
+//
+// Scores, softmax, delta and all sums are fp32.  The weights p and the scores' gradients ds are rounded to bf16 (half a step: 2^-8 of
+// each) for the second products: the matrix instruction takes them in the type of the other operand, and value and
+// remainder as two operands would be 3/2 of the forward kernel's products, 4/3 of dq's and 3/2 of dk/dv's.  The relative error against 64
+// bits, in the root mean square, is 0.0019 to 0.0021 forward and 0.0024 to 0.0025 for the gradients, where rounding nothing but the
+// outputs leaves 0.0016 and 0.0018.
 #include "hpd_finetune_dev.h"
 
 namespace {
