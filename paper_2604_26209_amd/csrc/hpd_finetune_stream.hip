@@ -11,8 +11,8 @@
 // Scores, softmax, delta and all sums are fp32.  The weights p and the scores' gradients ds are rounded to bf16 (half a step: 2^-8 of
 // each) for the second products: the matrix instruction takes them in the type of the other operand, and value and
 // remainder as two operands would be 3/2 of the forward kernel's products, 4/3 of dq's and 3/2 of dk/dv's.  The relative error against 64
-// bits, in the root mean square, is 0.0019 to 0.0021 forward and 0.0024 to 0.0025 for the gradients, where rounding nothing but the
-// outputs leaves 0.0016 and 0.0018.
+// bits, in the root mean square, is 0.0019 to 0.0022 forward and 0.0024 to 0.0028 for the gradients, where rounding nothing but the
+// outputs leaves 0.0016 and 0.0018 to 0.0022 (batches of perf/operators.py).
 #include "hpd_finetune_dev.h"
 
 namespace {
