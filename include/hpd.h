@@ -519,6 +519,85 @@ int hpd_token_logprobs_backward(int32_t dtype, int64_t n_rows, int32_t vocab, in
                                 const int32_t* targets, const float* lse, const float* entropy, const float* g_logprob,
                                 const float* g_entropy, void* d_logits, int64_t d_stride, void* stream);
 
+/* ---------------------------------------------------------------------------------------------
+ * The two ends of a layer stack around the attention: the gated feed-forward block and the vocabulary head with the
+ * log probabilities of given tokens, for training (with their gradients) and for the tokens of a decode step (few rows).
+ *
+ * Tensors are device memory, rows of `width`, `inner` or vocab elements of the dtype; the distance between rows
+ * is a stride in elements.  They start on 16 bytes and strides are multiples of 16 bytes, up to 2^23 bytes; width and inner are
+ * multiples of 8 (HPD_E_UNSUPPORTED otherwise), vocab and the number of rows are free.  Weights lie as a linear layer keeps
+ * them, [outputs][inputs].
+ * Products are accumulated in fp32 and every output is rounded once.  Under HPD_BF16 what one product hands to the next
+ * (h; dg, du; the logits' gradients) is rounded to bf16, the type in which the matrix instruction takes it.
+ * No output may overlap an input or the workspace (HPD_E_INVALID where they start at the same address).
+ * No atomics: equal calls give equal bits.  A row's outputs depend on that row and the weights alone.
+ * The calls only enqueue kernels, allocate nothing and may be captured in a HIP graph.  Workspaces: device memory, the bytes
+ * that the _workspace call reports (NULL if 0), 16-byte aligned, not shared by calls that overlap.
+ */
+enum hpd_activation {
+  HPD_ACT_SILU = 0,     /* x / (1 + exp(-x)) */
+  HPD_ACT_GELU = 1,     /* x (1 + erf(x / sqrt 2)) / 2 */
+  HPD_ACT_GELU_TANH = 2 /* x (1 + tanh(sqrt(2 / pi) (x + 0.044715 x^3))) / 2 */
+};
+
+typedef struct hpd_ffn_config {
+  int32_t width; /* of x and out */
+  int32_t inner; /* of gate and up */
+  int32_t dtype; /* hpd_dtype of all tensors */
+  int32_t activation; /* hpd_activation */
+} hpd_ffn_config;
+
+/* Elements from one row to the next (0 = the rows lie next to each other).  A NULL pointer in a call is all zeros. */
+typedef struct hpd_ffn_strides {
+  int64_t x, out, gate, up, w_gate, w_up, w_down;
+  int64_t d_out, d_x, d_w_gate, d_w_up, d_w_down;
+} hpd_ffn_strides;
+
+/* hpd_gated_ffn - out = (act(g) * u) w_down^T, g = x w_gate^T, u = x w_up^T.
+ *   x, out [n_rows][width]; w_gate, w_up [inner][width]; w_down [width][inner]
+ *   gate, up : [n_rows][inner], receive g and u for the backward call; each may be NULL.  (Halves of one buffer, and of one
+ *              matrix of both projections, are given by pointers and strides.)
+ */
+int hpd_gated_ffn(const hpd_ffn_config* cfg, int64_t n_rows, const void* x, const void* w_gate, const void* w_up,
+                  const void* w_down, void* out, void* gate, void* up, void* workspace, const hpd_ffn_strides* strides,
+                  void* stream);
+
+/* hpd_gated_ffn_backward - gradients of x and of the weights, from d_out and from what the forward call has left in gate
+ * and up.  Each of d_x, d_w_gate, d_w_up, d_w_down may be NULL: that gradient is not made (frozen weights).  They are written, not
+ * added to; without rows those of the weights are zeros. */
+int hpd_gated_ffn_backward(const hpd_ffn_config* cfg, int64_t n_rows, const void* x, const void* w_gate, const void* w_up,
+                           const void* w_down, const void* gate, const void* up, const void* d_out, void* d_x, void* d_w_gate,
+                           void* d_w_up, void* d_w_down, void* workspace, const hpd_ffn_strides* strides, void* stream);
+
+/* Bytes of the two calls' workspaces (each pointer may be NULL). */
+int hpd_gated_ffn_workspace(const hpd_ffn_config* cfg, int64_t n_rows, int64_t* forward_bytes, int64_t* backward_bytes);
+
+/* hpd_head_logprobs - what hpd_token_logprobs gives for the logits x = hidden weight^T (fp32, never in memory), without
+ * alternatives.
+ *   hidden [n_rows][width], weight [vocab][width]
+ *   targets : device int32 [n_rows] or NULL (then logprob is not written); a row whose target is outside [0, vocab) has
+ *             logprob 0
+ *   logprob, lse, entropy : device fp32 [n_rows], each may be NULL
+ */
+int hpd_head_logprobs(int32_t dtype, int64_t n_rows, int32_t width, int32_t vocab, const void* hidden, int64_t hidden_stride,
+                      const void* weight, int64_t weight_stride, const int32_t* targets, float* logprob, float* lse,
+                      float* entropy, void* workspace, void* stream);
+
+/* hpd_head_logprobs_backward - gradients of hidden and weight for given gradients of log probability and entropy: with
+ *   d_c = g_logprob ([c = target] - p_c) - g_entropy p_c (log p_c + entropy),  p = exp(x - lse),
+ * d_hidden = d weight, d_weight = d^T hidden.  The logits are computed again, in pieces of the vocabulary.
+ *   lse, entropy (needed with g_entropy only) : as the forward call has left them
+ *   g_logprob, g_entropy : device fp32 [n_rows] or NULL (0); rows without a target inside [0, vocab) take 0 as g_logprob
+ *   d_hidden, d_weight : each may be NULL (not made); written, not added to; without rows d_weight is zeros
+ */
+int hpd_head_logprobs_backward(int32_t dtype, int64_t n_rows, int32_t width, int32_t vocab, const void* hidden,
+                               int64_t hidden_stride, const void* weight, int64_t weight_stride, const int32_t* targets,
+                               const float* lse, const float* entropy, const float* g_logprob, const float* g_entropy,
+                               void* d_hidden, int64_t d_hidden_stride, void* d_weight, int64_t d_weight_stride,
+                               void* workspace, void* stream);
+int hpd_head_logprobs_workspace(int32_t dtype, int64_t n_rows, int32_t width, int32_t vocab, int64_t* forward_bytes,
+                                int64_t* backward_bytes);
+
 /* Selects the attention kernel: 0 = automatic (bf16: as 2 where that is allowed; fp32 decode under
  * HPD_MASK_BLOCK with head_dim 32, 64 or 128, up to 16 query heads per kv head and pools that start on
  * 16 bytes: a kernel on the fp32 matrix instruction, or the generic one for the steps for which the layout

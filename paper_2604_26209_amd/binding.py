@@ -51,6 +51,7 @@ HPD_KEY_BLOCK = 32
  HPD_C_N_TAIL_SLOTS, HPD_C_MAX_POS, HPD_C_TOTAL_LIVE, HPD_N_COUNTS) = range(9)
 
 HPD_FINETUNE_MAX_DIM, HPD_MAX_TOP = 128, 64
+HPD_ACT_SILU, HPD_ACT_GELU, HPD_ACT_GELU_TANH = range(3)
 HPD_FTQ_COUNTS, HPD_FTQ_SEQ_OFF, HPD_FTQ_POS, HPD_FTQ_RANK = range(4)
 (HPD_FTC_N_SEQ, HPD_FTC_N_TOKENS, HPD_FTC_MAX_LEN, HPD_FTC_MAX_POS, HPD_FTC_FORWARD_BYTES,
  HPD_FTC_BACKWARD_BYTES, HPD_N_FT_COUNTS) = range(7)
@@ -62,7 +63,8 @@ EXPORTS = ["hpd_build_layout", "hpd_layout_free", "hpd_layout_query", "hpd_prefi
            "hpd_dynamic_state", "hpd_dynamic_read", "hpd_set_tail_pages", "hpd_dynamic_begin_static",
            "hpd_build_finetune_layout", "hpd_finetune_layout_free", "hpd_finetune_layout_query", "hpd_finetune_rotate",
            "hpd_finetune_attention", "hpd_finetune_attention_backward", "hpd_token_logprobs",
-           "hpd_token_logprobs_workspace", "hpd_token_logprobs_backward"]
+           "hpd_token_logprobs_workspace", "hpd_token_logprobs_backward", "hpd_gated_ffn", "hpd_gated_ffn_backward",
+           "hpd_gated_ffn_workspace", "hpd_head_logprobs", "hpd_head_logprobs_backward", "hpd_head_logprobs_workspace"]
 # include/hpd_peaks.h: reference kernels for the benchmark's measured peaks
 PEAK_EXPORTS = ["hpd_peak_read", "hpd_peak_copy", "hpd_peak_mfma"]
 
@@ -84,6 +86,16 @@ class hpd_finetune_config(ctypes.Structure):
 class hpd_finetune_strides(ctypes.Structure):
     """Elements between tokens; 0 = no gap."""
     _fields_ = [(_f, ctypes.c_int64) for _f in ("q", "k", "v", "q_out", "k_out", "v_out")]
+
+
+class hpd_ffn_config(ctypes.Structure):
+    _fields_ = [(_f, ctypes.c_int32) for _f in ("width", "inner", "dtype", "activation")]
+
+
+class hpd_ffn_strides(ctypes.Structure):
+    """Elements between rows; 0 = no gap."""
+    _fields_ = [(_f, ctypes.c_int64) for _f in ("x", "out", "gate", "up", "w_gate", "w_up", "w_down", "d_out", "d_x",
+                                                "d_w_gate", "d_w_up", "d_w_down")]
 
 
 _vp, _i32, _i64p = ctypes.c_void_p, ctypes.c_int32, ctypes.POINTER(ctypes.c_int64)
@@ -120,6 +132,13 @@ _lib.hpd_finetune_attention_backward.argtypes = [_vp] * 13
 _lib.hpd_token_logprobs.argtypes = [_i32, _i64, _i32, _i64, _vp, _vp, _i32] + [_vp] * 7
 _lib.hpd_token_logprobs_workspace.argtypes = [_i32, _i64, _i32, _i32, _i64p]
 _lib.hpd_token_logprobs_backward.argtypes = [_i32, _i64, _i32, _i64] + [_vp] * 7 + [_i64, _vp]
+_ffnp = ctypes.POINTER(hpd_ffn_config)
+_lib.hpd_gated_ffn.argtypes = [_ffnp, _i64] + [_vp] * 10
+_lib.hpd_gated_ffn_backward.argtypes = [_ffnp, _i64] + [_vp] * 14
+_lib.hpd_gated_ffn_workspace.argtypes = [_ffnp, _i64, _i64p, _i64p]
+_lib.hpd_head_logprobs.argtypes = [_i32, _i64, _i32, _i32, _vp, _i64, _vp, _i64] + [_vp] * 6
+_lib.hpd_head_logprobs_backward.argtypes = [_i32, _i64, _i32, _i32, _vp, _i64, _vp, _i64] + [_vp] * 6 + [_i64, _vp, _i64] + [_vp] * 2
+_lib.hpd_head_logprobs_workspace.argtypes = [_i32, _i64, _i32, _i32, _i64p, _i64p]
 _lib.hpd_peak_read.argtypes = [_vp, ctypes.c_size_t, _vp, _vp]
 _lib.hpd_peak_copy.argtypes = [_vp, _vp, ctypes.c_size_t, _vp]
 _lib.hpd_peak_mfma.argtypes = [_vp, _i32, ctypes.POINTER(ctypes.c_double), _vp]
@@ -448,6 +467,64 @@ def hpd_token_logprobs_backward(dtype, n_rows, vocab, row_stride, logits, target
                                             _ptr(targets), _ptr(lse), _ptr(entropy), _ptr(g_logprob), _ptr(g_entropy),
                                             _ptr(d_logits), int(d_stride), _stream(stream)),
            "hpd_token_logprobs_backward")
+
+
+def hpd_gated_ffn_workspace(cfg: hpd_ffn_config, n_rows):
+    """(bytes of hpd_gated_ffn's workspace, of the backward call's)."""
+    f, b = ctypes.c_int64(0), ctypes.c_int64(0)
+    _check(_lib.hpd_gated_ffn_workspace(ctypes.byref(cfg), int(n_rows), ctypes.byref(f), ctypes.byref(b)),
+           "hpd_gated_ffn_workspace")
+    return int(f.value), int(b.value)
+
+
+def alloc_ffn_workspace(cfg, n_rows, backward=True, device="cuda"):
+    """The workspace of hpd_gated_ffn, or of the backward call."""
+    n = hpd_gated_ffn_workspace(cfg, n_rows)[bool(backward)]
+    return torch.empty(n, dtype=torch.uint8, device=device) if n else None
+
+
+def hpd_gated_ffn(cfg, n_rows, x, w_gate, w_up, w_down, out, gate=None, up=None, workspace=None, strides=None, stream=None):
+    _check(_lib.hpd_gated_ffn(ctypes.byref(cfg), int(n_rows), _ptr(x), _ptr(w_gate), _ptr(w_up), _ptr(w_down), _ptr(out),
+                              _ptr(gate), _ptr(up), _ptr(workspace), _strides(strides), _stream(stream)), "hpd_gated_ffn")
+
+
+def hpd_gated_ffn_backward(cfg, n_rows, x, w_gate, w_up, w_down, gate, up, d_out, d_x=None, d_w_gate=None, d_w_up=None,
+                           d_w_down=None, workspace=None, strides=None, stream=None):
+    _check(_lib.hpd_gated_ffn_backward(ctypes.byref(cfg), int(n_rows), _ptr(x), _ptr(w_gate), _ptr(w_up), _ptr(w_down),
+                                       _ptr(gate), _ptr(up), _ptr(d_out), _ptr(d_x), _ptr(d_w_gate), _ptr(d_w_up),
+                                       _ptr(d_w_down), _ptr(workspace), _strides(strides), _stream(stream)),
+           "hpd_gated_ffn_backward")
+
+
+def hpd_head_logprobs_workspace(dtype, n_rows, width, vocab):
+    """(bytes of hpd_head_logprobs' workspace, of the backward call's)."""
+    f, b = ctypes.c_int64(0), ctypes.c_int64(0)
+    _check(_lib.hpd_head_logprobs_workspace(int(dtype), int(n_rows), int(width), int(vocab), ctypes.byref(f),
+                                            ctypes.byref(b)), "hpd_head_logprobs_workspace")
+    return int(f.value), int(b.value)
+
+
+def alloc_head_workspace(dtype, n_rows, width, vocab, backward=True, device="cuda"):
+    """The workspace of hpd_head_logprobs, or of the backward call."""
+    n = hpd_head_logprobs_workspace(dtype, n_rows, width, vocab)[bool(backward)]
+    return torch.empty(n, dtype=torch.uint8, device=device) if n else None
+
+
+def hpd_head_logprobs(dtype, n_rows, width, vocab, hidden, hidden_stride, weight, weight_stride, targets=None, logprob=None,
+                      lse=None, entropy=None, workspace=None, stream=None):
+    _check(_lib.hpd_head_logprobs(int(dtype), int(n_rows), int(width), int(vocab), _ptr(hidden), int(hidden_stride),
+                                  _ptr(weight), int(weight_stride), _ptr(targets), _ptr(logprob), _ptr(lse), _ptr(entropy),
+                                  _ptr(workspace), _stream(stream)), "hpd_head_logprobs")
+
+
+def hpd_head_logprobs_backward(dtype, n_rows, width, vocab, hidden, hidden_stride, weight, weight_stride, targets, lse,
+                               entropy, g_logprob, g_entropy, d_hidden=None, d_hidden_stride=0, d_weight=None,
+                               d_weight_stride=0, workspace=None, stream=None):
+    _check(_lib.hpd_head_logprobs_backward(int(dtype), int(n_rows), int(width), int(vocab), _ptr(hidden),
+                                           int(hidden_stride), _ptr(weight), int(weight_stride), _ptr(targets), _ptr(lse),
+                                           _ptr(entropy), _ptr(g_logprob), _ptr(g_entropy), _ptr(d_hidden),
+                                           int(d_hidden_stride), _ptr(d_weight), int(d_weight_stride), _ptr(workspace),
+                                           _stream(stream)), "hpd_head_logprobs_backward")
 
 
 def hpd_peak_read(src, nbytes, sink, stream=None):

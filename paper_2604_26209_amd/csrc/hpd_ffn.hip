@@ -1,0 +1,166 @@
+// The gated feed-forward block and its gradient:
+//   g = x Wg^T, u = x Wu^T, h = act(g) u, out = h Wd^T
+//   dh = dout Wd, dg = dh u act'(g), du = dh act(g)
+//   dx = dg Wg + du Wu, dWg = dg^T x, dWu = du^T x, dWd = dout^T h
+// Forward: one kernel for both projections, activation and product (a tile has the same features of g and u by turns, in
+// the same wave), one for the second product.  Backward: one for dh and what follows from it element by element (dg, du and, for
+// dWd, h again), one for dx (one contraction over dg and du in turn), one for dWg and dWu together, one for dWd.
+#include "hpd_ffn.h"
+#include "hpd_product.h"
+
+namespace {
+
+using Tiles = Shape<128, 128, 2, 2, 2, 2>;
+
+// act(g) and its derivative
+template <typename T, int ACT>
+__device__ __forceinline__ void activation(float g, float& a, float& slope) {
+  if constexpr (ACT == HPD_ACT_GELU) {
+    const float c = sizeof(T) == 2 ? 0.5f + 0.5f * erff(g * 0.70710678118654752f) : 0.5f * erfcf(g * -0.70710678118654752f);
+    a = g * c;
+    slope = fmaf(g * 0.39894228040143268f, expf(-0.5f * g * g), c);
+  } else {
+    // silu: g / (1 + exp(-g)); gelu by tanh: g (1 + tanh w) / 2 = g / (1 + exp(-2 w)), w = sqrt(2 / pi) (g + 0.044715 g^3)
+    // (the logistic function is 0 or 1 long before |g| = 30, and g^3 stays finite)
+    const float c = fminf(fmaxf(g, -30.f), 30.f);
+    const float w = ACT == HPD_ACT_SILU ? g : 1.5957691216057308f * c * fmaf(0.044715f * c, c, 1.f);
+    const float s = 1.f / (1.f + expf(-w));
+    a = g * s;
+    const float dw = ACT == HPD_ACT_SILU ? 1.f : 1.5957691216057308f * fmaf(0.134145f * c, c, 1.f);
+    slope = fmaf(g * s * (1.f - s), dw, s);
+  }
+}
+
+template <typename T, int ACT>
+struct Activate {
+  T *h, *gate, *up;  // gate and up may be NULL
+  int64_t inner, rows, gate_stride, up_stride;
+  template <typename S, int MI, int NI>
+  __device__ __forceinline__ void operator()(floatx16 (&acc)[MI][NI], const Place& at, char*) const {
+    const int l = at.lane & 31, half = at.lane >> 5;
+#pragma unroll
+    for (int j = 0; j < NI; ++j) {
+      const int64_t row = at.row + 32 * j + l;
+      if (row >= rows) continue;
+#pragma unroll
+      for (int i = 0; i < MI; i += 2)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const int64_t m = at.feature + 16 * i + 8 * q + 4 * half;
+          if (m >= inner) continue;
+          float g[4], u[4], v[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            float slope;
+            g[e] = acc[i][j][4 * q + e];
+            u[e] = acc[i + 1][j][4 * q + e];
+            activation<T, ACT>(g[e], v[e], slope);
+            v[e] *= u[e];
+          }
+          store4(h + row * inner + m, v);
+          if (gate) store4(gate + row * gate_stride + m, g);
+          if (up) store4(up + row * up_stride + m, u);
+        }
+    }
+  }
+};
+
+// from dh: dg and du next to each other, h if it is wanted
+template <typename T, int ACT>
+struct InnerGradients {
+  const T *gate, *up;
+  T *d_inner, *h;
+  int64_t inner, rows, gate_stride, up_stride;
+  template <typename S, int MI, int NI>
+  __device__ __forceinline__ void operator()(floatx16 (&acc)[MI][NI], const Place& at, char*) const {
+    each4<MI, NI>(acc, at, inner, rows, [&](int64_t row, int64_t m, const float* dh) {
+      float g[4], u[4], dg[4], du[4], v[4];
+      fetch4(gate + row * gate_stride + m, g);
+      fetch4(up + row * up_stride + m, u);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        float a, slope;
+        activation<T, ACT>(g[e], a, slope);
+        v[e] = a * u[e];
+        dg[e] = dh[e] * u[e] * slope;
+        du[e] = dh[e] * a;
+      }
+      store4(d_inner + row * 2 * inner + m, dg);
+      store4(d_inner + row * 2 * inner + inner + m, du);
+      if (h) store4(h + row * inner + m, v);
+    });
+  }
+};
+
+int64_t round16(int64_t x) { return (x + 15) / 16 * 16; }
+
+template <typename T>
+hpd_operand operand(const void* p, int64_t stride, int64_t size, const void* second = nullptr) {
+  return {{p, second ? second : p}, stride * (int64_t)sizeof(T), (int32_t)size};
+}
+
+template <typename T, int ACT>
+hipError_t forward(const hpd_ffn_forward_args& a, hipStream_t s) {
+  const int64_t D = a.cfg.width, F = a.cfg.inner, N = a.n_rows;
+  T* const h = (T*)a.workspace;
+  const hpd_product_args in = {operand<T>(a.w_gate, a.st.w_gate, F, a.w_up), operand<T>(a.x, a.st.x, N), (int32_t)D, 1, 1, 0, 0};
+  const Activate<T, ACT> act = {h, (T*)a.gate, (T*)a.up, F, N, a.st.gate, a.st.up};
+  hipError_t e = launch_product<T, BY_ROWS, BY_ROWS, true, Tiles>(in, act, s);
+  if (e != hipSuccess) return e;
+  const hpd_product_args down = {operand<T>(a.w_down, a.st.w_down, D), operand<T>(h, F, N), (int32_t)F, 1, 1, 0, 0};
+  const StoreProduct<T> store = {{(T*)a.out, nullptr}, {a.st.out, 0}, N, D, N};
+  return launch_product<T, BY_ROWS, BY_ROWS, false, Tiles>(down, store, s);
+}
+
+template <typename T, int ACT>
+hipError_t backward(const hpd_ffn_backward_args& a, hipStream_t s) {
+  const int64_t D = a.cfg.width, F = a.cfg.inner, N = a.n_rows;
+  T* const d_inner = (T*)a.workspace;
+  T* const h = (T*)(a.workspace + round16(N * 2 * F * (int64_t)sizeof(T)));
+  hipError_t e = hipSuccess;
+  if (N > 0) {
+    const hpd_product_args g = {operand<T>(a.w_down, a.st.w_down, F), operand<T>(a.d_out, a.st.d_out, N), (int32_t)D, 1, 1, 0, 0};
+    const InnerGradients<T, ACT> grad = {(const T*)a.gate, (const T*)a.up, d_inner, a.d_w_down ? h : nullptr, F, N, a.st.gate, a.st.up};
+    e = launch_product<T, BY_COLUMNS, BY_ROWS, false, Tiles>(g, grad, s);
+  }
+  if (e == hipSuccess && a.d_x && N > 0) {
+    const hpd_product_args g = {operand<T>(a.w_gate, a.st.w_gate, D, a.w_up), operand<T>(d_inner, 2 * F, N, d_inner + F), (int32_t)F, 2, 1, 0, 0};
+    const StoreProduct<T> store = {{(T*)a.d_x, nullptr}, {a.st.d_x, 0}, N, D, N};
+    e = launch_product<T, BY_COLUMNS, BY_ROWS, false, Tiles>(g, store, s);
+  }
+  if (e == hipSuccess && (a.d_w_gate || a.d_w_up)) {  // (no rows: zeros)
+    // rows of the result: the gate's features, then the up projection's
+    const int64_t skip = a.d_w_gate ? 0 : F, rows = (a.d_w_gate ? F : 0) + (a.d_w_up ? F : 0);
+    const hpd_product_args g = {operand<T>(a.x, a.st.x, D), operand<T>(d_inner + skip, 2 * F, rows), (int32_t)N, 1, 1, 0, 0};
+    const StoreProduct<T> store = {{(T*)(skip ? a.d_w_up : a.d_w_gate), (T*)a.d_w_up},
+                                   {skip ? a.st.d_w_up : a.st.d_w_gate, a.st.d_w_up}, F, D, rows};
+    e = launch_product<T, BY_COLUMNS, BY_COLUMNS, false, Tiles>(g, store, s);
+  }
+  if (e == hipSuccess && a.d_w_down) {
+    const hpd_product_args g = {operand<T>(h, F, F), operand<T>(a.d_out, a.st.d_out, D), (int32_t)N, 1, 1, 0, 0};
+    const StoreProduct<T> store = {{(T*)a.d_w_down, nullptr}, {a.st.d_w_down, 0}, D, F, D};
+    e = launch_product<T, BY_COLUMNS, BY_COLUMNS, false, Tiles>(g, store, s);
+  }
+  return e;
+}
+
+int64_t elem_bytes(int32_t dtype) { return dtype == HPD_F32 ? 4 : 2; }
+
+}  // namespace
+
+int64_t hpd_ffn_forward_bytes(const hpd_ffn_config& cfg, int64_t n_rows) {
+  return round16(n_rows * cfg.inner * elem_bytes(cfg.dtype));
+}
+int64_t hpd_ffn_backward_bytes(const hpd_ffn_config& cfg, int64_t n_rows) {
+  return round16(n_rows * 2 * cfg.inner * elem_bytes(cfg.dtype)) + round16(n_rows * cfg.inner * elem_bytes(cfg.dtype));
+}
+
+#define BY_TYPE(call)                                                                                              \
+  (a.cfg.dtype == HPD_F32 ? (a.cfg.activation == HPD_ACT_SILU   ? call<float, HPD_ACT_SILU>(a, s)                  \
+                             : a.cfg.activation == HPD_ACT_GELU ? call<float, HPD_ACT_GELU>(a, s)                  \
+                                                                : call<float, HPD_ACT_GELU_TANH>(a, s))            \
+                          : (a.cfg.activation == HPD_ACT_SILU   ? call<hpd::bf16_t, HPD_ACT_SILU>(a, s)            \
+                             : a.cfg.activation == HPD_ACT_GELU ? call<hpd::bf16_t, HPD_ACT_GELU>(a, s)            \
+                                                                : call<hpd::bf16_t, HPD_ACT_GELU_TANH>(a, s)))
+hipError_t hpd_launch_ffn(const hpd_ffn_forward_args& a, hipStream_t s) { return BY_TYPE(forward); }
+hipError_t hpd_launch_ffn_backward(const hpd_ffn_backward_args& a, hipStream_t s) { return BY_TYPE(backward); }

@@ -1,0 +1,230 @@
+// Log probabilities of given tokens from hidden states and the vocabulary's weights, and their gradients; the logits
+// x = hidden W^T stay in registers.
+//
+// Forward: a tile's rows give (m, s, t) = (max x, sum e^(x - m), sum e^(x - m) (x - m)) of its tokens of the vocabulary; a
+// second kernel joins a row's tiles: lse = m + log s, entropy = log s - t / s.  The maximum is subtracted before anything is scaled, so
+// that logits of any finite size keep the accuracy that they have.
+// Backward: piece by piece of the vocabulary, the logits again and from them dx_c = g ([c = target] - p) - ge p (log p + entropy),
+// rounded to the inputs' type; then the piece's rows of dW = dx^T hidden, and its part of dhidden = dx W in fp32.
+#include <algorithm>
+
+#include "hpd_ffn.h"
+#include "hpd_product.h"
+
+namespace {
+
+using Tiles = Shape<128, 128, 2, 2, 2, 2>;
+constexpr float LOG2E = 1.44269504088896340736f;
+
+struct Sums {
+  float m, s, t;
+};
+// (a part without logits above -infinity: m = -infinity, s = 0)
+__device__ __forceinline__ Sums join(Sums a, Sums b) {
+  const float m = fmaxf(a.m, b.m);
+  const float da = a.s == 0.f ? 0.f : fmaxf(a.m - m, -1e4f), db = b.s == 0.f ? 0.f : fmaxf(b.m - m, -1e4f);
+  const float fa = fast_exp2(da * LOG2E), fb = fast_exp2(db * LOG2E);
+  return {m, fmaf(a.s, fa, b.s * fb), fmaf(da, a.s, a.t) * fa + fmaf(db, b.s, b.t) * fb};
+}
+
+// what the forward product leaves of a row and a tile of the vocabulary
+struct RowSums {
+  const int32_t* targets;
+  float* of_target;  // [rows]: the target's logit (written by the tile that has it)
+  float4* parts;     // [rows][tiles]
+  int32_t vocab, tiles;
+  int64_t rows;
+  template <typename S, int MI, int NI>
+  __device__ __forceinline__ void operator()(floatx16 (&acc)[MI][NI], const Place& at, char* smem) const {
+    const int l = at.lane & 31, h = at.lane >> 5;
+    __syncthreads();  // (the operands' stages make room)
+    float4* const shared = reinterpret_cast<float4*>(smem);  // [WM][BN]
+#pragma unroll
+    for (int j = 0; j < NI; ++j) {
+      const int64_t row = at.row + 32 * j + l;
+      const int32_t target = targets && row < rows ? targets[row] : -1;
+      const int32_t mine = target - (int32_t)at.feature;
+      Sums a = {-INFINITY, 0.f, 0.f};
+#pragma unroll
+      for (int i = 0; i < MI; ++i)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          const int m = 32 * i + block_row(r, h);
+          if (at.feature + m >= vocab) acc[i][j][r] = -INFINITY;
+          a.m = fmaxf(a.m, acc[i][j][r]);
+          if (mine == m && target < vocab) of_target[row] = acc[i][j][r];
+        }
+      // +infinity and NaN (which fmaxf passes over) make s NaN
+      const float m = a.m == -INFINITY ? 0.f : a.m;
+#pragma unroll
+      for (int i = 0; i < MI; ++i)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          const float d = acc[i][j][r] - m, e = fast_exp2(d * LOG2E);
+          a.s += e;
+          a.t = fmaf(e, d < -1e4f ? 0.f : d, a.t);
+        }
+      a = join(a, {__shfl_xor(a.m, 32), __shfl_xor(a.s, 32), __shfl_xor(a.t, 32)});
+      if (h == 0) shared[at.wave_m * S::BN + (at.wave_n * NI + j) * 32 + l] = make_float4(a.m, a.s, a.t, 0.f);
+    }
+    __syncthreads();
+    const int64_t first = at.row - at.wave_n * NI * 32;
+    for (int n = threadIdx.x; n < S::BN; n += 64 * S::WAVES) {
+      if (first + n >= rows) continue;
+      Sums a = {-INFINITY, 0.f, 0.f};
+#pragma unroll
+      for (int w = 0; w < S::WM; ++w) {
+        const float4 v = shared[w * S::BN + n];
+        a = w ? join(a, {v.x, v.y, v.z}) : Sums{v.x, v.y, v.z};
+      }
+      parts[(first + n) * tiles + at.tile_m] = make_float4(a.m, a.s, a.t, 0.f);
+    }
+  }
+};
+
+// one wave per row
+__global__ void __launch_bounds__(256) join_rows_kernel(const float4* parts, int32_t tiles, int64_t rows, const float* of_target,
+                                                        const int32_t* targets, int32_t vocab, float* logprob, float* lse,
+                                                        float* entropy) {
+  const int lane = threadIdx.x & 63;
+  const int64_t row = blockIdx.x * 4ll + (threadIdx.x >> 6);
+  if (row >= rows) return;
+  Sums a = {-INFINITY, 0.f, 0.f};
+  for (int32_t i = lane; i < tiles; i += 64) {
+    const float4 v = parts[row * tiles + i];
+    a = join(a, {v.x, v.y, v.z});
+  }
+#pragma unroll
+  for (int d = 32; d; d >>= 1) a = join(a, {__shfl_xor(a.m, d), __shfl_xor(a.s, d), __shfl_xor(a.t, d)});
+  if (lane) return;
+  const float log_s = logf(a.s), total = a.s == 0.f ? -INFINITY : a.m + log_s;
+  if (lse) lse[row] = total;
+  if (entropy) entropy[row] = a.s == 0.f ? 0.f : log_s - a.t / a.s;
+  if (logprob && targets) {
+    const int32_t t = targets[row];
+    float v = 0.f;
+    if (t >= 0 && t < vocab) v = a.s == 0.f ? -INFINITY : (of_target[row] - a.m) - log_s;
+    logprob[row] = v;
+  }
+}
+
+// the logits' gradients of a piece of the vocabulary, [rows][stride], zeros from vocab up to stride
+template <typename T>
+struct LogitGradients {
+  const int32_t* targets;
+  const float *lse, *entropy, *g_logprob, *g_entropy;
+  T* out;
+  int64_t stride, rows;
+  int32_t first, vocab;  // of the piece, in it
+  int32_t whole;         // tokens of the whole vocabulary
+  template <typename S, int MI, int NI>
+  __device__ __forceinline__ void operator()(floatx16 (&acc)[MI][NI], const Place& at, char*) const {
+    const int l = at.lane & 31, h = at.lane >> 5;
+#pragma unroll
+    for (int j = 0; j < NI; ++j) {
+      const int64_t row = at.row + 32 * j + l;
+      if (row >= rows) continue;
+      const int32_t t = targets ? targets[row] : -1, target = t < 0 ? -1 : t - first;
+      const float L = lse[row];
+      const float ge = g_entropy && L != -INFINITY ? g_entropy[row] : 0.f, H = g_entropy ? entropy[row] : 0.f;
+      float g = g_logprob ? g_logprob[row] : 0.f;
+      if (t < 0 || t >= whole || L == -INFINITY) g = 0.f;
+#pragma unroll
+      for (int i = 0; i < MI; ++i)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const int64_t m = at.feature + 32 * i + 8 * q + 4 * h;
+          if (m >= stride) continue;
+          float v[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const float lp = acc[i][j][4 * q + e] - L, p = L == -INFINITY ? 0.f : fast_exp2(lp * LOG2E);
+            float d = -p * (p > 0.f ? fmaf(ge, lp + H, g) : g);
+            if (m + e == target) d += g;
+            v[e] = m + e < vocab ? d : 0.f;
+          }
+          store4(out + row * stride + m, v);
+        }
+    }
+  }
+};
+
+int64_t round16(int64_t x) { return (x + 15) / 16 * 16; }
+int64_t elem_bytes(int32_t dtype) { return dtype == HPD_F32 ? 4 : 2; }
+
+template <typename T>
+hpd_operand operand(const void* p, int64_t stride, int64_t size) {
+  return {{p, p}, stride * (int64_t)sizeof(T), (int32_t)size};
+}
+
+int64_t vocab_tiles(int32_t vocab) { return (vocab + Tiles::BM - 1) / Tiles::BM; }
+
+// Pieces of the vocabulary: their gradients take at most 256 MB or so.
+int64_t piece_of(int32_t dtype, int64_t n_rows, int32_t vocab) {
+  const int64_t most = std::max<int64_t>(Tiles::BM, ((int64_t)256 << 20) / (std::max<int64_t>(n_rows, 1) * elem_bytes(dtype)) / Tiles::BM * Tiles::BM);
+  const int64_t pieces = (vocab + most - 1) / most;
+  return ((vocab + pieces - 1) / pieces + Tiles::BM - 1) / Tiles::BM * Tiles::BM;
+}
+
+template <typename T>
+hipError_t forward(const hpd_head_args& a, hipStream_t s) {
+  const int64_t tiles = vocab_tiles(a.vocab);
+  float4* const parts = (float4*)a.workspace;
+  float* const of_target = (float*)(a.workspace + a.n_rows * tiles * (int64_t)sizeof(float4));
+  const hpd_product_args g = {operand<T>(a.weight, a.weight_stride, a.vocab), operand<T>(a.hidden, a.hidden_stride, a.n_rows),
+                              a.width, 1, 1, 0, 0};
+  const int32_t* const targets = a.logprob ? a.targets : nullptr;
+  hipError_t e = launch_product<T, BY_ROWS, BY_ROWS, false, Tiles>(g, RowSums{targets, of_target, parts, a.vocab, (int32_t)tiles, a.n_rows}, s);
+  if (e != hipSuccess) return e;
+  join_rows_kernel<<<dim3((uint32_t)((a.n_rows + 3) / 4)), dim3(256), 0, s>>>(parts, (int32_t)tiles, a.n_rows, of_target, targets, a.vocab,
+                                                                             a.logprob, a.lse, a.entropy);
+  return hipGetLastError();
+}
+
+template <typename T>
+hipError_t backward(const hpd_head_backward_args& a, hipStream_t s) {
+  const int64_t N = a.n_rows, D = a.width, piece = piece_of(a.dtype, N, a.vocab);
+  T* const dx = (T*)a.workspace;
+  float* const part = (float*)(a.workspace + round16(N * piece * (int64_t)sizeof(T)));
+  hipError_t e = hipSuccess;
+  for (int64_t v0 = 0; v0 < a.vocab && e == hipSuccess; v0 += piece) {
+    const int64_t n = std::min<int64_t>(piece, a.vocab - v0);
+    const T* const w = (const T*)a.weight + v0 * a.weight_stride;
+    if (N > 0) {
+      const hpd_product_args g = {operand<T>(w, a.weight_stride, n), operand<T>(a.hidden, a.hidden_stride, N), (int32_t)D, 1, 1, 0, 0};
+      e = launch_product<T, BY_ROWS, BY_ROWS, false, Tiles>(
+          g, LogitGradients<T>{a.targets, a.lse, a.entropy, a.g_logprob, a.g_entropy, dx, piece, N, (int32_t)v0, (int32_t)n, a.vocab}, s);
+    }
+    if (e == hipSuccess && a.d_hidden && N > 0) {
+      const hpd_product_args g = {operand<T>(w, a.weight_stride, D), operand<T>(dx, piece, N), (int32_t)n, 1, 1, 0, 0};
+      e = launch_product<T, BY_COLUMNS, BY_ROWS, false, Tiles>(g, StorePart{part, D, N, v0 > 0}, s);
+    }
+    if (e == hipSuccess && a.d_weight) {  // (no rows: zeros)
+      const hpd_product_args g = {operand<T>(a.hidden, a.hidden_stride, D), operand<T>(dx, piece, n), (int32_t)N, 1, 1, 0, 0};
+      const StoreProduct<T> store = {{(T*)a.d_weight + v0 * a.d_weight_stride, nullptr}, {a.d_weight_stride, 0}, n, D, n};
+      e = launch_product<T, BY_COLUMNS, BY_COLUMNS, false, Tiles>(g, store, s);
+    }
+  }
+  if (e == hipSuccess && a.d_hidden && N > 0) {
+    const int64_t all = N * D / 4;
+    join_parts_kernel<T><<<dim3((uint32_t)std::min<int64_t>((all + 255) / 256, 1 << 16)), dim3(256), 0, s>>>(
+        part, 1, D, N, (T*)a.d_hidden, a.d_hidden_stride);
+    e = hipGetLastError();
+  }
+  return e;
+}
+
+}  // namespace
+
+int64_t hpd_head_forward_bytes(int32_t, int64_t n_rows, int32_t, int32_t vocab) {
+  return round16(n_rows * vocab_tiles(vocab) * (int64_t)sizeof(float4) + n_rows * 4);
+}
+int64_t hpd_head_backward_bytes(int32_t dtype, int64_t n_rows, int32_t width, int32_t vocab) {
+  return round16(n_rows * piece_of(dtype, n_rows, vocab) * elem_bytes(dtype)) + n_rows * width * 4;
+}
+hipError_t hpd_launch_head(const hpd_head_args& a, hipStream_t s) {
+  return a.dtype == HPD_F32 ? forward<float>(a, s) : forward<hpd::bf16_t>(a, s);
+}
+hipError_t hpd_launch_head_backward(const hpd_head_backward_args& a, hipStream_t s) {
+  return a.dtype == HPD_F32 ? backward<float>(a, s) : backward<hpd::bf16_t>(a, s);
+}

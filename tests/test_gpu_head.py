@@ -1,0 +1,249 @@
+"""Log probabilities from hidden states and the vocabulary's weights through the library, and their gradients, against the
+definitions in 64 bits."""
+import pytest
+import torch
+
+import ffn_ref as R
+from paper_2604_26209_amd import binding as B
+from test_gpu_ffn import DT, TD, Padded
+
+pytestmark = pytest.mark.gpu
+
+SIZES = [(1, 8, 1), (1, 64, 7), (3, 72, 129), (33, 136, 1000), (64, 256, 4099), (65, 64, 127), (130, 480, 1025), (257, 512, 128),
+         (300, 128, 2051)]
+
+
+def _inputs(rows, width, vocab, dtype, seed=0, scale=2.5):
+    gen = torch.Generator().manual_seed(seed)
+    w = (torch.randn((vocab, width), generator=gen) * scale * width ** -0.5).to(TD[dtype])
+    t = torch.randint(0, vocab, (rows,), generator=gen, dtype=torch.int32)
+    x = torch.randn((rows, width), generator=gen) + torch.rand((rows, 1), generator=gen) * 2 * w[t.long()].float()
+    t[5::7] = -1
+    t[6::11] = vocab
+    g, ge = (torch.randn(rows, generator=gen).cuda() for _ in range(2))
+    return dict(x=x.to(TD[dtype]).cuda(), w=w.cuda(), t=t.cuda(), g=g, ge=ge)
+
+
+def _forward(i, dtype, pad=8):
+    (rows, width), vocab = i["x"].shape, i["w"].shape[0]
+    x, w = (Padded(*i[k].shape, TD[dtype], i[k], pad) for k in ("x", "w"))
+    outs = [torch.full((rows + 2,), 77.0, device="cuda") for _ in range(3)]
+    ws = B.alloc_head_workspace(DT[dtype], rows, width, vocab, backward=False)
+    B.hpd_head_logprobs(DT[dtype], rows, width, vocab, x.t, x.t.stride(0), w.t, w.t.stride(0), i["t"],
+                        *[o[1:rows + 1] for o in outs], ws)
+    torch.cuda.synchronize()
+    assert all(o[0] == 77.0 and o[-1] == 77.0 for o in outs)
+    return [o[1:rows + 1] for o in outs]
+
+
+def _backward(i, dtype, lse, entropy, g=True, ge=True, hidden=True, weight=True, pad=8):
+    (rows, width), vocab = i["x"].shape, i["w"].shape[0]
+    x, w = (Padded(*i[k].shape, TD[dtype], i[k], pad) for k in ("x", "w"))
+    dx, dw = Padded(rows, width, TD[dtype], pad=pad), Padded(vocab, width, TD[dtype], pad=pad)
+    ws = B.alloc_head_workspace(DT[dtype], rows, width, vocab, backward=True)
+    if ws is not None:
+        ws.fill_(0xff)  # (NaN in both types)
+    B.hpd_head_logprobs_backward(DT[dtype], rows, width, vocab, x.t, x.t.stride(0), w.t, w.t.stride(0), i["t"], lse,
+                                 entropy if ge else None, i["g"] if g else None, i["ge"] if ge else None,
+                                 dx.t if hidden else None, dx.t.stride(0), dw.t if weight else None, dw.t.stride(0), ws)
+    torch.cuda.synchronize()
+    assert dx.untouched() and dw.untouched()
+    assert hidden or bool((dx.buf == 31744.0).all())
+    assert weight or bool((dw.buf == 31744.0).all())
+    return dx.t, dw.t
+
+
+def _check(i, dtype, ge=True):
+    x, w = i["x"].double(), i["w"].double()
+    got = _forward(i, dtype)
+    for name, a, want in zip(("logprob", "lse", "entropy"), got, R.head(x, w, i["t"])):
+        R.check(a, want, name)
+    _, lse, entropy = got
+    want = R.head_grad(x, w, i["t"], lse.double(), entropy.double(), i["g"].double(), i["ge"].double() if ge else None, TD[dtype])
+    for name, a, b in zip(("d_hidden", "d_weight"), _backward(i, dtype, lse, entropy, ge=ge), want):
+        R.check(a, b, name)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows, width, vocab", SIZES)
+@pytest.mark.parametrize("ge", [True, False])
+def test_head(rows, width, vocab, dtype, ge):
+    _check(_inputs(rows, width, vocab, dtype), dtype, ge)
+
+
+# large vocabularies in several pieces, many rows, few rows
+@pytest.mark.parametrize("dtype, rows, width, vocab", [("bf16", 2, 1152, 50021), ("bf16", 700, 256, 130013), ("f32", 300, 136, 50021),
+                                                       ("bf16", 3001, 512, 9001), ("bf16", 40, 4096, 12003), ("bf16", 4100, 72, 33000)])
+def test_larger(dtype, rows, width, vocab):
+    _check(_inputs(rows, width, vocab, dtype, seed=1), dtype)
+
+
+@pytest.mark.parametrize("hidden, weight, g, ge", [(1, 0, 1, 1), (0, 1, 1, 1), (1, 1, 0, 1), (1, 1, 1, 0), (1, 1, 0, 0)])
+def test_parts_that_are_not_wanted(hidden, weight, g, ge):
+    i = _inputs(70, 136, 500, "bf16", seed=2)
+    _, lse, entropy = _forward(i, "bf16")
+    want = R.head_grad(i["x"].double(), i["w"].double(), i["t"], lse.double(), entropy.double(), i["g"].double() if g else None,
+                       i["ge"].double() if ge else None, torch.bfloat16)
+    dx, dw = _backward(i, "bf16", lse, entropy, g, ge, hidden, weight)
+    if hidden:
+        R.check(dx, want[0], "d_hidden")
+    if weight:
+        R.check(dw, want[1], "d_weight")
+
+
+def test_outputs_that_are_not_wanted():
+    i = _inputs(70, 136, 500, "bf16", seed=3)
+    want = _forward(i, "bf16")
+    rows, width, vocab = 70, 136, 500
+    ws = B.alloc_head_workspace(B.HPD_BF16, rows, width, vocab, backward=False)
+    for n in range(3):
+        outs = [torch.empty(rows, device="cuda") if k == n else None for k in range(3)]
+        B.hpd_head_logprobs(B.HPD_BF16, rows, width, vocab, i["x"], width, i["w"], width, i["t"], *outs, ws)
+        assert torch.equal(outs[n], want[n])
+    lse = torch.empty(rows, device="cuda")
+    untouched = torch.full((rows,), 5.0, device="cuda")
+    B.hpd_head_logprobs(B.HPD_BF16, rows, width, vocab, i["x"], width, i["w"], width, None, untouched, lse, None, ws)
+    assert torch.equal(lse, want[1]) and bool((untouched == 5.0).all())
+
+
+def test_no_rows():
+    i = _inputs(0, 64, 40, "bf16")
+    _forward(i, "bf16")
+    none = torch.empty(1, device="cuda")
+    dx, dw = _backward(i, "bf16", none, none)
+    assert bool((dw == 0).all())
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows", [5, 150])
+def test_rows_that_are_not_finite(rows, dtype):
+    """+infinity and NaN among a row's logits: NaN in that row alone.  -infinity: a token of probability 0."""
+    width, vocab = 72, 300
+    i = _inputs(rows, width, vocab, dtype, seed=4)
+    i["t"][3] = 7
+    i["x"][:, 0] = 1.0
+    i["w"][:, 0] = 0.0
+    clean = [t.clone() for t in _forward(i, dtype)]
+    keep = torch.arange(rows, device="cuda") != 3
+    for bad in (float("nan"), float("inf")):
+        j = dict(i, x=i["x"].clone())
+        j["x"][3, 5] = bad
+        got = _forward(j, dtype)
+        for a, b in zip(got, clean):
+            assert torch.equal(a[keep], b[keep]) and bool(torch.isnan(a[3]))
+        dx, dw = _backward(j, dtype, got[1], got[2])
+        ref, _ = _backward(i, dtype, clean[1], clean[2])
+        assert torch.equal(dx[keep], ref[keep]) and bool(torch.isnan(dx[3]).all())
+    # an excluded token: its weights times a channel that is 1 in every row give -infinity
+    j = dict(i, w=i["w"].clone())
+    j["w"][17, 0] = float("-inf")
+    j["t"][2] = 17
+    logits = j["x"].double() @ i["w"].double().T
+    logits[:, 17] = float("-inf")
+    got = _forward(j, dtype)
+    e = width * R.U * (j["x"].double().abs() @ i["w"].double().abs().T)
+    for name, a, want in zip(("logprob", "lse", "entropy"), got, R.logprobs(logits, j["t"], e)):
+        value, bound = want
+        gone = torch.isinf(value)
+        assert torch.equal(a.double()[gone], value[gone])
+        R.check(a[~gone], (value[~gone], bound[~gone]), name)
+    # rows of nothing else
+    j["w"] = j["w"][17:18].clone()
+    j["t"] = torch.zeros_like(j["t"])
+    logprob, lse, entropy = _forward(j, dtype)
+    assert bool((lse == float("-inf")).all() and (logprob == float("-inf")).all() and (entropy == 0).all())
+
+
+@pytest.mark.parametrize("scale", [1e-3, 100.0, 3e4, 1e15])
+def test_logits_of_any_size(scale):
+    i = _inputs(40, 64, 700, "f32", seed=5, scale=scale)
+    for name, a, want in zip(("logprob", "lse", "entropy"), _forward(i, "f32"), R.head(i["x"].double(), i["w"].double(), i["t"])):
+        R.check(a, want, name)
+
+
+@pytest.mark.parametrize("rows", [3, 200])
+def test_equal_calls_give_equal_bits_on_any_stream_and_in_a_graph(rows):
+    width, vocab = 264, 5003
+    i = _inputs(rows, width, vocab, "bf16", seed=6)
+    outs = [torch.empty(rows, device="cuda") for _ in range(3)]
+    dx, dw = torch.empty_like(i["x"]), torch.empty_like(i["w"])
+    ws = [B.alloc_head_workspace(B.HPD_BF16, rows, width, vocab, b) for b in (False, True)]
+
+    def step():
+        B.hpd_head_logprobs(B.HPD_BF16, rows, width, vocab, i["x"], width, i["w"], width, i["t"], *outs, ws[0])
+        B.hpd_head_logprobs_backward(B.HPD_BF16, rows, width, vocab, i["x"], width, i["w"], width, i["t"], outs[1], outs[2], i["g"],
+                                     i["ge"], dx, width, dw, width, ws[1])
+
+    def results():
+        torch.cuda.synchronize()
+        return [t.clone() for t in (*outs, dx, dw)]
+
+    def forget():
+        for t in (*outs, dx, dw):
+            t.fill_(float("nan"))
+
+    step()
+    want = results()
+    forget()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.current_stream().wait_stream(side)
+    assert all(torch.equal(a, b) for a, b in zip(results(), want))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    x = i["x"].clone()
+    for n in range(4):
+        forget()
+        i["x"].copy_(x if n % 2 == 0 else x * 0.5)
+        graph.replay()
+        got = results()
+        forget()
+        step()
+        assert all(torch.equal(a, b) for a, b in zip(got, results())), n
+
+
+def test_the_same_as_from_stored_logits():
+    """hpd_token_logprobs on logits in fp32 gives the same numbers."""
+    i = _inputs(50, 136, 3001, "f32", seed=7)
+    got = _forward(i, "f32")
+    logits = (i["x"].double() @ i["w"].double().T).float()
+    outs = [torch.empty(50, device="cuda") for _ in range(3)]
+    ws = torch.empty(max(1, B.hpd_token_logprobs_workspace(B.HPD_F32, 50, 3001, 0)), dtype=torch.uint8, device="cuda")
+    B.hpd_token_logprobs(B.HPD_F32, 50, 3001, 3001, logits, i["t"], 0, *outs, None, None, ws)
+    # both within the bound of the definition
+    for a, b, (_, bound) in zip(got, outs, R.head(i["x"].double(), i["w"].double(), i["t"])):
+        assert bool(((a.double() - b.double()).abs() <= 2 * bound + 1e-37).all())
+
+
+def test_weights_behind_4_gb():
+    """Rows of weights further than 2^32 bytes from the first, in pieces and at once."""
+    rows, width, vocab = 4, 16384, 140001
+    gen = torch.Generator(device="cuda").manual_seed(8)
+    w = torch.zeros((vocab, width), dtype=torch.bfloat16, device="cuda")
+    far = torch.tensor([0, 1, 70000, 131071, 131072, 131073, 139999, 140000], device="cuda")
+    w[far] = (torch.randn((8, width), generator=gen, device="cuda") * width ** -0.5).bfloat16()
+    x = torch.randn((rows, width), generator=gen, device="cuda").bfloat16()
+    t = torch.tensor([140000, 131072, 3, 0], dtype=torch.int32, device="cuda")
+    outs = [torch.empty(rows, device="cuda") for _ in range(3)]
+    ws = B.alloc_head_workspace(B.HPD_BF16, rows, width, vocab, False)
+    B.hpd_head_logprobs(B.HPD_BF16, rows, width, vocab, x, width, w, width, t, *outs, ws)
+    logits = torch.zeros((rows, vocab), dtype=torch.float64, device="cuda")
+    logits[:, far] = x.double() @ w[far].double().T
+    e = torch.zeros_like(logits)
+    e[:, far] = width * R.U * (x.double().abs() @ w[far].double().abs().T)
+    for name, a, want in zip(("logprob", "lse", "entropy"), outs, R.logprobs(logits, t, e)):
+        R.check(a, want, name)
+    g = torch.ones(rows, device="cuda")
+    dx, dw = torch.empty_like(x), torch.empty_like(w)
+    ws = B.alloc_head_workspace(B.HPD_BF16, rows, width, vocab, True)
+    B.hpd_head_logprobs_backward(B.HPD_BF16, rows, width, vocab, x, width, w, width, t, outs[1], None, g, None, dx, width, dw, width, ws)
+    p = torch.exp(logits - outs[1].double()[:, None])
+    d = -p
+    d[torch.arange(rows, device="cuda"), t.long()] += 1
+    want = d[:, far] @ w[far].double()
+    assert bool(((dx.double() - want).abs() <= 2.0 ** -7 * (d[:, far].abs() @ w[far].double().abs()) + 1e-30).all())
+    want = d[:, far].T @ x.double()
+    assert bool(((dw[far].double() - want).abs() <= 2.0 ** -6 * (d[:, far].abs().T @ x.double().abs())).all())
