@@ -10,8 +10,6 @@
 
 namespace {
 
-using Tiles = Shape<128, 128, 2, 2, 2, 2>;
-
 // act(g) and its derivative
 template <typename T, int ACT>
 __device__ __forceinline__ void activation(float g, float& a, float& slope) {
@@ -92,6 +90,8 @@ struct InnerGradients {
   }
 };
 
+constexpr int MOST_SPLITS = 16;  // of a contraction over the inner width
+
 int64_t round16(int64_t x) { return (x + 15) / 16 * 16; }
 
 template <typename T>
@@ -99,34 +99,63 @@ hpd_operand operand(const void* p, int64_t stride, int64_t size, const void* sec
   return {{p, second ? second : p}, stride * (int64_t)sizeof(T), (int32_t)size};
 }
 
+int64_t part_bytes(Plan p, int64_t rows, int64_t features) { return p.splits > 1 ? p.splits * rows * features * 4 : 0; }
+
+// How the products are made, and where the workspace has what they leave for each other.
+template <typename T>
+struct ForwardPlan {
+  Plan in, down;
+  int64_t parts, bytes;
+  ForwardPlan(const hpd_ffn_config& c, int64_t n) {
+    in = plan_product<T>(c.inner, n, c.width, true, 1);
+    down = plan_product<T>(c.width, n, c.inner, false, MOST_SPLITS);
+    parts = round16(n * c.inner * (int64_t)sizeof(T));
+    bytes = parts + part_bytes(down, n, c.width);
+  }
+};
+template <typename T>
+struct BackwardPlan {
+  Plan inner, dx, in_weights, down_weights;
+  int64_t h, parts, bytes;
+  BackwardPlan(const hpd_ffn_config& c, int64_t n) {
+    inner = plan_product<T>(c.inner, n, c.width, false, 1);
+    dx = plan_product<T>(c.width, n, 2 * (int64_t)c.inner, false, MOST_SPLITS);
+    in_weights = plan_product<T>(c.width, 2 * (int64_t)c.inner, n, false, 1, 3);
+    down_weights = plan_product<T>(c.inner, c.width, n, false, 1, 3);
+    h = round16(n * 2 * c.inner * (int64_t)sizeof(T));
+    parts = h + round16(n * c.inner * (int64_t)sizeof(T));
+    bytes = parts + part_bytes(dx, n, c.width);
+  }
+};
+
 template <typename T, int ACT>
 hipError_t forward(const hpd_ffn_forward_args& a, hipStream_t s) {
   const int64_t D = a.cfg.width, F = a.cfg.inner, N = a.n_rows;
+  const ForwardPlan<T> plan(a.cfg, N);
   T* const h = (T*)a.workspace;
   const hpd_product_args in = {operand<T>(a.w_gate, a.st.w_gate, F, a.w_up), operand<T>(a.x, a.st.x, N), (int32_t)D, 1, 1, 0, 0};
   const Activate<T, ACT> act = {h, (T*)a.gate, (T*)a.up, F, N, a.st.gate, a.st.up};
-  hipError_t e = launch_product<T, BY_ROWS, BY_ROWS, true, Tiles>(in, act, s);
+  const hipError_t e = launch_product<T, BY_ROWS, BY_ROWS, true>(plan.in, in, act, s);
   if (e != hipSuccess) return e;
   const hpd_product_args down = {operand<T>(a.w_down, a.st.w_down, D), operand<T>(h, F, N), (int32_t)F, 1, 1, 0, 0};
-  const StoreProduct<T> store = {{(T*)a.out, nullptr}, {a.st.out, 0}, N, D, N};
-  return launch_product<T, BY_ROWS, BY_ROWS, false, Tiles>(down, store, s);
+  return store_product<T, BY_ROWS, BY_ROWS>(plan.down, down, (float*)(a.workspace + plan.parts), (T*)a.out, a.st.out, s);
 }
 
 template <typename T, int ACT>
 hipError_t backward(const hpd_ffn_backward_args& a, hipStream_t s) {
   const int64_t D = a.cfg.width, F = a.cfg.inner, N = a.n_rows;
+  const BackwardPlan<T> plan(a.cfg, N);
   T* const d_inner = (T*)a.workspace;
-  T* const h = (T*)(a.workspace + round16(N * 2 * F * (int64_t)sizeof(T)));
+  T* const h = (T*)(a.workspace + plan.h);
   hipError_t e = hipSuccess;
   if (N > 0) {
     const hpd_product_args g = {operand<T>(a.w_down, a.st.w_down, F), operand<T>(a.d_out, a.st.d_out, N), (int32_t)D, 1, 1, 0, 0};
     const InnerGradients<T, ACT> grad = {(const T*)a.gate, (const T*)a.up, d_inner, a.d_w_down ? h : nullptr, F, N, a.st.gate, a.st.up};
-    e = launch_product<T, BY_COLUMNS, BY_ROWS, false, Tiles>(g, grad, s);
+    e = launch_product<T, BY_COLUMNS, BY_ROWS, false>(plan.inner, g, grad, s);
   }
   if (e == hipSuccess && a.d_x && N > 0) {
     const hpd_product_args g = {operand<T>(a.w_gate, a.st.w_gate, D, a.w_up), operand<T>(d_inner, 2 * F, N, d_inner + F), (int32_t)F, 2, 1, 0, 0};
-    const StoreProduct<T> store = {{(T*)a.d_x, nullptr}, {a.st.d_x, 0}, N, D, N};
-    e = launch_product<T, BY_COLUMNS, BY_ROWS, false, Tiles>(g, store, s);
+    e = store_product<T, BY_COLUMNS, BY_ROWS>(plan.dx, g, (float*)(a.workspace + plan.parts), (T*)a.d_x, a.st.d_x, s);
   }
   if (e == hipSuccess && (a.d_w_gate || a.d_w_up)) {  // (no rows: zeros)
     // rows of the result: the gate's features, then the up projection's
@@ -134,25 +163,23 @@ hipError_t backward(const hpd_ffn_backward_args& a, hipStream_t s) {
     const hpd_product_args g = {operand<T>(a.x, a.st.x, D), operand<T>(d_inner + skip, 2 * F, rows), (int32_t)N, 1, 1, 0, 0};
     const StoreProduct<T> store = {{(T*)(skip ? a.d_w_up : a.d_w_gate), (T*)a.d_w_up},
                                    {skip ? a.st.d_w_up : a.st.d_w_gate, a.st.d_w_up}, F, D, rows};
-    e = launch_product<T, BY_COLUMNS, BY_COLUMNS, false, Tiles>(g, store, s);
+    e = launch_product<T, BY_COLUMNS, BY_COLUMNS, false>(plan.in_weights, g, store, s);
   }
   if (e == hipSuccess && a.d_w_down) {
     const hpd_product_args g = {operand<T>(h, F, F), operand<T>(a.d_out, a.st.d_out, D), (int32_t)N, 1, 1, 0, 0};
     const StoreProduct<T> store = {{(T*)a.d_w_down, nullptr}, {a.st.d_w_down, 0}, D, F, D};
-    e = launch_product<T, BY_COLUMNS, BY_COLUMNS, false, Tiles>(g, store, s);
+    e = launch_product<T, BY_COLUMNS, BY_COLUMNS, false>(plan.down_weights, g, store, s);
   }
   return e;
 }
 
-int64_t elem_bytes(int32_t dtype) { return dtype == HPD_F32 ? 4 : 2; }
-
 }  // namespace
 
 int64_t hpd_ffn_forward_bytes(const hpd_ffn_config& cfg, int64_t n_rows) {
-  return round16(n_rows * cfg.inner * elem_bytes(cfg.dtype));
+  return cfg.dtype == HPD_F32 ? ForwardPlan<float>(cfg, n_rows).bytes : ForwardPlan<hpd::bf16_t>(cfg, n_rows).bytes;
 }
 int64_t hpd_ffn_backward_bytes(const hpd_ffn_config& cfg, int64_t n_rows) {
-  return round16(n_rows * 2 * cfg.inner * elem_bytes(cfg.dtype)) + round16(n_rows * cfg.inner * elem_bytes(cfg.dtype));
+  return cfg.dtype == HPD_F32 ? BackwardPlan<float>(cfg, n_rows).bytes : BackwardPlan<hpd::bf16_t>(cfg, n_rows).bytes;
 }
 
 #define BY_TYPE(call)                                                                                              \

@@ -13,7 +13,6 @@
 
 namespace {
 
-using Tiles = Shape<128, 128, 2, 2, 2, 2>;
 constexpr float LOG2E = 1.44269504088896340736f;
 
 struct Sums {
@@ -149,78 +148,100 @@ struct LogitGradients {
   }
 };
 
+constexpr int MOST_SPLITS = 32;                      // of a contraction over a piece of the vocabulary
+constexpr int64_t PIECE_BYTES = (int64_t)256 << 20;  // of the logits' gradients of a piece, about
+
 int64_t round16(int64_t x) { return (x + 15) / 16 * 16; }
-int64_t elem_bytes(int32_t dtype) { return dtype == HPD_F32 ? 4 : 2; }
 
 template <typename T>
 hpd_operand operand(const void* p, int64_t stride, int64_t size) {
   return {{p, p}, stride * (int64_t)sizeof(T), (int32_t)size};
 }
 
-int64_t vocab_tiles(int32_t vocab) { return (vocab + Tiles::BM - 1) / Tiles::BM; }
-
-// Pieces of the vocabulary: their gradients take at most 256 MB or so.
-int64_t piece_of(int32_t dtype, int64_t n_rows, int32_t vocab) {
-  const int64_t most = std::max<int64_t>(Tiles::BM, ((int64_t)256 << 20) / (std::max<int64_t>(n_rows, 1) * elem_bytes(dtype)) / Tiles::BM * Tiles::BM);
-  const int64_t pieces = (vocab + most - 1) / most;
-  return ((vocab + pieces - 1) / pieces + Tiles::BM - 1) / Tiles::BM * Tiles::BM;
-}
+// How the products are made, and where the workspace has what they leave for each other.
+template <typename T>
+struct ForwardPlan {
+  Plan product;
+  int64_t tiles, of_target, bytes;
+  ForwardPlan(int64_t n, int32_t width, int32_t vocab) {
+    product = plan_product<T>(vocab, n, width, false, 1);
+    tiles = (vocab + product.bm() - 1) / product.bm();
+    of_target = n * tiles * (int64_t)sizeof(float4);
+    bytes = round16(of_target + n * 4);
+  }
+};
+template <typename T>
+struct BackwardPlan {
+  int64_t piece;  // tokens of the vocabulary, a multiple of a tile's
+  Plan logits, d_hidden, d_weight;
+  int64_t parts, bytes;
+  BackwardPlan(int64_t n, int32_t width, int32_t vocab) {
+    constexpr int64_t UNIT = 256;
+    const int64_t most = std::max(UNIT, PIECE_BYTES / (std::max<int64_t>(n, 1) * (int64_t)sizeof(T)) / UNIT * UNIT);
+    const int64_t pieces = (vocab + most - 1) / most;
+    piece = ((vocab + pieces - 1) / pieces + UNIT - 1) / UNIT * UNIT;
+    logits = plan_product<T>(std::min<int64_t>(piece, vocab), n, width, false, 1);
+    d_hidden = plan_product<T>(width, n, std::min<int64_t>(piece, vocab), false, MOST_SPLITS);
+    d_weight = plan_product<T>(width, std::min<int64_t>(piece, vocab), n, false, 1, 3);
+    parts = round16(n * piece * (int64_t)sizeof(T));
+    bytes = parts + d_hidden.splits * n * width * 4;
+  }
+};
 
 template <typename T>
 hipError_t forward(const hpd_head_args& a, hipStream_t s) {
-  const int64_t tiles = vocab_tiles(a.vocab);
+  const ForwardPlan<T> plan(a.n_rows, a.width, a.vocab);
+  const int32_t tiles = (int32_t)plan.tiles;
   float4* const parts = (float4*)a.workspace;
-  float* const of_target = (float*)(a.workspace + a.n_rows * tiles * (int64_t)sizeof(float4));
+  float* const of_target = (float*)(a.workspace + plan.of_target);
   const hpd_product_args g = {operand<T>(a.weight, a.weight_stride, a.vocab), operand<T>(a.hidden, a.hidden_stride, a.n_rows),
                               a.width, 1, 1, 0, 0};
   const int32_t* const targets = a.logprob ? a.targets : nullptr;
-  hipError_t e = launch_product<T, BY_ROWS, BY_ROWS, false, Tiles>(g, RowSums{targets, of_target, parts, a.vocab, (int32_t)tiles, a.n_rows}, s);
+  const hipError_t e = launch_product<T, BY_ROWS, BY_ROWS, false>(plan.product, g, RowSums{targets, of_target, parts, a.vocab, tiles, a.n_rows}, s);
   if (e != hipSuccess) return e;
-  join_rows_kernel<<<dim3((uint32_t)((a.n_rows + 3) / 4)), dim3(256), 0, s>>>(parts, (int32_t)tiles, a.n_rows, of_target, targets, a.vocab,
-                                                                             a.logprob, a.lse, a.entropy);
+  join_rows_kernel<<<dim3((uint32_t)((a.n_rows + 3) / 4)), dim3(256), 0, s>>>(parts, tiles, a.n_rows, of_target, targets, a.vocab, a.logprob,
+                                                                             a.lse, a.entropy);
   return hipGetLastError();
 }
 
 template <typename T>
 hipError_t backward(const hpd_head_backward_args& a, hipStream_t s) {
-  const int64_t N = a.n_rows, D = a.width, piece = piece_of(a.dtype, N, a.vocab);
+  const int64_t N = a.n_rows, D = a.width;
+  const BackwardPlan<T> plan(N, a.width, a.vocab);
+  const int64_t piece = plan.piece;
   T* const dx = (T*)a.workspace;
-  float* const part = (float*)(a.workspace + round16(N * piece * (int64_t)sizeof(T)));
+  float* const parts = (float*)(a.workspace + plan.parts);
   hipError_t e = hipSuccess;
   for (int64_t v0 = 0; v0 < a.vocab && e == hipSuccess; v0 += piece) {
     const int64_t n = std::min<int64_t>(piece, a.vocab - v0);
     const T* const w = (const T*)a.weight + v0 * a.weight_stride;
     if (N > 0) {
       const hpd_product_args g = {operand<T>(w, a.weight_stride, n), operand<T>(a.hidden, a.hidden_stride, N), (int32_t)D, 1, 1, 0, 0};
-      e = launch_product<T, BY_ROWS, BY_ROWS, false, Tiles>(
-          g, LogitGradients<T>{a.targets, a.lse, a.entropy, a.g_logprob, a.g_entropy, dx, piece, N, (int32_t)v0, (int32_t)n, a.vocab}, s);
+      e = launch_product<T, BY_ROWS, BY_ROWS, false>(
+          plan.logits, g,
+          LogitGradients<T>{a.targets, a.lse, a.entropy, a.g_logprob, a.g_entropy, dx, piece, N, (int32_t)v0, (int32_t)n, a.vocab}, s);
     }
     if (e == hipSuccess && a.d_hidden && N > 0) {
       const hpd_product_args g = {operand<T>(w, a.weight_stride, D), operand<T>(dx, piece, N), (int32_t)n, 1, 1, 0, 0};
-      e = launch_product<T, BY_COLUMNS, BY_ROWS, false, Tiles>(g, StorePart{part, D, N, v0 > 0}, s);
+      e = launch_product<T, BY_COLUMNS, BY_ROWS, false>(plan.d_hidden, g, StorePart{parts, D, N, v0 > 0}, s);
     }
     if (e == hipSuccess && a.d_weight) {  // (no rows: zeros)
       const hpd_product_args g = {operand<T>(a.hidden, a.hidden_stride, D), operand<T>(dx, piece, n), (int32_t)N, 1, 1, 0, 0};
       const StoreProduct<T> store = {{(T*)a.d_weight + v0 * a.d_weight_stride, nullptr}, {a.d_weight_stride, 0}, n, D, n};
-      e = launch_product<T, BY_COLUMNS, BY_COLUMNS, false, Tiles>(g, store, s);
+      e = launch_product<T, BY_COLUMNS, BY_COLUMNS, false>(plan.d_weight, g, store, s);
     }
   }
-  if (e == hipSuccess && a.d_hidden && N > 0) {
-    const int64_t all = N * D / 4;
-    join_parts_kernel<T><<<dim3((uint32_t)std::min<int64_t>((all + 255) / 256, 1 << 16)), dim3(256), 0, s>>>(
-        part, 1, D, N, (T*)a.d_hidden, a.d_hidden_stride);
-    e = hipGetLastError();
-  }
+  if (e == hipSuccess && a.d_hidden && N > 0) e = join_parts(parts, plan.d_hidden.splits, D, N, (T*)a.d_hidden, a.d_hidden_stride, s);
   return e;
 }
 
 }  // namespace
 
-int64_t hpd_head_forward_bytes(int32_t, int64_t n_rows, int32_t, int32_t vocab) {
-  return round16(n_rows * vocab_tiles(vocab) * (int64_t)sizeof(float4) + n_rows * 4);
+int64_t hpd_head_forward_bytes(int32_t dtype, int64_t n_rows, int32_t width, int32_t vocab) {
+  return dtype == HPD_F32 ? ForwardPlan<float>(n_rows, width, vocab).bytes : ForwardPlan<hpd::bf16_t>(n_rows, width, vocab).bytes;
 }
 int64_t hpd_head_backward_bytes(int32_t dtype, int64_t n_rows, int32_t width, int32_t vocab) {
-  return round16(n_rows * piece_of(dtype, n_rows, vocab) * elem_bytes(dtype)) + n_rows * width * 4;
+  return dtype == HPD_F32 ? BackwardPlan<float>(n_rows, width, vocab).bytes : BackwardPlan<hpd::bf16_t>(n_rows, width, vocab).bytes;
 }
 hipError_t hpd_launch_head(const hpd_head_args& a, hipStream_t s) {
   return a.dtype == HPD_F32 ? forward<float>(a, s) : forward<hpd::bf16_t>(a, s);

@@ -20,6 +20,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <algorithm>
+
 #include "hpd_attn_bf16.h"
 
 struct hpd_operand {
@@ -111,14 +113,12 @@ struct Tile {
       }
     }
   }
-  // the stage's load i to LDS; left: contracted elements from the stage's first on (< STAGE_K: the last stage)
+  // the stage's load i to LDS; left: contracted elements from the stage's first on
   __device__ __forceinline__ void load(int i, uint32_t lds, int32x4 b0, int32x4 b1, int wave, int lane, int left) const {
     const int f = wave * LOADS + i;
     uint32_t o = off[i];
-    if (left < STAGE_K<T>) {
-      const int k = FORM == BY_ROWS ? chunk_of(f, lane) * CHUNK<T> : k_of(f, lane);
-      if (k >= left) o = OUTSIDE;
-    }
+    const int k = FORM == BY_ROWS ? chunk_of(f, lane) * CHUNK<T> : k_of(f, lane);
+    if (k >= left) o = OUTSIDE;
     load_to_lds(__builtin_amdgcn_readfirstlane(lds + f * 1024), o, DUAL && (f >> 2 & 1) ? b1 : b0);
   }
 };
@@ -178,6 +178,11 @@ struct Shape {
   static constexpr int WAVES = WM * WN, MI = BM / 32 / WM, NI = BN / 32 / WN;
   static constexpr int STAGE_BYTES = (BM + BN) * 128;
 };
+using Large = Shape<256, 256, 2, 2, 2, 1>;
+using Middle = Shape<128, 128, 2, 2, 2, 2>;
+using Few64 = Shape<64, 64, 1, 1, 3, 3>;
+using Few32 = Shape<64, 32, 1, 1, 3, 4>;
+enum { LARGE = 0, MIDDLE = 1, FEW64 = 2, FEW32 = 3 };
 
 // The place of a wave's blocks: features feature + 32 i (dual: block i is half i % 2 of features feature + 32 (i / 2)), rows row + 32 j.
 struct Place {
@@ -229,18 +234,26 @@ __global__ void __launch_bounds__(64 * S::WAVES, (S::WGS * S::WAVES + 3) / 4) pr
   const int32_t begin = (int32_t)((int64_t)total * split / g.splits), end = (int32_t)((int64_t)total * (split + 1) / g.splits);
   const uint32_t lds = product_lds(smem);
 
-  auto load_stage = [&](int32_t t, int slot) {
+  // A stage's loads, by the piece: of the wave's LOADS, load i.  A stage behind the last has buffers without bytes: zeros into
+  // its place in LDS, and as many loads to wait for as ever.
+  struct Stage {
+    int32x4 a, a1, b;
+    uint32_t at;
+    int left;
+  };
+  auto stage_of = [&](int32_t t, int slot) -> Stage {
     const bool second = !DUAL && t >= of_segment;
     const int32_t u = second ? t - of_segment : t;
-    const int32_t left = g.k - u * K;
-    const int32x4 ba = buffer_of((second ? pa[1] : pa[0]) + u * step_a);
-    const int32x4 ba1 = DUAL ? buffer_of(pa[1] + u * step_a) : ba;
-    const int32x4 bb = buffer_of((second ? pb[1] : pb[0]) + u * step_b);
-    const uint32_t at = lds + slot * S::STAGE_BYTES;
-#pragma unroll
-    for (int i = 0; i < TA::LOADS; ++i) ta.load(i, at, ba, ba1, wave, lane, left);
-#pragma unroll
-    for (int i = 0; i < TB::LOADS; ++i) tb.load(i, at + TA::BYTES, bb, bb, wave, lane, left);
+    Stage st = {buffer_of((second ? pa[1] : pa[0]) + u * step_a), buffer_of(pa[1] + u * step_a),
+                buffer_of((second ? pb[1] : pb[0]) + u * step_b), lds + slot * S::STAGE_BYTES, g.k - u * K};
+    if (t >= end) st.a[2] = st.a1[2] = st.b[2] = 0;
+    return st;
+  };
+  auto load = [&](const Stage& st, int i) {
+    if (i < TA::LOADS)
+      ta.load(i, st.at, st.a, st.a1, wave, lane, st.left);
+    else
+      tb.load(i - TA::LOADS, st.at + TA::BYTES, st.b, st.b, wave, lane, st.left);
   };
 
   Reader<T, FA, S::BM> ra;
@@ -255,60 +268,65 @@ __global__ void __launch_bounds__(64 * S::WAVES, (S::WGS * S::WAVES + 3) / 4) pr
 #pragma unroll
       for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.f;
 
-  for (int s = 0; s < S::STAGES; ++s)
-    if (begin + s < end) load_stage(begin + s, s);
-  // stage t is there for all waves; every wave has read what it needs of the stage before
-  auto arrive = [&](int32_t t) {
-    if (S::STAGES > 2 && t + S::STAGES - 2 < end)
-      wait_loads<LOADS * (S::STAGES > 2 ? S::STAGES - 2 : 0)>();
-    else
-      wait_loads<0>();
-    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-    __builtin_amdgcn_s_barrier();
-    asm volatile("" ::: "memory");
-  };
   product_u4 fa[2][MI], fb[2][NI];
-  auto read_step = [&](uint32_t at, int step, int to) {
-#pragma unroll
-    for (int i = 0; i < MI; ++i) fa[to][i] = ra.read(at, i, step);
-#pragma unroll
-    for (int j = 0; j < NI; ++j) fb[to][j] = rb.read(at + TA::BYTES, j, step);
+  // operand i of a step's MI + NI
+  auto read = [&](uint32_t at, int step, int to, int i) {
+    if (i < NI)
+      fb[to][i] = rb.read(at + TA::BYTES, i, step);
+    else
+      fa[to][i - NI] = ra.read(at, i - NI, step);
   };
-  auto products = [&](int of) {
+  // the products of a step, between(n) after the n-th of `BLOCKS`
+  constexpr int BLOCKS = MI * NI, READS = MI + NI;
+  auto products = [&](int of, auto between) {
 #pragma unroll
     for (int i = 0; i < MI; ++i)
 #pragma unroll
-      for (int j = 0; j < NI; ++j) acc[i][j] = multiply<T>(fa[of][i], fb[of][j], acc[i][j]);
+      for (int j = 0; j < NI; ++j) {
+        acc[i][j] = multiply<T>(fa[of][i], fb[of][j], acc[i][j]);
+        between(i * NI + j);
+        __builtin_amdgcn_sched_barrier(0);
+      }
   };
-  if (begin < end) {
-    // (the first stage: as if S::STAGES - 1 others were behind it)
-    if (S::STAGES > 1 && begin + S::STAGES - 1 < end)
-      wait_loads<LOADS*(S::STAGES - 1)>();
-    else
-      wait_loads<0>();
+  // the oldest stage on its way is there for all waves, and every wave has read the last of the stage in front of it
+  auto meet = [&]() {
+    __builtin_amdgcn_s_waitcnt(0xc07f);  // lgkmcnt(0)
+    asm volatile("" ::: "memory");
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
-    read_step(lds, 0, 0);
+  };
+#pragma unroll
+  for (int s = 0; s < S::STAGES; ++s) {
+    const Stage st = stage_of(begin + s, s);
+#pragma unroll
+    for (int i = 0; i < LOADS; ++i) load(st, i);
   }
+  wait_loads<LOADS * (S::STAGES - 1)>();
+  meet();
+#pragma unroll
+  for (int i = 0; i < READS; ++i) read(lds, 0, 0, i);
   int slot = 0;
   for (int32_t t = begin; t < end; ++t) {
-    const uint32_t at = lds + slot * S::STAGE_BYTES;
     const int next = slot + 1 == S::STAGES ? 0 : slot + 1;
+    const uint32_t here = lds + slot * S::STAGE_BYTES, there = lds + next * S::STAGE_BYTES;
 #pragma unroll
-    for (int step = 0; step < 4; ++step) {
-      if (step < 3) {
-        read_step(at, step + 1, (step + 1) & 1);
-      } else if (t + 1 < end) {
-        arrive(t + 1);
-        read_step(lds + next * S::STAGE_BYTES, 0, 0);
-        if (t + S::STAGES < end) load_stage(t + S::STAGES, slot);
-      }
-      __builtin_amdgcn_sched_barrier(0);
-      products(step & 1);
-      __builtin_amdgcn_sched_barrier(0);
-    }
+    for (int step = 0; step < 3; ++step)
+      products(step & 1, [&](int n) {
+#pragma unroll
+        for (int i = n * READS / BLOCKS; i < (n + 1) * READS / BLOCKS; ++i) read(here, step + 1, (step + 1) & 1, i);
+      });
+    wait_loads<LOADS * (S::STAGES - 2)>();
+    meet();
+    const Stage st = stage_of(t + S::STAGES, slot);
+    products(1, [&](int n) {
+#pragma unroll
+      for (int i = n * READS / BLOCKS; i < (n + 1) * READS / BLOCKS; ++i) read(there, 0, 0, i);  // (behind the last stage: of no use)
+#pragma unroll
+      for (int i = n * LOADS / BLOCKS; i < (n + 1) * LOADS / BLOCKS; ++i) load(st, i);
+    });
     slot = next;
   }
+  wait_loads<0>();
   const Place at{m0 + wave_m * MI * (DUAL ? 16 : 32), n0 + wave_n * NI * 32, split, tm, wave_m, wave_n, lane};
   epilogue.template operator()<S, MI, NI>(acc, at, smem);
 }
@@ -403,13 +421,85 @@ __global__ void __launch_bounds__(256) join_parts_kernel(const float* parts, int
   }
 }
 
+template <typename T>
+hipError_t join_parts(const float* parts, int32_t n, int64_t features, int64_t rows, T* out, int64_t stride, hipStream_t s) {
+  const int64_t all = features / 4 * rows;
+  join_parts_kernel<T><<<dim3((uint32_t)std::min<int64_t>((all + 255) / 256, 1 << 16)), dim3(256), 0, s>>>(parts, n, features, rows, out, stride);
+  return hipGetLastError();
+}
+
+// Which tiles a product gets, and into how many parts its contraction is cut.
+struct Plan {
+  int shape, splits;
+  int64_t bm() const { return shape == LARGE ? 256 : shape == MIDDLE ? 128 : 64; }
+  int64_t bn() const { return shape == LARGE ? 256 : shape == MIDDLE ? 128 : shape == FEW64 ? 64 : 32; }
+};
+// The least time by a simple account, in us: a round of workgroups takes its stages and `fixed` for its start and end; a stage takes
+// `busy` where every place for a workgroup is taken, less where few are, `alone` at least.
+struct ShapeCost {
+  double busy, alone, fixed;
+};
+constexpr int CUS = 256;
+inline ShapeCost shape_cost(bool f32, int shape) {
+  constexpr ShapeCost BF16[] = {{1.5, 1.2, 8.0}, {1.05, 0.6, 5.0}, {1.3, 0.7, 4.0}, {1.6, 0.7, 4.0}};
+  constexpr ShapeCost F32[] = {{0, 0, 0}, {3.6, 2.0, 5.0}, {2.0, 2.0, 4.0}, {1.7, 1.0, 4.0}};
+  return f32 ? F32[shape] : BF16[shape];
+}
+// shapes: bits of those that the caller has kernels for; k: contracted elements, of all segments
+template <typename T>
+Plan plan_product(int64_t features, int64_t rows, int64_t k, bool dual, int most_splits, int shapes = 15) {
+  constexpr int PLACES[] = {CUS, 2 * CUS, 3 * CUS, 4 * CUS};
+  const bool f32 = sizeof(T) == 4;
+  const int64_t stages = (k + STAGE_K<T> - 1) / STAGE_K<T>;
+  Plan best = {MIDDLE, 1};
+  double least = 1e30;
+  for (int shape = f32 ? MIDDLE : LARGE; shape <= FEW32; ++shape) {
+    if (!(shapes >> shape & 1)) continue;
+    Plan p = {shape, 1};
+    const ShapeCost c = shape_cost(f32, shape);
+    const int64_t bm = dual ? p.bm() / 2 : p.bm();
+    const int64_t tiles = ((features + bm - 1) / bm) * ((rows + p.bn() - 1) / p.bn());
+    for (p.splits = 1; p.splits <= most_splits && (p.splits == 1 || stages / p.splits >= 4); ++p.splits) {
+      const int64_t all = tiles * p.splits, full = all / PLACES[shape], rest = all % PLACES[shape], deep = (stages + p.splits - 1) / p.splits;
+      double t = (double)full * (deep * c.busy + c.fixed);
+      if (rest) t += deep * std::max(c.alone, c.busy * rest / PLACES[shape]) + c.fixed;
+      if (p.splits > 1) t += 4.0 + (double)features * rows * p.splits * 8 / 4.0e6;
+      if (t < least) {
+        least = t;
+        best = p;
+      }
+    }
+  }
+  return best;
+}
+
 template <typename T, int FA, int FB, bool DUAL, typename S, typename Epilogue>
-hipError_t launch_product(hpd_product_args g, const Epilogue& e, hipStream_t s) {
+hipError_t launch_shape(hpd_product_args g, const Epilogue& e, hipStream_t s) {
   const int64_t bm = DUAL ? S::BM / 2 : S::BM;
   g.tiles_m = (int32_t)((g.a.size + bm - 1) / bm);
   g.tiles_n = (int32_t)((g.b.size + S::BN - 1) / S::BN);
   product_kernel<T, FA, FB, DUAL, S, Epilogue><<<dim3((uint32_t)g.tiles_m * g.tiles_n * g.splits), dim3(64 * S::WAVES), 0, s>>>(g, e);
   return hipGetLastError();
+}
+template <typename T, int FA, int FB, bool DUAL, typename Epilogue>
+hipError_t launch_product(Plan p, hpd_product_args g, const Epilogue& e, hipStream_t s) {
+  g.splits = p.splits;
+  if constexpr (sizeof(T) == 2)
+    if (p.shape == LARGE) return launch_shape<T, FA, FB, DUAL, Large>(g, e, s);
+  if constexpr (FB == BY_ROWS) {
+    if (p.shape == FEW64) return launch_shape<T, FA, FB, DUAL, Few64>(g, e, s);
+    if (p.shape == FEW32) return launch_shape<T, FA, FB, DUAL, Few32>(g, e, s);
+  }
+  return launch_shape<T, FA, FB, DUAL, Middle>(g, e, s);
+}
+
+// C as T, through parts in fp32 ([splits][rows][features] at `parts`) where the contraction is cut.
+template <typename T, int FA, int FB>
+hipError_t store_product(Plan p, const hpd_product_args& g, float* parts, T* out, int64_t stride, hipStream_t s) {
+  const int64_t features = g.a.size, rows = g.b.size;
+  if (p.splits == 1) return launch_product<T, FA, FB, false>(p, g, StoreProduct<T>{{out, nullptr}, {stride, 0}, rows, features, rows}, s);
+  const hipError_t e = launch_product<T, FA, FB, false>(p, g, StorePart{parts, features, rows, 0}, s);
+  return e != hipSuccess ? e : join_parts(parts, p.splits, features, rows, out, stride, s);
 }
 
 }  // namespace
