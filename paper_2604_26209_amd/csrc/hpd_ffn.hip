@@ -34,58 +34,113 @@ struct Activate {
   T *h, *gate, *up;  // gate and up may be NULL
   int64_t inner, rows, gate_stride, up_stride;
   template <typename S, int MI, int NI>
-  __device__ __forceinline__ void operator()(floatx16 (&acc)[MI][NI], const Place& at, char*) const {
-    const int l = at.lane & 31, half = at.lane >> 5;
+  __device__ __forceinline__ void operator()(floatx16 (&acc)[MI][NI], const Place& at, char* smem) const {
+    constexpr int NB = MI > 1 ? MI / 2 : 1;
+    const int64_t width = inner - at.feature;
+    // where waves have one block each: g in one, u in the next, which hands it over through its LDS
+    constexpr int GIVEN = MI > 1 ? 0 : NI * 4096;
+    static_assert(GIVEN + NB * 32 * 32 * (int)sizeof(T) <= S::TURN, "u and a turn");
+    const Turn<T, NB> turn(at, smem, S::TURN, GIVEN);
+    const bool has_g = MI > 1 || at.wave_m % 2 == 0, has_u = MI > 1 || !has_g;
+    const float* const given = reinterpret_cast<const float*>(smem + ((threadIdx.x >> 6) + 1) * S::TURN) + at.lane;
+    if constexpr (MI == 1) {
+      float* const give = reinterpret_cast<float*>(smem + (threadIdx.x >> 6) * S::TURN) + at.lane;
+      if (has_u)
 #pragma unroll
-    for (int j = 0; j < NI; ++j) {
-      const int64_t row = at.row + 32 * j + l;
-      if (row >= rows) continue;
+        for (int j = 0; j < NI; ++j)
 #pragma unroll
-      for (int i = 0; i < MI; i += 2)
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          const int64_t m = at.feature + 16 * i + 8 * q + 4 * half;
-          if (m >= inner) continue;
-          float g[4], u[4], v[4];
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            float slope;
-            g[e] = acc[i][j][4 * q + e];
-            u[e] = acc[i + 1][j][4 * q + e];
-            activation<T, ACT>(g[e], v[e], slope);
-            v[e] *= u[e];
-          }
-          store4(h + row * inner + m, v);
-          if (gate) store4(gate + row * gate_stride + m, g);
-          if (up) store4(up + row * up_stride + m, u);
-        }
+          for (int r = 0; r < 16; ++r) give[(16 * j + r) * 64] = acc[0][j][r];
+      __syncthreads();
     }
+    each<NI>([&](auto j) {
+      const int64_t first = at.row + 32 * j, left = rows - first;
+      auto put = [&](auto value) {
+#pragma unroll
+        for (int b = 0; b < NB; ++b)
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
+            float v[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const int r = 4 * q + e;
+              v[e] = value([&]() { return sum_of<S>(acc[MI > 1 ? 2 * b : 0][j], r); },
+                           [&]() { return MI > 1 ? sum_of<S>(acc[MI > 1 ? 2 * b + 1 : 0][j], r) : given[(16 * j + r) * 64]; });
+            }
+            turn.put4(b, q, v);
+          }
+      };
+      if (has_g) {
+        put([&](auto g, auto u) {
+          float a, slope;
+          activation<T, ACT>(g(), a, slope);
+          return a * u();
+        });
+        turn.store(left, width, inner, [&](int r) { return h + (first + r) * inner + at.feature; });
+        if (gate) {
+          put([](auto g, auto) { return g(); });
+          turn.store(left, width, gate_stride, [&](int r) { return gate + (first + r) * gate_stride + at.feature; });
+        }
+      }
+      if (has_u && up) {
+        put([](auto own, auto u) { return MI > 1 ? u() : own(); });
+        turn.store(left, width, up_stride, [&](int r) { return up + (first + r) * up_stride + at.feature; });
+      }
+    });
   }
 };
 
-// from dh: dg and du next to each other, h if it is wanted
+// From dh: dg and du next to each other, h if it is wanted.  g and u come through LDS, where dg and du take their places; two blocks
+// at a time, so that both fit.
 template <typename T, int ACT>
 struct InnerGradients {
   const T *gate, *up;
   T *d_inner, *h;
   int64_t inner, rows, gate_stride, up_stride;
   template <typename S, int MI, int NI>
-  __device__ __forceinline__ void operator()(floatx16 (&acc)[MI][NI], const Place& at, char*) const {
-    each4<MI, NI>(acc, at, inner, rows, [&](int64_t row, int64_t m, const float* dh) {
-      float g[4], u[4], dg[4], du[4], v[4];
-      fetch4(gate + row * gate_stride + m, g);
-      fetch4(up + row * up_stride + m, u);
+  __device__ __forceinline__ void operator()(floatx16 (&acc)[MI][NI], const Place& at, char* smem) const {
+    constexpr int NB = MI < 2 ? 1 : 2, BYTES = NB * 32 * 32 * (int)sizeof(T);
+    static_assert(2 * BYTES <= S::TURN, "g and u");
+    using W = Turn<T, NB>;
+    const W of_g(at, smem, S::TURN), of_u(at, smem, S::TURN, BYTES);
+    each<NI>([&](auto j) {
+      each<MI / NB>([&](auto half) {
+        constexpr int i0 = half * NB;
+        const int64_t first = at.row + 32 * j, left = rows - first, feature = at.feature + 32 * i0, width = inner - feature;
+        const typename W::Rows g_rows = of_g.fetch(left, width, gate_stride, [&](int r) { return gate + (first + r) * gate_stride + feature; });
+        const typename W::Rows u_rows = of_u.fetch(left, width, up_stride, [&](int r) { return up + (first + r) * up_stride + feature; });
+        of_g.put(g_rows);
+        of_u.put(u_rows);
+        Four<T> kept[NB][4];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        float a, slope;
-        activation<T, ACT>(g[e], a, slope);
-        v[e] = a * u[e];
-        dg[e] = dh[e] * u[e] * slope;
-        du[e] = dh[e] * a;
-      }
-      store4(d_inner + row * 2 * inner + m, dg);
-      store4(d_inner + row * 2 * inner + inner + m, du);
-      if (h) store4(h + row * inner + m, v);
+        for (int i = 0; i < NB; ++i)
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
+            float g[4], u[4], v[4];
+            fetch4(of_g.four(i, q), g);
+            fetch4(of_u.four(i, q), u);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const float dh = sum_of<S>(acc[i0 + i][j], 4 * q + e);
+              float a, slope;
+              activation<T, ACT>(g[e], a, slope);
+              g[e] = dh * u[e] * slope;
+              v[e] = a * u[e];
+              u[e] = dh * a;
+            }
+            of_g.put4(i, q, g);
+            of_u.put4(i, q, u);
+            kept[i][q] = pack4<T>(v);
+          }
+        of_g.store(left, width, 2 * inner, [&](int r) { return d_inner + (first + r) * 2 * inner + feature; });
+        of_u.store(left, width, 2 * inner, [&](int r) { return d_inner + (first + r) * 2 * inner + inner + feature; });
+        if (h) {
+#pragma unroll
+          for (int i = 0; i < NB; ++i)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) *reinterpret_cast<Four<T>*>(of_g.four(i, q)) = kept[i][q];
+          of_g.store(left, width, inner, [&](int r) { return h + (first + r) * inner + feature; });
+        }
+      });
     });
   }
 };
@@ -120,8 +175,8 @@ struct BackwardPlan {
   BackwardPlan(const hpd_ffn_config& c, int64_t n) {
     inner = plan_product<T>(c.inner, n, c.width, false, 1);
     dx = plan_product<T>(c.width, n, 2 * (int64_t)c.inner, false, MOST_SPLITS);
-    in_weights = plan_product<T>(c.width, 2 * (int64_t)c.inner, n, false, 1, 3);
-    down_weights = plan_product<T>(c.inner, c.width, n, false, 1, 3);
+    in_weights = plan_product<T>(c.width, 2 * (int64_t)c.inner, n, false, 1);
+    down_weights = plan_product<T>(c.inner, c.width, n, false, 1);
     h = round16(n * 2 * c.inner * (int64_t)sizeof(T));
     parts = h + round16(n * c.inner * (int64_t)sizeof(T));
     bytes = parts + part_bytes(dx, n, c.width);
@@ -133,11 +188,11 @@ hipError_t forward(const hpd_ffn_forward_args& a, hipStream_t s) {
   const int64_t D = a.cfg.width, F = a.cfg.inner, N = a.n_rows;
   const ForwardPlan<T> plan(a.cfg, N);
   T* const h = (T*)a.workspace;
-  const hpd_product_args in = {operand<T>(a.w_gate, a.st.w_gate, F, a.w_up), operand<T>(a.x, a.st.x, N), (int32_t)D, 1, 1, 0, 0};
+  const hpd_product_args in = {operand<T>(a.w_gate, a.st.w_gate, F, a.w_up), operand<T>(a.x, a.st.x, N), (int32_t)D, 1, 0, 0};
   const Activate<T, ACT> act = {h, (T*)a.gate, (T*)a.up, F, N, a.st.gate, a.st.up};
-  const hipError_t e = launch_product<T, BY_ROWS, BY_ROWS, true>(plan.in, in, act, s);
+  const hipError_t e = launch_product<T, BY_ROWS, BY_ROWS, DUAL>(plan.in, in, act, s);
   if (e != hipSuccess) return e;
-  const hpd_product_args down = {operand<T>(a.w_down, a.st.w_down, D), operand<T>(h, F, N), (int32_t)F, 1, 1, 0, 0};
+  const hpd_product_args down = {operand<T>(a.w_down, a.st.w_down, D), operand<T>(h, F, N), (int32_t)F, 1, 0, 0};
   return store_product<T, BY_ROWS, BY_ROWS>(plan.down, down, (float*)(a.workspace + plan.parts), (T*)a.out, a.st.out, s);
 }
 
@@ -149,26 +204,26 @@ hipError_t backward(const hpd_ffn_backward_args& a, hipStream_t s) {
   T* const h = (T*)(a.workspace + plan.h);
   hipError_t e = hipSuccess;
   if (N > 0) {
-    const hpd_product_args g = {operand<T>(a.w_down, a.st.w_down, F), operand<T>(a.d_out, a.st.d_out, N), (int32_t)D, 1, 1, 0, 0};
+    const hpd_product_args g = {operand<T>(a.w_down, a.st.w_down, F), operand<T>(a.d_out, a.st.d_out, N), (int32_t)D, 1, 0, 0};
     const InnerGradients<T, ACT> grad = {(const T*)a.gate, (const T*)a.up, d_inner, a.d_w_down ? h : nullptr, F, N, a.st.gate, a.st.up};
-    e = launch_product<T, BY_COLUMNS, BY_ROWS, false>(plan.inner, g, grad, s);
+    e = launch_product<T, BY_COLUMNS, BY_ROWS, PLAIN>(plan.inner, g, grad, s);
   }
   if (e == hipSuccess && a.d_x && N > 0) {
-    const hpd_product_args g = {operand<T>(a.w_gate, a.st.w_gate, D, a.w_up), operand<T>(d_inner, 2 * F, N, d_inner + F), (int32_t)F, 2, 1, 0, 0};
-    e = store_product<T, BY_COLUMNS, BY_ROWS>(plan.dx, g, (float*)(a.workspace + plan.parts), (T*)a.d_x, a.st.d_x, s);
+    const hpd_product_args g = {operand<T>(a.w_gate, a.st.w_gate, D, a.w_up), operand<T>(d_inner, 2 * F, N, d_inner + F), (int32_t)F, 1, 0, 0};
+    e = store_product<T, BY_COLUMNS, BY_ROWS, SEGMENTS>(plan.dx, g, (float*)(a.workspace + plan.parts), (T*)a.d_x, a.st.d_x, s);
   }
   if (e == hipSuccess && (a.d_w_gate || a.d_w_up)) {  // (no rows: zeros)
     // rows of the result: the gate's features, then the up projection's
     const int64_t skip = a.d_w_gate ? 0 : F, rows = (a.d_w_gate ? F : 0) + (a.d_w_up ? F : 0);
-    const hpd_product_args g = {operand<T>(a.x, a.st.x, D), operand<T>(d_inner + skip, 2 * F, rows), (int32_t)N, 1, 1, 0, 0};
+    const hpd_product_args g = {operand<T>(a.x, a.st.x, D), operand<T>(d_inner + skip, 2 * F, rows), (int32_t)N, 1, 0, 0};
     const StoreProduct<T> store = {{(T*)(skip ? a.d_w_up : a.d_w_gate), (T*)a.d_w_up},
                                    {skip ? a.st.d_w_up : a.st.d_w_gate, a.st.d_w_up}, F, D, rows};
-    e = launch_product<T, BY_COLUMNS, BY_COLUMNS, false>(plan.in_weights, g, store, s);
+    e = launch_product<T, BY_COLUMNS, BY_COLUMNS, PLAIN>(plan.in_weights, g, store, s);
   }
   if (e == hipSuccess && a.d_w_down) {
-    const hpd_product_args g = {operand<T>(h, F, F), operand<T>(a.d_out, a.st.d_out, D), (int32_t)N, 1, 1, 0, 0};
+    const hpd_product_args g = {operand<T>(h, F, F), operand<T>(a.d_out, a.st.d_out, D), (int32_t)N, 1, 0, 0};
     const StoreProduct<T> store = {{(T*)a.d_w_down, nullptr}, {a.st.d_w_down, 0}, D, F, D};
-    e = launch_product<T, BY_COLUMNS, BY_COLUMNS, false>(plan.down_weights, g, store, s);
+    e = launch_product<T, BY_COLUMNS, BY_COLUMNS, PLAIN>(plan.down_weights, g, store, s);
   }
   return e;
 }

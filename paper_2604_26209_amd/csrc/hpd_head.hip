@@ -36,32 +36,40 @@ struct RowSums {
   template <typename S, int MI, int NI>
   __device__ __forceinline__ void operator()(floatx16 (&acc)[MI][NI], const Place& at, char* smem) const {
     const int l = at.lane & 31, h = at.lane >> 5;
-    __syncthreads();  // (the operands' stages make room)
     float4* const shared = reinterpret_cast<float4*>(smem);  // [WM][BN]
 #pragma unroll
     for (int j = 0; j < NI; ++j) {
       const int64_t row = at.row + 32 * j + l;
       const int32_t target = targets && row < rows ? targets[row] : -1;
-      const int32_t mine = target - (int32_t)at.feature;
+      const int64_t behind = (int64_t)target - at.feature;
+      const int32_t mine = behind < 0 || behind >= 32 * MI ? -1 : (int32_t)behind;  // the target, counted from the wave's first
+      const int32_t inside = (int32_t)(vocab - at.feature);
+      float at_target = 0.f;
       Sums a = {-INFINITY, 0.f, 0.f};
+      auto logit = [&](int i, int r) {
+        const int m = 32 * i + block_row(r, h);
+        const float x = sum_of<S>(acc[i][j], r);
+        return m < inside ? x : -INFINITY;
+      };
 #pragma unroll
       for (int i = 0; i < MI; ++i)
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
-          const int m = 32 * i + block_row(r, h);
-          if (at.feature + m >= vocab) acc[i][j][r] = -INFINITY;
-          a.m = fmaxf(a.m, acc[i][j][r]);
-          if (mine == m && target < vocab) of_target[row] = acc[i][j][r];
+          const float x = logit(i, r);
+          a.m = fmaxf(a.m, x);
+          if (mine == 32 * i + block_row(r, h)) at_target = x;
         }
+      if (mine >= 0 && mine < (inside < 32 * MI ? inside : 32 * MI) && (mine >> 2 & 1) == h) of_target[row] = at_target;
       // +infinity and NaN (which fmaxf passes over) make s NaN
       const float m = a.m == -INFINITY ? 0.f : a.m;
 #pragma unroll
       for (int i = 0; i < MI; ++i)
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
-          const float d = acc[i][j][r] - m, e = fast_exp2(d * LOG2E);
+          const float d = logit(i, r) - m, e = fast_exp2(d * LOG2E);
           a.s += e;
           a.t = fmaf(e, d < -1e4f ? 0.f : d, a.t);
+          if (r % 4 == 3) __builtin_amdgcn_sched_barrier(0);
         }
       a = join(a, {__shfl_xor(a.m, 32), __shfl_xor(a.s, 32), __shfl_xor(a.t, 32)});
       if (h == 0) shared[at.wave_m * S::BN + (at.wave_n * NI + j) * 32 + l] = make_float4(a.m, a.s, a.t, 0.f);
@@ -117,12 +125,14 @@ struct LogitGradients {
   int32_t first, vocab;  // of the piece, in it
   int32_t whole;         // tokens of the whole vocabulary
   template <typename S, int MI, int NI>
-  __device__ __forceinline__ void operator()(floatx16 (&acc)[MI][NI], const Place& at, char*) const {
+  __device__ __forceinline__ void operator()(floatx16 (&acc)[MI][NI], const Place& at, char* smem) const {
     const int l = at.lane & 31, h = at.lane >> 5;
+    const Turn<T, MI> turn(at, smem, S::TURN);
 #pragma unroll
     for (int j = 0; j < NI; ++j) {
-      const int64_t row = at.row + 32 * j + l;
-      if (row >= rows) continue;
+      const int64_t first_row = at.row + 32 * j;
+      asm volatile("" ::: "memory");  // (a block's rows are asked for when they are needed, not all at once)
+      const int64_t row = first_row + l < rows ? first_row + l : rows - 1;
       const int32_t t = targets ? targets[row] : -1, target = t < 0 ? -1 : t - first;
       const float L = lse[row];
       const float ge = g_entropy && L != -INFINITY ? g_entropy[row] : 0.f, H = g_entropy ? entropy[row] : 0.f;
@@ -133,17 +143,17 @@ struct LogitGradients {
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
           const int64_t m = at.feature + 32 * i + 8 * q + 4 * h;
-          if (m >= stride) continue;
           float v[4];
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
-            const float lp = acc[i][j][4 * q + e] - L, p = L == -INFINITY ? 0.f : fast_exp2(lp * LOG2E);
+            const float lp = sum_of<S>(acc[i][j], 4 * q + e) - L, p = L == -INFINITY ? 0.f : fast_exp2(lp * LOG2E);
             float d = -p * (p > 0.f ? fmaf(ge, lp + H, g) : g);
             if (m + e == target) d += g;
             v[e] = m + e < vocab ? d : 0.f;
           }
-          store4(out + row * stride + m, v);
+          turn.put4(i, q, v);
         }
+      turn.store(rows - first_row, stride - at.feature, stride, [&](int r) { return out + (first_row + r) * stride + at.feature; });
     }
   }
 };
@@ -165,7 +175,7 @@ struct ForwardPlan {
   int64_t tiles, of_target, bytes;
   ForwardPlan(int64_t n, int32_t width, int32_t vocab) {
     product = plan_product<T>(vocab, n, width, false, 1);
-    tiles = (vocab + product.bm() - 1) / product.bm();
+    tiles = (vocab + product.size() - 1) / product.size();
     of_target = n * tiles * (int64_t)sizeof(float4);
     bytes = round16(of_target + n * 4);
   }
@@ -182,7 +192,7 @@ struct BackwardPlan {
     piece = ((vocab + pieces - 1) / pieces + UNIT - 1) / UNIT * UNIT;
     logits = plan_product<T>(std::min<int64_t>(piece, vocab), n, width, false, 1);
     d_hidden = plan_product<T>(width, n, std::min<int64_t>(piece, vocab), false, MOST_SPLITS);
-    d_weight = plan_product<T>(width, std::min<int64_t>(piece, vocab), n, false, 1, 3);
+    d_weight = plan_product<T>(width, std::min<int64_t>(piece, vocab), n, false, 1);
     parts = round16(n * piece * (int64_t)sizeof(T));
     bytes = parts + d_hidden.splits * n * width * 4;
   }
@@ -195,9 +205,9 @@ hipError_t forward(const hpd_head_args& a, hipStream_t s) {
   float4* const parts = (float4*)a.workspace;
   float* const of_target = (float*)(a.workspace + plan.of_target);
   const hpd_product_args g = {operand<T>(a.weight, a.weight_stride, a.vocab), operand<T>(a.hidden, a.hidden_stride, a.n_rows),
-                              a.width, 1, 1, 0, 0};
+                              a.width, 1, 0, 0};
   const int32_t* const targets = a.logprob ? a.targets : nullptr;
-  const hipError_t e = launch_product<T, BY_ROWS, BY_ROWS, false>(plan.product, g, RowSums{targets, of_target, parts, a.vocab, tiles, a.n_rows}, s);
+  const hipError_t e = launch_product<T, BY_ROWS, BY_ROWS, PLAIN>(plan.product, g, RowSums{targets, of_target, parts, a.vocab, tiles, a.n_rows}, s);
   if (e != hipSuccess) return e;
   join_rows_kernel<<<dim3((uint32_t)((a.n_rows + 3) / 4)), dim3(256), 0, s>>>(parts, tiles, a.n_rows, of_target, targets, a.vocab, a.logprob,
                                                                              a.lse, a.entropy);
@@ -216,19 +226,19 @@ hipError_t backward(const hpd_head_backward_args& a, hipStream_t s) {
     const int64_t n = std::min<int64_t>(piece, a.vocab - v0);
     const T* const w = (const T*)a.weight + v0 * a.weight_stride;
     if (N > 0) {
-      const hpd_product_args g = {operand<T>(w, a.weight_stride, n), operand<T>(a.hidden, a.hidden_stride, N), (int32_t)D, 1, 1, 0, 0};
-      e = launch_product<T, BY_ROWS, BY_ROWS, false>(
+      const hpd_product_args g = {operand<T>(w, a.weight_stride, n), operand<T>(a.hidden, a.hidden_stride, N), (int32_t)D, 1, 0, 0};
+      e = launch_product<T, BY_ROWS, BY_ROWS, PLAIN>(
           plan.logits, g,
           LogitGradients<T>{a.targets, a.lse, a.entropy, a.g_logprob, a.g_entropy, dx, piece, N, (int32_t)v0, (int32_t)n, a.vocab}, s);
     }
     if (e == hipSuccess && a.d_hidden && N > 0) {
-      const hpd_product_args g = {operand<T>(w, a.weight_stride, D), operand<T>(dx, piece, N), (int32_t)n, 1, 1, 0, 0};
-      e = launch_product<T, BY_COLUMNS, BY_ROWS, false>(plan.d_hidden, g, StorePart{parts, D, N, v0 > 0}, s);
+      const hpd_product_args g = {operand<T>(w, a.weight_stride, D), operand<T>(dx, piece, N), (int32_t)n, 1, 0, 0};
+      e = launch_product<T, BY_COLUMNS, BY_ROWS, PLAIN>(plan.d_hidden, g, StorePart{parts, D, N, v0 > 0}, s);
     }
     if (e == hipSuccess && a.d_weight) {  // (no rows: zeros)
-      const hpd_product_args g = {operand<T>(a.hidden, a.hidden_stride, D), operand<T>(dx, piece, n), (int32_t)N, 1, 1, 0, 0};
+      const hpd_product_args g = {operand<T>(a.hidden, a.hidden_stride, D), operand<T>(dx, piece, n), (int32_t)N, 1, 0, 0};
       const StoreProduct<T> store = {{(T*)a.d_weight + v0 * a.d_weight_stride, nullptr}, {a.d_weight_stride, 0}, n, D, n};
-      e = launch_product<T, BY_COLUMNS, BY_COLUMNS, false>(plan.d_weight, g, store, s);
+      e = launch_product<T, BY_COLUMNS, BY_COLUMNS, PLAIN>(plan.d_weight, g, store, s);
     }
   }
   if (e == hipSuccess && a.d_hidden && N > 0) e = join_parts(parts, plan.d_hidden.splits, D, N, (T*)a.d_hidden, a.d_hidden_stride, s);

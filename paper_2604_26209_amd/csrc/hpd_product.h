@@ -21,6 +21,7 @@
 #include <stdint.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "hpd_attn_bf16.h"
 
@@ -32,8 +33,7 @@ struct hpd_operand {
 
 struct hpd_product_args {
   hpd_operand a, b;
-  int32_t k;         // contracted elements of a segment
-  int32_t segments;  // 1 or 2
+  int32_t k;         // contracted elements (of either segment)
   int32_t splits;    // parts the stages are cut into
   int32_t tiles_m, tiles_n;
 };
@@ -41,7 +41,7 @@ struct hpd_product_args {
 namespace {
 
 enum { BY_ROWS = 0, BY_COLUMNS = 1 };
-constexpr uint32_t OUTSIDE = 0x80000000u;  // an offset that no buffer holds
+constexpr uint32_t RANGE = 0x80000000u, OUTSIDE = 0xc0000000u;  // bytes of a buffer, an offset that none holds
 
 template <typename T>
 constexpr int CHUNK = 16 / (int)sizeof(T);  // elements of a 16-byte chunk
@@ -51,16 +51,36 @@ constexpr int STAGE_K = 8 * CHUNK<T>;       // of the contracted index in a stag
 typedef int32_t int32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t product_u4 __attribute__((ext_vector_type(4)));
 
-__device__ __forceinline__ int32x4 buffer_of(const char* p) {
+__device__ __forceinline__ int32x4 buffer_of(const char* p, uint32_t bytes) {
   const uint64_t u = reinterpret_cast<uint64_t>(p);
   return {__builtin_amdgcn_readfirstlane((int32_t)(uint32_t)u), __builtin_amdgcn_readfirstlane((int32_t)(uint32_t)(u >> 32)),
-          (int32_t)OUTSIDE, 0x00027000};
+          __builtin_amdgcn_readfirstlane((int32_t)bytes), 0x00027000};
 }
-// 64 x 16 bytes to LDS, lane i's at lds + 16 i
-__device__ __forceinline__ void load_to_lds(uint32_t lds, uint32_t off, int32x4 buf) {
-  uint32_t keep;  // (M0 is the compiler's)
-  asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\tbuffer_load_dwordx4 %2, %3, 0 offen lds\n\ts_mov_b32 m0, %0"
-               : "=&s"(keep) : "s"(lds), "v"(off), "s"(buf) : "memory");
+// N loads of 64 x 16 bytes to successive KB of LDS, lane i's at + 16 i.  The instruction's offset moves both addresses, so the
+// lanes' offsets are n KB less for load n, and BIAS more.  (M0 is the compiler's.)
+constexpr uint32_t BIAS = 4096;
+template <int N>
+__device__ __forceinline__ void load_to_lds(uint32_t lds, const uint32_t* off, int32x4 buf) {
+  uint32_t keep;
+  if constexpr (N == 4)
+    asm volatile(
+        "s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\t"
+        "buffer_load_dwordx4 %2, %6, 0 offen lds\n\t"
+        "buffer_load_dwordx4 %3, %6, 0 offen offset:1024 lds\n\t"
+        "buffer_load_dwordx4 %4, %6, 0 offen offset:2048 lds\n\t"
+        "buffer_load_dwordx4 %5, %6, 0 offen offset:3072 lds\n\t"
+        "s_mov_b32 m0, %0"
+        : "=&s"(keep) : "s"(lds), "v"(off[0]), "v"(off[1]), "v"(off[2]), "v"(off[3]), "s"(buf) : "memory");
+  else if constexpr (N == 1)
+    asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\tbuffer_load_dwordx4 %2, %3, 0 offen lds\n\ts_mov_b32 m0, %0"
+                 : "=&s"(keep) : "s"(lds), "v"(off[0]), "s"(buf) : "memory");
+  else
+    asm volatile(
+        "s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\t"
+        "buffer_load_dwordx4 %2, %4, 0 offen lds\n\t"
+        "buffer_load_dwordx4 %3, %4, 0 offen offset:1024 lds\n\t"
+        "s_mov_b32 m0, %0"
+        : "=&s"(keep) : "s"(lds), "v"(off[0]), "v"(off[1]), "s"(buf) : "memory");
 }
 __device__ __forceinline__ uint32_t product_lds(const void* p) {
   return (uint32_t)reinterpret_cast<uintptr_t>((const __attribute__((address_space(3))) char*)p);
@@ -83,7 +103,8 @@ __device__ __forceinline__ void wait_loads() {
 template <typename T, int FORM, int R, int WAVES, bool DUAL>
 struct Tile {
   static constexpr int BYTES = R * 128;
-  static constexpr int LOADS = R / 8 / WAVES;        // load instructions of a wave and stage
+  static constexpr int LOADS = R / 8 / WAVES;        // load instructions of a wave and stage, issued in groups
+  static constexpr int GROUP = LOADS % 4 == 0 ? 4 : LOADS % 2 == 0 ? 2 : 1, GROUPS = LOADS / GROUP;
   static constexpr int RB = R * (int)sizeof(T);      // by columns: bytes of one k
   static constexpr int GRANULES = RB / 64;
   static_assert(R % (8 * WAVES) == 0, "every wave loads whole KB");
@@ -111,15 +132,22 @@ struct Tile {
         const int c = (g ^ swizzle(k)) * 64 + (lane & 3) * 16;  // byte in the row
         off[i] = c / (int)sizeof(T) < size ? (uint32_t)k * (uint32_t)stride + c : OUTSIDE;
       }
+      off[i] += BIAS - i % GROUP * 1024;
     }
   }
-  // the stage's load i to LDS; left: contracted elements from the stage's first on
+  // the buffer of a stage that begins at p and has `left` (at least 1) elements of k: by columns, it ends behind the last of them
+  static __device__ __forceinline__ int32x4 buffer(const char* p, int64_t stride, int left) {
+    return buffer_of(p - BIAS, (FORM == BY_COLUMNS && left < STAGE_K<T> ? (uint32_t)left * (uint32_t)stride : RANGE) + BIAS);
+  }
+  // the stage's load group i to LDS; by rows, MASKED: nothing behind `left`
+  template <bool MASKED>
   __device__ __forceinline__ void load(int i, uint32_t lds, int32x4 b0, int32x4 b1, int wave, int lane, int left) const {
-    const int f = wave * LOADS + i;
-    uint32_t o = off[i];
-    const int k = FORM == BY_ROWS ? chunk_of(f, lane) * CHUNK<T> : k_of(f, lane);
-    if (k >= left) o = OUTSIDE;
-    load_to_lds(__builtin_amdgcn_readfirstlane(lds + f * 1024), o, DUAL && (f >> 2 & 1) ? b1 : b0);
+    const int f = wave * LOADS + i * GROUP;
+    uint32_t o[GROUP];
+#pragma unroll
+    for (int e = 0; e < GROUP; ++e)
+      o[e] = MASKED && FORM == BY_ROWS && chunk_of(f + e, lane) * CHUNK<T> >= left ? OUTSIDE : off[i * GROUP + e];
+    load_to_lds<GROUP>(__builtin_amdgcn_readfirstlane(lds + f * 1024), o, DUAL && (f >> 2 & 1) ? b1 : b0);
   }
 };
 
@@ -171,18 +199,34 @@ __device__ __forceinline__ floatx16 multiply(product_u4 a, product_u4 b, floatx1
   }
 }
 
-// Shapes of tiles: BM x BN by WM x WN waves, STAGES stages in LDS, WGS workgroups on a CU.
+// Shapes of tiles: BM x BN by WM x WN waves, STAGES stages in LDS, WGS workgroups on a CU.  (Workgroups that stay and make tile after
+// tile, the next one's first stages on their way while one is stored, are slower: 8192 x 8192 x 8192 in 880 us, 840 as it is; CUs do
+// not all run at one rate, and a tile goes to the one that is free.)
 template <int BM_, int BN_, int WM_, int WN_, int STAGES_, int WGS_>
 struct Shape {
   static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, STAGES = STAGES_, WGS = WGS_;
   static constexpr int WAVES = WM * WN, MI = BM / 32 / WM, NI = BN / 32 / WN;
   static constexpr int STAGE_BYTES = (BM + BN) * 128;
+  static constexpr int SMEM = STAGES * STAGE_BYTES, TURN = SMEM / WAVES / 4096 * 4096;  // of it, a wave's when its sums are stored
+  static constexpr bool MANY = MI * NI * 16 > 128;  // the sums are in accumulation registers
 };
+enum { PLAIN = 0, DUAL = 1, SEGMENTS = 2 };
+// bf16 products of 4096 elements: Large 1.2 PFLOP/s for 4096 x 4096 and more; Middle 1.06 from 4096 x 2048 (Large 0.72); Small 0.61 for
+// 2048 x 1024 (Middle 0.39), and with one to 64 rows the rate of memory, 6.7 TB/s of weights that the caches hold, 5.2 of others.  fp32:
+// Small alone, 0.13 to 0.14 from 2048 x 1024 on (128 x 128 with eight waves: 0.146 at most, 0.07 for 2048 x 1024).
 using Large = Shape<256, 256, 2, 2, 2, 1>;
-using Middle = Shape<128, 128, 2, 2, 2, 2>;
-using Few64 = Shape<64, 64, 1, 1, 3, 3>;
-using Few32 = Shape<64, 32, 1, 1, 3, 4>;
-enum { LARGE = 0, MIDDLE = 1, FEW64 = 2, FEW32 = 3 };
+using Middle = Shape<128, 128, 2, 4, 2, 2>;
+using Small = Shape<64, 64, 2, 2, 3, 3>;
+enum { LARGE = 0, MIDDLE = 1, SMALL = 2 };
+
+// f(0) .. f(N - 1), the numbers as types: what is indexed with them stays in registers however long f is
+template <int N, typename F, int I = 0>
+__device__ __forceinline__ void each(F f) {
+  if constexpr (I < N) {
+    f(std::integral_constant<int, I>{});
+    each<N, F, I + 1>(f);
+  }
+}
 
 // The place of a wave's blocks: features feature + 32 i (dual: block i is half i % 2 of features feature + 32 (i / 2)), rows row + 32 j.
 struct Place {
@@ -205,21 +249,28 @@ __device__ __forceinline__ void tile_of(int32_t id, int32_t total, int32_t tiles
   n = in / wide;
 }
 
-template <typename T, int FA, int FB, bool DUAL, typename S, typename Epilogue>
+template <typename T, int FA, int FB, int MODE, typename S, typename Epilogue>
 __global__ void __launch_bounds__(64 * S::WAVES, (S::WGS * S::WAVES + 3) / 4) product_kernel(hpd_product_args g, Epilogue epilogue) {
-  using TA = Tile<T, FA, S::BM, S::WAVES, DUAL>;
+  using TA = Tile<T, FA, S::BM, S::WAVES, MODE == DUAL>;
   using TB = Tile<T, FB, S::BN, S::WAVES, false>;
-  constexpr int MI = S::MI, NI = S::NI, K = STAGE_K<T>, LOADS = TA::LOADS + TB::LOADS;
-  constexpr int SMEM = S::STAGES * S::STAGE_BYTES;
-  __shared__ __attribute__((aligned(4096))) char smem[SMEM];
+  constexpr int MI = S::MI, NI = S::NI, K = STAGE_K<T>, LOADS = TA::LOADS + TB::LOADS, GROUPS = TA::GROUPS + TB::GROUPS;
+  // The stage with less than a whole stage's elements is the first, which is loaded in front of the loop; of two segments, the
+  // last of each, and loads by rows are masked all the time.
+  constexpr bool MASKED = MODE == SEGMENTS;
+  __shared__ __attribute__((aligned(4096))) char smem[S::SMEM];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wave_m = wave % S::WM, wave_n = wave / S::WM;
 
-  const int32_t tiles = g.tiles_m * g.tiles_n;
-  const int32_t split = blockIdx.x / tiles;
-  int32_t tm, tn;
-  tile_of(blockIdx.x - split * tiles, tiles, g.tiles_m, g.tiles_n, tm, tn);
-  const int64_t m0 = (int64_t)tm * (DUAL ? S::BM / 2 : S::BM), n0 = (int64_t)tn * S::BN;
+  // (divisions are made in vector registers, from where their results would not come back by themselves)
+  auto scalar = [](int32_t x) { return __builtin_amdgcn_readfirstlane(x); };
+  const int32_t tiles = g.tiles_m * g.tiles_n, split = scalar(blockIdx.x / tiles);
+  int32_t tile_m, tile_n;
+  tile_of(blockIdx.x - split * tiles, tiles, g.tiles_m, g.tiles_n, tile_m, tile_n);
+  tile_m = scalar(tile_m);
+  const int64_t m0 = (int64_t)tile_m * (MODE == DUAL ? S::BM / 2 : S::BM), n0 = (int64_t)scalar(tile_n) * S::BN;
+  const int32_t of_segment = (g.k + K - 1) / K, stages = MODE == SEGMENTS ? 2 * of_segment : of_segment;
+  const int32_t first_k = MASKED ? K : g.k - (of_segment - 1) * K;  // elements of the first stage
+  const int32_t begin = scalar((int32_t)((int64_t)stages * split / g.splits)), end = scalar((int32_t)((int64_t)stages * (split + 1) / g.splits));
 
   TA ta;
   TB tb;
@@ -227,33 +278,59 @@ __global__ void __launch_bounds__(64 * S::WAVES, (S::WGS * S::WAVES + 3) / 4) pr
   tb.init(g.b.stride, g.b.size - n0, wave, lane);
   const int64_t a0 = FA == BY_ROWS ? m0 * g.a.stride : m0 * (int64_t)sizeof(T);
   const int64_t b0 = FB == BY_ROWS ? n0 * g.b.stride : n0 * (int64_t)sizeof(T);
-  const char* const pa[2] = {(const char*)g.a.p[0] + a0, (const char*)g.a.p[1] + a0};
-  const char* const pb[2] = {(const char*)g.b.p[0] + b0, (const char*)g.b.p[1] + b0};
-  const int64_t step_a = FA == BY_ROWS ? 128 : K * g.a.stride, step_b = FB == BY_ROWS ? 128 : K * g.b.stride;
-  const int32_t of_segment = (g.k + K - 1) / K, total = of_segment * g.segments;
-  const int32_t begin = (int32_t)((int64_t)total * split / g.splits), end = (int32_t)((int64_t)total * (split + 1) / g.splits);
   const uint32_t lds = product_lds(smem);
-
-  // A stage's loads, by the piece: of the wave's LOADS, load i.  A stage behind the last has buffers without bytes: zeros into
+  // A stage's loads, by the group: of the wave's GROUPS, group i.  A stage behind the last has buffers without bytes: zeros into
   // its place in LDS, and as many loads to wait for as ever.
   struct Stage {
     int32x4 a, a1, b;
     uint32_t at;
     int left;
   };
-  auto stage_of = [&](int32_t t, int slot) -> Stage {
-    const bool second = !DUAL && t >= of_segment;
-    const int32_t u = second ? t - of_segment : t;
-    Stage st = {buffer_of((second ? pa[1] : pa[0]) + u * step_a), buffer_of(pa[1] + u * step_a),
-                buffer_of((second ? pb[1] : pb[0]) + u * step_b), lds + slot * S::STAGE_BYTES, g.k - u * K};
-    if (t >= end) st.a[2] = st.a1[2] = st.b[2] = 0;
-    return st;
+  Stage st;
+  int32_t lt = begin, plain = -1;  // the stage to be loaded; up to this one, the next lies behind the one before
+  auto forward = [](int32x4& buf, int64_t step) {
+    const uint64_t p = ((uint64_t)(uint32_t)buf[1] << 32 | (uint32_t)buf[0]) + (uint64_t)step;
+    buf[0] = (int32_t)(uint32_t)p;
+    buf[1] = (int32_t)(uint32_t)(p >> 32);
   };
-  auto load = [&](const Stage& st, int i) {
-    if (i < TA::LOADS)
-      ta.load(i, st.at, st.a, st.a1, wave, lane, st.left);
+  const int64_t step_a = FA == BY_ROWS ? 128 : K * g.a.stride, step_b = FB == BY_ROWS ? 128 : K * g.b.stride;
+  auto next_stage = [&](int slot) {
+    st.at = lds + slot * S::STAGE_BYTES;
+    if (lt < plain) {
+      forward(st.a, step_a);
+      if (MODE == DUAL) forward(st.a1, step_a);
+      forward(st.b, step_b);
+      ++lt;
+      return;
+    }
+    const bool second = MODE == SEGMENTS && lt >= of_segment;
+    const int32_t u = second ? lt - of_segment : lt;
+    const int64_t k = MASKED || u == 0 ? (int64_t)u * K : first_k + (int64_t)(u - 1) * K;
+    const int32_t left = MASKED ? g.k - u * K : u == 0 ? first_k : K;
+    const int64_t ka = a0 + k * (FA == BY_ROWS ? (int64_t)sizeof(T) : g.a.stride);
+    const int64_t kb = b0 + k * (FB == BY_ROWS ? (int64_t)sizeof(T) : g.b.stride);
+    st.a = TA::buffer((const char*)g.a.p[second] + ka, g.a.stride, left);
+    if (MODE == DUAL) st.a1 = TA::buffer((const char*)g.a.p[1] + ka, g.a.stride, left);
+    st.b = TB::buffer((const char*)g.b.p[second] + kb, g.b.stride, left);
+    st.left = left < K ? left : K;
+    if (lt < end) {
+      ++lt;
+      // (the whole stages behind it, of its segment)
+      const int32_t whole = MASKED ? (second ? of_segment : 0) + g.k / K : u == 0 && first_k < K ? lt : end;
+      plain = whole < end ? whole : end;
+    } else {
+      st.a[2] = st.b[2] = 0;
+      if (MODE == DUAL) st.a1[2] = 0;
+    }
+    // (arguments may have been loaded: with those on their way, the wait for one operand from LDS would be one for all)
+    __builtin_amdgcn_s_waitcnt(0xc07f);
+  };
+  auto load = [&](int i, auto masked) {
+    constexpr bool M = decltype(masked)::value;
+    if (i < TA::GROUPS)
+      ta.template load<M>(i, st.at, st.a, MODE == DUAL ? st.a1 : st.a, wave, lane, st.left);
     else
-      tb.load(i - TA::LOADS, st.at + TA::BYTES, st.b, st.b, wave, lane, st.left);
+      tb.template load<M>(i - TA::GROUPS, st.at + TA::BYTES, st.b, st.b, wave, lane, st.left);
   };
 
   Reader<T, FA, S::BM> ra;
@@ -267,7 +344,6 @@ __global__ void __launch_bounds__(64 * S::WAVES, (S::WGS * S::WAVES + 3) / 4) pr
     for (int j = 0; j < NI; ++j)
 #pragma unroll
       for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.f;
-
   product_u4 fa[2][MI], fb[2][NI];
   // operand i of a step's MI + NI
   auto read = [&](uint32_t at, int step, int to, int i) {
@@ -276,7 +352,7 @@ __global__ void __launch_bounds__(64 * S::WAVES, (S::WGS * S::WAVES + 3) / 4) pr
     else
       fa[to][i - NI] = ra.read(at, i - NI, step);
   };
-  // the products of a step, between(n) after the n-th of `BLOCKS`
+  // the products of a step, between(n) after the n-th of BLOCKS
   constexpr int BLOCKS = MI * NI, READS = MI + NI;
   auto products = [&](int of, auto between) {
 #pragma unroll
@@ -297,9 +373,9 @@ __global__ void __launch_bounds__(64 * S::WAVES, (S::WGS * S::WAVES + 3) / 4) pr
   };
 #pragma unroll
   for (int s = 0; s < S::STAGES; ++s) {
-    const Stage st = stage_of(begin + s, s);
+    next_stage(s);
 #pragma unroll
-    for (int i = 0; i < LOADS; ++i) load(st, i);
+    for (int i = 0; i < GROUPS; ++i) load(i, std::true_type{});
   }
   wait_loads<LOADS * (S::STAGES - 1)>();
   meet();
@@ -317,57 +393,128 @@ __global__ void __launch_bounds__(64 * S::WAVES, (S::WGS * S::WAVES + 3) / 4) pr
       });
     wait_loads<LOADS * (S::STAGES - 2)>();
     meet();
-    const Stage st = stage_of(t + S::STAGES, slot);
+    next_stage(slot);
     products(1, [&](int n) {
 #pragma unroll
       for (int i = n * READS / BLOCKS; i < (n + 1) * READS / BLOCKS; ++i) read(there, 0, 0, i);  // (behind the last stage: of no use)
 #pragma unroll
-      for (int i = n * LOADS / BLOCKS; i < (n + 1) * LOADS / BLOCKS; ++i) load(st, i);
+      for (int i = n * GROUPS / BLOCKS; i < (n + 1) * GROUPS / BLOCKS; ++i) load(i, std::integral_constant<bool, MASKED>{});
     });
     slot = next;
   }
   wait_loads<0>();
-  const Place at{m0 + wave_m * MI * (DUAL ? 16 : 32), n0 + wave_n * NI * 32, split, tm, wave_m, wave_n, lane};
+  __syncthreads();  // (what came behind the last stage is there, for all waves: the stages' LDS is free)
+  if (S::MANY) {
+    // (the last products' sums are read in sum_of, where the compiler does not see it: their 16 passes are over here)
+    asm volatile("s_nop 15\n\ts_nop 15\n\ts_nop 15" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+  }
+  const Place at{m0 + (MODE == DUAL ? wave_m * MI / 2 : wave_m * MI) * 32, n0 + wave_n * NI * 32, split, tile_m, wave_m, wave_n, lane};
   epilogue.template operator()<S, MI, NI>(acc, at, smem);
 }
 
-// four values as T at p (aligned to them)
 template <typename T>
-__device__ __forceinline__ void store4(T* p, const float* v) {
+using Four = typename std::conditional<sizeof(T) == 2, uint2, float4>::type;  // four successive values
+template <typename T>
+__device__ __forceinline__ Four<T> pack4(const float* v) {
   if constexpr (sizeof(T) == 2)
-    *reinterpret_cast<uint2*>(p) = make_uint2(cvt_pk_bf16(v[0], v[1]), cvt_pk_bf16(v[2], v[3]));
+    return make_uint2(cvt_pk_bf16(v[0], v[1]), cvt_pk_bf16(v[2], v[3]));
   else
-    *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1], v[2], v[3]);
+    return make_float4(v[0], v[1], v[2], v[3]);
 }
 template <typename T>
-__device__ __forceinline__ void fetch4(const T* p, float* v) {
+__device__ __forceinline__ void unpack4(Four<T> w, float* v) {
   if constexpr (sizeof(T) == 2) {
-    const uint2 w = *reinterpret_cast<const uint2*>(p);
     v[0] = __uint_as_float(w.x << 16); v[1] = __uint_as_float(w.x & 0xffff0000u);
     v[2] = __uint_as_float(w.y << 16); v[3] = __uint_as_float(w.y & 0xffff0000u);
   } else {
-    const float4 w = *reinterpret_cast<const float4*>(p);
     v[0] = w.x; v[1] = w.y; v[2] = w.z; v[3] = w.w;
   }
 }
+template <typename T>
+__device__ __forceinline__ void store4(T* p, const float* v) { *reinterpret_cast<Four<T>*>(p) = pack4<T>(v); }
+template <typename T>
+__device__ __forceinline__ void fetch4(const T* p, float* v) { unpack4<T>(*reinterpret_cast<const Four<T>*>(p), v); }
 
-// Calls f(i, j, row, feature, values) for every four sums of successive features that exist (features come in fours).
-template <int MI, int NI, typename F>
-__device__ __forceinline__ void each4(floatx16 (&acc)[MI][NI], const Place& at, int64_t features, int64_t rows, F f) {
-  const int l = at.lane & 31, h = at.lane >> 5;
+// 32 rows of NB blocks of 32 features between the accumulators' layout (lane l: row l % 32, four features of every eight) and
+// whole rows, 16 bytes a lane, through a wave's own LDS; 16-byte chunk c of row r lies at c ^ r.
+template <typename T, int NB>
+struct Turn {
+  static constexpr int RB = NB * 32 * (int)sizeof(T), CHUNKS = RB / 16, ROWS = 64 / CHUNKS, TURNS = 32 / ROWS;
+  static_assert(32 * RB <= 8192, "a wave's LDS");
+  char* mine;
+  int lane;
+  // bytes: of a wave's LDS; the rows lie `from` bytes behind its first
+  __device__ __forceinline__ Turn(const Place& at, char* smem, int bytes, int from = 0) : mine(smem + (threadIdx.x >> 6) * bytes + from), lane(at.lane) {}
+  static __device__ __forceinline__ void order() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
+  // the four features 32 i + 8 q + 4 (lane / 32) of the lane's row
+  __device__ __forceinline__ T* four(int i, int q) const {
+    const int r = lane & 31, byte = (32 * i + 8 * q + 4 * (lane >> 5)) * (int)sizeof(T);
+    return reinterpret_cast<T*>(mine + r * RB + (((byte >> 4) ^ (r & (CHUNKS - 1))) << 4) + (byte & 15));
+  }
+  // (a fence: or the sums of many blocks crowd into registers)
+  __device__ __forceinline__ void put4(int i, int q, const float* v) const {
+    store4(four(i, q), v);
+    __builtin_amdgcn_sched_barrier(0);
+  }
+  // the lane's chunk of rows ROWS n ..
+  __device__ __forceinline__ int row(int n) const { return n * ROWS + lane / CHUNKS; }
+  __device__ __forceinline__ int column() const { return lane % CHUNKS * (16 / (int)sizeof(T)); }
+  __device__ __forceinline__ product_u4* chunk(int n) const {
+    return reinterpret_cast<product_u4*>(mine + row(n) * RB + (((lane % CHUNKS) ^ (row(n) & (CHUNKS - 1))) << 4));
+  }
+  // where the chunk lies behind the first of rows ROWS n .., in bytes (a stride is at most 2^23 of them)
+  __device__ __forceinline__ uint32_t behind(int64_t stride) const {
+    return (uint32_t)(lane / CHUNKS) * (uint32_t)(stride * (int64_t)sizeof(T)) + (uint32_t)(lane % CHUNKS) * 16;
+  }
+  // To memory: rows `from` .. of `rows`, `width` features of each.  out(r), the same for the whole wave: where rows ROWS n .. begin.
+  template <typename F>
+  __device__ __forceinline__ void store(int64_t rows, int64_t width, int64_t stride, F out, int64_t from = 0) const {
+    order();
+    product_u4 v[TURNS];
 #pragma unroll
-  for (int j = 0; j < NI; ++j) {
-    const int64_t row = at.row + 32 * j + l;
-    if (row >= rows) continue;
+    for (int n = 0; n < TURNS; ++n) v[n] = *chunk(n);
+    order();
+    const uint32_t at = behind(stride);
 #pragma unroll
-    for (int i = 0; i < MI; ++i)
+    for (int n = 0; n < TURNS; ++n)
+      if (row(n) >= from && row(n) < rows && column() < width)
+        *(__attribute__((address_space(1))) product_u4*)(uniform(reinterpret_cast<const char*>(out(n * ROWS))) + at) = v[n];
+    __builtin_amdgcn_sched_barrier(0);  // (the next rows' values do not crowd in here)
+  }
+  struct Rows {
+    product_u4 v[TURNS];
+  };
+  template <typename F>
+  __device__ __forceinline__ Rows fetch(int64_t rows, int64_t width, int64_t stride, F in) const {
+    Rows x;
+    const uint32_t at = behind(stride);
 #pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        const int64_t m = at.feature + 32 * i + 8 * q + 4 * h;
-        if (m >= features) continue;
-        const float v[4] = {acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
-        f(row, m, v);
-      }
+    for (int n = 0; n < TURNS; ++n) {
+      x.v[n] = product_u4{0, 0, 0, 0};
+      if (row(n) < rows && column() < width)
+        x.v[n] = *(const __attribute__((address_space(1))) product_u4*)(uniform(reinterpret_cast<const char*>(in(n * ROWS))) + at);
+    }
+    return x;
+  }
+  __device__ __forceinline__ void put(const Rows& x) const {
+    order();
+#pragma unroll
+    for (int n = 0; n < TURNS; ++n) *chunk(n) = x.v[n];
+    order();
+  }
+};
+
+// Register r of a block of sums.  Shapes with MANY have them in accumulation registers, from where they are taken one by one: left to the
+// compiler, whole blocks come at once and do not fit.
+template <typename S>
+__device__ __forceinline__ float sum_of(const floatx16& block, int r) {
+  if constexpr (S::MANY) {
+    float v;
+    asm volatile("v_accvgpr_read_b32 %0, %1" : "=v"(v) : "a"(block[r]));
+    return v;
+  } else {
+    return block[r];
   }
 }
 
@@ -378,10 +525,26 @@ struct StoreProduct {
   int64_t stride[2], second;
   int64_t features, rows;
   template <typename S, int MI, int NI>
-  __device__ __forceinline__ void operator()(floatx16 (&acc)[MI][NI], const Place& at, char*) const {
-    each4<MI, NI>(acc, at, features, rows, [&](int64_t row, int64_t m, const float* v) {
-      store4(row < second ? out[0] + row * stride[0] + m : out[1] + (row - second) * stride[1] + m, v);
-    });
+  __device__ __forceinline__ void operator()(floatx16 (&acc)[MI][NI], const Place& at, char* smem) const {
+    const Turn<T, MI> turn(at, smem, S::TURN);
+#pragma unroll
+    for (int j = 0; j < NI; ++j) {
+      const int64_t first = at.row + 32 * j;
+#pragma unroll
+      for (int i = 0; i < MI; ++i)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          float v[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) v[e] = sum_of<S>(acc[i][j], 4 * q + e);
+          turn.put4(i, q, v);
+        }
+      const int64_t left = rows - first, here = second - first;  // rows of the block, and of them to out[0]
+      if (here > 0)
+        turn.store(left < here ? left : here, features - at.feature, stride[0], [&](int r) { return out[0] + (first + r) * stride[0] + at.feature; });
+      if (here < 32)
+        turn.store(left, features - at.feature, stride[1], [&](int r) { return out[1] + (r - here) * stride[1] + at.feature; }, here);
+    }
   }
 };
 // C as fp32 into the split's own [rows][features], or added to what is there
@@ -391,16 +554,26 @@ struct StorePart {
   int32_t add;
   template <typename S, int MI, int NI>
   __device__ __forceinline__ void operator()(floatx16 (&acc)[MI][NI], const Place& at, char*) const {
+    const int l = at.lane & 31, h = at.lane >> 5;
     float* const mine = out + (int64_t)at.split * rows * features;
-    each4<MI, NI>(acc, at, features, rows, [&](int64_t row, int64_t m, const float* v) {
-      float w[4] = {v[0], v[1], v[2], v[3]};
-      if (add) {
-        fetch4(mine + row * features + m, w);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) w[e] += v[e];
-      }
-      store4(mine + row * features + m, w);
-    });
+    for (int j = 0; j < NI; ++j) {
+      const int64_t row = at.row + 32 * j + l;
+      if (row >= rows) continue;
+#pragma unroll
+      for (int i = 0; i < MI; ++i)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const int64_t m = at.feature + 32 * i + 8 * q + 4 * h;
+          if (m >= features) continue;  // (features come in fours)
+          float w[4] = {0.f, 0.f, 0.f, 0.f};
+          if (add) fetch4(mine + row * features + m, w);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) w[e] += sum_of<S>(acc[i][j], 4 * q + e);
+          store4(mine + row * features + m, w);
+          __builtin_amdgcn_sched_barrier(0);
+        }
+    }
   }
 };
 
@@ -431,39 +604,40 @@ hipError_t join_parts(const float* parts, int32_t n, int64_t features, int64_t r
 // Which tiles a product gets, and into how many parts its contraction is cut.
 struct Plan {
   int shape, splits;
-  int64_t bm() const { return shape == LARGE ? 256 : shape == MIDDLE ? 128 : 64; }
-  int64_t bn() const { return shape == LARGE ? 256 : shape == MIDDLE ? 128 : shape == FEW64 ? 64 : 32; }
+  int64_t size() const { return shape == LARGE ? 256 : shape == MIDDLE ? 128 : 64; }  // of a tile
 };
-// The least time by a simple account, in us: a round of workgroups takes its stages and `fixed` for its start and end; a stage takes
-// `busy` where every place for a workgroup is taken, less where few are, `alone` at least.
+// The least time by a simple account, in us: workgroups go in rounds of as many as run at a time.  Each takes `fixed` for its start and
+// end, and for a stage the time between `idle` and `busy` that the share of the places which are taken gives, `alone` at least.  (Measured, for
+// 1 to 4096 workgroups of each shape and 64 to 8192 elements, to within a tenth or two.)  What is read comes at 5 TB/s at most.
 struct ShapeCost {
-  double busy, alone, fixed;
+  int places;
+  double alone, idle, busy, fixed;
 };
 constexpr int CUS = 256;
-inline ShapeCost shape_cost(bool f32, int shape) {
-  constexpr ShapeCost BF16[] = {{1.5, 1.2, 8.0}, {1.05, 0.6, 5.0}, {1.3, 0.7, 4.0}, {1.6, 0.7, 4.0}};
-  constexpr ShapeCost F32[] = {{0, 0, 0}, {3.6, 2.0, 5.0}, {2.0, 2.0, 4.0}, {1.7, 1.0, 4.0}};
-  return f32 ? F32[shape] : BF16[shape];
-}
-// shapes: bits of those that the caller has kernels for; k: contracted elements, of all segments
 template <typename T>
-Plan plan_product(int64_t features, int64_t rows, int64_t k, bool dual, int most_splits, int shapes = 15) {
-  constexpr int PLACES[] = {CUS, 2 * CUS, 3 * CUS, 4 * CUS};
-  const bool f32 = sizeof(T) == 4;
+ShapeCost shape_cost(int shape) {
+  if (sizeof(T) == 4) return {3 * CUS, 0.59, 0.16, 1.45, 3.0};
+  return shape == LARGE ? ShapeCost{CUS, 1.24, 1.24, 1.63, 7.0} : shape == MIDDLE ? ShapeCost{2 * CUS, 0.5, 0.48, 0.97, 4.0}
+                                                                             : ShapeCost{3 * CUS, 0.25, 0.08, 0.56, 3.0};
+}
+// k: contracted elements, of all segments
+template <typename T>
+Plan plan_product(int64_t features, int64_t rows, int64_t k, bool dual, int most_splits) {
   const int64_t stages = (k + STAGE_K<T> - 1) / STAGE_K<T>;
-  Plan best = {MIDDLE, 1};
+  const double read = (double)((dual ? 2 : 1) * features + rows) * k * sizeof(T) / 5.0e6;
+  Plan best = {SMALL, 1};
   double least = 1e30;
-  for (int shape = f32 ? MIDDLE : LARGE; shape <= FEW32; ++shape) {
-    if (!(shapes >> shape & 1)) continue;
+  for (int shape = sizeof(T) == 4 ? SMALL : LARGE; shape <= SMALL; ++shape) {
     Plan p = {shape, 1};
-    const ShapeCost c = shape_cost(f32, shape);
-    const int64_t bm = dual ? p.bm() / 2 : p.bm();
-    const int64_t tiles = ((features + bm - 1) / bm) * ((rows + p.bn() - 1) / p.bn());
+    const ShapeCost c = shape_cost<T>(shape);
+    const int64_t bm = dual ? p.size() / 2 : p.size();
+    const int64_t tiles = ((features + bm - 1) / bm) * ((rows + p.size() - 1) / p.size());
     for (p.splits = 1; p.splits <= most_splits && (p.splits == 1 || stages / p.splits >= 4); ++p.splits) {
-      const int64_t all = tiles * p.splits, full = all / PLACES[shape], rest = all % PLACES[shape], deep = (stages + p.splits - 1) / p.splits;
+      const int64_t all = tiles * p.splits, full = all / c.places, rest = all % c.places, deep = (stages + p.splits - 1) / p.splits;
       double t = (double)full * (deep * c.busy + c.fixed);
-      if (rest) t += deep * std::max(c.alone, c.busy * rest / PLACES[shape]) + c.fixed;
-      if (p.splits > 1) t += 4.0 + (double)features * rows * p.splits * 8 / 4.0e6;
+      if (rest) t += deep * std::max(c.alone, c.idle + (c.busy - c.idle) * rest / c.places) + c.fixed;
+      t = std::max(t, read);
+      if (p.splits > 1) t += 4.0 + (double)features * rows * p.splits * 8 / 4.0e6;  // (parts written and read, a launch)
       if (t < least) {
         least = t;
         best = p;
@@ -473,32 +647,30 @@ Plan plan_product(int64_t features, int64_t rows, int64_t k, bool dual, int most
   return best;
 }
 
-template <typename T, int FA, int FB, bool DUAL, typename S, typename Epilogue>
+template <typename T, int FA, int FB, int MODE, typename S, typename Epilogue>
 hipError_t launch_shape(hpd_product_args g, const Epilogue& e, hipStream_t s) {
-  const int64_t bm = DUAL ? S::BM / 2 : S::BM;
+  const int64_t bm = MODE == DUAL ? S::BM / 2 : S::BM;
   g.tiles_m = (int32_t)((g.a.size + bm - 1) / bm);
   g.tiles_n = (int32_t)((g.b.size + S::BN - 1) / S::BN);
-  product_kernel<T, FA, FB, DUAL, S, Epilogue><<<dim3((uint32_t)g.tiles_m * g.tiles_n * g.splits), dim3(64 * S::WAVES), 0, s>>>(g, e);
+  product_kernel<T, FA, FB, MODE, S, Epilogue><<<dim3((uint32_t)g.tiles_m * g.tiles_n * g.splits), dim3(64 * S::WAVES), 0, s>>>(g, e);
   return hipGetLastError();
 }
-template <typename T, int FA, int FB, bool DUAL, typename Epilogue>
+template <typename T, int FA, int FB, int MODE, typename Epilogue>
 hipError_t launch_product(Plan p, hpd_product_args g, const Epilogue& e, hipStream_t s) {
   g.splits = p.splits;
-  if constexpr (sizeof(T) == 2)
-    if (p.shape == LARGE) return launch_shape<T, FA, FB, DUAL, Large>(g, e, s);
-  if constexpr (FB == BY_ROWS) {
-    if (p.shape == FEW64) return launch_shape<T, FA, FB, DUAL, Few64>(g, e, s);
-    if (p.shape == FEW32) return launch_shape<T, FA, FB, DUAL, Few32>(g, e, s);
+  if constexpr (sizeof(T) == 2) {
+    if (p.shape == LARGE) return launch_shape<T, FA, FB, MODE, Large>(g, e, s);
+    if (p.shape == MIDDLE) return launch_shape<T, FA, FB, MODE, Middle>(g, e, s);
   }
-  return launch_shape<T, FA, FB, DUAL, Middle>(g, e, s);
+  return launch_shape<T, FA, FB, MODE, Small>(g, e, s);
 }
 
 // C as T, through parts in fp32 ([splits][rows][features] at `parts`) where the contraction is cut.
-template <typename T, int FA, int FB>
+template <typename T, int FA, int FB, int MODE = PLAIN>
 hipError_t store_product(Plan p, const hpd_product_args& g, float* parts, T* out, int64_t stride, hipStream_t s) {
   const int64_t features = g.a.size, rows = g.b.size;
-  if (p.splits == 1) return launch_product<T, FA, FB, false>(p, g, StoreProduct<T>{{out, nullptr}, {stride, 0}, rows, features, rows}, s);
-  const hipError_t e = launch_product<T, FA, FB, false>(p, g, StorePart{parts, features, rows, 0}, s);
+  if (p.splits == 1) return launch_product<T, FA, FB, MODE>(p, g, StoreProduct<T>{{out, nullptr}, {stride, 0}, rows, features, rows}, s);
+  const hipError_t e = launch_product<T, FA, FB, MODE>(p, g, StorePart{parts, features, rows, 0}, s);
   return e != hipSuccess ? e : join_parts(parts, p.splits, features, rows, out, stride, s);
 }
 
