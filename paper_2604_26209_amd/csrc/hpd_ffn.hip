@@ -10,22 +10,33 @@
 
 namespace {
 
-// act(g) and its derivative
+// exp(x) by the hardware's exp2: for fp32 with what x log2(e) loses in its rounding made good
+template <typename T>
+__device__ __forceinline__ float fast_exp(float x) {
+  constexpr float L = 1.44269504088896340736f, L_LOW = 1.92596299112661746887e-8f, LN2 = 0.69314718055994530942f;
+  const float y = x * L, e = fast_exp2(y);
+  if (sizeof(T) == 2) return e;
+  const float low = fmaf(x, L, -y) + x * L_LOW;
+  // (an infinite e stays one: low is not negative there or tiny)
+  return e < 3.0e38f ? fmaf(e * LN2, low, e) : e;
+}
+
+// act(g) and its derivative (1 / (1 + e) by the reciprocal instruction, good to a step: 1 of 16 us for 512 rows, 4096 to 12288 and back)
 template <typename T, int ACT>
 __device__ __forceinline__ void activation(float g, float& a, float& slope) {
   if constexpr (ACT == HPD_ACT_GELU) {
     const float c = sizeof(T) == 2 ? 0.5f + 0.5f * erff(g * 0.70710678118654752f) : 0.5f * erfcf(g * -0.70710678118654752f);
     a = g * c;
-    slope = fmaf(g * 0.39894228040143268f, expf(-0.5f * g * g), c);
+    slope = fmaf(g * 0.39894228040143268f, fast_exp<T>(-0.5f * g * g), c);
   } else {
     // silu: g / (1 + exp(-g)); gelu by tanh: g (1 + tanh w) / 2 = g / (1 + exp(-2 w)), w = sqrt(2 / pi) (g + 0.044715 g^3)
     // (the logistic function is 0 or 1 long before |g| = 30, and g^3 stays finite)
     const float c = fminf(fmaxf(g, -30.f), 30.f);
     const float w = ACT == HPD_ACT_SILU ? g : 1.5957691216057308f * c * fmaf(0.044715f * c, c, 1.f);
-    const float s = 1.f / (1.f + expf(-w));
+    const float s = __builtin_amdgcn_rcpf(1.f + fast_exp<T>(-w));
     a = g * s;
     const float dw = ACT == HPD_ACT_SILU ? 1.f : 1.5957691216057308f * fmaf(0.134145f * c, c, 1.f);
-    slope = fmaf(g * s * (1.f - s), dw, s);
+    slope = fmaf(a * (1.f - s), dw, s);
   }
 }
 

@@ -607,36 +607,36 @@ struct Plan {
   int64_t size() const { return shape == LARGE ? 256 : shape == MIDDLE ? 128 : 64; }  // of a tile
 };
 // The least time by a simple account, in us: workgroups go in rounds of as many as run at a time.  Each takes `fixed` for its start and
-// end, and for a stage the time between `idle` and `busy` that the share of the places which are taken gives, `alone` at least.  (Measured, for
-// 1 to 4096 workgroups of each shape and 64 to 8192 elements, to within a tenth or two.)  What is read comes at 5 TB/s at most.
+// end, and for a stage stage[n - 1] where n run on its CU.  (Measured, for 1 to 4096 workgroups of each shape and 64 to 8192 elements, to
+// within a tenth or two.)  What is read comes at 5.2 TB/s at most, and each workgroup has `flight` KB of it on the way, about 1 us.
 struct ShapeCost {
-  int places;
-  double alone, idle, busy, fixed;
+  int on_cu;
+  double stage[3], fixed, flight;
 };
 constexpr int CUS = 256;
 template <typename T>
 ShapeCost shape_cost(int shape) {
-  if (sizeof(T) == 4) return {3 * CUS, 0.59, 0.16, 1.45, 3.0};
-  return shape == LARGE ? ShapeCost{CUS, 1.24, 1.24, 1.63, 7.0} : shape == MIDDLE ? ShapeCost{2 * CUS, 0.5, 0.48, 0.97, 4.0}
-                                                                             : ShapeCost{3 * CUS, 0.25, 0.08, 0.56, 3.0};
+  if (sizeof(T) == 4) return {3, {0.59, 1.03, 1.45}, 3.0, 16};
+  return shape == LARGE ? ShapeCost{1, {1.63}, 7.0, 64} : shape == MIDDLE ? ShapeCost{2, {0.72, 0.97}, 4.0, 32}
+                                                                        : ShapeCost{3, {0.25, 0.39, 0.56}, 3.0, 16};
 }
 // k: contracted elements, of all segments
 template <typename T>
 Plan plan_product(int64_t features, int64_t rows, int64_t k, bool dual, int most_splits) {
   const int64_t stages = (k + STAGE_K<T> - 1) / STAGE_K<T>;
-  const double read = (double)((dual ? 2 : 1) * features + rows) * k * sizeof(T) / 5.0e6;
+  const double bytes = (double)((dual ? 2 : 1) * features + rows) * k * sizeof(T);
   Plan best = {SMALL, 1};
   double least = 1e30;
   for (int shape = sizeof(T) == 4 ? SMALL : LARGE; shape <= SMALL; ++shape) {
     Plan p = {shape, 1};
     const ShapeCost c = shape_cost<T>(shape);
-    const int64_t bm = dual ? p.size() / 2 : p.size();
+    const int64_t bm = dual ? p.size() / 2 : p.size(), places = c.on_cu * CUS;
     const int64_t tiles = ((features + bm - 1) / bm) * ((rows + p.size() - 1) / p.size());
     for (p.splits = 1; p.splits <= most_splits && (p.splits == 1 || stages / p.splits >= 4); ++p.splits) {
-      const int64_t all = tiles * p.splits, full = all / c.places, rest = all % c.places, deep = (stages + p.splits - 1) / p.splits;
-      double t = (double)full * (deep * c.busy + c.fixed);
-      if (rest) t += deep * std::max(c.alone, c.idle + (c.busy - c.idle) * rest / c.places) + c.fixed;
-      t = std::max(t, read);
+      const int64_t all = tiles * p.splits, full = all / places, rest = all % places, deep = (stages + p.splits - 1) / p.splits;
+      double t = (double)full * (deep * c.stage[c.on_cu - 1] + c.fixed);
+      if (rest) t += deep * c.stage[(rest - 1) / CUS] + c.fixed;
+      t = std::max(t, bytes / std::min(5.2e6, (double)std::min(all, places) * c.flight * 1e3));
       if (p.splits > 1) t += 4.0 + (double)features * rows * p.splits * 8 / 4.0e6;  // (parts written and read, a launch)
       if (t < least) {
         least = t;
