@@ -186,8 +186,8 @@ struct BackwardPlan {
   BackwardPlan(const hpd_ffn_config& c, int64_t n) {
     inner = plan_product<T>(c.inner, n, c.width, false, 1);
     dx = plan_product<T>(c.width, n, 2 * (int64_t)c.inner, false, MOST_SPLITS);
-    in_weights = plan_product<T>(c.width, 2 * (int64_t)c.inner, n, false, 1);
-    down_weights = plan_product<T>(c.inner, c.width, n, false, 1);
+    in_weights = plan_product<T>(c.width, 2 * (int64_t)c.inner, n, false, 1, false);
+    down_weights = plan_product<T>(c.inner, c.width, n, false, 1, false);
     h = round16(n * 2 * c.inner * (int64_t)sizeof(T));
     parts = h + round16(n * c.inner * (int64_t)sizeof(T));
     bytes = parts + part_bytes(dx, n, c.width);

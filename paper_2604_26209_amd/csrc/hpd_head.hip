@@ -204,7 +204,7 @@ struct ForwardPlan {
   int64_t tiles, of_target, bytes;
   ForwardPlan(int64_t n, int32_t width, int32_t vocab) {
     product = plan_product<T>(vocab, n, width, false, 1);
-    tiles = (vocab + product.size() - 1) / product.size();
+    tiles = (vocab + product.bm() - 1) / product.bm();
     of_target = n * tiles * (int64_t)sizeof(float4);
     bytes = round16(of_target + n * 4);
   }
@@ -221,7 +221,7 @@ struct BackwardPlan {
     piece = ((vocab + pieces - 1) / pieces + UNIT - 1) / UNIT * UNIT;
     logits = plan_product<T>(std::min<int64_t>(piece, vocab), n, width, false, 1);
     d_hidden = plan_product<T>(width, n, std::min<int64_t>(piece, vocab), false, MOST_SPLITS);
-    d_weight = plan_product<T>(width, std::min<int64_t>(piece, vocab), n, false, 1);
+    d_weight = plan_product<T>(width, std::min<int64_t>(piece, vocab), n, false, 1, false);
     parts = round16(n * piece * (int64_t)sizeof(T));
     bytes = parts + d_hidden.splits * n * width * 4;
   }

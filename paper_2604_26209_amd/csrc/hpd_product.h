@@ -57,30 +57,38 @@ __device__ __forceinline__ int32x4 buffer_of(const char* p, uint32_t bytes) {
           __builtin_amdgcn_readfirstlane((int32_t)bytes), 0x00027000};
 }
 // N loads of 64 x 16 bytes to successive KB of LDS, lane i's at + 16 i.  The instruction's offset moves both addresses, so the
-// lanes' offsets are n KB less for load n, and BIAS more.  (M0 is the compiler's.)
+// lanes' offsets are n KB less for load n, and BIAS more.  (M0 is the compiler's.)  ONCE: the bytes will not be asked for again, the caches
+// need not keep them.
 constexpr uint32_t BIAS = 4096;
-template <int N>
+template <int N, bool ONCE>
 __device__ __forceinline__ void load_to_lds(uint32_t lds, const uint32_t* off, int32x4 buf) {
   uint32_t keep;
-  if constexpr (N == 4)
-    asm volatile(
-        "s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\t"
-        "buffer_load_dwordx4 %2, %6, 0 offen lds\n\t"
-        "buffer_load_dwordx4 %3, %6, 0 offen offset:1024 lds\n\t"
-        "buffer_load_dwordx4 %4, %6, 0 offen offset:2048 lds\n\t"
-        "buffer_load_dwordx4 %5, %6, 0 offen offset:3072 lds\n\t"
-        "s_mov_b32 m0, %0"
-        : "=&s"(keep) : "s"(lds), "v"(off[0]), "v"(off[1]), "v"(off[2]), "v"(off[3]), "s"(buf) : "memory");
-  else if constexpr (N == 1)
-    asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\tbuffer_load_dwordx4 %2, %3, 0 offen lds\n\ts_mov_b32 m0, %0"
+#define HPD_LOADS_TO_LDS(HINT)                                                                                              \
+  if constexpr (N == 4)                                                                                                     \
+    asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\t"                                                      \
+                 "buffer_load_dwordx4 %2, %6, 0 offen" HINT " lds\n\t"                                                      \
+                 "buffer_load_dwordx4 %3, %6, 0 offen offset:1024" HINT " lds\n\t"                                          \
+                 "buffer_load_dwordx4 %4, %6, 0 offen offset:2048" HINT " lds\n\t"                                          \
+                 "buffer_load_dwordx4 %5, %6, 0 offen offset:3072" HINT " lds\n\t"                                          \
+                 "s_mov_b32 m0, %0"                                                                                         \
+                 : "=&s"(keep) : "s"(lds), "v"(off[0]), "v"(off[1]), "v"(off[2]), "v"(off[3]), "s"(buf) : "memory");        \
+  else if constexpr (N == 2)                                                                                                \
+    asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\t"                                                      \
+                 "buffer_load_dwordx4 %2, %4, 0 offen" HINT " lds\n\t"                                                      \
+                 "buffer_load_dwordx4 %3, %4, 0 offen offset:1024" HINT " lds\n\t"                                          \
+                 "s_mov_b32 m0, %0"                                                                                         \
+                 : "=&s"(keep) : "s"(lds), "v"(off[0]), "v"(off[1]), "s"(buf) : "memory");                                  \
+  else                                                                                                                      \
+    asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\t"                                                      \
+                 "buffer_load_dwordx4 %2, %3, 0 offen" HINT " lds\n\t"                                                      \
+                 "s_mov_b32 m0, %0"                                                                                         \
                  : "=&s"(keep) : "s"(lds), "v"(off[0]), "s"(buf) : "memory");
-  else
-    asm volatile(
-        "s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\t"
-        "buffer_load_dwordx4 %2, %4, 0 offen lds\n\t"
-        "buffer_load_dwordx4 %3, %4, 0 offen offset:1024 lds\n\t"
-        "s_mov_b32 m0, %0"
-        : "=&s"(keep) : "s"(lds), "v"(off[0]), "v"(off[1]), "s"(buf) : "memory");
+  if constexpr (ONCE) {
+    HPD_LOADS_TO_LDS(" nt")
+  } else {
+    HPD_LOADS_TO_LDS("")
+  }
+#undef HPD_LOADS_TO_LDS
 }
 __device__ __forceinline__ uint32_t product_lds(const void* p) {
   return (uint32_t)reinterpret_cast<uintptr_t>((const __attribute__((address_space(3))) char*)p);
@@ -100,7 +108,7 @@ __device__ __forceinline__ void wait_loads() {
 }
 
 // One operand's tile of R rows (or columns) in a workgroup of WAVES waves.
-template <typename T, int FORM, int R, int WAVES, bool DUAL>
+template <typename T, int FORM, int R, int WAVES, bool DUAL, bool ONCE = false>
 struct Tile {
   static constexpr int BYTES = R * 128;
   static constexpr int LOADS = R / 8 / WAVES;        // load instructions of a wave and stage, issued in groups
@@ -147,7 +155,7 @@ struct Tile {
 #pragma unroll
     for (int e = 0; e < GROUP; ++e)
       o[e] = MASKED && FORM == BY_ROWS && chunk_of(f + e, lane) * CHUNK<T> >= left ? OUTSIDE : off[i * GROUP + e];
-    load_to_lds<GROUP>(__builtin_amdgcn_readfirstlane(lds + f * 1024), o, DUAL && (f >> 2 & 1) ? b1 : b0);
+    load_to_lds<GROUP, ONCE>(__builtin_amdgcn_readfirstlane(lds + f * 1024), o, DUAL && (f >> 2 & 1) ? b1 : b0);
   }
 };
 
@@ -202,8 +210,9 @@ __device__ __forceinline__ floatx16 multiply(product_u4 a, product_u4 b, floatx1
 // Shapes of tiles: BM x BN by WM x WN waves, STAGES stages in LDS, WGS workgroups on a CU.  (Workgroups that stay and make tile after
 // tile, the next one's first stages on their way while one is stored, are slower: 8192 x 8192 x 8192 in 880 us, 840 as it is; CUs do
 // not all run at one rate, and a tile goes to the one that is free.)
-template <int BM_, int BN_, int WM_, int WN_, int STAGES_, int WGS_>
+template <int BM_, int BN_, int WM_, int WN_, int STAGES_, int WGS_, bool ONCE_ = false>
 struct Shape {
+  static constexpr bool ONCE = ONCE_;  // no other workgroup reads the tile's A
   static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, STAGES = STAGES_, WGS = WGS_;
   static constexpr int WAVES = WM * WN, MI = BM / 32 / WM, NI = BN / 32 / WN;
   static constexpr int STAGE_BYTES = (BM + BN) * 128;
@@ -212,12 +221,15 @@ struct Shape {
 };
 enum { PLAIN = 0, DUAL = 1, SEGMENTS = 2 };
 // bf16 products of 4096 elements: Large 1.2 PFLOP/s for 4096 x 4096 and more; Middle 1.06 from 4096 x 2048 (Large 0.72); Small 0.61 for
-// 2048 x 1024 (Middle 0.39), and with one to 64 rows the rate of memory, 6.7 TB/s of weights that the caches hold, 5.2 of others.  fp32:
-// Small alone, 0.13 to 0.14 from 2048 x 1024 on (128 x 128 with eight waves: 0.146 at most, 0.07 for 2048 x 1024).
+// 2048 x 1024 (Middle 0.39).  Few rows, where the weights' bytes are what it takes: Few32 5.9 TB/s for 24576 features and a row, 6.4 for
+// 48000 (without the hint that the weights will not be read again 5.3 and 5.8; Small 4.9 and 5.5), Few64 4.5 for 64 rows (Small 4.2).  fp32:
+// Small 0.13 to 0.14 PFLOP/s from 2048 x 1024 on (128 x 128 with eight waves: 0.146 at most, 0.07 for 2048 x 1024), and Few.
 using Large = Shape<256, 256, 2, 2, 2, 1>;
 using Middle = Shape<128, 128, 2, 4, 2, 2>;
 using Small = Shape<64, 64, 2, 2, 3, 3>;
-enum { LARGE = 0, MIDDLE = 1, SMALL = 2 };
+using Few64 = Shape<64, 64, 2, 2, 4, 2, true>;
+using Few32 = Shape<64, 32, 2, 1, 4, 3, true>;
+enum { LARGE = 0, MIDDLE = 1, SMALL = 2, FEW64 = 3, FEW32 = 4 };
 
 // f(0) .. f(N - 1), the numbers as types: what is indexed with them stays in registers however long f is
 template <int N, typename F, int I = 0>
@@ -251,7 +263,7 @@ __device__ __forceinline__ void tile_of(int32_t id, int32_t total, int32_t tiles
 
 template <typename T, int FA, int FB, int MODE, typename S, typename Epilogue>
 __global__ void __launch_bounds__(64 * S::WAVES, (S::WGS * S::WAVES + 3) / 4) product_kernel(hpd_product_args g, Epilogue epilogue) {
-  using TA = Tile<T, FA, S::BM, S::WAVES, MODE == DUAL>;
+  using TA = Tile<T, FA, S::BM, S::WAVES, MODE == DUAL, S::ONCE>;
   using TB = Tile<T, FB, S::BN, S::WAVES, false>;
   constexpr int MI = S::MI, NI = S::NI, K = STAGE_K<T>, LOADS = TA::LOADS + TB::LOADS, GROUPS = TA::GROUPS + TB::GROUPS;
   // The stage with less than a whole stage's elements is the first, which is loaded in front of the loop; of two segments, the
@@ -604,39 +616,42 @@ hipError_t join_parts(const float* parts, int32_t n, int64_t features, int64_t r
 // Which tiles a product gets, and into how many parts its contraction is cut.
 struct Plan {
   int shape, splits;
-  int64_t size() const { return shape == LARGE ? 256 : shape == MIDDLE ? 128 : 64; }  // of a tile
+  int64_t bm() const { return shape == LARGE ? 256 : shape == MIDDLE ? 128 : 64; }
+  int64_t bn() const { return shape == FEW32 ? 32 : bm(); }
 };
 // The least time by a simple account, in us: workgroups go in rounds of as many as run at a time.  Each takes `fixed` for its start and
 // end, and for a stage stage[n - 1] where n run on its CU.  (Measured, for 1 to 4096 workgroups of each shape and 64 to 8192 elements, to
-// within a tenth or two.)  What is read comes at 5.2 TB/s at most, and each workgroup has `flight` KB of it on the way, about 1 us.
+// within a tenth or two.)  What is read comes at `rate` TB/s at most, and each workgroup has `flight` KB of it on the way, about 1 us.
 struct ShapeCost {
   int on_cu;
-  double stage[3], fixed, flight;
+  double stage[3], fixed, flight, rate;
 };
 constexpr int CUS = 256;
 template <typename T>
 ShapeCost shape_cost(int shape) {
-  if (sizeof(T) == 4) return {3, {0.59, 1.03, 1.45}, 3.0, 16};
-  return shape == LARGE ? ShapeCost{1, {1.63}, 7.0, 64} : shape == MIDDLE ? ShapeCost{2, {0.72, 0.97}, 4.0, 32}
-                                                                        : ShapeCost{3, {0.25, 0.39, 0.56}, 3.0, 16};
+  constexpr ShapeCost BF16[] = {{1, {1.63}, 7.0, 64, 5.2}, {2, {0.72, 0.97}, 4.0, 32, 5.2}, {3, {0.25, 0.39, 0.56}, 3.0, 16, 5.2},
+                                {2, {0.25, 0.39}, 3.0, 24, 5.7}, {3, {0.25, 0.3, 0.4}, 3.0, 24, 5.9}};
+  constexpr ShapeCost F32[] = {{}, {}, {3, {0.59, 1.03, 1.45}, 3.0, 16, 5.2}, {2, {0.59, 1.03}, 3.0, 24, 5.7}, {3, {0.35, 0.55, 0.75}, 3.0, 24, 5.9}};
+  return sizeof(T) == 4 ? F32[shape] : BF16[shape];
 }
-// k: contracted elements, of all segments
+// k: contracted elements, of all segments; by_rows: the rows' operand lies by rows (there are kernels for few of them)
 template <typename T>
-Plan plan_product(int64_t features, int64_t rows, int64_t k, bool dual, int most_splits) {
+Plan plan_product(int64_t features, int64_t rows, int64_t k, bool dual, int most_splits, bool by_rows = true) {
   const int64_t stages = (k + STAGE_K<T> - 1) / STAGE_K<T>;
   const double bytes = (double)((dual ? 2 : 1) * features + rows) * k * sizeof(T);
   Plan best = {SMALL, 1};
   double least = 1e30;
-  for (int shape = sizeof(T) == 4 ? SMALL : LARGE; shape <= SMALL; ++shape) {
+  for (int shape = sizeof(T) == 4 ? SMALL : LARGE; shape <= FEW32; ++shape) {
     Plan p = {shape, 1};
+    if (shape >= FEW64 && (!by_rows || rows > p.bn())) continue;
     const ShapeCost c = shape_cost<T>(shape);
-    const int64_t bm = dual ? p.size() / 2 : p.size(), places = c.on_cu * CUS;
-    const int64_t tiles = ((features + bm - 1) / bm) * ((rows + p.size() - 1) / p.size());
+    const int64_t bm = dual ? p.bm() / 2 : p.bm(), places = c.on_cu * CUS;
+    const int64_t tiles = ((features + bm - 1) / bm) * ((rows + p.bn() - 1) / p.bn());
     for (p.splits = 1; p.splits <= most_splits && (p.splits == 1 || stages / p.splits >= 4); ++p.splits) {
       const int64_t all = tiles * p.splits, full = all / places, rest = all % places, deep = (stages + p.splits - 1) / p.splits;
       double t = (double)full * (deep * c.stage[c.on_cu - 1] + c.fixed);
       if (rest) t += deep * c.stage[(rest - 1) / CUS] + c.fixed;
-      t = std::max(t, bytes / std::min(5.2e6, (double)std::min(all, places) * c.flight * 1e3));
+      t = std::max(t, bytes / std::min(c.rate * 1e6, (double)std::min(all, places) * c.flight * 1e3) + c.fixed);
       if (p.splits > 1) t += 4.0 + (double)features * rows * p.splits * 8 / 4.0e6;  // (parts written and read, a launch)
       if (t < least) {
         least = t;
@@ -661,6 +676,10 @@ hipError_t launch_product(Plan p, hpd_product_args g, const Epilogue& e, hipStre
   if constexpr (sizeof(T) == 2) {
     if (p.shape == LARGE) return launch_shape<T, FA, FB, MODE, Large>(g, e, s);
     if (p.shape == MIDDLE) return launch_shape<T, FA, FB, MODE, Middle>(g, e, s);
+  }
+  if constexpr (FB == BY_ROWS) {
+    if (p.shape == FEW64) return launch_shape<T, FA, FB, MODE, Few64>(g, e, s);
+    if (p.shape == FEW32) return launch_shape<T, FA, FB, MODE, Few32>(g, e, s);
   }
   return launch_shape<T, FA, FB, MODE, Small>(g, e, s);
 }
