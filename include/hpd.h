@@ -523,14 +523,15 @@ int hpd_token_logprobs_backward(int32_t dtype, int64_t n_rows, int32_t vocab, in
  * The two ends of a layer stack around the attention: the gated feed-forward block and the vocabulary head with the
  * log probabilities of given tokens, for training (with their gradients) and for the tokens of a decode step (few rows).
  *
- * Tensors are device memory, rows of `width`, `inner` or vocab elements of the dtype; the distance between rows
- * is a stride in elements.  They start on 16 bytes and strides are multiples of 16 bytes, up to 2^23 bytes; width and inner are
- * multiples of 8 (HPD_E_UNSUPPORTED otherwise), vocab and the number of rows are free.  Weights lie as a linear layer keeps
- * them, [outputs][inputs].
+ * Tensors are device memory, rows of `width` or `inner` elements of the dtype; the distance between rows is a stride in
+ * elements (0 = the rows lie next to each other).  They start on 16 bytes and strides are multiples of 16 bytes, up to 2^23 bytes
+ * (HPD_E_OVERFLOW beyond); width and inner are multiples of 8 (HPD_E_UNSUPPORTED otherwise), vocab and the number of rows are free.
+ * Weights lie as a linear layer keeps them, [outputs][inputs].
  * Products are accumulated in fp32 and every output is rounded once.  Under HPD_BF16 what one product hands to the next
  * (h; dg, du; the logits' gradients) is rounded to bf16, the type in which the matrix instruction takes it.
  * No output may overlap an input or the workspace (HPD_E_INVALID where they start at the same address).
- * No atomics: equal calls give equal bits.  A row's outputs depend on that row and the weights alone.
+ * No atomics: equal calls give equal bits.  A row's outputs and its gradient come from that row and the weights alone: what is not finite
+ * in a row stays there.  The weights' gradients are sums over all rows, and such a row reaches them even where its own gradient is 0.
  * The calls only enqueue kernels, allocate nothing and may be captured in a HIP graph.  Workspaces: device memory, the bytes
  * that the _workspace call reports (NULL if 0), 16-byte aligned, not shared by calls that overlap.
  */

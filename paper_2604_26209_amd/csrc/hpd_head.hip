@@ -99,35 +99,38 @@ struct RowSums {
   }
 };
 
-// a workgroup per row (a wave per row: 10 us instead of 6 for 3 rows of 1172 tiles)
-__global__ void __launch_bounds__(256) join_rows_kernel(const float4* parts, int32_t tiles, const float* of_target, const int32_t* targets,
-                                                        int32_t vocab, float* logprob, float* lse, float* entropy) {
+// a workgroup per row and round (a wave per row: 10 us instead of 5 for 3 rows of 1172 tiles)
+__global__ void __launch_bounds__(256) join_rows_kernel(const float4* parts, int32_t tiles, int64_t rows, const float* of_target,
+                                                        const int32_t* targets, int32_t vocab, float* logprob, float* lse, float* entropy) {
   __shared__ float4 of_wave[4];
-  const int64_t row = blockIdx.x;
-  const float4* const mine = parts + row * tiles;
-  Sums a = {-INFINITY, 0.f, 0.f};
-  for (int32_t i = threadIdx.x; i < tiles; i += 4 * 256) {
-    float4 v[4];
+  for (int64_t row = blockIdx.x; row < rows; row += gridDim.x) {
+    const float4* const mine = parts + row * tiles;
+    Sums a = {-INFINITY, 0.f, 0.f};
+    for (int32_t i = threadIdx.x; i < tiles; i += 4 * 256) {
+      float4 v[4];
 #pragma unroll
-    for (int n = 0; n < 4; ++n) v[n] = i + 256 * n < tiles ? mine[i + 256 * n] : make_float4(-INFINITY, 0.f, 0.f, 0.f);
+      for (int n = 0; n < 4; ++n) v[n] = i + 256 * n < tiles ? mine[i + 256 * n] : make_float4(-INFINITY, 0.f, 0.f, 0.f);
 #pragma unroll
-    for (int n = 0; n < 4; ++n) a = join(a, {v[n].x, v[n].y, v[n].z});
-  }
+      for (int n = 0; n < 4; ++n) a = join(a, {v[n].x, v[n].y, v[n].z});
+    }
 #pragma unroll
-  for (int d = 32; d; d >>= 1) a = join(a, {__shfl_xor(a.m, d), __shfl_xor(a.s, d), __shfl_xor(a.t, d)});
-  if ((threadIdx.x & 63) == 0) of_wave[threadIdx.x >> 6] = make_float4(a.m, a.s, a.t, 0.f);
-  __syncthreads();
-  if (threadIdx.x) return;
+    for (int d = 32; d; d >>= 1) a = join(a, {__shfl_xor(a.m, d), __shfl_xor(a.s, d), __shfl_xor(a.t, d)});
+    if ((threadIdx.x & 63) == 0) of_wave[threadIdx.x >> 6] = make_float4(a.m, a.s, a.t, 0.f);
+    __syncthreads();
+    if (threadIdx.x == 0) {
 #pragma unroll
-  for (int w = 1; w < 4; ++w) a = join(a, {of_wave[w].x, of_wave[w].y, of_wave[w].z});
-  const float log_s = logf(a.s), total = a.s == 0.f ? -INFINITY : a.m + log_s;
-  if (lse) lse[row] = total;
-  if (entropy) entropy[row] = a.s == 0.f ? 0.f : log_s - a.t / a.s;
-  if (logprob) {
-    const int32_t t = targets[row];
-    float v = 0.f;
-    if (t >= 0 && t < vocab) v = a.s == 0.f ? -INFINITY : (of_target[row] - a.m) - log_s;
-    logprob[row] = v;
+      for (int w = 1; w < 4; ++w) a = join(a, {of_wave[w].x, of_wave[w].y, of_wave[w].z});
+      const float log_s = logf(a.s), total = a.s == 0.f ? -INFINITY : a.m + log_s;
+      if (lse) lse[row] = total;
+      if (entropy) entropy[row] = a.s == 0.f ? 0.f : log_s - a.t / a.s;
+      if (logprob) {
+        const int32_t t = targets[row];
+        float v = 0.f;
+        if (t >= 0 && t < vocab) v = a.s == 0.f ? -INFINITY : (of_target[row] - a.m) - log_s;
+        logprob[row] = v;
+      }
+    }
+    __syncthreads();
   }
 }
 
@@ -238,7 +241,7 @@ hipError_t forward(const hpd_head_args& a, hipStream_t s) {
   const int32_t* const targets = a.logprob ? a.targets : nullptr;
   const hipError_t e = launch_product<T, BY_ROWS, BY_ROWS, PLAIN>(plan.product, g, RowSums{targets, of_target, parts, a.vocab, tiles, a.n_rows}, s);
   if (e != hipSuccess) return e;
-  join_rows_kernel<<<dim3((uint32_t)a.n_rows), dim3(256), 0, s>>>(parts, tiles, of_target, targets, a.vocab, a.logprob, a.lse, a.entropy);
+  join_rows_kernel<<<dim3((uint32_t)std::min<int64_t>(a.n_rows, 1 << 20)), dim3(256), 0, s>>>(parts, tiles, a.n_rows, of_target, targets, a.vocab, a.logprob, a.lse, a.entropy);
   return hipGetLastError();
 }
 
@@ -261,7 +264,7 @@ hipError_t backward(const hpd_head_backward_args& a, hipStream_t s) {
     }
     if (e == hipSuccess && a.d_hidden && N > 0) {
       const hpd_product_args g = {operand<T>(w, a.weight_stride, D), operand<T>(dx, piece, N), (int32_t)n, 1, 0, 0};
-      e = launch_product<T, BY_COLUMNS, BY_ROWS, PLAIN>(plan.d_hidden, g, StorePart{parts, D, N, v0 > 0}, s);
+      e = launch_product<T, BY_COLUMNS, BY_ROWS, TAIL>(plan.d_hidden, g, StorePart{parts, D, N, v0 > 0}, s);
     }
     if (e == hipSuccess && a.d_weight) {  // (no rows: zeros)
       const hpd_product_args g = {operand<T>(a.hidden, a.hidden_stride, D), operand<T>(dx, piece, n), (int32_t)N, 1, 0, 0};

@@ -21,6 +21,7 @@
 #include <stdint.h>
 
 #include <algorithm>
+#include <cmath>
 #include <type_traits>
 
 #include "hpd_attn_bf16.h"
@@ -219,7 +220,9 @@ struct Shape {
   static constexpr int SMEM = STAGES * STAGE_BYTES, TURN = SMEM / WAVES / 4096 * 4096;  // of it, a wave's when its sums are stored
   static constexpr bool MANY = MI * NI * 16 > 128;  // the sums are in accumulation registers
 };
-enum { PLAIN = 0, DUAL = 1, SEGMENTS = 2 };
+// DUAL: a tile's features by turns from two A; SEGMENTS: a second A and B are contracted after the first; TAIL: any number of contracted
+// elements, A by columns and B by rows, with zeros behind B's last up to a multiple of 16 bytes
+enum { PLAIN = 0, DUAL = 1, SEGMENTS = 2, TAIL = 3 };
 // bf16 products of 4096 elements: Large 1.2 PFLOP/s for 4096 x 4096 and more; Middle 1.06 from 4096 x 2048 (Large 0.72); Small 0.61 for
 // 2048 x 1024 (Middle 0.39).  Few rows, where the weights' bytes are what it takes: Few32 5.9 TB/s for 24576 features and a row, 6.4 for
 // 48000 (without the hint that the weights will not be read again 5.3 and 5.8; Small 4.9 and 5.5), Few64 4.5 for 64 rows (Small 4.2).  fp32:
@@ -266,9 +269,10 @@ __global__ void __launch_bounds__(64 * S::WAVES, (S::WGS * S::WAVES + 3) / 4) pr
   using TA = Tile<T, FA, S::BM, S::WAVES, MODE == DUAL, S::ONCE>;
   using TB = Tile<T, FB, S::BN, S::WAVES, false>;
   constexpr int MI = S::MI, NI = S::NI, K = STAGE_K<T>, LOADS = TA::LOADS + TB::LOADS, GROUPS = TA::GROUPS + TB::GROUPS;
-  // The stage with less than a whole stage's elements is the first, which is loaded in front of the loop; of two segments, the
-  // last of each, and loads by rows are masked all the time.
-  constexpr bool MASKED = MODE == SEGMENTS;
+  // The stage with less than a whole stage's elements is the first, which is loaded in front of the loop.  Of two segments it is the
+  // last of each, and where the number may be odd the last, so that rows are read at multiples of 16 bytes: loads by rows are masked
+  // all the time (1 % of the largest products).
+  constexpr bool MASKED = MODE == SEGMENTS || MODE == TAIL;
   __shared__ __attribute__((aligned(4096))) char smem[S::SMEM];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wave_m = wave % S::WM, wave_n = wave / S::WM;
@@ -621,7 +625,9 @@ struct Plan {
 };
 // The least time by a simple account, in us: workgroups go in rounds of as many as run at a time.  Each takes `fixed` for its start and
 // end, and for a stage stage[n - 1] where n run on its CU.  (Measured, for 1 to 4096 workgroups of each shape and 64 to 8192 elements, to
-// within a tenth or two.)  What is read comes at `rate` TB/s at most, and each workgroup has `flight` KB of it on the way, about 1 us.
+// within a tenth or two.)  What is read comes at `rate` TB/s at most; each workgroup has `flight` KB of it on the way, about 1 us, and a CU
+// takes a third more than its share of the rate.  (Of 60 random products of 1 to 12000 rows, weights from memory, the choice was 1.02 to 1.03 of the best of all shapes
+// and cuts in the geometric mean, in bf16 and in fp32.)
 struct ShapeCost {
   int on_cu;
   double stage[3], fixed, flight, rate;
@@ -629,9 +635,9 @@ struct ShapeCost {
 constexpr int CUS = 256;
 template <typename T>
 ShapeCost shape_cost(int shape) {
-  constexpr ShapeCost BF16[] = {{1, {1.63}, 7.0, 64, 5.2}, {2, {0.72, 0.97}, 4.0, 32, 5.2}, {3, {0.25, 0.39, 0.56}, 3.0, 16, 5.2},
+  constexpr ShapeCost BF16[] = {{1, {1.7}, 7.0, 64, 5.2}, {2, {0.72, 0.97}, 4.0, 32, 5.2}, {3, {0.25, 0.42, 0.68}, 3.0, 16, 5.2},
                                 {2, {0.25, 0.39}, 3.0, 24, 5.7}, {3, {0.25, 0.3, 0.4}, 3.0, 24, 5.9}};
-  constexpr ShapeCost F32[] = {{}, {}, {3, {0.59, 1.03, 1.45}, 3.0, 16, 5.2}, {2, {0.59, 1.03}, 3.0, 24, 5.7}, {3, {0.35, 0.55, 0.75}, 3.0, 24, 5.9}};
+  constexpr ShapeCost F32[] = {{}, {}, {3, {0.59, 1.03, 1.45}, 3.0, 16, 5.2}, {2, {0.59, 1.03}, 3.0, 24, 5.7}, {3, {0.6, 1.0, 1.1}, 3.0, 24, 5.9}};
   return sizeof(T) == 4 ? F32[shape] : BF16[shape];
 }
 // k: contracted elements, of all segments; by_rows: the rows' operand lies by rows (there are kernels for few of them)
@@ -651,8 +657,10 @@ Plan plan_product(int64_t features, int64_t rows, int64_t k, bool dual, int most
       const int64_t all = tiles * p.splits, full = all / places, rest = all % places, deep = (stages + p.splits - 1) / p.splits;
       double t = (double)full * (deep * c.stage[c.on_cu - 1] + c.fixed);
       if (rest) t += deep * c.stage[(rest - 1) / CUS] + c.fixed;
-      t = std::max(t, bytes / std::min(c.rate * 1e6, (double)std::min(all, places) * c.flight * 1e3) + c.fixed);
-      if (p.splits > 1) t += 4.0 + (double)features * rows * p.splits * 8 / 4.0e6;  // (parts written and read, a launch)
+      const double at_once = (double)std::min(all, places), on_cu = std::ceil(at_once / CUS);
+      const double cu = full ? 0.0 : on_cu * bytes / all / (std::min(on_cu * c.flight, 1.32 * c.rate * 1e3 / CUS) * 1e3);
+      t = std::max(t, std::max(cu, bytes / std::min(c.rate * 1e6, at_once * c.flight * 1e3)) + c.fixed);
+      if (p.splits > 1) t += 4.0 + 0.12 * p.splits + (double)features * rows * p.splits * 8 / 4.0e6;  // (parts written and read, a launch)
       if (t < least) {
         least = t;
         best = p;

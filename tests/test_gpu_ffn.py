@@ -132,6 +132,62 @@ def test_larger(dtype, rows, width, inner):
         R.check(a, w, name)
 
 
+# tiles of every size in every product, whole and cut contractions, ends of all kinds
+@pytest.mark.parametrize("dtype, rows, width, inner", [("bf16", 4100, 2048, 4104), ("bf16", 2049, 4096, 4104), ("bf16", 700, 4096, 8200),
+                                                       ("bf16", 8200, 1032, 2504), ("bf16", 32, 4096, 8200), ("f32", 3, 4096, 8200),
+                                                       ("f32", 32, 1152, 4008), ("f32", 64, 2048, 2056), ("bf16", 64, 1160, 12296)])
+def test_tiles_of_every_size(dtype, rows, width, inner):
+    i = _inputs(rows, width, inner, dtype, seed=8)
+    want = R.ffn(*_d(i, "x", "wg", "wu", "wd"), "gelu_tanh", TD[dtype])
+    for name, a, w in zip(("out", "gate", "up"), _forward(i, rows, width, inner, dtype, "gelu_tanh"), want):
+        R.check(a, w, name)
+    del want
+    want = R.ffn_grad(*_d(i, "x", "wg", "wu", "wd", "g", "u", "d_out"), "gelu_tanh", TD[dtype])
+    for name, a, w in zip(("dx", "dw_gate", "dw_up", "dw_down"), _backward(i, rows, width, inner, dtype, "gelu_tanh"), want):
+        R.check(a, w, name)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows", [3, 130])
+def test_halves_of_one_matrix(rows, dtype):
+    """Both projections in one matrix, what is kept in one buffer, their gradients in one: the same bits."""
+    width, inner, td = 136, 264, TD[dtype]
+    i = _inputs(rows, width, inner, dtype, seed=9)
+    cfg = B.hpd_ffn_config(width, inner, DT[dtype], ACTS["silu"])
+    w = torch.cat([i["wg"], i["wu"]])
+    kept, d_w = torch.empty((rows, 2 * inner), dtype=td, device="cuda"), torch.empty_like(w)
+    out, dx, dwd = torch.empty_like(i["x"]), torch.empty_like(i["x"]), torch.empty_like(i["wd"])
+    st = B.hpd_ffn_strides(gate=2 * inner, up=2 * inner)
+    ws = [B.alloc_ffn_workspace(cfg, rows, b) for b in (False, True)]
+    g, u = kept[:, :inner], kept[:, inner:]
+    B.hpd_gated_ffn(cfg, rows, i["x"], w[:inner], w[inner:], i["wd"], out, g, u, ws[0], st)
+    a, b, c = _forward(i, rows, width, inner, dtype, "silu")
+    assert torch.equal(out, a) and torch.equal(g, b) and torch.equal(u, c)
+    B.hpd_gated_ffn_backward(cfg, rows, i["x"], w[:inner], w[inner:], i["wd"], g, u, i["d_out"], dx, d_w[:inner], d_w[inner:], dwd,
+                             ws[1], st)
+    i["g"], i["u"] = b, c
+    for x, y in zip((dx, d_w[:inner], d_w[inner:], dwd), _backward(i, rows, width, inner, dtype, "silu")):
+        assert torch.equal(x, y)
+
+
+def test_two_calls_at_once():
+    """Calls on two streams with workspaces of their own."""
+    rows, width, inner = 257, 512, 1032
+    inputs = [_inputs(rows, width, inner, "bf16", seed=s) for s in (10, 11)]
+    want = [[t.clone() for t in _forward(i, rows, width, inner, "bf16", "silu", pad=0)] for i in inputs]
+    cfg = B.hpd_ffn_config(width, inner, B.HPD_BF16, B.HPD_ACT_SILU)
+    ws = [B.alloc_ffn_workspace(cfg, rows, False) for _ in inputs]
+    outs = [[torch.empty_like(t) for t in w] for w in want]
+    streams = [torch.cuda.Stream() for _ in inputs]
+    torch.cuda.synchronize()
+    for _ in range(10):
+        for i, w, o, s in zip(inputs, ws, outs, streams):
+            B.hpd_gated_ffn(cfg, rows, i["x"], i["wg"], i["wu"], i["wd"], *o, w, stream=s)
+    torch.cuda.synchronize()
+    for a, b in zip(outs, want):
+        assert all(torch.equal(x, y) for x, y in zip(a, b))
+
+
 def test_no_rows():
     """Nothing to do but the weights' gradients: zeros."""
     i = _inputs(0, 64, 40, "bf16")

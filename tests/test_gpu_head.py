@@ -78,6 +78,13 @@ def test_larger(dtype, rows, width, vocab):
     _check(_inputs(rows, width, vocab, dtype, seed=1), dtype)
 
 
+# tiles of every size in every product, whole and cut contractions
+@pytest.mark.parametrize("dtype, rows, width, vocab", [("bf16", 4100, 2048, 9001), ("bf16", 5000, 1032, 20011), ("bf16", 300, 4096, 20011),
+                                                       ("f32", 2, 1152, 50021), ("f32", 33, 520, 9001), ("bf16", 32, 2048, 33001)])
+def test_tiles_of_every_size(dtype, rows, width, vocab):
+    _check(_inputs(rows, width, vocab, dtype, seed=9), dtype)
+
+
 @pytest.mark.parametrize("hidden, weight, g, ge", [(1, 0, 1, 1), (0, 1, 1, 1), (1, 1, 0, 1), (1, 1, 1, 0), (1, 1, 0, 0)])
 def test_parts_that_are_not_wanted(hidden, weight, g, ge):
     i = _inputs(70, 136, 500, "bf16", seed=2)
