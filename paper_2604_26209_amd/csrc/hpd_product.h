@@ -68,15 +68,15 @@ __device__ __forceinline__ void load_to_lds(uint32_t lds, const uint32_t* off, i
   if constexpr (N == 4)                                                                                                     \
     asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\t"                                                      \
                  "buffer_load_dwordx4 %2, %6, 0 offen" HINT " lds\n\t"                                                      \
-                 "buffer_load_dwordx4 %3, %6, 0 offen offset:1024" HINT " lds\n\t"                                          \
-                 "buffer_load_dwordx4 %4, %6, 0 offen offset:2048" HINT " lds\n\t"                                          \
-                 "buffer_load_dwordx4 %5, %6, 0 offen offset:3072" HINT " lds\n\t"                                          \
+                 "buffer_load_dwordx4 %3, %6, 0 offen offset:0x400" HINT " lds\n\t"                                          \
+                 "buffer_load_dwordx4 %4, %6, 0 offen offset:0x800" HINT " lds\n\t"                                          \
+                 "buffer_load_dwordx4 %5, %6, 0 offen offset:0xc00" HINT " lds\n\t"                                          \
                  "s_mov_b32 m0, %0"                                                                                         \
                  : "=&s"(keep) : "s"(lds), "v"(off[0]), "v"(off[1]), "v"(off[2]), "v"(off[3]), "s"(buf) : "memory");        \
   else if constexpr (N == 2)                                                                                                \
     asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\t"                                                      \
                  "buffer_load_dwordx4 %2, %4, 0 offen" HINT " lds\n\t"                                                      \
-                 "buffer_load_dwordx4 %3, %4, 0 offen offset:1024" HINT " lds\n\t"                                          \
+                 "buffer_load_dwordx4 %3, %4, 0 offen offset:0x400" HINT " lds\n\t"                                          \
                  "s_mov_b32 m0, %0"                                                                                         \
                  : "=&s"(keep) : "s"(lds), "v"(off[0]), "v"(off[1]), "s"(buf) : "memory");                                  \
   else                                                                                                                      \
@@ -219,6 +219,10 @@ struct Shape {
   static constexpr int STAGE_BYTES = (BM + BN) * 128;
   static constexpr int SMEM = STAGES * STAGE_BYTES, TURN = SMEM / WAVES / 4096 * 4096;  // of it, a wave's when its sums are stored
   static constexpr bool MANY = MI * NI * 16 > 128;  // the sums are in accumulation registers
+  // Sums of a block, each over a part of a stage's steps, added up at the end.  A sum is rounded with every product: two halve the
+  // error of a long contraction, four quarter it (fp32 gradients of the block for 1801 rows: off by 5e-7 in place of 1e-6; the
+  // entropies of three rows of 150001 tokens: 4e-7, 1.5e-6).
+  static constexpr int SUMS = MANY ? 1 : 4 / (MI * NI);
 };
 // DUAL: a tile's features by turns from two A; SEGMENTS: a second A and B are contracted after the first; TAIL: any number of contracted
 // elements, A by columns and B by rows, with zeros behind B's last up to a multiple of 16 bytes
@@ -264,6 +268,10 @@ __device__ __forceinline__ void tile_of(int32_t id, int32_t total, int32_t tiles
   n = in / wide;
 }
 
+// The epilogue wants fp32 sums taken in the order of k.
+template <typename Epilogue>
+constexpr bool IN_ORDER = false;
+
 template <typename T, int FA, int FB, int MODE, typename S, typename Epilogue>
 __global__ void __launch_bounds__(64 * S::WAVES, (S::WGS * S::WAVES + 3) / 4) product_kernel(hpd_product_args g, Epilogue epilogue) {
   using TA = Tile<T, FA, S::BM, S::WAVES, MODE == DUAL, S::ONCE>;
@@ -273,6 +281,7 @@ __global__ void __launch_bounds__(64 * S::WAVES, (S::WGS * S::WAVES + 3) / 4) pr
   // last of each, and where the number may be odd the last, so that rows are read at multiples of 16 bytes: loads by rows are masked
   // all the time (1 % of the largest products).
   constexpr bool MASKED = MODE == SEGMENTS || MODE == TAIL;
+  constexpr int SUMS = sizeof(T) == 4 && IN_ORDER<Epilogue> && !S::ONCE ? 1 : S::SUMS;
   __shared__ __attribute__((aligned(4096))) char smem[S::SMEM];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wave_m = wave % S::WM, wave_n = wave / S::WM;
@@ -353,13 +362,15 @@ __global__ void __launch_bounds__(64 * S::WAVES, (S::WGS * S::WAVES + 3) / 4) pr
   Reader<T, FB, S::BN> rb;
   ra.init(wave_m * MI, lane);
   rb.init(wave_n * NI, lane);
-  floatx16 acc[MI][NI];
+  floatx16 sums[SUMS][MI][NI];
 #pragma unroll
-  for (int i = 0; i < MI; ++i)
+  for (int c = 0; c < SUMS; ++c)
 #pragma unroll
-    for (int j = 0; j < NI; ++j)
+    for (int i = 0; i < MI; ++i)
 #pragma unroll
-      for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.f;
+      for (int j = 0; j < NI; ++j)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) sums[c][i][j][r] = 0.f;
   product_u4 fa[2][MI], fb[2][NI];
   // operand i of a step's MI + NI
   auto read = [&](uint32_t at, int step, int to, int i) {
@@ -370,12 +381,13 @@ __global__ void __launch_bounds__(64 * S::WAVES, (S::WGS * S::WAVES + 3) / 4) pr
   };
   // the products of a step, between(n) after the n-th of BLOCKS
   constexpr int BLOCKS = MI * NI, READS = MI + NI;
-  auto products = [&](int of, auto between) {
+  auto products = [&](int step, auto between) {
+    const int of = step & 1, c = step % SUMS;
 #pragma unroll
     for (int i = 0; i < MI; ++i)
 #pragma unroll
       for (int j = 0; j < NI; ++j) {
-        acc[i][j] = multiply<T>(fa[of][i], fb[of][j], acc[i][j]);
+        sums[c][i][j] = multiply<T>(fa[of][i], fb[of][j], sums[c][i][j]);
         between(i * NI + j);
         __builtin_amdgcn_sched_barrier(0);
       }
@@ -403,14 +415,14 @@ __global__ void __launch_bounds__(64 * S::WAVES, (S::WGS * S::WAVES + 3) / 4) pr
     const uint32_t here = lds + slot * S::STAGE_BYTES, there = lds + next * S::STAGE_BYTES;
 #pragma unroll
     for (int step = 0; step < 3; ++step)
-      products(step & 1, [&](int n) {
+      products(step, [&](int n) {
 #pragma unroll
         for (int i = n * READS / BLOCKS; i < (n + 1) * READS / BLOCKS; ++i) read(here, step + 1, (step + 1) & 1, i);
       });
     wait_loads<LOADS * (S::STAGES - 2)>();
     meet();
     next_stage(slot);
-    products(1, [&](int n) {
+    products(3, [&](int n) {
 #pragma unroll
       for (int i = n * READS / BLOCKS; i < (n + 1) * READS / BLOCKS; ++i) read(there, 0, 0, i);  // (behind the last stage: of no use)
 #pragma unroll
@@ -425,6 +437,14 @@ __global__ void __launch_bounds__(64 * S::WAVES, (S::WGS * S::WAVES + 3) / 4) pr
     asm volatile("s_nop 15\n\ts_nop 15\n\ts_nop 15" ::: "memory");
     __builtin_amdgcn_sched_barrier(0);
   }
+  floatx16(&acc)[MI][NI] = sums[0];
+#pragma unroll
+  for (int i = 0; i < MI; ++i)
+#pragma unroll
+    for (int j = 0; j < NI; ++j) {
+      if (SUMS == 2) acc[i][j] += sums[1 % SUMS][i][j];
+      if (SUMS == 4) acc[i][j] = (acc[i][j] + sums[1 % SUMS][i][j]) + (sums[2 % SUMS][i][j] + sums[3 % SUMS][i][j]);
+    }
   const Place at{m0 + (MODE == DUAL ? wave_m * MI / 2 : wave_m * MI) * 32, n0 + wave_n * NI * 32, split, tile_m, wave_m, wave_n, lane};
   epilogue.template operator()<S, MI, NI>(acc, at, smem);
 }
