@@ -46,54 +46,34 @@ struct Activate {
   int64_t inner, rows, gate_stride, up_stride;
   template <typename S, int MI, int NI>
   __device__ __forceinline__ void operator()(floatx16 (&acc)[MI][NI], const Place& at, char* smem) const {
-    constexpr int NB = MI > 1 ? MI / 2 : 1;
+    const Turn<T, 16 * MI> turn(at, smem, S::TURN);
     const int64_t width = inner - at.feature;
-    // where waves have one block each: g in one, u in the next, which hands it over through its LDS
-    constexpr int GIVEN = MI > 1 ? 0 : NI * 4096;
-    static_assert(GIVEN + NB * 32 * 32 * (int)sizeof(T) <= S::TURN, "u and a turn");
-    const Turn<T, NB> turn(at, smem, S::TURN, GIVEN);
-    const bool has_g = MI > 1 || at.wave_m % 2 == 0, has_u = MI > 1 || !has_g;
-    const float* const given = reinterpret_cast<const float*>(smem + ((threadIdx.x >> 6) + 1) * S::TURN) + at.lane;
-    if constexpr (MI == 1) {
-      float* const give = reinterpret_cast<float*>(smem + (threadIdx.x >> 6) * S::TURN) + at.lane;
-      if (has_u)
-#pragma unroll
-        for (int j = 0; j < NI; ++j)
-#pragma unroll
-          for (int r = 0; r < 16; ++r) give[(16 * j + r) * 64] = acc[0][j][r];
-      __syncthreads();
-    }
     each<NI>([&](auto j) {
       const int64_t first = at.row + 32 * j, left = rows - first;
       auto put = [&](auto value) {
 #pragma unroll
-        for (int b = 0; b < NB; ++b)
+        for (int i = 0; i < MI; ++i)
 #pragma unroll
-          for (int q = 0; q < 4; ++q) {
+          for (int q = 0; q < 2; ++q) {
             float v[4];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const int r = 4 * q + e;
-              v[e] = value([&]() { return sum_of<S>(acc[MI > 1 ? 2 * b : 0][j], r); },
-                           [&]() { return MI > 1 ? sum_of<S>(acc[MI > 1 ? 2 * b + 1 : 0][j], r) : given[(16 * j + r) * 64]; });
-            }
-            turn.put4(b, q, v);
+            for (int e = 0; e < 4; ++e)
+              v[e] = value([&]() { return sum_of<S>(acc[i][j], 4 * q + e); }, [&]() { return sum_of<S>(acc[i][j], 4 * q + e + 8); });
+            turn.put4(16 * i + 8 * q, v);
           }
       };
-      if (has_g) {
-        put([&](auto g, auto u) {
-          float a, slope;
-          activation<T, ACT>(g(), a, slope);
-          return a * u();
-        });
-        turn.store(left, width, inner, [&](int r) { return h + (first + r) * inner + at.feature; });
-        if (gate) {
-          put([](auto g, auto) { return g(); });
-          turn.store(left, width, gate_stride, [&](int r) { return gate + (first + r) * gate_stride + at.feature; });
-        }
+      put([](auto g, auto u) {
+        float a, slope;
+        activation<T, ACT>(g(), a, slope);
+        return a * u();
+      });
+      turn.store(left, width, inner, [&](int r) { return h + (first + r) * inner + at.feature; });
+      if (gate) {
+        put([](auto g, auto) { return g(); });
+        turn.store(left, width, gate_stride, [&](int r) { return gate + (first + r) * gate_stride + at.feature; });
       }
-      if (has_u && up) {
-        put([](auto own, auto u) { return MI > 1 ? u() : own(); });
+      if (up) {
+        put([](auto, auto u) { return u(); });
         turn.store(left, width, up_stride, [&](int r) { return up + (first + r) * up_stride + at.feature; });
       }
     });
@@ -111,7 +91,7 @@ struct InnerGradients {
   __device__ __forceinline__ void operator()(floatx16 (&acc)[MI][NI], const Place& at, char* smem) const {
     constexpr int NB = MI < 2 ? 1 : 2, BYTES = NB * 32 * 32 * (int)sizeof(T);
     static_assert(2 * BYTES <= S::TURN, "g and u");
-    using W = Turn<T, NB>;
+    using W = Turn<T, 32 * NB>;
     const W of_g(at, smem, S::TURN), of_u(at, smem, S::TURN, BYTES);
     each<NI>([&](auto j) {
       each<MI / NB>([&](auto half) {
@@ -127,8 +107,8 @@ struct InnerGradients {
 #pragma unroll
           for (int q = 0; q < 4; ++q) {
             float g[4], u[4], v[4];
-            fetch4(of_g.four(i, q), g);
-            fetch4(of_u.four(i, q), u);
+            fetch4(of_g.four(32 * i + 8 * q), g);
+            fetch4(of_u.four(32 * i + 8 * q), u);
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
               const float dh = sum_of<S>(acc[i0 + i][j], 4 * q + e);
@@ -138,8 +118,8 @@ struct InnerGradients {
               v[e] = a * u[e];
               u[e] = dh * a;
             }
-            of_g.put4(i, q, g);
-            of_u.put4(i, q, u);
+            of_g.put4(32 * i + 8 * q, g);
+            of_u.put4(32 * i + 8 * q, u);
             kept[i][q] = pack4<T>(v);
           }
         of_g.store(left, width, 2 * inner, [&](int r) { return d_inner + (first + r) * 2 * inner + feature; });
@@ -148,7 +128,7 @@ struct InnerGradients {
 #pragma unroll
           for (int i = 0; i < NB; ++i)
 #pragma unroll
-            for (int q = 0; q < 4; ++q) *reinterpret_cast<Four<T>*>(of_g.four(i, q)) = kept[i][q];
+            for (int q = 0; q < 4; ++q) *reinterpret_cast<Four<T>*>(of_g.four(32 * i + 8 * q)) = kept[i][q];
           of_g.store(left, width, inner, [&](int r) { return h + (first + r) * inner + feature; });
         }
       });
@@ -173,8 +153,8 @@ struct ForwardPlan {
   Plan in, down;
   int64_t parts, bytes;
   ForwardPlan(const hpd_ffn_config& c, int64_t n) {
-    in = plan_product<T>(c.inner, n, c.width, true, 1);
-    down = plan_product<T>(c.width, n, c.inner, false, MOST_SPLITS);
+    in = plan_product<T, BY_ROWS, BY_ROWS>(c.inner, n, c.width, true, 1);
+    down = plan_product<T, BY_ROWS, BY_ROWS>(c.width, n, c.inner, false, MOST_SPLITS);
     parts = round16(n * c.inner * (int64_t)sizeof(T));
     bytes = parts + part_bytes(down, n, c.width);
   }
@@ -184,10 +164,10 @@ struct BackwardPlan {
   Plan inner, dx, in_weights, down_weights;
   int64_t h, parts, bytes;
   BackwardPlan(const hpd_ffn_config& c, int64_t n) {
-    inner = plan_product<T>(c.inner, n, c.width, false, 1);
-    dx = plan_product<T>(c.width, n, 2 * (int64_t)c.inner, false, MOST_SPLITS);
-    in_weights = plan_product<T>(c.width, 2 * (int64_t)c.inner, n, false, 1, false);
-    down_weights = plan_product<T>(c.inner, c.width, n, false, 1, false);
+    inner = plan_product<T, BY_COLUMNS, BY_ROWS>(c.inner, n, c.width, false, 1);
+    dx = plan_product<T, BY_COLUMNS, BY_ROWS>(c.width, n, 2 * (int64_t)c.inner, false, MOST_SPLITS);
+    in_weights = plan_product<T, BY_COLUMNS, BY_COLUMNS>(c.width, 2 * (int64_t)c.inner, n, false, 1);
+    down_weights = plan_product<T, BY_COLUMNS, BY_COLUMNS>(c.inner, c.width, n, false, 1);
     h = round16(n * 2 * c.inner * (int64_t)sizeof(T));
     parts = h + round16(n * c.inner * (int64_t)sizeof(T));
     bytes = parts + part_bytes(dx, n, c.width);

@@ -146,7 +146,7 @@ struct LogitGradients {
   template <typename S, int MI, int NI>
   __device__ __forceinline__ void operator()(floatx16 (&acc)[MI][NI], const Place& at, char* smem) const {
     const int l = at.lane & 31, h = at.lane >> 5;
-    const Turn<T, MI> turn(at, smem, S::TURN);
+    const Turn<T, 32 * MI> turn(at, smem, S::TURN);
 #pragma unroll
     for (int j = 0; j < NI; ++j) {
       const int64_t first_row = at.row + 32 * j;
@@ -183,7 +183,7 @@ struct LogitGradients {
             for (int e = 0; e < 4; ++e)
               if (32 * i + 8 * q + 4 * h + e >= inside) v[e] = 0.f;
           }
-          turn.put4(i, q, v);
+          turn.put4(32 * i + 8 * q, v);
         }
       turn.store(rows - first_row, stride - at.feature, stride, [&](int r) { return out + (first_row + r) * stride + at.feature; });
     }
@@ -215,7 +215,7 @@ struct ForwardPlan {
   Plan product;
   int64_t tiles, of_target, bytes;
   ForwardPlan(int64_t n, int32_t width, int32_t vocab) {
-    product = plan_product<T>(vocab, n, width, false, 1);
+    product = plan_product<T, BY_ROWS, BY_ROWS>(vocab, n, width, false, 1);
     tiles = (vocab + product.bm() - 1) / product.bm();
     of_target = n * tiles * (int64_t)sizeof(float4);
     bytes = round16(of_target + n * 4);
@@ -231,9 +231,9 @@ struct BackwardPlan {
     const int64_t most = std::max(UNIT, PIECE_BYTES / (std::max<int64_t>(n, 1) * (int64_t)sizeof(T)) / UNIT * UNIT);
     const int64_t pieces = (vocab + most - 1) / most;
     piece = ((vocab + pieces - 1) / pieces + UNIT - 1) / UNIT * UNIT;
-    logits = plan_product<T>(std::min<int64_t>(piece, vocab), n, width, false, 1);
-    d_hidden = plan_product<T>(width, n, std::min<int64_t>(piece, vocab), false, MOST_SPLITS);
-    d_weight = plan_product<T>(width, std::min<int64_t>(piece, vocab), n, false, 1, false);
+    logits = plan_product<T, BY_ROWS, BY_ROWS>(std::min<int64_t>(piece, vocab), n, width, false, 1);
+    d_hidden = plan_product<T, BY_COLUMNS, BY_ROWS>(width, n, std::min<int64_t>(piece, vocab), false, MOST_SPLITS);
+    d_weight = plan_product<T, BY_COLUMNS, BY_COLUMNS>(width, std::min<int64_t>(piece, vocab), n, false, 1);
     parts = round16(n * piece * (int64_t)sizeof(T));
     bytes = parts + d_hidden.splits * n * width * 4;
   }

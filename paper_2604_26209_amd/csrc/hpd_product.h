@@ -134,7 +134,7 @@ struct Tile {
       const int f = wave * LOADS + i;
       if (FORM == BY_ROWS) {
         int r = f * 8 + (lane >> 3);
-        if (DUAL) r = (r >> 6) * 32 + (r & 31);  // blocks of 32 by turns from both halves
+        if (DUAL) r %= R / 2;  // (one half's rows, then the other's)
         off[i] = r < size ? (uint32_t)r * (uint32_t)stride + chunk_of(f, lane) * 16 : OUTSIDE;
       } else {
         const int k = k_of(f, lane), g = ((lane * 16 + f * 1024) % RB) / 64;
@@ -156,12 +156,13 @@ struct Tile {
 #pragma unroll
     for (int e = 0; e < GROUP; ++e)
       o[e] = MASKED && FORM == BY_ROWS && chunk_of(f + e, lane) * CHUNK<T> >= left ? OUTSIDE : off[i * GROUP + e];
-    load_to_lds<GROUP, ONCE>(__builtin_amdgcn_readfirstlane(lds + f * 1024), o, DUAL && (f >> 2 & 1) ? b1 : b0);
+    load_to_lds<GROUP, ONCE>(__builtin_amdgcn_readfirstlane(lds + f * 1024), o, DUAL && f >= R / 16 ? b1 : b0);
   }
 };
 
 // Operands of a wave's products.  A lane's 16 bytes: row (column) lane % 32 of the block, elements CHUNK * (2 step + lane / 32) ..
-template <typename T, int FORM, int R>
+// DUAL: a block is 16 rows of one half and the same 16 of the other, whose sums then lie in the same lanes.
+template <typename T, int FORM, int R, bool DUAL>
 struct Reader {
   using TL = Tile<T, FORM, R, 1, false>;
   uint32_t at;      // by rows
@@ -171,7 +172,8 @@ struct Reader {
     const int l = lane & 31, h = lane >> 5;
     first = first_block;
     if (FORM == BY_ROWS) {
-      at = (uint32_t)(first_block * 4096 + l * 128 + ((h ^ ((l >> 1) & 7)) << 4));
+      const int row = DUAL ? first_block * 16 + (l >> 4) * (R / 2) + (l & 15) : first_block * 32 + l;
+      at = (uint32_t)(row * 128 + ((h ^ ((l >> 1) & 7)) << 4));
     } else if (sizeof(T) == 2) {
       const int a = lane & 15, j = a >> 2;
 #pragma unroll
@@ -184,7 +186,7 @@ struct Reader {
     }
   }
   __device__ __forceinline__ product_u4 read(uint32_t tile, int i, int step) const {
-    if (FORM == BY_ROWS) return read16(tile + (at ^ (step << 5)) + i * 4096);
+    if (FORM == BY_ROWS) return read16(tile + (at ^ (step << 5)) + i * (DUAL ? 2048 : 4096));
     const uint32_t p = tile + col[i];
     if (sizeof(T) == 2) {
       const uint2 x = read_tr8(p + step * 16 * TL::RB), y = read_tr8(p + (step * 16 + 4) * TL::RB);
@@ -222,9 +224,9 @@ struct Shape {
   // Sums of a block, each over a part of a stage's steps, added up at the end.  A sum is rounded with every product: two halve the
   // error of a long contraction, four quarter it (fp32 gradients of the block for 1801 rows: off by 5e-7 in place of 1e-6; the
   // entropies of three rows of 150001 tokens: 4e-7, 1.5e-6).
-  static constexpr int SUMS = MANY ? 1 : 4 / (MI * NI);
+  static constexpr int SUMS = MANY ? 1 : MI * NI > 2 ? 1 : 4 / (MI * NI);
 };
-// DUAL: a tile's features by turns from two A; SEGMENTS: a second A and B are contracted after the first; TAIL: any number of contracted
+// DUAL: a tile's features half and half from two A; SEGMENTS: a second A and B are contracted after the first; TAIL: any number of contracted
 // elements, A by columns and B by rows, with zeros behind B's last up to a multiple of 16 bytes
 enum { PLAIN = 0, DUAL = 1, SEGMENTS = 2, TAIL = 3 };
 // bf16 products of 4096 elements: Large 1.2 PFLOP/s for 4096 x 4096 and more; Middle 1.06 from 4096 x 2048 (Large 0.72); Small 0.61 for
@@ -236,7 +238,9 @@ using Middle = Shape<128, 128, 2, 4, 2, 2>;
 using Small = Shape<64, 64, 2, 2, 3, 3>;
 using Few64 = Shape<64, 64, 2, 2, 4, 2, true>;
 using Few32 = Shape<64, 32, 2, 1, 4, 3, true>;
-enum { LARGE = 0, MIDDLE = 1, SMALL = 2, FEW64 = 3, FEW32 = 4 };
+using Wide = Shape<192, 256, 2, 2, 2, 1>;
+using Few128 = Shape<64, 128, 2, 2, 3, 2, true>;
+enum { LARGE = 0, MIDDLE = 1, SMALL = 2, FEW64 = 3, FEW32 = 4, FEW128 = 5, WIDE = 6 };
 
 // f(0) .. f(N - 1), the numbers as types: what is indexed with them stays in registers however long f is
 template <int N, typename F, int I = 0>
@@ -247,7 +251,7 @@ __device__ __forceinline__ void each(F f) {
   }
 }
 
-// The place of a wave's blocks: features feature + 32 i (dual: block i is half i % 2 of features feature + 32 (i / 2)), rows row + 32 j.
+// The place of a wave's blocks: features feature + 32 i (dual: feature + 16 i, registers 0 to 7 one half's, 8 to 15 the other's), rows row + 32 j.
 struct Place {
   int64_t feature, row;
   int32_t split, tile_m;
@@ -358,8 +362,8 @@ __global__ void __launch_bounds__(64 * S::WAVES, (S::WGS * S::WAVES + 3) / 4) pr
       tb.template load<M>(i - TA::GROUPS, st.at + TA::BYTES, st.b, st.b, wave, lane, st.left);
   };
 
-  Reader<T, FA, S::BM> ra;
-  Reader<T, FB, S::BN> rb;
+  Reader<T, FA, S::BM, MODE == DUAL> ra;
+  Reader<T, FB, S::BN, false> rb;
   ra.init(wave_m * MI, lane);
   rb.init(wave_n * NI, lane);
   floatx16 sums[SUMS][MI][NI];
@@ -445,7 +449,7 @@ __global__ void __launch_bounds__(64 * S::WAVES, (S::WGS * S::WAVES + 3) / 4) pr
       if (SUMS == 2) acc[i][j] += sums[1 % SUMS][i][j];
       if (SUMS == 4) acc[i][j] = (acc[i][j] + sums[1 % SUMS][i][j]) + (sums[2 % SUMS][i][j] + sums[3 % SUMS][i][j]);
     }
-  const Place at{m0 + (MODE == DUAL ? wave_m * MI / 2 : wave_m * MI) * 32, n0 + wave_n * NI * 32, split, tile_m, wave_m, wave_n, lane};
+  const Place at{m0 + wave_m * MI * (MODE == DUAL ? 16 : 32), n0 + wave_n * NI * 32, split, tile_m, wave_m, wave_n, lane};
   epilogue.template operator()<S, MI, NI>(acc, at, smem);
 }
 
@@ -472,25 +476,26 @@ __device__ __forceinline__ void store4(T* p, const float* v) { *reinterpret_cast
 template <typename T>
 __device__ __forceinline__ void fetch4(const T* p, float* v) { unpack4<T>(*reinterpret_cast<const Four<T>*>(p), v); }
 
-// 32 rows of NB blocks of 32 features between the accumulators' layout (lane l: row l % 32, four features of every eight) and
+// 32 rows of WIDTH features between the accumulators' layout (lane l: row l % 32, four features of every eight) and
 // whole rows, 16 bytes a lane, through a wave's own LDS; 16-byte chunk c of row r lies at c ^ r.
-template <typename T, int NB>
+template <typename T, int WIDTH>
 struct Turn {
-  static constexpr int RB = NB * 32 * (int)sizeof(T), CHUNKS = RB / 16, ROWS = 64 / CHUNKS, TURNS = 32 / ROWS;
+  static constexpr int PLACES = WIDTH <= 16 ? 16 : WIDTH <= 32 ? 32 : WIDTH <= 64 ? 64 : 128;  // features a row has room for
+  static constexpr int RB = PLACES * (int)sizeof(T), CHUNKS = RB / 16, ROWS = 64 / CHUNKS, TURNS = 32 / ROWS;
   static_assert(32 * RB <= 8192, "a wave's LDS");
   char* mine;
   int lane;
   // bytes: of a wave's LDS; the rows lie `from` bytes behind its first
   __device__ __forceinline__ Turn(const Place& at, char* smem, int bytes, int from = 0) : mine(smem + (threadIdx.x >> 6) * bytes + from), lane(at.lane) {}
   static __device__ __forceinline__ void order() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
-  // the four features 32 i + 8 q + 4 (lane / 32) of the lane's row
-  __device__ __forceinline__ T* four(int i, int q) const {
-    const int r = lane & 31, byte = (32 * i + 8 * q + 4 * (lane >> 5)) * (int)sizeof(T);
+  // of the lane's row, of the eight features from c on the lane's four
+  __device__ __forceinline__ T* four(int c) const {
+    const int r = lane & 31, byte = (c + 4 * (lane >> 5)) * (int)sizeof(T);
     return reinterpret_cast<T*>(mine + r * RB + (((byte >> 4) ^ (r & (CHUNKS - 1))) << 4) + (byte & 15));
   }
   // (a fence: or the sums of many blocks crowd into registers)
-  __device__ __forceinline__ void put4(int i, int q, const float* v) const {
-    store4(four(i, q), v);
+  __device__ __forceinline__ void put4(int c, const float* v) const {
+    store4(four(c), v);
     __builtin_amdgcn_sched_barrier(0);
   }
   // the lane's chunk of rows ROWS n ..
@@ -514,7 +519,7 @@ struct Turn {
     const uint32_t at = behind(stride);
 #pragma unroll
     for (int n = 0; n < TURNS; ++n)
-      if (row(n) >= from && row(n) < rows && column() < width)
+      if (row(n) >= from && row(n) < rows && column() < width && column() < WIDTH)
         *(__attribute__((address_space(1))) product_u4*)(uniform(reinterpret_cast<const char*>(out(n * ROWS))) + at) = v[n];
     __builtin_amdgcn_sched_barrier(0);  // (the next rows' values do not crowd in here)
   }
@@ -528,7 +533,7 @@ struct Turn {
 #pragma unroll
     for (int n = 0; n < TURNS; ++n) {
       x.v[n] = product_u4{0, 0, 0, 0};
-      if (row(n) < rows && column() < width)
+      if (row(n) < rows && column() < width && column() < WIDTH)
         x.v[n] = *(const __attribute__((address_space(1))) product_u4*)(uniform(reinterpret_cast<const char*>(in(n * ROWS))) + at);
     }
     return x;
@@ -562,7 +567,7 @@ struct StoreProduct {
   int64_t features, rows;
   template <typename S, int MI, int NI>
   __device__ __forceinline__ void operator()(floatx16 (&acc)[MI][NI], const Place& at, char* smem) const {
-    const Turn<T, MI> turn(at, smem, S::TURN);
+    const Turn<T, 32 * MI> turn(at, smem, S::TURN);
 #pragma unroll
     for (int j = 0; j < NI; ++j) {
       const int64_t first = at.row + 32 * j;
@@ -573,7 +578,7 @@ struct StoreProduct {
           float v[4];
 #pragma unroll
           for (int e = 0; e < 4; ++e) v[e] = sum_of<S>(acc[i][j], 4 * q + e);
-          turn.put4(i, q, v);
+          turn.put4(32 * i + 8 * q, v);
         }
       const int64_t left = rows - first, here = second - first;  // rows of the block, and of them to out[0]
       if (here > 0)
@@ -640,47 +645,52 @@ hipError_t join_parts(const float* parts, int32_t n, int64_t features, int64_t r
 // Which tiles a product gets, and into how many parts its contraction is cut.
 struct Plan {
   int shape, splits;
-  int64_t bm() const { return shape == LARGE ? 256 : shape == MIDDLE ? 128 : 64; }
-  int64_t bn() const { return shape == FEW32 ? 32 : bm(); }
+  int64_t bm() const { return shape == LARGE ? 256 : shape == WIDE ? 192 : shape == MIDDLE ? 128 : 64; }
+  int64_t bn() const { return shape == FEW32 ? 32 : shape == FEW128 ? 128 : shape == WIDE ? 256 : bm(); }
 };
 // The least time by a simple account, in us: workgroups go in rounds of as many as run at a time.  Each takes `fixed` for its start and
-// end, and for a stage stage[n - 1] where n run on its CU.  (Measured, for 1 to 4096 workgroups of each shape and 64 to 8192 elements, to
-// within a tenth or two.)  What is read comes at `rate` TB/s at most; each workgroup has `flight` KB of it on the way, about 1 us, and a CU
-// takes a third more than its share of the rate.  (Of 60 random products of 1 to 12000 rows, weights from memory, the choice was 1.02 to 1.03 of the best of all shapes
-// and cuts in the geometric mean, in bf16 and in fp32.)
+// end, and for a stage stage[n - 1] where n run on its CU, `uneven` times that where contracted rows do not begin at multiples of 128 bytes
+// (a row's part of a stage is then in two lines).  What is read comes at `rate` TB/s at most; each workgroup has `flight` KB of it on the
+// way, about 1 us, and a CU takes a third more than its share of the rate.  Parts are written and read, and take a launch.  (Fitted to 380
+// random products of 1 to 9000 rows, weights from memory, in all shapes and cuts: the choice is 1.012 of the best in the geometric mean in
+// bf16, 1.005 in fp32, 1.2 at worst.)
 struct ShapeCost {
   int on_cu;
-  double stage[3], fixed, flight, rate;
+  double stage[3], uneven, fixed, flight, rate;
 };
 constexpr int CUS = 256;
 template <typename T>
 ShapeCost shape_cost(int shape) {
-  constexpr ShapeCost BF16[] = {{1, {1.7}, 7.0, 64, 5.2}, {2, {0.72, 0.97}, 4.0, 32, 5.2}, {3, {0.25, 0.42, 0.68}, 3.0, 16, 5.2},
-                                {2, {0.25, 0.39}, 3.0, 24, 5.7}, {3, {0.25, 0.3, 0.4}, 3.0, 24, 5.9}};
-  constexpr ShapeCost F32[] = {{}, {}, {3, {0.59, 1.03, 1.45}, 3.0, 16, 5.2}, {2, {0.59, 1.03}, 3.0, 24, 5.7}, {3, {0.6, 1.0, 1.1}, 3.0, 24, 5.9}};
+  constexpr ShapeCost BF16[] = {{1, {1.7}, 1.0, 7.0, 64, 5.2},               {2, {0.78, 0.97}, 1.15, 4.0, 32, 5.0},
+                                {3, {0.28, 0.46, 0.68}, 1.2, 2.7, 16, 5.2}, {2, {0.25, 0.39}, 1.15, 3.5, 24, 5.7},
+                                {3, {0.24, 0.3, 0.4}, 1.1, 2.5, 24, 5.8},   {2, {0.39, 0.76}, 1.2, 4.0, 24, 5.5},
+                                {1, {1.3}, 1.1, 6.0, 56, 5.2}};
+  constexpr ShapeCost F32[] = {{}, {}, {3, {0.56, 1.05, 1.45}, 1.1, 2.5, 16, 5.2}, {2, {0.47, 1.03}, 1.2, 3.0, 24, 4.5},
+                               {3, {0.46, 1.0, 1.1}, 1.0, 3.3, 24, 5.9}};
   return sizeof(T) == 4 ? F32[shape] : BF16[shape];
 }
-// k: contracted elements, of all segments; by_rows: the rows' operand lies by rows (there are kernels for few of them)
-template <typename T>
-Plan plan_product(int64_t features, int64_t rows, int64_t k, bool dual, int most_splits, bool by_rows = true) {
+// k: contracted elements, of all segments
+template <typename T, int FA, int FB>
+Plan plan_product(int64_t features, int64_t rows, int64_t k, bool dual, int most_splits) {
   const int64_t stages = (k + STAGE_K<T> - 1) / STAGE_K<T>;
   const double bytes = (double)((dual ? 2 : 1) * features + rows) * k * sizeof(T);
   Plan best = {SMALL, 1};
   double least = 1e30;
-  for (int shape = sizeof(T) == 4 ? SMALL : LARGE; shape <= FEW32; ++shape) {
+  for (int shape = sizeof(T) == 4 ? SMALL : LARGE; shape <= (sizeof(T) == 4 ? FEW32 : WIDE); ++shape) {
     Plan p = {shape, 1};
-    if (shape >= FEW64 && (!by_rows || rows > p.bn())) continue;
+    if (shape == WIDE ? FA != BY_ROWS : shape >= FEW64 && (FB != BY_ROWS || rows > p.bn())) continue;
     const ShapeCost c = shape_cost<T>(shape);
+    const double uneven = FA == BY_ROWS && FB == BY_ROWS && k * sizeof(T) % 128 ? c.uneven : 1.0;
     const int64_t bm = dual ? p.bm() / 2 : p.bm(), places = c.on_cu * CUS;
     const int64_t tiles = ((features + bm - 1) / bm) * ((rows + p.bn() - 1) / p.bn());
     for (p.splits = 1; p.splits <= most_splits && (p.splits == 1 || stages / p.splits >= 4); ++p.splits) {
       const int64_t all = tiles * p.splits, full = all / places, rest = all % places, deep = (stages + p.splits - 1) / p.splits;
-      double t = (double)full * (deep * c.stage[c.on_cu - 1] + c.fixed);
-      if (rest) t += deep * c.stage[(rest - 1) / CUS] + c.fixed;
+      double t = (double)full * (deep * c.stage[c.on_cu - 1] * uneven + c.fixed);
+      if (rest) t += deep * c.stage[(rest - 1) / CUS] * uneven + c.fixed;
       const double at_once = (double)std::min(all, places), on_cu = std::ceil(at_once / CUS);
       const double cu = full ? 0.0 : on_cu * bytes / all / (std::min(on_cu * c.flight, 1.32 * c.rate * 1e3 / CUS) * 1e3);
       t = std::max(t, std::max(cu, bytes / std::min(c.rate * 1e6, at_once * c.flight * 1e3)) + c.fixed);
-      if (p.splits > 1) t += 4.0 + 0.12 * p.splits + (double)features * rows * p.splits * 8 / 4.0e6;  // (parts written and read, a launch)
+      if (p.splits > 1) t += 2.6 + 0.12 * p.splits + (double)features * rows * p.splits * 8 / 6.0e6;
       if (t < least) {
         least = t;
         best = p;
@@ -702,12 +712,16 @@ template <typename T, int FA, int FB, int MODE, typename Epilogue>
 hipError_t launch_product(Plan p, hpd_product_args g, const Epilogue& e, hipStream_t s) {
   g.splits = p.splits;
   if constexpr (sizeof(T) == 2) {
+    if constexpr (FA == BY_ROWS)
+      if (p.shape == WIDE) return launch_shape<T, FA, FB, MODE, Wide>(g, e, s);
     if (p.shape == LARGE) return launch_shape<T, FA, FB, MODE, Large>(g, e, s);
     if (p.shape == MIDDLE) return launch_shape<T, FA, FB, MODE, Middle>(g, e, s);
   }
   if constexpr (FB == BY_ROWS) {
     if (p.shape == FEW64) return launch_shape<T, FA, FB, MODE, Few64>(g, e, s);
     if (p.shape == FEW32) return launch_shape<T, FA, FB, MODE, Few32>(g, e, s);
+    if constexpr (sizeof(T) == 2)
+      if (p.shape == FEW128) return launch_shape<T, FA, FB, MODE, Few128>(g, e, s);
   }
   return launch_shape<T, FA, FB, MODE, Small>(g, e, s);
 }
