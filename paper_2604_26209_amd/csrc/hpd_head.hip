@@ -2,7 +2,8 @@
 // x = hidden W^T stay in registers.
 //
 // Forward: a tile's rows give (m, s, t) = (max x, sum e^(x - m), sum e^(x - m) (x - m)) of its tokens of the vocabulary; a
-// second kernel joins a row's tiles: lse = m + log s, entropy = log s - t / s.  The maximum is subtracted before anything is scaled, so
+// second kernel joins a row's tiles: lse = m + log s, entropy = log s - t / s.  Few tokens: parts of the logits in fp32, summed and taken in
+// by the second kernel.  The maximum is subtracted before anything is scaled, so
 // that logits of any finite size keep the accuracy that they have.
 // Backward: piece by piece of the vocabulary, the logits again and from them dx_c = g ([c = target] - p) - ge p (log p + entropy),
 // rounded to the inputs' type; then the piece's rows of dW = dx^T hidden, and its part of dhidden = dx W in fp32.
@@ -99,6 +100,29 @@ struct RowSums {
   }
 };
 
+// A workgroup's threads have parts of a row's sums: the row's outputs.
+__device__ __forceinline__ void finish_row(Sums a, float4* of_wave, int64_t row, const float* at_target, const int32_t* targets, int32_t vocab,
+                                           float* logprob, float* lse, float* entropy) {
+#pragma unroll
+  for (int d = 32; d; d >>= 1) a = join(a, {__shfl_xor(a.m, d), __shfl_xor(a.s, d), __shfl_xor(a.t, d)});
+  if ((threadIdx.x & 63) == 0) of_wave[threadIdx.x >> 6] = make_float4(a.m, a.s, a.t, 0.f);
+  __syncthreads();
+  if (threadIdx.x == 0) {
+#pragma unroll
+    for (int w = 1; w < 4; ++w) a = join(a, {of_wave[w].x, of_wave[w].y, of_wave[w].z});
+    const float log_s = logf(a.s), total = a.s == 0.f ? -INFINITY : a.m + log_s;
+    if (lse) lse[row] = total;
+    if (entropy) entropy[row] = a.s == 0.f ? 0.f : log_s - a.t / a.s;
+    if (logprob) {
+      const int32_t t = targets[row];
+      float v = 0.f;
+      if (t >= 0 && t < vocab) v = a.s == 0.f ? -INFINITY : (*at_target - a.m) - log_s;
+      logprob[row] = v;
+    }
+  }
+  __syncthreads();
+}
+
 // a workgroup per row and round (a wave per row: 10 us instead of 5 for 3 rows of 1172 tiles)
 __global__ void __launch_bounds__(256) join_rows_kernel(const float4* parts, int32_t tiles, int64_t rows, const float* of_target,
                                                         const int32_t* targets, int32_t vocab, float* logprob, float* lse, float* entropy) {
@@ -113,24 +137,94 @@ __global__ void __launch_bounds__(256) join_rows_kernel(const float4* parts, int
 #pragma unroll
       for (int n = 0; n < 4; ++n) a = join(a, {v[n].x, v[n].y, v[n].z});
     }
+    finish_row(a, of_wave, row, of_target + row, targets, vocab, logprob, lse, entropy);
+  }
+}
+
+// Where a few tokens and a long width would leave CUs without work, the logits' contraction is cut: the logits come as parts in fp32,
+// [parts][rows][stride], stride a multiple of 4 (69 rows, 8192 channels and 1119 tokens in fp32: 31 us, 151 in whole sums; 12 rows, 5120 and
+// 2057 in bf16: 15, 27).  Four successive ones:
+__device__ __forceinline__ void sum_parts(const float* parts, int32_t n_parts, int64_t rows, int64_t stride, int64_t row, int64_t c, float* x) {
+  fetch4(parts + row * stride + c, x);
+  for (int32_t p = 1; p < n_parts; ++p) {
+    float v[4];
+    fetch4(parts + (p * rows + row) * stride + c, v);
 #pragma unroll
-    for (int d = 32; d; d >>= 1) a = join(a, {__shfl_xor(a.m, d), __shfl_xor(a.s, d), __shfl_xor(a.t, d)});
-    if ((threadIdx.x & 63) == 0) of_wave[threadIdx.x >> 6] = make_float4(a.m, a.s, a.t, 0.f);
-    __syncthreads();
-    if (threadIdx.x == 0) {
+    for (int e = 0; e < 4; ++e) x[e] += v[e];
+  }
+}
+__global__ void __launch_bounds__(256) rows_of_parts_kernel(const float* parts, int32_t n_parts, int64_t stride, int64_t rows, const int32_t* targets,
+                                                            int32_t vocab, float* logprob, float* lse, float* entropy) {
+  __shared__ float4 of_wave[4];
+  __shared__ float at_target;
+  for (int64_t row = blockIdx.x; row < rows; row += gridDim.x) {
+    const int32_t target = logprob ? targets[row] : -1;
+    Sums a = {-INFINITY, 0.f, 0.f};
+    for (int32_t c = 4 * threadIdx.x; c < vocab; c += 4 * 256) {
+      float x[4];
+      sum_parts(parts, n_parts, rows, stride, row, c, x);
+      Sums b = {-INFINITY, 0.f, 0.f};
 #pragma unroll
-      for (int w = 1; w < 4; ++w) a = join(a, {of_wave[w].x, of_wave[w].y, of_wave[w].z});
-      const float log_s = logf(a.s), total = a.s == 0.f ? -INFINITY : a.m + log_s;
-      if (lse) lse[row] = total;
-      if (entropy) entropy[row] = a.s == 0.f ? 0.f : log_s - a.t / a.s;
-      if (logprob) {
-        const int32_t t = targets[row];
-        float v = 0.f;
-        if (t >= 0 && t < vocab) v = a.s == 0.f ? -INFINITY : (of_target[row] - a.m) - log_s;
-        logprob[row] = v;
+      for (int e = 0; e < 4; ++e) {
+        if (c + e >= vocab) x[e] = -INFINITY;
+        if (c + e == target) at_target = x[e];
+        b.m = fmaxf(b.m, x[e]);
       }
+      const float m = b.m == -INFINITY ? 0.f : b.m;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const float d = x[e] - m, p = fast_exp2(d * LOG2E);
+        b.s += p;
+        b.t = fmaf(p, fmaxf(d, -1e4f), b.t);
+      }
+      a = join(a, b);
     }
-    __syncthreads();
+    finish_row(a, of_wave, row, &at_target, targets, vocab, logprob, lse, entropy);
+  }
+}
+
+// What a row's gradients take from it.
+struct RowGradient {
+  float L, some, g, ge, H;
+  int32_t target;
+  __device__ __forceinline__ RowGradient(int64_t row, const int32_t* targets, const float* lse, const float* entropy, const float* g_logprob,
+                                         const float* g_entropy, int32_t vocab) {
+    const int32_t t = targets ? targets[row] : -1;
+    // (a row of nothing but -infinity: no probability anywhere)
+    const float row_lse = lse[row];
+    L = row_lse == -INFINITY ? 0.f : row_lse;
+    some = row_lse == -INFINITY ? 0.f : 1.f;
+    ge = g_entropy && some != 0.f ? g_entropy[row] : 0.f;
+    H = g_entropy ? entropy[row] : 0.f;
+    g = g_logprob ? g_logprob[row] : 0.f;
+    if (t < 0 || t >= vocab || some == 0.f) g = 0.f;
+    target = t < 0 ? -1 : t;
+  }
+  // of logit x, without what the target's has besides
+  __device__ __forceinline__ float of(float x, bool with_entropy) const {
+    const float lp = x - L, p = fast_exp2(lp * LOG2E) * some;
+    return -p * (with_entropy && p > 0.f ? fmaf(ge, lp + H, g) : g);
+  }
+};
+
+// the logits' gradients from parts of the logits, [rows][out_stride], zeros from vocab up to a multiple of 8
+template <typename T>
+__global__ void __launch_bounds__(256) gradients_of_parts_kernel(const float* parts, int32_t n_parts, int64_t stride, int64_t rows, const int32_t* targets,
+                                                                 const float* lse, const float* entropy, const float* g_logprob, const float* g_entropy,
+                                                                 int32_t vocab, T* out, int64_t out_stride) {
+  const int64_t per = ((int64_t)vocab + 7) / 8 * 2, all = per * rows;
+  for (int64_t i = blockIdx.x * 256ll + threadIdx.x; i < all; i += gridDim.x * 256ll) {
+    const int64_t row = i / per, c = (i - row * per) * 4;
+    const RowGradient r(row, targets, lse, entropy, g_logprob, g_entropy, vocab);
+    float x[4] = {0.f, 0.f, 0.f, 0.f}, v[4];
+    if (c < stride) sum_parts(parts, n_parts, rows, stride, row, c, x);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      v[e] = r.of(x[e], g_entropy != nullptr);
+      if (c + e == r.target) v[e] += r.g;
+      if (c + e >= vocab) v[e] = 0.f;
+    }
+    store4(out + row * out_stride + c, v);
   }
 }
 
@@ -152,15 +246,10 @@ struct LogitGradients {
       const int64_t first_row = at.row + 32 * j;
       asm volatile("" ::: "memory");  // (a block's rows are asked for when they are needed, not all at once)
       const int64_t row = first_row + l < rows ? first_row + l : rows - 1;
-      const int32_t t = targets ? targets[row] : -1, target = t < 0 ? -1 : t - first;
-      // (a row of nothing but -infinity: no probability anywhere)
-      const float row_lse = lse[row], L = row_lse == -INFINITY ? 0.f : row_lse, some = row_lse == -INFINITY ? 0.f : 1.f;
-      const float ge = g_entropy && some != 0.f ? g_entropy[row] : 0.f, H = g_entropy ? entropy[row] : 0.f;
-      float g = g_logprob ? g_logprob[row] : 0.f;
-      if (t < 0 || t >= whole || some == 0.f) g = 0.f;
+      const RowGradient of_row(row, targets, lse, entropy, g_logprob, g_entropy, whole);
       // the lane's target and the end of the piece, counted from the wave's first token
-      const int64_t behind = (int64_t)target - at.feature, inside = vocab - at.feature;
-      const int32_t mine = target < 0 || behind < 0 || behind >= 32 * MI ? -1 : (int32_t)behind;
+      const int64_t behind = (int64_t)of_row.target - first - at.feature, inside = vocab - at.feature;
+      const int32_t mine = of_row.target < 0 || behind < 0 || behind >= 32 * MI ? -1 : (int32_t)behind;
       const bool any = __any(mine >= 0), edge = inside < 32 * MI;
 #pragma unroll
       for (int i = 0; i < MI; ++i)
@@ -168,15 +257,11 @@ struct LogitGradients {
         for (int q = 0; q < 4; ++q) {
           float v[4];
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const float lp = sum_of<S>(acc[i][j], 4 * q + e) - L, p = fast_exp2(lp * LOG2E) * some;
-            v[e] = -p * g;
-            if (g_entropy) v[e] = -p * (p > 0.f ? fmaf(ge, lp + H, g) : g);
-          }
+          for (int e = 0; e < 4; ++e) v[e] = of_row.of(sum_of<S>(acc[i][j], 4 * q + e), g_entropy != nullptr);
           if (any) {
 #pragma unroll
             for (int e = 0; e < 4; ++e)
-              if (mine == 32 * i + 8 * q + 4 * h + e) v[e] += g;
+              if (mine == 32 * i + 8 * q + 4 * h + e) v[e] += of_row.g;
           }
           if (edge) {
 #pragma unroll
@@ -203,6 +288,7 @@ constexpr int MOST_SPLITS = 32;                      // of a contraction over a 
 constexpr int64_t PIECE_BYTES = (int64_t)256 << 20;  // of the logits' gradients of a piece, about
 
 int64_t round16(int64_t x) { return (x + 15) / 16 * 16; }
+int64_t round4(int64_t x) { return (x + 3) / 4 * 4; }
 
 template <typename T>
 hpd_operand operand(const void* p, int64_t stride, int64_t size) {
@@ -215,10 +301,10 @@ struct ForwardPlan {
   Plan product;
   int64_t tiles, of_target, bytes;
   ForwardPlan(int64_t n, int32_t width, int32_t vocab) {
-    product = plan_product<T, BY_ROWS, BY_ROWS>(vocab, n, width, false, 1);
+    product = plan_product<T, BY_ROWS, BY_ROWS>(vocab, n, width, false, MOST_SPLITS, 1.2 * (vocab / 1024 + 1));  // (a row's turns in its one workgroup)
     tiles = (vocab + product.bm() - 1) / product.bm();
     of_target = n * tiles * (int64_t)sizeof(float4);
-    bytes = round16(of_target + n * 4);
+    bytes = product.splits > 1 ? product.splits * n * round4(vocab) * 4 : round16(of_target + n * 4);
   }
 };
 template <typename T>
@@ -231,11 +317,12 @@ struct BackwardPlan {
     const int64_t most = std::max(UNIT, PIECE_BYTES / (std::max<int64_t>(n, 1) * (int64_t)sizeof(T)) / UNIT * UNIT);
     const int64_t pieces = (vocab + most - 1) / most;
     piece = ((vocab + pieces - 1) / pieces + UNIT - 1) / UNIT * UNIT;
-    logits = plan_product<T, BY_ROWS, BY_ROWS>(std::min<int64_t>(piece, vocab), n, width, false, 1);
+    logits = plan_product<T, BY_ROWS, BY_ROWS>(std::min<int64_t>(piece, vocab), n, width, false, pieces == 1 ? MOST_SPLITS : 1);
     d_hidden = plan_product<T, BY_COLUMNS, BY_ROWS>(width, n, std::min<int64_t>(piece, vocab), false, MOST_SPLITS);
     d_weight = plan_product<T, BY_COLUMNS, BY_COLUMNS>(width, std::min<int64_t>(piece, vocab), n, false, 1);
     parts = round16(n * piece * (int64_t)sizeof(T));
-    bytes = parts + d_hidden.splits * n * width * 4;
+    // (the logits' parts have been read when those of dhidden are written)
+    bytes = parts + std::max<int64_t>(d_hidden.splits * n * width, logits.splits > 1 ? logits.splits * n * round4(vocab) : 0) * 4;
   }
 };
 
@@ -248,9 +335,17 @@ hipError_t forward(const hpd_head_args& a, hipStream_t s) {
   const hpd_product_args g = {operand<T>(a.weight, a.weight_stride, a.vocab), operand<T>(a.hidden, a.hidden_stride, a.n_rows),
                               a.width, 1, 0, 0};
   const int32_t* const targets = a.logprob ? a.targets : nullptr;
+  const dim3 a_row_each((uint32_t)std::min<int64_t>(a.n_rows, 1 << 20));
+  if (plan.product.splits > 1) {
+    float* const logits = (float*)a.workspace;
+    const hipError_t e = launch_product<T, BY_ROWS, BY_ROWS, PLAIN>(plan.product, g, StorePart{logits, round4(a.vocab), a.n_rows, 0}, s);
+    if (e != hipSuccess) return e;
+    rows_of_parts_kernel<<<a_row_each, dim3(256), 0, s>>>(logits, plan.product.splits, round4(a.vocab), a.n_rows, targets, a.vocab, a.logprob, a.lse, a.entropy);
+    return hipGetLastError();
+  }
   const hipError_t e = launch_product<T, BY_ROWS, BY_ROWS, PLAIN>(plan.product, g, RowSums{targets, of_target, parts, a.vocab, tiles, a.n_rows}, s);
   if (e != hipSuccess) return e;
-  join_rows_kernel<<<dim3((uint32_t)std::min<int64_t>(a.n_rows, 1 << 20)), dim3(256), 0, s>>>(parts, tiles, a.n_rows, of_target, targets, a.vocab, a.logprob, a.lse, a.entropy);
+  join_rows_kernel<<<a_row_each, dim3(256), 0, s>>>(parts, tiles, a.n_rows, of_target, targets, a.vocab, a.logprob, a.lse, a.entropy);
   return hipGetLastError();
 }
 
@@ -267,9 +362,18 @@ hipError_t backward(const hpd_head_backward_args& a, hipStream_t s) {
     const T* const w = (const T*)a.weight + v0 * a.weight_stride;
     if (N > 0) {
       const hpd_product_args g = {operand<T>(w, a.weight_stride, n), operand<T>(a.hidden, a.hidden_stride, N), (int32_t)D, 1, 0, 0};
-      e = launch_product<T, BY_ROWS, BY_ROWS, PLAIN>(
-          plan.logits, g,
-          LogitGradients<T>{a.targets, a.lse, a.entropy, a.g_logprob, a.g_entropy, dx, piece, N, (int32_t)v0, (int32_t)n, a.vocab}, s);
+      if (plan.logits.splits > 1) {
+        const int64_t stride = round4(a.vocab), all = (n + 7) / 8 * 2 * N;
+        e = launch_product<T, BY_ROWS, BY_ROWS, PLAIN>(plan.logits, g, StorePart{parts, stride, N, 0}, s);
+        if (e != hipSuccess) return e;
+        gradients_of_parts_kernel<T><<<dim3((uint32_t)std::min<int64_t>((all + 255) / 256, 1 << 16)), dim3(256), 0, s>>>(
+            parts, plan.logits.splits, stride, N, a.targets, a.lse, a.entropy, a.g_logprob, a.g_entropy, a.vocab, dx, piece);
+        e = hipGetLastError();
+      } else {
+        e = launch_product<T, BY_ROWS, BY_ROWS, PLAIN>(
+            plan.logits, g,
+            LogitGradients<T>{a.targets, a.lse, a.entropy, a.g_logprob, a.g_entropy, dx, piece, N, (int32_t)v0, (int32_t)n, a.vocab}, s);
+      }
     }
     if (e == hipSuccess && a.d_hidden && N > 0) {
       const hpd_product_args g = {operand<T>(w, a.weight_stride, D), operand<T>(dx, piece, N), (int32_t)n, 1, 0, 0};

@@ -669,9 +669,9 @@ ShapeCost shape_cost(int shape) {
                                {3, {0.46, 1.0, 1.1}, 1.0, 3.3, 24, 5.9}};
   return sizeof(T) == 4 ? F32[shape] : BF16[shape];
 }
-// k: contracted elements, of all segments
+// k: contracted elements, of all segments; cut: us that parts cost besides being written and read
 template <typename T, int FA, int FB>
-Plan plan_product(int64_t features, int64_t rows, int64_t k, bool dual, int most_splits) {
+Plan plan_product(int64_t features, int64_t rows, int64_t k, bool dual, int most_splits, double cut = 0.0) {
   const int64_t stages = (k + STAGE_K<T> - 1) / STAGE_K<T>;
   const double bytes = (double)((dual ? 2 : 1) * features + rows) * k * sizeof(T);
   Plan best = {SMALL, 1};
@@ -690,7 +690,7 @@ Plan plan_product(int64_t features, int64_t rows, int64_t k, bool dual, int most
       const double at_once = (double)std::min(all, places), on_cu = std::ceil(at_once / CUS);
       const double cu = full ? 0.0 : on_cu * bytes / all / (std::min(on_cu * c.flight, 1.32 * c.rate * 1e3 / CUS) * 1e3);
       t = std::max(t, std::max(cu, bytes / std::min(c.rate * 1e6, at_once * c.flight * 1e3)) + c.fixed);
-      if (p.splits > 1) t += 2.6 + 0.12 * p.splits + (double)features * rows * p.splits * 8 / 6.0e6;
+      if (p.splits > 1) t += cut + 2.6 + 0.12 * p.splits + (double)features * rows * p.splits * 8 / 6.0e6;
       if (t < least) {
         least = t;
         best = p;

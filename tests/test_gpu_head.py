@@ -85,6 +85,19 @@ def test_tiles_of_every_size(dtype, rows, width, vocab):
     _check(_inputs(rows, width, vocab, dtype, seed=9), dtype)
 
 
+def _cut(dtype, rows, width, vocab):
+    """Whether the forward call's workspace holds parts of the logits."""
+    return B.hpd_head_logprobs_workspace(DT[dtype], rows, width, vocab)[0] >= 2 * 4 * rows * vocab
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows, width, vocab, ge", [(1, 8192, 1, True), (5, 8192, 67, True), (69, 8192, 1119, False),
+                                                    (130, 5120, 385, True), (33, 4104, 4, True), (2, 16384, 2050, True)])
+def test_contractions_in_parts(rows, width, vocab, ge, dtype):
+    assert _cut(dtype, rows, width, vocab)
+    _check(_inputs(rows, width, vocab, dtype, seed=10), dtype, ge)
+
+
 @pytest.mark.parametrize("hidden, weight, g, ge", [(1, 0, 1, 1), (0, 1, 1, 1), (1, 1, 0, 1), (1, 1, 1, 0), (1, 1, 0, 0)])
 def test_parts_that_are_not_wanted(hidden, weight, g, ge):
     i = _inputs(70, 136, 500, "bf16", seed=2)
@@ -124,8 +137,17 @@ def test_no_rows():
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("rows", [5, 150])
 def test_rows_that_are_not_finite(rows, dtype):
+    _check_not_finite(rows, 72, 300, dtype)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_rows_that_are_not_finite_in_parts(dtype):
+    assert _cut(dtype, 5, 8192, 300) and _cut(dtype, 5, 8192, 1)
+    _check_not_finite(5, 8192, 300, dtype)
+
+
+def _check_not_finite(rows, width, vocab, dtype):
     """+infinity and NaN among a row's logits: NaN in that row alone.  -infinity: a token of probability 0."""
-    width, vocab = 72, 300
     i = _inputs(rows, width, vocab, dtype, seed=4)
     i["t"][3] = 7
     i["x"][:, 0] = 1.0
@@ -170,7 +192,15 @@ def test_logits_of_any_size(scale):
 
 @pytest.mark.parametrize("rows", [3, 200])
 def test_equal_calls_give_equal_bits_on_any_stream_and_in_a_graph(rows):
-    width, vocab = 264, 5003
+    _check_equal_bits(rows, 264, 5003)
+
+
+def test_equal_calls_give_equal_bits_in_parts():
+    assert _cut("bf16", 70, 8192, 515)
+    _check_equal_bits(70, 8192, 515)
+
+
+def _check_equal_bits(rows, width, vocab):
     i = _inputs(rows, width, vocab, "bf16", seed=6)
     outs = [torch.empty(rows, device="cuda") for _ in range(3)]
     dx, dw = torch.empty_like(i["x"]), torch.empty_like(i["w"])
