@@ -532,7 +532,8 @@ int hpd_token_logprobs_backward(int32_t dtype, int64_t n_rows, int32_t vocab, in
  * No output may overlap an input or the workspace (HPD_E_INVALID where they start at the same address).
  * No atomics: equal calls give equal bits.  A row's outputs and its gradient come from that row and the weights alone: what is not finite
  * in a row stays there.  The weights' gradients are sums over all rows, and such a row reaches them even where its own gradient is 0.
- * The calls only enqueue kernels, allocate nothing and may be captured in a HIP graph.  Workspaces: device memory, the bytes
+ * An infinite weight times a gradient of 0 is NaN, as in any product: gradients are for finite weights.
+ * The calls only enqueue kernels, on a stream of the current device, allocate nothing and may be captured in a HIP graph.  Workspaces: device memory, the bytes
  * that the _workspace call reports (NULL if 0), 16-byte aligned, not shared by calls that overlap.
  */
 enum hpd_activation {
@@ -575,7 +576,7 @@ int hpd_gated_ffn_workspace(const hpd_ffn_config* cfg, int64_t n_rows, int64_t* 
 
 /* hpd_head_logprobs - what hpd_token_logprobs gives for the logits x = hidden weight^T (fp32, never in memory), without
  * alternatives.
- *   hidden [n_rows][width], weight [vocab][width]
+ *   hidden [n_rows][width], weight [vocab][width]; a stride of 0: the rows lie next to each other
  *   targets : device int32 [n_rows] or NULL (then logprob is not written); a row whose target is outside [0, vocab) has
  *             logprob 0
  *   logprob, lse, entropy : device fp32 [n_rows], each may be NULL
@@ -587,7 +588,8 @@ int hpd_head_logprobs(int32_t dtype, int64_t n_rows, int32_t width, int32_t voca
 /* hpd_head_logprobs_backward - gradients of hidden and weight for given gradients of log probability and entropy: with
  *   d_c = g_logprob ([c = target] - p_c) - g_entropy p_c (log p_c + entropy),  p = exp(x - lse),
  * d_hidden = d weight, d_weight = d^T hidden.  The logits are computed again, in pieces of the vocabulary.
- *   lse, entropy (needed with g_entropy only) : as the forward call has left them
+ *   lse, entropy (needed with g_entropy only) : as the forward call has left them (where a token has nearly all of the probability,
+ *             1 - p is as far off as an lse from another product's logits is from these)
  *   g_logprob, g_entropy : device fp32 [n_rows] or NULL (0); rows without a target inside [0, vocab) take 0 as g_logprob
  *   d_hidden, d_weight : each may be NULL (not made); written, not added to; without rows d_weight is zeros
  */

@@ -224,15 +224,17 @@ struct Shape {
   // Sums of a block, each over a part of a stage's steps, added up at the end.  A sum is rounded with every product: two halve the
   // error of a long contraction, four quarter it (fp32 gradients of the block for 1801 rows: off by 5e-7 in place of 1e-6; the
   // entropies of three rows of 150001 tokens: 4e-7, 1.5e-6).
-  static constexpr int SUMS = MANY ? 1 : MI * NI > 2 ? 1 : 4 / (MI * NI);
+  static constexpr int SUMS = MANY ? 1 : 4 / (MI * NI);
 };
 // DUAL: a tile's features half and half from two A; SEGMENTS: a second A and B are contracted after the first; TAIL: any number of contracted
 // elements, A by columns and B by rows, with zeros behind B's last up to a multiple of 16 bytes
 enum { PLAIN = 0, DUAL = 1, SEGMENTS = 2, TAIL = 3 };
 // bf16 products of 4096 elements: Large 1.2 PFLOP/s for 4096 x 4096 and more; Middle 1.06 from 4096 x 2048 (Large 0.72); Small 0.61 for
-// 2048 x 1024 (Middle 0.39).  Few rows, where the weights' bytes are what it takes: Few32 5.9 TB/s for 24576 features and a row, 6.4 for
-// 48000 (without the hint that the weights will not be read again 5.3 and 5.8; Small 4.9 and 5.5), Few64 4.5 for 64 rows (Small 4.2).  fp32:
-// Small 0.13 to 0.14 PFLOP/s from 2048 x 1024 on (128 x 128 with eight waves: 0.146 at most, 0.07 for 2048 x 1024), and Few.
+// 2048 x 1024 (Middle 0.39).  Wide where its tiles go into fewer or fuller rounds: 256 of them for 24576 features x 512 rows in 107 us,
+// 192 of Large in 125.  Few rows, where the weights' bytes are what it takes: Few32 5.9 TB/s for 24576 features and a row, 6.4 for
+// 48000 (without the hint that the weights will not be read again 5.3 and 5.8; Small 4.9 and 5.5), Few64 4.5 for 64 rows (Small 4.2), Few128
+// 15544 features x 126 rows of 4096 in 36 us (Small 45, Middle 67; 64 x 192 tiles were never the best).  fp32: Small 0.13 to 0.14 PFLOP/s
+// from 2048 x 1024 on (128 x 128 with eight waves: 0.146 at most, 0.07 for 2048 x 1024), and Few.
 using Large = Shape<256, 256, 2, 2, 2, 1>;
 using Middle = Shape<128, 128, 2, 4, 2, 2>;
 using Small = Shape<64, 64, 2, 2, 3, 3>;
@@ -260,8 +262,8 @@ struct Place {
 // feature of register r in half h of the wave, counted from its block's first
 __device__ __forceinline__ int block_row(int r, int h) { return 8 * (r / 4) + 4 * h + r % 4; }
 
-// Workgroups go round the XCDs: each takes a run of tiles, so that what its L2 holds is shared.  Within a run, four tiles of m
-// for one of n after another.
+// Workgroups go round the XCDs: each takes a run of tiles, so that what its L2 holds is shared (12288 x 16384 x 4096 in bf16: 1421 us
+// and 2.4 GB read, 1534 and 6.6 without).  Within a run, four tiles of m for one of n after another (two or eight were no faster).
 __device__ __forceinline__ void tile_of(int32_t id, int32_t total, int32_t tiles_m, int32_t tiles_n, int32_t& m, int32_t& n) {
   const int32_t per = total / 8, rest = total % 8, x = id % 8;
   id = x * per + (x < rest ? x : rest) + id / 8;

@@ -170,6 +170,28 @@ def test_halves_of_one_matrix(rows, dtype):
         assert torch.equal(x, y)
 
 
+@pytest.mark.parametrize("dtype, rows, width, inner", [("bf16", 509, 4096, 12288), ("bf16", 515, 256, 520), ("f32", 300, 264, 136)])
+def test_rows_8_mb_apart(dtype, rows, width, inner):
+    """The widest strides, more than 4 GB from the first row to the last in bf16: the bits of rows without gaps."""
+    i, cfg = _inputs(rows, width, inner, dtype, seed=12), B.hpd_ffn_config(width, inner, DT[dtype], ACTS["silu"])
+    stride = (8 << 20) // i["x"].element_size()
+    far = torch.empty((rows, stride), dtype=TD[dtype], device="cuda")
+    x, out, d_out, dx = (far[:, k * width:(k + 1) * width] for k in range(4))
+    gate, up = (far[:, k:k + inner] for k in (stride // 2, stride // 2 + inner))
+    x.copy_(i["x"])
+    d_out.copy_(i["d_out"])
+    st = B.hpd_ffn_strides(x=stride, out=stride, gate=stride, up=stride, d_out=stride, d_x=stride)
+    ws = [B.alloc_ffn_workspace(cfg, rows, b) for b in (False, True)]
+    grads = [torch.empty_like(i[k]) for k in ("wg", "wu", "wd")]
+    B.hpd_gated_ffn(cfg, rows, x, i["wg"], i["wu"], i["wd"], out, gate, up, ws[0], st)
+    B.hpd_gated_ffn_backward(cfg, rows, x, i["wg"], i["wu"], i["wd"], gate, up, d_out, dx, *grads, ws[1], st)
+    near = [torch.empty_like(i[k]) for k in ("x", "g", "u", "x", "wg", "wu", "wd")]
+    B.hpd_gated_ffn(cfg, rows, i["x"], i["wg"], i["wu"], i["wd"], *near[:3], ws[0])
+    B.hpd_gated_ffn_backward(cfg, rows, i["x"], i["wg"], i["wu"], i["wd"], near[1], near[2], i["d_out"], *near[3:], ws[1])
+    for a, b in zip((out, gate, up, dx, *grads), near):
+        assert torch.equal(a, b)
+
+
 def test_two_calls_at_once():
     """Calls on two streams with workspaces of their own."""
     rows, width, inner = 257, 512, 1032

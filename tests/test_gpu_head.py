@@ -284,3 +284,24 @@ def test_weights_behind_4_gb():
     assert bool(((dx.double() - want).abs() <= 2.0 ** -7 * (d[:, far].abs() @ w[far].double().abs()) + 1e-30).all())
     want = d[:, far].T @ x.double()
     assert bool(((dw[far].double() - want).abs() <= 2.0 ** -6 * (d[:, far].abs().T @ x.double().abs())).all())
+
+
+@pytest.mark.parametrize("dtype, rows, width, vocab", [("bf16", 600, 256, 9001), ("f32", 300, 264, 501), ("bf16", 520, 4096, 33)])
+def test_rows_8_mb_apart(dtype, rows, width, vocab):
+    """The widest strides of hidden states and their gradients: the bits of rows without gaps."""
+    i = _inputs(rows, width, vocab, dtype, seed=11)
+    stride = (8 << 20) // i["x"].element_size()
+    far = torch.empty((rows, stride), dtype=TD[dtype], device="cuda")
+    x, dx = far[:, :width], far[:, width:2 * width]
+    x.copy_(i["x"])
+    ws = [B.alloc_head_workspace(DT[dtype], rows, width, vocab, b) for b in (False, True)]
+
+    def run(x, x_stride, dx):
+        outs, dw = [torch.empty(rows, device="cuda") for _ in range(3)], torch.empty_like(i["w"])
+        B.hpd_head_logprobs(DT[dtype], rows, width, vocab, x, x_stride, i["w"], 0, i["t"], *outs, ws[0])
+        B.hpd_head_logprobs_backward(DT[dtype], rows, width, vocab, x, x_stride, i["w"], 0, i["t"], outs[1], outs[2], i["g"], i["ge"],
+                                     dx, x_stride, dw, 0, ws[1])
+        return (*outs, dx, dw)
+
+    for a, b in zip(run(x, stride, dx), run(i["x"], 0, torch.empty_like(i["x"]))):
+        assert torch.equal(a, b)
