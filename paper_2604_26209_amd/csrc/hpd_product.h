@@ -91,6 +91,14 @@ __device__ __forceinline__ void load_to_lds(uint32_t lds, const uint32_t* off, i
   }
 #undef HPD_LOADS_TO_LDS
 }
+// a dword a lane to 256 bytes of LDS that nobody reads: the lines come to the L2
+__device__ __forceinline__ void touch(uint32_t lds, uint32_t off, int32x4 buf) {
+  uint32_t keep;
+  asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\t"
+               "buffer_load_dword %2, %3, 0 offen lds\n\t"
+               "s_mov_b32 m0, %0"
+               : "=&s"(keep) : "s"(lds), "v"(off), "s"(buf) : "memory");
+}
 __device__ __forceinline__ uint32_t product_lds(const void* p) {
   return (uint32_t)reinterpret_cast<uintptr_t>((const __attribute__((address_space(3))) char*)p);
 }
@@ -143,6 +151,18 @@ struct Tile {
       }
       off[i] += BIAS - i % GROUP * 1024;
     }
+  }
+  // the lane's line of a stage, of those that the wave touches
+  static __device__ __forceinline__ uint32_t line(int64_t stride, int64_t size, int wave, int lane) {
+    constexpr int MINE = R / WAVES;
+    const int n = wave * MINE + lane;
+    if (lane >= MINE) return OUTSIDE;
+    if (FORM == BY_ROWS) {
+      const int r = DUAL ? n % (R / 2) : n;
+      return r < size ? (uint32_t)r * (uint32_t)stride + BIAS : OUTSIDE;
+    }
+    const int k = n / (RB / 128), c = n % (RB / 128) * 128;
+    return c / (int)sizeof(T) < size ? (uint32_t)k * (uint32_t)stride + c + BIAS : OUTSIDE;
   }
   // the buffer of a stage that begins at p and has `left` (at least 1) elements of k: by columns, it ends behind the last of them
   static __device__ __forceinline__ int32x4 buffer(const char* p, int64_t stride, int left) {
@@ -221,6 +241,11 @@ struct Shape {
   static constexpr int STAGE_BYTES = (BM + BN) * 128;
   static constexpr int SMEM = STAGES * STAGE_BYTES, TURN = SMEM / WAVES / 4096 * 4096;  // of it, a wave's when its sums are stored
   static constexpr bool MANY = MI * NI * 16 > 128;  // the sums are in accumulation registers
+  // Two stages on their way are less than the latency of memory takes: each wave touches lines of A two stages further on.  In bf16, features x rows x
+  // contracted, of equal values (under the least power): 24576 x 512 x 4096 99 -> 87 us, 16544 x 3520 x 5120 513 -> 437, 5120 x 2274 x 12256
+  // 276 -> 225, 8192 x 8192 x 8192 716 -> 692.  (One stage further on: the same where rows are of whole lines, else less; three, B's
+  // lines too, or 128 x 128 tiles: slower.)
+  static constexpr int TOUCH = STAGES == 2 && WGS == 1;
   // Sums of a block, each over a part of a stage's steps, added up at the end.  A sum is rounded with every product: two halve the
   // error of a long contraction, four quarter it (fp32 gradients of the block for 1801 rows: off by 5e-7 in place of 1e-6; the
   // entropies of three rows of 150001 tokens: 4e-7, 1.5e-6).
@@ -288,7 +313,7 @@ __global__ void __launch_bounds__(64 * S::WAVES, (S::WGS * S::WAVES + 3) / 4) pr
   // all the time (1 % of the largest products).
   constexpr bool MASKED = MODE == SEGMENTS || MODE == TAIL;
   constexpr int SUMS = sizeof(T) == 4 && IN_ORDER<Epilogue> && !S::ONCE ? 1 : S::SUMS;
-  __shared__ __attribute__((aligned(4096))) char smem[S::SMEM];
+  __shared__ __attribute__((aligned(4096))) char smem[S::SMEM + S::TOUCH * 256];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wave_m = wave % S::WM, wave_n = wave / S::WM;
 
@@ -356,6 +381,19 @@ __global__ void __launch_bounds__(64 * S::WAVES, (S::WGS * S::WAVES + 3) / 4) pr
     // (arguments may have been loaded: with those on their way, the wait for one operand from LDS would be one for all)
     __builtin_amdgcn_s_waitcnt(0xc07f);
   };
+  // of A's stage two behind the one that was loaded last, if it is a whole one behind that
+  const uint32_t line = TA::line(g.a.stride, g.a.size - m0, wave, lane), nowhere = __builtin_amdgcn_readfirstlane(lds + S::SMEM);
+  auto touch_ahead = [&]() {
+    if constexpr (S::TOUCH) {
+      int32x4 buf = st.a;
+      if (MODE == DUAL)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) buf[i] = wave >= S::WAVES / 2 ? st.a1[i] : st.a[i];
+      forward(buf, 2 * step_a);
+      buf[2] = lt + 1 < plain ? (int32_t)(RANGE + BIAS) : 0;
+      touch(nowhere, line, buf);
+    }
+  };
   auto load = [&](int i, auto masked) {
     constexpr bool M = decltype(masked)::value;
     if (i < TA::GROUPS)
@@ -410,8 +448,9 @@ __global__ void __launch_bounds__(64 * S::WAVES, (S::WGS * S::WAVES + 3) / 4) pr
     next_stage(s);
 #pragma unroll
     for (int i = 0; i < GROUPS; ++i) load(i, std::true_type{});
+    touch_ahead();
   }
-  wait_loads<LOADS * (S::STAGES - 1)>();
+  wait_loads<LOADS * (S::STAGES - 1) + S::TOUCH * S::STAGES>();
   meet();
 #pragma unroll
   for (int i = 0; i < READS; ++i) read(lds, 0, 0, i);
@@ -425,7 +464,7 @@ __global__ void __launch_bounds__(64 * S::WAVES, (S::WGS * S::WAVES + 3) / 4) pr
 #pragma unroll
         for (int i = n * READS / BLOCKS; i < (n + 1) * READS / BLOCKS; ++i) read(here, step + 1, (step + 1) & 1, i);
       });
-    wait_loads<LOADS * (S::STAGES - 2)>();
+    wait_loads<LOADS * (S::STAGES - 2) + S::TOUCH * (S::STAGES - 1)>();
     meet();
     next_stage(slot);
     products(3, [&](int n) {
@@ -434,6 +473,7 @@ __global__ void __launch_bounds__(64 * S::WAVES, (S::WGS * S::WAVES + 3) / 4) pr
 #pragma unroll
       for (int i = n * GROUPS / BLOCKS; i < (n + 1) * GROUPS / BLOCKS; ++i) load(i, std::integral_constant<bool, MASKED>{});
     });
+    touch_ahead();
     slot = next;
   }
   wait_loads<0>();
