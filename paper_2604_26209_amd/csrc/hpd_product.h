@@ -693,9 +693,9 @@ struct Plan {
 // The least time by a simple account, in us: workgroups go in rounds of as many as run at a time.  Each takes `fixed` for its start and
 // end, and for a stage stage[n - 1] where n run on its CU, `uneven` times that where contracted rows do not begin at multiples of 128 bytes
 // (a row's part of a stage is then in two lines).  What is read comes at `rate` TB/s at most; each workgroup has `flight` KB of it on the
-// way, about 1 us, and a CU takes a third more than its share of the rate.  Parts are written and read, and take a launch.  (Fitted to 380
-// random products of 1 to 9000 rows, weights from memory, in all shapes and cuts: the choice is 1.012 of the best in the geometric mean in
-// bf16, 1.005 in fp32, 1.2 at worst.)
+// way, about 1 us, and a CU takes a third more than its share of the rate.  Parts are written and read, and take a launch.  (Fitted to
+// random products of 1 to 9000 rows, weights from memory, in all shapes and cuts: of 460 in bf16 and 240 in fp32 the choice takes 1.01 times
+// the best one's time in the geometric mean, 1.2 at worst.)
 struct ShapeCost {
   int on_cu;
   double stage[3], uneven, fixed, flight, rate;
@@ -703,10 +703,10 @@ struct ShapeCost {
 constexpr int CUS = 256;
 template <typename T>
 ShapeCost shape_cost(int shape) {
-  constexpr ShapeCost BF16[] = {{1, {1.7}, 1.0, 7.0, 64, 5.2},               {2, {0.78, 0.97}, 1.15, 4.0, 32, 5.0},
+  constexpr ShapeCost BF16[] = {{1, {1.55}, 1.0, 7.0, 64, 5.2},              {2, {0.78, 0.97}, 1.15, 4.0, 32, 5.0},
                                 {3, {0.28, 0.46, 0.68}, 1.2, 2.7, 16, 5.2}, {2, {0.25, 0.39}, 1.15, 3.5, 24, 5.7},
                                 {3, {0.24, 0.3, 0.4}, 1.1, 2.5, 24, 5.8},   {2, {0.39, 0.76}, 1.2, 4.0, 24, 5.5},
-                                {1, {1.3}, 1.1, 6.0, 56, 5.2}};
+                                {1, {1.22}, 1.1, 6.0, 56, 5.2}};
   constexpr ShapeCost F32[] = {{}, {}, {3, {0.56, 1.05, 1.45}, 1.1, 2.5, 16, 5.2}, {2, {0.47, 1.03}, 1.2, 3.0, 24, 4.5},
                                {3, {0.46, 1.0, 1.1}, 1.0, 3.3, 24, 5.9}};
   return sizeof(T) == 4 ? F32[shape] : BF16[shape];
