@@ -6,10 +6,10 @@
 // the same wave), one for the second product.  Backward: one for dh and what follows from it element by element (dg, du and, for
 // dWd, h again), one for dx (one contraction over dg and du in turn), one for dWg and dWu together, one for dWd.
 //
-// What bounds it: many rows, the matrix units under the clock that their power leaves (bf16: 14903 rows, 4096 to 12288 and back, 3.85 ms,
-// 1.17 PFLOP/s; gradients of 8191 rows 4.2 ms, 1.18; fp32: gradients of 1801 rows, 1152 to 4008, 0.85 ms, 0.118 PFLOP/s, 85 % of the matrix
+// What bounds it: many rows, the matrix units under the clock that their power leaves (bf16: 14903 rows, 4096 to 12288 and back, 3.9 ms,
+// 1.15 PFLOP/s; gradients of 8191 rows 4.15 ms, 1.19; fp32: gradients of 1801 rows, 1152 to 4008, 0.85 ms, 0.118 PFLOP/s, 85 % of the matrix
 // units' time in the largest product); few rows, the weights' bytes (a row 57 us, 5.3 TB/s); in between, a product in one round of
-// workgroups (512 rows 182 us); small calls, three launches one after another (333 rows, 256 to 1000, fp32, 21 us).
+// workgroups (512 rows 175 us); small calls, three launches one after another (333 rows, 256 to 1000, fp32, 21 us).
 #include "hpd_ffn.h"
 #include "hpd_product.h"
 

@@ -10,7 +10,7 @@
 // are at most about 256 MB, what the memory side caches hold, so that both products read them from there.
 //
 // What bounds it: the matrix units under the clock that their power leaves (bf16: 6144 rows of 130013 tokens, 4096 channels, 5.45 ms, 1.20
-// PFLOP/s; gradients of 4096 rows of 32000 tokens 2.75 ms, 1.17; fp32: gradients of 700 rows of 50021 tokens and 1152 channels 1.26 ms, 0.128
+// PFLOP/s; gradients of 4096 rows of 32000 tokens 2.75 ms, 1.17, of 2021 of 130013 5.75, 1.12; fp32: gradients of 700 rows of 50021 tokens and 1152 channels 1.26 ms, 0.128
 // PFLOP/s); few rows, the weights' bytes (three rows of 150001 tokens 190 us, 6.4 TB/s).
 #include <algorithm>
 

@@ -244,7 +244,7 @@ struct Shape {
   // Two stages on their way are less than the latency of memory takes: each wave touches lines of A two stages further on.  In bf16, features x rows x
   // contracted, of equal values (under the least power): 24576 x 512 x 4096 99 -> 87 us, 16544 x 3520 x 5120 513 -> 437, 5120 x 2274 x 12256
   // 276 -> 225, 8192 x 8192 x 8192 716 -> 692.  (One stage further on: the same where rows are of whole lines, else less; three, B's
-  // lines too, or 128 x 128 tiles: slower.)
+  // lines too, or 128 x 128 and 64-wide tiles: slower.)
   static constexpr int TOUCH = STAGES == 2 && WGS == 1;
   // Sums of a block, each over a part of a stage's steps, added up at the end.  A sum is rounded with every product: two halve the
   // error of a long contraction, four quarter it (fp32 gradients of the block for 1801 rows: off by 5e-7 in place of 1e-6; the
@@ -255,8 +255,8 @@ struct Shape {
 // elements, A by columns and B by rows, with zeros behind B's last up to a multiple of 16 bytes
 enum { PLAIN = 0, DUAL = 1, SEGMENTS = 2, TAIL = 3 };
 // bf16 products of 4096 elements: Large 1.2 PFLOP/s for 4096 x 4096 and more; Middle 1.06 from 4096 x 2048 (Large 0.72); Small 0.61 for
-// 2048 x 1024 (Middle 0.39).  Wide where its tiles go into fewer or fuller rounds: 256 of them for 24576 features x 512 rows in 107 us,
-// 192 of Large in 125.  Few rows, where the weights' bytes are what it takes: Few32 5.9 TB/s for 24576 features and a row, 6.4 for
+// 2048 x 1024 (Middle 0.39).  Wide where its tiles go into fewer or fuller rounds: 256 of them for 24576 features x 512 rows in 101 us,
+// 192 of Large in 114.  Few rows, where the weights' bytes are what it takes: Few32 5.9 TB/s for 24576 features and a row, 6.4 for
 // 48000 (without the hint that the weights will not be read again 5.3 and 5.8; Small 4.9 and 5.5), Few64 4.5 for 64 rows (Small 4.2), Few128
 // 15544 features x 126 rows of 4096 in 36 us (Small 45, Middle 67; 64 x 192 tiles were never the best).  fp32: Small 0.13 to 0.14 PFLOP/s
 // from 2048 x 1024 on (128 x 128 with eight waves: 0.146 at most, 0.07 for 2048 x 1024), and Few.
