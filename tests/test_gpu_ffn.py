@@ -147,6 +147,13 @@ def test_tiles_of_every_size(dtype, rows, width, inner):
         R.check(a, w, name)
 
 
+# 64 x 128 tiles in each product, 192 x 256 with odd ends, a middle number of rows
+@pytest.mark.parametrize("dtype, rows, width, inner", [("bf16", 100, 4096, 6008), ("bf16", 120, 2048, 8200), ("bf16", 65, 4104, 4104),
+                                                       ("bf16", 1001, 2048, 8200), ("bf16", 509, 4096, 12296)])
+def test_tiles_between(dtype, rows, width, inner):
+    test_tiles_of_every_size(dtype, rows, width, inner)
+
+
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("rows", [3, 130])
 def test_halves_of_one_matrix(rows, dtype):

@@ -85,6 +85,13 @@ def test_tiles_of_every_size(dtype, rows, width, vocab):
     _check(_inputs(rows, width, vocab, dtype, seed=9), dtype)
 
 
+# 192 x 256 tiles of logits, 64 x 128 of gradients
+@pytest.mark.parametrize("dtype, rows, width, vocab", [("bf16", 500, 1032, 24011), ("bf16", 100, 1032, 30001), ("bf16", 100, 2048, 20011),
+                                                       ("bf16", 1000, 1032, 12001), ("bf16", 125, 4096, 9001)])
+def test_tiles_between(dtype, rows, width, vocab):
+    _check(_inputs(rows, width, vocab, dtype, seed=12), dtype)
+
+
 def _cut(dtype, rows, width, vocab):
     """Whether the forward call's workspace holds parts of the logits."""
     return B.hpd_head_logprobs_workspace(DT[dtype], rows, width, vocab)[0] >= 2 * 4 * rows * vocab
