@@ -105,6 +105,20 @@ def test_contractions_in_parts(rows, width, vocab, ge, dtype):
     _check(_inputs(rows, width, vocab, dtype, seed=10), dtype, ge)
 
 
+def test_contractions_in_parts_not_all_wanted():
+    rows, width, vocab = 70, 8192, 515
+    assert _cut("bf16", rows, width, vocab)
+    i = _inputs(rows, width, vocab, "bf16", seed=13)
+    _, lse, entropy = _forward(i, "bf16")
+    ws, one, two = B.alloc_head_workspace(B.HPD_BF16, rows, width, vocab, False), *torch.zeros((2, rows), device="cuda")
+    B.hpd_head_logprobs(B.HPD_BF16, rows, width, vocab, i["x"], 0, i["w"], 0, None, None, one, None, ws)
+    B.hpd_head_logprobs(B.HPD_BF16, rows, width, vocab, i["x"], 0, i["w"], 0, None, None, None, two, ws)
+    assert torch.equal(one, lse) and torch.equal(two, entropy)
+    dx, dw = _backward(i, "bf16", lse, entropy)
+    assert torch.equal(_backward(i, "bf16", lse, entropy, weight=False)[0], dx)
+    assert torch.equal(_backward(i, "bf16", lse, entropy, hidden=False)[1], dw)
+
+
 @pytest.mark.parametrize("hidden, weight, g, ge", [(1, 0, 1, 1), (0, 1, 1, 1), (1, 1, 0, 1), (1, 1, 1, 0), (1, 1, 0, 0)])
 def test_parts_that_are_not_wanted(hidden, weight, g, ge):
     i = _inputs(70, 136, 500, "bf16", seed=2)
