@@ -534,7 +534,8 @@ int hpd_token_logprobs_backward(int32_t dtype, int64_t n_rows, int32_t vocab, in
  * in a row stays there.  The weights' gradients are sums over all rows, and such a row reaches them even where its own gradient is 0.
  * An infinite weight times a gradient of 0 is NaN, as in any product: gradients are for finite weights.
  * The calls only enqueue kernels, on a stream of the current device, allocate nothing and may be captured in a HIP graph.  Workspaces: device memory, the bytes
- * that the _workspace call reports (NULL if 0), 16-byte aligned, not shared by calls that overlap.
+ * that the _workspace call reports (NULL if 0), 16-byte aligned, not shared by calls that overlap.  What is reported for a number of rows is enough for
+ * any smaller one of the same call, sizes and type, and never less than is reported for that.
  */
 enum hpd_activation {
   HPD_ACT_SILU = 0,     /* x / (1 + exp(-x)) */

@@ -478,7 +478,7 @@ def hpd_gated_ffn_workspace(cfg: hpd_ffn_config, n_rows):
 
 
 def alloc_ffn_workspace(cfg, n_rows, backward=True, device="cuda"):
-    """The workspace of hpd_gated_ffn, or of the backward call."""
+    """The workspace of hpd_gated_ffn, or of the backward call, for up to n_rows rows."""
     n = hpd_gated_ffn_workspace(cfg, n_rows)[bool(backward)]
     return torch.empty(n, dtype=torch.uint8, device=device) if n else None
 
@@ -505,7 +505,7 @@ def hpd_head_logprobs_workspace(dtype, n_rows, width, vocab):
 
 
 def alloc_head_workspace(dtype, n_rows, width, vocab, backward=True, device="cuda"):
-    """The workspace of hpd_head_logprobs, or of the backward call."""
+    """The workspace of hpd_head_logprobs, or of the backward call, for up to n_rows rows."""
     n = hpd_head_logprobs_workspace(dtype, n_rows, width, vocab)[bool(backward)]
     return torch.empty(n, dtype=torch.uint8, device=device) if n else None
 

@@ -142,48 +142,15 @@ struct InnerGradients {
   }
 };
 
-constexpr int MOST_SPLITS = 16;  // of a contraction over the inner width
-
-int64_t round16(int64_t x) { return (x + 15) / 16 * 16; }
-
 template <typename T>
 hpd_operand operand(const void* p, int64_t stride, int64_t size, const void* second = nullptr) {
   return {{p, second ? second : p}, stride * (int64_t)sizeof(T), (int32_t)size};
 }
 
-int64_t part_bytes(Plan p, int64_t rows, int64_t features) { return p.splits > 1 ? p.splits * rows * features * 4 : 0; }
-
-// How the products are made, and where the workspace has what they leave for each other.
-template <typename T>
-struct ForwardPlan {
-  Plan in, down;
-  int64_t parts, bytes;
-  ForwardPlan(const hpd_ffn_config& c, int64_t n) {
-    in = plan_product<T, BY_ROWS, BY_ROWS>(c.inner, n, c.width, true, 1);
-    down = plan_product<T, BY_ROWS, BY_ROWS>(c.width, n, c.inner, false, MOST_SPLITS);
-    parts = round16(n * c.inner * (int64_t)sizeof(T));
-    bytes = parts + part_bytes(down, n, c.width);
-  }
-};
-template <typename T>
-struct BackwardPlan {
-  Plan inner, dx, in_weights, down_weights;
-  int64_t h, parts, bytes;
-  BackwardPlan(const hpd_ffn_config& c, int64_t n) {
-    inner = plan_product<T, BY_COLUMNS, BY_ROWS>(c.inner, n, c.width, false, 1);
-    dx = plan_product<T, BY_COLUMNS, BY_ROWS>(c.width, n, 2 * (int64_t)c.inner, false, MOST_SPLITS);
-    in_weights = plan_product<T, BY_COLUMNS, BY_COLUMNS>(c.width, 2 * (int64_t)c.inner, n, false, 1);
-    down_weights = plan_product<T, BY_COLUMNS, BY_COLUMNS>(c.inner, c.width, n, false, 1);
-    h = round16(n * 2 * c.inner * (int64_t)sizeof(T));
-    parts = h + round16(n * c.inner * (int64_t)sizeof(T));
-    bytes = parts + part_bytes(dx, n, c.width);
-  }
-};
-
 template <typename T, int ACT>
 hipError_t forward(const hpd_ffn_forward_args& a, hipStream_t s) {
   const int64_t D = a.cfg.width, F = a.cfg.inner, N = a.n_rows;
-  const ForwardPlan<T> plan(a.cfg, N);
+  const FfnForwardPlan<T> plan(a.cfg, N);
   T* const h = (T*)a.workspace;
   const hpd_product_args in = {operand<T>(a.w_gate, a.st.w_gate, F, a.w_up), operand<T>(a.x, a.st.x, N), (int32_t)D, 1, 0, 0};
   const Activate<T, ACT> act = {h, (T*)a.gate, (T*)a.up, F, N, a.st.gate, a.st.up};
@@ -196,7 +163,7 @@ hipError_t forward(const hpd_ffn_forward_args& a, hipStream_t s) {
 template <typename T, int ACT>
 hipError_t backward(const hpd_ffn_backward_args& a, hipStream_t s) {
   const int64_t D = a.cfg.width, F = a.cfg.inner, N = a.n_rows;
-  const BackwardPlan<T> plan(a.cfg, N);
+  const FfnBackwardPlan<T> plan(a.cfg, N);
   T* const d_inner = (T*)a.workspace;
   T* const h = (T*)(a.workspace + plan.h);
   hipError_t e = hipSuccess;
@@ -228,10 +195,10 @@ hipError_t backward(const hpd_ffn_backward_args& a, hipStream_t s) {
 }  // namespace
 
 int64_t hpd_ffn_forward_bytes(const hpd_ffn_config& cfg, int64_t n_rows) {
-  return cfg.dtype == HPD_F32 ? ForwardPlan<float>(cfg, n_rows).bytes : ForwardPlan<hpd::bf16_t>(cfg, n_rows).bytes;
+  return cfg.dtype == HPD_F32 ? FfnForwardPlan<float>(cfg, n_rows).bytes : FfnForwardPlan<hpd::bf16_t>(cfg, n_rows).bytes;
 }
 int64_t hpd_ffn_backward_bytes(const hpd_ffn_config& cfg, int64_t n_rows) {
-  return cfg.dtype == HPD_F32 ? BackwardPlan<float>(cfg, n_rows).bytes : BackwardPlan<hpd::bf16_t>(cfg, n_rows).bytes;
+  return cfg.dtype == HPD_F32 ? FfnBackwardPlan<float>(cfg, n_rows).bytes : FfnBackwardPlan<hpd::bf16_t>(cfg, n_rows).bytes;
 }
 
 #define BY_TYPE(call)                                                                                              \

@@ -289,51 +289,14 @@ constexpr bool IN_ORDER<RowSums> = true;
 template <>
 constexpr bool IN_ORDER<LogitGradients<float>> = true;
 
-constexpr int MOST_SPLITS = 32;                      // of a contraction over a piece of the vocabulary
-constexpr int64_t PIECE_BYTES = (int64_t)256 << 20;  // of the logits' gradients of a piece, about
-
-int64_t round16(int64_t x) { return (x + 15) / 16 * 16; }
-int64_t round4(int64_t x) { return (x + 3) / 4 * 4; }
-
 template <typename T>
 hpd_operand operand(const void* p, int64_t stride, int64_t size) {
   return {{p, p}, stride * (int64_t)sizeof(T), (int32_t)size};
 }
 
-// How the products are made, and where the workspace has what they leave for each other.
-template <typename T>
-struct ForwardPlan {
-  Plan product;
-  int64_t tiles, of_target, bytes;
-  ForwardPlan(int64_t n, int32_t width, int32_t vocab) {
-    product = plan_product<T, BY_ROWS, BY_ROWS>(vocab, n, width, false, MOST_SPLITS, 1.2 * (vocab / 1024 + 1));  // (a row's turns in its one workgroup)
-    tiles = (vocab + product.bm() - 1) / product.bm();
-    of_target = n * tiles * (int64_t)sizeof(float4);
-    bytes = product.splits > 1 ? product.splits * n * round4(vocab) * 4 : round16(of_target + n * 4);
-  }
-};
-template <typename T>
-struct BackwardPlan {
-  int64_t piece;  // tokens of the vocabulary, a multiple of a tile's
-  Plan logits, d_hidden, d_weight;
-  int64_t parts, bytes;
-  BackwardPlan(int64_t n, int32_t width, int32_t vocab) {
-    constexpr int64_t UNIT = 256;
-    const int64_t most = std::max(UNIT, PIECE_BYTES / (std::max<int64_t>(n, 1) * (int64_t)sizeof(T)) / UNIT * UNIT);
-    const int64_t pieces = (vocab + most - 1) / most;
-    piece = ((vocab + pieces - 1) / pieces + UNIT - 1) / UNIT * UNIT;
-    logits = plan_product<T, BY_ROWS, BY_ROWS>(std::min<int64_t>(piece, vocab), n, width, false, pieces == 1 ? MOST_SPLITS : 1);
-    d_hidden = plan_product<T, BY_COLUMNS, BY_ROWS>(width, n, std::min<int64_t>(piece, vocab), false, MOST_SPLITS);
-    d_weight = plan_product<T, BY_COLUMNS, BY_COLUMNS>(width, std::min<int64_t>(piece, vocab), n, false, 1);
-    parts = round16(n * piece * (int64_t)sizeof(T));
-    // (the logits' parts have been read when those of dhidden are written)
-    bytes = parts + std::max<int64_t>(d_hidden.splits * n * width, logits.splits > 1 ? logits.splits * n * round4(vocab) : 0) * 4;
-  }
-};
-
 template <typename T>
 hipError_t forward(const hpd_head_args& a, hipStream_t s) {
-  const ForwardPlan<T> plan(a.n_rows, a.width, a.vocab);
+  const HeadForwardPlan<T> plan(a.n_rows, a.width, a.vocab);
   const int32_t tiles = (int32_t)plan.tiles;
   float4* const parts = (float4*)a.workspace;
   float* const of_target = (float*)(a.workspace + plan.of_target);
@@ -357,7 +320,7 @@ hipError_t forward(const hpd_head_args& a, hipStream_t s) {
 template <typename T>
 hipError_t backward(const hpd_head_backward_args& a, hipStream_t s) {
   const int64_t N = a.n_rows, D = a.width;
-  const BackwardPlan<T> plan(N, a.width, a.vocab);
+  const HeadBackwardPlan<T> plan(N, a.width, a.vocab);
   const int64_t piece = plan.piece;
   T* const dx = (T*)a.workspace;
   float* const parts = (float*)(a.workspace + plan.parts);
@@ -397,10 +360,10 @@ hipError_t backward(const hpd_head_backward_args& a, hipStream_t s) {
 }  // namespace
 
 int64_t hpd_head_forward_bytes(int32_t dtype, int64_t n_rows, int32_t width, int32_t vocab) {
-  return dtype == HPD_F32 ? ForwardPlan<float>(n_rows, width, vocab).bytes : ForwardPlan<hpd::bf16_t>(n_rows, width, vocab).bytes;
+  return dtype == HPD_F32 ? HeadForwardPlan<float>(n_rows, width, vocab).bytes : HeadForwardPlan<hpd::bf16_t>(n_rows, width, vocab).bytes;
 }
 int64_t hpd_head_backward_bytes(int32_t dtype, int64_t n_rows, int32_t width, int32_t vocab) {
-  return dtype == HPD_F32 ? BackwardPlan<float>(n_rows, width, vocab).bytes : BackwardPlan<hpd::bf16_t>(n_rows, width, vocab).bytes;
+  return dtype == HPD_F32 ? HeadBackwardPlan<float>(n_rows, width, vocab).bytes : HeadBackwardPlan<hpd::bf16_t>(n_rows, width, vocab).bytes;
 }
 hipError_t hpd_launch_head(const hpd_head_args& a, hipStream_t s) {
   return a.dtype == HPD_F32 ? forward<float>(a, s) : forward<hpd::bf16_t>(a, s);

@@ -21,10 +21,10 @@
 #include <stdint.h>
 
 #include <algorithm>
-#include <cmath>
 #include <type_traits>
 
 #include "hpd_attn_bf16.h"
+#include "hpd_product_plan.h"
 
 struct hpd_operand {
   const void* p[2];  // second: the other half of a dual tile, or the second segment of the contraction
@@ -41,13 +41,7 @@ struct hpd_product_args {
 
 namespace {
 
-enum { BY_ROWS = 0, BY_COLUMNS = 1 };
 constexpr uint32_t RANGE = 0x80000000u, OUTSIDE = 0xc0000000u;  // bytes of a buffer, an offset that none holds
-
-template <typename T>
-constexpr int CHUNK = 16 / (int)sizeof(T);  // elements of a 16-byte chunk
-template <typename T>
-constexpr int STAGE_K = 8 * CHUNK<T>;       // of the contracted index in a stage
 
 typedef int32_t int32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t product_u4 __attribute__((ext_vector_type(4)));
@@ -267,7 +261,6 @@ using Few64 = Shape<64, 64, 2, 2, 4, 2, true>;
 using Few32 = Shape<64, 32, 2, 1, 4, 3, true>;
 using Wide = Shape<192, 256, 2, 2, 2, 1>;
 using Few128 = Shape<64, 128, 2, 2, 3, 2, true>;
-enum { LARGE = 0, MIDDLE = 1, SMALL = 2, FEW64 = 3, FEW32 = 4, FEW128 = 5, WIDE = 6 };
 
 // f(0) .. f(N - 1), the numbers as types: what is indexed with them stays in registers however long f is
 template <int N, typename F, int I = 0>
@@ -682,64 +675,6 @@ hipError_t join_parts(const float* parts, int32_t n, int64_t features, int64_t r
   const int64_t all = features / 4 * rows;
   join_parts_kernel<T><<<dim3((uint32_t)std::min<int64_t>((all + 255) / 256, 1 << 16)), dim3(256), 0, s>>>(parts, n, features, rows, out, stride);
   return hipGetLastError();
-}
-
-// Which tiles a product gets, and into how many parts its contraction is cut.
-struct Plan {
-  int shape, splits;
-  int64_t bm() const { return shape == LARGE ? 256 : shape == WIDE ? 192 : shape == MIDDLE ? 128 : 64; }
-  int64_t bn() const { return shape == FEW32 ? 32 : shape == FEW128 ? 128 : shape == WIDE ? 256 : bm(); }
-};
-// The least time by a simple account, in us: workgroups go in rounds of as many as run at a time.  Each takes `fixed` for its start and
-// end, and for a stage stage[n - 1] where n run on its CU, `uneven` times that where contracted rows do not begin at multiples of 128 bytes
-// (a row's part of a stage is then in two lines).  What is read comes at `rate` TB/s at most; each workgroup has `flight` KB of it on the
-// way, about 1 us, and a CU takes a third more than its share of the rate.  Parts are written and read, and take a launch.  (Fitted to
-// random products of 1 to 9000 rows, weights from memory, in all shapes and cuts: of 460 in bf16 and 240 in fp32 the choice takes 1.01 times
-// the best one's time in the geometric mean, 1.2 at worst.)
-struct ShapeCost {
-  int on_cu;
-  double stage[3], uneven, fixed, flight, rate;
-};
-constexpr int CUS = 256;
-template <typename T>
-ShapeCost shape_cost(int shape) {
-  constexpr ShapeCost BF16[] = {{1, {1.55}, 1.0, 7.0, 64, 5.2},              {2, {0.78, 0.97}, 1.15, 4.0, 32, 5.0},
-                                {3, {0.28, 0.46, 0.68}, 1.2, 2.7, 16, 5.2}, {2, {0.25, 0.39}, 1.15, 3.5, 24, 5.7},
-                                {3, {0.24, 0.3, 0.4}, 1.1, 2.5, 24, 5.8},   {2, {0.39, 0.76}, 1.2, 4.0, 24, 5.5},
-                                {1, {1.22}, 1.1, 6.0, 56, 5.2}};
-  constexpr ShapeCost F32[] = {{}, {}, {3, {0.56, 1.05, 1.45}, 1.1, 2.5, 16, 5.2}, {2, {0.47, 1.03}, 1.2, 3.0, 24, 4.5},
-                               {3, {0.46, 1.0, 1.1}, 1.0, 3.3, 24, 5.9}};
-  return sizeof(T) == 4 ? F32[shape] : BF16[shape];
-}
-// k: contracted elements, of all segments; cut: us that parts cost besides being written and read
-template <typename T, int FA, int FB>
-Plan plan_product(int64_t features, int64_t rows, int64_t k, bool dual, int most_splits, double cut = 0.0) {
-  const int64_t stages = (k + STAGE_K<T> - 1) / STAGE_K<T>;
-  const double bytes = (double)((dual ? 2 : 1) * features + rows) * k * sizeof(T);
-  Plan best = {SMALL, 1};
-  double least = 1e30;
-  for (int shape = sizeof(T) == 4 ? SMALL : LARGE; shape <= (sizeof(T) == 4 ? FEW32 : WIDE); ++shape) {
-    Plan p = {shape, 1};
-    if (shape == WIDE ? FA != BY_ROWS : shape >= FEW64 && (FB != BY_ROWS || rows > p.bn())) continue;
-    const ShapeCost c = shape_cost<T>(shape);
-    const double uneven = FA == BY_ROWS && FB == BY_ROWS && k * sizeof(T) % 128 ? c.uneven : 1.0;
-    const int64_t bm = dual ? p.bm() / 2 : p.bm(), places = c.on_cu * CUS;
-    const int64_t tiles = ((features + bm - 1) / bm) * ((rows + p.bn() - 1) / p.bn());
-    for (p.splits = 1; p.splits <= most_splits && (p.splits == 1 || stages / p.splits >= 4); ++p.splits) {
-      const int64_t all = tiles * p.splits, full = all / places, rest = all % places, deep = (stages + p.splits - 1) / p.splits;
-      double t = (double)full * (deep * c.stage[c.on_cu - 1] * uneven + c.fixed);
-      if (rest) t += deep * c.stage[(rest - 1) / CUS] * uneven + c.fixed;
-      const double at_once = (double)std::min(all, places), on_cu = std::ceil(at_once / CUS);
-      const double cu = full ? 0.0 : on_cu * bytes / all / (std::min(on_cu * c.flight, 1.32 * c.rate * 1e3 / CUS) * 1e3);
-      t = std::max(t, std::max(cu, bytes / std::min(c.rate * 1e6, at_once * c.flight * 1e3)) + c.fixed);
-      if (p.splits > 1) t += cut + 2.6 + 0.12 * p.splits + (double)features * rows * p.splits * 8 / 6.0e6;
-      if (t < least) {
-        least = t;
-        best = p;
-      }
-    }
-  }
-  return best;
 }
 
 template <typename T, int FA, int FB, int MODE, typename S, typename Epilogue>
