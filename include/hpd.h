@@ -589,8 +589,8 @@ int hpd_head_logprobs(int32_t dtype, int64_t n_rows, int32_t width, int32_t voca
 /* hpd_head_logprobs_backward - gradients of hidden and weight for given gradients of log probability and entropy: with
  *   d_c = g_logprob ([c = target] - p_c) - g_entropy p_c (log p_c + entropy),  p = exp(x - lse),
  * d_hidden = d weight, d_weight = d^T hidden.  The logits are computed again, in pieces of the vocabulary.
- *   lse, entropy (needed with g_entropy only) : as the forward call has left them (where a token has nearly all of the probability,
- *             1 - p is as far off as an lse from another product's logits is from these)
+ *   lse, entropy (needed with g_entropy only) : as the forward call has left them for as many rows (its logits are these, to the bit; where
+ *             a token has nearly all of the probability, 1 - p is as far off as an lse from another product's logits is from these)
  *   g_logprob, g_entropy : device fp32 [n_rows] or NULL (0); rows without a target inside [0, vocab) take 0 as g_logprob
  *   d_hidden, d_weight : each may be NULL (not made); written, not added to; without rows d_weight is zeros
  */

@@ -280,10 +280,10 @@ struct LogitGradients {
   }
 };
 
-// The gradients' logits go with an lse that was made before, perhaps from logits that a plain product left; where a token has nearly all of the
-// probability, 1 - p is as far off as the two are apart.  In fp32, both calls sum in the order of k, as such products do: with a plain
-// product's lse the gradients of 700 rows of 50021 tokens are off by 1.4e-6 of their norm, with the forward call's 1.1e-6 (in four sums each:
-// 2.5e-6 to 4.1e-6, and 7e-7).  For few rows plain products have other orders, and four sums are nearer with both.
+// Both calls make a logit by the same sums (HeadLogitsPlan).  Those of 64 x 64 tiles in fp32 that are not cut are in the order of k, as a plain
+// product's are: the lse may come from one, and where a token has nearly all of the probability, 1 - p is as far off as the two orders are
+// apart.  With a plain product's lse the gradients of 700 rows of 50021 tokens are off by 1.4e-6 of their norm, with the forward call's by
+// 1.1e-6 (in four sums each: 2.5e-6 to 4.1e-6, and 7e-7).  For few rows plain products have other orders, and four sums are nearer with both.
 template <>
 constexpr bool IN_ORDER<RowSums> = true;
 template <>

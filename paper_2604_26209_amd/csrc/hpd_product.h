@@ -261,6 +261,10 @@ using Few64 = Shape<64, 64, 2, 2, 4, 2, true>;
 using Few32 = Shape<64, 32, 2, 1, 4, 3, true>;
 using Wide = Shape<192, 256, 2, 2, 2, 1>;
 using Few128 = Shape<64, 128, 2, 2, 3, 2, true>;
+static_assert(Large::SUMS == SHAPE_SUMS[LARGE] && Middle::SUMS == SHAPE_SUMS[MIDDLE] && Small::SUMS == SHAPE_SUMS[SMALL] &&
+                  Few64::SUMS == SHAPE_SUMS[FEW64] && Few32::SUMS == SHAPE_SUMS[FEW32] && Few128::SUMS == SHAPE_SUMS[FEW128] &&
+                  Wide::SUMS == SHAPE_SUMS[WIDE],
+              "what the plans go by");
 
 // f(0) .. f(N - 1), the numbers as types: what is indexed with them stays in registers however long f is
 template <int N, typename F, int I = 0>

@@ -17,6 +17,7 @@ namespace {
 
 enum { BY_ROWS = 0, BY_COLUMNS = 1 };
 enum { LARGE = 0, MIDDLE = 1, SMALL = 2, FEW64 = 3, FEW32 = 4, FEW128 = 5, WIDE = 6 };
+constexpr int SHAPE_SUMS[] = {1, 2, 4, 4, 4, 2, 1};  // that a block's contraction is added up in
 
 template <typename T>
 constexpr int CHUNK = 16 / (int)sizeof(T);  // elements of a 16-byte chunk
@@ -130,41 +131,62 @@ struct FfnBackwardPlan {
 
 // ---- vocabulary head
 constexpr int HEAD_SPLITS = 32;                 // of a contraction, at most
-constexpr int64_t LOGIT_PART_BYTES = 128 * MB;  // parts of the logits, or sums of their rows
+constexpr int64_t LOGIT_PART_BYTES = 128 * MB;  // parts of the logits, or sums of their rows (of 8000 random heads of up to 20000 rows and 160000
+                                                // tokens none wanted more)
 constexpr int64_t HIDDEN_PART_BYTES = 256 * MB; // parts of dhidden
 constexpr int64_t PIECE_BYTES = 256 * MB;       // the logits' gradients of a piece of the vocabulary, about
 
+// The logits' product.  Both calls sum a logit's products in the same order, so that the gradients' logits are those that lse was made from, to
+// the bit: 1 - p of a confident token is the difference of the two (logits of 300, a contraction of 480 to 2048: with a plan of each
+// call's own 1 - p = 1e-4 was off by its own size and more).  The order is that of the parts, and in a part of a tile's sums.  So the whole
+// vocabulary is planned once, with what parts cost the forward call; a piece of it may take another shape with as many sums.
+template <typename T>
+struct HeadLogitsPlan {
+  static constexpr int64_t UNIT = 256;
+  int64_t pieces, piece;  // of the vocabulary in the backward call; a multiple of a tile's tokens
+  int64_t of_parts, of_sums;
+  Plan whole, of_piece;
+  static int sums(Plan p) { return sizeof(T) == 4 && p.shape == SMALL && p.splits == 1 ? 1 : SHAPE_SUMS[p.shape]; }  // (fp32: IN_ORDER)
+  static int64_t sum_bytes(int64_t n, int64_t vocab, int64_t bm) { return round16(n * ((vocab + bm - 1) / bm * 16 + 4)); }
+  HeadLogitsPlan(int64_t n, int32_t width, int32_t vocab) {
+    const int64_t most = std::max(UNIT, PIECE_BYTES / (std::max<int64_t>(n, 1) * (int64_t)sizeof(T)) / UNIT * UNIT);
+    pieces = (vocab + most - 1) / most;
+    piece = ((vocab + pieces - 1) / pieces + UNIT - 1) / UNIT * UNIT;
+    of_parts = std::min(HEAD_SPLITS * n * round4(vocab) * 4, LOGIT_PART_BYTES);
+    // (the largest tiles leave the least sums: they always fit)
+    of_sums = std::max(sum_bytes(n, vocab, sizeof(T) == 4 ? 64 : 256), std::min(sum_bytes(n, vocab, 64), LOGIT_PART_BYTES));
+    whole = plan_product<T, BY_ROWS, BY_ROWS>(vocab, n, width, false, pieces == 1 ? HEAD_SPLITS : 1, 1.2 * (vocab / 1024 + 1),  // (a row's turns in its one workgroup)
+                                              [&](Plan p) { return needs(p, n, vocab) <= (p.splits > 1 ? of_parts : of_sums); });
+    of_piece = whole;
+    if (pieces > 1)
+      of_piece = plan_product<T, BY_ROWS, BY_ROWS>(piece, n, width, false, 1, 0.0, [&](Plan p) { return sums(p) == sums(whole); });
+  }
+  static int64_t needs(Plan p, int64_t n, int64_t vocab) { return p.splits > 1 ? part_bytes(p, n, round4(vocab)) : sum_bytes(n, vocab, p.bm()); }
+};
 template <typename T>
 struct HeadForwardPlan {
   Plan product;
   int64_t tiles, of_target, needs, bytes;
-  static int64_t sum_bytes(int64_t n, int64_t vocab, int64_t bm) { return round16(n * ((vocab + bm - 1) / bm * 16 + 4)); }
-  static int64_t need(Plan p, int64_t n, int64_t vocab) { return p.splits > 1 ? part_bytes(p, n, round4(vocab)) : sum_bytes(n, vocab, p.bm()); }
   HeadForwardPlan(int64_t n, int32_t width, int32_t vocab) {
-    // (the largest tiles leave the least sums: they always fit)
-    const int64_t least = sum_bytes(n, vocab, sizeof(T) == 4 ? 64 : 256);
-    bytes = std::max(least, std::min(std::max(sum_bytes(n, vocab, 64), HEAD_SPLITS * n * round4(vocab) * 4), LOGIT_PART_BYTES));
-    product = plan_product<T, BY_ROWS, BY_ROWS>(vocab, n, width, false, HEAD_SPLITS, 1.2 * (vocab / 1024 + 1),  // (a row's turns in its one workgroup)
-                                                [&](Plan p) { return need(p, n, vocab) <= bytes; });
+    const HeadLogitsPlan<T> l(n, width, vocab);
+    product = l.whole;
     tiles = (vocab + product.bm() - 1) / product.bm();
     of_target = n * tiles * 16;
-    needs = need(product, n, vocab);
+    needs = HeadLogitsPlan<T>::needs(product, n, vocab);
+    bytes = std::max(l.of_sums, l.of_parts);
   }
 };
 template <typename T>
 struct HeadBackwardPlan {
-  int64_t piece;  // tokens of the vocabulary, a multiple of a tile's
+  int64_t piece;
   Plan logits, d_hidden, d_weight;
   int64_t parts, needs, bytes;
   HeadBackwardPlan(int64_t n, int32_t width, int32_t vocab) {
-    constexpr int64_t UNIT = 256;
-    const int64_t most = std::max(UNIT, PIECE_BYTES / (std::max<int64_t>(n, 1) * (int64_t)sizeof(T)) / UNIT * UNIT);
-    const int64_t pieces = (vocab + most - 1) / most;
-    piece = ((vocab + pieces - 1) / pieces + UNIT - 1) / UNIT * UNIT;
-    const int64_t of_logits = std::min(HEAD_SPLITS * n * round4(vocab) * 4, LOGIT_PART_BYTES);
+    constexpr int64_t UNIT = HeadLogitsPlan<T>::UNIT;
+    const HeadLogitsPlan<T> l(n, width, vocab);
+    logits = l.of_piece;
+    piece = l.piece;
     const int64_t of_hidden = std::max(n * width * 4, std::min(HEAD_SPLITS * n * width * 4, HIDDEN_PART_BYTES));
-    logits = plan_product<T, BY_ROWS, BY_ROWS>(std::min<int64_t>(piece, vocab), n, width, false, pieces == 1 ? HEAD_SPLITS : 1, 0.0,
-                                               [&](Plan p) { return part_bytes(p, n, round4(vocab)) <= of_logits; });
     d_hidden = plan_product<T, BY_COLUMNS, BY_ROWS>(width, n, std::min<int64_t>(piece, vocab), false, HEAD_SPLITS, 0.0,
                                                     [&](Plan p) { return p.splits * n * width * 4 <= of_hidden; });
     d_weight = plan_product<T, BY_COLUMNS, BY_COLUMNS>(width, std::min<int64_t>(piece, vocab), n, false, 1, 0.0, [](Plan) { return true; });
@@ -172,7 +194,7 @@ struct HeadBackwardPlan {
     // (the logits' parts have been read when those of dhidden are written)
     needs = parts + std::max(d_hidden.splits * n * width * 4, part_bytes(logits, n, round4(vocab)));
     const int64_t whole = (vocab + UNIT - 1) / UNIT * UNIT;
-    bytes = round16(std::min(n * whole * (int64_t)sizeof(T), std::max(n * UNIT * (int64_t)sizeof(T), PIECE_BYTES))) + std::max(of_hidden, of_logits);
+    bytes = round16(std::min(n * whole * (int64_t)sizeof(T), std::max(n * UNIT * (int64_t)sizeof(T), PIECE_BYTES))) + std::max(of_hidden, l.of_parts);
   }
 };
 

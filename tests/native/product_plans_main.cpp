@@ -1,5 +1,5 @@
 // The plans of the feed-forward block's and the vocabulary head's products over many sizes: a workspace that is reported for a number of rows
-// holds what any smaller number needs.  Exit code 0 = no finding.
+// holds what any smaller number needs, and both of the head's calls sum logits in the same order.  Exit code 0 = no finding.
 #include <cstdint>
 #include <cstdio>
 #include <cstdlib>
@@ -49,6 +49,10 @@ static void head(int32_t width, int32_t vocab) {
     const HeadBackwardPlan<T> b(n, width, vocab);
     CHECK(f.needs <= f.bytes && b.needs <= b.bytes, "head, %lld rows, %d of %d", (long long)n, width, vocab);
     CHECK(f.bytes >= forward && b.bytes >= backward, "head, fewer bytes for %lld rows, %d of %d", (long long)n, width, vocab);
+    // the same sums in both calls
+    using L = HeadLogitsPlan<T>;
+    CHECK(f.product.splits == b.logits.splits && L::sums(f.product) == L::sums(b.logits), "logits, %lld rows, %d of %d", (long long)n, width, vocab);
+    CHECK(b.logits.splits == 1 || b.piece >= vocab, "parts of pieces, %lld rows, %d of %d", (long long)n, width, vocab);
     forward = f.bytes;
     backward = b.bytes;
   });

@@ -1,5 +1,7 @@
 """Log probabilities from hidden states and the vocabulary's weights through the library, and their gradients, against the
 definitions in 64 bits."""
+import math
+
 import pytest
 import torch
 
@@ -326,3 +328,41 @@ def test_rows_8_mb_apart(dtype, rows, width, vocab):
 
     for a, b in zip(run(x, stride, dx), run(i["x"], 0, torch.empty_like(i["x"]))):
         assert torch.equal(a, b)
+
+
+# sizes for which a plan of each call's own would sum the logits in another order
+@pytest.mark.parametrize("dtype, rows, width, vocab", [("f32", 117, 480, 2057), ("f32", 231, 1152, 2057), ("f32", 4, 480, 1100),
+                                                       ("f32", 14, 1152, 10404), ("f32", 40, 480, 2057), ("f32", 17, 2048, 23311),
+                                                       ("bf16", 6, 2048, 4037), ("bf16", 20, 2048, 6176), ("f32", 300, 1152, 50021),
+                                                       ("bf16", 700, 1152, 9001), ("bf16", 1500, 512, 100003)])
+def test_confident_tokens(rows, width, vocab, dtype):
+    """1 - p of about 1e-4 where the logits are about 300: both calls have the same logits, to the bit, so that what a sum of `width`
+    products is off by does not count; only the rounding of lse does, and the sum of the exponentials."""
+    gen = torch.Generator().manual_seed(14)
+    w = torch.randn((vocab, width), generator=gen) * 2.5 * width ** -0.5
+    w[:, 0] = 1.0
+    w = w.to(TD[dtype])
+    t = torch.randperm(vocab, generator=gen)[:rows]
+    near = w[t].float()
+    near[:, 0] = 0.0
+    x = near * (math.log(vocab) + 9) / (near * near).sum(1, keepdim=True)
+    x[:, 0] = 300.0
+    i = dict(x=x.to(TD[dtype]).cuda(), w=w.cuda(), t=t.to(torch.int32).cuda(), g=torch.ones(rows, device="cuda"), ge=None)
+    _, lse, _ = _forward(i, dtype)
+    got = _backward(i, dtype, lse, None, ge=False)
+    x, w, t = i["x"].double(), i["w"].double(), t.cuda()[:, None]
+    logits, e = R.product(x, w)
+    want_lse = torch.logsumexp(logits, 1, keepdim=True)
+    p = (logits - want_lse).exp()
+    rest = p.scatter(1, t, 0.0)  # (1 - p of the target, without a difference)
+    missing = rest.sum(1, keepdim=True)
+    d = (-rest).scatter(1, t, missing)
+    # of the target: lse's rounding by half a step; the sum's roundings (as in ffn_ref.logprobs) and those of exponential and difference;
+    # 1 - p itself by a logit's error at both ends.  Of others: p by the logit's and the lse's.
+    off = 2.0 ** -24 * want_lse.abs() + R.U * (102 + vocab / 4096)
+    e = e.amax(1, keepdim=True)
+    ed = (rest * (2 * e + off)).scatter(1, t, off + missing * (2 * e + off))
+    eps = R.half_step(TD[dtype])
+    ed = ed + eps * (d.abs() + ed)
+    for name, a, (c, ec) in zip(("d_hidden", "d_weight"), got, (R.product(d, w.T, ed), R.product(d.T, x.T, ed.T))):
+        R.check(a, (c, ec + eps * (c.abs() + ec)), name)
