@@ -22,8 +22,8 @@ __device__ __forceinline__ float fast_exp(float x) {
   const float y = x * L, e = fast_exp2(y);
   if (sizeof(T) == 2) return e;
   const float low = fmaf(x, L, -y) + x * L_LOW;
-  // (an infinite e stays one: low is not negative there or tiny)
-  return e < 3.0e38f ? fmaf(e * LN2, low, e) : e;
+  // (0 and infinity stay as they are: where y itself is infinite, low is not a number)
+  return e > 0.f && e < 3.0e38f ? fmaf(e * LN2, low, e) : e;
 }
 
 // act(g) and its derivative (1 / (1 + e) by the reciprocal instruction, good to a step; divisions, and the slope where it is not asked for,

@@ -336,3 +336,30 @@ def test_gradients_against_differences():
         numeric, analytic = (sums[1] - sums[0]) / 2e-4, (d.double() * way.double()).sum().item()
         # third derivatives of order 10 times 1e-8, and the gradient's own roundings over its elements
         assert abs(numeric - analytic) <= 1e-5 * (d.double() * way.double()).abs().sum().item() + 1e-5, name
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("act", list(ACTS))
+def test_activations_at_the_ends_of_the_range(act, dtype):
+    """Any finite g: act(g) is g or 0 and its slope 1 or 0, though squares and multiples of g overflow; act(+infinity) is +infinity."""
+    g = torch.tensor([1e12, 1e19, 2e19, 3e19, 1e25, 1e30, 1.2e38, 2e38, 2.4e38, 3e38, 3.3e38, 30.0])
+    g = torch.cat([g, -g]).to(TD[dtype])
+    n = len(g)
+    eye, none = torch.eye(n), torch.zeros((n, n))
+    i = dict(x=torch.cat([torch.diag(g.float()), eye / 16], 1), wg=torch.cat([eye, none], 1), wu=torch.cat([none, eye], 1),
+             wd=torch.cat([eye, none]), g=g[None].float(), u=torch.ones((1, n)), d_out=torch.ones((1, 2 * n)))
+    i = {k: v.to(TD[dtype]).cuda().contiguous() for k, v in i.items()}
+    out, gate, up = _forward(i, n, 2 * n, n, dtype, act)
+    assert torch.equal(gate.cpu(), torch.diag(g)) and bool((up.diagonal() == 1 / 16).all())
+    want = torch.where(g > 0, g, 0.0).double() / 16
+    got = out.double().cpu().diagonal()
+    assert bool(((got - want).abs() <= R.FUNC * want + 1e-11).all()), (got, want)
+    j = dict(i, wu=torch.zeros_like(i["wu"]))
+    dx = _backward(j, 1, 2 * n, n, dtype, act, (1, 0, 0, 0))[0].double().cpu()[0, :n]
+    assert bool(((dx - (g > 0).double()).abs() <= R.FUNC + R.half_step(TD[dtype])).all()), dx
+    # a sum that overflows in the gate
+    i = {k: torch.zeros((8, 8)) for k in ("x", "wg", "wu", "wd")}
+    i["x"][0, 0], i["wg"][0, 0], i["wu"][0, 0] = 3e38, 2.0, 2.0 ** -126
+    i["wd"] += 1.0
+    out, gate, _ = _forward({k: v.to(TD[dtype]).cuda() for k, v in i.items()}, 8, 8, 8, dtype, act)
+    assert float(gate[0, 0]) == float("inf") and bool((out[0] == float("inf")).all()) and bool((out[1:] == 0).all())
