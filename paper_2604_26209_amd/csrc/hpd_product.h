@@ -28,7 +28,7 @@
 
 struct hpd_operand {
   const void* p[2];  // second: the other half of a dual tile, or the second segment of the contraction
-  int64_t stride;    // bytes from one row (by rows: of m or n; by columns: of k) to the next
+  int64_t stride;    // bytes from one row (by rows: of m or n; by columns: of k) to the next, at most 2^23
   int32_t size;      // m or n of the whole operand
 };
 
@@ -129,7 +129,7 @@ struct Tile {
   static __device__ __forceinline__ int chunk_of(int f, int lane) { return (lane & 7) ^ ((4 * f + (lane >> 4)) & 7); }
   static __device__ __forceinline__ int k_of(int f, int lane) { return (f * 1024 + lane * 16) / RB; }
 
-  // size: rows (columns) from the tile's first on
+  // size: rows (columns) from the tile's first on.  (A stride is at most 2^23 bytes, a stage has at most 64 k and a tile 256 rows: 31 bits)
   __device__ __forceinline__ void init(int64_t stride, int64_t size, int wave, int lane) {
 #pragma unroll
     for (int i = 0; i < LOADS; ++i) {

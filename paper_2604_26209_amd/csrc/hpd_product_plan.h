@@ -134,7 +134,10 @@ constexpr int HEAD_SPLITS = 32;                 // of a contraction, at most
 constexpr int64_t LOGIT_PART_BYTES = 128 * MB;  // parts of the logits, or sums of their rows (of 8000 random heads of up to 20000 rows and 160000
                                                 // tokens none wanted more)
 constexpr int64_t HIDDEN_PART_BYTES = 256 * MB; // parts of dhidden
-constexpr int64_t PIECE_BYTES = 256 * MB;       // the logits' gradients of a piece of the vocabulary, about
+// The logits' gradients of a piece of the vocabulary: what the memory side caches hold (more from 524288 bf16 or 262144 fp32 rows on: a
+// piece has 256 tokens at least).  Their rows are an operand of the products behind, with a stride as any: a stage's 64 rows of bf16, those
+// behind the last among them, begin within 32 bits of the first.
+constexpr int64_t PIECE_BYTES = 256 * MB, PIECE_ROW_BYTES = 8 * MB;
 
 // The logits' product.  Both calls sum a logit's products in the same order, so that the gradients' logits are those that lse was made from, to
 // the bit: 1 - p of a confident token is the difference of the two (logits of 300, a contraction of 480 to 2048: with a plan of each
@@ -149,7 +152,8 @@ struct HeadLogitsPlan {
   static int sums(Plan p) { return sizeof(T) == 4 && p.shape == SMALL && p.splits == 1 ? 1 : SHAPE_SUMS[p.shape]; }  // (fp32: IN_ORDER)
   static int64_t sum_bytes(int64_t n, int64_t vocab, int64_t bm) { return round16(n * ((vocab + bm - 1) / bm * 16 + 4)); }
   HeadLogitsPlan(int64_t n, int32_t width, int32_t vocab) {
-    const int64_t most = std::max(UNIT, PIECE_BYTES / (std::max<int64_t>(n, 1) * (int64_t)sizeof(T)) / UNIT * UNIT);
+    const int64_t row_bytes = std::min(PIECE_ROW_BYTES, PIECE_BYTES / std::max<int64_t>(n, 1));
+    const int64_t most = std::max(UNIT, row_bytes / (int64_t)sizeof(T) / UNIT * UNIT);
     pieces = (vocab + most - 1) / most;
     piece = ((vocab + pieces - 1) / pieces + UNIT - 1) / UNIT * UNIT;
     of_parts = std::min(HEAD_SPLITS * n * round4(vocab) * 4, LOGIT_PART_BYTES);
@@ -194,7 +198,8 @@ struct HeadBackwardPlan {
     // (the logits' parts have been read when those of dhidden are written)
     needs = parts + std::max(d_hidden.splits * n * width * 4, part_bytes(logits, n, round4(vocab)));
     const int64_t whole = (vocab + UNIT - 1) / UNIT * UNIT;
-    bytes = round16(std::min(n * whole * (int64_t)sizeof(T), std::max(n * UNIT * (int64_t)sizeof(T), PIECE_BYTES))) + std::max(of_hidden, l.of_parts);
+    bytes = round16(std::min(n * std::min(whole * (int64_t)sizeof(T), PIECE_ROW_BYTES), std::max(n * UNIT * (int64_t)sizeof(T), PIECE_BYTES))) +
+            std::max(of_hidden, l.of_parts);
   }
 };
 

@@ -1,5 +1,6 @@
 // The plans of the feed-forward block's and the vocabulary head's products over many sizes: a workspace that is reported for a number of rows
-// holds what any smaller number needs, and both of the head's calls sum logits in the same order.  Exit code 0 = no finding.
+// holds what any smaller number needs, both of the head's calls sum logits in the same order, and a row of a
+// piece's gradients is no longer than a stride may be.  Exit code 0 = no finding.
 #include <cstdint>
 #include <cstdio>
 #include <cstdlib>
@@ -52,6 +53,7 @@ static void head(int32_t width, int32_t vocab) {
     // the same sums in both calls
     using L = HeadLogitsPlan<T>;
     CHECK(f.product.splits == b.logits.splits && L::sums(f.product) == L::sums(b.logits), "logits, %lld rows, %d of %d", (long long)n, width, vocab);
+    CHECK(b.piece % 256 == 0 && b.piece * (int64_t)sizeof(T) <= 1 << 23, "a piece's rows, %lld rows, %d of %d", (long long)n, width, vocab);
     CHECK(b.logits.splits == 1 || b.piece >= vocab, "parts of pieces, %lld rows, %d of %d", (long long)n, width, vocab);
     forward = f.bytes;
     backward = b.bytes;
@@ -70,6 +72,10 @@ int main() {
   ffn<uint16_t>(4096, 12288);
   head<uint16_t>(4096, 2057);
   head<float>(1152, 50021);
+  for (const int vocab : {(1 << 21) + 1, (1 << 22) + 777, 1 << 25, 1 << 28}) {
+    head<uint16_t>(8, vocab);
+    head<float>(8, vocab);
+  }
   // (what the GPU tests of contractions in parts go by)
   const int32_t cut[][3] = {{1, 8192, 1},     {5, 8192, 67},   {69, 8192, 1119}, {130, 5120, 385}, {33, 4104, 4}, {2, 16384, 2050},
                             {70, 8192, 515}, {5, 8192, 300}, {640, 4096, 2057}};

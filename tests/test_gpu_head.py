@@ -366,3 +366,12 @@ def test_confident_tokens(rows, width, vocab, dtype):
     ed = ed + eps * (d.abs() + ed)
     for name, a, (c, ec) in zip(("d_hidden", "d_weight"), got, (R.product(d, w.T, ed), R.product(d.T, x.T, ed.T))):
         R.check(a, (c, ec + eps * (c.abs() + ec)), name)
+
+
+@pytest.mark.parametrize("dtype, rows, width, vocab", [("bf16", 3, 8, (1 << 22) + 777), ("f32", 2, 16, (1 << 21) + 5)])
+def test_vocabularies_of_millions(dtype, rows, width, vocab):
+    """More tokens than a row of a piece's gradients has room for; targets on both sides of the pieces' borders."""
+    i = _inputs(rows, width, vocab, dtype, seed=15)
+    piece = ((vocab + 1) // 2 + 255) // 256 * 256
+    i["t"] = torch.tensor([piece, piece - 1, vocab - 1][:rows], dtype=torch.int32, device="cuda")
+    _check(i, dtype)
