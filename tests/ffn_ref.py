@@ -136,3 +136,81 @@ def check(got, want, what):
         i = tuple(int(k) for k in torch.nonzero(bad)[0])
         raise AssertionError(f"{what}: {int(bad.sum())} of {bad.numel()} are off, first {i}: {got[i].item()} for "
                              f"{value[i].item()}, allowed {bound[i].item()}")
+
+
+# ---------------------------------------------------------------------------
+# Bounds by likelihood: a long contraction's worst case would let a lost element through.  Roundings are taken as independent of each
+# other and of the signs of what they are multiplied with.  A value's rounding, at most half a step, has a standard deviation of
+# half a step / sqrt 3; a sum of K products rounds K times (an addition each, a product goes in unrounded or with a rounding that is
+# small next to the sum's), each time at most 2^-24 of a partial sum, which on its way is of the size of the end result c
+# or of sqrt(sum a^2 b^2), what a sum of random signs has.  Errors of fp32 functions, FUNC, have the signs of what they are
+# multiplied with.  A result may be LIKELY deviations off (7: 3e-12 of normal values are, of 4e7 in a test) and its own last rounding.
+# ---------------------------------------------------------------------------
+LIKELY = 7.0
+
+
+def likely_product(a, b, deviation_a=None):
+    """a b^T and the standard deviation of its error, for that of a's elements."""
+    c = a @ b.T
+    squares = b.T ** 2
+    variance = a.shape[1] * 2.0 ** -48 * ((a ** 2) @ squares + c ** 2)
+    if deviation_a is not None:
+        variance = variance + (deviation_a ** 2) @ squares
+    return c, variance.sqrt()
+
+
+def _likely(v, deviation, eps):
+    e = LIKELY * deviation
+    return v, e + eps * (v.abs() + e)
+
+
+def _norm(*terms):
+    return sum(t ** 2 for t in terms).sqrt()
+
+
+def likely_ffn(x, wg, wu, wd, name, dtype):
+    """(value, bound) of out, gate and up."""
+    eps = half_step(dtype)
+    g, sg = likely_product(x, wg)
+    u, su = likely_product(x, wu)
+    a, _ = act(g, name)
+    h = a * u
+    sh = _norm(SLOPE * sg * u, a * su, FUNC * g * u, eps / math.sqrt(3) * h)
+    return [_likely(v, s, eps) for v, s in (likely_product(h, wd, sh), (g, sg), (u, su))]
+
+
+def likely_ffn_grad(x, wg, wu, wd, g, u, d_out, name, dtype):
+    """(value, bound) of dx, dwg, dwu, dwd for the given g and u."""
+    eps = half_step(dtype)
+    step = eps / math.sqrt(3)
+    a, slope = act(g, name)
+    dh, sdh = likely_product(d_out, wd.T)
+    h, dg, du = a * u, dh * u * slope, dh * a
+    sh = _norm(FUNC * g * u, step * h)
+    sdg = _norm(sdh * u * SLOPE, FUNC * dh * u * (1 + g.abs()), step * dg)
+    sdu = _norm(sdh * a, FUNC * dh * g, step * du)
+    dx = likely_product(torch.cat([dg, du], 1), torch.cat([wg, wu], 0).T, torch.cat([sdg, sdu], 1))
+    dwg, dwu = likely_product(dg.T, x.T, sdg.T), likely_product(du.T, x.T, sdu.T)
+    dwd = likely_product(h.T, d_out.T, sh.T)
+    return [_likely(v, s, eps) for v, s in (dx, dwg, dwu, (dwd[0].T, dwd[1].T))]
+
+
+def likely_head(x, w, targets):
+    """(value, bound) of logprob, lse and entropy."""
+    logits, s = likely_product(x, w)
+    return logprobs(logits, targets, LIKELY * s)
+
+
+def likely_head_grad(x, w, targets, g_logprob, dtype):
+    """(value, bound) of d_hidden and d_weight, no entropy: with an lse that the same kernels made."""
+    eps = half_step(dtype)
+    logits, s = likely_product(x, w)
+    lse = torch.logsumexp(logits, 1, keepdim=True)
+    p = (logits - lse).exp()
+    at = targets.long()[:, None]
+    hot = torch.zeros_like(p).scatter_(1, at, 1.0)
+    d = g_logprob[:, None] * (hot - p)
+    # p by its logit's error and by the lse's: the mean of the logits' by their p, its sum's and its own rounding; the product is rounded
+    e_lse = (p * s).sum(1, keepdim=True) + U * (100 + w.shape[0] / 4096) + U * lse.abs()
+    sd = _norm(g_logprob[:, None] * p * (s + e_lse + U * (2 + (logits - lse).abs())), eps / math.sqrt(3) * d, U * g_logprob[:, None] * hot)
+    return [_likely(v, e, eps) for v, e in (likely_product(d, w.T, sd), likely_product(d.T, x.T, sd.T))]
