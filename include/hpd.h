@@ -566,8 +566,8 @@ int hpd_gated_ffn(const hpd_ffn_config* cfg, int64_t n_rows, const void* x, cons
                   void* stream);
 
 /* hpd_gated_ffn_backward - gradients of x and of the weights, from d_out and from what the forward call has left in gate
- * and up.  Each of d_x, d_w_gate, d_w_up, d_w_down may be NULL: that gradient is not made (frozen weights).  They are written, not
- * added to; without rows those of the weights are zeros. */
+ * and up.  Each of d_x, d_w_gate, d_w_up, d_w_down may be NULL: that gradient is not made (frozen weights; the inputs are given all the
+ * same).  They are written, not added to; without rows those of the weights are zeros. */
 int hpd_gated_ffn_backward(const hpd_ffn_config* cfg, int64_t n_rows, const void* x, const void* w_gate, const void* w_up,
                            const void* w_down, const void* gate, const void* up, const void* d_out, void* d_x, void* d_w_gate,
                            void* d_w_up, void* d_w_down, void* workspace, const hpd_ffn_strides* strides, void* stream);
