@@ -24,6 +24,14 @@ constexpr int CHUNK = 16 / (int)sizeof(T);  // elements of a 16-byte chunk
 template <typename T>
 constexpr int STAGE_K = 8 * CHUNK<T>;       // of the contracted index in a stage
 
+constexpr int LEAST_STAGES = 4;  // of a part
+// how many parts a contraction of k elements can have, of `most`; 0: it is never cut
+template <typename T>
+int64_t most_parts(int64_t k, int64_t most) {
+  const int64_t parts = std::min(most, (k + STAGE_K<T> - 1) / STAGE_K<T> / LEAST_STAGES);
+  return parts > 1 ? parts : 0;
+}
+
 struct Plan {
   int shape, splits;
   int64_t bm() const { return shape == LARGE ? 256 : shape == WIDE ? 192 : shape == MIDDLE ? 128 : 64; }
@@ -64,7 +72,7 @@ Plan plan_product(int64_t features, int64_t rows, int64_t k, bool dual, int most
     const double uneven = FA == BY_ROWS && FB == BY_ROWS && k * sizeof(T) % 128 ? c.uneven : 1.0;
     const int64_t bm = dual ? p.bm() / 2 : p.bm(), places = c.on_cu * CUS;
     const int64_t tiles = ((features + bm - 1) / bm) * ((rows + p.bn() - 1) / p.bn());
-    for (p.splits = 1; p.splits <= most_splits && (p.splits == 1 || stages / p.splits >= 4); ++p.splits) {
+    for (p.splits = 1; p.splits <= most_splits && (p.splits == 1 || stages / p.splits >= LEAST_STAGES); ++p.splits) {
       if (!fits(p)) continue;
       const int64_t all = tiles * p.splits, full = all / places, rest = all % places, deep = (stages + p.splits - 1) / p.splits;
       double t = (double)full * (deep * c.stage[c.on_cu - 1] * uneven + c.fixed);
@@ -94,14 +102,15 @@ constexpr int FFN_SPLITS = 16;  // of a contraction over the inner width, at mos
 // Parts take up to 512 MB: random blocks of up to 20000 rows and 8192 channels then have the account's best choice but for 1 %
 // of them, which take up to 1.10 times its time (256 MB: 3 %, 1.25).
 constexpr int64_t FFN_PART_BYTES = 512 * MB;
-inline int64_t ffn_part_allowance(int64_t n, int64_t width) { return std::min(FFN_SPLITS * n * width * 4, FFN_PART_BYTES); }
+template <typename T>
+int64_t ffn_part_allowance(int64_t n, int64_t width, int64_t k) { return std::min(most_parts<T>(k, FFN_SPLITS) * n * width * 4, FFN_PART_BYTES); }
 
 template <typename T>
 struct FfnForwardPlan {
   Plan in, down;
   int64_t parts, needs, bytes;
   FfnForwardPlan(const hpd_ffn_config& c, int64_t n) {
-    const int64_t allowance = ffn_part_allowance(n, c.width);
+    const int64_t allowance = ffn_part_allowance<T>(n, c.width, c.inner);
     in = plan_product<T, BY_ROWS, BY_ROWS>(c.inner, n, c.width, true, 1, 0.0, [](Plan) { return true; });
     down = plan_product<T, BY_ROWS, BY_ROWS>(c.width, n, c.inner, false, FFN_SPLITS, 0.0,
                                              [&](Plan p) { return part_bytes(p, n, c.width) <= allowance; });
@@ -115,7 +124,7 @@ struct FfnBackwardPlan {
   Plan inner, dx, in_weights, down_weights;
   int64_t h, parts, needs, bytes;
   FfnBackwardPlan(const hpd_ffn_config& c, int64_t n) {
-    const int64_t allowance = ffn_part_allowance(n, c.width);
+    const int64_t allowance = ffn_part_allowance<T>(n, c.width, 2 * (int64_t)c.inner);
     auto any = [](Plan) { return true; };
     inner = plan_product<T, BY_COLUMNS, BY_ROWS>(c.inner, n, c.width, false, 1, 0.0, any);
     dx = plan_product<T, BY_COLUMNS, BY_ROWS>(c.width, n, 2 * (int64_t)c.inner, false, FFN_SPLITS, 0.0,
@@ -156,7 +165,7 @@ struct HeadLogitsPlan {
     const int64_t most = std::max(UNIT, row_bytes / (int64_t)sizeof(T) / UNIT * UNIT);
     pieces = (vocab + most - 1) / most;
     piece = ((vocab + pieces - 1) / pieces + UNIT - 1) / UNIT * UNIT;
-    of_parts = std::min(HEAD_SPLITS * n * round4(vocab) * 4, LOGIT_PART_BYTES);
+    of_parts = std::min(most_parts<T>(width, HEAD_SPLITS) * n * round4(vocab) * 4, LOGIT_PART_BYTES);
     // (the largest tiles leave the least sums: they always fit)
     of_sums = std::max(sum_bytes(n, vocab, sizeof(T) == 4 ? 64 : 256), std::min(sum_bytes(n, vocab, 64), LOGIT_PART_BYTES));
     whole = plan_product<T, BY_ROWS, BY_ROWS>(vocab, n, width, false, pieces == 1 ? HEAD_SPLITS : 1, 1.2 * (vocab / 1024 + 1),  // (a row's turns in its one workgroup)
@@ -190,7 +199,7 @@ struct HeadBackwardPlan {
     const HeadLogitsPlan<T> l(n, width, vocab);
     logits = l.of_piece;
     piece = l.piece;
-    const int64_t of_hidden = std::max(n * width * 4, std::min(HEAD_SPLITS * n * width * 4, HIDDEN_PART_BYTES));
+    const int64_t of_hidden = std::max(n * width * 4, std::min(most_parts<T>(vocab, HEAD_SPLITS) * n * width * 4, HIDDEN_PART_BYTES));
     d_hidden = plan_product<T, BY_COLUMNS, BY_ROWS>(width, n, std::min<int64_t>(piece, vocab), false, HEAD_SPLITS, 0.0,
                                                     [&](Plan p) { return p.splits * n * width * 4 <= of_hidden; });
     d_weight = plan_product<T, BY_COLUMNS, BY_COLUMNS>(width, std::min<int64_t>(piece, vocab), n, false, 1, 0.0, [](Plan) { return true; });

@@ -31,3 +31,18 @@ def test_a_workspace_is_enough_for_fewer_rows(width, other, dtype):
         now = B.hpd_gated_ffn_workspace(cfg, n) + B.hpd_head_logprobs_workspace(dtype, n, width, other)
         assert all(a >= b for a, b in zip(now, last)), n
         last = now
+
+
+def test_workspaces_of_short_contractions():
+    """A part has four stages of 64 elements (fp32: 32) at least: fewer than eight stages leave nothing but what the products have for each
+    other, eight (504 and 2 x 248 elements of bf16, 248 of fp32) two parts of the result."""
+    rows, width = 5000, 4096
+    for inner, parts in ((448, 0), (504, 2)):
+        cfg = B.hpd_ffn_config(width, inner, B.HPD_BF16, B.HPD_ACT_SILU)
+        assert B.hpd_gated_ffn_workspace(cfg, rows)[0] == rows * inner * 2 + parts * rows * width * 4
+    for inner, parts in ((224, 0), (248, 2)):
+        cfg = B.hpd_ffn_config(width, inner, B.HPD_BF16, B.HPD_ACT_SILU)
+        assert B.hpd_gated_ffn_workspace(cfg, rows)[1] == 3 * rows * inner * 2 + parts * rows * width * 4
+    # rows' sums of 100 tiles and the target's logit, or two parts of the logits up to 128 MB
+    assert B.hpd_head_logprobs_workspace(B.HPD_F32, rows, 224, 6400)[0] == rows * (100 * 16 + 4)
+    assert B.hpd_head_logprobs_workspace(B.HPD_F32, rows, 248, 6400)[0] == 128 << 20
